@@ -15,7 +15,8 @@
  * Further entry points cover the rest of the method around that step: the
  * post-FFN and pre-MLP RMSNorm VJPs and per-layer signals (fpo_rmsnorm_vjp,
  * fpo_layer_signals, fpo_layer_update_grouped_signals), optimizers with the relative clip
- * (fpo_layer_optimize_grouped), the gate/up signals through the cached
+ * (fpo_layer_optimize_grouped), LayerNorm and its VJP (fpo_layernorm,
+ * fpo_layernorm_vjp), the gate/up signals through the cached
  * W3_init (fpo_gate_up_signals) and the App. C update-magnitude ratio
  * (fpo_norm_ratio).  fpo_h2d_copy stages a step's inputs from host memory.
  *
@@ -310,6 +311,51 @@ int32_t fpo_layer_signals(int32_t n_layers, int64_t T, int64_t d, int32_t dtype,
  */
 int32_t fpo_rmsnorm_vjp(int64_t T, int64_t d, int32_t dtype, const void* g, const void* x,
                         const void* gamma, float eps, float min_rms, void* g_out, void* stream);
+
+/*
+ * fpo_layernorm -- LayerNorm over the rows of x, for model families whose blocks
+ * normalise with the mean removed (the paper's families all use RMSNorm; the error
+ * signal composes with either through the VJPs):
+ *
+ *   mu = mean_j x_j,  sigma = sqrt(mean_j (x_j - mu)^2 + eps)
+ *   y  = gamma (.) (x - mu) / sigma + beta
+ *
+ * x, y [T, d] and gamma, beta [d] in dtype; gamma NULL: ones, beta NULL: zeros.
+ * mean_out, rstd_out [T] fp32 mu and 1 / sigma, each may be NULL.  y may not overlap x
+ * (FPO_ERR_ARG for y == x).
+ * Statistics and sums in fp32, the variance around the row's own mean; one rounding
+ * to dtype.  bf16 needs d % 8 == 0, fp32 takes any d; d <= 2^29.  Pointers 16-byte
+ * aligned.  No workspace; asynchronous on `stream`; T = 0 enqueues nothing.
+ */
+int32_t fpo_layernorm(int64_t T, int64_t d, int32_t dtype, const void* x, const void* gamma,
+                      const void* beta, float eps, void* y, float* mean_out, float* rstd_out,
+                      void* stream);
+
+/* Bytes of workspace fpo_layernorm_vjp needs for dgamma / dbeta (0 on invalid sizes). */
+size_t fpo_layernorm_vjp_workspace(int64_t T, int64_t d, int32_t dtype);
+
+/*
+ * fpo_layernorm_vjp -- the closed-form LayerNorm Jacobian applied to an upstream
+ * gradient, with the min-RMS clamp of App. E on its 1 / sigma prefactor as
+ * fpo_rmsnorm_vjp has it on 1 / rho, and the gradients of the weight and the bias:
+ *
+ *   xhat   = (x - mu) / sigma,  u = gamma (.) g
+ *   g_out  = (u - mean(u) - xhat mean(u (.) xhat)) / max(sigma, min_rms)
+ *   dgamma = sum_t g_t (.) xhat_t,   dbeta = sum_t g_t
+ *
+ * min_rms = 0 gives the exact gradient of fpo_layernorm.  mu and sigma are formed from
+ * x again (the row is read in any case): no statistics need saving.
+ *
+ * g, x, g_out [T, d] and gamma [d] in dtype; gamma NULL: ones.  dgamma, dbeta [d] fp32.
+ * Each output may be NULL (not all three).  g_out may not overlap g or x (FPO_ERR_ARG
+ * where it is either).  The weight sums are added in a fixed order that depends on T and d only
+ * (repeat calls give identical bits).  workspace: fpo_layernorm_vjp_workspace() bytes, 256-byte aligned,
+ * not read or needed when dgamma and dbeta are both NULL; it holds no status word.
+ * T = 0 sets dgamma and dbeta to zero.  Types, sizes and alignment as fpo_layernorm.
+ */
+int32_t fpo_layernorm_vjp(int64_t T, int64_t d, int32_t dtype, const void* g, const void* x,
+                          const void* gamma, float eps, float min_rms, void* g_out, float* dgamma,
+                          float* dbeta, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Optimizers of Sec. 3.1 on the fp32 master copies. */
 typedef enum fpo_optimizer_kind {

@@ -78,6 +78,14 @@ _lib.fpo_layer_signals.argtypes = [_i32, _i64, _i64, _i32, _vp, _vp, _vp, _vp, _
                                    _vp, _vp]
 _lib.fpo_layer_signals.restype = _i32
 
+_lib.fpo_layernorm.argtypes = [_i64, _i64, _i32, _vp, _vp, _vp, _f32, _vp, _vp, _vp, _vp]
+_lib.fpo_layernorm.restype = _i32
+_lib.fpo_layernorm_vjp_workspace.argtypes = [_i64, _i64, _i32]
+_lib.fpo_layernorm_vjp_workspace.restype = _sz
+_lib.fpo_layernorm_vjp.argtypes = [_i64, _i64, _i32, _vp, _vp, _vp, _f32, _f32, _vp, _vp, _vp, _vp,
+                                   _sz, _vp]
+_lib.fpo_layernorm_vjp.restype = _i32
+
 
 class OptimizerDesc(ctypes.Structure):
     """Mirror of fpo_optimizer_desc."""
@@ -397,6 +405,54 @@ def rmsnorm_vjp(g, x, gamma, g_out, *, eps=1e-6, min_rms=0.5, stream=None):
     rc = _lib.fpo_rmsnorm_vjp(T, d, _dtype_code(x), _ptr(g), _ptr(x), _ptr(gamma), float(eps),
                               float(min_rms), _ptr(g_out), _stream(stream))
     _check(rc, "fpo_rmsnorm_vjp")
+    return g_out
+
+
+# --------------------------------------------------------------------------- LayerNorm
+def _expect(t, shape, dtype, name):
+    """The C entry points see pointers only: a tensor's shape and type are checked here."""
+    if t is not None and (t.shape != shape or t.dtype != dtype):
+        raise ValueError(f"{name}: expected {dtype} of shape {tuple(shape)}, "
+                         f"got {t.dtype} of {tuple(t.shape)}")
+
+
+def layernorm(x, gamma, beta, y, *, eps=1e-5, mean_out=None, rstd_out=None, stream=None):
+    """fpo_layernorm: y = gamma (x - mean) / sqrt(var + eps) + beta over the rows of x [T, d];
+    gamma and beta may be None, mean_out and rstd_out are fp32 [T] or None."""
+    T, d = x.shape
+    _expect(y, x.shape, x.dtype, "y")
+    _expect(gamma, (d,), x.dtype, "gamma")
+    _expect(beta, (d,), x.dtype, "beta")
+    _expect(mean_out, (T,), torch.float32, "mean_out")
+    _expect(rstd_out, (T,), torch.float32, "rstd_out")
+    rc = _lib.fpo_layernorm(T, d, _dtype_code(x), _ptr(x), _ptr(gamma), _ptr(beta), float(eps),
+                            _ptr(y), _ptr(mean_out), _ptr(rstd_out), _stream(stream))
+    _check(rc, "fpo_layernorm")
+    return y
+
+
+def layernorm_vjp_workspace(T, d, dtype=BF16) -> int:
+    return int(_lib.fpo_layernorm_vjp_workspace(int(T), int(d), int(dtype)))
+
+
+def layernorm_vjp(g, x, gamma, g_out, *, eps=1e-5, min_rms=0.5, dgamma=None, dbeta=None,
+                  workspace=None, stream=None):
+    """fpo_layernorm_vjp: the LayerNorm Jacobian (with the min-RMS clamp; 0 for the exact
+    gradient) applied to g at x into g_out, and the fp32 weight and bias gradients into dgamma
+    and dbeta where given.  gamma and g_out may be None."""
+    T, d = x.shape
+    _expect(g, x.shape, x.dtype, "g")
+    _expect(gamma, (d,), x.dtype, "gamma")
+    _expect(g_out, x.shape, x.dtype, "g_out")
+    _expect(dgamma, (d,), torch.float32, "dgamma")
+    _expect(dbeta, (d,), torch.float32, "dbeta")
+    if workspace is None and (dgamma is not None or dbeta is not None):
+        workspace = _workspace(layernorm_vjp_workspace(T, d, _dtype_code(x)), x.device)
+    rc = _lib.fpo_layernorm_vjp(T, d, _dtype_code(x), _ptr(g), _ptr(x), _ptr(gamma), float(eps),
+                                float(min_rms), _ptr(g_out), _ptr(dgamma), _ptr(dbeta),
+                                _ptr(workspace), 0 if workspace is None else _nbytes(workspace),
+                                _stream(stream))
+    _check(rc, "fpo_layernorm_vjp")
     return g_out
 
 

@@ -720,6 +720,73 @@ int32_t fpo_layer_signals(int32_t n_layers, int64_t T, int64_t d, int32_t dtype,
                                             static_cast<cudaStream_t>(stream)));
 }
 
+namespace {
+// d of a LayerNorm row: its offsets, twice over, stay within 32 bits
+constexpr int64_t kLnMaxD = 1 << 29;
+
+int32_t ln_check(int64_t T, int64_t d, int32_t dtype) {
+    if (dtype != FPO_F32 && dtype != FPO_BF16) return FPO_ERR_DTYPE;
+    if (T < 0 || d <= 0 || T > INT_MAX || d > kLnMaxD) return FPO_ERR_SHAPE;
+    if (dtype == FPO_BF16 && d % 8 != 0) return FPO_ERR_SHAPE;
+    return FPO_OK;
+}
+}  // namespace
+
+int32_t fpo_layernorm(int64_t T, int64_t d, int32_t dtype, const void* x, const void* gamma,
+                      const void* beta, float eps, void* y, float* mean_out, float* rstd_out,
+                      void* stream) {
+    int32_t rc = ln_check(T, d, dtype);
+    if (rc != FPO_OK) return rc;
+    if (!(eps >= 0.f)) return FPO_ERR_ARG;
+    if (T > 0 && (!x || !y)) return FPO_ERR_NULL;
+    if (!aligned16(x) || !aligned16(gamma) || !aligned16(beta) || !aligned16(y) ||
+        !aligned16(mean_out) || !aligned16(rstd_out))
+        return FPO_ERR_ALIGN;
+    if (y && y == x) return FPO_ERR_ARG;
+    rc = check_arch();
+    if (rc != FPO_OK) return rc;
+    return cuda_status(launch_layernorm_fwd(dtype, x, gamma, beta, static_cast<int>(T),
+                                            static_cast<int>(d), eps, y, mean_out, rstd_out,
+                                            static_cast<cudaStream_t>(stream)));
+}
+
+size_t fpo_layernorm_vjp_workspace(int64_t T, int64_t d, int32_t dtype) {
+    if (ln_check(T, d, dtype) != FPO_OK) return 0;
+    return align_up(layernorm_vjp_floats(dtype, static_cast<int>(T), static_cast<int>(d)) *
+                        sizeof(float) +
+                    1);
+}
+
+int32_t fpo_layernorm_vjp(int64_t T, int64_t d, int32_t dtype, const void* g, const void* x,
+                          const void* gamma, float eps, float min_rms, void* g_out, float* dgamma,
+                          float* dbeta, void* workspace, size_t workspace_bytes, void* stream) {
+    int32_t rc = ln_check(T, d, dtype);
+    if (rc != FPO_OK) return rc;
+    if (!(eps >= 0.f) || !(min_rms >= 0.f)) return FPO_ERR_ARG;
+    if (T > 0 && (!g || !x)) return FPO_ERR_NULL;
+    if (!g_out && !dgamma && !dbeta) return FPO_ERR_NULL;
+    if (!aligned16(g) || !aligned16(x) || !aligned16(gamma) || !aligned16(g_out) ||
+        !aligned16(dgamma) || !aligned16(dbeta))
+        return FPO_ERR_ALIGN;
+    if (g_out && (g_out == g || g_out == x)) return FPO_ERR_ARG;
+    if (dgamma || dbeta) {
+        if (!workspace || workspace_bytes < fpo_layernorm_vjp_workspace(T, d, dtype))
+            return FPO_ERR_WORKSPACE;
+        if ((reinterpret_cast<uintptr_t>(workspace) % kAlign) != 0) return FPO_ERR_ALIGN;
+    }
+    rc = check_arch();
+    if (rc != FPO_OK) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (T == 0) {  // empty sums
+        if (dgamma) FPO_TRY(cudaMemsetAsync(dgamma, 0, static_cast<size_t>(d) * sizeof(float), st));
+        if (dbeta) FPO_TRY(cudaMemsetAsync(dbeta, 0, static_cast<size_t>(d) * sizeof(float), st));
+        return FPO_OK;
+    }
+    return cuda_status(launch_layernorm_vjp(dtype, g, x, gamma, static_cast<int>(T),
+                                            static_cast<int>(d), eps, min_rms, g_out, dgamma, dbeta,
+                                            static_cast<float*>(workspace), st));
+}
+
 int32_t fpo_layer_update(int64_t T, int64_t d, int64_t d_ff, int32_t dtype, const void* g,
                          const void* A, float lr, float* W_master, void* W_out, void* G_out,
                          void* workspace, size_t workspace_bytes, void* stream) {

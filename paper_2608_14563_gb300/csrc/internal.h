@@ -272,6 +272,17 @@ cudaError_t launch_layer_signals(int dtype, int n_layers, const void* g, const v
                                  const void* const* gamma_pre, void* const* out, int T, int d,
                                  float eps, float min_rms, cudaStream_t st);
 
+// LayerNorm forward (mean_out, rstd_out: [T] or null) and backward.  dtype 0 = fp32, 1 = bf16;
+// gamma, beta null: 1, 0.  Backward: out, dgamma, dbeta may be null; the weight sums need
+// layernorm_vjp_floats() floats of ws.  T > 0.
+cudaError_t launch_layernorm_fwd(int dtype, const void* x, const void* gamma, const void* beta,
+                                 int T, int d, float eps, void* y, float* mean_out,
+                                 float* rstd_out, cudaStream_t st);
+size_t layernorm_vjp_floats(int dtype, int T, int d);
+cudaError_t launch_layernorm_vjp(int dtype, const void* g, const void* x, const void* gamma, int T,
+                                 int d, float eps, float min_rms, void* out, float* dgamma,
+                                 float* dbeta, float* ws, cudaStream_t st);
+
 // One block waiting on an mbarrier nothing arrives on, bounded by limit_ns.
 cudaError_t launch_wait_timeout(unsigned* status, uint64_t limit_ns, cudaStream_t st);
 
