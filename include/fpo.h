@@ -15,7 +15,7 @@
  * Further entry points cover the rest of the method around that step: the
  * post-FFN and pre-MLP RMSNorm VJPs and per-layer signals (fpo_rmsnorm_vjp,
  * fpo_layer_signals, fpo_layer_update_grouped_signals), optimizers with the relative clip
- * (fpo_layer_optimize_grouped), LayerNorm and its VJP (fpo_layernorm,
+ * (fpo_layer_optimize_grouped, fpo_layer_muon_grouped; fpo_orthogonalize_grouped), LayerNorm and its VJP (fpo_layernorm,
  * fpo_layernorm_vjp), the gate/up signals through the cached
  * W3_init (fpo_gate_up_signals) and the App. C update-magnitude ratio
  * (fpo_norm_ratio).  fpo_h2d_copy stages a step's inputs from host memory.
@@ -39,7 +39,8 @@
  *   MMA with fp32 accumulation and fp32 elementwise math.  d, V and d_ff must be
  *   multiples of 8 (16-byte rows for the TMA engine).
  *   dtype FPO_F32: every floating-point tensor is fp32 and all arithmetic is
- *   fp32 FFMA (no TF32); any positive shape is accepted.
+ *   fp32 FFMA (no TF32), but for the Newton-Schulz products (fpo_orthogonalize_grouped
+ *   says how); any positive shape is accepted.
  * - The library only runs on compute capability 10.3 (GB300); any other
  *   device returns FPO_ERR_ARCH.
  * - Every call runs on the calling thread's current device.  One process may
@@ -408,6 +409,89 @@ int32_t fpo_layer_optimize_grouped(int32_t n_layers, int64_t T, int64_t d, int64
                                    void* const* W_out, float* const* state1,
                                    float* const* state2, void* workspace, size_t workspace_bytes,
                                    void* stream);
+
+/* Largest side of a matrix that fpo_orthogonalize_grouped and fpo_layer_muon_grouped take. */
+#define FPO_MAX_NS_SIDE 65536
+
+/* Bytes of workspace fpo_orthogonalize_grouped needs (0 on invalid sizes): per matrix of
+ * rows x cols with smaller side m about 6 rows cols + 4 m^2 bytes (bf16) or 12 rows cols +
+ * 8 m^2 (fp32). */
+size_t fpo_orthogonalize_workspace(int32_t n_layers, int64_t rows, int64_t cols, int32_t dtype);
+
+/*
+ * fpo_orthogonalize_grouped -- Newton-Schulz orthogonalisation of n_layers matrices of one
+ * shape (1 <= n_layers <= FPO_MAX_GROUPED_LAYERS), e.g. the pseudogradients that
+ * fpo_layer_update_grouped leaves in G_out: with G = U S V^T,
+ *   X_0     = G / max(||G||_F, eps)
+ *   X_{k+1} = a_k X_k + (b_k A + c_k A^2) X_k,   A = X_k X_k^T        k = 0 .. steps - 1
+ *   O       = X_steps = U p(S / max(||G||_F, eps)) V^T
+ * p the composition of a_k s + b_k s^3 + c_k s^5 (for rows > cols the products are taken on
+ * the other side, with A = X_k^T X_k).  It draws the singular values toward 1 without an SVD.
+ *
+ * G, O    HOST arrays of n_layers device pointers, [rows, cols] in dtype.  Every G is read
+ *         before any O is written: O[l] may be G[l] (no partial overlap).  O entries may not
+ *         repeat (FPO_ERR_ARG).
+ * steps   1 to 32
+ * coeffs  HOST array of 3 steps floats (a, b, c of every step), or NULL for the quintic
+ *         3.4445, -4.7750, 2.0315 in every step.  The polynomials have to keep the singular
+ *         values' bound (1 at the start) within 2^-16 .. 2^16, and the coefficients within
+ *         2^16 (FPO_ERR_ARG).
+ * eps     1e-30 to 1e30 (1e-7): a zero matrix gives O = 0
+ * workspace  fpo_orthogonalize_workspace() bytes, 256-byte aligned (device status word first)
+ *
+ * bf16: products of fp16 operands scaled by powers of two from the bounds (11 bits instead of
+ * bf16's 8), fp32 accumulation, the linear term a X from 22 bits of X, whatever its rank;
+ * rows and cols multiples of 8.  fp32: operands as sums of two fp16 numbers (22 bits), three
+ * products, fp32 sums rounded to nearest every 64 products, the linear term in fp32; any
+ * sizes.  Sides up to FPO_MAX_NS_SIDE.  A matrix with a NaN or an infinity gives NaN
+ * throughout, and no other matrix changes.  Deterministic, and independent of what else is in
+ * the group.
+ */
+int32_t fpo_orthogonalize_grouped(int32_t n_layers, int64_t rows, int64_t cols, int32_t dtype,
+                                  const void* const* G, int32_t steps, const float* coeffs, float eps,
+                                  void* const* O, void* workspace, size_t workspace_bytes,
+                                  void* stream);
+
+typedef struct fpo_muon_desc {
+    float lr;             /* learning rate                                              */
+    float momentum;       /* mu in [0, 1) (0.95)                                        */
+    float weight_decay;   /* decoupled weight decay (0)                                 */
+    float scale;          /* factor of O in the step, e.g. sqrt(max(1, d / d_ff)), or
+                             0.2 sqrt(max(d, d_ff)) for the RMS of an AdamW step        */
+    float eps;            /* floor of the update's norm (1e-7)                          */
+    int32_t nesterov;     /* 1: U = G + mu M, 0: U = M                                  */
+    int32_t steps;        /* Newton-Schulz steps (5)                                    */
+    const float* coeffs;  /* HOST array of 3 steps floats, or NULL for the quintic      */
+} fpo_muon_desc;
+
+/* Bytes of workspace fpo_layer_muon_grouped needs (0 on invalid sizes): that of
+ * fpo_orthogonalize_grouped and 4 d d_ff bytes per layer. */
+size_t fpo_layer_muon_workspace(int32_t n_layers, int64_t d, int64_t d_ff, int32_t dtype);
+
+/*
+ * fpo_layer_muon_grouped -- the pseudogradient of every target layer (Eq. (w3update), as in
+ * fpo_layer_update_grouped_signals) followed by a Muon step on its fp32 master, a third
+ * optimizer beside those of fpo_layer_optimize_grouped:
+ *   G_l = g[l]^T A[l]                                   fp32, in the workspace
+ *   momentum_l <- mu momentum_l + G_l
+ *   U_l = G_l + mu momentum_l (nesterov) or momentum_l
+ *   O_l = orthogonalised U_l (fpo_orthogonalize_grouped)
+ *   W_master,l <- (1 - lr weight_decay) W_master,l - lr scale O_l;  W_out,l = W_master,l
+ *                                                       rounded to dtype
+ * in the last product's epilogue.  For the gate and up matrices g is dA or dB of
+ * fpo_gate_up_signals and A the MLP input, so d is there the taller side.
+ *
+ * g [T, d], A [T, d_ff] in dtype (not read for T = 0: G_l = 0), W_master and momentum
+ * [d, d_ff] fp32, updated in place, W_out [d, d_ff] in dtype (the array or an entry may be
+ * NULL); all HOST arrays of n_layers device pointers.  g and A entries may repeat, the others
+ * not (FPO_ERR_ARG).  No relative clip: the step's norm is lr scale ||O_l||_F, about lr scale sqrt(rank).
+ * workspace: fpo_layer_muon_workspace() bytes, 256-byte aligned (device status word first).
+ * Sizes and precision as fpo_orthogonalize_grouped.
+ */
+int32_t fpo_layer_muon_grouped(int32_t n_layers, int64_t T, int64_t d, int64_t d_ff, int32_t dtype,
+                               const void* const* g, const void* const* A, const fpo_muon_desc* opt,
+                               float* const* W_master, void* const* W_out, float* const* momentum,
+                               void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * fpo_gate_up_signals -- the hidden-space signals for the gate (W1) and up (W2)

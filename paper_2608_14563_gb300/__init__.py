@@ -103,6 +103,28 @@ _lib.fpo_layer_optimize_grouped.argtypes = [_i32, _i64, _i64, _i64, _i32, ctypes
                                             ctypes.POINTER(_vp), ctypes.POINTER(_vp),
                                             ctypes.POINTER(_vp), ctypes.POINTER(_vp), _vp, _sz, _vp]
 _lib.fpo_layer_optimize_grouped.restype = _i32
+
+
+class MuonDesc(ctypes.Structure):
+    """Mirror of fpo_muon_desc."""
+    _fields_ = [("lr", _f32), ("momentum", _f32), ("weight_decay", _f32), ("scale", _f32),
+                ("eps", _f32), ("nesterov", _i32), ("steps", _i32),
+                ("coeffs", ctypes.POINTER(_f32))]
+
+
+_lib.fpo_orthogonalize_workspace.argtypes = [_i32, _i64, _i64, _i32]
+_lib.fpo_orthogonalize_workspace.restype = _sz
+_lib.fpo_orthogonalize_grouped.argtypes = [_i32, _i64, _i64, _i32, ctypes.POINTER(_vp), _i32,
+                                           ctypes.POINTER(_f32), _f32, ctypes.POINTER(_vp), _vp,
+                                           _sz, _vp]
+_lib.fpo_orthogonalize_grouped.restype = _i32
+_lib.fpo_layer_muon_workspace.argtypes = [_i32, _i64, _i64, _i32]
+_lib.fpo_layer_muon_workspace.restype = _sz
+_lib.fpo_layer_muon_grouped.argtypes = [_i32, _i64, _i64, _i64, _i32, ctypes.POINTER(_vp),
+                                        ctypes.POINTER(_vp), ctypes.POINTER(MuonDesc),
+                                        ctypes.POINTER(_vp), ctypes.POINTER(_vp),
+                                        ctypes.POINTER(_vp), _vp, _sz, _vp]
+_lib.fpo_layer_muon_grouped.restype = _i32
 _lib.fpo_gate_up_signals.argtypes = [_i64, _i64, _i64, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
                                      _sz, _vp]
 _lib.fpo_gate_up_signals.restype = _i32
@@ -223,6 +245,13 @@ def _nbytes(t: torch.Tensor) -> int:
 
 def _workspace(nbytes: int, device) -> torch.Tensor:
     return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
+
+
+def _expect(t, shape, dtype, name):
+    """The C entry points see pointers only: a tensor's shape and type are checked here."""
+    if t is not None and (t.shape != shape or t.dtype != dtype):
+        raise ValueError(f"{name}: expected {dtype} of shape {tuple(shape)}, "
+                         f"got {t.dtype} of {tuple(t.shape)}")
 
 
 # --------------------------------------------------------------------------- error signal
@@ -365,6 +394,86 @@ def layer_optimize_grouped(gs, As, opt, W_masters, *, W_outs=None, states1=None,
     return workspace
 
 
+def _coeffs(coeffs, steps):
+    """None, or steps triples (a, b, c) as a C array; the caller keeps it alive."""
+    if coeffs is None:
+        return None
+    flat = [float(v) for row in coeffs for v in row]
+    if len(coeffs) != steps or len(flat) != 3 * steps:
+        raise ValueError("coeffs needs one (a, b, c) per step")
+    return (_f32 * len(flat))(*flat)
+
+
+def _expect_all(ts, n, shape, dtype, name):
+    if ts is None:
+        return
+    if len(ts) != n:
+        raise ValueError(f"{name}: one entry per layer expected")
+    for t in ts:
+        _expect(t, shape, dtype, name)
+
+
+def orthogonalize_workspace(n_layers, rows, cols, dtype=BF16) -> int:
+    return int(_lib.fpo_orthogonalize_workspace(int(n_layers), int(rows), int(cols), int(dtype)))
+
+
+def orthogonalize_grouped(Gs, Os, *, steps=5, coeffs=None, eps=1e-7, workspace=None, stream=None):
+    """fpo_orthogonalize_grouped: Os[l] = Newton-Schulz orthogonalisation of Gs[l] (one shape
+    and dtype; Os[l] may be Gs[l]).  coeffs: None, or ``steps`` triples (a, b, c).  Returns the
+    workspace tensor (its first word holds the device status)."""
+    n, G = len(Gs), Gs[0]
+    rows, cols = G.shape
+    _expect_all(Gs, n, G.shape, G.dtype, "Gs")
+    _expect_all(Os, n, G.shape, G.dtype, "Os")
+    dt = _dtype_code(G)
+    if workspace is None:
+        workspace = _workspace(orthogonalize_workspace(n, rows, cols, dt), G.device)
+    co = _coeffs(coeffs, steps)
+    rc = _lib.fpo_orthogonalize_grouped(n, rows, cols, dt, _ptr_array(Gs, n), int(steps), co,
+                                        float(eps), _ptr_array(Os, n), _ptr(workspace),
+                                        _nbytes(workspace), _stream(stream))
+    _check(rc, "fpo_orthogonalize_grouped")
+    return workspace
+
+
+def muon_desc(*, lr=1e-4, momentum=0.95, weight_decay=0.0, scale=1.0, nesterov=True, steps=5,
+              coeffs=None, eps=1e-7):
+    """fpo_muon_desc; coeffs as in orthogonalize_grouped."""
+    co = _coeffs(coeffs, steps)
+    d = MuonDesc(float(lr), float(momentum), float(weight_decay), float(scale), float(eps),
+                 1 if nesterov else 0, int(steps),
+                 None if co is None else ctypes.cast(co, ctypes.POINTER(_f32)))
+    d._keep = co
+    return d
+
+
+def layer_muon_workspace(n_layers, d, d_ff, dtype=BF16) -> int:
+    return int(_lib.fpo_layer_muon_workspace(int(n_layers), int(d), int(d_ff), int(dtype)))
+
+
+def layer_muon_grouped(gs, As, opt, W_masters, momenta, *, W_outs=None, workspace=None,
+                       stream=None):
+    """fpo_layer_muon_grouped: G_l = gs[l]^T As[l], momentum, orthogonalisation, weight step."""
+    n = len(As)
+    T, d = gs[0].shape
+    d_ff = As[0].shape[1]
+    dtype = gs[0].dtype
+    _expect_all(gs, n, (T, d), dtype, "gs")
+    _expect_all(As, n, (T, d_ff), dtype, "As")
+    _expect_all(W_masters, n, (d, d_ff), torch.float32, "W_masters")
+    _expect_all(momenta, n, (d, d_ff), torch.float32, "momenta")
+    _expect_all(W_outs, n, (d, d_ff), dtype, "W_outs")
+    dt = _dtype_code(gs[0])
+    if workspace is None:
+        workspace = _workspace(layer_muon_workspace(n, d, d_ff, dt), gs[0].device)
+    rc = _lib.fpo_layer_muon_grouped(n, T, d, d_ff, dt, _ptr_array(gs, n), _ptr_array(As, n),
+                                     ctypes.byref(opt), _ptr_array(W_masters, n),
+                                     _ptr_array(W_outs, n), _ptr_array(momenta, n),
+                                     _ptr(workspace), _nbytes(workspace), _stream(stream))
+    _check(rc, "fpo_layer_muon_grouped")
+    return workspace
+
+
 def gate_up_signals(g, W3_init, a, b, dA, dB, *, workspace=None, stream=None):
     """fpo_gate_up_signals: SwiGLU W1/W2 signals through the cached W3_init feedback."""
     T, d = g.shape
@@ -409,13 +518,6 @@ def rmsnorm_vjp(g, x, gamma, g_out, *, eps=1e-6, min_rms=0.5, stream=None):
 
 
 # --------------------------------------------------------------------------- LayerNorm
-def _expect(t, shape, dtype, name):
-    """The C entry points see pointers only: a tensor's shape and type are checked here."""
-    if t is not None and (t.shape != shape or t.dtype != dtype):
-        raise ValueError(f"{name}: expected {dtype} of shape {tuple(shape)}, "
-                         f"got {t.dtype} of {tuple(t.shape)}")
-
-
 def layernorm(x, gamma, beta, y, *, eps=1e-5, mean_out=None, rstd_out=None, stream=None):
     """fpo_layernorm: y = gamma (x - mean) / sqrt(var + eps) + beta over the rows of x [T, d];
     gamma and beta may be None, mean_out and rstd_out are fp32 [T] or None."""

@@ -639,6 +639,138 @@ int32_t fpo_layer_optimize_grouped(int32_t n_layers, int64_t T, int64_t d, int64
                                         partials, scales, norms_done, st));
 }
 
+namespace {
+
+// The usual quintic: p(1) = 0.70, p'(0) = 3.44, and every singular value of 0.01 and more
+// within [0.68, 1.20] after five steps.
+constexpr float kNsQuintic[3] = {3.4445f, -4.7750f, 2.0315f};
+constexpr int kNsMaxSteps = 32;
+
+// Whether two of n pointers are the same (a buffer written for two layers); nulls aside.
+bool repeats(int32_t n, const void* const* p) {
+    if (!p) return false;
+    for (int i = 1; i < n; ++i)
+        for (int j = 0; j < i; ++j)
+            if (p[i] && p[i] == p[j]) return true;
+    return false;
+}
+
+// The coefficients of every step (the quintic where none are given), or an error.
+int32_t ns_coeffs(int32_t steps, const float* coeffs, float eps, float (&out)[3 * kNsMaxSteps]) {
+    if (steps < 1 || steps > kNsMaxSteps) return FPO_ERR_ARG;
+    if (!(eps >= 1e-30f) || !(eps <= 1e30f)) return FPO_ERR_ARG;
+    for (int i = 0; i < 3 * steps; ++i) out[i] = coeffs ? coeffs[i] : kNsQuintic[i % 3];
+    return ns_coeffs_ok(steps, out) ? FPO_OK : FPO_ERR_ARG;
+}
+
+int32_t ns_check_shape(int32_t n_layers, int64_t rows, int64_t cols, int32_t dtype) {
+    if (dtype != FPO_F32 && dtype != FPO_BF16) return FPO_ERR_DTYPE;
+    if (n_layers < 1 || n_layers > FPO_MAX_GROUPED_LAYERS) return FPO_ERR_SHAPE;
+    if (rows <= 0 || cols <= 0 || rows > FPO_MAX_NS_SIDE || cols > FPO_MAX_NS_SIDE)
+        return FPO_ERR_SHAPE;
+    if (dtype == FPO_BF16 && (rows % 8 != 0 || cols % 8 != 0)) return FPO_ERR_SHAPE;
+    return FPO_OK;
+}
+
+}  // namespace
+
+size_t fpo_orthogonalize_workspace(int32_t n_layers, int64_t rows, int64_t cols, int32_t dtype) {
+    if (ns_check_shape(n_layers, rows, cols, dtype) != FPO_OK) return 0;
+    return ns_workspace_bytes(n_layers, static_cast<int>(rows), static_cast<int>(cols), dtype, false);
+}
+
+int32_t fpo_orthogonalize_grouped(int32_t n_layers, int64_t rows, int64_t cols, int32_t dtype,
+                                  const void* const* G, int32_t steps, const float* coeffs, float eps,
+                                  void* const* O, void* workspace, size_t workspace_bytes,
+                                  void* stream) {
+    int32_t rc = ns_check_shape(n_layers, rows, cols, dtype);
+    if (rc != FPO_OK) return rc;
+    float co[3 * kNsMaxSteps];
+    rc = ns_coeffs(steps, coeffs, eps, co);
+    if (rc != FPO_OK) return rc;
+    if (!G || !O) return FPO_ERR_NULL;
+    for (int l = 0; l < n_layers; ++l) {
+        if (!G[l] || !O[l]) return FPO_ERR_NULL;
+        if (!aligned16(G[l]) || !aligned16(O[l])) return FPO_ERR_ALIGN;
+    }
+    if (repeats(n_layers, O)) return FPO_ERR_ARG;
+    if (!workspace || workspace_bytes < fpo_orthogonalize_workspace(n_layers, rows, cols, dtype))
+        return FPO_ERR_WORKSPACE;
+    if ((reinterpret_cast<uintptr_t>(workspace) % kAlign) != 0) return FPO_ERR_ALIGN;
+    rc = check_arch();
+    if (rc != FPO_OK) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    unsigned* status = static_cast<unsigned*>(workspace);
+    FPO_TRY(cudaMemsetAsync(status, 0, sizeof(unsigned), st));
+    const NsTarget to{O, nullptr, 0.f, 0.f};
+    return cuda_status(launch_newton_schulz(n_layers, static_cast<int>(rows), static_cast<int>(cols),
+                                            dtype, G, nullptr, eps, steps, co, to, workspace, status,
+                                            st));
+}
+
+size_t fpo_layer_muon_workspace(int32_t n_layers, int64_t d, int64_t d_ff, int32_t dtype) {
+    if (ns_check_shape(n_layers, d, d_ff, dtype) != FPO_OK) return 0;
+    return ns_workspace_bytes(n_layers, static_cast<int>(d), static_cast<int>(d_ff), dtype, true);
+}
+
+int32_t fpo_layer_muon_grouped(int32_t n_layers, int64_t T, int64_t d, int64_t d_ff, int32_t dtype,
+                               const void* const* g, const void* const* A, const fpo_muon_desc* opt,
+                               float* const* W_master, void* const* W_out, float* const* momentum,
+                               void* workspace, size_t workspace_bytes, void* stream) {
+    if (!opt) return FPO_ERR_NULL;
+    int32_t rc = ns_check_shape(n_layers, d, d_ff, dtype);
+    if (rc != FPO_OK) return rc;
+    if (T < 0 || T > INT_MAX) return FPO_ERR_SHAPE;
+    float co[3 * kNsMaxSteps];
+    rc = ns_coeffs(opt->steps, opt->coeffs, opt->eps, co);
+    if (rc != FPO_OK) return rc;
+    if (!std::isfinite(opt->lr) || !std::isfinite(opt->scale) || !std::isfinite(opt->weight_decay) ||
+        !(opt->momentum >= 0.f && opt->momentum < 1.f) || (opt->nesterov != 0 && opt->nesterov != 1))
+        return FPO_ERR_ARG;
+    if (!W_master || !momentum || (T > 0 && (!g || !A))) return FPO_ERR_NULL;
+    for (int l = 0; l < n_layers; ++l) {
+        if ((T > 0 && (!A[l] || !g[l])) || !W_master[l] || !momentum[l]) return FPO_ERR_NULL;
+        if ((T > 0 && (!aligned16(g[l]) || !aligned16(A[l]))) || !aligned16(W_master[l]) ||
+            !aligned16(momentum[l]) || !aligned16(W_out ? W_out[l] : nullptr))
+            return FPO_ERR_ALIGN;
+    }
+    if (repeats(n_layers, reinterpret_cast<const void* const*>(W_master)) ||
+        repeats(n_layers, reinterpret_cast<const void* const*>(momentum)) ||
+        repeats(n_layers, W_out))
+        return FPO_ERR_ARG;
+    if (!workspace || workspace_bytes < fpo_layer_muon_workspace(n_layers, d, d_ff, dtype))
+        return FPO_ERR_WORKSPACE;
+    if ((reinterpret_cast<uintptr_t>(workspace) % kAlign) != 0) return FPO_ERR_ALIGN;
+    rc = check_arch();
+    if (rc != FPO_OK) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    unsigned* status = static_cast<unsigned*>(workspace);
+    FPO_TRY(cudaMemsetAsync(status, 0, sizeof(unsigned), st));
+    const int Ti = static_cast<int>(T), di = static_cast<int>(d), fi = static_cast<int>(d_ff);
+    // G_l = g_l^T A_l (fp32)
+    float* G[FPO_MAX_GROUPED_LAYERS];
+    for (int l = 0; l < n_layers; ++l)
+        G[l] = ns_update_buffer(workspace, n_layers, di, fi, dtype, l);
+    if (T == 0) {
+        FPO_TRY(cudaMemsetAsync(G[0], 0, static_cast<size_t>(G[n_layers - 1] - G[0]) * 4 +
+                                             static_cast<size_t>(d) * d_ff * 4, st));
+    } else if (dtype == FPO_BF16) {
+        FPO_TRY(launch_grad_bf16(n_layers, Ti, di, fi, g, A, G, nullptr,
+                                 reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) +
+                                                          kStatusBytes),
+                                 status, st));
+    } else {
+        FPO_TRY(launch_update_f32(n_layers, Ti, di, fi, reinterpret_cast<const float* const*>(g),
+                                  reinterpret_cast<const float* const*>(A), 0.f, nullptr, nullptr, G,
+                                  st));
+    }
+    // momentum, orthogonalisation, W <- (1 - lr wd) W - lr scale O
+    const NsMomentum mom{momentum, opt->momentum, opt->nesterov != 0};
+    const NsTarget to{W_out, W_master, 1.f - opt->lr * opt->weight_decay, opt->lr * opt->scale};
+    return cuda_status(launch_newton_schulz(n_layers, di, fi, dtype, nullptr, &mom, opt->eps,
+                                            opt->steps, co, to, workspace, status, st));
+}
+
 int32_t fpo_gate_up_signals(int64_t T, int64_t d, int64_t d_ff, int32_t dtype, const void* g,
                             const void* W3_init, const void* a, const void* b, void* dA, void* dB,
                             void* workspace, size_t workspace_bytes, void* stream) {

@@ -283,6 +283,32 @@ cudaError_t launch_layernorm_vjp(int dtype, const void* g, const void* x, const 
                                  int d, float eps, float min_rms, void* out, float* dgamma,
                                  float* dbeta, float* ws, cudaStream_t st);
 
+// ------------------------------------------------------------ Newton-Schulz (newton_schulz.cu)
+// Momentum in front of the iteration: M <- mu M + G, U = G + mu M (nesterov) or M, with G in
+// ns_update_buffer() (fp32, one per layer), which U replaces.
+struct NsMomentum {
+    float* const* M;
+    float mu;
+    bool nesterov;
+};
+// What becomes of the result: out[l] = O in dtype, or with W set W[l] <- keep W[l] - rate O and
+// out[l] (out or its entry may be null) = W[l] in dtype.
+struct NsTarget {
+    void* const* out;
+    float* const* W;
+    float keep, rate;
+};
+// Whether finite coefficients (3 per step) keep the iteration's bounds in range.
+bool ns_coeffs_ok(int steps, const float* coeffs);
+size_t ns_workspace_bytes(int n, int rows, int cols, int dtype, bool muon);
+float* ns_update_buffer(void* ws, int n, int rows, int cols, int dtype, int layer);
+// n matrices [rows, cols] (G in dtype, or mom) through `steps` iterations.  dtype 0 = fp32,
+// 1 = bf16 (cols a multiple of 8).
+cudaError_t launch_newton_schulz(int n, int rows, int cols, int dtype, const void* const* G,
+                                 const NsMomentum* mom, double eps, int steps, const float* coeffs,
+                                 const NsTarget& to, void* workspace, unsigned* status,
+                                 cudaStream_t st);
+
 // One block waiting on an mbarrier nothing arrives on, bounded by limit_ns.
 cudaError_t launch_wait_timeout(unsigned* status, uint64_t limit_ns, cudaStream_t st);
 

@@ -1,0 +1,586 @@
+// newton_schulz.cu -- orthogonalised updates: K steps of an odd quintic iteration on the
+// matrix of every layer, and the optimizer step that takes them (the orthogonalised momentum
+// of the Muon optimizer on the fp32 masters of Sec. 3.1).
+//
+//   X_0 = G / max(||G||_F, eps)                 singular values in [0, 1]
+//   X_{k+1} = a X_k + (b A + c A^2) X_k,  A = X_k X_k^T     p_k(s) = a s + b s^3 + c s^5
+//
+// (X (b A + c A^2) with A = X^T X when X is taller than wide: the products of the smaller
+// side).  Per step m^2 n + m^3 + 2 m^2 n operations for sides m <= n, the first two halved by
+// symmetry; bound by the tensor cores for all but small matrices.
+//
+// Number formats.  Operands are fp16 (11 bits; bf16's 8 leave 1e-2 of error in the result)
+// scaled by powers of two: the host bounds every X_k, A and B from the polynomials' maxima on
+// the interval that the singular values can reach, so nothing overflows, and fp16's small end
+// lies 2^-39 below the bound.  bf16 calls keep X's low part for the linear term (EpiApply);
+// measured against fp64 the result is then off by 0.7e-3 to 1.9e-3 in norm, whatever the
+// rank, less than the bf16 rounding of the output itself (1.7e-3).  fp32 calls take every
+// operand as the sum of two fp16 matrices (22 bits) and three products.
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <math.h>
+
+#include <atomic>
+#include <mutex>
+
+#include "internal.h"
+#include "ns_gemm.cuh"
+
+namespace fpo {
+namespace {
+
+constexpr int kPassThreads = 256;
+constexpr int kNormBlocks = 128;  // per layer, at most
+
+struct NsPtrs {
+    const void* in[kMaxGroups];  // G, or U (fp32)
+    float* M[kMaxGroups];        // momentum, or null
+};
+
+__device__ __forceinline__ double block_sum_d(double x) {
+    __shared__ double sh[kPassThreads / 32];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = x;
+    __syncthreads();
+    double t = 0.0;
+#pragma unroll
+    for (int k = 0; k < kPassThreads / 32; ++k) t += sh[k];
+    return t;
+}
+
+// Sum of the squares of 16 values: fp32 where that neither overflows nor loses digits to
+// underflow, else fp64 (GB300 adds two fp64 numbers per SM and clock).
+__device__ __forceinline__ double square_sum16(const float (&v)[16]) {
+    float s = 0.f;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) s = fmaf(v[k], v[k], s);
+    if (s >= 1e-30f && s <= 3e38f) return s;
+    double d = 0.0;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) d += static_cast<double>(v[k]) * v[k];
+    return d;
+}
+
+// 16 consecutive elements of an array of n, zeros behind its end.  16-byte aligned base.
+__device__ __forceinline__ void load16(const float* p, size_t i, size_t n, float (&v)[16]) {
+    if (i + 16 <= n) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float4 a = reinterpret_cast<const float4*>(p + i)[k];
+            v[4 * k] = a.x;
+            v[4 * k + 1] = a.y;
+            v[4 * k + 2] = a.z;
+            v[4 * k + 3] = a.w;
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 16; ++k) v[k] = i + k < n ? p[i + k] : 0.f;
+    }
+}
+__device__ __forceinline__ void load16(const __nv_bfloat16* p, size_t i, size_t n, float (&v)[16]) {
+    if (i + 16 <= n) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const uint4 a = reinterpret_cast<const uint4*>(p + i)[k];
+            const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                v[8 * k + 2 * j] = __uint_as_float(w[j] << 16);
+                v[8 * k + 2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 16; ++k) v[k] = i + k < n ? __bfloat162float(p[i + k]) : 0.f;
+    }
+}
+__device__ __forceinline__ void store16(float* p, size_t i, size_t n, const float (&v)[16]) {
+    if (i + 16 <= n) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            reinterpret_cast<float4*>(p + i)[k] =
+                make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 16; ++k)
+            if (i + k < n) p[i + k] = v[k];
+    }
+}
+
+// part[layer][block] = sum of squares over the block's share of the layer's n elements.
+template <typename TT>
+__global__ void __launch_bounds__(kPassThreads)
+    ns_norm_kernel(const __grid_constant__ NsPtrs p, size_t n, double* part) {
+    grid_dependency_trigger();
+    grid_dependency_wait();
+    const int layer = blockIdx.y;
+    const size_t step = static_cast<size_t>(gridDim.x) * kPassThreads * 16;
+    double acc = 0.0;
+    for (size_t i = (blockIdx.x * static_cast<size_t>(kPassThreads) + threadIdx.x) * 16; i < n;
+         i += step) {
+        float v[16];
+        load16(static_cast<const TT*>(p.in[layer]), i, n, v);
+        acc += square_sum16(v);
+    }
+    const double t = block_sum_d(acc);
+    if (threadIdx.x == 0) part[static_cast<size_t>(layer) * gridDim.x + blockIdx.x] = t;
+}
+
+// The momentum: M <- mu M + G and U = G + mu M (nesterov) or M, U over G; sums of the squares of
+// U as ns_norm_kernel leaves them.  (Launched plainly, behind the gradient's GEMM.)
+__global__ void __launch_bounds__(kPassThreads)
+    ns_momentum_kernel(const __grid_constant__ NsPtrs p, size_t n, float mu, bool nesterov,
+                       double* part) {
+    const int layer = blockIdx.y;
+    float* U = static_cast<float*>(const_cast<void*>(p.in[layer]));
+    float* M = p.M[layer];
+    const size_t step = static_cast<size_t>(gridDim.x) * kPassThreads * 16;
+    double acc = 0.0;
+    for (size_t i = (blockIdx.x * static_cast<size_t>(kPassThreads) + threadIdx.x) * 16; i < n;
+         i += step) {
+        float v[16], m[16];
+        load16(U, i, n, v);
+        load16(M, i, n, m);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            m[k] = fmaf(mu, m[k], v[k]);
+            v[k] = nesterov ? fmaf(mu, m[k], v[k]) : m[k];
+        }
+        store16(M, i, n, m);
+        store16(U, i, n, v);
+        acc += square_sum16(v);
+    }
+    const double t = block_sum_d(acc);
+    if (threadIdx.x == 0) part[static_cast<size_t>(layer) * gridDim.x + blockIdx.x] = t;
+}
+
+// X_0, scaled: fp16 high and low parts (kSplit: and the fp32 value), rows padded from cols to
+// ld with zeros.  Thread: 8 columns of a row.  The layer's norm from its `blocks` partial sums.
+// A layer with a non-finite norm (a NaN, an infinity) becomes NaN as a whole.
+template <typename TT, bool kSplit>
+__global__ void __launch_bounds__(kPassThreads)
+    ns_cast_kernel(const __grid_constant__ NsPtrs p, int rows, int cols, int ld, const double* part,
+                   int blocks, double eps, double scale, __half* hi, __half* lo, float* x32,
+                   size_t stride) {
+    grid_dependency_trigger();
+    grid_dependency_wait();
+    const int layer = blockIdx.y;
+    double s = threadIdx.x < blocks ? part[static_cast<size_t>(layer) * blocks + threadIdx.x] : 0.0;
+    s = sqrt(block_sum_d(s));
+    const float f = s <= 1.7e308 ? static_cast<float>(scale / fmax(s, eps)) : NAN;
+    const TT* src = static_cast<const TT*>(p.in[layer]);
+    const int per = ld / 8;
+    const bool vec = cols % 8 == 0;  // rows then start on 16 bytes
+    const size_t n = static_cast<size_t>(rows) * per;
+    for (size_t i = blockIdx.x * static_cast<size_t>(kPassThreads) + threadIdx.x; i < n;
+         i += static_cast<size_t>(gridDim.x) * kPassThreads) {
+        const size_t row = i / per;
+        const int col = static_cast<int>(i - row * per) * 8;
+        const TT* q = src + row * cols + col;
+        float v[8];
+        if (vec) {
+            if constexpr (sizeof(TT) == 2) {
+                const uint4 a = *reinterpret_cast<const uint4*>(q);
+                const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    v[2 * j] = __uint_as_float(w[j] << 16);
+                    v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+                }
+            } else {
+                const float4 a = reinterpret_cast<const float4*>(q)[0];
+                const float4 b = reinterpret_cast<const float4*>(q)[1];
+                v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+                v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = col + k < cols ? static_cast<float>(q[k]) : 0.f;
+        }
+        uint32_t h[4], l[4];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] *= f;
+        if (!vec) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = col + k < cols ? v[k] : 0.f;
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            h[k] = pack_f16x2(v[2 * k], v[2 * k + 1]);
+            const float2 g = unpack_f16x2(h[k]);
+            l[k] = pack_f16x2(v[2 * k] - g.x, v[2 * k + 1] - g.y);
+        }
+        const size_t o = layer * stride + row * ld + col;
+        *reinterpret_cast<uint4*>(hi + o) = make_uint4(h[0], h[1], h[2], h[3]);
+        *reinterpret_cast<uint4*>(lo + o) = make_uint4(l[0], l[1], l[2], l[3]);
+        if constexpr (kSplit) {
+            reinterpret_cast<float4*>(x32 + o)[0] = make_float4(v[0], v[1], v[2], v[3]);
+            reinterpret_cast<float4*>(x32 + o)[1] = make_float4(v[4], v[5], v[6], v[7]);
+        }
+    }
+}
+
+size_t round_up(size_t x, size_t m) { return (x + m - 1) / m * m; }
+
+int norm_blocks(size_t n) {
+    const size_t b = (n + kPassThreads * 16 - 1) / (kPassThreads * 16);
+    return static_cast<int>(b < kNormBlocks ? b : kNormBlocks);
+}
+
+// Byte offsets of the workspace behind the status word's 256 bytes.
+struct NsLayout {
+    int m, ld, ldm;              // the smaller side, row strides of X and of A, B
+    size_t xs, ms;               // elements of one layer's X, A
+    size_t part, U, u_stride, hi[2], lo[2], x32, A[2], B[2], total;
+};
+
+NsLayout ns_layout(int n, int rows, int cols, bool split, bool muon) {
+    NsLayout L = {};
+    L.m = rows < cols ? rows : cols;
+    L.ld = static_cast<int>(round_up(cols, 8));
+    L.ldm = static_cast<int>(round_up(L.m, 8));
+    L.xs = static_cast<size_t>(rows) * L.ld;
+    L.ms = static_cast<size_t>(L.m) * L.ldm;
+    L.u_stride = round_up(static_cast<size_t>(rows) * cols, 64);
+    size_t at = 256;
+    auto take = [&](size_t bytes) {
+        const size_t o = at;
+        at += round_up(bytes, 256);
+        return o;
+    };
+    const size_t x = n * L.xs * 2, a = n * L.ms * 2;
+    L.part = take(static_cast<size_t>(n) * kNormBlocks * sizeof(double));
+    L.U = muon ? take(n * L.u_stride * 4) : 0;
+    L.hi[0] = take(x);
+    L.hi[1] = take(x);
+    L.lo[0] = take(x);
+    L.lo[1] = split ? take(x) : L.lo[0];  // a linear term's low part is updated in place
+    L.x32 = split ? take(2 * x) : 0;
+    L.A[0] = take(a);
+    L.B[0] = take(a);
+    L.A[1] = split ? take(a) : 0;
+    L.B[1] = split ? take(a) : 0;
+    L.total = at;
+    return L;
+}
+
+using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
+                                   const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                   const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                   CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiledFn encode_fn() {
+    static EncodeTiledFn fn = nullptr;
+    static std::once_flag once;
+    std::call_once(once, [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault,
+                                             &q) == cudaSuccess &&
+            q == cudaDriverEntryPointSuccess)
+            fn = reinterpret_cast<EncodeTiledFn>(p);
+    });
+    return fn;
+}
+
+// A batch [n][outer][inner] of fp16 matrices (row stride ld, matrix stride `stride` elements) as
+// a GEMM operand: K-major (inner = k: boxes of 64 k x 128 rows) or MN-major (64 columns x 64 k);
+// 128-byte swizzle, zeros outside each matrix.
+bool ns_map(CUtensorMap* m, const __half* base, int inner, int outer, int n, int ld, size_t stride,
+            bool mn) {
+    const EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    cuuint64_t dims[3] = {static_cast<cuuint64_t>(inner), static_cast<cuuint64_t>(outer),
+                          static_cast<cuuint64_t>(n)};
+    cuuint64_t strides[2] = {static_cast<cuuint64_t>(ld) * 2, stride * 2};
+    cuuint32_t box[3] = {64, mn ? 64u : 128u, 1};
+    cuuint32_t es[3] = {1, 1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<__half*>(base), dims, strides, box, es,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Pair clusters of a kernel that can be resident at once on the current device, computed once
+// per device (after the kernel's shared-memory limit is raised there).
+template <auto Kern>
+int resident_clusters(int threads, int smem_bytes, int sm_count) {
+    static std::atomic<int> cache[kMaxDevices];
+    const int dev = current_device();
+    if (dev < 0) return sm_count / 2;
+    int n = cache[dev].load(std::memory_order_relaxed);
+    if (n > 0) return n;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(sm_count / 2 * 2), 1, 1);
+    cfg.blockDim = dim3(static_cast<unsigned>(threads), 1, 1);
+    cfg.dynamicSmemBytes = static_cast<size_t>(smem_bytes);
+    if (cudaOccupancyMaxActiveClusters(&n, Kern, &cfg) != cudaSuccess || n < 1) {
+        cudaGetLastError();
+        n = sm_count / 2;
+    }
+    cache[dev].store(n, std::memory_order_relaxed);
+    return n;
+}
+
+// One batch of GEMMs on the pair kernel.
+template <bool A_MN, bool B_MN, bool kSplit, class Epi>
+cudaError_t run_ns(const NsMaps& maps, const typename Epi::Params& ep, int M, int N, int K,
+                   int groups, bool tri, unsigned* status, cudaStream_t st) {
+    constexpr auto kern = ns_gemm_kernel<A_MN, B_MN, kSplit, Epi>;
+    cudaError_t e = set_smem_limit<kern>(NsSmem::kBytes);
+    if (e != cudaSuccess) return e;
+    DevInfo di;
+    if (!current_device_info(&di)) return cudaErrorUnknown;
+    NsShape sh = {};
+    sh.tri = tri;
+    sh.g.M = M;
+    sh.g.N = N;
+    sh.g.K = K;
+    sh.g.m_blocks = (M + kPairBM - 1) / kPairBM;
+    sh.g.n_blocks = (N + kNsBN - 1) / kNsBN;
+    sh.g.k_blocks = (K + kBK - 1) / kBK;
+    sh.g.groups = groups;
+    sh.g.band = 16;
+    const long long per = tri ? static_cast<long long>(sh.g.m_blocks) * (sh.g.m_blocks + 1) / 2
+                              : static_cast<long long>(sh.g.m_blocks) * sh.g.n_blocks;
+    sh.g.tiles = groups * per;
+    const int max_clusters = resident_clusters<kern>(kNsThreads, NsSmem::kBytes, di.sm_count);
+    const long long clusters = sh.g.tiles < max_clusters ? sh.g.tiles : max_clusters;
+    return launch_chained(kern, dim3(static_cast<unsigned>(2 * clusters)), kNsThreads,
+                          NsSmem::kBytes, st, maps, ep, sh, status, wait_limit_ns());
+}
+
+// Largest |c1 s + c3 s^3 + c5 s^5| (odd) on [0, u].
+double odd_max(double c1, double c3, double c5, double u) {
+    double best = fabs(u * (c1 + u * u * (c3 + u * u * c5)));
+    auto at = [&](double z) {  // z = s^2 of a critical point
+        if (z > 0.0 && z < u * u) {
+            const double s = sqrt(z);
+            const double v = fabs(s * (c1 + z * (c3 + z * c5)));
+            if (v > best) best = v;
+        }
+    };
+    // c1 + 3 c3 z + 5 c5 z^2 = 0
+    if (c5 != 0.0) {
+        const double q = 9.0 * c3 * c3 - 20.0 * c5 * c1;
+        if (q >= 0.0) {
+            at((-3.0 * c3 + sqrt(q)) / (10.0 * c5));
+            at((-3.0 * c3 - sqrt(q)) / (10.0 * c5));
+        }
+    } else if (c3 != 0.0) {
+        at(-c1 / (3.0 * c3));
+    }
+    return best;
+}
+
+// Largest |b t + c t^2| on [0, t1].
+double quad_max(double b, double c, double t1) {
+    double best = fabs(t1 * (b + c * t1));
+    if (c != 0.0) {
+        const double t = -b / (2.0 * c);
+        if (t > 0.0 && t < t1) best = fmax(best, fabs(t * (b + c * t)));
+    }
+    return best;
+}
+
+// The power of two that brings a bound to at most 2^15, half of fp16's largest value: what
+// rounding adds to a bound stays far below the other half.
+int scale_exp(double bound) { return 15 - static_cast<int>(ceil(log2(bound))); }
+
+template <bool kSplit, int kOut>
+cudaError_t run_apply(bool tall, const NsLayout& L, uint8_t* ws, int cur, bool next_lo,
+                      typename EpiApply<kSplit, kOut>::Params& ep, int n, int rows, int cols,
+                      unsigned* status, cudaStream_t st) {
+    NsMaps maps;
+    for (int h = 0; h < (kSplit ? 2 : 1); ++h) {
+        const __half* X = reinterpret_cast<const __half*>(ws + (h ? L.lo[cur] : L.hi[cur]));
+        const __half* B = reinterpret_cast<const __half*>(ws + L.B[h]);
+        CUtensorMap* mb = tall ? &maps.b[h] : &maps.a[h];
+        CUtensorMap* mx = tall ? &maps.a[h] : &maps.b[h];
+        if (!ns_map(mb, B, L.m, L.m, n, L.ldm, L.ms, false) ||
+            !ns_map(mx, X, cols, rows, n, L.ld, L.xs, !tall))
+            return cudaErrorInvalidValue;
+    }
+    if (!kSplit) {
+        maps.a[1] = maps.a[0];
+        maps.b[1] = maps.b[0];
+    }
+    ep.hi = reinterpret_cast<const __half*>(ws + L.hi[cur]);
+    ep.lo = reinterpret_cast<__half*>(ws + L.lo[cur]);
+    ep.x32 = kSplit ? reinterpret_cast<float*>(ws + L.x32) : nullptr;
+    ep.next_hi = reinterpret_cast<__half*>(ws + L.hi[cur ^ 1]);
+    ep.next_lo = next_lo ? reinterpret_cast<__half*>(ws + L.lo[cur ^ 1]) : nullptr;
+    ep.stride = static_cast<long long>(L.xs);
+    ep.M = rows;
+    ep.N = cols;
+    ep.ld = L.ld;
+    // wide: B X with B K-major and X MN-major; tall: X B, both K-major (B is symmetric)
+    if (tall)
+        return run_ns<false, false, kSplit, EpiApply<kSplit, kOut>>(maps, ep, rows, cols, cols, n,
+                                                                    false, status, st);
+    return run_ns<false, true, kSplit, EpiApply<kSplit, kOut>>(maps, ep, rows, cols, rows, n, false,
+                                                               status, st);
+}
+
+// The iteration on the X_0 in the workspace.
+template <bool kSplit>
+cudaError_t run_steps(const NsLayout& L, uint8_t* ws, int n, int rows, int cols, int steps,
+                      const float* coeffs, const NsTarget& to, unsigned* status, cudaStream_t st) {
+    constexpr int kParts = kSplit ? 2 : 1;
+    const bool tall = rows > cols;
+    double u = 1.0;            // bound of the singular values of X_k
+    int sx = scale_exp(u);     // X_k is stored times 2^sx
+    int cur = 0;
+    for (int k = 0; k < steps; ++k) {
+        const double a = coeffs[3 * k], b = coeffs[3 * k + 1], c = coeffs[3 * k + 2];
+        const double ub = quad_max(b, c, u * u), un = odd_max(a, b, c, u);
+        const int sa = scale_exp(u * u), sb = ub > 0.0 ? scale_exp(ub) : 0,
+                  sn = un > 0.0 ? scale_exp(un) : 0;
+
+        typename EpiSym<kSplit>::Params sp = {};
+        sp.stride = static_cast<long long>(L.ms);
+        sp.M = L.m;
+        sp.ld = L.ldm;
+        NsMaps maps;
+        // A = X X^T
+        for (int h = 0; h < kParts; ++h) {
+            const __half* X = reinterpret_cast<const __half*>(ws + (h ? L.lo[cur] : L.hi[cur]));
+            if (!ns_map(&maps.a[h], X, cols, rows, n, L.ld, L.xs, tall)) return cudaErrorInvalidValue;
+            sp.out[h] = reinterpret_cast<__half*>(ws + L.A[h]);
+        }
+        if (!kSplit) maps.a[1] = maps.a[0];
+        maps.b[0] = maps.a[0];
+        maps.b[1] = maps.a[1];
+        sp.acc_coef = static_cast<float>(ldexp(1.0, sa - 2 * sx));
+        cudaError_t e =
+            tall ? run_ns<true, true, kSplit, EpiSym<kSplit>>(maps, sp, L.m, L.m, rows, n, true,
+                                                              status, st)
+                 : run_ns<false, false, kSplit, EpiSym<kSplit>>(maps, sp, L.m, L.m, cols, n, true,
+                                                                status, st);
+        if (e != cudaSuccess) return e;
+        // B = b A + c A^2
+        for (int h = 0; h < kParts; ++h) {
+            const __half* A = reinterpret_cast<const __half*>(ws + L.A[h]);
+            if (!ns_map(&maps.a[h], A, L.m, L.m, n, L.ldm, L.ms, false)) return cudaErrorInvalidValue;
+            sp.lin[h] = A;
+            sp.out[h] = reinterpret_cast<__half*>(ws + L.B[h]);
+        }
+        if (!kSplit) maps.a[1] = maps.a[0];
+        maps.b[0] = maps.a[0];
+        maps.b[1] = maps.a[1];
+        sp.lin_coef = static_cast<float>(ldexp(b, sb - sa));
+        sp.acc_coef = static_cast<float>(ldexp(c, sb - 2 * sa));
+        e = run_ns<false, false, kSplit, EpiSym<kSplit>>(maps, sp, L.m, L.m, L.m, n, true, status, st);
+        if (e != cudaSuccess) return e;
+        // X' = a X + B X.  The last step takes the linear term of fp16 calls from the operand
+        // itself: nothing grows after it, and the same X in both terms is the smaller error.
+        const bool last = k == steps - 1;
+        auto coefs = [&](auto& ep) {
+            const int so = last ? 0 : sn;
+            ep.lin_coef = static_cast<float>(ldexp(a, so - sx));
+            ep.acc_coef = static_cast<float>(ldexp(1.0, so - sb - sx));
+            ep.lin_lo = !last;
+        };
+        if (!last) {
+            typename EpiApply<kSplit, kNext>::Params ep = {};
+            coefs(ep);
+            e = run_apply<kSplit, kNext>(tall, L, ws, cur, kSplit || k + 2 < steps, ep, n, rows, cols,
+                                         status, st);
+        } else if (to.W) {
+            typename EpiApply<kSplit, kWeight>::Params ep = {};
+            coefs(ep);
+            ep.keep = to.keep;
+            ep.rate = to.rate;
+            for (int l = 0; l < n; ++l) {
+                ep.W[l] = to.W[l];
+                ep.out[l] = to.out ? static_cast<typename EpiApply<kSplit, kWeight>::Out*>(to.out[l])
+                                   : nullptr;
+            }
+            e = run_apply<kSplit, kWeight>(tall, L, ws, cur, false, ep, n, rows, cols, status, st);
+        } else {
+            typename EpiApply<kSplit, kResult>::Params ep = {};
+            coefs(ep);
+            for (int l = 0; l < n; ++l)
+                ep.out[l] = static_cast<typename EpiApply<kSplit, kResult>::Out*>(to.out[l]);
+            e = run_apply<kSplit, kResult>(tall, L, ws, cur, false, ep, n, rows, cols, status, st);
+        }
+        if (e != cudaSuccess) return e;
+        cur ^= 1;
+        u = un;
+        sx = sn;
+    }
+    return cudaSuccess;
+}
+
+}  // namespace
+
+bool ns_coeffs_ok(int steps, const float* coeffs) {
+    double u = 1.0;
+    for (int k = 0; k < steps; ++k) {
+        const double a = coeffs[3 * k], b = coeffs[3 * k + 1], c = coeffs[3 * k + 2];
+        if (!isfinite(a) || !isfinite(b) || !isfinite(c)) return false;
+        u = odd_max(a, b, c, u);
+        // bounds within 2^+-16: every coefficient of an epilogue is then a normal fp32 number
+        if (!(u >= 0x1p-16 && u <= 0x1p16)) return false;
+        if (fabs(a) > 0x1p16 || fabs(b) > 0x1p16 || fabs(c) > 0x1p16) return false;
+    }
+    return true;
+}
+
+size_t ns_workspace_bytes(int n, int rows, int cols, int dtype, bool muon) {
+    return ns_layout(n, rows, cols, dtype == 0, muon).total;
+}
+
+float* ns_update_buffer(void* ws, int n, int rows, int cols, int dtype, int layer) {
+    const NsLayout L = ns_layout(n, rows, cols, dtype == 0, true);
+    return reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + L.U) + layer * L.u_stride;
+}
+
+cudaError_t launch_newton_schulz(int n, int rows, int cols, int dtype, const void* const* G,
+                                 const NsMomentum* mom, double eps, int steps, const float* coeffs,
+                                 const NsTarget& to, void* workspace, unsigned* status,
+                                 cudaStream_t st) {
+    const bool split = dtype == 0;
+    const NsLayout L = ns_layout(n, rows, cols, split, mom != nullptr);
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    double* part = reinterpret_cast<double*>(ws + L.part);
+    const size_t numel = static_cast<size_t>(rows) * cols;
+    const int blocks = norm_blocks(numel);
+    NsPtrs p = {};
+    for (int l = 0; l < n; ++l) {
+        p.in[l] = mom ? reinterpret_cast<float*>(ws + L.U) + l * L.u_stride : G[l];
+        p.M[l] = mom ? mom->M[l] : nullptr;
+    }
+    const dim3 grid(blocks, n);
+    cudaError_t e;
+    if (mom) {
+        ns_momentum_kernel<<<grid, kPassThreads, 0, st>>>(p, numel, mom->mu, mom->nesterov, part),
+            note_launch();
+        e = cudaGetLastError();
+    } else if (split) {
+        e = launch_chained(ns_norm_kernel<float>, grid, kPassThreads, 0, st, p, numel, part);
+    } else {
+        e = launch_chained(ns_norm_kernel<__nv_bfloat16>, grid, kPassThreads, 0, st, p, numel, part);
+    }
+    if (e != cudaSuccess) return e;
+    const size_t vecs = static_cast<size_t>(rows) * (L.ld / 8);
+    const size_t want = (vecs + kPassThreads - 1) / kPassThreads;
+    const dim3 cgrid(static_cast<unsigned>(want < 1024 ? want : 1024), n);
+    __half* hi = reinterpret_cast<__half*>(ws + L.hi[0]);
+    __half* lo = reinterpret_cast<__half*>(ws + L.lo[0]);
+    float* x32 = split ? reinterpret_cast<float*>(ws + L.x32) : nullptr;
+    const double scale = ldexp(1.0, scale_exp(1.0));
+    if (split)
+        e = launch_chained(ns_cast_kernel<float, true>, cgrid, kPassThreads, 0, st, p, rows, cols, L.ld, part, blocks, eps, scale, hi, lo, x32, L.xs);
+    else if (mom)
+        e = launch_chained(ns_cast_kernel<float, false>, cgrid, kPassThreads, 0, st, p, rows, cols, L.ld, part, blocks, eps, scale, hi, lo, x32, L.xs);
+    else
+        e = launch_chained(ns_cast_kernel<__nv_bfloat16, false>, cgrid, kPassThreads, 0, st, p, rows, cols, L.ld, part, blocks, eps, scale, hi, lo, x32, L.xs);
+    if (e != cudaSuccess) return e;
+    if (split) return run_steps<true>(L, ws, n, rows, cols, steps, coeffs, to, status, st);
+    return run_steps<false>(L, ws, n, rows, cols, steps, coeffs, to, status, st);
+}
+
+}  // namespace fpo
