@@ -77,11 +77,13 @@ struct RowVec<float, 1> {
 };
 
 // Sums of N values over the W warps that share a row, the same bits in every thread: a
-// butterfly per warp, then the warps' sums in warp order.  `buf` alternates between two
+// butterfly per warp, then one over the warps' sums, which every warp reads one to a lane (all
+// threads adding all W of them took 0.6 us a row with 16 warps).  `at` alternates between two
 // areas from call to call, so one barrier a call is enough.
 template <int N, int W>
 struct RowSum {
-    float (*sh)[2][N][W];  // shared (W > 1 only)
+    float (*sh)[2][N][W];  // shared (W > 1 only), this row group's
+    int group;             // of the block's row groups
     int at;
     __device__ __forceinline__ void operator()(float (&v)[N]) {
 #pragma unroll
@@ -90,103 +92,166 @@ struct RowSum {
             for (int k = 0; k < N; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
         }
         if constexpr (W > 1) {
-            const int w = threadIdx.x >> 5;
-            if ((threadIdx.x & 31) == 0) {
+            const int w = (threadIdx.x >> 5) % W, lane = threadIdx.x & 31;
+            if (lane == 0) {
 #pragma unroll
                 for (int k = 0; k < N; ++k) (*sh)[at][k][w] = v[k];
             }
-            __syncthreads();
+            // the row group's own barrier (0 is __syncthreads)
+            asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(32 * W) : "memory");
 #pragma unroll
-            for (int k = 0; k < N; ++k) {
-                v[k] = 0.f;
+            for (int k = 0; k < N; ++k) v[k] = (*sh)[at][k][lane % W];
 #pragma unroll
-                for (int i = 0; i < W; ++i) v[k] += (*sh)[at][k][i];
+            for (int o = W / 2; o > 0; o >>= 1) {
+#pragma unroll
+                for (int k = 0; k < N; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
             }
             at ^= 1;
         }
     }
 };
 
-// TH threads to a row (a warp: 8 rows per block), NV vectors of VEC elements per thread:
-// vector v of thread t holds elements (v TH + t) VEC ...
+// TH threads to a row, blocks of 256 threads (512 for the longest rows) with 256 / TH rows at a
+// time, NV vectors of VEC elements per thread: vector v of thread t of a row holds elements
+// (v TH + t) VEC ...
 template <int TH>
 constexpr int ln_threads() {
-    return TH == 32 ? 256 : TH;
+    return TH == 512 ? 512 : 256;
 }
 template <int TH>
 constexpr int ln_rows() {
     return ln_threads<TH>() / TH;
 }
+// Elements of a row per thread, at most; twice that for the longest fp32 rows.
+template <typename TT, int TH = 256>
+constexpr int ln_ept() {
+    return sizeof(TT) == 2 || TH == 512 ? 16 : 8;
+}
+// Blocks per SM that the registers have to leave room for.
+template <int TH, bool kBack>
+constexpr int ln_min_blocks() {
+    return TH == 512 ? 1 : kBack ? 2 : 3;
+}
 
+// A thread's vectors of a row, and their elements in pairs for packed arithmetic (a last odd
+// one with a zero).  The number of instructions bounds the passes over a row as much as its
+// bytes do: with scalar arithmetic and the weights read again in every pass the backward
+// pass of T 16384, d 4096 took 124 us.
 template <typename TT, int VEC, int NV, int TH>
-__global__ void __launch_bounds__(ln_threads<TH>())
-    layernorm_fwd_kernel(const TT* __restrict__ x, const TT* __restrict__ gamma,
-                         const TT* __restrict__ beta, int T, int d, float eps,
-                         TT* __restrict__ y, float* __restrict__ mean_out,
-                         float* __restrict__ rstd_out) {
+struct RowPart {
+    static constexpr int kE = VEC * NV, kPairs = (kE + 1) / 2;
     using V = RowVec<TT, VEC>;
-    constexpr int kW = TH / 32;
-    __shared__ float sh[2][1][kW];
-    RowSum<1, kW> row_sum{&sh, 0};
-    const int t = threadIdx.x % TH;
-    const float inv_d = 1.f / static_cast<float>(d);
-    V nx[NV];
-    auto load = [&](long long row) {
+    V r[NV];
+    // (outside the row: zeros)
+    __device__ __forceinline__ void load(const TT* p, int t, int d) {
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int k = (v * TH + t) * VEC;
             if (k < d)
-                nx[v].load(x + row * d + k);
+                r[v].load(p + k);
             else
-                nx[v].zero();
+                r[v].zero();
         }
-    };
-    const long long step = gridDim.x * ln_rows<TH>();
-    long long row = blockIdx.x * ln_rows<TH>() + threadIdx.x / TH;
-    if (row < T) load(row);
-    for (; row < T; row += step) {
-        float c[NV][VEC];
-        float s[1] = {0.f};
+    }
+    __device__ __forceinline__ void get(float2 (&f)[kPairs]) const {
+        float e[2 * kPairs];
+        if constexpr (kE % 2) e[kE] = 0.f;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            nx[v].get(c[v]);
+            float x[VEC];
+            r[v].get(x);
 #pragma unroll
-            for (int q = 0; q < VEC; ++q) s[0] += c[v][q];
+            for (int q = 0; q < VEC; ++q) e[v * VEC + q] = x[q];
         }
-        if (row + step < T) load(row + step);
-        row_sum(s);
-        const float mu = __fmul_rn(s[0], inv_d);
-        s[0] = 0.f;
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const bool in = (v * TH + t) * VEC < d;
-#pragma unroll
-            for (int q = 0; q < VEC; ++q) {
-                c[v][q] = in ? c[v][q] - mu : 0.f;
-                s[0] = fmaf(c[v][q], c[v][q], s[0]);
-            }
-        }
-        row_sum(s);
-        const float rstd = 1.f / sqrtf(fmaf(s[0], inv_d, eps));
+        for (int i = 0; i < kPairs; ++i) f[i] = make_float2(e[2 * i], e[2 * i + 1]);
+    }
+    static __device__ __forceinline__ void store(TT* p, int t, int d, const float2 (&f)[kPairs]) {
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int k = (v * TH + t) * VEC;
-            if (k >= d) continue;
-            float w[VEC], b[VEC], o[VEC];
-            V u;
-            if (gamma) {
-                u.load(gamma + k);
-                u.get(w);
-            }
-            if (beta) {
-                u.load(beta + k);
-                u.get(b);
-            }
+            float x[VEC];
 #pragma unroll
-            for (int q = 0; q < VEC; ++q)
-                o[q] = fmaf(c[v][q] * rstd, gamma ? w[q] : 1.f, beta ? b[q] : 0.f);
-            V::store(y + row * d + k, o);
+            for (int q = 0; q < VEC; ++q) {
+                const float2& w = f[(v * VEC + q) / 2];
+                x[q] = (v * VEC + q) % 2 ? w.y : w.x;
+            }
+            if (k < d) V::store(p + k, x);
         }
+    }
+    // Whether element e of the thread's is inside the row.
+    static __device__ __forceinline__ bool in(int e, int t, int d) {
+        return e < kE && (e / VEC * TH + t) * VEC < d;
+    }
+};
+
+__device__ __forceinline__ float2 both(float a) { return make_float2(a, a); }
+
+// x - mu, zero outside the row.
+template <class P, int TH>
+__device__ __forceinline__ void center(float2 (&x)[P::kPairs], float mu, int t, int d, bool full) {
+    const float2 m = both(-mu);
+#pragma unroll
+    for (int i = 0; i < P::kPairs; ++i) x[i] = __fadd2_rn(x[i], m);
+    if (full) return;
+#pragma unroll
+    for (int i = 0; i < P::kPairs; ++i) {
+        if (!P::in(2 * i, t, d)) x[i].x = 0.f;
+        if (!P::in(2 * i + 1, t, d)) x[i].y = 0.f;
+    }
+}
+
+template <typename TT, int VEC, int NV, int TH>
+__global__ void __launch_bounds__(ln_threads<TH>(), ln_min_blocks<TH, false>())
+    layernorm_fwd_kernel(const TT* __restrict__ x, const TT* __restrict__ gamma,
+                         const TT* __restrict__ beta, int T, int d, float eps,
+                         TT* __restrict__ y, float* __restrict__ mean_out,
+                         float* __restrict__ rstd_out) {
+    using P = RowPart<TT, VEC, NV, TH>;
+    constexpr int kW = TH / 32;
+    __shared__ float sh[ln_rows<TH>()][2][1][kW];
+    const int group = threadIdx.x / TH;
+    RowSum<1, kW> row_sum{&sh[group], group, 0};
+    const int t = threadIdx.x % TH;
+    const float inv_d = 1.f / static_cast<float>(d);
+    const bool full = d == TH * NV * VEC && P::kE % 2 == 0;  // every thread's elements inside
+    P nx, w, b;
+    if (gamma) w.load(gamma, t, d);
+    if (beta) b.load(beta, t, d);
+    const long long step = gridDim.x * ln_rows<TH>();
+    long long row = blockIdx.x * ln_rows<TH>() + group;
+    if (row < T) nx.load(x + row * d, t, d);
+    for (; row < T; row += step) {
+        float2 c[P::kPairs];
+        float2 a = both(0.f);
+        nx.get(c);
+#pragma unroll
+        for (int i = 0; i < P::kPairs; ++i) a = __fadd2_rn(a, c[i]);
+        if (row + step < T) nx.load(x + (row + step) * d, t, d);
+        float s[1] = {a.x + a.y};
+        row_sum(s);
+        const float mu = s[0] * inv_d;
+        center<P, TH>(c, mu, t, d, full);
+        a = both(0.f);
+#pragma unroll
+        for (int i = 0; i < P::kPairs; ++i) a = __ffma2_rn(c[i], c[i], a);
+        s[0] = a.x + a.y;
+        row_sum(s);
+        const float rstd = 1.f / sqrtf(fmaf(s[0], inv_d, eps));
+        float2 wf[P::kPairs], bf[P::kPairs];
+        if (gamma) w.get(wf);
+        if (beta) b.get(bf);
+#pragma unroll
+        for (int i = 0; i < P::kPairs; ++i) {
+            c[i] = __fmul2_rn(c[i], both(rstd));
+            if (gamma && beta)
+                c[i] = __ffma2_rn(c[i], wf[i], bf[i]);
+            else if (gamma)
+                c[i] = __fmul2_rn(c[i], wf[i]);
+            else if (beta)
+                c[i] = __fadd2_rn(c[i], bf[i]);
+        }
+        P::store(y + row * d, t, d, c);
         if (t == 0) {
             if (mean_out) mean_out[row] = mu;
             if (rstd_out) rstd_out[row] = rstd;
@@ -194,116 +259,97 @@ __global__ void __launch_bounds__(ln_threads<TH>())
     }
 }
 
-// part (kW only): [grid][2][d] sums of g xhat and of g over the block's rows.
+// part (kSums only): [grid][2][d] sums of g xhat and of g over the block's rows.
 template <typename TT, int VEC, int NV, int TH, bool kSums>
-__global__ void __launch_bounds__(ln_threads<TH>())
+__global__ void __launch_bounds__(ln_threads<TH>(), ln_min_blocks<TH, true>())
     layernorm_vjp_kernel(const TT* __restrict__ g, const TT* __restrict__ x,
                          const TT* __restrict__ gamma, int T, int d, float eps, float min_rms,
                          TT* __restrict__ out, float* __restrict__ part) {
-    using V = RowVec<TT, VEC>;
-    constexpr int kW = TH / 32;
-    __shared__ float sh1[2][2][kW], sh2[2][2][kW];
-    RowSum<2, kW> sum1{&sh1, 0}, sum2{&sh2, 0};
+    using P = RowPart<TT, VEC, NV, TH>;
+    constexpr int kPairs = P::kPairs, kW = TH / 32;
+    __shared__ float sh[ln_rows<TH>()][2][2][kW];
+    const int group = threadIdx.x / TH;
+    RowSum<2, kW> row_sum{&sh[group], group, 0};
     grid_dependency_trigger();
     const int t = threadIdx.x % TH;
     const float inv_d = 1.f / static_cast<float>(d);
-    V nx[NV], ng[NV], w[NV];
+    const bool full = d == TH * NV * VEC && P::kE % 2 == 0;
+    P nx, ng, w;
+    if (gamma) w.load(gamma, t, d);
+    float2 dg[kSums ? kPairs : 1], db[kSums ? kPairs : 1];
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        w[v].zero();
-        const int k = (v * TH + t) * VEC;
-        if (gamma && k < d) w[v].load(gamma + k);
-    }
-    auto load = [&](long long row) {
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int k = (v * TH + t) * VEC;
-            if (k < d) {
-                nx[v].load(x + row * d + k);
-                ng[v].load(g + row * d + k);
-            } else {
-                nx[v].zero();
-                ng[v].zero();
-            }
-        }
-    };
-    float dg[kSums ? NV : 1][VEC], db[kSums ? NV : 1][VEC];
-#pragma unroll
-    for (int v = 0; v < (kSums ? NV : 1); ++v) {
-#pragma unroll
-        for (int q = 0; q < VEC; ++q) dg[v][q] = db[v][q] = 0.f;
-    }
+    for (int i = 0; i < (kSums ? kPairs : 1); ++i) dg[i] = db[i] = both(0.f);
     const long long step = gridDim.x * ln_rows<TH>();
-    long long row = blockIdx.x * ln_rows<TH>() + threadIdx.x / TH;
-    if (row < T) load(row);
+    long long row = blockIdx.x * ln_rows<TH>() + group;
+    if (row < T) {
+        nx.load(x + row * d, t, d);
+        ng.load(g + row * d, t, d);
+    }
     for (; row < T; row += step) {
-        float c[NV][VEC], gv[NV][VEC];
-        float s[2] = {0.f, 0.f};  // x, then u
-        auto weight = [&](int v, int q) {
-            float wv[VEC];
-            w[v].get(wv);
-            return gamma ? wv[q] : 1.f;
-        };
+        float2 c[kPairs], gv[kPairs], u[kPairs];
+        float2 a0 = both(0.f), a1 = both(0.f);  // sums of x and of u = gamma g
+        nx.get(c);
+        ng.get(gv);
+        if (gamma) {
+            float2 wf[kPairs];
+            w.get(wf);
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            nx[v].get(c[v]);
-            ng[v].get(gv[v]);
+            for (int i = 0; i < kPairs; ++i) u[i] = __fmul2_rn(gv[i], wf[i]);
+        } else {
 #pragma unroll
-            for (int q = 0; q < VEC; ++q) {
-                s[0] += c[v][q];
-                s[1] = fmaf(gv[v][q], weight(v, q), s[1]);
-            }
+            for (int i = 0; i < kPairs; ++i) u[i] = gv[i];
         }
-        if (row + step < T) load(row + step);
-        sum1(s);
-        // (explicit roundings and FMAs from here: the same bits with and without the sums)
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) {
+            a0 = __fadd2_rn(a0, c[i]);
+            a1 = __fadd2_rn(a1, u[i]);
+        }
+        if (row + step < T) {
+            nx.load(x + (row + step) * d, t, d);
+            ng.load(g + (row + step) * d, t, d);
+        }
+        float s[2] = {a0.x + a0.y, a1.x + a1.y};
+        row_sum(s);
         const float mu = __fmul_rn(s[0], inv_d), um = __fmul_rn(s[1], inv_d);
-        s[0] = s[1] = 0.f;  // (x - mu)^2, then u (x - mu)
+        center<P, TH>(c, mu, t, d, full);
+        a0 = a1 = both(0.f);  // sums of (x - mu)^2 and of u (x - mu)
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const bool in = (v * TH + t) * VEC < d;
-#pragma unroll
-            for (int q = 0; q < VEC; ++q) {
-                c[v][q] = in ? c[v][q] - mu : 0.f;
-                s[0] = fmaf(c[v][q], c[v][q], s[0]);
-                s[1] = fmaf(__fmul_rn(gv[v][q], weight(v, q)), c[v][q], s[1]);
-            }
+        for (int i = 0; i < kPairs; ++i) {
+            a0 = __ffma2_rn(c[i], c[i], a0);
+            a1 = __ffma2_rn(u[i], c[i], a1);
         }
-        sum2(s);
+        s[0] = a0.x + a0.y;
+        s[1] = a1.x + a1.y;
+        row_sum(s);
         const float sigma = sqrtf(fmaf(s[0], inv_d, eps));
         const float rstd = 1.f / sigma;
         const float cm = __fmul_rn(__fmul_rn(s[1], inv_d), rstd);  // mean(u xhat)
-        const float pref = 1.f / fmaxf(sigma, min_rms);
+        const float2 pref = both(1.f / fmaxf(sigma, min_rms)), r2 = both(rstd), nc = both(-cm),
+                     nu = both(-um);
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int k = (v * TH + t) * VEC;
-            float o[VEC];
-#pragma unroll
-            for (int q = 0; q < VEC; ++q) {
-                const float xh = __fmul_rn(c[v][q], rstd);
-                o[q] = fmaf(-xh, cm, fmaf(gv[v][q], weight(v, q), -um)) * pref;
-                if constexpr (kSums) {
-                    dg[v][q] = fmaf(gv[v][q], xh, dg[v][q]);
-                    db[v][q] += gv[v][q];
-                }
+        for (int i = 0; i < kPairs; ++i) {
+            c[i] = __fmul2_rn(c[i], r2);  // xhat
+            if constexpr (kSums) {
+                dg[i] = __ffma2_rn(gv[i], c[i], dg[i]);
+                db[i] = __fadd2_rn(db[i], gv[i]);
             }
-            if (out && k < d) V::store(out + row * d + k, o);
+            u[i] = __fmul2_rn(__ffma2_rn(c[i], nc, __fadd2_rn(u[i], nu)), pref);
         }
+        if (out) P::store(out + row * d, t, d, u);
     }
     if constexpr (kSums) {
         float* p = part + static_cast<size_t>(blockIdx.x) * 2 * d;
         if constexpr (ln_rows<TH>() > 1) {
-            // the block's 8 warps hold the same columns: their sums in warp order
+            // the block's row groups hold the same columns: their sums in group order
             constexpr int kCols = NV * TH * VEC;
             __shared__ float acc[ln_rows<TH>()][kCols];
 #pragma unroll
             for (int which = 0; which < 2; ++which) {
                 __syncthreads();
 #pragma unroll
-                for (int v = 0; v < NV; ++v) {
-#pragma unroll
-                    for (int q = 0; q < VEC; ++q)
-                        acc[threadIdx.x / TH][(v * TH + t) * VEC + q] = which ? db[v][q] : dg[v][q];
+                for (int e = 0; e < P::kE; ++e) {
+                    const float2& f = which ? db[e / 2] : dg[e / 2];
+                    acc[group][(e / VEC * TH + t) * VEC + e % VEC] = e % 2 ? f.y : f.x;
                 }
                 __syncthreads();
                 for (int k = threadIdx.x; k < d; k += ln_threads<TH>()) {
@@ -314,16 +360,16 @@ __global__ void __launch_bounds__(ln_threads<TH>())
                 }
             }
         } else {
+            float2 z[kPairs];
 #pragma unroll
-            for (int v = 0; v < NV; ++v) {
+            for (int which = 0; which < 2; ++which) {
 #pragma unroll
-                for (int q = 0; q < VEC; ++q) {
-                    const int k = (v * TH + t) * VEC + q;
-                    if (k < d) {
-                        p[k] = dg[v][q];
-                        p[d + k] = db[v][q];
-                    }
-                }
+                for (int i = 0; i < kPairs; ++i) z[i] = which ? db[i] : dg[i];
+#pragma unroll
+                for (int e = 0; e < P::kE; ++e)
+                    if (P::in(e, t, d))
+                        p[which * d + (e / VEC * TH + t) * VEC + e % VEC] = e % 2 ? z[e / 2].y
+                                                                                : z[e / 2].x;
             }
         }
     }
@@ -370,7 +416,7 @@ __global__ void __launch_bounds__(kLongThreads)
                               float* __restrict__ rstd_out) {
     using V = RowVec<TT, VEC>;
     __shared__ float sh[2][2][kLongThreads / 32];
-    RowSum<2, kLongThreads / 32> sum{&sh, 0};
+    RowSum<2, kLongThreads / 32> sum{&sh, 0, 0};
     for (long long row = blockIdx.x; row < T; row += gridDim.x) {
         const TT* xr = x + row * d;
         const float2 st = long_stats<TT, VEC>(xr, d, eps, sum);
@@ -408,7 +454,7 @@ __global__ void __launch_bounds__(kLongThreads)
                               TT* __restrict__ out, float2* __restrict__ stats) {
     using V = RowVec<TT, VEC>;
     __shared__ float sh[2][2][kLongThreads / 32];
-    RowSum<2, kLongThreads / 32> sum{&sh, 0};
+    RowSum<2, kLongThreads / 32> sum{&sh, 0, 0};
     grid_dependency_trigger();
     const float inv_d = 1.f / static_cast<float>(d);
     for (long long row = blockIdx.x; row < T; row += gridDim.x) {
@@ -483,9 +529,9 @@ __global__ void __launch_bounds__(kColThreads)
     p[d + k] = db;
 }
 
-// dgamma, dbeta [d] from part [n][2][d]: 32 columns per block, 8 threads to a column, each
+// dgamma, dbeta [d] from part [n][2][d]: 32 columns per block, 16 threads to a column, each
 // a contiguous range of the n; the ranges' sums in order.
-constexpr int kFinCols = 32, kFinRanges = 8;
+constexpr int kFinCols = 32, kFinRanges = 16;
 __global__ void __launch_bounds__(kFinCols* kFinRanges)
     layernorm_cols_final_kernel(const float* part, int n, int d, float* dgamma, float* dbeta) {
     __shared__ float sh[kFinRanges][kFinCols];
@@ -511,18 +557,20 @@ __global__ void __launch_bounds__(kFinCols* kFinRanges)
 }
 
 // Vectors per thread and threads per row of the register kernels for rows of d elements in
-// vectors of vec; up to 16 elements per thread (with 32 the backward pass's sums spill).
+// vectors of VEC: the fewest threads (a row's sums then cross few warps, and several rows share
+// an SM), up to 512.
 struct RowForm {
     int nv, th;  // 0: a long row
 };
-RowForm row_form(int d, int vec) {
-    const int n = (d + vec - 1) / vec;
-    if (n <= 32) return {1, 32};
-    if (n <= 64) return {2, 32};
-    if (n <= 128) return {1, 128};
-    if (n <= 256) return {1, 256};
-    for (int nv = 1; nv * vec <= 16; nv *= 2)
-        if (n <= 512 * nv) return {nv, 512};
+template <typename TT, int VEC>
+RowForm row_form(int d) {
+    constexpr int kMax = ln_ept<TT>() / VEC, kMax512 = ln_ept<TT, 512>() / VEC;
+    const int n = (d + VEC - 1) / VEC;
+    for (int nv = 1; nv <= kMax; nv *= 2)
+        if (n <= 32 * nv) return {nv, 32};
+    for (int th = 64; th <= 256; th *= 2)
+        if (n <= th * kMax) return {kMax, th};
+    if (n <= 512 * kMax512) return {kMax512, 512};
     return {0, 0};
 }
 
@@ -532,36 +580,43 @@ int sms() {
 }
 
 // Blocks of the register kernels of the backward pass, each with its share of the weight
-// sums: enough for two of 512 threads (more of the smaller ones) on each of 152 SMs.
+// sums: as many as are resident on 152 SMs (ln_min_blocks).
 int vjp_blocks(int T, const RowForm& f) {
-    const int rows = f.th == 32 ? 8 : 1, cap = f.th == 512 ? 304 : 608;
+    const int rows = f.th == 512 ? 1 : 256 / f.th, cap = f.th == 512 ? 152 : 304;
     const int want = T / rows + (T % rows != 0);
     return want < cap ? want : cap;
 }
 constexpr int kLongRanges = 64;
 int long_ranges(int T) { return T < kLongRanges ? T : kLongRanges; }
 
-int vec_of(int dtype, int d) { return dtype == 1 ? 8 : d % 4 == 0 ? 4 : 1; }
-
 // Calls f with (vectors per thread, threads per row) as compile-time constants.
 template <int N>
 struct Int {
     static constexpr int value = N;
 };
-template <int VEC, class F>
+template <typename TT, int VEC, class F>
 cudaError_t with_form(const RowForm& f, F&& fn) {
-    if (f.th == 32) return f.nv == 1 ? fn(Int<1>{}, Int<32>{}) : fn(Int<2>{}, Int<32>{});
-    if (f.th == 128) return fn(Int<1>{}, Int<128>{});
-    if (f.th == 256) return fn(Int<1>{}, Int<256>{});
-    if (f.nv == 1) return fn(Int<1>{}, Int<512>{});
-    if constexpr (VEC <= 4) {
-        if (f.nv == 4) return fn(Int<4>{}, Int<512>{});
+    constexpr int kMax = ln_ept<TT>() / VEC, kMax512 = ln_ept<TT, 512>() / VEC;
+    switch (f.th) {
+        case 64: return fn(Int<kMax>{}, Int<64>{});
+        case 128: return fn(Int<kMax>{}, Int<128>{});
+        case 256: return fn(Int<kMax>{}, Int<256>{});
+        case 512: return fn(Int<kMax512>{}, Int<512>{});
+        default: break;
     }
-    if constexpr (VEC == 1) {
-        if (f.nv == 8) return fn(Int<8>{}, Int<512>{});
-        if (f.nv == 16) return fn(Int<16>{}, Int<512>{});
+    if constexpr (kMax >= 16) {
+        if (f.nv == 16) return fn(Int<16>{}, Int<32>{});
     }
-    return fn(Int<2>{}, Int<512>{});
+    if constexpr (kMax >= 8) {
+        if (f.nv == 8) return fn(Int<8>{}, Int<32>{});
+    }
+    if constexpr (kMax >= 4) {
+        if (f.nv == 4) return fn(Int<4>{}, Int<32>{});
+    }
+    if constexpr (kMax >= 2) {
+        if (f.nv == 2) return fn(Int<2>{}, Int<32>{});
+    }
+    return fn(Int<1>{}, Int<32>{});
 }
 
 template <typename TT, int VEC>
@@ -571,7 +626,7 @@ cudaError_t run_fwd(const void* x, const void* gamma, const void* beta, int T, i
     const auto* gg = static_cast<const TT*>(gamma);
     const auto* bb = static_cast<const TT*>(beta);
     auto* yy = static_cast<TT*>(y);
-    const RowForm f = row_form(d, VEC);
+    const RowForm f = row_form<TT, VEC>(d);
     if (f.nv == 0) {
         const int grid = T < 4 * sms() ? T : 4 * sms();
         layernorm_fwd_long_kernel<TT, VEC>
@@ -579,10 +634,10 @@ cudaError_t run_fwd(const void* x, const void* gamma, const void* beta, int T, i
             note_launch();
         return cudaGetLastError();
     }
-    return with_form<VEC>(f, [&](auto nv, auto th) {
+    return with_form<TT, VEC>(f, [&](auto nv, auto th) {
         constexpr int NV = decltype(nv)::value, TH = decltype(th)::value;
         const int blocks = T / ln_rows<TH>() + (T % ln_rows<TH>() != 0);
-        const int cap = sms() * (2048 / ln_threads<TH>());
+        const int cap = sms() * ln_min_blocks<TH, false>();
         layernorm_fwd_kernel<TT, VEC, NV, TH>
             <<<blocks < cap ? blocks : cap, ln_threads<TH>(), 0, st>>>(xx, gg, bb, T, d, eps, yy,
                                                                       mean_out, rstd_out),
@@ -600,7 +655,7 @@ cudaError_t run_vjp(const void* g, const void* x, const void* gamma, int T, int 
     const auto* ww = static_cast<const TT*>(gamma);
     auto* oo = static_cast<TT*>(out);
     const bool sums = dgamma || dbeta;
-    const RowForm f = row_form(d, VEC);
+    const RowForm f = row_form<TT, VEC>(d);
     int parts = 0;
     cudaError_t e;
     if (f.nv == 0) {
@@ -618,7 +673,7 @@ cudaError_t run_vjp(const void* g, const void* x, const void* gamma, int T, int 
                            xx, static_cast<const float2*>(stats), T, d, ws);
     } else {
         parts = vjp_blocks(T, f);
-        e = with_form<VEC>(f, [&](auto nv, auto th) {
+        e = with_form<TT, VEC>(f, [&](auto nv, auto th) {
             constexpr int NV = decltype(nv)::value, TH = decltype(th)::value;
             if (sums)
                 layernorm_vjp_kernel<TT, VEC, NV, TH, true><<<parts, ln_threads<TH>(), 0, st>>>(
@@ -640,8 +695,9 @@ cudaError_t run_vjp(const void* g, const void* x, const void* gamma, int T, int 
 }  // namespace
 
 size_t layernorm_vjp_floats(int dtype, int T, int d) {
-    const int vec = vec_of(dtype, d);
-    const RowForm f = row_form(d, vec);
+    const RowForm f = dtype == 1   ? row_form<__nv_bfloat16, 8>(d)
+                      : d % 4 == 0 ? row_form<float, 4>(d)
+                                   : row_form<float, 1>(d);
     const size_t stats = f.nv == 0 ? 2 * static_cast<size_t>(T) : 0;
     const size_t parts = f.nv == 0 ? long_ranges(T) : vjp_blocks(T, f);
     return stats + parts * 2 * static_cast<size_t>(d);

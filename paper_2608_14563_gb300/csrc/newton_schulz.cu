@@ -32,7 +32,7 @@ namespace fpo {
 namespace {
 
 constexpr int kPassThreads = 256;
-constexpr int kNormBlocks = 128;  // per layer, at most
+constexpr int kNormBlocks = 304;  // per layer, at most: 2 on each of 152 SMs
 
 struct NsPtrs {
     const void* in[kMaxGroups];  // G, or U (fp32)
@@ -119,11 +119,14 @@ __global__ void __launch_bounds__(kPassThreads)
     const int layer = blockIdx.y;
     const size_t step = static_cast<size_t>(gridDim.x) * kPassThreads * 16;
     double acc = 0.0;
+    const TT* src = static_cast<const TT*>(p.in[layer]);
     for (size_t i = (blockIdx.x * static_cast<size_t>(kPassThreads) + threadIdx.x) * 16; i < n;
-         i += step) {
-        float v[16];
-        load16(static_cast<const TT*>(p.in[layer]), i, n, v);
-        acc += square_sum16(v);
+         i += 4 * step) {
+        float v[4][16];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) load16(src, i + q * step, n, v[q]);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) acc += square_sum16(v[q]);
     }
     const double t = block_sum_d(acc);
     if (threadIdx.x == 0) part[static_cast<size_t>(layer) * gridDim.x + blockIdx.x] = t;
@@ -168,7 +171,9 @@ __global__ void __launch_bounds__(kPassThreads)
     grid_dependency_trigger();
     grid_dependency_wait();
     const int layer = blockIdx.y;
-    double s = threadIdx.x < blocks ? part[static_cast<size_t>(layer) * blocks + threadIdx.x] : 0.0;
+    double s = 0.0;
+    for (int b = threadIdx.x; b < blocks; b += kPassThreads)
+        s += part[static_cast<size_t>(layer) * blocks + b];
     s = sqrt(block_sum_d(s));
     const float f = s <= 1.7e308 ? static_cast<float>(scale / fmax(s, eps)) : NAN;
     const TT* src = static_cast<const TT*>(p.in[layer]);
@@ -286,19 +291,25 @@ EncodeTiledFn encode_fn() {
     return fn;
 }
 
-// A batch [n][outer][inner] of fp16 matrices (row stride ld, matrix stride `stride` elements) as
-// a GEMM operand: K-major (inner = k: boxes of 64 k x 128 rows) or MN-major (64 columns x 64 k);
-// 128-byte swizzle, zeros outside each matrix.
-bool ns_map(CUtensorMap* m, const __half* base, int inner, int outer, int n, int ld, size_t stride,
-            bool mn) {
+// A batch [n][outer][inner] of fp16 matrices (row stride ld, matrix stride `stride` elements), the
+// high and (kSplit) low parts.
+struct NsOperand {
+    const __half* p[2];
+    int inner, outer, n, ld;
+    size_t stride;
+};
+
+// One part as a GEMM operand: K-major (inner = k: boxes of 64 k x `rows` rows) or MN-major (64
+// columns x 64 k); 128-byte swizzle, zeros outside each matrix.
+bool ns_map(CUtensorMap* m, const NsOperand& o, int part, bool mn, int rows) {
     const EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
-    cuuint64_t dims[3] = {static_cast<cuuint64_t>(inner), static_cast<cuuint64_t>(outer),
-                          static_cast<cuuint64_t>(n)};
-    cuuint64_t strides[2] = {static_cast<cuuint64_t>(ld) * 2, stride * 2};
-    cuuint32_t box[3] = {64, mn ? 64u : 128u, 1};
+    cuuint64_t dims[3] = {static_cast<cuuint64_t>(o.inner), static_cast<cuuint64_t>(o.outer),
+                          static_cast<cuuint64_t>(o.n)};
+    cuuint64_t strides[2] = {static_cast<cuuint64_t>(o.ld) * 2, o.stride * 2};
+    cuuint32_t box[3] = {64, mn ? 64u : static_cast<cuuint32_t>(rows), 1};
     cuuint32_t es[3] = {1, 1, 1};
-    return fn(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<__half*>(base), dims, strides, box, es,
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<__half*>(o.p[part]), dims, strides, box, es,
               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
               CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -324,12 +335,22 @@ int resident_clusters(int threads, int smem_bytes, int sm_count) {
     return n;
 }
 
-// One batch of GEMMs on the pair kernel.
-template <bool A_MN, bool B_MN, bool kSplit, class Epi>
-cudaError_t run_ns(const NsMaps& maps, const typename Epi::Params& ep, int M, int N, int K,
-                   int groups, bool tri, unsigned* status, cudaStream_t st) {
-    constexpr auto kern = ns_gemm_kernel<A_MN, B_MN, kSplit, Epi>;
-    cudaError_t e = set_smem_limit<kern>(NsSmem::kBytes);
+// One batch of GEMMs, C[M, N] = sum_k A B over K, on the pair kernel with 256 x BN tiles.
+template <int BN, bool A_MN, bool B_MN, bool kSplit, class Epi>
+cudaError_t run_ns_tiles(const NsOperand& A, const NsOperand& B, const typename Epi::Params& ep,
+                         int M, int N, int K, bool tri, unsigned* status, cudaStream_t st) {
+    using S = NsSmem<BN>;
+    NsMaps maps;
+    for (int h = 0; h < 2; ++h) {
+        if (h == 1 && !kSplit) {
+            maps.a[1] = maps.a[0];
+            maps.b[1] = maps.b[0];
+        } else if (!ns_map(&maps.a[h], A, h, A_MN, 128) || !ns_map(&maps.b[h], B, h, B_MN, BN / 2)) {
+            return cudaErrorInvalidValue;
+        }
+    }
+    constexpr auto kern = ns_gemm_kernel<BN, A_MN, B_MN, kSplit, Epi>;
+    cudaError_t e = set_smem_limit<kern>(S::kBytes);
     if (e != cudaSuccess) return e;
     DevInfo di;
     if (!current_device_info(&di)) return cudaErrorUnknown;
@@ -339,18 +360,46 @@ cudaError_t run_ns(const NsMaps& maps, const typename Epi::Params& ep, int M, in
     sh.g.N = N;
     sh.g.K = K;
     sh.g.m_blocks = (M + kPairBM - 1) / kPairBM;
-    sh.g.n_blocks = (N + kNsBN - 1) / kNsBN;
+    sh.g.n_blocks = (N + BN - 1) / BN;
     sh.g.k_blocks = (K + kBK - 1) / kBK;
-    sh.g.groups = groups;
+    sh.g.groups = A.n;
     sh.g.band = 16;
-    const long long per = tri ? static_cast<long long>(sh.g.m_blocks) * (sh.g.m_blocks + 1) / 2
-                              : static_cast<long long>(sh.g.m_blocks) * sh.g.n_blocks;
-    sh.g.tiles = groups * per;
-    const int max_clusters = resident_clusters<kern>(kNsThreads, NsSmem::kBytes, di.sm_count);
+    const long long per =
+        tri ? static_cast<long long>(sh.g.m_blocks) * (sh.g.m_blocks + 1) / 2 * (kPairBM / BN)
+            : static_cast<long long>(sh.g.m_blocks) * sh.g.n_blocks;
+    sh.g.tiles = A.n * per;
+    const int max_clusters = resident_clusters<kern>(kNsThreads, S::kBytes, di.sm_count);
     const long long clusters = sh.g.tiles < max_clusters ? sh.g.tiles : max_clusters;
-    return launch_chained(kern, dim3(static_cast<unsigned>(2 * clusters)), kNsThreads,
-                          NsSmem::kBytes, st, maps, ep, sh, status, wait_limit_ns());
+    return launch_chained(kern, dim3(static_cast<unsigned>(2 * clusters)), kNsThreads, S::kBytes, st,
+                          maps, ep, sh, status, wait_limit_ns());
 }
+
+// fp32 calls on 128-column tiles.  fp16 ones too where twice as many tiles still have a cluster
+// each: an epilogue is then half as long.
+template <bool A_MN, bool B_MN, bool kSplit, template <int> class Epi>
+cudaError_t run_ns(const NsOperand& A, const NsOperand& B, const typename Epi<128>::Params& ep, int M,
+                   int N, int K, bool tri, unsigned* status, cudaStream_t st) {
+    if constexpr (!kSplit) {
+        DevInfo di;
+        if (!current_device_info(&di)) return cudaErrorUnknown;
+        const long long mb = (M + 255) / 256, nb = (N + 255) / 256;
+        const long long tiles = A.n * (tri ? mb * (mb + 1) / 2 : mb * nb);
+        if (4 * tiles > di.sm_count)
+            return run_ns_tiles<256, A_MN, B_MN, kSplit, Epi<256>>(A, B, ep, M, N, K, tri, status, st);
+    }
+    return run_ns_tiles<128, A_MN, B_MN, kSplit, Epi<128>>(A, B, ep, M, N, K, tri, status, st);
+}
+
+template <bool kSplit>
+struct SymOf {
+    template <int BN>
+    using T = EpiSym<BN, kSplit>;
+};
+template <bool kSplit, int kOut>
+struct ApplyOf {
+    template <int BN>
+    using T = EpiApply<BN, kSplit, kOut>;
+};
 
 // Largest |c1 s + c3 s^3 + c5 s^5| (odd) on [0, u].
 double odd_max(double c1, double c3, double c5, double u) {
@@ -389,25 +438,13 @@ double quad_max(double b, double c, double t1) {
 // rounding adds to a bound stays far below the other half.
 int scale_exp(double bound) { return 15 - static_cast<int>(ceil(log2(bound))); }
 
+// X' = a X + B X (tall: a X + X B) and what becomes of it; ep holds the coefficients and targets.
 template <bool kSplit, int kOut>
-cudaError_t run_apply(bool tall, const NsLayout& L, uint8_t* ws, int cur, bool next_lo,
-                      typename EpiApply<kSplit, kOut>::Params& ep, int n, int rows, int cols,
+cudaError_t run_apply(const NsOperand& X, const NsOperand& B, bool tall, const NsLayout& L, uint8_t* ws,
+                      int cur, bool next_lo, typename EpiApplyBase<kSplit, kOut>::Params& ep,
                       unsigned* status, cudaStream_t st) {
-    NsMaps maps;
-    for (int h = 0; h < (kSplit ? 2 : 1); ++h) {
-        const __half* X = reinterpret_cast<const __half*>(ws + (h ? L.lo[cur] : L.hi[cur]));
-        const __half* B = reinterpret_cast<const __half*>(ws + L.B[h]);
-        CUtensorMap* mb = tall ? &maps.b[h] : &maps.a[h];
-        CUtensorMap* mx = tall ? &maps.a[h] : &maps.b[h];
-        if (!ns_map(mb, B, L.m, L.m, n, L.ldm, L.ms, false) ||
-            !ns_map(mx, X, cols, rows, n, L.ld, L.xs, !tall))
-            return cudaErrorInvalidValue;
-    }
-    if (!kSplit) {
-        maps.a[1] = maps.a[0];
-        maps.b[1] = maps.b[0];
-    }
-    ep.hi = reinterpret_cast<const __half*>(ws + L.hi[cur]);
+    const int rows = X.outer, cols = X.inner;
+    ep.hi = X.p[0];
     ep.lo = reinterpret_cast<__half*>(ws + L.lo[cur]);
     ep.x32 = kSplit ? reinterpret_cast<float*>(ws + L.x32) : nullptr;
     ep.next_hi = reinterpret_cast<__half*>(ws + L.hi[cur ^ 1]);
@@ -418,18 +455,20 @@ cudaError_t run_apply(bool tall, const NsLayout& L, uint8_t* ws, int cur, bool n
     ep.ld = L.ld;
     // wide: B X with B K-major and X MN-major; tall: X B, both K-major (B is symmetric)
     if (tall)
-        return run_ns<false, false, kSplit, EpiApply<kSplit, kOut>>(maps, ep, rows, cols, cols, n,
-                                                                    false, status, st);
-    return run_ns<false, true, kSplit, EpiApply<kSplit, kOut>>(maps, ep, rows, cols, rows, n, false,
-                                                               status, st);
+        return run_ns<false, false, kSplit, ApplyOf<kSplit, kOut>::template T>(X, B, ep, rows, cols,
+                                                                              cols, false, status, st);
+    return run_ns<false, true, kSplit, ApplyOf<kSplit, kOut>::template T>(B, X, ep, rows, cols, rows,
+                                                                         false, status, st);
 }
 
 // The iteration on the X_0 in the workspace.
 template <bool kSplit>
 cudaError_t run_steps(const NsLayout& L, uint8_t* ws, int n, int rows, int cols, int steps,
                       const float* coeffs, const NsTarget& to, unsigned* status, cudaStream_t st) {
-    constexpr int kParts = kSplit ? 2 : 1;
     const bool tall = rows > cols;
+    auto at = [&](size_t off) { return reinterpret_cast<__half*>(ws + off); };
+    const NsOperand A = {{at(L.A[0]), at(L.A[1])}, L.m, L.m, n, L.ldm, L.ms};
+    const NsOperand B = {{at(L.B[0]), at(L.B[1])}, L.m, L.m, n, L.ldm, L.ms};
     double u = 1.0;            // bound of the singular values of X_k
     int sx = scale_exp(u);     // X_k is stored times 2^sx
     int cur = 0;
@@ -438,41 +477,30 @@ cudaError_t run_steps(const NsLayout& L, uint8_t* ws, int n, int rows, int cols,
         const double ub = quad_max(b, c, u * u), un = odd_max(a, b, c, u);
         const int sa = scale_exp(u * u), sb = ub > 0.0 ? scale_exp(ub) : 0,
                   sn = un > 0.0 ? scale_exp(un) : 0;
+        const NsOperand X = {{at(L.hi[cur]), at(L.lo[cur])}, cols, rows, n, L.ld, L.xs};
 
-        typename EpiSym<kSplit>::Params sp = {};
+        // A = X X^T
+        typename EpiSymBase<kSplit>::Params sp = {};
         sp.stride = static_cast<long long>(L.ms);
         sp.M = L.m;
         sp.ld = L.ldm;
-        NsMaps maps;
-        // A = X X^T
-        for (int h = 0; h < kParts; ++h) {
-            const __half* X = reinterpret_cast<const __half*>(ws + (h ? L.lo[cur] : L.hi[cur]));
-            if (!ns_map(&maps.a[h], X, cols, rows, n, L.ld, L.xs, tall)) return cudaErrorInvalidValue;
-            sp.out[h] = reinterpret_cast<__half*>(ws + L.A[h]);
-        }
-        if (!kSplit) maps.a[1] = maps.a[0];
-        maps.b[0] = maps.a[0];
-        maps.b[1] = maps.a[1];
+        sp.out[0] = at(L.A[0]);
+        sp.out[1] = at(L.A[1]);
         sp.acc_coef = static_cast<float>(ldexp(1.0, sa - 2 * sx));
-        cudaError_t e =
-            tall ? run_ns<true, true, kSplit, EpiSym<kSplit>>(maps, sp, L.m, L.m, rows, n, true,
-                                                              status, st)
-                 : run_ns<false, false, kSplit, EpiSym<kSplit>>(maps, sp, L.m, L.m, cols, n, true,
-                                                                status, st);
+        cudaError_t e = tall ? run_ns<true, true, kSplit, SymOf<kSplit>::template T>(
+                                   X, X, sp, L.m, L.m, rows, true, status, st)
+                             : run_ns<false, false, kSplit, SymOf<kSplit>::template T>(
+                                   X, X, sp, L.m, L.m, cols, true, status, st);
         if (e != cudaSuccess) return e;
         // B = b A + c A^2
-        for (int h = 0; h < kParts; ++h) {
-            const __half* A = reinterpret_cast<const __half*>(ws + L.A[h]);
-            if (!ns_map(&maps.a[h], A, L.m, L.m, n, L.ldm, L.ms, false)) return cudaErrorInvalidValue;
-            sp.lin[h] = A;
-            sp.out[h] = reinterpret_cast<__half*>(ws + L.B[h]);
-        }
-        if (!kSplit) maps.a[1] = maps.a[0];
-        maps.b[0] = maps.a[0];
-        maps.b[1] = maps.a[1];
+        sp.lin[0] = at(L.A[0]);
+        sp.lin[1] = at(L.A[1]);
+        sp.out[0] = at(L.B[0]);
+        sp.out[1] = at(L.B[1]);
         sp.lin_coef = static_cast<float>(ldexp(b, sb - sa));
         sp.acc_coef = static_cast<float>(ldexp(c, sb - 2 * sa));
-        e = run_ns<false, false, kSplit, EpiSym<kSplit>>(maps, sp, L.m, L.m, L.m, n, true, status, st);
+        e = run_ns<false, false, kSplit, SymOf<kSplit>::template T>(A, A, sp, L.m, L.m, L.m, true,
+                                                                    status, st);
         if (e != cudaSuccess) return e;
         // X' = a X + B X.  The last step takes the linear term of fp16 calls from the operand
         // itself: nothing grows after it, and the same X in both terms is the smaller error.
@@ -484,27 +512,26 @@ cudaError_t run_steps(const NsLayout& L, uint8_t* ws, int n, int rows, int cols,
             ep.lin_lo = !last;
         };
         if (!last) {
-            typename EpiApply<kSplit, kNext>::Params ep = {};
+            typename EpiApplyBase<kSplit, kNext>::Params ep = {};
             coefs(ep);
-            e = run_apply<kSplit, kNext>(tall, L, ws, cur, kSplit || k + 2 < steps, ep, n, rows, cols,
-                                         status, st);
+            e = run_apply<kSplit, kNext>(X, B, tall, L, ws, cur, kSplit || k + 2 < steps, ep, status, st);
         } else if (to.W) {
-            typename EpiApply<kSplit, kWeight>::Params ep = {};
+            typename EpiApplyBase<kSplit, kWeight>::Params ep = {};
             coefs(ep);
             ep.keep = to.keep;
             ep.rate = to.rate;
             for (int l = 0; l < n; ++l) {
                 ep.W[l] = to.W[l];
-                ep.out[l] = to.out ? static_cast<typename EpiApply<kSplit, kWeight>::Out*>(to.out[l])
+                ep.out[l] = to.out ? static_cast<typename EpiApplyBase<kSplit, kWeight>::Out*>(to.out[l])
                                    : nullptr;
             }
-            e = run_apply<kSplit, kWeight>(tall, L, ws, cur, false, ep, n, rows, cols, status, st);
+            e = run_apply<kSplit, kWeight>(X, B, tall, L, ws, cur, false, ep, status, st);
         } else {
-            typename EpiApply<kSplit, kResult>::Params ep = {};
+            typename EpiApplyBase<kSplit, kResult>::Params ep = {};
             coefs(ep);
             for (int l = 0; l < n; ++l)
-                ep.out[l] = static_cast<typename EpiApply<kSplit, kResult>::Out*>(to.out[l]);
-            e = run_apply<kSplit, kResult>(tall, L, ws, cur, false, ep, n, rows, cols, status, st);
+                ep.out[l] = static_cast<typename EpiApplyBase<kSplit, kResult>::Out*>(to.out[l]);
+            e = run_apply<kSplit, kResult>(X, B, tall, L, ws, cur, false, ep, status, st);
         }
         if (e != cudaSuccess) return e;
         cur ^= 1;

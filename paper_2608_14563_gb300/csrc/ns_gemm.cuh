@@ -7,11 +7,11 @@
 //
 // The roles, barriers, bounded waits and teardown are those of tc_gemm_pair_kernel: a cluster
 // of two CTAs, a TMA producer in each, one MMA issuer in the leader, 8 epilogue warps in each,
-// 256 x 256 tiles.  A pipeline stage is four boxes of 128 rows x 64 k (16 KB each):
-//   fp16   the A boxes of two consecutive k-blocks, then the B boxes; a full barrier for
-//          each k-block
-//   kSplit A high, A low, B high, B low of one k-block (each operand the sum of two fp16
-//          matrices, 22 bits); one full barrier
+// 256 x BN tiles.  A pipeline stage is two A boxes of 128 rows x 64 k (16 KB each) and two B
+// boxes of BN / 2 rows:
+//   fp16   the boxes of two consecutive k-blocks; a full barrier for each k-block
+//   kSplit high and low parts of one k-block (each operand the sum of two fp16 matrices, 22
+//          bits); one full barrier
 //
 // A and A A are symmetric: their GEMMs visit the tiles on and under the diagonal only, and the
 // epilogue writes each tile a second time, turned over.
@@ -21,7 +21,9 @@
 // ten and more.  So an accumulator holds one 64-deep k-block only: the 8 MMAs with one low
 // operand first, while the sums (and what is truncated of them) are 2^-11 of the final size,
 // then the 4 high x high MMAs; the epilogue warps add it to sums in their registers, rounding
-// to nearest, while the next k-block fills the other accumulator.
+// to nearest, while the next k-block fills the other accumulator.  BN is 128 there: 64 sums per
+// thread of 8 warps (with 128, and 168 registers, the loop spilled and took 2.7 us a k-block,
+// three times its MMAs).
 #pragma once
 
 #include <cuda_bf16.h>
@@ -65,55 +67,62 @@ __host__ __device__ constexpr uint32_t idesc_f16_f32(int M, int N, bool a_mn, bo
     return idesc_bf16_f32(M, N, a_mn, b_mn) & ~((1u << 7) | (1u << 10));
 }
 
-constexpr int kNsBN = 256;
-constexpr int kNsStages = 3;
-constexpr int kNsBox = 128 * kBK * 2;         // bytes of one operand box
 constexpr int kNsWarps = 8;                   // epilogue warps
 constexpr int kNsThreads = 64 + 32 * kNsWarps;
-constexpr int kNsWarpCols = kNsBN / 2;        // columns of one epilogue warp
 
+template <int BN>
 struct NsSmem {
-    static constexpr int kStageBytes = 4 * kNsBox;
-    static constexpr int kOutOffset = kNsStages * kStageBytes;
+    static constexpr int kStages = BN == 256 ? 3 : 4;
+    static constexpr int kABox = 128 * kBK * 2;        // bytes of one operand box
+    static constexpr int kBBox = (BN / 2) * kBK * 2;
+    static constexpr int kStageBytes = 2 * (kABox + kBBox);
+    static constexpr int kOutOffset = kStages * kStageBytes;
     static constexpr int kBarOffset = kOutOffset + kNsWarps * kOutBufBytes;
-    static constexpr int kNumBars = 3 * kNsStages + 5;
+    static constexpr int kNumBars = 3 * kStages + 5;
     static constexpr int kMiscOffset = kBarOffset + kNumBars * 8;
     static constexpr int kBytes = kMiscOffset + 16 + 1024;
 };
 
 struct NsShape {
     GemmShape g;   // M, N, K, blocks; tiles of all matrices
-    bool tri;      // tiles on and under the diagonal only (M = N)
+    bool tri;      // only tiles that reach under or onto the diagonal (M = N)
 };
 
 struct NsMaps {
     CUtensorMap a[2], b[2];  // high and low parts (low: kSplit only)
 };
 
+// Tile t: matrix g, block row mb of 256, block column nb of BN.  tri: block row mb has the
+// columns up to its own last one, (mb + 1) 256 / BN blocks (those past the matrix, in the last
+// block row, are empty).
+template <int BN>
 __device__ __forceinline__ void ns_tile(long long t, const NsShape& sh, int& g, int& mb, int& nb) {
     if (!sh.tri) {
         tile_coords(t, sh.g, g, mb, nb);
         return;
     }
+    constexpr int kRatio = kPairBM / BN;
     const int n = sh.g.m_blocks;
-    const int per = n * (n + 1) / 2;
+    const int per = kRatio * (n * (n + 1) / 2);
     g = static_cast<int>(t / per);
     const int r = static_cast<int>(t - static_cast<long long>(g) * per);
-    mb = static_cast<int>((sqrtf(8.f * r + 1.f) - 1.f) * 0.5f);
-    while (mb * (mb + 1) / 2 > r) --mb;
-    while ((mb + 1) * (mb + 2) / 2 <= r) ++mb;
-    nb = r - mb * (mb + 1) / 2;
+    const int q = r / kRatio;  // of the 256 x 256 blocks
+    mb = static_cast<int>((sqrtf(8.f * q + 1.f) - 1.f) * 0.5f);
+    while (mb * (mb + 1) / 2 > q) --mb;
+    while ((mb + 1) * (mb + 2) / 2 <= q) ++mb;
+    nb = r - kRatio * (mb * (mb + 1) / 2);
 }
 
-// One CTA's box (128 rows x 64 k, or turned) of matrix z, counted on the leader's barrier.
-template <bool MN>
+// One CTA's box (ROWS rows x 64 k, or turned) of matrix z, counted on the leader's barrier.
+template <bool MN, int ROWS>
 __device__ __forceinline__ void ns_load(const CUtensorMap* map, uint32_t dst, uint32_t bar, int row0,
                                         int k0, int z) {
     if constexpr (!MN) {
         tma_load_3d_pair(map, dst, bar, k0, row0, z);
     } else {
-        tma_load_3d_pair(map, dst, bar, row0, k0, z);
-        tma_load_3d_pair(map, dst + kNsBox / 2, bar, row0 + 64, k0, z);
+#pragma unroll
+        for (int i = 0; i < ROWS / 64; ++i)
+            tma_load_3d_pair(map, dst + i * (64 * kBK * 2), bar, row0 + 64 * i, k0, z);
     }
 }
 
@@ -131,7 +140,7 @@ __device__ __forceinline__ float2 unpack_f16x2(uint32_t w) {
 // the row layout of the accumulator; both are [M, ld], ld a multiple of 8, the columns from M to
 // ld zero.
 template <bool kSplit>
-struct EpiSym {
+struct EpiSymBase {
     struct Params {
         const __half* lin[2];  // high, low parts of L, or null
         __half* out[2];
@@ -139,7 +148,13 @@ struct EpiSym {
         int M, ld;
         float lin_coef, acc_coef;
     };
+};
+
+template <int BN, bool kSplit>
+struct EpiSym : EpiSymBase<kSplit> {
+    using Params = typename EpiSymBase<kSplit>::Params;
     static constexpr int kParts = kSplit ? 2 : 1;
+    static constexpr int kChunks = BN / 2 / 32;
 
     const Params& p;
     long long base;
@@ -185,7 +200,7 @@ struct EpiSym {
                     }
                 }
             }
-            if (c + 1 < kNsWarpCols / 32) fetch(c + 1);
+            if (c + 1 < kChunks) fetch(c + 1);
         }
         if (row >= p.M) return;
         const int cc = col0 + 32 * c;
@@ -234,7 +249,7 @@ struct EpiSym {
 enum NsOut { kNext = 0, kResult = 1, kWeight = 2 };
 
 template <bool kSplit, int kOut>
-struct EpiApply {
+struct EpiApplyBase {
     using Out = std::conditional_t<kSplit, float, __nv_bfloat16>;
     struct Params {
         const __half* hi;     // X (fp16)
@@ -250,6 +265,13 @@ struct EpiApply {
         Out* out[kMaxGroups];          // kResult: O; kWeight: W_out or null
         float* W[kMaxGroups];          // kWeight
     };
+};
+
+template <int BN, bool kSplit, int kOut>
+struct EpiApply : EpiApplyBase<kSplit, kOut> {
+    using Out = typename EpiApplyBase<kSplit, kOut>::Out;
+    using Params = typename EpiApplyBase<kSplit, kOut>::Params;
+    static constexpr int kChunks = BN / 2 / 32;
     static constexpr int kAcc = 8;     // accesses of a chunk: 4 rows, 8 lanes of 4 columns to a row
 
     const Params& p;
@@ -368,20 +390,21 @@ struct EpiApply {
                 }
             }
         }
-        if (c + 1 < kNsWarpCols / 32) fetch(c + 1);
+        if (c + 1 < kChunks) fetch(c + 1);
         __syncwarp();
     }
 };
 
 // ---------------------------------------------------------------------------
-template <bool A_MN, bool B_MN, bool kSplit, class Epi>
+template <int BN, bool A_MN, bool B_MN, bool kSplit, class Epi>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
     ns_gemm_kernel(const __grid_constant__ NsMaps maps,
                    const __grid_constant__ typename Epi::Params ep, const NsShape sh,
                    unsigned int* status, unsigned long long wait_limit_ns) {
-    using L = NsSmem;
+    using L = NsSmem<BN>;
+    constexpr int kStages = L::kStages;
     constexpr int kSub = kSplit ? 1 : 2;   // k-blocks (and full barriers) per stage
-    constexpr uint32_t kIdesc = idesc_f16_f32(kPairBM, kNsBN, A_MN, B_MN);
+    constexpr uint32_t kIdesc = idesc_f16_f32(kPairBM, BN, A_MN, B_MN);
     constexpr uint16_t kBoth = 0x3;
 
     extern __shared__ uint8_t smem_raw[];
@@ -397,12 +420,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
     const int stages_k = (sh.g.k_blocks + kSub - 1) / kSub;  // stages per tile
 
     const uint32_t bar0 = sbase + L::kBarOffset;
-    constexpr int kFull = kNsStages * kSub;
+    constexpr int kFull = kStages * kSub;
     auto full_bar = [&](int s, int j) { return bar0 + 8u * (s * kSub + j); };
     auto empty_bar = [&](int s) { return bar0 + 8u * (kFull + s); };
-    auto tfull_bar = [&](int a) { return bar0 + 8u * (kFull + kNsStages + a); };
-    auto tempty_bar = [&](int a) { return bar0 + 8u * (kFull + kNsStages + 2 + a); };
-    const uint32_t drain_bar = bar0 + 8u * (kFull + kNsStages + 4);
+    auto tfull_bar = [&](int a) { return bar0 + 8u * (kFull + kStages + a); };
+    auto tempty_bar = [&](int a) { return bar0 + 8u * (kFull + kStages + 2 + a); };
+    const uint32_t drain_bar = bar0 + 8u * (kFull + kStages + 4);
     uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(smem + L::kMiscOffset + kMiscTmem);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + L::kMiscOffset + kMiscAbort);
     uint32_t* issued_word = reinterpret_cast<uint32_t*>(smem + L::kMiscOffset + kMiscIssued);
@@ -411,7 +434,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
     const int lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kNsStages; ++s) {
+        for (int s = 0; s < kStages; ++s) {
             for (int j = 0; j < kSub; ++j) mbar_init(full_bar(s, j), 1);
             mbar_init(empty_bar(s), 1);
         }
@@ -427,7 +450,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
         tma_prefetch_desc(&maps.b[0]);
     }
     if (warp == 1) {
-        tmem_alloc_pair<512>(smem_u32(tmem_holder));
+        tmem_alloc_pair<2 * BN>(smem_u32(tmem_holder));
         tmem_relinquish_pair();
     }
     tc_fence_before();
@@ -447,12 +470,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
             bool ok = true;
             for (long long t = cluster; ok && t < sh.g.tiles; t += n_clusters) {
                 int g, mb, nb;
-                ns_tile(t, sh, g, mb, nb);
+                ns_tile<BN>(t, sh, g, mb, nb);
                 const int a_row = mb * kPairBM + 128 * static_cast<int>(rank);
-                const int b_row = nb * kNsBN + 128 * static_cast<int>(rank);
+                const int b_row = nb * BN + (BN / 2) * static_cast<int>(rank);
                 for (int kb = 0; kb < stages_k; ++kb) {
                     if (!mbar_wait_cl(empty_bar(stage), phase ^ 1u, guard)) { ok = false; break; }
-                    const uint32_t sa = sbase + stage * L::kStageBytes, sb = sa + 2 * kNsBox;
+                    const uint32_t sa = sbase + stage * L::kStageBytes, sb = sa + 2 * L::kABox;
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
                         const int bar_j = kSplit ? 0 : j, part = kSplit ? j : 0;
@@ -461,11 +484,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
                             mbar_arrive_expect_tx(full_bar(stage, bar_j),
                                                   2 * (L::kStageBytes / kSub));
                         const int k0 = (kSplit ? kb : 2 * kb + j) * kBK;
-                        ns_load<A_MN>(&maps.a[part], sa + j * kNsBox, fb, a_row, k0, g);
-                        ns_load<B_MN>(&maps.b[part], sb + j * kNsBox, fb, b_row, k0, g);
+                        ns_load<A_MN, 128>(&maps.a[part], sa + j * L::kABox, fb, a_row, k0, g);
+                        ns_load<B_MN, BN / 2>(&maps.b[part], sb + j * L::kBBox, fb, b_row, k0, g);
                     }
                     ++issued;
-                    if (++stage == kNsStages) { stage = 0; phase ^= 1u; }
+                    if (++stage == kStages) { stage = 0; phase ^= 1u; }
                 }
             }
             *issued_word = issued;
@@ -487,8 +510,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
                         }
                         tc_fence_after();
                     }
-                    const uint32_t d_tmem = tmem_base + static_cast<uint32_t>(acc * kNsBN);
-                    const uint32_t sa = sbase + stage * L::kStageBytes, sb = sa + 2 * kNsBox;
+                    const uint32_t d_tmem = tmem_base + static_cast<uint32_t>(acc * BN);
+                    const uint32_t sa = sbase + stage * L::kStageBytes, sb = sa + 2 * L::kABox;
                     if constexpr (kSplit) {
                         if (!mbar_wait_cl_poll(full_bar(stage, 0), phase, guard)) { ok = false; break; }
                         tc_fence_after();
@@ -498,8 +521,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
 #pragma unroll
                             for (int kk = 0; kk < kBK / kUmmaK; ++kk)
                                 tc_mma_bf16_pair(
-                                    d_tmem, operand_desc<A_MN>(sa + (m == 1 ? kNsBox : 0), kk),
-                                    operand_desc<B_MN>(sb + (m == 0 ? kNsBox : 0), kk), kIdesc,
+                                    d_tmem, operand_desc<A_MN>(sa + (m == 1 ? L::kABox : 0), kk),
+                                    operand_desc<B_MN>(sb + (m == 0 ? L::kBBox : 0), kk), kIdesc,
                                     (m != 0 || kk != 0) ? 1u : 0u);
                         }
                     } else {
@@ -509,8 +532,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
                             tc_fence_after();
 #pragma unroll
                             for (int kk = 0; kk < kBK / kUmmaK; ++kk)
-                                tc_mma_bf16_pair(d_tmem, operand_desc<A_MN>(sa + j * kNsBox, kk),
-                                                 operand_desc<B_MN>(sb + j * kNsBox, kk), kIdesc,
+                                tc_mma_bf16_pair(d_tmem, operand_desc<A_MN>(sa + j * L::kABox, kk),
+                                                 operand_desc<B_MN>(sb + j * L::kBBox, kk), kIdesc,
                                                  (kb != 0 || j != 0 || kk != 0) ? 1u : 0u);
                             issued_any = true;
                         }
@@ -518,7 +541,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
                     }
                     issued_any = true;
                     tc_commit_pair_multicast(empty_bar(stage), kBoth);
-                    if (++stage == kNsStages) { stage = 0; phase ^= 1u; }
+                    if (++stage == kStages) { stage = 0; phase ^= 1u; }
                     if (kSplit || kb == stages_k - 1) {
                         tc_commit_pair_multicast(tfull_bar(acc), kBoth);
                         if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
@@ -534,7 +557,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
     } else {
         // ------------------------------------------------------- epilogue (both CTAs)
         const int q = warp & 3;               // TMEM lanes [32 q, 32 q + 32)
-        const int half = (warp - 2) / 4;      // columns [128 half, 128 half + 128)
+        const int half = (warp - 2) / 4;
+        constexpr int kWarpCols = BN / 2;     // columns [kWarpCols half, kWarpCols (half + 1))
         const uint32_t buf = sbase + L::kOutOffset + static_cast<uint32_t>(warp - 2) * kOutBufBytes;
         int acc = 0;
         uint32_t acc_phase = 0;
@@ -556,15 +580,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
         };
         auto t_row = [&] {
             return tmem_base + (static_cast<uint32_t>(q * 32) << 16) +
-                   static_cast<uint32_t>(acc * kNsBN + half * kNsWarpCols);
+                   static_cast<uint32_t>(acc * BN + half * kWarpCols);
         };
-        constexpr int kChunks = kNsWarpCols / 32;
+        constexpr int kChunks = kWarpCols / 32;
         bool ok = true;
         for (long long t = cluster; ok && t < sh.g.tiles; t += n_clusters) {
             int g, mb, nb;
-            ns_tile(t, sh, g, mb, nb);
+            ns_tile<BN>(t, sh, g, mb, nb);
             const int row0 = mb * kPairBM + 128 * static_cast<int>(rank) + 32 * q;
-            const int col0 = nb * kNsBN + half * kNsWarpCols;
+            const int col0 = nb * BN + half * kWarpCols;
+            const bool mirror = sh.tri && nb * BN / kPairBM != mb;
             if constexpr (kSplit) {
                 float s[kChunks][32];
 #pragma unroll
@@ -584,12 +609,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
                     release();
                 }
                 if (!ok) break;
-                Epi epi(ep, g, row0, col0, lane, sh.tri && mb != nb);
+                Epi epi(ep, g, row0, col0, lane, mirror);
 #pragma unroll
                 for (int c = 0; c < kChunks; ++c) epi.chunk(s[c], buf, lane, c);
                 __syncwarp();
             } else {
-                Epi epi(ep, g, row0, col0, lane, sh.tri && mb != nb);
+                Epi epi(ep, g, row0, col0, lane, mirror);
                 ok = ready();
                 if (!ok) break;
                 const uint32_t tr = t_row();
@@ -611,14 +636,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
     __syncthreads();
     cluster_sync();
     if (leader && threadIdx.x == 0)
-        pair_drain_copies<kNsStages, kSub>(bar0, *issued_word,
+        pair_drain_copies<kStages, kSub>(bar0, *issued_word,
                                            ld_shared_cluster_u32(mapa_shared(smem_u32(issued_word), 1)),
                                            L::kStageBytes / kSub);
     __syncthreads();
     cluster_sync();
     if (warp == 1) {
         tc_fence_after();
-        tmem_dealloc_pair<512>(tmem_base);
+        tmem_dealloc_pair<2 * BN>(tmem_base);
     }
 }
 
