@@ -465,16 +465,16 @@ typedef struct fpo_muon_desc {
 } fpo_muon_desc;
 
 /* Bytes of workspace fpo_layer_muon_grouped needs (0 on invalid sizes): that of
- * fpo_orthogonalize_grouped and 4 d d_ff bytes per layer. */
+ * fpo_orthogonalize_grouped and a little more than 4 d d_ff bytes per layer. */
 size_t fpo_layer_muon_workspace(int32_t n_layers, int64_t d, int64_t d_ff, int32_t dtype);
 
 /*
  * fpo_layer_muon_grouped -- the pseudogradient of every target layer (Eq. (w3update), as in
  * fpo_layer_update_grouped_signals) followed by a Muon step on its fp32 master, a third
  * optimizer beside those of fpo_layer_optimize_grouped:
- *   G_l = g[l]^T A[l]                                   fp32, in the workspace
+ *   G_l = g[l]^T A[l]                                   fp32 accumulation
  *   momentum_l <- mu momentum_l + G_l
- *   U_l = G_l + mu momentum_l (nesterov) or momentum_l
+ *   U_l = G_l + mu momentum_l (nesterov) or momentum_l  fp32, in the workspace
  *   O_l = orthogonalised U_l (fpo_orthogonalize_grouped)
  *   W_master,l <- (1 - lr weight_decay) W_master,l - lr scale O_l;  W_out,l = W_master,l
  *                                                       rounded to dtype

@@ -701,7 +701,7 @@ int32_t fpo_orthogonalize_grouped(int32_t n_layers, int64_t rows, int64_t cols, 
     if (rc != FPO_OK) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     unsigned* status = static_cast<unsigned*>(workspace);
-    FPO_TRY(cudaMemsetAsync(status, 0, sizeof(unsigned), st));
+    FPO_TRY(cudaMemsetAsync(status, 0, 2 * sizeof(unsigned), st));  // and the phase counter
     const NsTarget to{O, nullptr, 0.f, 0.f};
     return cuda_status(launch_newton_schulz(n_layers, static_cast<int>(rows), static_cast<int>(cols),
                                             dtype, G, nullptr, eps, steps, co, to, workspace, status,
@@ -745,9 +745,10 @@ int32_t fpo_layer_muon_grouped(int32_t n_layers, int64_t T, int64_t d, int64_t d
     if (rc != FPO_OK) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     unsigned* status = static_cast<unsigned*>(workspace);
-    FPO_TRY(cudaMemsetAsync(status, 0, sizeof(unsigned), st));
+    FPO_TRY(cudaMemsetAsync(status, 0, 2 * sizeof(unsigned), st));  // and the phase counter
     const int Ti = static_cast<int>(T), di = static_cast<int>(d), fi = static_cast<int>(d_ff);
-    // G_l = g_l^T A_l (fp32)
+    // G_l = g_l^T A_l: with the momentum for bf16, else (fp32) into the update buffers
+    NsMomentum mom{momentum, opt->momentum, opt->nesterov != 0, nullptr, nullptr, Ti};
     float* G[FPO_MAX_GROUPED_LAYERS];
     for (int l = 0; l < n_layers; ++l)
         G[l] = ns_update_buffer(workspace, n_layers, di, fi, dtype, l);
@@ -755,17 +756,14 @@ int32_t fpo_layer_muon_grouped(int32_t n_layers, int64_t T, int64_t d, int64_t d
         FPO_TRY(cudaMemsetAsync(G[0], 0, static_cast<size_t>(G[n_layers - 1] - G[0]) * 4 +
                                              static_cast<size_t>(d) * d_ff * 4, st));
     } else if (dtype == FPO_BF16) {
-        FPO_TRY(launch_grad_bf16(n_layers, Ti, di, fi, g, A, G, nullptr,
-                                 reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) +
-                                                          kStatusBytes),
-                                 status, st));
+        mom.g = g;
+        mom.A = A;
     } else {
         FPO_TRY(launch_update_f32(n_layers, Ti, di, fi, reinterpret_cast<const float* const*>(g),
                                   reinterpret_cast<const float* const*>(A), 0.f, nullptr, nullptr, G,
                                   st));
     }
     // momentum, orthogonalisation, W <- (1 - lr wd) W - lr scale O
-    const NsMomentum mom{momentum, opt->momentum, opt->nesterov != 0};
     const NsTarget to{W_out, W_master, 1.f - opt->lr * opt->weight_decay, opt->lr * opt->scale};
     return cuda_status(launch_newton_schulz(n_layers, di, fi, dtype, nullptr, &mom, opt->eps,
                                             opt->steps, co, to, workspace, status, st));

@@ -284,12 +284,16 @@ cudaError_t launch_layernorm_vjp(int dtype, const void* g, const void* x, const 
                                  float* dbeta, float* ws, cudaStream_t st);
 
 // ------------------------------------------------------------ Newton-Schulz (newton_schulz.cu)
-// Momentum in front of the iteration: M <- mu M + G, U = G + mu M (nesterov) or M, with G in
-// ns_update_buffer() (fp32, one per layer), which U replaces.
+// Momentum in front of the iteration: M <- mu M + G, U = G + mu M (nesterov) or M.  G = g[l]^T A[l]
+// (bf16, T > 0 tokens), or with g null in ns_update_buffer() (fp32, one per layer), which U
+// replaces.
 struct NsMomentum {
     float* const* M;
     float mu;
     bool nesterov;
+    const void* const* g;
+    const void* const* A;
+    int T;
 };
 // What becomes of the result: out[l] = O in dtype, or with W set W[l] <- keep W[l] - rate O and
 // out[l] (out or its entry may be null) = W[l] in dtype.
@@ -305,7 +309,7 @@ float* ns_update_buffer(void* ws, int n, int rows, int cols, int dtype, int laye
 // n matrices [rows, cols] (G in dtype, or mom) through `steps` iterations.  dtype 0 = fp32,
 // 1 = bf16 (cols a multiple of 8).
 cudaError_t launch_newton_schulz(int n, int rows, int cols, int dtype, const void* const* G,
-                                 const NsMomentum* mom, double eps, int steps, const float* coeffs,
+                                 const NsMomentum* mom, float eps, int steps, const float* coeffs,
                                  const NsTarget& to, void* workspace, unsigned* status,
                                  cudaStream_t st);
 

@@ -97,6 +97,7 @@ struct RowSum {
 #pragma unroll
                 for (int k = 0; k < N; ++k) (*sh)[at][k][w] = v[k];
             }
+            __syncwarp();
             // the row group's own barrier (0 is __syncthreads)
             asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(32 * W) : "memory");
 #pragma unroll

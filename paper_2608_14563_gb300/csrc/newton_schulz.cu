@@ -58,6 +58,10 @@ __device__ __forceinline__ double square_sum16(const float (&v)[16]) {
 #pragma unroll
     for (int k = 0; k < 16; ++k) s = fmaf(v[k], v[k], s);
     if (s >= 1e-30f && s <= 3e38f) return s;
+    uint32_t any = 0;  // zeros are frequent, and need no fp64
+#pragma unroll
+    for (int k = 0; k < 16; ++k) any |= __float_as_uint(v[k]) << 1;
+    if (any == 0) return 0.0;
     double d = 0.0;
 #pragma unroll
     for (int k = 0; k < 16; ++k) d += static_cast<double>(v[k]) * v[k];
@@ -107,6 +111,20 @@ __device__ __forceinline__ void store16(float* p, size_t i, size_t n, const floa
 #pragma unroll
         for (int k = 0; k < 16; ++k)
             if (i + k < n) p[i + k] = v[k];
+    }
+}
+
+__device__ __forceinline__ void store16(__nv_bfloat16* p, size_t i, size_t n, const float (&v)[16]) {
+    if (i + 16 <= n) {
+        uint32_t w[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[k] = pack_bf16x2(v[2 * k], v[2 * k + 1]);
+        reinterpret_cast<uint4*>(p + i)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        reinterpret_cast<uint4*>(p + i)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 16; ++k)
+            if (i + k < n) p[i + k] = __float2bfloat16_rn(v[k]);
     }
 }
 
@@ -160,13 +178,77 @@ __global__ void __launch_bounds__(kPassThreads)
     if (threadIdx.x == 0) part[static_cast<size_t>(layer) * gridDim.x + blockIdx.x] = t;
 }
 
+// W <- keep W - rate O, and out (or null) = W in the call's type.  A pass of its own: 12 to 18 bytes
+// an element.
+struct NsWeights {
+    const float* O[kMaxGroups];
+    float* W[kMaxGroups];
+    void* out[kMaxGroups];
+};
+
+template <typename TT>
+__global__ void __launch_bounds__(kPassThreads)
+    ns_weight_kernel(const __grid_constant__ NsWeights p, size_t n, float keep, float rate) {
+    grid_dependency_trigger();
+    grid_dependency_wait();
+    const int layer = blockIdx.y;
+    const float* O = p.O[layer];
+    float* W = p.W[layer];
+    TT* out = static_cast<TT*>(p.out[layer]);
+    const size_t step = static_cast<size_t>(gridDim.x) * kPassThreads * 16;
+    for (size_t i = (blockIdx.x * static_cast<size_t>(kPassThreads) + threadIdx.x) * 16; i < n;
+         i += step) {
+        float v[16], w[16];
+        load16(O, i, n, v);
+        load16(W, i, n, w);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) w[k] = fmaf(-rate, v[k], keep * w[k]);
+        store16(W, i, n, w);
+        if (out) store16(out, i, n, w);
+    }
+}
+
+// sum[layer] of the layer's `blocks` partial sums, in a fixed order.
+constexpr int kSumThreads = 1024;
+__global__ void __launch_bounds__(kSumThreads)
+    ns_sum_kernel(const double* part, int blocks, double* sum) {
+    __shared__ double sh[kSumThreads / 32];
+    grid_dependency_trigger();
+    grid_dependency_wait();
+    const double* p = part + static_cast<size_t>(blockIdx.x) * blocks;
+    double x = 0.0;
+    for (int b = threadIdx.x; b < blocks; b += kSumThreads) x += p[b];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = x;
+    __syncthreads();
+    if (threadIdx.x >= 32) return;
+    x = sh[threadIdx.x];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    if (threadIdx.x == 0) sum[blockIdx.x] = x;
+}
+
+// scale / max(sqrt(s), eps) in fp32 arithmetic (fp64 roots and quotients take microseconds here);
+// NaN if s is not finite.
+__device__ __forceinline__ float norm_factor(double s, float scale, float eps) {
+    const long long bits = __double_as_longlong(s);
+    const int e = static_cast<int>((bits >> 52) & 0x7ff) - 1023;  // s = m 2^e
+    if (e == 1024) return NAN;
+    if (e == -1023) return scale / eps;  // zero
+    const int h = e >> 1;  // s = (m 2^(e - 2 h)) 4^h, the bracket in [1, 4)
+    const float r = sqrtf(static_cast<float>(__longlong_as_double(
+        (bits & 0x000fffffffffffffll) | (static_cast<long long>(1023 + e - 2 * h) << 52))));
+    return ldexpf(r, h) < eps ? scale / eps : ldexpf(scale / r, -h);
+}
+
 // X_0, scaled: fp16 high and low parts (kSplit: and the fp32 value), rows padded from cols to
 // ld with zeros.  Thread: 8 columns of a row.  The layer's norm from its `blocks` partial sums.
 // A layer with a non-finite norm (a NaN, an infinity) becomes NaN as a whole.
 template <typename TT, bool kSplit>
 __global__ void __launch_bounds__(kPassThreads)
     ns_cast_kernel(const __grid_constant__ NsPtrs p, int rows, int cols, int ld, const double* part,
-                   int blocks, double eps, double scale, __half* hi, __half* lo, float* x32,
+                   int blocks, float eps, float scale, __half* hi, __half* lo, float* x32,
                    size_t stride) {
     grid_dependency_trigger();
     grid_dependency_wait();
@@ -174,8 +256,7 @@ __global__ void __launch_bounds__(kPassThreads)
     double s = 0.0;
     for (int b = threadIdx.x; b < blocks; b += kPassThreads)
         s += part[static_cast<size_t>(layer) * blocks + b];
-    s = sqrt(block_sum_d(s));
-    const float f = s <= 1.7e308 ? static_cast<float>(scale / fmax(s, eps)) : NAN;
+    const float f = norm_factor(block_sum_d(s), scale, eps);
     const TT* src = static_cast<const TT*>(p.in[layer]);
     const int per = ld / 8;
     const bool vec = cols % 8 == 0;  // rows then start on 16 bytes
@@ -235,11 +316,19 @@ int norm_blocks(size_t n) {
     return static_cast<int>(b < kNormBlocks ? b : kNormBlocks);
 }
 
+// Partial sums of squares of one layer: a block's of the norm pass, or a warp's of a tile of the
+// gradient's GEMM (of at most 256 x 128).
+size_t norm_parts(int rows, int cols, bool muon) {
+    const size_t tiles = static_cast<size_t>((rows + 255) / 256) * ((cols + 127) / 128);
+    const size_t slots = muon ? tiles * 2 * kNsWarps : 0;
+    return slots > kNormBlocks ? slots : kNormBlocks;
+}
+
 // Byte offsets of the workspace behind the status word's 256 bytes.
 struct NsLayout {
     int m, ld, ldm;              // the smaller side, row strides of X and of A, B
     size_t xs, ms;               // elements of one layer's X, A
-    size_t part, U, u_stride, hi[2], lo[2], x32, A[2], B[2], total;
+    size_t part, sum, U, u_stride, hi[2], lo[2], x32, A[2], B[2], total;
 };
 
 NsLayout ns_layout(int n, int rows, int cols, bool split, bool muon) {
@@ -257,7 +346,8 @@ NsLayout ns_layout(int n, int rows, int cols, bool split, bool muon) {
         return o;
     };
     const size_t x = n * L.xs * 2, a = n * L.ms * 2;
-    L.part = take(static_cast<size_t>(n) * kNormBlocks * sizeof(double));
+    L.part = take(static_cast<size_t>(n) * norm_parts(rows, cols, muon) * sizeof(double));
+    L.sum = take(static_cast<size_t>(n) * sizeof(double));
     L.U = muon ? take(n * L.u_stride * 4) : 0;
     L.hi[0] = take(x);
     L.hi[1] = take(x);
@@ -301,7 +391,8 @@ struct NsOperand {
 
 // One part as a GEMM operand: K-major (inner = k: boxes of 64 k x `rows` rows) or MN-major (64
 // columns x 64 k); 128-byte swizzle, zeros outside each matrix.
-bool ns_map(CUtensorMap* m, const NsOperand& o, int part, bool mn, int rows) {
+bool ns_map(CUtensorMap* m, const NsOperand& o, int part, bool mn, int rows,
+            CUtensorMapDataType type = CU_TENSOR_MAP_DATA_TYPE_FLOAT16) {
     const EncodeTiledFn fn = encode_fn();
     if (!fn) return false;
     cuuint64_t dims[3] = {static_cast<cuuint64_t>(o.inner), static_cast<cuuint64_t>(o.outer),
@@ -309,7 +400,7 @@ bool ns_map(CUtensorMap* m, const NsOperand& o, int part, bool mn, int rows) {
     cuuint64_t strides[2] = {static_cast<cuuint64_t>(o.ld) * 2, o.stride * 2};
     cuuint32_t box[3] = {64, mn ? 64u : static_cast<cuuint32_t>(rows), 1};
     cuuint32_t es[3] = {1, 1, 1};
-    return fn(m, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<__half*>(o.p[part]), dims, strides, box, es,
+    return fn(m, type, 3, const_cast<__half*>(o.p[part]), dims, strides, box, es,
               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
               CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -335,20 +426,10 @@ int resident_clusters(int threads, int smem_bytes, int sm_count) {
     return n;
 }
 
-// One batch of GEMMs, C[M, N] = sum_k A B over K, on the pair kernel with 256 x BN tiles.
 template <int BN, bool A_MN, bool B_MN, bool kSplit, class Epi>
-cudaError_t run_ns_tiles(const NsOperand& A, const NsOperand& B, const typename Epi::Params& ep,
-                         int M, int N, int K, bool tri, unsigned* status, cudaStream_t st) {
+cudaError_t launch_ns(const typename Epi::Maps& maps, const typename Epi::Params& ep, int M, int N,
+                      int K, int groups, bool tri, unsigned* status, cudaStream_t st) {
     using S = NsSmem<BN>;
-    NsMaps maps;
-    for (int h = 0; h < 2; ++h) {
-        if (h == 1 && !kSplit) {
-            maps.a[1] = maps.a[0];
-            maps.b[1] = maps.b[0];
-        } else if (!ns_map(&maps.a[h], A, h, A_MN, 128) || !ns_map(&maps.b[h], B, h, B_MN, BN / 2)) {
-            return cudaErrorInvalidValue;
-        }
-    }
     constexpr auto kern = ns_gemm_kernel<BN, A_MN, B_MN, kSplit, Epi>;
     cudaError_t e = set_smem_limit<kern>(S::kBytes);
     if (e != cudaSuccess) return e;
@@ -362,16 +443,32 @@ cudaError_t run_ns_tiles(const NsOperand& A, const NsOperand& B, const typename 
     sh.g.m_blocks = (M + kPairBM - 1) / kPairBM;
     sh.g.n_blocks = (N + BN - 1) / BN;
     sh.g.k_blocks = (K + kBK - 1) / kBK;
-    sh.g.groups = A.n;
+    sh.g.groups = groups;
     sh.g.band = 16;
     const long long per =
         tri ? static_cast<long long>(sh.g.m_blocks) * (sh.g.m_blocks + 1) / 2 * (kPairBM / BN)
             : static_cast<long long>(sh.g.m_blocks) * sh.g.n_blocks;
-    sh.g.tiles = A.n * per;
+    sh.g.tiles = groups * per;
     const int max_clusters = resident_clusters<kern>(kNsThreads, S::kBytes, di.sm_count);
     const long long clusters = sh.g.tiles < max_clusters ? sh.g.tiles : max_clusters;
     return launch_chained(kern, dim3(static_cast<unsigned>(2 * clusters)), kNsThreads, S::kBytes, st,
                           maps, ep, sh, status, wait_limit_ns());
+}
+
+// One batch of GEMMs, C[M, N] = sum_k A B over K, on the pair kernel with 256 x BN tiles.
+template <int BN, bool A_MN, bool B_MN, bool kSplit, class Epi>
+cudaError_t run_ns_tiles(const NsOperand& A, const NsOperand& B, const typename Epi::Params& ep,
+                         int M, int N, int K, bool tri, unsigned* status, cudaStream_t st) {
+    NsMaps maps;
+    for (int h = 0; h < 2; ++h) {
+        if (h == 1 && !kSplit) {
+            maps.a[1] = maps.a[0];
+            maps.b[1] = maps.b[0];
+        } else if (!ns_map(&maps.a[h], A, h, A_MN, 128) || !ns_map(&maps.b[h], B, h, B_MN, BN / 2)) {
+            return cudaErrorInvalidValue;
+        }
+    }
+    return launch_ns<BN, A_MN, B_MN, kSplit, Epi>(maps, ep, M, N, K, A.n, tri, status, st);
 }
 
 // fp32 calls on 128-column tiles.  fp16 ones too where twice as many tiles still have a cluster
@@ -444,11 +541,11 @@ cudaError_t run_apply(const NsOperand& X, const NsOperand& B, bool tall, const N
                       int cur, bool next_lo, typename EpiApplyBase<kSplit, kOut>::Params& ep,
                       unsigned* status, cudaStream_t st) {
     const int rows = X.outer, cols = X.inner;
-    ep.hi = X.p[0];
-    ep.lo = reinterpret_cast<__half*>(ws + L.lo[cur]);
+    ep.s.hi = X.p[0];
+    ep.s.lo = reinterpret_cast<__half*>(ws + L.lo[cur]);
+    ep.s.next_hi = reinterpret_cast<__half*>(ws + L.hi[cur ^ 1]);
+    ep.s.next_lo = next_lo ? reinterpret_cast<__half*>(ws + L.lo[cur ^ 1]) : nullptr;
     ep.x32 = kSplit ? reinterpret_cast<float*>(ws + L.x32) : nullptr;
-    ep.next_hi = reinterpret_cast<__half*>(ws + L.hi[cur ^ 1]);
-    ep.next_lo = next_lo ? reinterpret_cast<__half*>(ws + L.lo[cur ^ 1]) : nullptr;
     ep.stride = static_cast<long long>(L.xs);
     ep.M = rows;
     ep.N = cols;
@@ -461,24 +558,45 @@ cudaError_t run_apply(const NsOperand& X, const NsOperand& B, bool tall, const N
                                                                          false, status, st);
 }
 
-// The iteration on the X_0 in the workspace.
-template <bool kSplit>
-cudaError_t run_steps(const NsLayout& L, uint8_t* ws, int n, int rows, int cols, int steps,
-                      const float* coeffs, const NsTarget& to, unsigned* status, cudaStream_t st) {
-    const bool tall = rows > cols;
-    auto at = [&](size_t off) { return reinterpret_cast<__half*>(ws + off); };
-    const NsOperand A = {{at(L.A[0]), at(L.A[1])}, L.m, L.m, n, L.ldm, L.ms};
-    const NsOperand B = {{at(L.B[0]), at(L.B[1])}, L.m, L.m, n, L.ldm, L.ms};
+// The coefficients of every product with the powers of two that X, A and B are stored with: X_k
+// times 2^sx (2^15 for X_0, 1 for the result), A times 2^sa, B times 2^sb.
+void ns_steps(int steps, const float* coeffs, NsChainStep* out) {
     double u = 1.0;            // bound of the singular values of X_k
-    int sx = scale_exp(u);     // X_k is stored times 2^sx
-    int cur = 0;
+    int sx = scale_exp(u);
     for (int k = 0; k < steps; ++k) {
         const double a = coeffs[3 * k], b = coeffs[3 * k + 1], c = coeffs[3 * k + 2];
         const double ub = quad_max(b, c, u * u), un = odd_max(a, b, c, u);
         const int sa = scale_exp(u * u), sb = ub > 0.0 ? scale_exp(ub) : 0,
-                  sn = un > 0.0 ? scale_exp(un) : 0;
-        const NsOperand X = {{at(L.hi[cur]), at(L.lo[cur])}, cols, rows, n, L.ld, L.xs};
+                  sn = k == steps - 1 ? 0 : scale_exp(un);
+        out[k].a_acc = static_cast<float>(ldexp(1.0, sa - 2 * sx));
+        out[k].b_lin = static_cast<float>(ldexp(b, sb - sa));
+        out[k].b_acc = static_cast<float>(ldexp(c, sb - 2 * sa));
+        out[k].x_lin = static_cast<float>(ldexp(a, sn - sx));
+        out[k].x_acc = static_cast<float>(ldexp(1.0, sn - sb - sx));
+        u = un;
+        sx = sn;
+    }
+}
 
+template <bool kSplit, int kOut>
+void set_target(typename EpiApplyBase<kSplit, kOut>::Params& ep, int n, void* const* O) {
+    using Out = typename EpiApplyBase<kSplit, kOut>::Out;
+    for (int l = 0; l < n; ++l) ep.out[l] = static_cast<Out*>(O[l]);
+}
+
+// The iteration on the X_0 in the workspace, a launch per product.  The last step takes the
+// linear term of fp16 calls from the operand itself: nothing grows after it, and the same X in
+// both terms is the smaller error.
+template <bool kSplit, int kOut>
+cudaError_t run_steps(const NsLayout& L, uint8_t* ws, int n, int rows, int cols, int steps,
+                      const NsChainStep* co, void* const* O, unsigned* status, cudaStream_t st) {
+    const bool tall = rows > cols;
+    auto at = [&](size_t off) { return reinterpret_cast<__half*>(ws + off); };
+    const NsOperand A = {{at(L.A[0]), at(L.A[1])}, L.m, L.m, n, L.ldm, L.ms};
+    const NsOperand B = {{at(L.B[0]), at(L.B[1])}, L.m, L.m, n, L.ldm, L.ms};
+    int cur = 0;
+    for (int k = 0; k < steps; ++k) {
+        const NsOperand X = {{at(L.hi[cur]), at(L.lo[cur])}, cols, rows, n, L.ld, L.xs};
         // A = X X^T
         typename EpiSymBase<kSplit>::Params sp = {};
         sp.stride = static_cast<long long>(L.ms);
@@ -486,7 +604,7 @@ cudaError_t run_steps(const NsLayout& L, uint8_t* ws, int n, int rows, int cols,
         sp.ld = L.ldm;
         sp.out[0] = at(L.A[0]);
         sp.out[1] = at(L.A[1]);
-        sp.acc_coef = static_cast<float>(ldexp(1.0, sa - 2 * sx));
+        sp.acc_coef = co[k].a_acc;
         cudaError_t e = tall ? run_ns<true, true, kSplit, SymOf<kSplit>::template T>(
                                    X, X, sp, L.m, L.m, rows, true, status, st)
                              : run_ns<false, false, kSplit, SymOf<kSplit>::template T>(
@@ -497,48 +615,166 @@ cudaError_t run_steps(const NsLayout& L, uint8_t* ws, int n, int rows, int cols,
         sp.lin[1] = at(L.A[1]);
         sp.out[0] = at(L.B[0]);
         sp.out[1] = at(L.B[1]);
-        sp.lin_coef = static_cast<float>(ldexp(b, sb - sa));
-        sp.acc_coef = static_cast<float>(ldexp(c, sb - 2 * sa));
+        sp.lin_coef = co[k].b_lin;
+        sp.acc_coef = co[k].b_acc;
         e = run_ns<false, false, kSplit, SymOf<kSplit>::template T>(A, A, sp, L.m, L.m, L.m, true,
                                                                     status, st);
         if (e != cudaSuccess) return e;
-        // X' = a X + B X.  The last step takes the linear term of fp16 calls from the operand
-        // itself: nothing grows after it, and the same X in both terms is the smaller error.
+        // X' = a X + B X
         const bool last = k == steps - 1;
-        auto coefs = [&](auto& ep) {
-            const int so = last ? 0 : sn;
-            ep.lin_coef = static_cast<float>(ldexp(a, so - sx));
-            ep.acc_coef = static_cast<float>(ldexp(1.0, so - sb - sx));
-            ep.lin_lo = !last;
+        auto coefs = [&](NsApplyStep& s) {
+            s.lin_coef = co[k].x_lin;
+            s.acc_coef = co[k].x_acc;
+            s.lin_lo = !last;
         };
         if (!last) {
             typename EpiApplyBase<kSplit, kNext>::Params ep = {};
-            coefs(ep);
+            coefs(ep.s);
             e = run_apply<kSplit, kNext>(X, B, tall, L, ws, cur, kSplit || k + 2 < steps, ep, status, st);
-        } else if (to.W) {
-            typename EpiApplyBase<kSplit, kWeight>::Params ep = {};
-            coefs(ep);
-            ep.keep = to.keep;
-            ep.rate = to.rate;
-            for (int l = 0; l < n; ++l) {
-                ep.W[l] = to.W[l];
-                ep.out[l] = to.out ? static_cast<typename EpiApplyBase<kSplit, kWeight>::Out*>(to.out[l])
-                                   : nullptr;
-            }
-            e = run_apply<kSplit, kWeight>(X, B, tall, L, ws, cur, false, ep, status, st);
         } else {
-            typename EpiApplyBase<kSplit, kResult>::Params ep = {};
-            coefs(ep);
-            for (int l = 0; l < n; ++l)
-                ep.out[l] = static_cast<typename EpiApplyBase<kSplit, kResult>::Out*>(to.out[l]);
-            e = run_apply<kSplit, kResult>(X, B, tall, L, ws, cur, false, ep, status, st);
+            typename EpiApplyBase<kSplit, kOut>::Params ep = {};
+            coefs(ep.s);
+            set_target<kSplit, kOut>(ep, n, O);
+            e = run_apply<kSplit, kOut>(X, B, tall, L, ws, cur, false, ep, status, st);
         }
         if (e != cudaSuccess) return e;
         cur ^= 1;
-        u = un;
-        sx = sn;
     }
     return cudaSuccess;
+}
+
+// The same in one launch.
+template <bool kSplit, int kOut>
+cudaError_t run_chain(const NsLayout& L, uint8_t* ws, int n, int rows, int cols, int steps,
+                      const NsChainStep* co, void* const* O, long long tiles, unsigned* status,
+                      cudaStream_t st) {
+    constexpr auto kern = ns_chain_kernel<kSplit, kOut>;
+    using S = NsSmem<128>;
+    const bool tall = rows > cols;
+    auto at = [&](size_t off) { return reinterpret_cast<__half*>(ws + off); };
+    NsChainParams<kSplit, kOut> p = {};
+    const NsOperand A = {{at(L.A[0]), at(L.A[1])}, L.m, L.m, n, L.ldm, L.ms};
+    const NsOperand B = {{at(L.B[0]), at(L.B[1])}, L.m, L.m, n, L.ldm, L.ms};
+    bool ok = true;
+    for (int cur = 0; cur < 2; ++cur) {
+        const NsOperand X = {{at(L.hi[cur]), at(L.lo[cur])}, cols, rows, n, L.ld, L.xs};
+        for (int h = 0; h < (kSplit ? 2 : 1); ++h) {
+            ok = ok && ns_map(&p.map[0][cur][0][h], X, h, tall, 128) &&
+                 ns_map(&p.map[0][cur][1][h], X, h, tall, 64);
+            if (cur == 0)
+                ok = ok && ns_map(&p.map[1][0][0][h], A, h, false, 128) &&
+                     ns_map(&p.map[1][0][1][h], A, h, false, 64);
+            else
+                for (int o = 0; o < 2; ++o) p.map[1][1][o][h] = p.map[1][0][o][h];
+            if (tall)
+                ok = ok && ns_map(&p.map[2][cur][0][h], X, h, false, 128) &&
+                     ns_map(&p.map[2][cur][1][h], B, h, false, 64);
+            else
+                ok = ok && ns_map(&p.map[2][cur][0][h], B, h, false, 128) &&
+                     ns_map(&p.map[2][cur][1][h], X, h, true, 64);
+        }
+    }
+    if (!ok) return cudaErrorInvalidValue;
+    p.ap.x32 = kSplit ? reinterpret_cast<float*>(ws + L.x32) : nullptr;
+    p.ap.stride = static_cast<long long>(L.xs);
+    p.ap.M = rows;
+    p.ap.N = cols;
+    p.ap.ld = L.ld;
+    set_target<kSplit, kOut>(p.ap, n, O);
+    for (int k = 0; k < steps; ++k) p.step[k] = co[k];
+    for (int h = 0; h < 2; ++h) {
+        p.A[h] = at(L.A[h]);
+        p.B[h] = at(L.B[h]);
+        p.hi[h] = at(L.hi[h]);
+        p.lo[h] = at(L.lo[h]);
+    }
+    p.ms = static_cast<long long>(L.ms);
+    p.m = L.m;
+    p.ldm = L.ldm;
+    p.steps = steps;
+    p.groups = n;
+    p.rows = rows;
+    p.cols = cols;
+    p.tall = tall;
+    p.count = status + 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(2 * tiles), 1, 1);
+    cfg.blockDim = dim3(kNsThreads, 1, 1);
+    cfg.dynamicSmemBytes = S::kBytes;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeCooperative;
+    attr[0].val.cooperative = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    note_launch();
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, p, status, wait_limit_ns());
+    if (e != cudaSuccess) cudaGetLastError();
+    return e;
+}
+
+template <bool kSplit, int kOut>
+cudaError_t run_iteration(const NsLayout& L, uint8_t* ws, int n, int rows, int cols, int steps,
+                          const float* coeffs, void* const* O, unsigned* status,
+                          cudaStream_t st) {
+    NsChainStep co[kNsMaxSteps];
+    if (steps > kNsMaxSteps) return cudaErrorInvalidValue;
+    ns_steps(steps, coeffs, co);
+    // 256 x 128 tiles of the products, and the clusters that hold one each
+    const long long mb = (L.m + 255) / 256;
+    const long long sym = n * mb * (mb + 1);
+    const long long app = static_cast<long long>(n) * ((rows + 255) / 256) * ((cols + 127) / 128);
+    const long long tiles = sym > app ? sym : app;
+    constexpr auto kern = ns_chain_kernel<kSplit, kOut>;
+    const cudaError_t e = set_smem_limit<kern>(NsSmem<128>::kBytes);
+    if (e != cudaSuccess) return e;
+    DevInfo di;
+    if (!current_device_info(&di)) return cudaErrorUnknown;
+    if (tiles <= resident_clusters<kern>(kNsThreads, NsSmem<128>::kBytes, di.sm_count))
+        return run_chain<kSplit, kOut>(L, ws, n, rows, cols, steps, co, O, tiles, status, st);
+    return run_steps<kSplit, kOut>(L, ws, n, rows, cols, steps, co, O, status, st);
+}
+
+// G_l = g[l]^T A[l] (bf16) with the momentum in the epilogue; *parts: the partial sums per layer.
+cudaError_t run_momentum(int n, int T, int rows, int cols, const NsMomentum& mom, float* U,
+                         size_t u_stride, double* part, int* parts, unsigned* status,
+                         cudaStream_t st) {
+    NsGradMaps maps;
+    EpiMomentumBase::Params ep = {};
+    for (int l = 0; l < n; ++l) {
+        const NsOperand g = {{static_cast<const __half*>(mom.g[l]), nullptr}, rows, T, 1, rows,
+                             static_cast<size_t>(T) * rows};
+        const NsOperand A = {{static_cast<const __half*>(mom.A[l]), nullptr}, cols, T, 1, cols,
+                             static_cast<size_t>(T) * cols};
+        if (!ns_map(&maps.a[l], g, 0, true, 64, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16) ||
+            !ns_map(&maps.b[l], A, 0, true, 64, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16))
+            return cudaErrorInvalidValue;
+        ep.M[l] = mom.M[l];
+    }
+    for (int l = n; l < kMaxGroups; ++l) {
+        maps.a[l] = maps.a[0];
+        maps.b[l] = maps.b[0];
+        ep.M[l] = ep.M[0];
+    }
+    ep.U = U;
+    ep.u_stride = static_cast<long long>(u_stride);
+    ep.part = part;
+    ep.rows = rows;
+    ep.cols = cols;
+    ep.mu = mom.mu;
+    ep.nesterov = mom.nesterov;
+    ep.m_blocks = (rows + 255) / 256;
+    DevInfo di;
+    if (!current_device_info(&di)) return cudaErrorUnknown;
+    const long long tiles = static_cast<long long>(n) * ep.m_blocks * ((cols + 255) / 256);
+    const bool narrow = 4 * tiles <= di.sm_count;  // as in run_ns
+    ep.n_blocks = narrow ? (cols + 127) / 128 : (cols + 255) / 256;
+    *parts = ep.m_blocks * ep.n_blocks * 2 * kNsWarps;
+    if (narrow)
+        return launch_ns<128, true, true, false, EpiMomentum<128>>(maps, ep, rows, cols, T, n, false,
+                                                                   status, st);
+    return launch_ns<256, true, true, false, EpiMomentum<256>>(maps, ep, rows, cols, T, n, false,
+                                                               status, st);
 }
 
 }  // namespace
@@ -566,7 +802,7 @@ float* ns_update_buffer(void* ws, int n, int rows, int cols, int dtype, int laye
 }
 
 cudaError_t launch_newton_schulz(int n, int rows, int cols, int dtype, const void* const* G,
-                                 const NsMomentum* mom, double eps, int steps, const float* coeffs,
+                                 const NsMomentum* mom, float eps, int steps, const float* coeffs,
                                  const NsTarget& to, void* workspace, unsigned* status,
                                  cudaStream_t st) {
     const bool split = dtype == 0;
@@ -574,7 +810,7 @@ cudaError_t launch_newton_schulz(int n, int rows, int cols, int dtype, const voi
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     double* part = reinterpret_cast<double*>(ws + L.part);
     const size_t numel = static_cast<size_t>(rows) * cols;
-    const int blocks = norm_blocks(numel);
+    int blocks = norm_blocks(numel);
     NsPtrs p = {};
     for (int l = 0; l < n; ++l) {
         p.in[l] = mom ? reinterpret_cast<float*>(ws + L.U) + l * L.u_stride : G[l];
@@ -582,7 +818,10 @@ cudaError_t launch_newton_schulz(int n, int rows, int cols, int dtype, const voi
     }
     const dim3 grid(blocks, n);
     cudaError_t e;
-    if (mom) {
+    if (mom && mom->g) {  // bf16, T > 0
+        e = run_momentum(n, mom->T, rows, cols, *mom, reinterpret_cast<float*>(ws + L.U), L.u_stride,
+                         part, &blocks, status, st);
+    } else if (mom) {
         ns_momentum_kernel<<<grid, kPassThreads, 0, st>>>(p, numel, mom->mu, mom->nesterov, part),
             note_launch();
         e = cudaGetLastError();
@@ -592,13 +831,21 @@ cudaError_t launch_newton_schulz(int n, int rows, int cols, int dtype, const voi
         e = launch_chained(ns_norm_kernel<__nv_bfloat16>, grid, kPassThreads, 0, st, p, numel, part);
     }
     if (e != cudaSuccess) return e;
+    if (blocks > kNormBlocks) {  // too many for every block of the cast to add up
+        double* sum = reinterpret_cast<double*>(ws + L.sum);
+        e = launch_chained(ns_sum_kernel, dim3(n), kSumThreads, 0, st,
+                           static_cast<const double*>(part), blocks, sum);
+        if (e != cudaSuccess) return e;
+        part = sum;
+        blocks = 1;
+    }
     const size_t vecs = static_cast<size_t>(rows) * (L.ld / 8);
     const size_t want = (vecs + kPassThreads - 1) / kPassThreads;
     const dim3 cgrid(static_cast<unsigned>(want < 1024 ? want : 1024), n);
     __half* hi = reinterpret_cast<__half*>(ws + L.hi[0]);
     __half* lo = reinterpret_cast<__half*>(ws + L.lo[0]);
     float* x32 = split ? reinterpret_cast<float*>(ws + L.x32) : nullptr;
-    const double scale = ldexp(1.0, scale_exp(1.0));
+    const float scale = ldexpf(1.f, scale_exp(1.0));
     if (split)
         e = launch_chained(ns_cast_kernel<float, true>, cgrid, kPassThreads, 0, st, p, rows, cols, L.ld, part, blocks, eps, scale, hi, lo, x32, L.xs);
     else if (mom)
@@ -606,8 +853,30 @@ cudaError_t launch_newton_schulz(int n, int rows, int cols, int dtype, const voi
     else
         e = launch_chained(ns_cast_kernel<__nv_bfloat16, false>, cgrid, kPassThreads, 0, st, p, rows, cols, L.ld, part, blocks, eps, scale, hi, lo, x32, L.xs);
     if (e != cudaSuccess) return e;
-    if (split) return run_steps<true>(L, ws, n, rows, cols, steps, coeffs, to, status, st);
-    return run_steps<false>(L, ws, n, rows, cols, steps, coeffs, to, status, st);
+    void* O32[kMaxGroups];
+    if (mom)  // in place of U, which is in X_0 by now
+        for (int l = 0; l < n; ++l) O32[l] = const_cast<void*>(p.in[l]);
+    void* const* O = mom ? O32 : to.out;
+    if (split)
+        e = run_iteration<true, kResult>(L, ws, n, rows, cols, steps, coeffs, O, status, st);
+    else if (mom)
+        e = run_iteration<false, kResult32>(L, ws, n, rows, cols, steps, coeffs, O, status, st);
+    else
+        e = run_iteration<false, kResult>(L, ws, n, rows, cols, steps, coeffs, O, status, st);
+    if (e != cudaSuccess || !mom) return e;
+    NsWeights w = {};
+    for (int l = 0; l < n; ++l) {
+        w.O[l] = static_cast<const float*>(p.in[l]);
+        w.W[l] = to.W[l];
+        w.out[l] = to.out ? to.out[l] : nullptr;
+    }
+    const size_t units = (numel + kPassThreads * 16 - 1) / (kPassThreads * 16);
+    const dim3 wgrid(static_cast<unsigned>(units < 2048 ? units : 2048), n);
+    if (split)
+        return launch_chained(ns_weight_kernel<float>, wgrid, kPassThreads, 0, st, w, numel, to.keep,
+                              to.rate);
+    return launch_chained(ns_weight_kernel<__nv_bfloat16>, wgrid, kPassThreads, 0, st, w, numel,
+                          to.keep, to.rate);
 }
 
 }  // namespace fpo

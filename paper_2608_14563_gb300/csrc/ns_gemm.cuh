@@ -46,22 +46,6 @@ __device__ __forceinline__ void tma_load_3d_pair(const CUtensorMap* map, uint32_
         : "memory");
 }
 
-// tmem_ld_32x32b_x32 (ptx.cuh) for 16 columns.
-__device__ __forceinline__ void tmem_ld_32x32b_x16(uint32_t taddr, float (&v)[16]) {
-    uint32_t r[16];
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
-          "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
-          "=r"(r[14]), "=r"(r[15])
-        : "r"(taddr)
-        : "memory");
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
-}
-
 // idesc_bf16_f32 (ptx.cuh) with fp16 A and B (format fields 0).
 __host__ __device__ constexpr uint32_t idesc_f16_f32(int M, int N, bool a_mn, bool b_mn) {
     return idesc_bf16_f32(M, N, a_mn, b_mn) & ~((1u << 7) | (1u << 10));
@@ -89,7 +73,17 @@ struct NsShape {
 };
 
 struct NsMaps {
-    CUtensorMap a[2], b[2];  // high and low parts (low: kSplit only)
+    CUtensorMap a[2], b[2];  // of a batch: high and low parts (low: kSplit only)
+    __device__ __forceinline__ const CUtensorMap* A(int part, int) const { return &a[part]; }
+    __device__ __forceinline__ const CUtensorMap* B(int part, int) const { return &b[part]; }
+    static __device__ __forceinline__ int z(int g) { return g; }
+};
+
+struct NsGradMaps {          // a matrix of its own for every g
+    CUtensorMap a[kMaxGroups], b[kMaxGroups];
+    __device__ __forceinline__ const CUtensorMap* A(int, int g) const { return &a[g]; }
+    __device__ __forceinline__ const CUtensorMap* B(int, int g) const { return &b[g]; }
+    static __device__ __forceinline__ int z(int) { return 0; }
 };
 
 // Tile t: matrix g, block row mb of 256, block column nb of BN.  tri: block row mb has the
@@ -152,41 +146,56 @@ struct EpiSymBase {
 
 template <int BN, bool kSplit>
 struct EpiSym : EpiSymBase<kSplit> {
+    using Maps = NsMaps;
+    static constexpr bool kBf16 = false;
     using Params = typename EpiSymBase<kSplit>::Params;
     static constexpr int kParts = kSplit ? 2 : 1;
     static constexpr int kChunks = BN / 2 / 32;
 
-    const Params& p;
-    long long base;
+    // (by value: a reference to a kernel's parameters, kept in an object, turns into an address
+    // that global loads do not accept)
+    const __half* lin[kParts];  // of this matrix, or null
+    __half* out[kParts];
+    int M, ld;
+    float lin_coef, acc_coef;
     int row, col0;
     bool mirror;
     uint4 l[kParts][4];  // the next chunk's 32 elements of L
 
     __device__ __forceinline__ void fetch(int c) {
-        if (!p.lin[0]) return;
+        if (!lin[0]) return;
 #pragma unroll
         for (int h = 0; h < kParts; ++h) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const int col = col0 + 32 * c + 8 * q;
-                l[h][q] = row < p.M && col < p.ld
+                l[h][q] = row < M && col < ld
                               ? *reinterpret_cast<const uint4*>(
-                                    p.lin[h] + base + static_cast<long long>(row) * p.ld + col)
+                                    lin[h] + static_cast<long long>(row) * ld + col)
                               : make_uint4(0u, 0u, 0u, 0u);
             }
         }
     }
 
-    __device__ __forceinline__ EpiSym(const Params& p_, int g, int row0, int col0_, int lane,
+    __device__ __forceinline__ EpiSym(const Params& p, int g, int row0, int col0_, int lane,
                                       bool mirror_)
-        : p(p_), base(g * p_.stride), row(row0 + lane), col0(col0_), mirror(mirror_) {
+        : M(p.M), ld(p.ld), lin_coef(p.lin_coef), acc_coef(p.acc_coef), row(row0 + lane),
+          col0(col0_), mirror(mirror_) {
+        const long long base = g * p.stride;
+#pragma unroll
+        for (int h = 0; h < kParts; ++h) {
+            lin[h] = p.lin[h] ? p.lin[h] + base : nullptr;
+            out[h] = p.out[h] + base;
+        }
         fetch(0);
     }
 
+    __device__ __forceinline__ void finish(int) {}
+
     __device__ __forceinline__ void chunk(float (&v)[32], uint32_t, int, int c) {
 #pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] *= p.acc_coef;
-        if (p.lin[0]) {
+        for (int j = 0; j < 32; ++j) v[j] *= acc_coef;
+        if (lin[0]) {
 #pragma unroll
             for (int h = 0; h < kParts; ++h) {
 #pragma unroll
@@ -195,32 +204,31 @@ struct EpiSym : EpiSymBase<kSplit> {
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         const float2 f = unpack_f16x2(w[k]);
-                        v[8 * q + 2 * k] = fmaf(p.lin_coef, f.x, v[8 * q + 2 * k]);
-                        v[8 * q + 2 * k + 1] = fmaf(p.lin_coef, f.y, v[8 * q + 2 * k + 1]);
+                        v[8 * q + 2 * k] = fmaf(lin_coef, f.x, v[8 * q + 2 * k]);
+                        v[8 * q + 2 * k + 1] = fmaf(lin_coef, f.y, v[8 * q + 2 * k + 1]);
                     }
                 }
             }
             if (c + 1 < kChunks) fetch(c + 1);
         }
-        if (row >= p.M) return;
+        if (row >= M) return;
         const int cc = col0 + 32 * c;
 #pragma unroll
         for (int h = 0; h < kParts; ++h) {
-            __half* o = p.out[h] + base;
             uint32_t w[16];
 #pragma unroll
             for (int k = 0; k < 16; ++k) w[k] = pack_f16x2(v[2 * k], v[2 * k + 1]);
-            uint4* dst = reinterpret_cast<uint4*>(o + static_cast<long long>(row) * p.ld + cc);
+            uint4* dst = reinterpret_cast<uint4*>(out[h] + static_cast<long long>(row) * ld + cc);
 #pragma unroll
             for (int q = 0; q < 4; ++q)
-                if (cc + 8 * q < p.ld)
+                if (cc + 8 * q < ld)
                     dst[q] = make_uint4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]);
             if (mirror) {  // a column of the tile: 32 lanes, 64 bytes of one row
-                unsigned short* m = reinterpret_cast<unsigned short*>(o) + row;
+                unsigned short* m = reinterpret_cast<unsigned short*>(out[h]) + row;
 #pragma unroll
                 for (int j = 0; j < 32; ++j)
-                    if (cc + j < p.M)
-                        m[static_cast<long long>(cc + j) * p.ld] =
+                    if (cc + j < M)
+                        m[static_cast<long long>(cc + j) * ld] =
                             static_cast<unsigned short>(w[j / 2] >> (16 * (j % 2)));
             }
             if constexpr (kSplit) {
@@ -238,72 +246,70 @@ struct EpiSym : EpiSymBase<kSplit> {
 // ---------------------------------------------------------------------------
 // X' = lin_coef X + acc_coef acc over [M, N] (row stride ld, a multiple of 8, what lies
 // between N and ld zero).  What becomes of it:
-//   kNext    the next X: its high part, and its low part (not kSplit: for the linear term
-//            only) or (kSplit) low part and the fp32 value
-//   kResult  O [M, N] (row stride N) in the call's type
-//   kWeight  W <- keep W - rate X', and W_out in the call's type
+//   kNext     the next X: its high part, and its low part (not kSplit: for the linear term
+//             only) or (kSplit) low part and the fp32 value
+//   kResult   O [M, N] (row stride N) in the call's type
+//   kResult32 O in fp32
 // The linear term takes X in more bits than the operands have: of a direction in which X is
 // small B X is next to nothing, so a X carries it, 3.4 times larger after every step, and with
 // it any rounding of X (fp16: up to 10% of the result for a matrix of low rank).  fp16 reads
 // the low part where it was kept (lin_lo), kSplit the fp32 value.
-enum NsOut { kNext = 0, kResult = 1, kWeight = 2 };
+enum NsOut { kNext = 0, kResult = 1, kResult32 = 2 };
+
+struct NsApplyStep {      // what changes from step to step
+    const __half* hi;     // X (fp16)
+    const __half* lo;     // X's low part, read if lin_lo
+    __half* next_hi;      // kNext
+    __half* next_lo;      // kNext, or null (may be lo)
+    float lin_coef, acc_coef;
+    bool lin_lo;
+};
 
 template <bool kSplit, int kOut>
 struct EpiApplyBase {
-    using Out = std::conditional_t<kSplit, float, __nv_bfloat16>;
+    using Out = std::conditional_t<kSplit || kOut == kResult32, float, __nv_bfloat16>;
     struct Params {
-        const __half* hi;     // X (fp16)
-        __half* lo;           // X's low part: read if lin_lo, written (kNext) if next_lo
+        NsApplyStep s;
         float* x32;           // kSplit: X in fp32, updated in place (kNext)
-        __half* next_hi;      // kNext
-        __half* next_lo;
         long long stride;     // of one matrix in a batch
         int M, N, ld;
-        float lin_coef, acc_coef;
-        bool lin_lo;
-        float keep, rate;              // kWeight
-        Out* out[kMaxGroups];          // kResult: O; kWeight: W_out or null
-        float* W[kMaxGroups];          // kWeight
+        Out* out[kMaxGroups];          // kResult, kResult32: O
     };
 };
 
 template <int BN, bool kSplit, int kOut>
 struct EpiApply : EpiApplyBase<kSplit, kOut> {
+    using Maps = NsMaps;
+    static constexpr bool kBf16 = false;
     using Out = typename EpiApplyBase<kSplit, kOut>::Out;
     using Params = typename EpiApplyBase<kSplit, kOut>::Params;
     static constexpr int kChunks = BN / 2 / 32;
     static constexpr int kAcc = 8;     // accesses of a chunk: 4 rows, 8 lanes of 4 columns to a row
 
-    const Params& p;
-    long long base;
-    float* W;    // of this matrix (kWeight)
-    Out* out;    // of this matrix
+    // (by value, as in EpiSym)
+    const __half *hi_p, *lo_p;   // of this matrix, from its first element
+    __half *next_hi, *next_lo;   // kNext (next_lo: or null)
+    float* x32;                  // kSplit
+    Out* out;                    // kResult, kResult32
+    int M, N, ld;
+    float lin_coef, acc_coef;
     int r0, c0;
     uint2 hi[kSplit ? 1 : kAcc], lo[kSplit ? 1 : kAcc];
-    float4 x[kSplit ? kAcc : 1], w[kOut == kWeight ? kAcc : 1];
+    float4 x[kSplit ? kAcc : 1];
 
     __device__ __forceinline__ bool in(int i, int c) const {
-        return r0 + 4 * i < p.M && c0 + 32 * c < (kOut == kNext ? p.ld : p.N);
+        return r0 + 4 * i < M && c0 + 32 * c < (kOut == kNext ? ld : N);
     }
-    // 4 elements of a row of N floats from column col, those inside it (N > col)
-    __device__ __forceinline__ float4 ld4(const float* q, int col) const {
-        if ((p.N & 3) == 0) return *reinterpret_cast<const float4*>(q);
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        v.x = q[0];
-        if (col + 1 < p.N) v.y = q[1];
-        if (col + 2 < p.N) v.z = q[2];
-        if (col + 3 < p.N) v.w = q[3];
-        return v;
-    }
+    // 4 elements of a row of N from column col, those inside it (N > col)
     __device__ __forceinline__ void st4(float* q, const float4& v, int col) const {
-        if ((p.N & 3) == 0) {
+        if ((N & 3) == 0) {
             *reinterpret_cast<float4*>(q) = v;
             return;
         }
         q[0] = v.x;
-        if (col + 1 < p.N) q[1] = v.y;
-        if (col + 2 < p.N) q[2] = v.z;
-        if (col + 3 < p.N) q[3] = v.w;
+        if (col + 1 < N) q[1] = v.y;
+        if (col + 2 < N) q[2] = v.z;
+        if (col + 3 < N) q[3] = v.w;
     }
     // (N is a multiple of 8 for bf16)
     __device__ __forceinline__ void st4(__nv_bfloat16* q, const float4& v, int) const {
@@ -314,26 +320,38 @@ struct EpiApply : EpiApplyBase<kSplit, kOut> {
 #pragma unroll
         for (int i = 0; i < kAcc; ++i) {
             const bool ok = in(i, c);
-            const long long o =
-                ok ? base + static_cast<long long>(r0 + 4 * i) * p.ld + c0 + 32 * c : base;
+            const long long o = static_cast<long long>(r0 + 4 * i) * ld + c0 + 32 * c;
             if constexpr (kSplit) {
-                x[i] = *reinterpret_cast<const float4*>(p.x32 + o);
+                x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (ok) x[i] = *reinterpret_cast<const float4*>(x32 + o);
             } else {
-                hi[i] = *reinterpret_cast<const uint2*>(p.hi + o);
-                if (p.lin_lo) lo[i] = *reinterpret_cast<const uint2*>(p.lo + o);
-            }
-            if constexpr (kOut == kWeight) {
-                const int col = ok ? c0 + 32 * c : 0;
-                w[i] = ld4(W + (ok ? static_cast<long long>(r0 + 4 * i) * p.N + col : 0), col);
+                hi[i] = lo[i] = make_uint2(0u, 0u);
+                if (ok) hi[i] = *reinterpret_cast<const uint2*>(hi_p + o);
+                if (ok && lo_p) lo[i] = *reinterpret_cast<const uint2*>(lo_p + o);
             }
         }
     }
 
-    __device__ __forceinline__ EpiApply(const Params& p_, int g, int row0, int col0, int lane, bool)
-        : p(p_), base(g * p_.stride), W(kOut == kWeight ? p_.W[g] : nullptr),
-          out(kOut == kNext ? nullptr : p_.out[g]), r0(row0 + lane / 8), c0(col0 + 4 * (lane % 8)) {
+    __device__ __forceinline__ EpiApply(const Params& p, int g, int row0, int col0, int lane, bool)
+        : EpiApply(p, p.s, g, row0, col0, lane) {}
+    __device__ __forceinline__ EpiApply(const Params& p, const NsApplyStep& s, int g, int row0,
+                                        int col0, int lane)
+        : M(p.M), N(p.N), ld(p.ld), lin_coef(s.lin_coef), acc_coef(s.acc_coef),
+          r0(row0 + lane / 8), c0(col0 + 4 * (lane % 8)) {
+        const long long base = g * p.stride;
+        hi_p = s.hi + base;
+        lo_p = s.lin_lo ? s.lo + base : nullptr;
+        if constexpr (kOut == kNext) {
+            next_hi = s.next_hi + base;
+            next_lo = s.next_lo ? s.next_lo + base : nullptr;
+        } else {
+            out = p.out[g];
+        }
+        if constexpr (kSplit) x32 = p.x32 + base;
         fetch(0);
     }
+
+    __device__ __forceinline__ void finish(int) {}
 
     __device__ __forceinline__ void chunk(float (&v)[32], uint32_t buf, int lane, int c) {
         uint32_t u[32];
@@ -351,7 +369,7 @@ struct EpiApply : EpiApplyBase<kSplit, kOut> {
             } else {
                 const float2 h0 = unpack_f16x2(hi[i].x), h1 = unpack_f16x2(hi[i].y);
                 xl = make_float4(h0.x, h0.y, h1.x, h1.y);
-                if (p.lin_lo) {
+                if (lo_p) {
                     const float2 l0 = unpack_f16x2(lo[i].x), l1 = unpack_f16x2(lo[i].y);
                     xl.x += l0.x;
                     xl.y += l0.y;
@@ -359,35 +377,26 @@ struct EpiApply : EpiApplyBase<kSplit, kOut> {
                     xl.w += l1.y;
                 }
             }
-            a.x = fmaf(p.lin_coef, xl.x, a.x * p.acc_coef);
-            a.y = fmaf(p.lin_coef, xl.y, a.y * p.acc_coef);
-            a.z = fmaf(p.lin_coef, xl.z, a.z * p.acc_coef);
-            a.w = fmaf(p.lin_coef, xl.w, a.w * p.acc_coef);
+            a.x = fmaf(lin_coef, xl.x, a.x * acc_coef);
+            a.y = fmaf(lin_coef, xl.y, a.y * acc_coef);
+            a.z = fmaf(lin_coef, xl.z, a.z * acc_coef);
+            a.w = fmaf(lin_coef, xl.w, a.w * acc_coef);
             if (!in(i, c)) continue;
             const int row = r0 + 4 * i, col = c0 + 32 * c;
             if constexpr (kOut == kNext) {
-                const long long o = base + static_cast<long long>(row) * p.ld + col;
+                const long long o = static_cast<long long>(row) * ld + col;
                 const uint2 h = make_uint2(pack_f16x2(a.x, a.y), pack_f16x2(a.z, a.w));
-                *reinterpret_cast<uint2*>(p.next_hi + o) = h;
-                if (p.next_lo) {
+                *reinterpret_cast<uint2*>(next_hi + o) = h;
+                if (next_lo) {
                     const float2 h0 = unpack_f16x2(h.x), h1 = unpack_f16x2(h.y);
-                    *reinterpret_cast<uint2*>(p.next_lo + o) =
+                    *reinterpret_cast<uint2*>(next_lo + o) =
                         make_uint2(pack_f16x2(a.x - h0.x, a.y - h0.y),
                                    pack_f16x2(a.z - h1.x, a.w - h1.y));
                 }
-                if constexpr (kSplit) *reinterpret_cast<float4*>(p.x32 + o) = a;
+                if constexpr (kSplit) *reinterpret_cast<float4*>(x32 + o) = a;
             } else {
-                const long long o = static_cast<long long>(row) * p.N + col;
-                if constexpr (kOut == kWeight) {
-                    a.x = fmaf(-p.rate, a.x, p.keep * w[i].x);
-                    a.y = fmaf(-p.rate, a.y, p.keep * w[i].y);
-                    a.z = fmaf(-p.rate, a.z, p.keep * w[i].z);
-                    a.w = fmaf(-p.rate, a.w, p.keep * w[i].w);
-                    st4(W + o, a, col);
-                    if (out) st4(out + o, a, col);
-                } else {
-                    st4(out + o, a, col);
-                }
+                const long long o = static_cast<long long>(row) * N + col;
+                st4(out + o, a, col);
             }
         }
         if (c + 1 < kChunks) fetch(c + 1);
@@ -396,15 +405,124 @@ struct EpiApply : EpiApplyBase<kSplit, kOut> {
 };
 
 // ---------------------------------------------------------------------------
+// The pseudogradient G = g^T A of bf16 operands and the momentum: M <- mu M + G, U = G + mu M
+// (nesterov) or M, both fp32 [M, N] (N a multiple of 8), and the sum of U's squares over the
+// warp's part of the tile to part[matrix][tile][16 warps of the pair].  (The library's
+// EpiStoreGroupF32 followed by a pass over G, M and U took 97 us for two 8192 x 2048 matrices.)
+struct EpiMomentumBase {
+    struct Params {
+        float* M[kMaxGroups];
+        float* U;             // [groups], u_stride apart
+        long long u_stride;
+        double* part;
+        int rows, cols, m_blocks, n_blocks;
+        float mu;
+        bool nesterov;
+    };
+};
+
+// Sum of 4 squares where fp32 neither overflows nor loses digits to underflow; else 0, and the
+// fp64 sum is added to `exact`.
+__device__ __forceinline__ float square_sum4(const float4& v, double& exact) {
+    const float s = fmaf(v.x, v.x, fmaf(v.y, v.y, fmaf(v.z, v.z, v.w * v.w)));
+    if (s >= 1e-30f && s <= 1e30f) return s;
+    if (((__float_as_uint(v.x) | __float_as_uint(v.y) | __float_as_uint(v.z) |
+          __float_as_uint(v.w)) << 1) != 0)
+        exact += static_cast<double>(v.x) * v.x + static_cast<double>(v.y) * v.y +
+                 static_cast<double>(v.z) * v.z + static_cast<double>(v.w) * v.w;
+    return 0.f;
+}
+
+template <int BN>
+struct EpiMomentum : EpiMomentumBase {
+    using Maps = NsGradMaps;
+    static constexpr bool kBf16 = true;
+    static constexpr int kChunks = BN / 2 / 32;
+    static constexpr int kAcc = 8;
+
+    float *M, *U;      // (by value, as in EpiSym)
+    double* slot;
+    int r0, c0, rows, cols;
+    float mu;
+    bool nesterov;
+    double squares;
+    float4 m[kAcc];
+
+    __device__ __forceinline__ bool in(int i, int c) const {
+        return r0 + 4 * i < rows && c0 + 32 * c < cols;
+    }
+    __device__ __forceinline__ void fetch(int c) {
+#pragma unroll
+        for (int i = 0; i < kAcc; ++i) {
+            m[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (in(i, c))
+                m[i] = *reinterpret_cast<const float4*>(M + static_cast<long long>(r0 + 4 * i) * cols +
+                                                        c0 + 32 * c);
+        }
+    }
+    __device__ __forceinline__ EpiMomentum(const Params& p, int g, int row0, int col0, int lane, bool)
+        : M(p.M[g]), U(p.U + g * p.u_stride), r0(row0 + lane / 8), c0(col0 + 4 * (lane % 8)),
+          rows(p.rows), cols(p.cols), mu(p.mu), nesterov(p.nesterov), squares(0.0) {
+        const int warps = 2 * kNsWarps;  // of a tile: 8 blocks of 32 rows x 2 halves of the columns
+        const long long tile = (static_cast<long long>(g) * p.m_blocks + row0 / kPairBM) * p.n_blocks +
+                               col0 / BN;
+        slot = p.part + tile * warps + row0 % kPairBM / 32 * 2 + col0 % BN / (BN / 2);
+        fetch(0);
+    }
+    __device__ __forceinline__ void chunk(float (&v)[32], uint32_t buf, int lane, int c) {
+        uint32_t w[32];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) w[j] = __float_as_uint(v[j]);
+        out_stage_row(buf, lane, w);
+        __syncwarp();
+        float run = 0.f;
+#pragma unroll
+        for (int i = 0; i < kAcc; ++i) {
+            const uint32_t r = static_cast<uint32_t>(4 * i + lane / 8);
+            const float4 g = ld_shared_f4(buf + r * 128u + (((lane % 8) ^ (r & 7u)) << 4));
+            float4 a = m[i], u;
+            a.x = fmaf(mu, a.x, g.x);
+            a.y = fmaf(mu, a.y, g.y);
+            a.z = fmaf(mu, a.z, g.z);
+            a.w = fmaf(mu, a.w, g.w);
+            u = a;
+            if (nesterov) {
+                u.x = fmaf(mu, a.x, g.x);
+                u.y = fmaf(mu, a.y, g.y);
+                u.z = fmaf(mu, a.z, g.z);
+                u.w = fmaf(mu, a.w, g.w);
+            }
+            if (in(i, c)) {
+                const long long o = static_cast<long long>(r0 + 4 * i) * cols + c0 + 32 * c;
+                *reinterpret_cast<float4*>(M + o) = a;
+                *reinterpret_cast<float4*>(U + o) = u;
+                run += square_sum4(u, squares);
+            }
+        }
+        squares += run;
+        if (c + 1 < kChunks) fetch(c + 1);
+        __syncwarp();
+    }
+    __device__ __forceinline__ void finish(int lane) {
+        double t = squares;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+        if (lane == 0) *slot = t;
+        __syncwarp();
+    }
+};
+
+// ---------------------------------------------------------------------------
 template <int BN, bool A_MN, bool B_MN, bool kSplit, class Epi>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
-    ns_gemm_kernel(const __grid_constant__ NsMaps maps,
+    ns_gemm_kernel(const __grid_constant__ typename Epi::Maps maps,
                    const __grid_constant__ typename Epi::Params ep, const NsShape sh,
                    unsigned int* status, unsigned long long wait_limit_ns) {
     using L = NsSmem<BN>;
     constexpr int kStages = L::kStages;
     constexpr int kSub = kSplit ? 1 : 2;   // k-blocks (and full barriers) per stage
-    constexpr uint32_t kIdesc = idesc_f16_f32(kPairBM, BN, A_MN, B_MN);
+    constexpr uint32_t kIdesc = Epi::kBf16 ? idesc_bf16_f32(kPairBM, BN, A_MN, B_MN)
+                                           : idesc_f16_f32(kPairBM, BN, A_MN, B_MN);
     constexpr uint16_t kBoth = 0x3;
 
     extern __shared__ uint8_t smem_raw[];
@@ -484,8 +602,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
                             mbar_arrive_expect_tx(full_bar(stage, bar_j),
                                                   2 * (L::kStageBytes / kSub));
                         const int k0 = (kSplit ? kb : 2 * kb + j) * kBK;
-                        ns_load<A_MN, 128>(&maps.a[part], sa + j * L::kABox, fb, a_row, k0, g);
-                        ns_load<B_MN, BN / 2>(&maps.b[part], sb + j * L::kBBox, fb, b_row, k0, g);
+                        ns_load<A_MN, 128>(maps.A(part, g), sa + j * L::kABox, fb, a_row, k0, maps.z(g));
+                        ns_load<B_MN, BN / 2>(maps.B(part, g), sb + j * L::kBBox, fb, b_row, k0, maps.z(g));
                     }
                     ++issued;
                     if (++stage == kStages) { stage = 0; phase ^= 1u; }
@@ -562,8 +680,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
         const uint32_t buf = sbase + L::kOutOffset + static_cast<uint32_t>(warp - 2) * kOutBufBytes;
         int acc = 0;
         uint32_t acc_phase = 0;
+        // The lanes poll one by one, and lane 0 arrives alone: the warp is brought together after
+        // both, for tcgen05.ld writes the registers of all its lanes (without this, now and then
+        // over those of a lane still on its way).
         auto ready = [&] {
-            if (!mbar_wait_cl(tfull_bar(acc), acc_phase, guard)) return false;
+            const bool in_time = mbar_wait_cl(tfull_bar(acc), acc_phase, guard);
+            if (!__all_sync(0xffffffffu, in_time)) return false;
             tc_fence_after();
             return true;
         };
@@ -576,6 +698,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
                 else
                     mbar_arrive_cluster(mapa_shared(tempty_bar(acc), 0));
             }
+            __syncwarp();
             if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
         };
         auto t_row = [&] {
@@ -599,20 +722,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
                 for (int kb = 0; ok && kb < stages_k; ++kb) {
                     ok = ready();
                     if (!ok) break;
+                    const uint32_t tr = t_row();
 #pragma unroll
-                    for (int c = 0; c < 2 * kChunks; ++c) {
-                        float v[16];
-                        tmem_ld_32x32b_x16(t_row() + 16 * c, v);
+                    for (int c = 0; c < kChunks; ++c) {
+                        float v[32];
+                        tmem_ld_32x32b_x32(tr + 32 * c, v);
+                        if (c == kChunks - 1) release();  // it is all in registers
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) s[c / 2][16 * (c % 2) + j] += v[j];
+                        for (int j = 0; j < 32; ++j) s[c][j] += v[j];
                     }
-                    release();
                 }
                 if (!ok) break;
                 Epi epi(ep, g, row0, col0, lane, mirror);
 #pragma unroll
                 for (int c = 0; c < kChunks; ++c) epi.chunk(s[c], buf, lane, c);
                 __syncwarp();
+                epi.finish(lane);
             } else {
                 Epi epi(ep, g, row0, col0, lane, mirror);
                 ok = ready();
@@ -626,6 +751,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
                     epi.chunk(v, buf, lane, c);
                     __syncwarp();
                 }
+                epi.finish(lane);
             }
         }
         __syncwarp();
@@ -639,6 +765,427 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
         pair_drain_copies<kStages, kSub>(bar0, *issued_word,
                                            ld_shared_cluster_u32(mapa_shared(smem_u32(issued_word), 1)),
                                            L::kStageBytes / kSub);
+    __syncthreads();
+    cluster_sync();
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc_pair<2 * BN>(tmem_base);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// The whole iteration in one launch, for batches whose products have at most one 256 x 128 tile
+// per resident cluster: there a launch per product (15 of them) costs 7 us each, most of it
+// set-up, the wait for the kernel before and the first operand's way in.  The roles walk the
+// products ("phases": A, B, X of every step) with one counter in global memory between them:
+// every block adds one when its stores of a phase are done, and the producers and epilogues of
+// the next phase wait until all have.  A cooperative launch: every cluster is resident.  The
+// waits are bounded like the barriers'.
+struct NsChainStep {
+    float a_acc;             // A = a_acc acc
+    float b_lin, b_acc;      // B = b_lin A + b_acc acc
+    float x_lin, x_acc;      // X' = x_lin X + x_acc acc
+};
+constexpr int kNsMaxSteps = 32;
+
+template <bool kSplit, int kOut>
+struct NsChainParams {
+    // operands of the phases: [A, B, X][X buffer][A operand, B operand][high, low]
+    CUtensorMap map[3][2][2][kSplit ? 2 : 1];
+    typename EpiApplyBase<kSplit, kOut>::Params ap;  // of the last step (s unused)
+    NsChainStep step[kNsMaxSteps];
+    __half* A[2];
+    __half* B[2];
+    __half* hi[2];
+    __half* lo[2];
+    long long ms;            // elements of one A
+    int m, ldm, steps, groups, rows, cols;
+    bool tall;
+    unsigned* count;         // zero at the start
+};
+
+__device__ __forceinline__ unsigned ld_acquire_u32(const unsigned* p) {
+    unsigned v;
+    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
+
+// Until *count reaches `target` (one thread); false: given up.
+__device__ __forceinline__ bool ns_wait_count(const unsigned* count, unsigned target,
+                                              const WaitGuard& g) {
+    if (ld_acquire_u32(count) >= target) return true;
+    const uint64_t t0 = global_timer_ns();
+    for (uint32_t i = 1;; ++i) {
+        if (ld_acquire_u32(count) >= target) return true;
+        if ((i & 31u) == 0) {
+            if (*g.abort_flag) return false;
+            if (global_timer_ns() - t0 > g.limit_ns) {
+                *g.abort_flag = 1;
+                if (g.status) atomicOr(g.status, kDevTimeout);
+                return false;
+            }
+        }
+    }
+}
+
+// Orders global-memory accesses of this thread through the generic proxy with those of TMA.
+__device__ __forceinline__ void fence_proxy_async_global() {
+    asm volatile("fence.proxy.async.global;" ::: "memory");
+}
+
+template <bool kSplit, int kOut>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
+    ns_chain_kernel(const __grid_constant__ NsChainParams<kSplit, kOut> p, unsigned int* status,
+                    unsigned long long wait_limit_ns) {
+    constexpr int BN = 128;
+    using L = NsSmem<BN>;
+    constexpr int kStages = L::kStages;
+    constexpr int kSub = kSplit ? 1 : 2;
+    constexpr int kParts = kSplit ? 2 : 1;
+    constexpr uint16_t kBoth = 0x3;
+
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw);
+    const uint32_t pad = (1024u - (raw & 1023u)) & 1023u;
+    uint8_t* smem = smem_raw + pad;
+    const uint32_t sbase = raw + pad;
+
+    const uint32_t rank = cluster_ctarank();
+    const bool leader = rank == 0;
+    const long long cluster = blockIdx.x / 2;
+    const long long n_clusters = gridDim.x / 2;
+
+    const uint32_t bar0 = sbase + L::kBarOffset;
+    constexpr int kFull = kStages * kSub;
+    auto full_bar = [&](int s, int j) { return bar0 + 8u * (s * kSub + j); };
+    auto empty_bar = [&](int s) { return bar0 + 8u * (kFull + s); };
+    auto tfull_bar = [&](int a) { return bar0 + 8u * (kFull + kStages + a); };
+    auto tempty_bar = [&](int a) { return bar0 + 8u * (kFull + kStages + 2 + a); };
+    const uint32_t drain_bar = bar0 + 8u * (kFull + kStages + 4);
+    uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(smem + L::kMiscOffset + kMiscTmem);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + L::kMiscOffset + kMiscAbort);
+    uint32_t* issued_word = reinterpret_cast<uint32_t*>(smem + L::kMiscOffset + kMiscIssued);
+
+    const int warp = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            for (int j = 0; j < kSub; ++j) mbar_init(full_bar(s, j), 1);
+            mbar_init(empty_bar(s), 1);
+        }
+        for (int a = 0; a < 2; ++a) {
+            mbar_init(tfull_bar(a), 1);
+            mbar_init(tempty_bar(a), 2 * kNsWarps);
+        }
+        mbar_init(drain_bar, 1);
+        *abort_flag = 0;
+        *issued_word = 0;
+        fence_mbar_init();
+    }
+    if (warp == 1) {
+        tmem_alloc_pair<2 * BN>(smem_u32(tmem_holder));
+        tmem_relinquish_pair();
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_holder;
+
+    const WaitGuard guard{abort_flag, status, wait_limit_ns};
+
+    // Phase f: 0 A, 1 B, 2 X of step f / 3.  (Closures hold copies of the parameters they use.)
+    auto shape = [m = p.m, rows = p.rows, cols = p.cols, groups = p.groups, tall = p.tall](int f) {
+        NsShape sh = {};
+        const bool sym = f % 3 != 2;
+        sh.tri = sym;
+        sh.g.M = sym ? m : rows;
+        sh.g.N = sym ? m : cols;
+        sh.g.K = f % 3 == 0 ? (tall ? rows : cols) : m;
+        sh.g.m_blocks = (sh.g.M + kPairBM - 1) / kPairBM;
+        sh.g.n_blocks = (sh.g.N + BN - 1) / BN;
+        sh.g.k_blocks = (sh.g.K + kBK - 1) / kBK;
+        sh.g.groups = groups;
+        sh.g.band = 16;
+        sh.g.tiles = static_cast<long long>(groups) *
+                     (sym ? sh.g.m_blocks * (sh.g.m_blocks + 1) / 2 * (kPairBM / BN)
+                          : sh.g.m_blocks * sh.g.n_blocks);
+        return sh;
+    };
+    const int phases = 3 * p.steps;
+    const unsigned arrivals = gridDim.x;  // of a phase
+
+    if (warp == 0) {
+        // ------------------------------------------------------- TMA producer (both CTAs)
+        if (lane == 0) {
+            int stage = 0;
+            uint32_t phase = 0, issued = 0;
+            bool ok = true;
+            for (int f = 0; ok && f < phases; ++f) {
+                const NsShape sh = shape(f);
+                if (cluster >= sh.g.tiles) continue;
+                if (!ns_wait_count(p.count, f * arrivals, guard)) break;
+                fence_proxy_async_global();
+                const CUtensorMap(&mp)[2][kParts] = p.map[f % 3][(f / 3) & 1];
+                const bool a_mn = f % 3 == 0 && p.tall;
+                const bool b_mn = f % 3 == 0 ? p.tall : f % 3 == 2 && !p.tall;
+                const int stages_k = (sh.g.k_blocks + kSub - 1) / kSub;
+                for (long long t = cluster; ok && t < sh.g.tiles; t += n_clusters) {
+                    int g, mb, nb;
+                    ns_tile<BN>(t, sh, g, mb, nb);
+                    const int a_row = mb * kPairBM + 128 * static_cast<int>(rank);
+                    const int b_row = nb * BN + (BN / 2) * static_cast<int>(rank);
+                    for (int kb = 0; kb < stages_k; ++kb) {
+                        if (!mbar_wait_cl(empty_bar(stage), phase ^ 1u, guard)) { ok = false; break; }
+                        const uint32_t sa = sbase + stage * L::kStageBytes, sb = sa + 2 * L::kABox;
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const int bar_j = kSplit ? 0 : j, part = kSplit ? j : 0;
+                            const uint32_t fb = mapa_shared(full_bar(stage, bar_j), 0);
+                            if (leader && (!kSplit || j == 0))
+                                mbar_arrive_expect_tx(full_bar(stage, bar_j),
+                                                      2 * (L::kStageBytes / kSub));
+                            const int k0 = (kSplit ? kb : 2 * kb + j) * kBK;
+                            if (a_mn)
+                                ns_load<true, 128>(&mp[0][part], sa + j * L::kABox, fb, a_row, k0, g);
+                            else
+                                ns_load<false, 128>(&mp[0][part], sa + j * L::kABox, fb, a_row, k0, g);
+                            if (b_mn)
+                                ns_load<true, BN / 2>(&mp[1][part], sb + j * L::kBBox, fb, b_row, k0, g);
+                            else
+                                ns_load<false, BN / 2>(&mp[1][part], sb + j * L::kBBox, fb, b_row, k0, g);
+                        }
+                        ++issued;
+                        if (++stage == kStages) { stage = 0; phase ^= 1u; }
+                    }
+                }
+            }
+            *issued_word = issued;
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        // ------------------------------------------------------- pair MMA (leader only)
+        if (leader && lane == 0) {
+            int stage = 0, acc = 0;
+            uint32_t phase = 0, acc_phase = 0;
+            bool ok = true, issued_any = false;
+            // the MMAs of one stage (one k-block of it: j) with the operands' layouts
+            auto stage_mmas = [&](auto amn, auto bmn, uint32_t d_tmem, uint32_t sa, uint32_t sb, int j,
+                                  bool first) {
+                constexpr bool A_MN = decltype(amn)::value, B_MN = decltype(bmn)::value;
+                constexpr uint32_t kIdesc = idesc_f16_f32(kPairBM, BN, A_MN, B_MN);
+                if constexpr (kSplit) {
+#pragma unroll
+                    for (int m = 0; m < 3; ++m) {
+#pragma unroll
+                        for (int kk = 0; kk < kBK / kUmmaK; ++kk)
+                            tc_mma_bf16_pair(d_tmem,
+                                             operand_desc<A_MN>(sa + (m == 1 ? L::kABox : 0), kk),
+                                             operand_desc<B_MN>(sb + (m == 0 ? L::kBBox : 0), kk),
+                                             kIdesc, (m != 0 || kk != 0) ? 1u : 0u);
+                    }
+                } else {
+#pragma unroll
+                    for (int kk = 0; kk < kBK / kUmmaK; ++kk)
+                        tc_mma_bf16_pair(d_tmem, operand_desc<A_MN>(sa + j * L::kABox, kk),
+                                         operand_desc<B_MN>(sb + j * L::kBBox, kk), kIdesc,
+                                         (!first || kk != 0) ? 1u : 0u);
+                }
+            };
+            for (int f = 0; ok && f < phases; ++f) {
+                const NsShape sh = shape(f);
+                const int stages_k = (sh.g.k_blocks + kSub - 1) / kSub;
+                const bool both_mn = f % 3 == 0 && p.tall, b_mn = f % 3 == 2 && !p.tall;
+                for (long long t = cluster; ok && t < sh.g.tiles; t += n_clusters) {
+                    for (int kb = 0; kb < stages_k; ++kb) {
+                        if (kSplit || kb == 0) {
+                            if (!mbar_wait_cl(tempty_bar(acc), acc_phase ^ 1u, guard)) {
+                                ok = false;
+                                break;
+                            }
+                            tc_fence_after();
+                        }
+                        const uint32_t d_tmem = tmem_base + static_cast<uint32_t>(acc * BN);
+                        const uint32_t sa = sbase + stage * L::kStageBytes, sb = sa + 2 * L::kABox;
+#pragma unroll
+                        for (int j = 0; j < kSub; ++j) {
+                            // (not mbar_wait_cl_poll: this wait spans the wait between phases)
+                            if (!mbar_wait_cl(full_bar(stage, j), phase, guard)) { ok = false; break; }
+                            tc_fence_after();
+                            const bool first = kb == 0 && j == 0;
+                            if (both_mn)
+                                stage_mmas(std::true_type{}, std::true_type{}, d_tmem, sa, sb, j, first);
+                            else if (b_mn)
+                                stage_mmas(std::false_type{}, std::true_type{}, d_tmem, sa, sb, j, first);
+                            else
+                                stage_mmas(std::false_type{}, std::false_type{}, d_tmem, sa, sb, j, first);
+                            issued_any = true;
+                        }
+                        if (!ok) break;
+                        tc_commit_pair_multicast(empty_bar(stage), kBoth);
+                        if (++stage == kStages) { stage = 0; phase ^= 1u; }
+                        if (kSplit || kb == stages_k - 1) {
+                            tc_commit_pair_multicast(tfull_bar(acc), kBoth);
+                            if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+                        }
+                    }
+                }
+            }
+            if (issued_any) {
+                tc_commit_pair_multicast(drain_bar, 0x1);
+                mbar_wait_cl_drain(drain_bar, 0, kDrainLimitNs);
+            }
+        }
+        __syncwarp();
+    } else {
+        // ------------------------------------------------------- epilogue (both CTAs)
+        const int q = warp & 3;
+        const int half = (warp - 2) / 4;
+        constexpr int kWarpCols = BN / 2;
+        constexpr int kChunks = kWarpCols / 32;
+        const uint32_t buf = sbase + L::kOutOffset + static_cast<uint32_t>(warp - 2) * kOutBufBytes;
+        int acc = 0;
+        uint32_t acc_phase = 0;
+        bool ok = true;
+        auto release = [&] {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if (leader)
+                    mbar_arrive(tempty_bar(acc));
+                else
+                    mbar_arrive_cluster(mapa_shared(tempty_bar(acc), 0));
+            }
+            __syncwarp();
+            if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+        };
+        // the sums of one tile through `epi`
+        auto tile = [&](auto&& epi, int stages_k) {
+            auto t_row = [&] {
+                return tmem_base + (static_cast<uint32_t>(q * 32) << 16) +
+                       static_cast<uint32_t>(acc * BN + half * kWarpCols);
+            };
+            auto ready = [&] {  // (as in ns_gemm_kernel)
+                const bool in_time = mbar_wait_cl(tfull_bar(acc), acc_phase, guard);
+                if (!__all_sync(0xffffffffu, in_time)) return false;
+                tc_fence_after();
+                return true;
+            };
+            if constexpr (kSplit) {
+                float s[kChunks][32];
+#pragma unroll
+                for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) s[c][j] = 0.f;
+                for (int kb = 0; kb < stages_k; ++kb) {
+                    if (!ready()) return false;
+                    const uint32_t tr = t_row();
+#pragma unroll
+                    for (int c = 0; c < kChunks; ++c) {
+                        float v[32];
+                        tmem_ld_32x32b_x32(tr + 32 * c, v);
+                        if (c == kChunks - 1) release();  // it is all in registers
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) s[c][j] += v[j];
+                    }
+                }
+#pragma unroll
+                for (int c = 0; c < kChunks; ++c) {
+                    epi.chunk(s[c], buf, lane, c);
+                    __syncwarp();
+                }
+            } else {
+                if (!ready()) return false;
+                const uint32_t tr = t_row();
+#pragma unroll 1
+                for (int c = 0; c < kChunks; ++c) {
+                    float v[32];
+                    tmem_ld_32x32b_x32(tr + 32 * c, v);
+                    if (c == kChunks - 1) release();
+                    epi.chunk(v, buf, lane, c);
+                    __syncwarp();
+                }
+            }
+            return true;
+        };
+        // the 8 warps' own barrier; all of them reach it twice in every phase, also after giving up
+        auto epilogue_sync = [&] {
+            __syncwarp();
+            asm volatile("bar.sync 1, %0;" ::"n"(32 * kNsWarps) : "memory");
+        };
+        for (int f = 0; f < phases; ++f) {
+            const NsShape sh = shape(f);
+            const int k = f / 3, cur = k & 1;
+            const bool last = k == p.steps - 1;
+            const int stages_k = (sh.g.k_blocks + kSub - 1) / kSub;
+            // one thread of the block polls (a failure is in the abort flag); every block waits
+            // here, also one without a tile: none may count for a phase ahead of time
+            if (warp == 2 && lane == 0 && ok) ns_wait_count(p.count, f * arrivals, guard);
+            epilogue_sync();
+            ok = ok && !*abort_flag;
+            for (long long t = cluster; ok && t < sh.g.tiles; t += n_clusters) {
+                int g, mb, nb;
+                ns_tile<BN>(t, sh, g, mb, nb);
+                const int row0 = mb * kPairBM + 128 * static_cast<int>(rank) + 32 * q;
+                const int col0 = nb * BN + half * kWarpCols;
+                if (f % 3 != 2) {
+                    typename EpiSymBase<kSplit>::Params sp;
+                    const bool gram = f % 3 == 0;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        sp.lin[h] = gram ? nullptr : p.A[h];
+                        sp.out[h] = gram ? p.A[h] : p.B[h];
+                    }
+                    sp.stride = p.ms;
+                    sp.M = p.m;
+                    sp.ld = p.ldm;
+                    sp.lin_coef = p.step[k].b_lin;
+                    sp.acc_coef = gram ? p.step[k].a_acc : p.step[k].b_acc;
+                    ok = tile(EpiSym<BN, kSplit>(sp, g, row0, col0, lane, nb * BN / kPairBM != mb),
+                              stages_k);
+                } else {
+                    NsApplyStep st;
+                    st.hi = p.hi[cur];
+                    st.lo = p.lo[cur];
+                    st.next_hi = p.hi[cur ^ 1];
+                    st.next_lo = kSplit || k + 2 < p.steps ? p.lo[cur ^ 1] : nullptr;
+                    st.lin_coef = p.step[k].x_lin;
+                    st.acc_coef = p.step[k].x_acc;
+                    st.lin_lo = !last;
+                    if (last) {
+                        ok = tile(EpiApply<BN, kSplit, kOut>(p.ap, st, g, row0, col0, lane), stages_k);
+                    } else {
+                        typename EpiApplyBase<kSplit, kNext>::Params np;
+                        np.x32 = p.ap.x32;
+                        np.stride = p.ap.stride;
+                        np.M = p.rows;
+                        np.N = p.cols;
+                        np.ld = p.ap.ld;
+                        ok = tile(EpiApply<BN, kSplit, kNext>(np, st, g, row0, col0, lane), stages_k);
+                    }
+                }
+            }
+            // the block's part of the phase is done, and visible to TMA
+            fence_proxy_async_global();
+            epilogue_sync();
+            if (warp == 2 && lane == 0 && ok) {
+                __threadfence();
+                atomicAdd(p.count, 1u);
+            }
+            __syncwarp();
+        }
+        __syncwarp();
+    }
+
+    // Teardown, as in tc_gemm_pair_kernel.
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();
+    if (leader && threadIdx.x == 0)
+        pair_drain_copies<kStages, kSub>(bar0, *issued_word,
+                                         ld_shared_cluster_u32(mapa_shared(smem_u32(issued_word), 1)),
+                                         L::kStageBytes / kSub);
     __syncthreads();
     cluster_sync();
     if (warp == 1) {

@@ -27,7 +27,8 @@ def test_workspace_queries(fpo):
     assert 0 <= q(1, m, n) - (6 * m * n + 4 * m * m) < 8192
     assert q(1, n, m) == q(1, m, n)
     assert 0 <= q(2, m, n, fpo.F32) - 2 * (12 * m * n + 8 * m * m) < 8192
-    assert 0 <= fpo.layer_muon_workspace(1, m, n) - q(1, m, n) - 4 * m * n < 8192
+    # the update in fp32, and 16 partial norms per tile of 256 x 128
+    assert 0 <= fpo.layer_muon_workspace(1, m, n) - q(1, m, n) - 4 * m * n < 8192 + m * n // 128
     assert fpo.layer_muon_workspace(1, 60, 64) == 0
     # the largest sides of the largest group fit 64 bits
     assert q(64, 65536, 65536, fpo.F32) > 64 * 20 * 65536 * 65536
