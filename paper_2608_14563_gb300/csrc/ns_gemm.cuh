@@ -129,10 +129,33 @@ __device__ __forceinline__ float2 unpack_f16x2(uint32_t w) {
 }
 
 // ---------------------------------------------------------------------------
+// Epilogues.  A warp has 32 rows x BN / 2 columns of a tile and takes them 32 columns at a time:
+// the accumulator's chunk (one row per lane) goes through the warp's staging buffer, and each
+// lane takes 4 columns of 8 rows back (access i: row 4 i + lane / 8), so that a global access of
+// the warp covers 64 or 128 bytes of 4 rows.  (One row per lane makes it touch 32 rows: the LSU then takes
+// 32 cycles an access, and the epilogue of one small tile 1.5 us.)  What a chunk reads is loaded
+// two chunks ahead in one of two slots of registers (kSplit, whose sums fill them: one ahead).
+template <bool kSplit>
+constexpr int ns_slots() {
+    return kSplit ? 1 : 2;
+}
+
+// The staged chunk: access i of this lane, and where it lies.
+__device__ __forceinline__ uint32_t ns_piece(uint32_t buf, int lane, int i) {
+    const uint32_t r = static_cast<uint32_t>(4 * i + lane / 8);
+    return buf + r * 128u + (((lane % 8) ^ (r & 7u)) << 4);
+}
+__device__ __forceinline__ void ns_stage(uint32_t buf, int lane, const float (&v)[32]) {
+    uint32_t u[32];
+#pragma unroll
+    for (int j = 0; j < 32; ++j) u[j] = __float_as_uint(v[j]);
+    out_stage_row(buf, lane, u);
+    __syncwarp();
+}
+
 // Symmetric results S [M, M] of one matrix: s = lin_coef L + acc_coef acc, rounded to fp16 (with
-// kSplit: high and low parts), to (row, col) and (col, row).  L (null: no such term) is read in
-// the row layout of the accumulator; both are [M, ld], ld a multiple of 8, the columns from M to
-// ld zero.
+// kSplit: high and low parts), to (row, col) and, off the diagonal blocks, to (col, row).  L
+// null: no such term.  L and S are [M, ld], ld a multiple of 8, the columns from M to ld zero.
 template <bool kSplit>
 struct EpiSymBase {
     struct Params {
@@ -158,88 +181,103 @@ struct EpiSym : EpiSymBase<kSplit> {
     __half* out[kParts];
     int M, ld;
     float lin_coef, acc_coef;
-    int row, col0;
+    int row0, col0, r0, c0;
     bool mirror;
-    uint4 l[kParts][4];  // the next chunk's 32 elements of L
+    static constexpr int kAcc = 8, kSlots = ns_slots<kSplit>();
+    uint2 l[kSlots][kParts][kAcc];
 
+    __device__ __forceinline__ bool in(int i, int c) const {
+        return r0 + 4 * i < M && c0 + 32 * c < ld;
+    }
+    template <int SLOT>
     __device__ __forceinline__ void fetch(int c) {
         if (!lin[0]) return;
 #pragma unroll
         for (int h = 0; h < kParts; ++h) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int col = col0 + 32 * c + 8 * q;
-                l[h][q] = row < M && col < ld
-                              ? *reinterpret_cast<const uint4*>(
-                                    lin[h] + static_cast<long long>(row) * ld + col)
-                              : make_uint4(0u, 0u, 0u, 0u);
+            for (int i = 0; i < kAcc; ++i) {
+                l[SLOT][h][i] = make_uint2(0u, 0u);
+                if (in(i, c))
+                    l[SLOT][h][i] = *reinterpret_cast<const uint2*>(
+                        lin[h] + static_cast<long long>(r0 + 4 * i) * ld + c0 + 32 * c);
             }
         }
     }
 
-    __device__ __forceinline__ EpiSym(const Params& p, int g, int row0, int col0_, int lane,
+    __device__ __forceinline__ EpiSym(const Params& p, int g, int row0_, int col0_, int lane,
                                       bool mirror_)
-        : M(p.M), ld(p.ld), lin_coef(p.lin_coef), acc_coef(p.acc_coef), row(row0 + lane),
-          col0(col0_), mirror(mirror_) {
+        : M(p.M), ld(p.ld), lin_coef(p.lin_coef), acc_coef(p.acc_coef), row0(row0_), col0(col0_),
+          r0(row0_ + lane / 8), c0(col0_ + 4 * (lane % 8)), mirror(mirror_) {
         const long long base = g * p.stride;
 #pragma unroll
         for (int h = 0; h < kParts; ++h) {
             lin[h] = p.lin[h] ? p.lin[h] + base : nullptr;
             out[h] = p.out[h] + base;
         }
-        fetch(0);
+        fetch<0>(0);
+        if constexpr (kSlots == 2) fetch<1>(1);
     }
 
     __device__ __forceinline__ void finish(int) {}
 
-    __device__ __forceinline__ void chunk(float (&v)[32], uint32_t, int, int c) {
+    template <int SLOT>
+    __device__ __forceinline__ void chunk(const float (&v)[32], uint32_t buf, int lane, int c) {
+        ns_stage(buf, lane, v);
 #pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] *= acc_coef;
-        if (lin[0]) {
+        for (int i = 0; i < kAcc; ++i) {
+            const uint32_t at = ns_piece(buf, lane, i);
+            float4 a = ld_shared_f4(at);
+            a = make_float4(a.x * acc_coef, a.y * acc_coef, a.z * acc_coef, a.w * acc_coef);
+            if (lin[0]) {
+#pragma unroll
+                for (int h = 0; h < kParts; ++h) {
+                    const float2 f0 = unpack_f16x2(l[SLOT][h][i].x), f1 = unpack_f16x2(l[SLOT][h][i].y);
+                    a.x = fmaf(lin_coef, f0.x, a.x);
+                    a.y = fmaf(lin_coef, f0.y, a.y);
+                    a.z = fmaf(lin_coef, f1.x, a.z);
+                    a.w = fmaf(lin_coef, f1.y, a.w);
+                }
+            }
+            if (mirror)
+                st_shared_v4(at, __float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(a.z),
+                             __float_as_uint(a.w));
 #pragma unroll
             for (int h = 0; h < kParts; ++h) {
+                const uint2 w = make_uint2(pack_f16x2(a.x, a.y), pack_f16x2(a.z, a.w));
+                if (in(i, c))
+                    *reinterpret_cast<uint2*>(out[h] + static_cast<long long>(r0 + 4 * i) * ld + c0 +
+                                              32 * c) = w;
+                if constexpr (kSplit) {
+                    const float2 f0 = unpack_f16x2(w.x), f1 = unpack_f16x2(w.y);
+                    a = make_float4(a.x - f0.x, a.y - f0.y, a.z - f1.x, a.w - f1.y);
+                }
+            }
+        }
+        if (mirror) {  // the block is turned over: a lane's row becomes 32 elements of a column
+            __syncwarp();
+            const int row = row0 + lane, col = col0 + 32 * c;
+            if (row < M) {
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const uint32_t w[4] = {l[h][q].x, l[h][q].y, l[h][q].z, l[h][q].w};
+                for (int k = 0; k < 8; ++k) {
+                    const float4 f = ld_shared_f4(buf + lane * 128u + ((k ^ (lane & 7)) << 4));
+                    const float e[4] = {f.x, f.y, f.z, f.w};
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const float2 f = unpack_f16x2(w[k]);
-                        v[8 * q + 2 * k] = fmaf(lin_coef, f.x, v[8 * q + 2 * k]);
-                        v[8 * q + 2 * k + 1] = fmaf(lin_coef, f.y, v[8 * q + 2 * k + 1]);
+                    for (int j = 0; j < 4; ++j) {
+                        if (col + 4 * k + j >= M) continue;
+                        const long long o = static_cast<long long>(col + 4 * k + j) * ld + row;
+                        const __half hi = __float2half_rn(e[j]);
+                        out[0][o] = hi;
+                        if constexpr (kSplit) out[1][o] = __float2half_rn(e[j] - __half2float(hi));
                     }
                 }
             }
-            if (c + 1 < kChunks) fetch(c + 1);
         }
-        if (row >= M) return;
-        const int cc = col0 + 32 * c;
-#pragma unroll
-        for (int h = 0; h < kParts; ++h) {
-            uint32_t w[16];
-#pragma unroll
-            for (int k = 0; k < 16; ++k) w[k] = pack_f16x2(v[2 * k], v[2 * k + 1]);
-            uint4* dst = reinterpret_cast<uint4*>(out[h] + static_cast<long long>(row) * ld + cc);
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                if (cc + 8 * q < ld)
-                    dst[q] = make_uint4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]);
-            if (mirror) {  // a column of the tile: 32 lanes, 64 bytes of one row
-                unsigned short* m = reinterpret_cast<unsigned short*>(out[h]) + row;
-#pragma unroll
-                for (int j = 0; j < 32; ++j)
-                    if (cc + j < M)
-                        m[static_cast<long long>(cc + j) * ld] =
-                            static_cast<unsigned short>(w[j / 2] >> (16 * (j % 2)));
-            }
-            if constexpr (kSplit) {
-#pragma unroll
-                for (int k = 0; k < 16; ++k) {
-                    const float2 f = unpack_f16x2(w[k]);
-                    v[2 * k] -= f.x;
-                    v[2 * k + 1] -= f.y;
-                }
-            }
+        if constexpr (kSlots == 2) {
+            if (c + 2 < kChunks) fetch<SLOT>(c + 2);
+        } else {
+            if (c + 1 < kChunks) fetch<SLOT>(c + 1);
         }
+        __syncwarp();
     }
 };
 
@@ -284,7 +322,7 @@ struct EpiApply : EpiApplyBase<kSplit, kOut> {
     using Out = typename EpiApplyBase<kSplit, kOut>::Out;
     using Params = typename EpiApplyBase<kSplit, kOut>::Params;
     static constexpr int kChunks = BN / 2 / 32;
-    static constexpr int kAcc = 8;     // accesses of a chunk: 4 rows, 8 lanes of 4 columns to a row
+    static constexpr int kAcc = 8, kSlots = ns_slots<kSplit>();
 
     // (by value, as in EpiSym)
     const __half *hi_p, *lo_p;   // of this matrix, from its first element
@@ -294,7 +332,7 @@ struct EpiApply : EpiApplyBase<kSplit, kOut> {
     int M, N, ld;
     float lin_coef, acc_coef;
     int r0, c0;
-    uint2 hi[kSplit ? 1 : kAcc], lo[kSplit ? 1 : kAcc];
+    uint2 hi[kSlots][kSplit ? 1 : kAcc], lo[kSlots][kSplit ? 1 : kAcc];
     float4 x[kSplit ? kAcc : 1];
 
     __device__ __forceinline__ bool in(int i, int c) const {
@@ -316,6 +354,7 @@ struct EpiApply : EpiApplyBase<kSplit, kOut> {
         *reinterpret_cast<uint2*>(q) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
     }
 
+    template <int SLOT>
     __device__ __forceinline__ void fetch(int c) {
 #pragma unroll
         for (int i = 0; i < kAcc; ++i) {
@@ -325,9 +364,9 @@ struct EpiApply : EpiApplyBase<kSplit, kOut> {
                 x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
                 if (ok) x[i] = *reinterpret_cast<const float4*>(x32 + o);
             } else {
-                hi[i] = lo[i] = make_uint2(0u, 0u);
-                if (ok) hi[i] = *reinterpret_cast<const uint2*>(hi_p + o);
-                if (ok && lo_p) lo[i] = *reinterpret_cast<const uint2*>(lo_p + o);
+                hi[SLOT][i] = lo[SLOT][i] = make_uint2(0u, 0u);
+                if (ok) hi[SLOT][i] = *reinterpret_cast<const uint2*>(hi_p + o);
+                if (ok && lo_p) lo[SLOT][i] = *reinterpret_cast<const uint2*>(lo_p + o);
             }
         }
     }
@@ -348,29 +387,26 @@ struct EpiApply : EpiApplyBase<kSplit, kOut> {
             out = p.out[g];
         }
         if constexpr (kSplit) x32 = p.x32 + base;
-        fetch(0);
+        fetch<0>(0);
+        if constexpr (kSlots == 2) fetch<1>(1);
     }
 
     __device__ __forceinline__ void finish(int) {}
 
-    __device__ __forceinline__ void chunk(float (&v)[32], uint32_t buf, int lane, int c) {
-        uint32_t u[32];
-#pragma unroll
-        for (int j = 0; j < 32; ++j) u[j] = __float_as_uint(v[j]);
-        out_stage_row(buf, lane, u);
-        __syncwarp();
+    template <int SLOT>
+    __device__ __forceinline__ void chunk(const float (&v)[32], uint32_t buf, int lane, int c) {
+        ns_stage(buf, lane, v);
 #pragma unroll
         for (int i = 0; i < kAcc; ++i) {
-            const uint32_t r = static_cast<uint32_t>(4 * i + lane / 8);
-            float4 a = ld_shared_f4(buf + r * 128u + (((lane % 8) ^ (r & 7u)) << 4));
+            float4 a = ld_shared_f4(ns_piece(buf, lane, i));
             float4 xl;
             if constexpr (kSplit) {
                 xl = x[i];
             } else {
-                const float2 h0 = unpack_f16x2(hi[i].x), h1 = unpack_f16x2(hi[i].y);
+                const float2 h0 = unpack_f16x2(hi[SLOT][i].x), h1 = unpack_f16x2(hi[SLOT][i].y);
                 xl = make_float4(h0.x, h0.y, h1.x, h1.y);
                 if (lo_p) {
-                    const float2 l0 = unpack_f16x2(lo[i].x), l1 = unpack_f16x2(lo[i].y);
+                    const float2 l0 = unpack_f16x2(lo[SLOT][i].x), l1 = unpack_f16x2(lo[SLOT][i].y);
                     xl.x += l0.x;
                     xl.y += l0.y;
                     xl.z += l1.x;
@@ -399,7 +435,11 @@ struct EpiApply : EpiApplyBase<kSplit, kOut> {
                 st4(out + o, a, col);
             }
         }
-        if (c + 1 < kChunks) fetch(c + 1);
+        if constexpr (kSlots == 2) {
+            if (c + 2 < kChunks) fetch<SLOT>(c + 2);
+        } else {
+            if (c + 1 < kChunks) fetch<SLOT>(c + 1);
+        }
         __syncwarp();
     }
 };
@@ -438,7 +478,7 @@ struct EpiMomentum : EpiMomentumBase {
     using Maps = NsGradMaps;
     static constexpr bool kBf16 = true;
     static constexpr int kChunks = BN / 2 / 32;
-    static constexpr int kAcc = 8;
+    static constexpr int kAcc = 8, kSlots = 2;
 
     float *M, *U;      // (by value, as in EpiSym)
     double* slot;
@@ -446,17 +486,18 @@ struct EpiMomentum : EpiMomentumBase {
     float mu;
     bool nesterov;
     double squares;
-    float4 m[kAcc];
+    float4 m[kSlots][kAcc];
 
     __device__ __forceinline__ bool in(int i, int c) const {
         return r0 + 4 * i < rows && c0 + 32 * c < cols;
     }
+    template <int SLOT>
     __device__ __forceinline__ void fetch(int c) {
 #pragma unroll
         for (int i = 0; i < kAcc; ++i) {
-            m[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            m[SLOT][i] = make_float4(0.f, 0.f, 0.f, 0.f);
             if (in(i, c))
-                m[i] = *reinterpret_cast<const float4*>(M + static_cast<long long>(r0 + 4 * i) * cols +
+                m[SLOT][i] = *reinterpret_cast<const float4*>(M + static_cast<long long>(r0 + 4 * i) * cols +
                                                         c0 + 32 * c);
         }
     }
@@ -467,20 +508,17 @@ struct EpiMomentum : EpiMomentumBase {
         const long long tile = (static_cast<long long>(g) * p.m_blocks + row0 / kPairBM) * p.n_blocks +
                                col0 / BN;
         slot = p.part + tile * warps + row0 % kPairBM / 32 * 2 + col0 % BN / (BN / 2);
-        fetch(0);
+        fetch<0>(0);
+        fetch<1>(1);
     }
-    __device__ __forceinline__ void chunk(float (&v)[32], uint32_t buf, int lane, int c) {
-        uint32_t w[32];
-#pragma unroll
-        for (int j = 0; j < 32; ++j) w[j] = __float_as_uint(v[j]);
-        out_stage_row(buf, lane, w);
-        __syncwarp();
+    template <int SLOT>
+    __device__ __forceinline__ void chunk(const float (&v)[32], uint32_t buf, int lane, int c) {
+        ns_stage(buf, lane, v);
         float run = 0.f;
 #pragma unroll
         for (int i = 0; i < kAcc; ++i) {
-            const uint32_t r = static_cast<uint32_t>(4 * i + lane / 8);
-            const float4 g = ld_shared_f4(buf + r * 128u + (((lane % 8) ^ (r & 7u)) << 4));
-            float4 a = m[i], u;
+            const float4 g = ld_shared_f4(ns_piece(buf, lane, i));
+            float4 a = m[SLOT][i], u;
             a.x = fmaf(mu, a.x, g.x);
             a.y = fmaf(mu, a.y, g.y);
             a.z = fmaf(mu, a.z, g.z);
@@ -500,7 +538,7 @@ struct EpiMomentum : EpiMomentumBase {
             }
         }
         squares += run;
-        if (c + 1 < kChunks) fetch(c + 1);
+        if (c + 2 < kChunks) fetch<SLOT>(c + 2);
         __syncwarp();
     }
     __device__ __forceinline__ void finish(int lane) {
@@ -735,8 +773,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
                 if (!ok) break;
                 Epi epi(ep, g, row0, col0, lane, mirror);
 #pragma unroll
-                for (int c = 0; c < kChunks; ++c) epi.chunk(s[c], buf, lane, c);
-                __syncwarp();
+                for (int c = 0; c < kChunks; ++c) epi.template chunk<0>(s[c], buf, lane, c);
                 epi.finish(lane);
             } else {
                 Epi epi(ep, g, row0, col0, lane, mirror);
@@ -744,12 +781,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
                 if (!ok) break;
                 const uint32_t tr = t_row();
 #pragma unroll 1
-                for (int c = 0; c < kChunks; ++c) {
+                for (int c = 0; c < kChunks; c += 2) {
                     float v[32];
                     tmem_ld_32x32b_x32(tr + 32 * c, v);
-                    if (c == kChunks - 1) release();
-                    epi.chunk(v, buf, lane, c);
-                    __syncwarp();
+                    epi.template chunk<0>(v, buf, lane, c);
+                    tmem_ld_32x32b_x32(tr + 32 * c + 32, v);
+                    if (c == kChunks - 2) release();
+                    epi.template chunk<1>(v, buf, lane, c + 1);
                 }
                 epi.finish(lane);
             }
@@ -1091,21 +1129,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
                     }
                 }
 #pragma unroll
-                for (int c = 0; c < kChunks; ++c) {
-                    epi.chunk(s[c], buf, lane, c);
-                    __syncwarp();
-                }
+                for (int c = 0; c < kChunks; ++c) epi.template chunk<0>(s[c], buf, lane, c);
             } else {
                 if (!ready()) return false;
+                static_assert(kChunks == 2, "one chunk per slot");
                 const uint32_t tr = t_row();
-#pragma unroll 1
-                for (int c = 0; c < kChunks; ++c) {
-                    float v[32];
-                    tmem_ld_32x32b_x32(tr + 32 * c, v);
-                    if (c == kChunks - 1) release();
-                    epi.chunk(v, buf, lane, c);
-                    __syncwarp();
-                }
+                float v[32];
+                tmem_ld_32x32b_x32(tr, v);
+                epi.template chunk<0>(v, buf, lane, 0);
+                tmem_ld_32x32b_x32(tr + 32, v);
+                release();
+                epi.template chunk<1>(v, buf, lane, 1);
             }
             return true;
         };
