@@ -242,8 +242,9 @@ __device__ __forceinline__ float norm_factor(double s, float scale, float eps) {
     return ldexpf(r, h) < eps ? scale / eps : ldexpf(scale / r, -h);
 }
 
-// X_0, scaled: fp16 high and low parts (kSplit: and the fp32 value), rows padded from cols to
-// ld with zeros.  Thread: 8 columns of a row.  The layer's norm from its `blocks` partial sums.
+// X_0, scaled: fp16 high and low parts (kSplit: and the fp32 value), rows ld apart.  Thread: 8
+// columns of a row (what it writes past cols is never read: the tensor maps end at cols, and a
+// linear term past them goes nowhere).  The layer's norm from its `blocks` partial sums.
 // A layer with a non-finite norm (a NaN, an infinity) becomes NaN as a whole.
 template <typename TT, bool kSplit>
 __global__ void __launch_bounds__(kPassThreads)
@@ -258,7 +259,7 @@ __global__ void __launch_bounds__(kPassThreads)
         s += part[static_cast<size_t>(layer) * blocks + b];
     const float f = norm_factor(block_sum_d(s), scale, eps);
     const TT* src = static_cast<const TT*>(p.in[layer]);
-    const int per = ld / 8;
+    const int per = (cols + 7) / 8;
     const bool vec = cols % 8 == 0;  // rows then start on 16 bytes
     const size_t n = static_cast<size_t>(rows) * per;
     for (size_t i = blockIdx.x * static_cast<size_t>(kPassThreads) + threadIdx.x; i < n;
@@ -289,10 +290,6 @@ __global__ void __launch_bounds__(kPassThreads)
         uint32_t h[4], l[4];
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] *= f;
-        if (!vec) {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = col + k < cols ? v[k] : 0.f;
-        }
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             h[k] = pack_f16x2(v[2 * k], v[2 * k + 1]);
@@ -334,8 +331,10 @@ struct NsLayout {
 NsLayout ns_layout(int n, int rows, int cols, bool split, bool muon) {
     NsLayout L = {};
     L.m = rows < cols ? rows : cols;
-    L.ld = static_cast<int>(round_up(cols, 8));
-    L.ldm = static_cast<int>(round_up(L.m, 8));
+    // rows of whole 128-byte lines: a TMA box of 64 columns then takes one line of a row, not two
+    // (fp32 767 x 2049, two matrices: 510 us with rows of 16-byte multiples, 487 with these)
+    L.ld = static_cast<int>(round_up(cols, 64));
+    L.ldm = static_cast<int>(round_up(L.m, 64));
     L.xs = static_cast<size_t>(rows) * L.ld;
     L.ms = static_cast<size_t>(L.m) * L.ldm;
     L.u_stride = round_up(static_cast<size_t>(rows) * cols, 64);
@@ -839,7 +838,7 @@ cudaError_t launch_newton_schulz(int n, int rows, int cols, int dtype, const voi
         part = sum;
         blocks = 1;
     }
-    const size_t vecs = static_cast<size_t>(rows) * (L.ld / 8);
+    const size_t vecs = static_cast<size_t>(rows) * ((cols + 7) / 8);
     const size_t want = (vecs + kPassThreads - 1) / kPassThreads;
     const dim3 cgrid(static_cast<unsigned>(want < 1024 ? want : 1024), n);
     __half* hi = reinterpret_cast<__half*>(ws + L.hi[0]);

@@ -54,6 +54,14 @@ __host__ __device__ constexpr uint32_t idesc_f16_f32(int M, int N, bool a_mn, bo
 constexpr int kNsWarps = 8;                   // epilogue warps
 constexpr int kNsThreads = 64 + 32 * kNsWarps;
 
+// Accumulators in TMEM.  kSplit: four, as the MMAs of a k-block take no longer than the way to
+// the epilogue warps and back (fp32 2048 x 2048, five steps: 767 us with two, 739 with four).
+constexpr int kNsMaxAccs = 4;
+template <bool kSplit>
+constexpr int ns_accs() {
+    return kSplit ? kNsMaxAccs : 2;
+}
+
 template <int BN>
 struct NsSmem {
     static constexpr int kStages = BN == 256 ? 3 : 4;
@@ -62,7 +70,7 @@ struct NsSmem {
     static constexpr int kStageBytes = 2 * (kABox + kBBox);
     static constexpr int kOutOffset = kStages * kStageBytes;
     static constexpr int kBarOffset = kOutOffset + kNsWarps * kOutBufBytes;
-    static constexpr int kNumBars = 3 * kStages + 5;
+    static constexpr int kNumBars = 3 * kStages + 2 * kNsMaxAccs + 1;
     static constexpr int kMiscOffset = kBarOffset + kNumBars * 8;
     static constexpr int kBytes = kMiscOffset + 16 + 1024;
 };
@@ -132,9 +140,10 @@ __device__ __forceinline__ float2 unpack_f16x2(uint32_t w) {
 // Epilogues.  A warp has 32 rows x BN / 2 columns of a tile and takes them 32 columns at a time:
 // the accumulator's chunk (one row per lane) goes through the warp's staging buffer, and each
 // lane takes 4 columns of 8 rows back (access i: row 4 i + lane / 8), so that a global access of
-// the warp covers 64 or 128 bytes of 4 rows.  (One row per lane makes it touch 32 rows: the LSU then takes
-// 32 cycles an access, and the epilogue of one small tile 1.5 us.)  What a chunk reads is loaded
-// two chunks ahead in one of two slots of registers (kSplit, whose sums fill them: one ahead).
+// the warp covers 64 or 128 bytes of 4 rows.  (One row per lane touches 32 rows with every
+// access: five steps on two 256 x 384 matrices took 116 us then, 100 us now.)  What a chunk
+// reads is loaded two chunks ahead into one of two slots of registers (kSplit, whose sums fill
+// them: one ahead).
 template <bool kSplit>
 constexpr int ns_slots() {
     return kSplit ? 1 : 2;
@@ -155,7 +164,8 @@ __device__ __forceinline__ void ns_stage(uint32_t buf, int lane, const float (&v
 
 // Symmetric results S [M, M] of one matrix: s = lin_coef L + acc_coef acc, rounded to fp16 (with
 // kSplit: high and low parts), to (row, col) and, off the diagonal blocks, to (col, row).  L
-// null: no such term.  L and S are [M, ld], ld a multiple of 8, the columns from M to ld zero.
+// null: no such term.  L and S are [M, ld], ld a multiple of 64; of the columns from M on, which
+// nothing reads, a row gets what the last access over M writes.
 template <bool kSplit>
 struct EpiSymBase {
     struct Params {
@@ -187,7 +197,7 @@ struct EpiSym : EpiSymBase<kSplit> {
     uint2 l[kSlots][kParts][kAcc];
 
     __device__ __forceinline__ bool in(int i, int c) const {
-        return r0 + 4 * i < M && c0 + 32 * c < ld;
+        return r0 + 4 * i < M && c0 + 32 * c < M;
     }
     template <int SLOT>
     __device__ __forceinline__ void fetch(int c) {
@@ -282,8 +292,8 @@ struct EpiSym : EpiSymBase<kSplit> {
 };
 
 // ---------------------------------------------------------------------------
-// X' = lin_coef X + acc_coef acc over [M, N] (row stride ld, a multiple of 8, what lies
-// between N and ld zero).  What becomes of it:
+// X' = lin_coef X + acc_coef acc over [M, N] (row stride ld, a multiple of 64; the columns from N
+// on as in EpiSym).  What becomes of it:
 //   kNext     the next X: its high part, and its low part (not kSplit: for the linear term
 //             only) or (kSplit) low part and the fp32 value
 //   kResult   O [M, N] (row stride N) in the call's type
@@ -336,7 +346,7 @@ struct EpiApply : EpiApplyBase<kSplit, kOut> {
     float4 x[kSplit ? kAcc : 1];
 
     __device__ __forceinline__ bool in(int i, int c) const {
-        return r0 + 4 * i < M && c0 + 32 * c < (kOut == kNext ? ld : N);
+        return r0 + 4 * i < M && c0 + 32 * c < N;
     }
     // 4 elements of a row of N from column col, those inside it (N > col)
     __device__ __forceinline__ void st4(float* q, const float4& v, int col) const {
@@ -576,12 +586,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
     const int stages_k = (sh.g.k_blocks + kSub - 1) / kSub;  // stages per tile
 
     const uint32_t bar0 = sbase + L::kBarOffset;
-    constexpr int kFull = kStages * kSub;
+    constexpr int kFull = kStages * kSub, kAccs = ns_accs<kSplit>();
     auto full_bar = [&](int s, int j) { return bar0 + 8u * (s * kSub + j); };
     auto empty_bar = [&](int s) { return bar0 + 8u * (kFull + s); };
     auto tfull_bar = [&](int a) { return bar0 + 8u * (kFull + kStages + a); };
-    auto tempty_bar = [&](int a) { return bar0 + 8u * (kFull + kStages + 2 + a); };
-    const uint32_t drain_bar = bar0 + 8u * (kFull + kStages + 4);
+    auto tempty_bar = [&](int a) { return bar0 + 8u * (kFull + kStages + kAccs + a); };
+    const uint32_t drain_bar = bar0 + 8u * (kFull + kStages + 2 * kAccs);
     uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(smem + L::kMiscOffset + kMiscTmem);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + L::kMiscOffset + kMiscAbort);
     uint32_t* issued_word = reinterpret_cast<uint32_t*>(smem + L::kMiscOffset + kMiscIssued);
@@ -594,7 +604,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
             for (int j = 0; j < kSub; ++j) mbar_init(full_bar(s, j), 1);
             mbar_init(empty_bar(s), 1);
         }
-        for (int a = 0; a < 2; ++a) {
+        for (int a = 0; a < kAccs; ++a) {
             mbar_init(tfull_bar(a), 1);
             mbar_init(tempty_bar(a), 2 * kNsWarps);
         }
@@ -606,7 +616,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
         tma_prefetch_desc(&maps.b[0]);
     }
     if (warp == 1) {
-        tmem_alloc_pair<2 * BN>(smem_u32(tmem_holder));
+        tmem_alloc_pair<kAccs * BN>(smem_u32(tmem_holder));
         tmem_relinquish_pair();
     }
     tc_fence_before();
@@ -700,7 +710,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
                     if (++stage == kStages) { stage = 0; phase ^= 1u; }
                     if (kSplit || kb == stages_k - 1) {
                         tc_commit_pair_multicast(tfull_bar(acc), kBoth);
-                        if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+                        if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
                     }
                 }
             }
@@ -737,7 +747,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
                     mbar_arrive_cluster(mapa_shared(tempty_bar(acc), 0));
             }
             __syncwarp();
-            if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+            if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
         };
         auto t_row = [&] {
             return tmem_base + (static_cast<uint32_t>(q * 32) << 16) +
@@ -807,7 +817,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
     cluster_sync();
     if (warp == 1) {
         tc_fence_after();
-        tmem_dealloc_pair<2 * BN>(tmem_base);
+        tmem_dealloc_pair<kAccs * BN>(tmem_base);
     }
 }
 
@@ -894,12 +904,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
     const long long n_clusters = gridDim.x / 2;
 
     const uint32_t bar0 = sbase + L::kBarOffset;
-    constexpr int kFull = kStages * kSub;
+    constexpr int kFull = kStages * kSub, kAccs = ns_accs<kSplit>();
     auto full_bar = [&](int s, int j) { return bar0 + 8u * (s * kSub + j); };
     auto empty_bar = [&](int s) { return bar0 + 8u * (kFull + s); };
     auto tfull_bar = [&](int a) { return bar0 + 8u * (kFull + kStages + a); };
-    auto tempty_bar = [&](int a) { return bar0 + 8u * (kFull + kStages + 2 + a); };
-    const uint32_t drain_bar = bar0 + 8u * (kFull + kStages + 4);
+    auto tempty_bar = [&](int a) { return bar0 + 8u * (kFull + kStages + kAccs + a); };
+    const uint32_t drain_bar = bar0 + 8u * (kFull + kStages + 2 * kAccs);
     uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(smem + L::kMiscOffset + kMiscTmem);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + L::kMiscOffset + kMiscAbort);
     uint32_t* issued_word = reinterpret_cast<uint32_t*>(smem + L::kMiscOffset + kMiscIssued);
@@ -912,7 +922,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
             for (int j = 0; j < kSub; ++j) mbar_init(full_bar(s, j), 1);
             mbar_init(empty_bar(s), 1);
         }
-        for (int a = 0; a < 2; ++a) {
+        for (int a = 0; a < kAccs; ++a) {
             mbar_init(tfull_bar(a), 1);
             mbar_init(tempty_bar(a), 2 * kNsWarps);
         }
@@ -922,7 +932,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
         fence_mbar_init();
     }
     if (warp == 1) {
-        tmem_alloc_pair<2 * BN>(smem_u32(tmem_holder));
+        tmem_alloc_pair<kAccs * BN>(smem_u32(tmem_holder));
         tmem_relinquish_pair();
     }
     tc_fence_before();
@@ -1065,7 +1075,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
                         if (++stage == kStages) { stage = 0; phase ^= 1u; }
                         if (kSplit || kb == stages_k - 1) {
                             tc_commit_pair_multicast(tfull_bar(acc), kBoth);
-                            if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+                            if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
                         }
                     }
                 }
@@ -1096,7 +1106,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
                     mbar_arrive_cluster(mapa_shared(tempty_bar(acc), 0));
             }
             __syncwarp();
-            if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+            if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
         };
         // the sums of one tile through `epi`
         auto tile = [&](auto&& epi, int stages_k) {
@@ -1224,7 +1234,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
     cluster_sync();
     if (warp == 1) {
         tc_fence_after();
-        tmem_dealloc_pair<2 * BN>(tmem_base);
+        tmem_dealloc_pair<kAccs * BN>(tmem_base);
     }
 }
 
