@@ -332,7 +332,8 @@ int32_t fpo_layernorm(int64_t T, int64_t d, int32_t dtype, const void* x, const 
                       const void* beta, float eps, void* y, float* mean_out, float* rstd_out,
                       void* stream);
 
-/* Bytes of workspace fpo_layernorm_vjp needs for dgamma / dbeta (0 on invalid sizes). */
+/* Bytes of workspace fpo_layernorm_vjp needs for dgamma / dbeta: 0 for short batches (at most
+ * 32 to 256 rows, the more the shorter the rows), and on invalid sizes. */
 size_t fpo_layernorm_vjp_workspace(int64_t T, int64_t d, int32_t dtype);
 
 /*
@@ -350,8 +351,9 @@ size_t fpo_layernorm_vjp_workspace(int64_t T, int64_t d, int32_t dtype);
  * g, x, g_out [T, d] and gamma [d] in dtype; gamma NULL: ones.  dgamma, dbeta [d] fp32.
  * Each output may be NULL (not all three).  g_out may not overlap g or x (FPO_ERR_ARG
  * where it is either).  The weight sums are added in a fixed order that depends on T and d only
- * (repeat calls give identical bits).  workspace: fpo_layernorm_vjp_workspace() bytes, 256-byte aligned,
- * not read or needed when dgamma and dbeta are both NULL; it holds no status word.
+ * (repeat calls give identical bits).  workspace: fpo_layernorm_vjp_workspace() bytes,
+ * 256-byte aligned; may be NULL where that is 0 and when dgamma and dbeta are both NULL; it
+ * holds no status word.
  * T = 0 sets dgamma and dbeta to zero.  Types, sizes and alignment as fpo_layernorm.
  */
 int32_t fpo_layernorm_vjp(int64_t T, int64_t d, int32_t dtype, const void* g, const void* x,

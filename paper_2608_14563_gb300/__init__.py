@@ -549,7 +549,9 @@ def layernorm_vjp(g, x, gamma, g_out, *, eps=1e-5, min_rms=0.5, dgamma=None, dbe
     _expect(dgamma, (d,), torch.float32, "dgamma")
     _expect(dbeta, (d,), torch.float32, "dbeta")
     if workspace is None and (dgamma is not None or dbeta is not None):
-        workspace = _workspace(layernorm_vjp_workspace(T, d, _dtype_code(x)), x.device)
+        need = layernorm_vjp_workspace(T, d, _dtype_code(x))
+        if need:  # (0: a short batch)
+            workspace = _workspace(need, x.device)
     rc = _lib.fpo_layernorm_vjp(T, d, _dtype_code(x), _ptr(g), _ptr(x), _ptr(gamma), float(eps),
                                 float(min_rms), _ptr(g_out), _ptr(dgamma), _ptr(dbeta),
                                 _ptr(workspace), 0 if workspace is None else _nbytes(workspace),

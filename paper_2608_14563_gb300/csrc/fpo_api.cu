@@ -883,8 +883,7 @@ int32_t fpo_layernorm(int64_t T, int64_t d, int32_t dtype, const void* x, const 
 size_t fpo_layernorm_vjp_workspace(int64_t T, int64_t d, int32_t dtype) {
     if (ln_check(T, d, dtype) != FPO_OK) return 0;
     return align_up(layernorm_vjp_floats(dtype, static_cast<int>(T), static_cast<int>(d)) *
-                        sizeof(float) +
-                    1);
+                    sizeof(float));
 }
 
 int32_t fpo_layernorm_vjp(int64_t T, int64_t d, int32_t dtype, const void* g, const void* x,
@@ -900,8 +899,8 @@ int32_t fpo_layernorm_vjp(int64_t T, int64_t d, int32_t dtype, const void* g, co
         return FPO_ERR_ALIGN;
     if (g_out && (g_out == g || g_out == x)) return FPO_ERR_ARG;
     if (dgamma || dbeta) {
-        if (!workspace || workspace_bytes < fpo_layernorm_vjp_workspace(T, d, dtype))
-            return FPO_ERR_WORKSPACE;
+        const size_t need = fpo_layernorm_vjp_workspace(T, d, dtype);
+        if (need > 0 && (!workspace || workspace_bytes < need)) return FPO_ERR_WORKSPACE;
         if ((reinterpret_cast<uintptr_t>(workspace) % kAlign) != 0) return FPO_ERR_ALIGN;
     }
     rc = check_arch();

@@ -7,13 +7,14 @@
 //             g_out = (u - mean(u) - xhat mean(u (.) xhat)) / max(sigma, min_rms)
 //             dgamma = sum_t g_t (.) xhat_t,  dbeta = sum_t g_t
 //
-// Rows of up to 8192 elements stay in a block's registers and are read once: the variance is the sum of squares around the row's own mean (a difference of two large
-// sums would lose it), and the backward pass forms mu and sigma again from the row that it
-// has to read anyway, so no statistics are saved between the passes.  A row's next vectors
-// are loaded before the reductions of the one at hand.  Each thread keeps the same columns
-// for every row of its block, so the weight sums stay in its registers until the last row;
-// the blocks' sums are then added in block order by a second kernel (no atomics: repeat calls
-// give identical bits).  Longer rows go through the row in several passes, and their weight
+// Rows of up to 8192 elements stay in a block's registers and are read once: the variance is
+// the sum of squares around the row's own mean (a difference of two large sums would lose it),
+// and the backward pass forms mu and sigma again from the row that it has to read anyway, so no
+// statistics are saved between the passes.  A row's next vectors are loaded before the
+// reductions of the one at hand.  Each thread keeps the same columns for every row of its
+// block, so the weight sums stay in its registers until the last row; the blocks' sums are then
+// added in block order by a second kernel, or in a short batch within its one cluster (no
+// atomics: repeat calls give identical bits).  Longer rows go through the row in several passes, and their weight
 // sums through a kernel of their own.
 //
 // Bound: HBM.
@@ -22,6 +23,7 @@
 #include <math.h>
 
 #include "internal.h"
+#include "ptx.cuh"
 
 namespace fpo {
 namespace {
@@ -260,13 +262,21 @@ __global__ void __launch_bounds__(ln_threads<TH>(), ln_min_blocks<TH, false>())
     }
 }
 
-// part (kSums only): [grid][2][d] sums of g xhat and of g over the block's rows.
-template <typename TT, int VEC, int NV, int TH, bool kSums>
+// What becomes of the sums of g xhat and of g:
+//   kPartSums     every block's to part[grid][2][d]; layernorm_cols_final_kernel adds them
+//   kClusterSums  the grid is one cluster, whose blocks add each other's from shared memory, in
+//                 block order, and write dgamma and dbeta: one launch and no workspace
+enum LnSums { kNoSums = 0, kPartSums = 1, kClusterSums = 2 };
+constexpr int kLnCluster = 8;
+
+template <typename TT, int VEC, int NV, int TH, int kMode>
 __global__ void __launch_bounds__(ln_threads<TH>(), ln_min_blocks<TH, true>())
     layernorm_vjp_kernel(const TT* __restrict__ g, const TT* __restrict__ x,
                          const TT* __restrict__ gamma, int T, int d, float eps, float min_rms,
-                         TT* __restrict__ out, float* __restrict__ part) {
+                         TT* __restrict__ out, float* __restrict__ part,
+                         float* __restrict__ dgamma, float* __restrict__ dbeta) {
     using P = RowPart<TT, VEC, NV, TH>;
+    constexpr bool kSums = kMode != kNoSums;
     constexpr int kPairs = P::kPairs, kW = TH / 32;
     __shared__ float sh[ln_rows<TH>()][2][2][kW];
     const int group = threadIdx.x / TH;
@@ -339,10 +349,11 @@ __global__ void __launch_bounds__(ln_threads<TH>(), ln_min_blocks<TH, true>())
         if (out) P::store(out + row * d, t, d, u);
     }
     if constexpr (kSums) {
-        float* p = part + static_cast<size_t>(blockIdx.x) * 2 * d;
+        constexpr int kCols = NV * TH * VEC;
+        __shared__ float tot[kMode == kClusterSums ? 2 * kCols : 1];
+        float* p = kMode == kClusterSums ? tot : part + static_cast<size_t>(blockIdx.x) * 2 * d;
         if constexpr (ln_rows<TH>() > 1) {
             // the block's row groups hold the same columns: their sums in group order
-            constexpr int kCols = NV * TH * VEC;
             __shared__ float acc[ln_rows<TH>()][kCols];
 #pragma unroll
             for (int which = 0; which < 2; ++which) {
@@ -372,6 +383,22 @@ __global__ void __launch_bounds__(ln_threads<TH>(), ln_min_blocks<TH, true>())
                         p[which * d + (e / VEC * TH + t) * VEC + e % VEC] = e % 2 ? z[e / 2].y
                                                                                 : z[e / 2].x;
             }
+        }
+        if constexpr (kMode == kClusterSums) {
+            __syncwarp();
+            cluster_sync();
+            for (int k = blockIdx.x * ln_threads<TH>() + threadIdx.x; k < 2 * d;
+                 k += kLnCluster * ln_threads<TH>()) {
+                const uint32_t at = smem_u32(tot + k);
+                float a = 0.f;
+#pragma unroll
+                for (int r = 0; r < kLnCluster; ++r)
+                    a += __uint_as_float(ld_shared_cluster_u32(mapa_shared(at, r)));
+                float* dst = k < d ? dgamma : dbeta;
+                if (dst) dst[k < d ? k : k - d] = a;
+            }
+            __syncwarp();
+            cluster_sync();  // until every block has read this one's
         }
     }
 }
@@ -587,6 +614,14 @@ int vjp_blocks(int T, const RowForm& f) {
     const int want = T / rows + (T % rows != 0);
     return want < cap ? want : cap;
 }
+// Short batches: all of it on one cluster, in at most kLnClusterRounds rounds over the blocks'
+// row groups.  bf16 200 x 256, 4 rounds: a call takes 7.7 us, 16.2 on the two kernels with a
+// fresh workspace (4.8 and 3.7 us on the GPU, in a graph); at 8 rounds (512 x 256) 8.4 and
+// 16.5, but 6.8 and 4.1 on the GPU.
+constexpr int kLnClusterRounds = 4;
+bool one_cluster(int T, const RowForm& f) {
+    return f.nv != 0 && f.th != 512 && T <= kLnClusterRounds * kLnCluster * (256 / f.th);
+}
 constexpr int kLongRanges = 64;
 int long_ranges(int T) { return T < kLongRanges ? T : kLongRanges; }
 
@@ -672,17 +707,39 @@ cudaError_t run_vjp(const void* g, const void* x, const void* gamma, int T, int 
         e = launch_chained(layernorm_cols_kernel<TT>,
                            dim3((d + kColThreads - 1) / kColThreads, parts), kColThreads, 0, st, gg,
                            xx, static_cast<const float2*>(stats), T, d, ws);
+    } else if (sums && one_cluster(T, f)) {
+        return with_form<TT, VEC>(f, [&](auto nv, auto th) {
+            constexpr int NV = decltype(nv)::value, TH = decltype(th)::value;
+            if constexpr (TH != 512) {
+                cudaLaunchConfig_t cfg = {};
+                cfg.gridDim = dim3(kLnCluster, 1, 1);
+                cfg.blockDim = dim3(ln_threads<TH>(), 1, 1);
+                cfg.stream = st;
+                cudaLaunchAttribute at[1];
+                at[0].id = cudaLaunchAttributeClusterDimension;
+                at[0].val.clusterDim.x = kLnCluster;
+                at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+                cfg.attrs = at;
+                cfg.numAttrs = 1;
+                note_launch();
+                return cudaLaunchKernelEx(&cfg, layernorm_vjp_kernel<TT, VEC, NV, TH, kClusterSums>,
+                                          gg, xx, ww, T, d, eps, min_rms, oo,
+                                          static_cast<float*>(nullptr), dgamma, dbeta);
+            } else {
+                return cudaErrorInvalidValue;  // (one_cluster)
+            }
+        });
     } else {
         parts = vjp_blocks(T, f);
         e = with_form<TT, VEC>(f, [&](auto nv, auto th) {
             constexpr int NV = decltype(nv)::value, TH = decltype(th)::value;
             if (sums)
-                layernorm_vjp_kernel<TT, VEC, NV, TH, true><<<parts, ln_threads<TH>(), 0, st>>>(
-                    gg, xx, ww, T, d, eps, min_rms, oo, ws),
+                layernorm_vjp_kernel<TT, VEC, NV, TH, kPartSums><<<parts, ln_threads<TH>(), 0, st>>>(
+                    gg, xx, ww, T, d, eps, min_rms, oo, ws, nullptr, nullptr),
                     note_launch();
             else
-                layernorm_vjp_kernel<TT, VEC, NV, TH, false><<<parts, ln_threads<TH>(), 0, st>>>(
-                    gg, xx, ww, T, d, eps, min_rms, oo, nullptr),
+                layernorm_vjp_kernel<TT, VEC, NV, TH, kNoSums><<<parts, ln_threads<TH>(), 0, st>>>(
+                    gg, xx, ww, T, d, eps, min_rms, oo, nullptr, nullptr, nullptr),
                     note_launch();
             return cudaGetLastError();
         });
@@ -699,6 +756,7 @@ size_t layernorm_vjp_floats(int dtype, int T, int d) {
     const RowForm f = dtype == 1   ? row_form<__nv_bfloat16, 8>(d)
                       : d % 4 == 0 ? row_form<float, 4>(d)
                                    : row_form<float, 1>(d);
+    if (one_cluster(T, f)) return 0;
     const size_t stats = f.nv == 0 ? 2 * static_cast<size_t>(T) : 0;
     const size_t parts = f.nv == 0 ? long_ranges(T) : vjp_blocks(T, f);
     return stats + parts * 2 * static_cast<size_t>(d);

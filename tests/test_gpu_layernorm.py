@@ -106,6 +106,32 @@ def test_backward_matches_the_definition(fpo, dtype, T, d, min_rms):
     assert torch.equal(dg, dg2) and torch.equal(db, db2)
 
 
+@pytest.mark.parametrize("dtype,d", [("f32", 33), ("f32", 512), ("f32", 2047), ("bf16", 64),
+                                     ("bf16", 2048), ("bf16", 4096)])
+def test_weight_sums_of_short_batches(fpo, dtype, d):
+    """Batches on both sides of the largest that one cluster takes (no workspace), a block's rows
+    and one more: dgamma and dbeta as the definition's, either one alone the same bits."""
+    limit = 1
+    while fpo.layernorm_vjp_workspace(limit + 1, d, 1 if dtype == "bf16" else 0) == 0:
+        limit += 1
+    assert limit >= 32
+    for T in (1, 2, 9, limit - 1, limit, limit + 1):
+        x, gamma, beta, g = inputs(dtype, T, d, seed=T)
+        ref = definition(x, gamma, beta, g, 0.5)
+        dg, db = (torch.full((d,), float("nan"), device="cuda") for _ in range(2))
+        out = torch.empty_like(x)
+        fpo.layernorm_vjp(g, x, gamma, out, eps=EPS, dgamma=dg, dbeta=db)
+        sigma = 1 / ref["rstd"][:, None]
+        xh = (x.double() - ref["mean"][:, None]) / sigma
+        off = 1 + x.double().abs().amax(1, keepdim=True) / sigma
+        close(dg, ref["dgamma"], 2.0 ** -24, (g.double() * (xh.abs() + 1) * off).abs().sum(0))
+        close(db, ref["dbeta"], 2.0 ** -24, ref["sbeta"])
+        dg1, db1, out1 = torch.empty_like(dg), torch.empty_like(db), torch.empty_like(x)
+        fpo.layernorm_vjp(g, x, gamma, out1, eps=EPS, dgamma=dg1)
+        fpo.layernorm_vjp(g, x, gamma, None, eps=EPS, dbeta=db1)
+        assert torch.equal(dg, dg1) and torch.equal(db, db1) and torch.equal(out, out1)
+
+
 @pytest.mark.parametrize("T,d", [(3, 7), (4, 96)])
 def test_backward_matches_differences(fpo, T, d):
     """g_out, dgamma and dbeta are the derivatives of <g, layernorm(x)>: fourth-order central
@@ -179,10 +205,10 @@ def test_large_offset_keeps_the_variance(fpo):
     assert ((rstd.double() - want) / want).abs().max() < 1e-5
 
 
-def test_repeat_calls_other_streams_and_graphs(fpo):
+@pytest.mark.parametrize("T, d", [(999, 1032), (60, 1032)])
+def test_repeat_calls_other_streams_and_graphs(fpo, T, d):
     """Same bits from repeat calls, a side stream, two graphs that share a workspace (replayed
-    one after the other), and replays on new inputs."""
-    T, d = 999, 1032
+    one after the other), and replays on new inputs.  (60 rows: no workspace.)"""
     x, gamma, beta, g = inputs("bf16", T, d)
     x2, _, _, g2 = inputs("bf16", T, d, seed=9)
     ws = torch.empty(fpo.layernorm_vjp_workspace(T, d), dtype=torch.uint8, device="cuda")
