@@ -701,7 +701,9 @@ int32_t fpo_orthogonalize_grouped(int32_t n_layers, int64_t rows, int64_t cols, 
     if (rc != FPO_OK) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     unsigned* status = static_cast<unsigned*>(workspace);
-    FPO_TRY(cudaMemsetAsync(status, 0, 2 * sizeof(unsigned), st));  // and the phase counter
+    FPO_TRY(cudaMemsetAsync(status, 0,
+                            ns_clear_bytes(n_layers, static_cast<int>(rows), static_cast<int>(cols),
+                                           dtype, false), st));
     const NsTarget to{O, nullptr, 0.f, 0.f};
     return cuda_status(launch_newton_schulz(n_layers, static_cast<int>(rows), static_cast<int>(cols),
                                             dtype, G, nullptr, eps, steps, co, to, workspace, status,
@@ -724,7 +726,7 @@ int32_t fpo_layer_muon_grouped(int32_t n_layers, int64_t T, int64_t d, int64_t d
     float co[3 * kNsMaxSteps];
     rc = ns_coeffs(opt->steps, opt->coeffs, opt->eps, co);
     if (rc != FPO_OK) return rc;
-    if (!std::isfinite(opt->lr) || !std::isfinite(opt->scale) || !std::isfinite(opt->weight_decay) ||
+    if (!std::isfinite(opt->lr * opt->scale) || !std::isfinite(opt->lr * opt->weight_decay) ||
         !(opt->momentum >= 0.f && opt->momentum < 1.f) || (opt->nesterov != 0 && opt->nesterov != 1))
         return FPO_ERR_ARG;
     if (!W_master || !momentum || (T > 0 && (!g || !A))) return FPO_ERR_NULL;
@@ -745,8 +747,8 @@ int32_t fpo_layer_muon_grouped(int32_t n_layers, int64_t T, int64_t d, int64_t d
     if (rc != FPO_OK) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     unsigned* status = static_cast<unsigned*>(workspace);
-    FPO_TRY(cudaMemsetAsync(status, 0, 2 * sizeof(unsigned), st));  // and the phase counter
     const int Ti = static_cast<int>(T), di = static_cast<int>(d), fi = static_cast<int>(d_ff);
+    FPO_TRY(cudaMemsetAsync(status, 0, ns_clear_bytes(n_layers, di, fi, dtype, true), st));
     // G_l = g_l^T A_l: with the momentum for bf16, else (fp32) into the update buffers
     NsMomentum mom{momentum, opt->momentum, opt->nesterov != 0, nullptr, nullptr, Ti};
     float* G[FPO_MAX_GROUPED_LAYERS];

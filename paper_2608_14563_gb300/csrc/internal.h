@@ -305,6 +305,8 @@ struct NsTarget {
 // Whether finite coefficients (3 per step) keep the iteration's bounds in range.
 bool ns_coeffs_ok(int steps, const float* coeffs);
 size_t ns_workspace_bytes(int n, int rows, int cols, int dtype, bool muon);
+// Bytes at the workspace's start (status word, counters) that are zero before a call.
+size_t ns_clear_bytes(int n, int rows, int cols, int dtype, bool muon);
 float* ns_update_buffer(void* ws, int n, int rows, int cols, int dtype, int layer);
 // n matrices [rows, cols] (G in dtype, or mom) through `steps` iterations.  dtype 0 = fp32,
 // 1 = bf16 (cols a multiple of 8).

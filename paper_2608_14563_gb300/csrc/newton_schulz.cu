@@ -325,8 +325,26 @@ size_t norm_parts(int rows, int cols, bool muon) {
 struct NsLayout {
     int m, ld, ldm;              // the smaller side, row strides of X and of A, B
     size_t xs, ms;               // elements of one layer's X, A
+    size_t counts, slots;        // split: of the products' ranges (NsShape)
     size_t part, sum, U, u_stride, hi[2], lo[2], x32, A[2], B[2], total;
+    size_t clear;                // bytes from the start to be zero before a call
 };
+
+// Tiles of one matrix of a kSplit product [M, N], and the ranges that their k-blocks are split
+// into: as many as half of the 76 clusters hold of one matrix, of 16 k-blocks or more.  It goes
+// by the matrix's sizes only, so that its result does not depend on the group.  Five steps, with
+// and without: 767 x 2049 one matrix 334 and 387 us, two 414 and 465, eight 1129 and 1116; eight
+// 256 x 4096 432 and 610, eight 512 x 2048 645 and 593; two 64 x 8192 239 and 695.  (Ranges of 8
+// k-blocks: eight 512 x 1024 413 instead of 354.)
+long long ns_matrix_tiles(int M, int N, bool tri) {
+    const long long mb = (M + 255) / 256;
+    return tri ? mb * (mb + 1) : mb * ((N + 127) / 128);
+}
+int ns_splits(long long tiles, int K) {
+    const long long clusters = 38 / tiles, blocks = (K + kBK - 1) / kBK / 16;
+    const long long s = clusters < blocks ? clusters : blocks;
+    return s < 1 ? 1 : static_cast<int>(s);
+}
 
 NsLayout ns_layout(int n, int rows, int cols, bool split, bool muon) {
     NsLayout L = {};
@@ -344,6 +362,23 @@ NsLayout ns_layout(int n, int rows, int cols, bool split, bool muon) {
         at += round_up(bytes, 256);
         return o;
     };
+    L.clear = 2 * sizeof(unsigned);  // the status word and the chain kernel's counter
+    if (split) {
+        const long long sym = ns_matrix_tiles(L.m, L.m, true), app = ns_matrix_tiles(rows, cols, false);
+        long long tiles = 0, units = 0;  // of the products that are split
+        auto product = [&](long long t, int K) {
+            const int s = ns_splits(t, K);
+            if (s == 1) return;
+            if (t > tiles) tiles = t;
+            if (t * s > units) units = t * s;
+        };
+        product(sym, rows < cols ? cols : rows);
+        product(sym, L.m);
+        product(app, L.m);
+        L.counts = take(n * tiles * 2 * kNsWarps * sizeof(unsigned));
+        L.clear = at;
+        L.slots = take(n * units * (kPairBM * 128 * sizeof(float)));
+    }
     const size_t x = n * L.xs * 2, a = n * L.ms * 2;
     L.part = take(static_cast<size_t>(n) * norm_parts(rows, cols, muon) * sizeof(double));
     L.sum = take(static_cast<size_t>(n) * sizeof(double));
@@ -425,9 +460,16 @@ int resident_clusters(int threads, int smem_bytes, int sm_count) {
     return n;
 }
 
+// Where the ranges of a kSplit product leave their sums.
+struct NsRanges {
+    float* slots;
+    unsigned* counts;
+};
+
 template <int BN, bool A_MN, bool B_MN, bool kSplit, class Epi>
 cudaError_t launch_ns(const typename Epi::Maps& maps, const typename Epi::Params& ep, int M, int N,
-                      int K, int groups, bool tri, unsigned* status, cudaStream_t st) {
+                      int K, int groups, bool tri, const NsRanges& rg, unsigned* status,
+                      cudaStream_t st) {
     using S = NsSmem<BN>;
     constexpr auto kern = ns_gemm_kernel<BN, A_MN, B_MN, kSplit, Epi>;
     cudaError_t e = set_smem_limit<kern>(S::kBytes);
@@ -448,8 +490,12 @@ cudaError_t launch_ns(const typename Epi::Maps& maps, const typename Epi::Params
         tri ? static_cast<long long>(sh.g.m_blocks) * (sh.g.m_blocks + 1) / 2 * (kPairBM / BN)
             : static_cast<long long>(sh.g.m_blocks) * sh.g.n_blocks;
     sh.g.tiles = groups * per;
+    sh.splits = kSplit ? ns_splits(per, K) : 1;
+    sh.slots = rg.slots;
+    sh.counts = rg.counts;
     const int max_clusters = resident_clusters<kern>(kNsThreads, S::kBytes, di.sm_count);
-    const long long clusters = sh.g.tiles < max_clusters ? sh.g.tiles : max_clusters;
+    const long long units = sh.g.tiles * sh.splits;
+    const long long clusters = units < max_clusters ? units : max_clusters;
     return launch_chained(kern, dim3(static_cast<unsigned>(2 * clusters)), kNsThreads, S::kBytes, st,
                           maps, ep, sh, status, wait_limit_ns());
 }
@@ -457,7 +503,8 @@ cudaError_t launch_ns(const typename Epi::Maps& maps, const typename Epi::Params
 // One batch of GEMMs, C[M, N] = sum_k A B over K, on the pair kernel with 256 x BN tiles.
 template <int BN, bool A_MN, bool B_MN, bool kSplit, class Epi>
 cudaError_t run_ns_tiles(const NsOperand& A, const NsOperand& B, const typename Epi::Params& ep,
-                         int M, int N, int K, bool tri, unsigned* status, cudaStream_t st) {
+                         int M, int N, int K, bool tri, const NsRanges& rg, unsigned* status,
+                         cudaStream_t st) {
     NsMaps maps;
     for (int h = 0; h < 2; ++h) {
         if (h == 1 && !kSplit) {
@@ -467,23 +514,24 @@ cudaError_t run_ns_tiles(const NsOperand& A, const NsOperand& B, const typename 
             return cudaErrorInvalidValue;
         }
     }
-    return launch_ns<BN, A_MN, B_MN, kSplit, Epi>(maps, ep, M, N, K, A.n, tri, status, st);
+    return launch_ns<BN, A_MN, B_MN, kSplit, Epi>(maps, ep, M, N, K, A.n, tri, rg, status, st);
 }
 
 // fp32 calls on 128-column tiles.  fp16 ones too where twice as many tiles still have a cluster
 // each: an epilogue is then half as long.
 template <bool A_MN, bool B_MN, bool kSplit, template <int> class Epi>
 cudaError_t run_ns(const NsOperand& A, const NsOperand& B, const typename Epi<128>::Params& ep, int M,
-                   int N, int K, bool tri, unsigned* status, cudaStream_t st) {
+                   int N, int K, bool tri, const NsRanges& rg, unsigned* status, cudaStream_t st) {
     if constexpr (!kSplit) {
         DevInfo di;
         if (!current_device_info(&di)) return cudaErrorUnknown;
         const long long mb = (M + 255) / 256, nb = (N + 255) / 256;
         const long long tiles = A.n * (tri ? mb * (mb + 1) / 2 : mb * nb);
         if (4 * tiles > di.sm_count)
-            return run_ns_tiles<256, A_MN, B_MN, kSplit, Epi<256>>(A, B, ep, M, N, K, tri, status, st);
+            return run_ns_tiles<256, A_MN, B_MN, kSplit, Epi<256>>(A, B, ep, M, N, K, tri, rg, status,
+                                                                     st);
     }
-    return run_ns_tiles<128, A_MN, B_MN, kSplit, Epi<128>>(A, B, ep, M, N, K, tri, status, st);
+    return run_ns_tiles<128, A_MN, B_MN, kSplit, Epi<128>>(A, B, ep, M, N, K, tri, rg, status, st);
 }
 
 template <bool kSplit>
@@ -534,12 +582,17 @@ double quad_max(double b, double c, double t1) {
 // rounding adds to a bound stays far below the other half.
 int scale_exp(double bound) { return 15 - static_cast<int>(ceil(log2(bound))); }
 
+NsRanges ns_ranges(const NsLayout& L, uint8_t* ws) {
+    return {reinterpret_cast<float*>(ws + L.slots), reinterpret_cast<unsigned*>(ws + L.counts)};
+}
+
 // X' = a X + B X (tall: a X + X B) and what becomes of it; ep holds the coefficients and targets.
 template <bool kSplit, int kOut>
 cudaError_t run_apply(const NsOperand& X, const NsOperand& B, bool tall, const NsLayout& L, uint8_t* ws,
                       int cur, bool next_lo, typename EpiApplyBase<kSplit, kOut>::Params& ep,
                       unsigned* status, cudaStream_t st) {
     const int rows = X.outer, cols = X.inner;
+    const NsRanges rg = ns_ranges(L, ws);
     ep.s.hi = X.p[0];
     ep.s.lo = reinterpret_cast<__half*>(ws + L.lo[cur]);
     ep.s.next_hi = reinterpret_cast<__half*>(ws + L.hi[cur ^ 1]);
@@ -552,9 +605,10 @@ cudaError_t run_apply(const NsOperand& X, const NsOperand& B, bool tall, const N
     // wide: B X with B K-major and X MN-major; tall: X B, both K-major (B is symmetric)
     if (tall)
         return run_ns<false, false, kSplit, ApplyOf<kSplit, kOut>::template T>(X, B, ep, rows, cols,
-                                                                              cols, false, status, st);
+                                                                              cols, false, rg, status,
+                                                                              st);
     return run_ns<false, true, kSplit, ApplyOf<kSplit, kOut>::template T>(B, X, ep, rows, cols, rows,
-                                                                         false, status, st);
+                                                                         false, rg, status, st);
 }
 
 // The coefficients of every product with the powers of two that X, A and B are stored with: X_k
@@ -590,6 +644,7 @@ template <bool kSplit, int kOut>
 cudaError_t run_steps(const NsLayout& L, uint8_t* ws, int n, int rows, int cols, int steps,
                       const NsChainStep* co, void* const* O, unsigned* status, cudaStream_t st) {
     const bool tall = rows > cols;
+    const NsRanges rg = ns_ranges(L, ws);
     auto at = [&](size_t off) { return reinterpret_cast<__half*>(ws + off); };
     const NsOperand A = {{at(L.A[0]), at(L.A[1])}, L.m, L.m, n, L.ldm, L.ms};
     const NsOperand B = {{at(L.B[0]), at(L.B[1])}, L.m, L.m, n, L.ldm, L.ms};
@@ -605,9 +660,9 @@ cudaError_t run_steps(const NsLayout& L, uint8_t* ws, int n, int rows, int cols,
         sp.out[1] = at(L.A[1]);
         sp.acc_coef = co[k].a_acc;
         cudaError_t e = tall ? run_ns<true, true, kSplit, SymOf<kSplit>::template T>(
-                                   X, X, sp, L.m, L.m, rows, true, status, st)
+                                   X, X, sp, L.m, L.m, rows, true, rg, status, st)
                              : run_ns<false, false, kSplit, SymOf<kSplit>::template T>(
-                                   X, X, sp, L.m, L.m, cols, true, status, st);
+                                   X, X, sp, L.m, L.m, cols, true, rg, status, st);
         if (e != cudaSuccess) return e;
         // B = b A + c A^2
         sp.lin[0] = at(L.A[0]);
@@ -616,7 +671,7 @@ cudaError_t run_steps(const NsLayout& L, uint8_t* ws, int n, int rows, int cols,
         sp.out[1] = at(L.B[1]);
         sp.lin_coef = co[k].b_lin;
         sp.acc_coef = co[k].b_acc;
-        e = run_ns<false, false, kSplit, SymOf<kSplit>::template T>(A, A, sp, L.m, L.m, L.m, true,
+        e = run_ns<false, false, kSplit, SymOf<kSplit>::template T>(A, A, sp, L.m, L.m, L.m, true, rg,
                                                                     status, st);
         if (e != cudaSuccess) return e;
         // X' = a X + B X
@@ -643,47 +698,37 @@ cudaError_t run_steps(const NsLayout& L, uint8_t* ws, int n, int rows, int cols,
 }
 
 // The same in one launch.
-template <bool kSplit, int kOut>
+template <int kOut>
 cudaError_t run_chain(const NsLayout& L, uint8_t* ws, int n, int rows, int cols, int steps,
                       const NsChainStep* co, void* const* O, long long tiles, unsigned* status,
                       cudaStream_t st) {
-    constexpr auto kern = ns_chain_kernel<kSplit, kOut>;
+    constexpr auto kern = ns_chain_kernel<kOut>;
     using S = NsSmem<128>;
     const bool tall = rows > cols;
     auto at = [&](size_t off) { return reinterpret_cast<__half*>(ws + off); };
-    NsChainParams<kSplit, kOut> p = {};
-    const NsOperand A = {{at(L.A[0]), at(L.A[1])}, L.m, L.m, n, L.ldm, L.ms};
-    const NsOperand B = {{at(L.B[0]), at(L.B[1])}, L.m, L.m, n, L.ldm, L.ms};
-    bool ok = true;
+    NsChainParams<kOut> p = {};
+    const NsOperand A = {{at(L.A[0]), nullptr}, L.m, L.m, n, L.ldm, L.ms};
+    const NsOperand B = {{at(L.B[0]), nullptr}, L.m, L.m, n, L.ldm, L.ms};
+    bool ok = ns_map(&p.map[1][0][0], A, 0, false, 128) && ns_map(&p.map[1][0][1], A, 0, false, 64);
+    p.map[1][1][0] = p.map[1][0][0];
+    p.map[1][1][1] = p.map[1][0][1];
     for (int cur = 0; cur < 2; ++cur) {
-        const NsOperand X = {{at(L.hi[cur]), at(L.lo[cur])}, cols, rows, n, L.ld, L.xs};
-        for (int h = 0; h < (kSplit ? 2 : 1); ++h) {
-            ok = ok && ns_map(&p.map[0][cur][0][h], X, h, tall, 128) &&
-                 ns_map(&p.map[0][cur][1][h], X, h, tall, 64);
-            if (cur == 0)
-                ok = ok && ns_map(&p.map[1][0][0][h], A, h, false, 128) &&
-                     ns_map(&p.map[1][0][1][h], A, h, false, 64);
-            else
-                for (int o = 0; o < 2; ++o) p.map[1][1][o][h] = p.map[1][0][o][h];
-            if (tall)
-                ok = ok && ns_map(&p.map[2][cur][0][h], X, h, false, 128) &&
-                     ns_map(&p.map[2][cur][1][h], B, h, false, 64);
-            else
-                ok = ok && ns_map(&p.map[2][cur][0][h], B, h, false, 128) &&
-                     ns_map(&p.map[2][cur][1][h], X, h, true, 64);
-        }
+        const NsOperand X = {{at(L.hi[cur]), nullptr}, cols, rows, n, L.ld, L.xs};
+        ok = ok && ns_map(&p.map[0][cur][0], X, 0, tall, 128) &&
+             ns_map(&p.map[0][cur][1], X, 0, tall, 64) &&
+             ns_map(&p.map[2][cur][0], tall ? X : B, 0, false, 128) &&
+             ns_map(&p.map[2][cur][1], tall ? B : X, 0, !tall, 64);
     }
     if (!ok) return cudaErrorInvalidValue;
-    p.ap.x32 = kSplit ? reinterpret_cast<float*>(ws + L.x32) : nullptr;
     p.ap.stride = static_cast<long long>(L.xs);
     p.ap.M = rows;
     p.ap.N = cols;
     p.ap.ld = L.ld;
-    set_target<kSplit, kOut>(p.ap, n, O);
+    set_target<false, kOut>(p.ap, n, O);
     for (int k = 0; k < steps; ++k) p.step[k] = co[k];
+    p.A = at(L.A[0]);
+    p.B = at(L.B[0]);
     for (int h = 0; h < 2; ++h) {
-        p.A[h] = at(L.A[h]);
-        p.B[h] = at(L.B[h]);
         p.hi[h] = at(L.hi[h]);
         p.lo[h] = at(L.lo[h]);
     }
@@ -719,18 +764,21 @@ cudaError_t run_iteration(const NsLayout& L, uint8_t* ws, int n, int rows, int c
     NsChainStep co[kNsMaxSteps];
     if (steps > kNsMaxSteps) return cudaErrorInvalidValue;
     ns_steps(steps, coeffs, co);
-    // 256 x 128 tiles of the products, and the clusters that hold one each
-    const long long mb = (L.m + 255) / 256;
-    const long long sym = n * mb * (mb + 1);
-    const long long app = static_cast<long long>(n) * ((rows + 255) / 256) * ((cols + 127) / 128);
-    const long long tiles = sym > app ? sym : app;
-    constexpr auto kern = ns_chain_kernel<kSplit, kOut>;
-    const cudaError_t e = set_smem_limit<kern>(NsSmem<128>::kBytes);
-    if (e != cudaSuccess) return e;
-    DevInfo di;
-    if (!current_device_info(&di)) return cudaErrorUnknown;
-    if (tiles <= resident_clusters<kern>(kNsThreads, NsSmem<128>::kBytes, di.sm_count))
-        return run_chain<kSplit, kOut>(L, ws, n, rows, cols, steps, co, O, tiles, status, st);
+    // fp16, with a cluster for every 256 x 128 tile: one launch.  (Two 256 x 384 matrices, five
+    // steps: 107 us, 115 a launch per product; four 1024 x 1024 with two tiles to a cluster 268
+    // and 273, one 2048 x 2048 292 and 281.  fp32 products are longer and lose by it: two
+    // 512 x 1024 matrices 288 and 265.)
+    if constexpr (!kSplit) {
+        const long long sym = n * ns_matrix_tiles(L.m, L.m, true),
+                        app = n * ns_matrix_tiles(rows, cols, false), tiles = sym > app ? sym : app;
+        constexpr auto kern = ns_chain_kernel<kOut>;
+        const cudaError_t e = set_smem_limit<kern>(NsSmem<128>::kBytes);
+        if (e != cudaSuccess) return e;
+        DevInfo di;
+        if (!current_device_info(&di)) return cudaErrorUnknown;
+        if (tiles <= resident_clusters<kern>(kNsThreads, NsSmem<128>::kBytes, di.sm_count))
+            return run_chain<kOut>(L, ws, n, rows, cols, steps, co, O, tiles, status, st);
+    }
     return run_steps<kSplit, kOut>(L, ws, n, rows, cols, steps, co, O, status, st);
 }
 
@@ -770,9 +818,9 @@ cudaError_t run_momentum(int n, int T, int rows, int cols, const NsMomentum& mom
     ep.n_blocks = narrow ? (cols + 127) / 128 : (cols + 255) / 256;
     *parts = ep.m_blocks * ep.n_blocks * 2 * kNsWarps;
     if (narrow)
-        return launch_ns<128, true, true, false, EpiMomentum<128>>(maps, ep, rows, cols, T, n, false,
+        return launch_ns<128, true, true, false, EpiMomentum<128>>(maps, ep, rows, cols, T, n, false, {},
                                                                    status, st);
-    return launch_ns<256, true, true, false, EpiMomentum<256>>(maps, ep, rows, cols, T, n, false,
+    return launch_ns<256, true, true, false, EpiMomentum<256>>(maps, ep, rows, cols, T, n, false, {},
                                                                status, st);
 }
 
@@ -793,6 +841,10 @@ bool ns_coeffs_ok(int steps, const float* coeffs) {
 
 size_t ns_workspace_bytes(int n, int rows, int cols, int dtype, bool muon) {
     return ns_layout(n, rows, cols, dtype == 0, muon).total;
+}
+
+size_t ns_clear_bytes(int n, int rows, int cols, int dtype, bool muon) {
+    return ns_layout(n, rows, cols, dtype == 0, muon).clear;
 }
 
 float* ns_update_buffer(void* ws, int n, int rows, int cols, int dtype, int layer) {

@@ -78,6 +78,13 @@ struct NsSmem {
 struct NsShape {
     GemmShape g;   // M, N, K, blocks; tiles of all matrices
     bool tri;      // only tiles that reach under or onto the diagonal (M = N)
+    // kSplit: a tile's k-blocks in `splits` ranges of their own units (unit u: range u % splits of
+    // tile u / splits).  With splits > 1 every warp of a unit leaves its sums in slots[unit][CTA]
+    // [warp], and the last of a tile to arrive at counts[tile][CTA][warp] (zero before and
+    // after) adds them in the ranges' order and goes on to the epilogue: none waits.
+    int splits;
+    float* slots;
+    unsigned* counts;
 };
 
 struct NsMaps {
@@ -583,7 +590,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
     const bool leader = rank == 0;
     const long long cluster = blockIdx.x / 2;
     const long long n_clusters = gridDim.x / 2;
-    const int stages_k = (sh.g.k_blocks + kSub - 1) / kSub;  // stages per tile
+    const int tile_k = (sh.g.k_blocks + kSub - 1) / kSub;  // stages per tile
+    const int splits = kSplit ? sh.splits : 1;
+    const long long units = sh.g.tiles * splits;
+    // first stage of a unit's range
+    auto first_k = [&](long long u, int add) {
+        if (splits == 1) return add * tile_k;
+        return static_cast<int>((u % splits + add) * tile_k / splits);
+    };
 
     const uint32_t bar0 = sbase + L::kBarOffset;
     constexpr int kFull = kStages * kSub, kAccs = ns_accs<kSplit>();
@@ -634,12 +648,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
             int stage = 0;
             uint32_t phase = 0, issued = 0;
             bool ok = true;
-            for (long long t = cluster; ok && t < sh.g.tiles; t += n_clusters) {
+            for (long long u = cluster; ok && u < units; u += n_clusters) {
                 int g, mb, nb;
-                ns_tile<BN>(t, sh, g, mb, nb);
+                ns_tile<BN>(u / splits, sh, g, mb, nb);
                 const int a_row = mb * kPairBM + 128 * static_cast<int>(rank);
                 const int b_row = nb * BN + (BN / 2) * static_cast<int>(rank);
-                for (int kb = 0; kb < stages_k; ++kb) {
+                const int k1 = first_k(u, 1);
+                for (int kb = first_k(u, 0); kb < k1; ++kb) {
                     if (!mbar_wait_cl(empty_bar(stage), phase ^ 1u, guard)) { ok = false; break; }
                     const uint32_t sa = sbase + stage * L::kStageBytes, sb = sa + 2 * L::kABox;
 #pragma unroll
@@ -667,8 +682,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
             int stage = 0, acc = 0;
             uint32_t phase = 0, acc_phase = 0;
             bool ok = true, issued_any = false;
-            for (long long t = cluster; ok && t < sh.g.tiles; t += n_clusters) {
-                for (int kb = 0; kb < stages_k; ++kb) {
+            for (long long u = cluster; ok && u < units; u += n_clusters) {
+                const int k1 = first_k(u, 1);
+                for (int kb = first_k(u, 0); kb < k1; ++kb) {
                     if (kSplit || kb == 0) {
                         if (!mbar_wait_cl(tempty_bar(acc), acc_phase ^ 1u, guard)) {
                             ok = false;
@@ -708,7 +724,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
                     issued_any = true;
                     tc_commit_pair_multicast(empty_bar(stage), kBoth);
                     if (++stage == kStages) { stage = 0; phase ^= 1u; }
-                    if (kSplit || kb == stages_k - 1) {
+                    if (kSplit || kb == k1 - 1) {
                         tc_commit_pair_multicast(tfull_bar(acc), kBoth);
                         if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
                     }
@@ -755,7 +771,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
         };
         constexpr int kChunks = kWarpCols / 32;
         bool ok = true;
-        for (long long t = cluster; ok && t < sh.g.tiles; t += n_clusters) {
+        for (long long u = cluster; ok && u < units; u += n_clusters) {
+            const long long t = u / splits;
             int g, mb, nb;
             ns_tile<BN>(t, sh, g, mb, nb);
             const int row0 = mb * kPairBM + 128 * static_cast<int>(rank) + 32 * q;
@@ -767,7 +784,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
                 for (int c = 0; c < kChunks; ++c)
 #pragma unroll
                     for (int j = 0; j < 32; ++j) s[c][j] = 0.f;
-                for (int kb = 0; ok && kb < stages_k; ++kb) {
+                const int k1 = first_k(u, 1);
+                for (int kb = first_k(u, 0); ok && kb < k1; ++kb) {
                     ok = ready();
                     if (!ok) break;
                     const uint32_t tr = t_row();
@@ -781,6 +799,38 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
                     }
                 }
                 if (!ok) break;
+                if (splits > 1) {
+                    constexpr int kWarpSums = kChunks * 32 * 32;
+                    const int w = static_cast<int>(rank) * kNsWarps + warp - 2;
+                    float* mine = sh.slots + (u * 2 * kNsWarps + w) * kWarpSums + lane;
+#pragma unroll
+                    for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) mine[(c * 32 + j) * 32] = s[c][j];
+                    __threadfence();
+                    __syncwarp();
+                    unsigned* count = sh.counts + t * 2 * kNsWarps + w;
+                    unsigned before = 0;
+                    if (lane == 0) before = atomicAdd(count, 1u);
+                    before = __shfl_sync(0xffffffffu, before, 0);
+                    if (before + 1 != static_cast<unsigned>(splits)) continue;
+                    __threadfence();
+                    if (lane == 0) *count = 0;
+#pragma unroll
+                    for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) s[c][j] = 0.f;
+                    const float* from =
+                        sh.slots + (t * splits * 2 * kNsWarps + w) * kWarpSums + lane;
+                    for (int r = 0; r < splits; ++r) {
+#pragma unroll
+                        for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+                            for (int j = 0; j < 32; ++j)
+                                s[c][j] += __ldcg(from + (c * 32 + j) * 32);
+                        from += 2 * kNsWarps * kWarpSums;
+                    }
+                }
                 Epi epi(ep, g, row0, col0, lane, mirror);
 #pragma unroll
                 for (int c = 0; c < kChunks; ++c) epi.template chunk<0>(s[c], buf, lane, c);
@@ -822,8 +872,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
 }
 
 // ---------------------------------------------------------------------------
-// The whole iteration in one launch, for batches whose products have at most one 256 x 128 tile
-// per resident cluster: there a launch per product (15 of them) costs 7 us each, most of it
+// The whole iteration in one launch, for fp16 batches whose products have at most one 256 x 128
+// tile per resident cluster: there a launch per product (15 of them) costs 7 us each, most of it
 // set-up, the wait for the kernel before and the first operand's way in.  The roles walk the
 // products ("phases": A, B, X of every step) with one counter in global memory between them:
 // every block adds one when its stores of a phase are done, and the producers and epilogues of
@@ -836,14 +886,13 @@ struct NsChainStep {
 };
 constexpr int kNsMaxSteps = 32;
 
-template <bool kSplit, int kOut>
+template <int kOut>
 struct NsChainParams {
-    // operands of the phases: [A, B, X][X buffer][A operand, B operand][high, low]
-    CUtensorMap map[3][2][2][kSplit ? 2 : 1];
-    typename EpiApplyBase<kSplit, kOut>::Params ap;  // of the last step (s unused)
+    CUtensorMap map[3][2][2];  // operands of the phases: [A, B, X][X buffer][A operand, B operand]
+    typename EpiApplyBase<false, kOut>::Params ap;  // of the last step (s unused)
     NsChainStep step[kNsMaxSteps];
-    __half* A[2];
-    __half* B[2];
+    __half* A;
+    __half* B;
     __half* hi[2];
     __half* lo[2];
     long long ms;            // elements of one A
@@ -881,15 +930,14 @@ __device__ __forceinline__ void fence_proxy_async_global() {
     asm volatile("fence.proxy.async.global;" ::: "memory");
 }
 
-template <bool kSplit, int kOut>
+template <int kOut>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
-    ns_chain_kernel(const __grid_constant__ NsChainParams<kSplit, kOut> p, unsigned int* status,
+    ns_chain_kernel(const __grid_constant__ NsChainParams<kOut> p, unsigned int* status,
                     unsigned long long wait_limit_ns) {
     constexpr int BN = 128;
     using L = NsSmem<BN>;
     constexpr int kStages = L::kStages;
-    constexpr int kSub = kSplit ? 1 : 2;
-    constexpr int kParts = kSplit ? 2 : 1;
+    constexpr int kSub = 2;
     constexpr uint16_t kBoth = 0x3;
 
     extern __shared__ uint8_t smem_raw[];
@@ -904,7 +952,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
     const long long n_clusters = gridDim.x / 2;
 
     const uint32_t bar0 = sbase + L::kBarOffset;
-    constexpr int kFull = kStages * kSub, kAccs = ns_accs<kSplit>();
+    constexpr int kFull = kStages * kSub, kAccs = ns_accs<false>();
     auto full_bar = [&](int s, int j) { return bar0 + 8u * (s * kSub + j); };
     auto empty_bar = [&](int s) { return bar0 + 8u * (kFull + s); };
     auto tfull_bar = [&](int a) { return bar0 + 8u * (kFull + kStages + a); };
@@ -975,7 +1023,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
                 if (cluster >= sh.g.tiles) continue;
                 if (!ns_wait_count(p.count, f * arrivals, guard)) break;
                 fence_proxy_async_global();
-                const CUtensorMap(&mp)[2][kParts] = p.map[f % 3][(f / 3) & 1];
+                const CUtensorMap(&mp)[2] = p.map[f % 3][(f / 3) & 1];
                 const bool a_mn = f % 3 == 0 && p.tall;
                 const bool b_mn = f % 3 == 0 ? p.tall : f % 3 == 2 && !p.tall;
                 const int stages_k = (sh.g.k_blocks + kSub - 1) / kSub;
@@ -989,20 +1037,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
                         const uint32_t sa = sbase + stage * L::kStageBytes, sb = sa + 2 * L::kABox;
 #pragma unroll
                         for (int j = 0; j < 2; ++j) {
-                            const int bar_j = kSplit ? 0 : j, part = kSplit ? j : 0;
-                            const uint32_t fb = mapa_shared(full_bar(stage, bar_j), 0);
-                            if (leader && (!kSplit || j == 0))
-                                mbar_arrive_expect_tx(full_bar(stage, bar_j),
+                            const uint32_t fb = mapa_shared(full_bar(stage, j), 0);
+                            if (leader)
+                                mbar_arrive_expect_tx(full_bar(stage, j),
                                                       2 * (L::kStageBytes / kSub));
-                            const int k0 = (kSplit ? kb : 2 * kb + j) * kBK;
+                            const int k0 = (2 * kb + j) * kBK;
                             if (a_mn)
-                                ns_load<true, 128>(&mp[0][part], sa + j * L::kABox, fb, a_row, k0, g);
+                                ns_load<true, 128>(&mp[0], sa + j * L::kABox, fb, a_row, k0, g);
                             else
-                                ns_load<false, 128>(&mp[0][part], sa + j * L::kABox, fb, a_row, k0, g);
+                                ns_load<false, 128>(&mp[0], sa + j * L::kABox, fb, a_row, k0, g);
                             if (b_mn)
-                                ns_load<true, BN / 2>(&mp[1][part], sb + j * L::kBBox, fb, b_row, k0, g);
+                                ns_load<true, BN / 2>(&mp[1], sb + j * L::kBBox, fb, b_row, k0, g);
                             else
-                                ns_load<false, BN / 2>(&mp[1][part], sb + j * L::kBBox, fb, b_row, k0, g);
+                                ns_load<false, BN / 2>(&mp[1], sb + j * L::kBBox, fb, b_row, k0, g);
                         }
                         ++issued;
                         if (++stage == kStages) { stage = 0; phase ^= 1u; }
@@ -1023,23 +1070,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
                                   bool first) {
                 constexpr bool A_MN = decltype(amn)::value, B_MN = decltype(bmn)::value;
                 constexpr uint32_t kIdesc = idesc_f16_f32(kPairBM, BN, A_MN, B_MN);
-                if constexpr (kSplit) {
 #pragma unroll
-                    for (int m = 0; m < 3; ++m) {
-#pragma unroll
-                        for (int kk = 0; kk < kBK / kUmmaK; ++kk)
-                            tc_mma_bf16_pair(d_tmem,
-                                             operand_desc<A_MN>(sa + (m == 1 ? L::kABox : 0), kk),
-                                             operand_desc<B_MN>(sb + (m == 0 ? L::kBBox : 0), kk),
-                                             kIdesc, (m != 0 || kk != 0) ? 1u : 0u);
-                    }
-                } else {
-#pragma unroll
-                    for (int kk = 0; kk < kBK / kUmmaK; ++kk)
-                        tc_mma_bf16_pair(d_tmem, operand_desc<A_MN>(sa + j * L::kABox, kk),
-                                         operand_desc<B_MN>(sb + j * L::kBBox, kk), kIdesc,
-                                         (!first || kk != 0) ? 1u : 0u);
-                }
+                for (int kk = 0; kk < kBK / kUmmaK; ++kk)
+                    tc_mma_bf16_pair(d_tmem, operand_desc<A_MN>(sa + j * L::kABox, kk),
+                                     operand_desc<B_MN>(sb + j * L::kBBox, kk), kIdesc,
+                                     (!first || kk != 0) ? 1u : 0u);
             };
             for (int f = 0; ok && f < phases; ++f) {
                 const NsShape sh = shape(f);
@@ -1047,7 +1082,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
                 const bool both_mn = f % 3 == 0 && p.tall, b_mn = f % 3 == 2 && !p.tall;
                 for (long long t = cluster; ok && t < sh.g.tiles; t += n_clusters) {
                     for (int kb = 0; kb < stages_k; ++kb) {
-                        if (kSplit || kb == 0) {
+                        if (kb == 0) {
                             if (!mbar_wait_cl(tempty_bar(acc), acc_phase ^ 1u, guard)) {
                                 ok = false;
                                 break;
@@ -1073,7 +1108,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
                         if (!ok) break;
                         tc_commit_pair_multicast(empty_bar(stage), kBoth);
                         if (++stage == kStages) { stage = 0; phase ^= 1u; }
-                        if (kSplit || kb == stages_k - 1) {
+                        if (kb == stages_k - 1) {
                             tc_commit_pair_multicast(tfull_bar(acc), kBoth);
                             if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
                         }
@@ -1109,7 +1144,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
             if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
         };
         // the sums of one tile through `epi`
-        auto tile = [&](auto&& epi, int stages_k) {
+        auto tile = [&](auto&& epi) {
             auto t_row = [&] {
                 return tmem_base + (static_cast<uint32_t>(q * 32) << 16) +
                        static_cast<uint32_t>(acc * BN + half * kWarpCols);
@@ -1120,37 +1155,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
                 tc_fence_after();
                 return true;
             };
-            if constexpr (kSplit) {
-                float s[kChunks][32];
-#pragma unroll
-                for (int c = 0; c < kChunks; ++c)
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) s[c][j] = 0.f;
-                for (int kb = 0; kb < stages_k; ++kb) {
-                    if (!ready()) return false;
-                    const uint32_t tr = t_row();
-#pragma unroll
-                    for (int c = 0; c < kChunks; ++c) {
-                        float v[32];
-                        tmem_ld_32x32b_x32(tr + 32 * c, v);
-                        if (c == kChunks - 1) release();  // it is all in registers
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) s[c][j] += v[j];
-                    }
-                }
-#pragma unroll
-                for (int c = 0; c < kChunks; ++c) epi.template chunk<0>(s[c], buf, lane, c);
-            } else {
-                if (!ready()) return false;
-                static_assert(kChunks == 2, "one chunk per slot");
-                const uint32_t tr = t_row();
-                float v[32];
-                tmem_ld_32x32b_x32(tr, v);
-                epi.template chunk<0>(v, buf, lane, 0);
-                tmem_ld_32x32b_x32(tr + 32, v);
-                release();
-                epi.template chunk<1>(v, buf, lane, 1);
-            }
+            if (!ready()) return false;
+            static_assert(kChunks == 2, "one chunk per slot");
+            const uint32_t tr = t_row();
+            float v[32];
+            tmem_ld_32x32b_x32(tr, v);
+            epi.template chunk<0>(v, buf, lane, 0);
+            tmem_ld_32x32b_x32(tr + 32, v);
+            release();
+            epi.template chunk<1>(v, buf, lane, 1);
             return true;
         };
         // the 8 warps' own barrier; all of them reach it twice in every phase, also after giving up
@@ -1162,7 +1175,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
             const NsShape sh = shape(f);
             const int k = f / 3, cur = k & 1;
             const bool last = k == p.steps - 1;
-            const int stages_k = (sh.g.k_blocks + kSub - 1) / kSub;
             // one thread of the block polls (a failure is in the abort flag); every block waits
             // here, also one without a tile: none may count for a phase ahead of time
             if (warp == 2 && lane == 0 && ok) ns_wait_count(p.count, f * arrivals, guard);
@@ -1174,39 +1186,34 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
                 const int row0 = mb * kPairBM + 128 * static_cast<int>(rank) + 32 * q;
                 const int col0 = nb * BN + half * kWarpCols;
                 if (f % 3 != 2) {
-                    typename EpiSymBase<kSplit>::Params sp;
+                    typename EpiSymBase<false>::Params sp;
                     const bool gram = f % 3 == 0;
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        sp.lin[h] = gram ? nullptr : p.A[h];
-                        sp.out[h] = gram ? p.A[h] : p.B[h];
-                    }
+                    sp.lin[0] = gram ? nullptr : p.A;
+                    sp.out[0] = gram ? p.A : p.B;
                     sp.stride = p.ms;
                     sp.M = p.m;
                     sp.ld = p.ldm;
                     sp.lin_coef = p.step[k].b_lin;
                     sp.acc_coef = gram ? p.step[k].a_acc : p.step[k].b_acc;
-                    ok = tile(EpiSym<BN, kSplit>(sp, g, row0, col0, lane, nb * BN / kPairBM != mb),
-                              stages_k);
+                    ok = tile(EpiSym<BN, false>(sp, g, row0, col0, lane, nb * BN / kPairBM != mb));
                 } else {
                     NsApplyStep st;
                     st.hi = p.hi[cur];
                     st.lo = p.lo[cur];
                     st.next_hi = p.hi[cur ^ 1];
-                    st.next_lo = kSplit || k + 2 < p.steps ? p.lo[cur ^ 1] : nullptr;
+                    st.next_lo = k + 2 < p.steps ? p.lo[cur ^ 1] : nullptr;
                     st.lin_coef = p.step[k].x_lin;
                     st.acc_coef = p.step[k].x_acc;
                     st.lin_lo = !last;
                     if (last) {
-                        ok = tile(EpiApply<BN, kSplit, kOut>(p.ap, st, g, row0, col0, lane), stages_k);
+                        ok = tile(EpiApply<BN, false, kOut>(p.ap, st, g, row0, col0, lane));
                     } else {
-                        typename EpiApplyBase<kSplit, kNext>::Params np;
-                        np.x32 = p.ap.x32;
+                        typename EpiApplyBase<false, kNext>::Params np;
                         np.stride = p.ap.stride;
                         np.M = p.rows;
                         np.N = p.cols;
                         np.ld = p.ap.ld;
-                        ok = tile(EpiApply<BN, kSplit, kNext>(np, st, g, row0, col0, lane), stages_k);
+                        ok = tile(EpiApply<BN, false, kNext>(np, st, g, row0, col0, lane));
                     }
                 }
             }
