@@ -14,8 +14,9 @@
 // reductions of the one at hand.  Each thread keeps the same columns for every row of its
 // block, so the weight sums stay in its registers until the last row; the blocks' sums are then
 // added in block order by a second kernel, or in a short batch within its one cluster (no
-// atomics: repeat calls give identical bits).  Longer rows go through the row in several passes, and their weight
-// sums through a kernel of their own.
+// atomics: repeat calls give identical bits).  Large batches of long rows go through a ring in
+// shared memory instead, with the roles on warps of their own.  Rows of more than 8192 elements
+// are read in several passes, and their weight sums by a kernel of their own.
 //
 // Bound: HBM.
 #include <cuda_bf16.h>
@@ -187,6 +188,17 @@ struct RowPart {
         return e < kE && (e / VEC * TH + t) * VEC < d;
     }
 };
+
+// An untiled bulk copy of `bytes` (a multiple of 16, both addresses on 16 bytes) to shared memory,
+// counted on `bar`.
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes,
+                                          uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::
+            "r"(dst),
+        "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(bar)
+        : "memory");
+}
 
 __device__ __forceinline__ float2 both(float a) { return make_float2(a, a); }
 
@@ -399,6 +411,398 @@ __global__ void __launch_bounds__(ln_threads<TH>(), ln_min_blocks<TH, true>())
             }
             __syncwarp();
             cluster_sync();  // until every block has read this one's
+        }
+    }
+}
+
+// ------------------------------------------------------------------ many rows
+// The backward pass of large batches of long rows.  A block's rows pass through a ring in
+// shared memory: a loader warp fills the slots with bulk copies, SW warps form the statistics
+// of a row each, and CW warps, whose threads keep the same NV vectors of columns throughout,
+// apply them in row order.  A row costs 25 shuffles and no barrier of the block; with a row's
+// sums over 256 threads (layernorm_vjp_kernel) 256 shuffles and two barriers of the block were
+// most of its time.  bf16 16384 x 4096: 67 us, 6.0 TB/s (floor 59), and 5 us for the last sums.
+//
+// The statistics take one pass, with the mean s of the row's first 32 vectors as the origin:
+//   var = mean((x - s)^2) - mean(x - s)^2,  mean(u (x - mu)) = mean(u (x - s)) - mean(x - s) mean(u)
+// With n elements in s, (s - mu)^2 <= (d / n) sigma^2 (the squares around mu of those n are part of
+// d sigma^2): the difference loses a factor of 1 + 2 d / n of its 24 bits, at most.
+//
+// Every wait is bounded.  One that runs out ends the block, which leaves NaN in the rows that it
+// did not reach and in its weight sums.
+constexpr int kLnMaxSlots = 16;
+constexpr int kLnStreamSmem = 220 * 1024;  // of dynamic shared memory: weights and slots
+
+template <int CW, int SW>
+struct LnStream {
+    static constexpr int kThreads = 32 * (CW + SW + 1);
+};
+
+__device__ __forceinline__ bool ln_wait(uint32_t bar, uint32_t parity, volatile int* lost,
+                                        uint64_t limit_ns) {
+    if (mbar_try_wait(bar, parity)) return true;
+    const uint64_t t0 = global_timer_ns();
+    while (!mbar_try_wait(bar, parity)) {
+        if (*lost) return false;
+        if (global_timer_ns() - t0 > limit_ns) {
+            *lost = 1;
+            return false;
+        }
+    }
+    return true;
+}
+
+// Mean of a row's first 32 vectors (inv_n: 1 / their elements), in every lane of the warp.
+template <typename TT, int VEC>
+__device__ __forceinline__ float ln_origin(const TT* xs, int lane, int n, float inv_n) {
+    float a = 0.f;
+    if (lane < n) {
+        float v[VEC];
+        RowVec<TT, VEC> r;
+        r.load(xs + lane * VEC);
+        r.get(v);
+#pragma unroll
+        for (int q = 0; q < VEC; ++q) a += v[q];
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
+    return a * inv_n;
+}
+
+// The loader's end: the last min(slots, filled) copies are waited for, so that the block leaves
+// none in flight.
+__device__ __forceinline__ void ln_drain(uint64_t* full, int slots, int filled, uint64_t limit_ns) {
+    for (int j = filled > slots ? filled - slots : 0; j < filled; ++j) {
+        const uint64_t t0 = global_timer_ns();
+        while (!mbar_try_wait(smem_u32(&full[j % slots]), (j / slots) & 1) &&
+               global_timer_ns() - t0 < limit_ns) {
+        }
+    }
+}
+
+// Rows of block b of `blocks`: b, b + blocks, ... below T.
+__device__ __forceinline__ int ln_block_rows(int T) {
+    return static_cast<int>((T - static_cast<long long>(blockIdx.x) + gridDim.x - 1) / gridDim.x);
+}
+__device__ __forceinline__ long long ln_block_row(int i) {
+    return blockIdx.x + static_cast<long long>(i) * gridDim.x;
+}
+
+// The forward pass: every warp takes whole rows from the ring, so a row costs it 15 shuffles and
+// no barrier of the block.
+constexpr int kLnFwdWarps = 16;
+template <typename TT, int VEC>
+__global__ void __launch_bounds__(32 * (kLnFwdWarps + 1), 1)
+    layernorm_fwd_stream_kernel(const TT* __restrict__ x, const TT* __restrict__ gamma,
+                                const TT* __restrict__ beta, int T, int d, float eps,
+                                TT* __restrict__ y, float* __restrict__ mean_out,
+                                float* __restrict__ rstd_out, int slots, uint64_t limit_ns) {
+    using V = RowVec<TT, VEC>;
+    extern __shared__ __align__(16) char ln_smem[];
+    __shared__ uint64_t full[kLnMaxSlots], empty[kLnMaxSlots];
+    __shared__ int lost_word;
+    volatile int* lost = &lost_word;
+    TT* const w_sm = reinterpret_cast<TT*>(ln_smem);
+    TT* const b_sm = w_sm + d;
+    TT* const ring = b_sm + d;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < slots; ++i) {
+            mbar_init(smem_u32(&full[i]), 1);
+            mbar_init(smem_u32(&empty[i]), 1);
+        }
+        lost_word = 0;
+        fence_mbar_init();
+    }
+    for (int k = threadIdx.x * VEC; k < d; k += 32 * (kLnFwdWarps + 1) * VEC) {
+        V v;
+        if (gamma) {
+            v.load(gamma + k);
+            *reinterpret_cast<V*>(w_sm + k) = v;
+        }
+        if (beta) {
+            v.load(beta + k);
+            *reinterpret_cast<V*>(b_sm + k) = v;
+        }
+    }
+    __syncthreads();
+    const int rows = ln_block_rows(T);
+    if (warp == kLnFwdWarps) {
+        if (lane == 0) {
+            const uint32_t bytes = static_cast<uint32_t>(d) * sizeof(TT);
+            int s = 0, i = 0;
+            uint32_t phase = 0;
+            for (; i < rows; ++i) {
+                if (i >= slots && !ln_wait(smem_u32(&empty[s]), phase ^ 1u, lost, limit_ns)) break;
+                mbar_arrive_expect_tx(smem_u32(&full[s]), bytes);
+                bulk_load(smem_u32(ring + static_cast<size_t>(s) * d), x + ln_block_row(i) * d, bytes,
+                          smem_u32(&full[s]));
+                if (++s == slots) { s = 0; phase ^= 1u; }
+            }
+            ln_drain(full, slots, i, limit_ns);
+        }
+        return;
+    }
+    const int n = d / VEC;
+    const float inv_d = 1.f / static_cast<float>(d);
+    const float inv_n = 1.f / static_cast<float>(VEC * (n < 32 ? n : 32));
+    // (a slot is always the same warp's, so its waits cannot mistake a phase)
+    const int warps = slots < kLnFwdWarps ? slots : kLnFwdWarps;
+    int i = warp < warps ? warp : rows;
+    for (; i < rows; i += warps) {
+        const int s = i % slots;
+        if (!__all_sync(0xffffffffu, ln_wait(smem_u32(&full[s]), (i / slots) & 1, lost, limit_ns)))
+            break;
+        const TT* xs = ring + static_cast<size_t>(s) * d;
+        const float origin = ln_origin<TT, VEC>(xs, lane, n, inv_n);
+        const float2 shift = both(-origin);
+        float2 a0 = both(0.f), a1 = a0;
+        for (int k = lane * VEC; k < d; k += 32 * VEC) {
+            float v[VEC];
+            V r;
+            r.load(xs + k);
+            r.get(v);
+#pragma unroll
+            for (int q = 0; q < VEC; q += 2) {
+                const float2 c = __fadd2_rn(make_float2(v[q], v[q + 1]), shift);
+                a0 = __fadd2_rn(a0, c);
+                a1 = __ffma2_rn(c, c, a1);
+            }
+        }
+        float v2[2] = {a0.x + a0.y, a1.x + a1.y};
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            v2[0] += __shfl_xor_sync(0xffffffffu, v2[0], o);
+            v2[1] += __shfl_xor_sync(0xffffffffu, v2[1], o);
+        }
+        const float off = v2[0] * inv_d, mu = origin + off;
+        const float rstd = 1.f / sqrtf(fmaxf(fmaf(-off, off, v2[1] * inv_d), 0.f) + eps);
+        const long long row = ln_block_row(i);
+        TT* yr = y + row * d;
+        const float2 m2 = both(-mu), r2 = both(rstd);
+        for (int k = lane * VEC; k < d; k += 32 * VEC) {
+            float v[VEC], wv[VEC], bv[VEC];
+            V r;
+            r.load(xs + k);
+            r.get(v);
+            if (gamma) {
+                r.load(w_sm + k);
+                r.get(wv);
+            }
+            if (beta) {
+                r.load(b_sm + k);
+                r.get(bv);
+            }
+#pragma unroll
+            for (int q = 0; q < VEC; q += 2) {
+                float2 c = __fmul2_rn(__fadd2_rn(make_float2(v[q], v[q + 1]), m2), r2);
+                const float2 w2 = gamma ? make_float2(wv[q], wv[q + 1]) : both(1.f);
+                if (beta)
+                    c = __ffma2_rn(c, w2, make_float2(bv[q], bv[q + 1]));
+                else
+                    c = __fmul2_rn(c, w2);
+                v[q] = c.x;
+                v[q + 1] = c.y;
+            }
+            V::store(yr + k, v);
+        }
+        __syncwarp();
+        if (lane == 0) {
+            mbar_arrive(smem_u32(&empty[s]));
+            if (mean_out) mean_out[row] = mu;
+            if (rstd_out) rstd_out[row] = rstd;
+        }
+    }
+    for (; i < rows && warp < warps; i += warps) {  // given up
+        const float nan = __int_as_float(0x7fffffff);
+        float v[VEC];
+#pragma unroll
+        for (int q = 0; q < VEC; ++q) v[q] = nan;
+        const long long row = ln_block_row(i);
+        for (int k = lane * VEC; k < d; k += 32 * VEC) V::store(y + row * d + k, v);
+        if (lane == 0) {
+            if (mean_out) mean_out[row] = nan;
+            if (rstd_out) rstd_out[row] = nan;
+        }
+    }
+}
+
+template <typename TT, int VEC, int NV, int CW, int SW, bool kSums>
+__global__ void __launch_bounds__(LnStream<CW, SW>::kThreads, 1)
+    layernorm_vjp_stream_kernel(const TT* __restrict__ g, const TT* __restrict__ x,
+                                const TT* __restrict__ gamma, int T, int d, float eps,
+                                float min_rms, TT* __restrict__ out, float* __restrict__ part,
+                                int slots, uint64_t limit_ns) {
+    using P = RowPart<TT, VEC, NV, 32 * CW>;
+    using V = RowVec<TT, VEC>;
+    constexpr int kPairs = P::kPairs;
+    extern __shared__ __align__(16) char ln_smem[];
+    __shared__ uint64_t full[kLnMaxSlots], ready[kLnMaxSlots], empty[kLnMaxSlots];
+    __shared__ float stat[kLnMaxSlots][5];  // mu, 1 / sigma, mean u, mean(u xhat), prefactor
+    __shared__ int lost_word;
+    volatile int* lost = &lost_word;
+    grid_dependency_trigger();
+    TT* const w_sm = reinterpret_cast<TT*>(ln_smem);
+    TT* const ring = w_sm + d;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < slots; ++i) {
+            mbar_init(smem_u32(&full[i]), 1);
+            mbar_init(smem_u32(&ready[i]), 1);
+            mbar_init(smem_u32(&empty[i]), CW);
+        }
+        lost_word = 0;
+        fence_mbar_init();
+    }
+    if (gamma)
+        for (int k = threadIdx.x * VEC; k < d; k += LnStream<CW, SW>::kThreads * VEC) {
+            V v;
+            v.load(gamma + k);
+            *reinterpret_cast<V*>(w_sm + k) = v;
+        }
+    __syncthreads();
+    const int rows = ln_block_rows(T);
+    auto slot_x = [&](int s) { return ring + static_cast<size_t>(2 * s) * d; };
+
+    if (warp == CW + SW) {
+        // ----------------------------------------------------------------- loader
+        if (lane == 0) {
+            const uint32_t bytes = static_cast<uint32_t>(d) * sizeof(TT);
+            int s = 0, i = 0;
+            uint32_t phase = 0;
+            for (; i < rows; ++i) {
+                if (i >= slots && !ln_wait(smem_u32(&empty[s]), phase ^ 1u, lost, limit_ns)) break;
+                const uint32_t bar = smem_u32(&full[s]);
+                mbar_arrive_expect_tx(bar, 2 * bytes);
+                bulk_load(smem_u32(slot_x(s)), x + ln_block_row(i) * d, bytes, bar);
+                bulk_load(smem_u32(slot_x(s) + d), g + ln_block_row(i) * d, bytes, bar);
+                if (++s == slots) { s = 0; phase ^= 1u; }
+            }
+            ln_drain(full, slots, i, limit_ns);
+        }
+        __syncwarp();
+    } else if (warp >= CW) {
+        // ----------------------------------------------------------------- statistics
+        const int n = d / VEC;  // vectors of a row
+        const float inv_d = 1.f / static_cast<float>(d);
+        const float inv_n = 1.f / static_cast<float>(VEC * (n < 32 ? n : 32));
+        const int stride = SW < slots ? SW : slots;
+        for (int i = warp - CW < stride ? warp - CW : rows; i < rows; i += stride) {
+            const int s = i % slots, p = i / slots;
+            // A wait tells a phase from the one before it only: the slot's last row has to be
+            // gone first.  (That wait is at most one phase ahead in turn, the columns being in
+            // row order and stride <= slots.)
+            const bool in_time =
+                (p == 0 || ln_wait(smem_u32(&empty[s]), (p - 1) & 1, lost, limit_ns)) &&
+                ln_wait(smem_u32(&full[s]), p & 1, lost, limit_ns);
+            if (!__all_sync(0xffffffffu, in_time)) break;
+            const TT *xs = slot_x(s), *gs = xs + d;
+            const float origin = ln_origin<TT, VEC>(xs, lane, n, inv_n);
+            const float2 shift = both(-origin);
+            float2 a0 = both(0.f), a1 = a0, a2 = a0, a3 = a0;
+            for (int k = lane * VEC; k < d; k += 32 * VEC) {
+                float xv[VEC], gv[VEC], wv[VEC];
+                V r;
+                r.load(xs + k);
+                r.get(xv);
+                r.load(gs + k);
+                r.get(gv);
+                if (gamma) {
+                    r.load(w_sm + k);
+                    r.get(wv);
+                }
+#pragma unroll
+                for (int q = 0; q < VEC; q += 2) {
+                    const float2 c = __fadd2_rn(make_float2(xv[q], xv[q + 1]), shift);
+                    float2 u = make_float2(gv[q], gv[q + 1]);
+                    if (gamma) u = __fmul2_rn(u, make_float2(wv[q], wv[q + 1]));
+                    a0 = __fadd2_rn(a0, c);
+                    a1 = __ffma2_rn(c, c, a1);
+                    a2 = __fadd2_rn(a2, u);
+                    a3 = __ffma2_rn(u, c, a3);
+                }
+            }
+            float v[4] = {a0.x + a0.y, a1.x + a1.y, a2.x + a2.y, a3.x + a3.y};
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+            }
+            if (lane == 0) {
+                const float off = v[0] * inv_d, um = v[2] * inv_d;
+                const float var = fmaxf(fmaf(-off, off, v[1] * inv_d), 0.f);
+                const float sigma = sqrtf(var + eps), rstd = 1.f / sigma;
+                stat[s][0] = origin + off;
+                stat[s][1] = rstd;
+                stat[s][2] = um;
+                stat[s][3] = fmaf(-off, um, v[3] * inv_d) * rstd;
+                stat[s][4] = 1.f / fmaxf(sigma, min_rms);
+                mbar_arrive(smem_u32(&ready[s]));
+            }
+            __syncwarp();
+        }
+    } else {
+        // ----------------------------------------------------------------- columns
+        const int t = threadIdx.x;
+        P w;
+        if (gamma) w.load(gamma, t, d);
+        float2 dg[kSums ? kPairs : 1], db[kSums ? kPairs : 1];
+#pragma unroll
+        for (int i = 0; i < (kSums ? kPairs : 1); ++i) dg[i] = db[i] = both(0.f);
+        int s = 0, i = 0;
+        uint32_t phase = 0;
+        for (; i < rows; ++i) {
+            const bool in_time = ln_wait(smem_u32(&full[s]), phase, lost, limit_ns) &&
+                                 ln_wait(smem_u32(&ready[s]), phase, lost, limit_ns);
+            if (!__all_sync(0xffffffffu, in_time)) break;
+            P xr, gr;
+            xr.load(slot_x(s), t, d);
+            gr.load(slot_x(s) + d, t, d);
+            const float mu = stat[s][0], rstd = stat[s][1], um = stat[s][2], cm = stat[s][3],
+                        pref = stat[s][4];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&empty[s]));  // all of it is in registers
+            if (++s == slots) { s = 0; phase ^= 1u; }
+            float2 c[kPairs], gv[kPairs], wf[kPairs];
+            xr.get(c);
+            gr.get(gv);
+            if (gamma) w.get(wf);
+            const float2 m2 = both(-mu), r2 = both(rstd), nu = both(-um), nc = both(-cm),
+                         p2 = both(pref);
+#pragma unroll
+            for (int k = 0; k < kPairs; ++k) {
+                c[k] = __fmul2_rn(__fadd2_rn(c[k], m2), r2);  // xhat
+                if constexpr (kSums) {
+                    dg[k] = __ffma2_rn(gv[k], c[k], dg[k]);
+                    db[k] = __fadd2_rn(db[k], gv[k]);
+                }
+                const float2 u = gamma ? __fmul2_rn(gv[k], wf[k]) : gv[k];
+                c[k] = __fmul2_rn(__ffma2_rn(c[k], nc, __fadd2_rn(u, nu)), p2);
+            }
+            if (out) P::store(out + ln_block_row(i) * d, t, d, c);
+        }
+        if (i < rows) {  // given up
+            const float nan = __int_as_float(0x7fffffff);
+            float2 f[kPairs];
+#pragma unroll
+            for (int k = 0; k < kPairs; ++k) f[k] = both(nan);
+            if (out)
+                for (; i < rows; ++i) P::store(out + ln_block_row(i) * d, t, d, f);
+#pragma unroll
+            for (int k = 0; k < (kSums ? kPairs : 1); ++k) dg[k] = db[k] = f[0];
+        }
+        if constexpr (kSums) {
+            float* p = part + static_cast<size_t>(blockIdx.x) * 2 * d;
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                const int k = (v * 32 * CW + t) * VEC;
+                if (k >= d) continue;
+#pragma unroll
+                for (int q = 0; q < VEC; q += 2) {
+                    *reinterpret_cast<float2*>(p + k + q) = dg[(v * VEC + q) / 2];
+                    *reinterpret_cast<float2*>(p + d + k + q) = db[(v * VEC + q) / 2];
+                }
+            }
         }
     }
 }
@@ -622,6 +1026,20 @@ constexpr int kLnClusterRounds = 4;
 bool one_cluster(int T, const RowForm& f) {
     return f.nv != 0 && f.th != 512 && T <= kLnClusterRounds * kLnCluster * (256 / f.th);
 }
+// Many long rows of 16-byte vectors: the stream kernels, a block to an SM.  Backward (us, stream
+// kernel and register kernel): bf16 16384 x 4096 72 and 90, 16384 x 2560 66 and 84, 8192 x 8192
+// 87 and 95, 300 x 4096 11 and 18; fp32 8192 x 4096 67 and 175, 16384 x 2048 71 and 73; rows of 4 KB
+// come out even (bf16 16384 x 2048 50 and 48), shorter ones worse (32768 x 1024 81 and 46).
+bool streamed(int T, int d, int vec, int esz) {
+    return vec > 1 && T >= 256 && d * esz > 4096 && d <= 8192;
+}
+// Forward: where a row leaves threads of the register kernel without elements.  bf16 8192 x 5120
+// 33 and 50 us, 16384 x 2560 34 and 40, fp32 8192 x 4096 47 and 59; full ones: bf16 16384 x
+// 4096 48 and 47, fp32 4096 x 8192 60 and 46, and 1024 x 4096 6.5 and 4.3.
+bool fwd_streamed(int T, int d, int vec, int esz, const RowForm& f) {
+    return T >= 4096 && d * esz > 4096 && d < f.nv * f.th * vec;
+}
+int stream_blocks(int T) { return T < 152 ? T : 152; }
 constexpr int kLongRanges = 64;
 int long_ranges(int T) { return T < kLongRanges ? T : kLongRanges; }
 
@@ -670,6 +1088,19 @@ cudaError_t run_fwd(const void* x, const void* gamma, const void* beta, int T, i
             note_launch();
         return cudaGetLastError();
     }
+    if constexpr (VEC > 1) {
+        if (fwd_streamed(T, d, VEC, sizeof(TT), f)) {
+            constexpr auto kern = layernorm_fwd_stream_kernel<TT, VEC>;
+            const cudaError_t e = set_smem_limit<kern>(kLnStreamSmem);
+            if (e != cudaSuccess) return e;
+            const int row = d * static_cast<int>(sizeof(TT)), fit = kLnStreamSmem / row - 2;
+            const int slots = fit < kLnMaxSlots ? fit : kLnMaxSlots;
+            kern<<<stream_blocks(T), 32 * (kLnFwdWarps + 1), (slots + 2) * row, st>>>(
+                xx, gg, bb, T, d, eps, yy, mean_out, rstd_out, slots, wait_limit_ns()),
+                note_launch();
+            return cudaGetLastError();
+        }
+    }
     return with_form<TT, VEC>(f, [&](auto nv, auto th) {
         constexpr int NV = decltype(nv)::value, TH = decltype(th)::value;
         const int blocks = T / ln_rows<TH>() + (T % ln_rows<TH>() != 0);
@@ -707,6 +1138,36 @@ cudaError_t run_vjp(const void* g, const void* x, const void* gamma, int T, int 
         e = launch_chained(layernorm_cols_kernel<TT>,
                            dim3((d + kColThreads - 1) / kColThreads, parts), kColThreads, 0, st, gg,
                            xx, static_cast<const float2*>(stats), T, d, ws);
+    } else if (streamed(T, d, VEC, sizeof(TT))) {
+        if constexpr (VEC > 1) {
+            parts = stream_blocks(T);
+            auto launch = [&](auto nv, auto cw, auto sw, auto mode) {
+                constexpr int CW = decltype(cw)::value, SW = decltype(sw)::value;
+                using S = LnStream<CW, SW>;
+                constexpr auto kern = layernorm_vjp_stream_kernel<TT, VEC, decltype(nv)::value, CW, SW,
+                                                                  decltype(mode)::value != 0>;
+                const cudaError_t le = set_smem_limit<kern>(kLnStreamSmem);
+                if (le != cudaSuccess) return le;
+                const int row = d * static_cast<int>(sizeof(TT)), fit = (kLnStreamSmem - row) / (2 * row);
+                const int slots = fit < kLnMaxSlots ? fit : kLnMaxSlots;
+                kern<<<parts, S::kThreads, (2 * slots + 1) * row, st>>>(
+                    gg, xx, ww, T, d, eps, min_rms, oo, ws, slots, wait_limit_ns()),
+                    note_launch();
+                return cudaGetLastError();
+            };
+            auto form = [&](auto nv, auto cw, auto sw) {
+                return sums ? launch(nv, cw, sw, Int<1>{}) : launch(nv, cw, sw, Int<0>{});
+            };
+            const int n = d / VEC;
+            if constexpr (VEC == 4)
+                e = n <= 512    ? form(Int<2>{}, Int<8>{}, Int<8>{})
+                    : n <= 1024 ? form(Int<4>{}, Int<8>{}, Int<8>{})
+                                : form(Int<4>{}, Int<16>{}, Int<3>{});
+            else
+                e = n <= 512 ? form(Int<2>{}, Int<8>{}, Int<8>{}) : form(Int<2>{}, Int<16>{}, Int<7>{});
+        } else {
+            e = cudaErrorInvalidValue;  // (streamed)
+        }
     } else if (sums && one_cluster(T, f)) {
         return with_form<TT, VEC>(f, [&](auto nv, auto th) {
             constexpr int NV = decltype(nv)::value, TH = decltype(th)::value;
@@ -758,7 +1219,10 @@ size_t layernorm_vjp_floats(int dtype, int T, int d) {
                                    : row_form<float, 1>(d);
     if (one_cluster(T, f)) return 0;
     const size_t stats = f.nv == 0 ? 2 * static_cast<size_t>(T) : 0;
-    const size_t parts = f.nv == 0 ? long_ranges(T) : vjp_blocks(T, f);
+    const size_t parts = f.nv == 0 ? long_ranges(T)
+                         : streamed(T, d, dtype == 1 ? 8 : d % 4 == 0 ? 4 : 1, dtype == 1 ? 2 : 4)
+                             ? stream_blocks(T)
+                             : vjp_blocks(T, f);
     return stats + parts * 2 * static_cast<size_t>(d);
 }
 

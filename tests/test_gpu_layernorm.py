@@ -22,10 +22,13 @@ ARITH = 400 * 2.0 ** -24
 # one element, one warp's rows, ragged rows of each form, its limits, and long rows
 SHAPES = [("bf16", 1, 8), ("bf16", 7, 256), ("bf16", 200, 256), ("bf16", 33, 264),
           ("bf16", 19, 520), ("bf16", 5, 1032), ("bf16", 700, 2048), ("bf16", 3, 4096),
-          ("bf16", 650, 4104), ("bf16", 4, 8192), ("bf16", 70, 8200), ("bf16", 3, 20000),
+          ("bf16", 650, 4104), ("bf16", 1100, 4096), ("bf16", 2049, 1288), ("bf16", 1024, 2056),
+          ("bf16", 4100, 2568), ("bf16", 4, 8192), ("bf16", 300, 8192), ("bf16", 70, 8200), ("bf16", 3, 20000),
           ("f32", 1, 1), ("f32", 9, 3), ("f32", 77, 33), ("f32", 130, 128), ("f32", 11, 260),
-          ("f32", 300, 1023), ("f32", 5, 2047), ("f32", 6, 2052), ("f32", 3, 4099),
-          ("f32", 2, 8191), ("f32", 3, 8192), ("f32", 70, 8193), ("f32", 3, 12000)]
+          ("f32", 300, 1023), ("f32", 1025, 4096), ("f32", 1111, 1028), ("f32", 3000, 520),
+          ("f32", 5, 2047), ("f32", 6, 2052), ("f32", 3, 4099),
+          ("f32", 2, 8191), ("f32", 3, 8192), ("f32", 400, 8192), ("f32", 256, 5004), ("f32", 4096, 2052),
+          ("f32", 4096, 5000), ("f32", 70, 8193), ("f32", 3, 12000)]
 
 
 def inputs(dtype, T, d, seed=0):
@@ -132,6 +135,32 @@ def test_weight_sums_of_short_batches(fpo, dtype, d):
         assert torch.equal(dg, dg1) and torch.equal(db, db1) and torch.equal(out, out1)
 
 
+@pytest.mark.parametrize("case", ["first", "last", "mean"])
+@pytest.mark.parametrize("dtype,T,d", [("bf16", 4100, 2568), ("f32", 4096, 5000), ("f32", 40, 5000)])
+def test_outliers_and_large_means(fpo, dtype, T, d, case):
+    """A feature 300 times the others (among the first elements, which the one-pass statistics
+    take their origin from, or behind them), and a mean of 100 times the spread."""
+    x, gamma, beta, g = inputs(dtype, T, d)
+    x = x.clone()
+    if case == "mean":
+        x += 100 * x.float().std(1, keepdim=True).to(x.dtype)
+    else:
+        x[:, 3 if case == "first" else -2] *= 300
+    ref = definition(x, gamma, beta, g, 0.0)
+    y, out = torch.empty_like(x), torch.empty_like(x)
+    dg, db = (torch.empty(d, device="cuda") for _ in range(2))
+    fpo.layernorm(x, gamma, beta, y, eps=EPS)
+    fpo.layernorm_vjp(g, x, gamma, out, eps=EPS, min_rms=0.0, dgamma=dg, dbeta=db)
+    off = 1 + x.double().abs().amax(1, keepdim=True) * ref["rstd"][:, None]
+    xh = (x.double() - ref["mean"][:, None]) * ref["rstd"][:, None]
+    close(y, ref["y"], HALF[dtype], (ref["y"].abs().amax(1, keepdim=True) + gamma.double().abs().max()) * off)
+    u = (gamma.double() * g.double()).abs().amax(1, keepdim=True)
+    close(out, ref["g_out"], HALF[dtype],
+          u * ref["rstd"][:, None] * (1 + xh.abs().amax(1, keepdim=True)) * off)
+    close(dg, ref["dgamma"], 2.0 ** -24, (g.double() * (xh.abs() + 1) * off).abs().sum(0))
+    close(db, ref["dbeta"], 2.0 ** -24, ref["sbeta"])
+
+
 @pytest.mark.parametrize("T,d", [(3, 7), (4, 96)])
 def test_backward_matches_differences(fpo, T, d):
     """g_out, dgamma and dbeta are the derivatives of <g, layernorm(x)>: fourth-order central
@@ -205,10 +234,11 @@ def test_large_offset_keeps_the_variance(fpo):
     assert ((rstd.double() - want) / want).abs().max() < 1e-5
 
 
-@pytest.mark.parametrize("T, d", [(999, 1032), (60, 1032)])
+@pytest.mark.parametrize("T, d", [(999, 1032), (60, 1032), (4099, 2200)])
 def test_repeat_calls_other_streams_and_graphs(fpo, T, d):
     """Same bits from repeat calls, a side stream, two graphs that share a workspace (replayed
-    one after the other), and replays on new inputs.  (60 rows: no workspace.)"""
+    one after the other), and replays on new inputs.  (60 rows: no workspace; 4099: the stream
+    kernels.)"""
     x, gamma, beta, g = inputs("bf16", T, d)
     x2, _, _, g2 = inputs("bf16", T, d, seed=9)
     ws = torch.empty(fpo.layernorm_vjp_workspace(T, d), dtype=torch.uint8, device="cuda")

@@ -56,7 +56,7 @@ def test_workspace_query(lib):
     # short batches need none
     assert q(0, 4096, 1) == 0 and q(1, 4096, 1) == 0 and q(200, 256, 1) == 0 and q(1, 64, 0) == 0
     # two rows of d sums per block, at most as many blocks as rows
-    assert q(304, 4096, 1) >= 304 * 2 * 4096 * 4
+    assert q(128, 4096, 1) >= 128 * 2 * 4096 * 4
     assert q(16384, 4096, 1) <= 608 * 2 * 4096 * 4 + 512
     # long rows: the statistics of every row too
     assert q(1000, 20000, 0) >= 1000 * 8 + 64 * 2 * 20000 * 4
