@@ -15,8 +15,8 @@
  * Further entry points cover the rest of the method around that step: the
  * post-FFN and pre-MLP RMSNorm VJPs and per-layer signals (fpo_rmsnorm_vjp,
  * fpo_layer_signals, fpo_layer_update_grouped_signals), optimizers with the relative clip
- * (fpo_layer_optimize_grouped, fpo_layer_muon_grouped; fpo_orthogonalize_grouped), LayerNorm and its VJP (fpo_layernorm,
- * fpo_layernorm_vjp), the gate/up signals through the cached
+ * (fpo_layer_optimize_grouped, fpo_layer_muon_grouped; fpo_orthogonalize_grouped), LayerNorm
+ * and its VJP (fpo_layernorm, fpo_layernorm_vjp), the gate/up signals through the cached
  * W3_init (fpo_gate_up_signals) and the App. C update-magnitude ratio
  * (fpo_norm_ratio).  fpo_h2d_copy stages a step's inputs from host memory.
  *
@@ -322,8 +322,8 @@ int32_t fpo_rmsnorm_vjp(int64_t T, int64_t d, int32_t dtype, const void* g, cons
  *   y  = gamma (.) (x - mu) / sigma + beta
  *
  * x, y [T, d] and gamma, beta [d] in dtype; gamma NULL: ones, beta NULL: zeros.
- * mean_out, rstd_out [T] fp32 mu and 1 / sigma, each may be NULL.  y may not overlap x
- * (FPO_ERR_ARG for y == x).
+ * mean_out, rstd_out [T] fp32 mu and 1 / sigma, each may be NULL.  y may not overlap x, nor
+ * mean_out rstd_out (FPO_ERR_ARG where they are the same).
  * Statistics and sums in fp32, the variance around the row's own mean; one rounding
  * to dtype.  bf16 needs d % 8 == 0, fp32 takes any d; d <= 2^29.  Pointers 16-byte
  * aligned.  No workspace; asynchronous on `stream`; T = 0 enqueues nothing.
@@ -349,12 +349,14 @@ size_t fpo_layernorm_vjp_workspace(int64_t T, int64_t d, int32_t dtype);
  * x again (the row is read in any case): no statistics need saving.
  *
  * g, x, g_out [T, d] and gamma [d] in dtype; gamma NULL: ones.  dgamma, dbeta [d] fp32.
- * Each output may be NULL (not all three).  g_out may not overlap g or x (FPO_ERR_ARG
- * where it is either).  The weight sums are added in a fixed order that depends on T and d only
+ * Each output may be NULL (not all three).  g_out may not overlap g or x, nor dgamma dbeta
+ * (FPO_ERR_ARG where they are the same).  The weight sums are added in a fixed order that depends on T and d only
  * (repeat calls give identical bits).  workspace: fpo_layernorm_vjp_workspace() bytes,
  * 256-byte aligned; may be NULL where that is 0 and when dgamma and dbeta are both NULL; it
  * holds no status word.
  * T = 0 sets dgamma and dbeta to zero.  Types, sizes and alignment as fpo_layernorm.
+ * A wait of either kernel that runs out (fpo_set_wait_limit_ns) leaves NaN in the rows that
+ * it did not reach, and in dgamma and dbeta.
  */
 int32_t fpo_layernorm_vjp(int64_t T, int64_t d, int32_t dtype, const void* g, const void* x,
                           const void* gamma, float eps, float min_rms, void* g_out, float* dgamma,
@@ -480,13 +482,14 @@ size_t fpo_layer_muon_workspace(int32_t n_layers, int64_t d, int64_t d_ff, int32
  *   O_l = orthogonalised U_l (fpo_orthogonalize_grouped)
  *   W_master,l <- (1 - lr weight_decay) W_master,l - lr scale O_l;  W_out,l = W_master,l
  *                                                       rounded to dtype
- * in the last product's epilogue.  For the gate and up matrices g is dA or dB of
+ * For the gate and up matrices g is dA or dB of
  * fpo_gate_up_signals and A the MLP input, so d is there the taller side.
  *
  * g [T, d], A [T, d_ff] in dtype (not read for T = 0: G_l = 0), W_master and momentum
  * [d, d_ff] fp32, updated in place, W_out [d, d_ff] in dtype (the array or an entry may be
  * NULL); all HOST arrays of n_layers device pointers.  g and A entries may repeat, the others
- * not (FPO_ERR_ARG).  No relative clip: the step's norm is lr scale ||O_l||_F, about lr scale sqrt(rank).
+ * not; nor may one stand in two arrays, but for W_out[l] = W_master[l] in fp32 (FPO_ERR_ARG).
+ * No relative clip: the step's norm is lr scale ||O_l||_F, about lr scale sqrt(rank).
  * workspace: fpo_layer_muon_workspace() bytes, 256-byte aligned (device status word first).
  * Sizes and precision as fpo_orthogonalize_grouped.
  */

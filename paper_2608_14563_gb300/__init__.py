@@ -421,7 +421,10 @@ def orthogonalize_grouped(Gs, Os, *, steps=5, coeffs=None, eps=1e-7, workspace=N
     """fpo_orthogonalize_grouped: Os[l] = Newton-Schulz orthogonalisation of Gs[l] (one shape
     and dtype; Os[l] may be Gs[l]).  coeffs: None, or ``steps`` triples (a, b, c).  Returns the
     workspace tensor (its first word holds the device status)."""
-    n, G = len(Gs), Gs[0]
+    n = len(Gs)
+    if n == 0:
+        raise ValueError("Gs and Os need one tensor per layer")
+    G = Gs[0]
     rows, cols = G.shape
     _expect_all(Gs, n, G.shape, G.dtype, "Gs")
     _expect_all(Os, n, G.shape, G.dtype, "Os")
@@ -455,6 +458,8 @@ def layer_muon_grouped(gs, As, opt, W_masters, momenta, *, W_outs=None, workspac
                        stream=None):
     """fpo_layer_muon_grouped: G_l = gs[l]^T As[l], momentum, orthogonalisation, weight step."""
     n = len(As)
+    if n == 0 or n != len(gs):
+        raise ValueError("gs and As need one tensor per layer")
     T, d = gs[0].shape
     d_ff = As[0].shape[1]
     dtype = gs[0].dtype

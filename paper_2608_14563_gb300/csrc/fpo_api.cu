@@ -740,6 +740,14 @@ int32_t fpo_layer_muon_grouped(int32_t n_layers, int64_t T, int64_t d, int64_t d
         repeats(n_layers, reinterpret_cast<const void* const*>(momentum)) ||
         repeats(n_layers, W_out))
         return FPO_ERR_ARG;
+    // a momentum is no master and no W_out, and another layer's master no W_out
+    for (int l = 0; l < n_layers; ++l) {
+        const void* w = W_out ? W_out[l] : nullptr;
+        for (int k = 0; k < n_layers; ++k)
+            if (momentum[l] == W_master[k] ||
+                (w && (w == momentum[k] || (w == W_master[k] && (k != l || dtype == FPO_BF16)))))
+                return FPO_ERR_ARG;
+    }
     if (!workspace || workspace_bytes < fpo_layer_muon_workspace(n_layers, d, d_ff, dtype))
         return FPO_ERR_WORKSPACE;
     if ((reinterpret_cast<uintptr_t>(workspace) % kAlign) != 0) return FPO_ERR_ALIGN;
@@ -874,7 +882,7 @@ int32_t fpo_layernorm(int64_t T, int64_t d, int32_t dtype, const void* x, const 
     if (!aligned16(x) || !aligned16(gamma) || !aligned16(beta) || !aligned16(y) ||
         !aligned16(mean_out) || !aligned16(rstd_out))
         return FPO_ERR_ALIGN;
-    if (y && y == x) return FPO_ERR_ARG;
+    if ((y && y == x) || (mean_out && mean_out == rstd_out)) return FPO_ERR_ARG;
     rc = check_arch();
     if (rc != FPO_OK) return rc;
     return cuda_status(launch_layernorm_fwd(dtype, x, gamma, beta, static_cast<int>(T),
@@ -899,7 +907,7 @@ int32_t fpo_layernorm_vjp(int64_t T, int64_t d, int32_t dtype, const void* g, co
     if (!aligned16(g) || !aligned16(x) || !aligned16(gamma) || !aligned16(g_out) ||
         !aligned16(dgamma) || !aligned16(dbeta))
         return FPO_ERR_ALIGN;
-    if (g_out && (g_out == g || g_out == x)) return FPO_ERR_ARG;
+    if ((g_out && (g_out == g || g_out == x)) || (dgamma && dgamma == dbeta)) return FPO_ERR_ARG;
     if (dgamma || dbeta) {
         const size_t need = fpo_layernorm_vjp_workspace(T, d, dtype);
         if (need > 0 && (!workspace || workspace_bytes < need)) return FPO_ERR_WORKSPACE;

@@ -469,15 +469,17 @@ __device__ __forceinline__ float ln_origin(const TT* xs, int lane, int n, float 
     return a * inv_n;
 }
 
-// The loader's end: the last min(slots, filled) copies are waited for, so that the block leaves
-// none in flight.
-__device__ __forceinline__ void ln_drain(uint64_t* full, int slots, int filled, uint64_t limit_ns) {
-    for (int j = filled > slots ? filled - slots : 0; j < filled; ++j) {
-        const uint64_t t0 = global_timer_ns();
-        while (!mbar_try_wait(smem_u32(&full[j % slots]), (j / slots) & 1) &&
-               global_timer_ns() - t0 < limit_ns) {
-        }
-    }
+// mean((x - s)^2) - mean(x - s)^2, not below zero (a NaN stays one).
+__device__ __forceinline__ float ln_variance(float off, float square) {
+    const float v = fmaf(-off, off, square);
+    return v < 0.f ? 0.f : v;
+}
+
+// The loader's end: the last min(slots, filled) copies are waited for, whatever the wait limit, so
+// that the block leaves none in flight.
+__device__ __forceinline__ void ln_drain(uint64_t* full, int slots, int filled) {
+    for (int j = filled > slots ? filled - slots : 0; j < filled; ++j)
+        mbar_wait_drain(smem_u32(&full[j % slots]), (j / slots) & 1, 2000000000ull);
 }
 
 // Rows of block b of `blocks`: b, b + blocks, ... below T.
@@ -539,7 +541,7 @@ __global__ void __launch_bounds__(32 * (kLnFwdWarps + 1), 1)
                           smem_u32(&full[s]));
                 if (++s == slots) { s = 0; phase ^= 1u; }
             }
-            ln_drain(full, slots, i, limit_ns);
+            ln_drain(full, slots, i);
         }
         return;
     }
@@ -576,7 +578,7 @@ __global__ void __launch_bounds__(32 * (kLnFwdWarps + 1), 1)
             v2[1] += __shfl_xor_sync(0xffffffffu, v2[1], o);
         }
         const float off = v2[0] * inv_d, mu = origin + off;
-        const float rstd = 1.f / sqrtf(fmaxf(fmaf(-off, off, v2[1] * inv_d), 0.f) + eps);
+        const float rstd = 1.f / sqrtf(ln_variance(off, v2[1] * inv_d) + eps);
         const long long row = ln_block_row(i);
         TT* yr = y + row * d;
         const float2 m2 = both(-mu), r2 = both(rstd);
@@ -678,7 +680,7 @@ __global__ void __launch_bounds__(LnStream<CW, SW>::kThreads, 1)
                 bulk_load(smem_u32(slot_x(s) + d), g + ln_block_row(i) * d, bytes, bar);
                 if (++s == slots) { s = 0; phase ^= 1u; }
             }
-            ln_drain(full, slots, i, limit_ns);
+            ln_drain(full, slots, i);
         }
         __syncwarp();
     } else if (warp >= CW) {
@@ -730,8 +732,8 @@ __global__ void __launch_bounds__(LnStream<CW, SW>::kThreads, 1)
             }
             if (lane == 0) {
                 const float off = v[0] * inv_d, um = v[2] * inv_d;
-                const float var = fmaxf(fmaf(-off, off, v[1] * inv_d), 0.f);
-                const float sigma = sqrtf(var + eps), rstd = 1.f / sigma;
+                const float sigma = sqrtf(ln_variance(off, v[1] * inv_d) + eps);
+                const float rstd = 1.f / sigma;
                 stat[s][0] = origin + off;
                 stat[s][1] = rstd;
                 stat[s][2] = um;

@@ -161,6 +161,93 @@ def test_outliers_and_large_means(fpo, dtype, T, d, case):
     close(db, ref["dbeta"], 2.0 ** -24, ref["sbeta"])
 
 
+@pytest.mark.parametrize("dtype,T,d", [("bf16", 9, 264), ("bf16", 300, 2568), ("bf16", 4100, 2568),
+                                       ("f32", 700, 33), ("f32", 4097, 2052), ("f32", 7, 9000)])
+def test_nan_and_infinity_stay_in_their_row(fpo, dtype, T, d):
+    """A row of x with a NaN or an infinity gives NaN throughout, one of g with a NaN too; the
+    other rows are as without it (every form of the kernels)."""
+    x, gamma, beta, g = inputs(dtype, T, d)
+    y0, o0 = torch.empty_like(x), torch.empty_like(x)
+    fpo.layernorm(x, gamma, beta, y0, eps=EPS)
+    fpo.layernorm_vjp(g, x, gamma, o0, eps=EPS)
+    bad, badg = x.clone(), g.clone()
+    bad[0, d // 2] = float("nan")
+    bad[T // 2, d - 1] = float("inf")
+    badg[T - 1, 0] = float("nan")
+    y, out = torch.empty_like(x), torch.empty_like(x)
+    rstd = torch.empty(T, device="cuda")
+    fpo.layernorm(bad, gamma, beta, y, eps=EPS, rstd_out=rstd)
+    dg, db = (torch.zeros(d, device="cuda") for _ in range(2))
+    fpo.layernorm_vjp(badg, bad, gamma, out, eps=EPS, dgamma=dg, dbeta=db)
+    for r in (0, T // 2):
+        assert y[r].isnan().all() and out[r].isnan().all() and rstd[r].isnan()
+    assert out[T - 1].isnan().all() and dg.isnan().all() and db[0].isnan() and not db[1:].isnan().any()
+    keep = torch.ones(T, dtype=torch.bool, device="cuda")
+    keep[[0, T // 2]] = False
+    assert torch.equal(y[keep], y0[keep])
+    keep[T - 1] = False
+    assert torch.equal(out[keep], o0[keep])
+
+
+def test_calls_on_two_streams_at_once(fpo):
+    """The stream kernels and the short-batch cluster, side by side on two streams."""
+    sets = [inputs("bf16", T, 2568, seed=T) for T in (4100, 4100, 30)]
+    def bufs(x):
+        return [torch.empty_like(x), torch.empty_like(x), torch.empty(x.shape[1], device="cuda"),
+                torch.empty(x.shape[1], device="cuda")]
+
+    def call(s, b, stream):
+        x, gamma, beta, g = s
+        fpo.layernorm(x, gamma, beta, b[0], eps=EPS, stream=stream)
+        fpo.layernorm_vjp(g, x, gamma, b[1], eps=EPS, dgamma=b[2], dbeta=b[3], workspace=b[4],
+                          stream=stream)
+
+    want = []
+    for s in sets:
+        b = bufs(s[0])
+        b.append(torch.empty(max(256, fpo.layernorm_vjp_workspace(*s[0].shape)), dtype=torch.uint8,
+                             device="cuda"))
+        call(s, b, None)
+        want.append(b)
+    torch.cuda.synchronize()
+    got = [[torch.empty_like(t) for t in b] for b in want]
+    streams = [torch.cuda.Stream() for _ in sets]
+    for _ in range(10):
+        for s, b, st in zip(sets, got, streams):
+            call(s, b, st)
+    torch.cuda.synchronize()
+    for a, b in zip(want, got):
+        assert all(torch.equal(u, v) for u, v in zip(a[:4], b[:4]))
+
+
+def test_a_wait_that_runs_out_leaves_nan(fpo):
+    """With the wait limit at a microsecond the stream kernels may give up: every row is right or
+    NaN; with the default limit the results are as before."""
+    x, gamma, beta, g = inputs("bf16", 4100, 2568)
+    d = x.shape[1]
+
+    def call():
+        y, out = torch.empty_like(x), torch.empty_like(x)
+        dg, db = (torch.empty(d, device="cuda") for _ in range(2))
+        fpo.layernorm(x, gamma, beta, y, eps=EPS)
+        fpo.layernorm_vjp(g, x, gamma, out, eps=EPS, dgamma=dg, dbeta=db)
+        torch.cuda.synchronize()
+        return y, out, dg, db
+
+    want = call()
+    try:
+        fpo.set_wait_limit_ns(1000)
+        short = call()
+    finally:
+        fpo.set_wait_limit_ns(2_000_000_000)
+    for a, b in zip(want[:2], short[:2]):
+        lost = b.isnan().all(1)
+        assert torch.equal(a[~lost], b[~lost])
+    for a, b in zip(want[2:], short[2:]):
+        assert (b.isnan() | (a == b)).all()
+    assert all(torch.equal(a, b) for a, b in zip(want, call()))
+
+
 @pytest.mark.parametrize("T,d", [(3, 7), (4, 96)])
 def test_backward_matches_differences(fpo, T, d):
     """g_out, dgamma and dbeta are the derivatives of <g, layernorm(x)>: fourth-order central

@@ -217,6 +217,50 @@ def test_large_group(fpo, dtype, rows, cols):
         assert rel(O, definition(G)) < (4.5e-3 if dtype == "bf16" else 1e-5)
 
 
+def test_calls_on_two_streams_at_once(fpo):
+    """The one-launch form (every cluster of a call waits for the others) and the launches per
+    product, calls overlapping on three streams with workspaces of their own."""
+    shapes = [("bf16", 1024, 1024, 2), ("bf16", 512, 2048, 2), ("f32", 257, 2300, 2)]
+    jobs = []
+    for dtype, r, c, n in shapes:
+        G = [matrix(r, c, "full", seed=l).to(DT[dtype]) for l in range(n)]
+        ref = [torch.empty_like(t) for t in G]
+        fpo.orthogonalize_grouped(G, ref)
+        O = [torch.full_like(t, float("nan")) for t in G]
+        need = fpo.orthogonalize_workspace(n, r, c, fpo.BF16 if dtype == "bf16" else fpo.F32)
+        jobs.append((G, O, ref, torch.empty(need, dtype=torch.uint8, device="cuda"),
+                     torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for G, O, _, ws, s in jobs:
+            fpo.orthogonalize_grouped(G, O, workspace=ws, stream=s)
+    torch.cuda.synchronize()
+    for _, O, ref, ws, _ in jobs:
+        assert fpo.get_device_status(ws) == fpo.OK
+        assert all(torch.equal(a, b) for a, b in zip(O, ref))
+
+
+@pytest.mark.parametrize("dtype,rows,cols,n", [("bf16", 512, 2048, 1), ("bf16", 512, 2048, 8),
+                                               ("f32", 257, 2300, 2)])
+def test_waits_that_run_out_are_reported(fpo, dtype, rows, cols, n):
+    """Every form with the wait limit at a microsecond: the status says so, and the next call, with
+    the default limit and the same workspace, gives the same bits as before."""
+    G = [matrix(rows, cols, "full", seed=l).to(DT[dtype]) for l in range(n)]
+    ref, O = ([torch.empty_like(t) for t in G] for _ in range(2))
+    ws = fpo.orthogonalize_grouped(G, ref)
+    assert fpo.get_device_status(ws) == fpo.OK
+    for _ in range(2):
+        try:
+            fpo.set_wait_limit_ns(1000)
+            fpo.orthogonalize_grouped(G, O, workspace=ws)
+            assert fpo.get_device_status(ws) == 9  # FPO_ERR_TIMEOUT
+        finally:
+            fpo.set_wait_limit_ns(2_000_000_000)
+    fpo.orthogonalize_grouped(G, O, workspace=ws)
+    assert fpo.get_device_status(ws) == fpo.OK
+    assert all(torch.equal(a, b) for a, b in zip(O, ref))
+
+
 # ------------------------------------------------------------------------ Muon step
 def muon_inputs(dtype, T, d, d_ff, n, seed=0):
     gen = torch.Generator(device="cuda").manual_seed(seed + T + 3 * d + d_ff)

@@ -15,7 +15,7 @@ def lib():
 
 
 def test_forward_refusals(lib):
-    def call(T=4, d=64, dtype=1, x=P, gamma=P, beta=P, eps=1e-5, y=2 * P, mean=P, rstd=P):
+    def call(T=4, d=64, dtype=1, x=P, gamma=P, beta=P, eps=1e-5, y=2 * P, mean=P, rstd=3 * P):
         return lib.fpo_layernorm(T, d, dtype, x, gamma, beta, eps, y, mean, rstd, None)
 
     assert call(dtype=2) == DTYPE
@@ -26,14 +26,15 @@ def test_forward_refusals(lib):
     for k in ("x", "gamma", "beta", "y", "mean", "rstd"):
         assert call(**{k: MIS}) == ALIGN
     assert call(y=P) == ARG  # in place
+    assert call(mean=8 * P, rstd=8 * P) == ARG
 
 
 def test_backward_refusals(lib):
     need = lib.fpo_layernorm_vjp_workspace(4000, 64, 1)
     assert need > 0
 
-    def call(T=4000, d=64, dtype=1, g=P, x=2 * P, gamma=P, eps=1e-5, min_rms=0.5, out=3 * P, dg=P,
-             db=P, ws=P, n=need):
+    def call(T=4000, d=64, dtype=1, g=P, x=2 * P, gamma=P, eps=1e-5, min_rms=0.5, out=3 * P, dg=4 * P,
+             db=5 * P, ws=P, n=need):
         return lib.fpo_layernorm_vjp(T, d, dtype, g, x, gamma, eps, min_rms, out, dg, db, ws,
                                      ctypes.c_size_t(n), None)
 
@@ -45,7 +46,7 @@ def test_backward_refusals(lib):
     assert call(out=None, dg=None, db=None) == NULL
     for k in ("g", "x", "gamma", "out", "dg", "db"):
         assert call(**{k: MIS}) == ALIGN
-    assert call(out=P) == ARG and call(out=2 * P) == ARG
+    assert call(out=P) == ARG and call(out=2 * P) == ARG and call(db=4 * P) == ARG
     assert call(ws=None) == WORKSPACE and call(n=need - 1) == WORKSPACE
     assert call(ws=P + 16) == ALIGN
 

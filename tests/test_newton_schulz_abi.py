@@ -3,6 +3,7 @@ GPU needed)."""
 import ctypes
 
 import pytest
+import torch
 
 OK, NULL, SHAPE, DTYPE, ALIGN, WORKSPACE, ARG = 0, 1, 2, 3, 4, 5, 10
 P = 1 << 20   # never dereferenced: validation fails first
@@ -95,6 +96,25 @@ def test_muon_refusals(fpo):
                 size=two) == ARG                        # one master twice
     assert call(n=2, g=ptrs(P, P), A=ptrs(P, P), W=ptrs(P, 4 * P), M=ptrs(2 * P, 2 * P),
                 size=two) == ARG
+    # one buffer in two arrays
+    assert call(W=ptrs(2 * P)) == ARG and call(Wo=ptrs(2 * P)) == ARG and call(Wo=ptrs(P)) == ARG
+    assert call(n=2, g=ptrs(P, P), A=ptrs(P, P), W=ptrs(P, 4 * P), M=ptrs(2 * P, 3 * P),
+                Wo=ptrs(5 * P, P), size=two) == ARG
+
+
+def test_binding_refuses_empty_and_uneven_lists(fpo):
+    opt = fpo.muon_desc(lr=1e-3)
+    t = torch.zeros(8, 8)
+    with pytest.raises(ValueError):
+        fpo.orthogonalize_grouped([], [])
+    with pytest.raises(ValueError):
+        fpo.orthogonalize_grouped([t], [])
+    with pytest.raises(ValueError):
+        fpo.layer_muon_grouped([], [], opt, [], [])
+    with pytest.raises(ValueError):
+        fpo.layer_muon_grouped([t, t], [t], opt, [t], [t])
+    with pytest.raises(ValueError):
+        fpo.layer_muon_grouped([t], [t], opt, [t], [])
 
 
 def test_muon_desc_keeps_its_coefficients(fpo):
