@@ -475,6 +475,7 @@ struct EpiMomentumBase {
         int rows, cols, m_blocks, n_blocks;
         float mu;
         bool nesterov;
+        bool add, last;       // U holds the sums of the tokens before; these are the last tokens
     };
 };
 
@@ -495,38 +496,39 @@ struct EpiMomentum : EpiMomentumBase {
     using Maps = NsGradMaps;
     static constexpr bool kBf16 = true;
     static constexpr int kChunks = BN / 2 / 32;
-    static constexpr int kAcc = 8, kSlots = 2;
+    static constexpr int kAcc = 8;
 
     float *M, *U;      // (by value, as in EpiSym)
     double* slot;
     int r0, c0, rows, cols;
     float mu;
-    bool nesterov;
+    bool nesterov, add, last;
     double squares;
-    float4 m[kSlots][kAcc];
+    float4 m[kAcc];           // of the next chunk: M, before the last tokens the sums so far
 
     __device__ __forceinline__ bool in(int i, int c) const {
         return r0 + 4 * i < rows && c0 + 32 * c < cols;
     }
-    template <int SLOT>
+    __device__ __forceinline__ long long at(int i, int c) const {
+        return static_cast<long long>(r0 + 4 * i) * cols + c0 + 32 * c;
+    }
     __device__ __forceinline__ void fetch(int c) {
 #pragma unroll
         for (int i = 0; i < kAcc; ++i) {
-            m[SLOT][i] = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (in(i, c))
-                m[SLOT][i] = *reinterpret_cast<const float4*>(M + static_cast<long long>(r0 + 4 * i) * cols +
-                                                        c0 + 32 * c);
+            m[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (in(i, c) && (last || add))
+                m[i] = *reinterpret_cast<const float4*>((last ? M : U) + at(i, c));
         }
     }
     __device__ __forceinline__ EpiMomentum(const Params& p, int g, int row0, int col0, int lane, bool)
         : M(p.M[g]), U(p.U + g * p.u_stride), r0(row0 + lane / 8), c0(col0 + 4 * (lane % 8)),
-          rows(p.rows), cols(p.cols), mu(p.mu), nesterov(p.nesterov), squares(0.0) {
+          rows(p.rows), cols(p.cols), mu(p.mu), nesterov(p.nesterov), add(p.add), last(p.last),
+          squares(0.0) {
         const int warps = 2 * kNsWarps;  // of a tile: 8 blocks of 32 rows x 2 halves of the columns
         const long long tile = (static_cast<long long>(g) * p.m_blocks + row0 / kPairBM) * p.n_blocks +
                                col0 / BN;
         slot = p.part + tile * warps + row0 % kPairBM / 32 * 2 + col0 % BN / (BN / 2);
-        fetch<0>(0);
-        fetch<1>(1);
+        fetch(0);
     }
     template <int SLOT>
     __device__ __forceinline__ void chunk(const float (&v)[32], uint32_t buf, int lane, int c) {
@@ -534,35 +536,42 @@ struct EpiMomentum : EpiMomentumBase {
         float run = 0.f;
 #pragma unroll
         for (int i = 0; i < kAcc; ++i) {
-            const float4 g = ld_shared_f4(ns_piece(buf, lane, i));
-            float4 a = m[SLOT][i], u;
-            a.x = fmaf(mu, a.x, g.x);
-            a.y = fmaf(mu, a.y, g.y);
-            a.z = fmaf(mu, a.z, g.z);
-            a.w = fmaf(mu, a.w, g.w);
-            u = a;
-            if (nesterov) {
-                u.x = fmaf(mu, a.x, g.x);
-                u.y = fmaf(mu, a.y, g.y);
-                u.z = fmaf(mu, a.z, g.z);
-                u.w = fmaf(mu, a.w, g.w);
+            float4 g = ld_shared_f4(ns_piece(buf, lane, i));
+            if (add) {
+                float4 s = m[i];
+                if (last && in(i, c)) s = *reinterpret_cast<const float4*>(U + at(i, c));
+                g = make_float4(g.x + s.x, g.y + s.y, g.z + s.z, g.w + s.w);
             }
-            if (in(i, c)) {
-                const long long o = static_cast<long long>(r0 + 4 * i) * cols + c0 + 32 * c;
-                *reinterpret_cast<float4*>(M + o) = a;
-                *reinterpret_cast<float4*>(U + o) = u;
-                run += square_sum4(u, squares);
+            float4 u = g;
+            if (last) {
+                float4 a = m[i];
+                a.x = fmaf(mu, a.x, g.x);
+                a.y = fmaf(mu, a.y, g.y);
+                a.z = fmaf(mu, a.z, g.z);
+                a.w = fmaf(mu, a.w, g.w);
+                u = a;
+                if (nesterov) {
+                    u.x = fmaf(mu, a.x, g.x);
+                    u.y = fmaf(mu, a.y, g.y);
+                    u.z = fmaf(mu, a.z, g.z);
+                    u.w = fmaf(mu, a.w, g.w);
+                }
+                if (in(i, c)) {
+                    *reinterpret_cast<float4*>(M + at(i, c)) = a;
+                    run += square_sum4(u, squares);
+                }
             }
+            if (in(i, c)) *reinterpret_cast<float4*>(U + at(i, c)) = u;
         }
         squares += run;
-        if (c + 2 < kChunks) fetch<SLOT>(c + 2);
+        if (c + 1 < kChunks) fetch(c + 1);
         __syncwarp();
     }
     __device__ __forceinline__ void finish(int lane) {
         double t = squares;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
-        if (lane == 0) *slot = t;
+        if (lane == 0 && last) *slot = t;
         __syncwarp();
     }
 };

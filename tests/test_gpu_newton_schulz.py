@@ -284,6 +284,7 @@ def muon_definition(g, A, W, M, lr, mu, wd, scale, nesterov):
 
 
 MUON = [("bf16", 200, 256, 384, 2), ("bf16", 1, 64, 136, 3), ("bf16", 700, 520, 264, 2),
+        ("bf16", 4160, 64, 136, 2), ("bf16", 9000, 72, 64, 1), ("bf16", 4200, 1032, 2056, 2),
         ("bf16", 0, 64, 64, 1), ("f32", 128, 64, 256, 2), ("f32", 77, 65, 33, 2),
         ("f32", 0, 9, 30, 1), ("f32", 300, 31, 500, 1)]
 
@@ -311,6 +312,19 @@ def test_muon_step_matches_the_definition(fpo, dtype, T, d, d_ff, n, nesterov):
         floor = 2.0 ** -23 * W0[l].double().norm() / (lr * scale * Or.norm())
         assert rel(step, -f32(lr) * f32(scale) * Or) < tol + floor
         assert torch.equal(Wo[l], W[l].to(DT[dtype]))
+
+
+def test_many_tokens_of_one_sign(fpo):
+    """The tensor core's sums truncate, so those of positive products come out too small: by up to
+    2^-23 of the running sum (on average half the final one) at each of the 256 16-deep steps of
+    the 4096 tokens of one accumulator, and no more for more tokens."""
+    T, d, d_ff = 16384, 64, 128
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    g = torch.rand(T, d, generator=gen, device="cuda").bfloat16()
+    A = torch.rand(T, d_ff, generator=gen, device="cuda").bfloat16()
+    W, M = (torch.zeros(d, d_ff, device="cuda") for _ in range(2))
+    fpo.layer_muon_grouped([g], [A], fpo.muon_desc(lr=1e-3), [W], [M])
+    assert rel(M, g.double().T @ A.double()) < 256 * 2.0 ** -24 + 8 * 2.0 ** -24
 
 
 def test_muon_step_without_weight_copy_in_a_graph(fpo):
