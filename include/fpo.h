@@ -445,7 +445,7 @@ size_t fpo_orthogonalize_workspace(int32_t n_layers, int64_t rows, int64_t cols,
  *
  * bf16: products of fp16 operands scaled by powers of two from the bounds (11 bits instead of
  * bf16's 8), fp32 accumulation, the linear term a X from 22 bits of X, whatever its rank;
- * rows and cols multiples of 8.  fp32: operands as sums of two fp16 numbers (22 bits), three
+ * rows and cols multiples of 8; a side of at most 64 as in fp32 calls.  fp32: operands as sums of two fp16 numbers (22 bits), three
  * products, fp32 sums rounded to nearest every 64 products, the linear term in fp32; any
  * sizes.  Sides up to FPO_MAX_NS_SIDE.  A matrix with a NaN or an infinity gives NaN
  * throughout, and no other matrix changes.  Deterministic, and independent of what else is in

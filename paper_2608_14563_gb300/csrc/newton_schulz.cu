@@ -13,9 +13,16 @@
 // scaled by powers of two: the host bounds every X_k, A and B from the polynomials' maxima on
 // the interval that the singular values can reach, so nothing overflows, and fp16's small end
 // lies 2^-39 below the bound.  bf16 calls keep X's low part for the linear term (EpiApply);
-// measured against fp64 the result is then off by 0.7e-3 to 1.9e-3 in norm, whatever the
-// rank, less than the bf16 rounding of the output itself (1.7e-3).  fp32 calls take every
-// operand as the sum of two fp16 matrices (22 bits) and three products.
+// against fp64 their result is then off by 0.7e-3 to 1.9e-3 in norm before its own rounding
+// (1.7e-3), whatever the rank.  fp32 calls, and bf16 ones of few rows or columns (ns_split), take
+// every operand as the sum of two fp16 matrices (22 bits) and three products: 1e-6 to 2e-6.
+//
+// Launches: norm, cast, then A, B, X' of every step (in one launch where few tiles make its
+// waits cheaper than launches, ns_chain_kernel).  4096 x 11008, five steps (us, one launch each,
+// alone): norm 29, cast 46, A 118, B 51, X' 242 (last 218): the products at 70 to 84% of the tensor
+// rate in whole waves of tiles on 76 clusters, 136 tiles of A taking two and the 688 of X' ten.
+// Muon: the gradient's GEMM with the momentum and the squares in its epilogue, and a last pass
+// over the masters at the copy rate (4096 x 11008 twice: 476 and 186 us).
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -346,7 +353,17 @@ int ns_splits(long long tiles, int K) {
     return s < 1 ? 1 : static_cast<int>(s);
 }
 
-NsLayout ns_layout(int n, int rows, int cols, bool split, bool muon) {
+// kSplit: fp32 calls, and bf16 ones of few rows or columns: there the rounding errors of single
+// entries of A and B average out least.  In norm the bf16 result of fp16 products is off by 2.3e-3 to
+// 3.9e-3 for sides of 8 to 64, 2.1e-3 to 2.4e-3 for longer ones (its own rounding, and all of
+// it with kSplit: 1.7e-3).  Two 64 x 256 matrices take 125 us instead of 90, sixteen 64 x 4096
+// 431 instead of 285, one 16 x 8192 211 instead of 248.
+bool ns_split(int dtype, int rows, int cols) {
+    return dtype == 0 || rows <= 64 || cols <= 64;
+}
+
+NsLayout ns_layout(int n, int rows, int cols, int dtype, bool muon) {
+    const bool split = ns_split(dtype, rows, cols);
     NsLayout L = {};
     L.m = rows < cols ? rows : cols;
     // rows of whole 128-byte lines: a TMA box of 64 columns then takes one line of a row, not two
@@ -856,15 +873,15 @@ bool ns_coeffs_ok(int steps, const float* coeffs) {
 }
 
 size_t ns_workspace_bytes(int n, int rows, int cols, int dtype, bool muon) {
-    return ns_layout(n, rows, cols, dtype == 0, muon).total;
+    return ns_layout(n, rows, cols, dtype, muon).total;
 }
 
 size_t ns_clear_bytes(int n, int rows, int cols, int dtype, bool muon) {
-    return ns_layout(n, rows, cols, dtype == 0, muon).clear;
+    return ns_layout(n, rows, cols, dtype, muon).clear;
 }
 
 float* ns_update_buffer(void* ws, int n, int rows, int cols, int dtype, int layer) {
-    const NsLayout L = ns_layout(n, rows, cols, dtype == 0, true);
+    const NsLayout L = ns_layout(n, rows, cols, dtype, true);
     return reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + L.U) + layer * L.u_stride;
 }
 
@@ -872,8 +889,8 @@ cudaError_t launch_newton_schulz(int n, int rows, int cols, int dtype, const voi
                                  const NsMomentum* mom, float eps, int steps, const float* coeffs,
                                  const NsTarget& to, void* workspace, unsigned* status,
                                  cudaStream_t st) {
-    const bool split = dtype == 0;
-    const NsLayout L = ns_layout(n, rows, cols, split, mom != nullptr);
+    const bool split = ns_split(dtype, rows, cols), f32 = dtype == 0;
+    const NsLayout L = ns_layout(n, rows, cols, dtype, mom != nullptr);
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     double* part = reinterpret_cast<double*>(ws + L.part);
     const size_t numel = static_cast<size_t>(rows) * cols;
@@ -892,7 +909,7 @@ cudaError_t launch_newton_schulz(int n, int rows, int cols, int dtype, const voi
         ns_momentum_kernel<<<grid, kPassThreads, 0, st>>>(p, numel, mom->mu, mom->nesterov, part),
             note_launch();
         e = cudaGetLastError();
-    } else if (split) {
+    } else if (f32) {
         e = launch_chained(ns_norm_kernel<float>, grid, kPassThreads, 0, st, p, numel, part);
     } else {
         e = launch_chained(ns_norm_kernel<__nv_bfloat16>, grid, kPassThreads, 0, st, p, numel, part);
@@ -913,23 +930,24 @@ cudaError_t launch_newton_schulz(int n, int rows, int cols, int dtype, const voi
     __half* lo = reinterpret_cast<__half*>(ws + L.lo[0]);
     float* x32 = split ? reinterpret_cast<float*>(ws + L.x32) : nullptr;
     const float scale = ldexpf(1.f, scale_exp(1.0));
-    if (split)
-        e = launch_chained(ns_cast_kernel<float, true>, cgrid, kPassThreads, 0, st, p, rows, cols, L.ld, part, blocks, eps, scale, hi, lo, x32, L.xs);
-    else if (mom)
-        e = launch_chained(ns_cast_kernel<float, false>, cgrid, kPassThreads, 0, st, p, rows, cols, L.ld, part, blocks, eps, scale, hi, lo, x32, L.xs);
+    auto cast = [&](auto kern) {
+        return launch_chained(kern, cgrid, kPassThreads, 0, st, p, rows, cols, L.ld, part, blocks, eps,
+                              scale, hi, lo, x32, L.xs);
+    };
+    if (f32 || mom)
+        e = split ? cast(ns_cast_kernel<float, true>) : cast(ns_cast_kernel<float, false>);
     else
-        e = launch_chained(ns_cast_kernel<__nv_bfloat16, false>, cgrid, kPassThreads, 0, st, p, rows, cols, L.ld, part, blocks, eps, scale, hi, lo, x32, L.xs);
+        e = split ? cast(ns_cast_kernel<__nv_bfloat16, true>) : cast(ns_cast_kernel<__nv_bfloat16, false>);
     if (e != cudaSuccess) return e;
     void* O32[kMaxGroups];
     if (mom)  // in place of U, which is in X_0 by now
         for (int l = 0; l < n; ++l) O32[l] = const_cast<void*>(p.in[l]);
     void* const* O = mom ? O32 : to.out;
-    if (split)
-        e = run_iteration<true, kResult>(L, ws, n, rows, cols, steps, coeffs, O, status, st);
-    else if (mom)
-        e = run_iteration<false, kResult32>(L, ws, n, rows, cols, steps, coeffs, O, status, st);
+    auto iterate = [&](auto run) { return run(L, ws, n, rows, cols, steps, coeffs, O, status, st); };
+    if (f32 || mom)
+        e = split ? iterate(run_iteration<true, kResult32>) : iterate(run_iteration<false, kResult32>);
     else
-        e = run_iteration<false, kResult>(L, ws, n, rows, cols, steps, coeffs, O, status, st);
+        e = split ? iterate(run_iteration<true, kResult>) : iterate(run_iteration<false, kResult>);
     if (e != cudaSuccess || !mom) return e;
     NsWeights w = {};
     for (int l = 0; l < n; ++l) {
@@ -939,7 +957,7 @@ cudaError_t launch_newton_schulz(int n, int rows, int cols, int dtype, const voi
     }
     const size_t units = (numel + kPassThreads * 16 - 1) / (kPassThreads * 16);
     const dim3 wgrid(static_cast<unsigned>(units < 2048 ? units : 2048), n);
-    if (split)
+    if (f32)
         return launch_chained(ns_weight_kernel<float>, wgrid, kPassThreads, 0, st, w, numel, to.keep,
                               to.rate);
     return launch_chained(ns_weight_kernel<__nv_bfloat16>, wgrid, kPassThreads, 0, st, w, numel,

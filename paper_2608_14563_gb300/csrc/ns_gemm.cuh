@@ -303,7 +303,7 @@ struct EpiSym : EpiSymBase<kSplit> {
 // on as in EpiSym).  What becomes of it:
 //   kNext     the next X: its high part, and its low part (not kSplit: for the linear term
 //             only) or (kSplit) low part and the fp32 value
-//   kResult   O [M, N] (row stride N) in the call's type
+//   kResult   O [M, N] (row stride N) in bf16
 //   kResult32 O in fp32
 // The linear term takes X in more bits than the operands have: of a direction in which X is
 // small B X is next to nothing, so a X carries it, 3.4 times larger after every step, and with
@@ -322,7 +322,7 @@ struct NsApplyStep {      // what changes from step to step
 
 template <bool kSplit, int kOut>
 struct EpiApplyBase {
-    using Out = std::conditional_t<kSplit || kOut == kResult32, float, __nv_bfloat16>;
+    using Out = std::conditional_t<kOut == kResult, __nv_bfloat16, float>;
     struct Params {
         NsApplyStep s;
         float* x32;           // kSplit: X in fp32, updated in place (kNext)

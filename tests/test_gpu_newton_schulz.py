@@ -88,6 +88,19 @@ def test_orthogonalize_matches_the_definition(fpo, dtype, rows, cols, kind):
         assert rel(O, definition(G)) < limit(dtype, kind)
 
 
+@pytest.mark.parametrize("rows,cols", [(8, 8), (64, 256), (2048, 32), (16, 8192)])
+def test_small_sides_are_exact_to_the_rounding(fpo, rows, cols):
+    """bf16 matrices with a side of at most 64: the fp32 products' 1e-5, and the rounding of the
+    result, 2^-8 of every element at most, 2^-8 / sqrt 3 in norm where they are spread."""
+    Gs = [matrix(rows, cols, "full", seed=l).bfloat16() for l in range(3)]
+    Os = [torch.empty_like(G) for G in Gs]
+    fpo.orthogonalize_grouped(Gs, Os)
+    for G, O in zip(Gs, Os):
+        want = definition(G)
+        assert ((O.double() - want).abs() <= 2.0 ** -8 * want.abs() + 1e-5 * want.norm()).all()
+        assert rel(O, want.bfloat16().double()) < 1e-3  # few round the other way
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_result_is_near_orthogonal(fpo, dtype):
     """Singular values of a square Gaussian matrix's bulk land in the quintic's band."""
