@@ -143,6 +143,16 @@ __device__ __forceinline__ float2 unpack_f16x2(uint32_t w) {
     return __half22float2(*reinterpret_cast<const __half2*>(&w));
 }
 
+// An accumulator is free again: arrival on the barrier `bar` of the pair's leader.  Relaxed: what
+// goes before it are TMEM loads, which tcgen05.wait::ld and the tcgen05 fence order, and nothing in
+// memory is handed over.  (A release at cluster scope waits for the warp's stores and took most
+// of a k-block's turn in the kSplit kernels: fp32 2048 x 8192, five steps, 2046 us and 1649.)
+__device__ __forceinline__ void arrive_leader(uint32_t bar) {
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(
+                     mapa_shared(bar, 0))
+                 : "memory");
+}
+
 // ---------------------------------------------------------------------------
 // Epilogues.  A warp has 32 rows x BN / 2 columns of a tile and takes them 32 columns at a time:
 // the accumulator's chunk (one row per lane) goes through the warp's staging buffer, and each
@@ -765,12 +775,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
         auto release = [&] {
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) {
-                if (leader)
-                    mbar_arrive(tempty_bar(acc));
-                else
-                    mbar_arrive_cluster(mapa_shared(tempty_bar(acc), 0));
-            }
+            if (lane == 0) arrive_leader(tempty_bar(acc));
             __syncwarp();
             if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
         };
@@ -987,6 +992,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
         *abort_flag = 0;
         *issued_word = 0;
         fence_mbar_init();
+        for (int f = 0; f < 3; ++f)
+            for (int k = 0; k < 4; ++k) tma_prefetch_desc(&p.map[f][k / 2][k % 2]);
     }
     if (warp == 1) {
         tmem_alloc_pair<kAccs * BN>(smem_u32(tmem_holder));
@@ -1143,12 +1150,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
         auto release = [&] {
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) {
-                if (leader)
-                    mbar_arrive(tempty_bar(acc));
-                else
-                    mbar_arrive_cluster(mapa_shared(tempty_bar(acc), 0));
-            }
+            if (lane == 0) arrive_leader(tempty_bar(acc));
             __syncwarp();
             if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
         };

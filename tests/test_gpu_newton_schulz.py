@@ -256,15 +256,15 @@ def test_calls_on_two_streams_at_once(fpo):
 @pytest.mark.parametrize("dtype,rows,cols,n", [("bf16", 512, 2048, 1), ("bf16", 512, 2048, 8),
                                                ("f32", 257, 2300, 2)])
 def test_waits_that_run_out_are_reported(fpo, dtype, rows, cols, n):
-    """Every form with the wait limit at a microsecond: the status says so, and the next call, with
-    the default limit and the same workspace, gives the same bits as before."""
+    """Every form with a wait limit far below the first operands' way in: the status says so, and
+    the next call, with the default limit and the same workspace, gives the same bits as before."""
     G = [matrix(rows, cols, "full", seed=l).to(DT[dtype]) for l in range(n)]
     ref, O = ([torch.empty_like(t) for t in G] for _ in range(2))
     ws = fpo.orthogonalize_grouped(G, ref)
     assert fpo.get_device_status(ws) == fpo.OK
     for _ in range(2):
         try:
-            fpo.set_wait_limit_ns(1000)
+            fpo.set_wait_limit_ns(100)
             fpo.orthogonalize_grouped(G, O, workspace=ws)
             assert fpo.get_device_status(ws) == 9  # FPO_ERR_TIMEOUT
         finally:
