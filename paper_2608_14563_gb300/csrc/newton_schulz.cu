@@ -340,9 +340,9 @@ struct NsLayout {
 // Tiles of one matrix of a kSplit product [M, N], and the ranges that their k-blocks are split
 // into: as many as half of the 76 clusters hold of one matrix, of 16 k-blocks or more.  It goes
 // by the matrix's sizes only, so that its result does not depend on the group.  Five steps, with
-// and without: 767 x 2049 one matrix 334 and 387 us, two 414 and 465, eight 1129 and 1116; eight
-// 256 x 4096 432 and 610, eight 512 x 2048 645 and 593; two 64 x 8192 239 and 695.  (Ranges of 8
-// k-blocks: eight 512 x 1024 413 instead of 354.)
+// and without: 767 x 2049 one matrix 314 and 349 us, two 380 and 413, eight 977 and 944; eight
+// 256 x 4096 388 and 510, eight 512 x 2048 580 and 525; two 64 x 8192 231 and 555.  (Ranges of 8
+// k-blocks: eight 512 x 1024 392 instead of 332.)
 long long ns_matrix_tiles(int M, int N, bool tri) {
     const long long mb = (M + 255) / 256;
     return tri ? mb * (mb + 1) : mb * ((N + 127) / 128);
@@ -356,8 +356,8 @@ int ns_splits(long long tiles, int K) {
 // kSplit: fp32 calls, and bf16 ones of few rows or columns: there the rounding errors of single
 // entries of A and B average out least.  In norm the bf16 result of fp16 products is off by 2.3e-3 to
 // 3.9e-3 for sides of 8 to 64, 2.1e-3 to 2.4e-3 for longer ones (its own rounding, and all of
-// it with kSplit: 1.7e-3).  Two 64 x 256 matrices take 125 us instead of 90, sixteen 64 x 4096
-// 431 instead of 285, one 16 x 8192 211 instead of 248.
+// it with kSplit: 1.7e-3).  Two 64 x 256 matrices take 121 us instead of 83, sixteen 64 x 4096
+// 399 instead of 280, one 16 x 8192 200 instead of 239.
 bool ns_split(int dtype, int rows, int cols) {
     return dtype == 0 || rows <= 64 || cols <= 64;
 }
@@ -782,8 +782,8 @@ cudaError_t run_iteration(const NsLayout& L, uint8_t* ws, int n, int rows, int c
     if (steps > kNsMaxSteps) return cudaErrorInvalidValue;
     ns_steps(steps, coeffs, co);
     // fp16, with a cluster for every 256 x 128 tile: one launch.  (Two 256 x 384 matrices, five
-    // steps: 107 us, 115 a launch per product; four 1024 x 1024 with two tiles to a cluster 268
-    // and 273, one 2048 x 2048 292 and 281.  fp32 products are longer and lose by it: two
+    // steps: 97 us, 107 a launch per product; two 1024 x 1024 169 and 185; with two tiles to a
+    // cluster, one 2048 x 2048 292 and 281.  fp32 products are longer and lost by it: two
     // 512 x 1024 matrices 288 and 265.)
     if constexpr (!kSplit) {
         const long long sym = n * ns_matrix_tiles(L.m, L.m, true),
