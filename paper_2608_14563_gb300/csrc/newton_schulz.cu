@@ -383,15 +383,16 @@ NsLayout ns_layout(int n, int rows, int cols, int dtype, bool muon) {
     if (split) {
         const long long sym = ns_matrix_tiles(L.m, L.m, true), app = ns_matrix_tiles(rows, cols, false);
         long long tiles = 0, units = 0;  // of the products that are split
-        auto product = [&](long long t, int K) {
+        // `wide`: tiles of 128 columns that those of 256 cover
+        auto product = [&](long long t, long long wide, int K) {
             const int s = ns_splits(t, K);
             if (s == 1) return;
             if (t > tiles) tiles = t;
-            if (t * s > units) units = t * s;
+            if (wide * s > units) units = wide * s;
         };
-        product(sym, rows < cols ? cols : rows);
-        product(sym, L.m);
-        product(app, L.m);
+        product(sym, sym, rows < cols ? cols : rows);
+        product(sym, sym, L.m);
+        product(app, 2ll * ((rows + 255) / 256) * ((cols + 255) / 256), L.m);
         L.counts = take(n * tiles * 2 * kNsWarps * sizeof(unsigned));
         L.clear = at;
         L.slots = take(n * units * (kPairBM * 128 * sizeof(float)));
@@ -507,14 +508,28 @@ cudaError_t launch_ns(const typename Epi::Maps& maps, const typename Epi::Params
         tri ? static_cast<long long>(sh.g.m_blocks) * (sh.g.m_blocks + 1) / 2 * (kPairBM / BN)
             : static_cast<long long>(sh.g.m_blocks) * sh.g.n_blocks;
     sh.g.tiles = groups * per;
-    sh.splits = kSplit ? ns_splits(per, K) : 1;
+    sh.splits = kSplit ? ns_splits(ns_matrix_tiles(M, N, tri), K) : 1;
     sh.slots = rg.slots;
     sh.counts = rg.counts;
-    const int max_clusters = resident_clusters<kern>(kNsThreads, S::kBytes, di.sm_count);
+    constexpr int kThreads = ns_threads<BN, kSplit>();
+    if constexpr (ns_first_warp<BN, kSplit>() == 4) {
+        // the warpgroups' new shares have to fit into what the block is launched with: an increase
+        // beyond it would never be granted
+        static std::atomic<int> regs{0};
+        if (regs.load(std::memory_order_relaxed) == 0) {
+            cudaFuncAttributes at;
+            e = cudaFuncGetAttributes(&at, kern);
+            if (e != cudaSuccess) return e;
+            regs.store(at.numRegs, std::memory_order_relaxed);
+        }
+        if (regs.load(std::memory_order_relaxed) * kThreads < 128 * (kNsFewRegs + 2 * kNsManyRegs))
+            return cudaErrorLaunchOutOfResources;
+    }
+    const int max_clusters = resident_clusters<kern>(kThreads, S::kBytes, di.sm_count);
     const long long units = sh.g.tiles * sh.splits;
     const long long clusters = units < max_clusters ? units : max_clusters;
-    return launch_chained(kern, dim3(static_cast<unsigned>(2 * clusters)), kNsThreads, S::kBytes, st,
-                          maps, ep, sh, status, wait_limit_ns());
+    return launch_chained(kern, dim3(static_cast<unsigned>(2 * clusters)), kThreads, S::kBytes, st, maps,
+                          ep, sh, status, wait_limit_ns());
 }
 
 // One batch of GEMMs, C[M, N] = sum_k A B over K, on the pair kernel with 256 x BN tiles.
@@ -534,20 +549,29 @@ cudaError_t run_ns_tiles(const NsOperand& A, const NsOperand& B, const typename 
     return launch_ns<BN, A_MN, B_MN, kSplit, Epi>(maps, ep, M, N, K, A.n, tri, rg, status, st);
 }
 
-// fp32 calls on 128-column tiles.  fp16 ones too where twice as many tiles still have a cluster
-// each: an epilogue is then half as long.
+// Tiles of 256 columns or of 128 (the same bits).  fp16: 128 where twice as many tiles still have a
+// cluster each, an epilogue is then half as long.  kSplit, whose epilogue no MMAs hide, by the waves
+// of tiles on the clusters times a tile's time: 1.03 us a 64-deep k-block and 12 us of set-up and
+// epilogue with 256 columns, 0.85 and 4 with 128.  (Five steps, 128 columns alone and by this rule:
+// one 2048 x 8192 1636 and 1475 us, two 767 x 2049 380 and 355, eight 512 x 1024 332 and 321;
+// 256 wherever fp16 takes them: eight 256 x 4096 405 instead of 381.)
 template <bool A_MN, bool B_MN, bool kSplit, template <int> class Epi>
 cudaError_t run_ns(const NsOperand& A, const NsOperand& B, const typename Epi<128>::Params& ep, int M,
                    int N, int K, bool tri, const NsRanges& rg, unsigned* status, cudaStream_t st) {
-    if constexpr (!kSplit) {
-        DevInfo di;
-        if (!current_device_info(&di)) return cudaErrorUnknown;
-        const long long mb = (M + 255) / 256, nb = (N + 255) / 256;
-        const long long tiles = A.n * (tri ? mb * (mb + 1) / 2 : mb * nb);
-        if (4 * tiles > di.sm_count)
-            return run_ns_tiles<256, A_MN, B_MN, kSplit, Epi<256>>(A, B, ep, M, N, K, tri, rg, status,
-                                                                     st);
+    DevInfo di;
+    if (!current_device_info(&di)) return cudaErrorUnknown;
+    const long long mb = (M + 255) / 256, nb = (N + 255) / 256;
+    const long long tiles = A.n * (tri ? mb * (mb + 1) / 2 : mb * nb);
+    bool wide = 4 * tiles > di.sm_count;
+    if constexpr (kSplit) {
+        const long long narrow = ns_matrix_tiles(M, N, tri), clusters = di.sm_count / 2;
+        const int splits = ns_splits(narrow, K), blocks = (K + kBK - 1) / kBK / splits;
+        auto waves = [&](long long units) { return (units + clusters - 1) / clusters; };
+        wide = waves(tiles * splits) * (1030 * blocks + 12000) <
+               waves(A.n * narrow * splits) * (850 * blocks + 4000);
     }
+    if (wide)
+        return run_ns_tiles<256, A_MN, B_MN, kSplit, Epi<256>>(A, B, ep, M, N, K, tri, rg, status, st);
     return run_ns_tiles<128, A_MN, B_MN, kSplit, Epi<128>>(A, B, ep, M, N, K, tri, rg, status, st);
 }
 

@@ -21,9 +21,10 @@
 // ten and more.  So an accumulator holds one 64-deep k-block only: the 8 MMAs with one low
 // operand first, while the sums (and what is truncated of them) are 2^-11 of the final size,
 // then the 4 high x high MMAs; the epilogue warps add it to sums in their registers, rounding
-// to nearest, while the next k-block fills the other accumulator.  BN is 128 there: 64 sums per
-// thread of 8 warps (with 128, and 168 registers, the loop spilled and took 2.7 us a k-block,
-// three times its MMAs).
+// to nearest, while the next k-blocks fill other accumulators: 64 sums per thread with BN 128,
+// 0.85 us a k-block (0.4 of MMAs at the tensor rate, 0.6 of operands from shared memory), and 128
+// with BN 256, 1.03 us (0.8 of MMAs), where the warps share registers out anew (with 168 each
+// the loop spilled and took 2.7 us).
 #pragma once
 
 #include <cuda_bf16.h>
@@ -57,9 +58,30 @@ constexpr int kNsThreads = 64 + 32 * kNsWarps;
 // Accumulators in TMEM.  kSplit: four, as the MMAs of a k-block take no longer than the way to
 // the epilogue warps and back (eight fp32 256 x 4096, five steps: 421 us with two, 388 with four).
 constexpr int kNsMaxAccs = 4;
-template <bool kSplit>
+template <bool kSplit, int BN = 128>
 constexpr int ns_accs() {
-    return kSplit ? kNsMaxAccs : 2;
+    return kSplit && BN == 128 ? kNsMaxAccs : 2;
+}
+
+// Warps before the epilogue's.  kSplit with 256 columns: a warpgroup of its own for the producer and
+// the MMA issuer, whose registers the epilogue's two warpgroups take over (128 sums a thread):
+// 384 threads are launched with 168 each (launch_ns looks), and go on with 40, 232 and 232.
+constexpr int kNsFewRegs = 40, kNsManyRegs = 232;
+template <int BN, bool kSplit>
+constexpr int ns_first_warp() {
+    return kSplit && BN == 256 ? 4 : 2;
+}
+template <int BN, bool kSplit>
+constexpr int ns_threads() {
+    return 32 * (ns_first_warp<BN, kSplit>() + kNsWarps);
+}
+template <int R>
+__device__ __forceinline__ void ns_more_registers() {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(R));
+}
+template <int R>
+__device__ __forceinline__ void ns_fewer_registers() {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(R));
 }
 
 template <int BN>
@@ -588,7 +610,7 @@ struct EpiMomentum : EpiMomentumBase {
 
 // ---------------------------------------------------------------------------
 template <int BN, bool A_MN, bool B_MN, bool kSplit, class Epi>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ns_threads<BN, kSplit>(), 1)
     ns_gemm_kernel(const __grid_constant__ typename Epi::Maps maps,
                    const __grid_constant__ typename Epi::Params ep, const NsShape sh,
                    unsigned int* status, unsigned long long wait_limit_ns) {
@@ -619,7 +641,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
     };
 
     const uint32_t bar0 = sbase + L::kBarOffset;
-    constexpr int kFull = kStages * kSub, kAccs = ns_accs<kSplit>();
+    constexpr int kFull = kStages * kSub, kAccs = ns_accs<kSplit, BN>();
+    constexpr int kFirst = ns_first_warp<BN, kSplit>();
     auto full_bar = [&](int s, int j) { return bar0 + 8u * (s * kSub + j); };
     auto empty_bar = [&](int s) { return bar0 + 8u * (kFull + s); };
     auto tfull_bar = [&](int a) { return bar0 + 8u * (kFull + kStages + a); };
@@ -661,106 +684,110 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
 
     const WaitGuard guard{abort_flag, status, wait_limit_ns};
 
-    if (warp == 0) {
-        // ------------------------------------------------------- TMA producer (both CTAs)
-        if (lane == 0) {
-            int stage = 0;
-            uint32_t phase = 0, issued = 0;
-            bool ok = true;
-            for (long long u = cluster; ok && u < units; u += n_clusters) {
-                int g, mb, nb;
-                ns_tile<BN>(u / splits, sh, g, mb, nb);
-                const int a_row = mb * kPairBM + 128 * static_cast<int>(rank);
-                const int b_row = nb * BN + (BN / 2) * static_cast<int>(rank);
-                const int k1 = first_k(u, 1);
-                for (int kb = first_k(u, 0); kb < k1; ++kb) {
-                    if (!mbar_wait_cl(empty_bar(stage), phase ^ 1u, guard)) { ok = false; break; }
-                    const uint32_t sa = sbase + stage * L::kStageBytes, sb = sa + 2 * L::kABox;
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const int bar_j = kSplit ? 0 : j, part = kSplit ? j : 0;
-                        const uint32_t fb = mapa_shared(full_bar(stage, bar_j), 0);
-                        if (leader && (!kSplit || j == 0))
-                            mbar_arrive_expect_tx(full_bar(stage, bar_j),
-                                                  2 * (L::kStageBytes / kSub));
-                        const int k0 = (kSplit ? kb : 2 * kb + j) * kBK;
-                        ns_load<A_MN, 128>(maps.A(part, g), sa + j * L::kABox, fb, a_row, k0, maps.z(g));
-                        ns_load<B_MN, BN / 2>(maps.B(part, g), sb + j * L::kBBox, fb, b_row, k0, maps.z(g));
-                    }
-                    ++issued;
-                    if (++stage == kStages) { stage = 0; phase ^= 1u; }
-                }
-            }
-            *issued_word = issued;
-            grid_dependency_trigger();
-        }
-        __syncwarp();
-    } else if (warp == 1) {
-        // ------------------------------------------------------- pair MMA (leader only)
-        if (leader && lane == 0) {
-            int stage = 0, acc = 0;
-            uint32_t phase = 0, acc_phase = 0;
-            bool ok = true, issued_any = false;
-            for (long long u = cluster; ok && u < units; u += n_clusters) {
-                const int k1 = first_k(u, 1);
-                for (int kb = first_k(u, 0); kb < k1; ++kb) {
-                    if (kSplit || kb == 0) {
-                        if (!mbar_wait_cl(tempty_bar(acc), acc_phase ^ 1u, guard)) {
-                            ok = false;
-                            break;
-                        }
-                        tc_fence_after();
-                    }
-                    const uint32_t d_tmem = tmem_base + static_cast<uint32_t>(acc * BN);
-                    const uint32_t sa = sbase + stage * L::kStageBytes, sb = sa + 2 * L::kABox;
-                    if constexpr (kSplit) {
-                        if (!mbar_wait_cl_poll(full_bar(stage, 0), phase, guard)) { ok = false; break; }
-                        tc_fence_after();
-                        // high x low, low x high, then high x high
-#pragma unroll
-                        for (int m = 0; m < 3; ++m) {
-#pragma unroll
-                            for (int kk = 0; kk < kBK / kUmmaK; ++kk)
-                                tc_mma_bf16_pair(
-                                    d_tmem, operand_desc<A_MN>(sa + (m == 1 ? L::kABox : 0), kk),
-                                    operand_desc<B_MN>(sb + (m == 0 ? L::kBBox : 0), kk), kIdesc,
-                                    (m != 0 || kk != 0) ? 1u : 0u);
-                        }
-                    } else {
+    if (warp < kFirst) {
+        if constexpr (kFirst == 4) ns_fewer_registers<kNsFewRegs>();
+        if (warp == 0) {
+            // ------------------------------------------------------- TMA producer (both CTAs)
+            if (lane == 0) {
+                int stage = 0;
+                uint32_t phase = 0, issued = 0;
+                bool ok = true;
+                for (long long u = cluster; ok && u < units; u += n_clusters) {
+                    int g, mb, nb;
+                    ns_tile<BN>(u / splits, sh, g, mb, nb);
+                    const int a_row = mb * kPairBM + 128 * static_cast<int>(rank);
+                    const int b_row = nb * BN + (BN / 2) * static_cast<int>(rank);
+                    const int k1 = first_k(u, 1);
+                    for (int kb = first_k(u, 0); kb < k1; ++kb) {
+                        if (!mbar_wait_cl(empty_bar(stage), phase ^ 1u, guard)) { ok = false; break; }
+                        const uint32_t sa = sbase + stage * L::kStageBytes, sb = sa + 2 * L::kABox;
 #pragma unroll
                         for (int j = 0; j < 2; ++j) {
-                            if (!mbar_wait_cl_poll(full_bar(stage, j), phase, guard)) { ok = false; break; }
-                            tc_fence_after();
-#pragma unroll
-                            for (int kk = 0; kk < kBK / kUmmaK; ++kk)
-                                tc_mma_bf16_pair(d_tmem, operand_desc<A_MN>(sa + j * L::kABox, kk),
-                                                 operand_desc<B_MN>(sb + j * L::kBBox, kk), kIdesc,
-                                                 (kb != 0 || j != 0 || kk != 0) ? 1u : 0u);
-                            issued_any = true;
+                            const int bar_j = kSplit ? 0 : j, part = kSplit ? j : 0;
+                            const uint32_t fb = mapa_shared(full_bar(stage, bar_j), 0);
+                            if (leader && (!kSplit || j == 0))
+                                mbar_arrive_expect_tx(full_bar(stage, bar_j),
+                                                      2 * (L::kStageBytes / kSub));
+                            const int k0 = (kSplit ? kb : 2 * kb + j) * kBK;
+                            ns_load<A_MN, 128>(maps.A(part, g), sa + j * L::kABox, fb, a_row, k0, maps.z(g));
+                            ns_load<B_MN, BN / 2>(maps.B(part, g), sb + j * L::kBBox, fb, b_row, k0, maps.z(g));
                         }
-                        if (!ok) break;
-                    }
-                    issued_any = true;
-                    tc_commit_pair_multicast(empty_bar(stage), kBoth);
-                    if (++stage == kStages) { stage = 0; phase ^= 1u; }
-                    if (kSplit || kb == k1 - 1) {
-                        tc_commit_pair_multicast(tfull_bar(acc), kBoth);
-                        if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
+                        ++issued;
+                        if (++stage == kStages) { stage = 0; phase ^= 1u; }
                     }
                 }
+                *issued_word = issued;
+                grid_dependency_trigger();
             }
-            if (issued_any) {
-                tc_commit_pair_multicast(drain_bar, 0x1);
-                mbar_wait_cl_drain(drain_bar, 0, kDrainLimitNs);
+            __syncwarp();
+        } else if (warp == 1) {
+            // ------------------------------------------------------- pair MMA (leader only)
+            if (leader && lane == 0) {
+                int stage = 0, acc = 0;
+                uint32_t phase = 0, acc_phase = 0;
+                bool ok = true, issued_any = false;
+                for (long long u = cluster; ok && u < units; u += n_clusters) {
+                    const int k1 = first_k(u, 1);
+                    for (int kb = first_k(u, 0); kb < k1; ++kb) {
+                        if (kSplit || kb == 0) {
+                            if (!mbar_wait_cl(tempty_bar(acc), acc_phase ^ 1u, guard)) {
+                                ok = false;
+                                break;
+                            }
+                            tc_fence_after();
+                        }
+                        const uint32_t d_tmem = tmem_base + static_cast<uint32_t>(acc * BN);
+                        const uint32_t sa = sbase + stage * L::kStageBytes, sb = sa + 2 * L::kABox;
+                        if constexpr (kSplit) {
+                            if (!mbar_wait_cl_poll(full_bar(stage, 0), phase, guard)) { ok = false; break; }
+                            tc_fence_after();
+                            // high x low, low x high, then high x high
+#pragma unroll
+                            for (int m = 0; m < 3; ++m) {
+#pragma unroll
+                                for (int kk = 0; kk < kBK / kUmmaK; ++kk)
+                                    tc_mma_bf16_pair(
+                                        d_tmem, operand_desc<A_MN>(sa + (m == 1 ? L::kABox : 0), kk),
+                                        operand_desc<B_MN>(sb + (m == 0 ? L::kBBox : 0), kk), kIdesc,
+                                        (m != 0 || kk != 0) ? 1u : 0u);
+                            }
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < 2; ++j) {
+                                if (!mbar_wait_cl_poll(full_bar(stage, j), phase, guard)) { ok = false; break; }
+                                tc_fence_after();
+#pragma unroll
+                                for (int kk = 0; kk < kBK / kUmmaK; ++kk)
+                                    tc_mma_bf16_pair(d_tmem, operand_desc<A_MN>(sa + j * L::kABox, kk),
+                                                     operand_desc<B_MN>(sb + j * L::kBBox, kk), kIdesc,
+                                                     (kb != 0 || j != 0 || kk != 0) ? 1u : 0u);
+                                issued_any = true;
+                            }
+                            if (!ok) break;
+                        }
+                        issued_any = true;
+                        tc_commit_pair_multicast(empty_bar(stage), kBoth);
+                        if (++stage == kStages) { stage = 0; phase ^= 1u; }
+                        if (kSplit || kb == k1 - 1) {
+                            tc_commit_pair_multicast(tfull_bar(acc), kBoth);
+                            if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
+                        }
+                    }
+                }
+                if (issued_any) {
+                    tc_commit_pair_multicast(drain_bar, 0x1);
+                    mbar_wait_cl_drain(drain_bar, 0, kDrainLimitNs);
+                }
             }
+            __syncwarp();
         }
-        __syncwarp();
     } else {
+        if constexpr (kFirst == 4) ns_more_registers<kNsManyRegs>();
         // ------------------------------------------------------- epilogue (both CTAs)
         const int q = warp & 3;               // TMEM lanes [32 q, 32 q + 32)
-        const int half = (warp - 2) / 4;
+        const int half = (warp - kFirst) / 4;
         constexpr int kWarpCols = BN / 2;     // columns [kWarpCols half, kWarpCols (half + 1))
-        const uint32_t buf = sbase + L::kOutOffset + static_cast<uint32_t>(warp - 2) * kOutBufBytes;
+        const uint32_t buf = sbase + L::kOutOffset + static_cast<uint32_t>(warp - kFirst) * kOutBufBytes;
         int acc = 0;
         uint32_t acc_phase = 0;
         // The lanes poll one by one, and lane 0 arrives alone: the warp is brought together after
@@ -815,7 +842,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
                 if (!ok) break;
                 if (splits > 1) {
                     constexpr int kWarpSums = kChunks * 32 * 32;
-                    const int w = static_cast<int>(rank) * kNsWarps + warp - 2;
+                    const int w = static_cast<int>(rank) * kNsWarps + warp - kFirst;
                     float* mine = sh.slots + (u * 2 * kNsWarps + w) * kWarpSums + lane;
 #pragma unroll
                     for (int c = 0; c < kChunks; ++c)

@@ -67,7 +67,7 @@ def matrix(rows, cols, kind, seed=0):
 SHAPES16 = [(8, 8), (16, 264), (64, 64), (256, 384), (384, 256), (264, 520), (520, 264),
             (1024, 256), (776, 1544), (1544, 776), (8, 2048)]
 SHAPES32 = [(1, 1), (1, 7), (9, 1), (33, 70), (64, 64), (70, 33), (255, 257), (300, 517),
-            (517, 300), (767, 1025)]
+            (517, 300), (767, 1025), (700, 2049), (2049, 700)]
 
 
 def limit(dtype, kind):
@@ -163,11 +163,12 @@ def test_a_bad_matrix_spoils_itself_only(fpo):
 
 
 # (bf16 512 x 2048: one launch for one matrix, a launch per product and wider tiles for four;
-# f32: with and without k-blocks in ranges)
+# f32: with and without k-blocks in ranges; 700 x 2049: 128-column tiles for one, 256 for four)
 @pytest.mark.parametrize("dtype,rows,cols", [("bf16", 264, 520), ("bf16", 512, 2048),
                                              ("bf16", 2048, 520), ("f32", 129, 263),
                                              ("f32", 257, 2300), ("f32", 2300, 130),
-                                             ("f32", 3, 5000)])
+                                             ("f32", 3, 5000), ("f32", 700, 2049),
+                                             ("f32", 2049, 700)])
 def test_in_place_groups_streams_and_graphs(fpo, dtype, rows, cols):
     """In place, in any group, on another stream, and in two graphs that share a workspace:
     the same bits.  Nothing behind the outputs is written."""
@@ -254,7 +255,7 @@ def test_calls_on_two_streams_at_once(fpo):
 
 
 @pytest.mark.parametrize("dtype,rows,cols,n", [("bf16", 512, 2048, 1), ("bf16", 512, 2048, 8),
-                                               ("f32", 257, 2300, 2)])
+                                               ("f32", 257, 2300, 2), ("f32", 700, 2049, 4)])
 def test_waits_that_run_out_are_reported(fpo, dtype, rows, cols, n):
     """Every form with a wait limit far below the first operands' way in: the status says so, and
     the next call, with the default limit and the same workspace, gives the same bits as before."""
