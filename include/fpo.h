@@ -350,8 +350,8 @@ size_t fpo_layernorm_vjp_workspace(int64_t T, int64_t d, int32_t dtype);
  *
  * g, x, g_out [T, d] and gamma [d] in dtype; gamma NULL: ones.  dgamma, dbeta [d] fp32.
  * Each output may be NULL (not all three).  g_out may not overlap g or x, nor dgamma dbeta
- * (FPO_ERR_ARG where they are the same).  The weight sums are added in a fixed order that depends on T and d only
- * (repeat calls give identical bits).  workspace: fpo_layernorm_vjp_workspace() bytes,
+ * (FPO_ERR_ARG where they are the same).  The weight sums are added in a fixed order that
+ * depends on T and d only (repeat calls give identical bits).  workspace: fpo_layernorm_vjp_workspace() bytes,
  * 256-byte aligned; may be NULL where that is 0 and when dgamma and dbeta are both NULL; it
  * holds no status word.
  * T = 0 sets dgamma and dbeta to zero.  Types, sizes and alignment as fpo_layernorm.
@@ -418,8 +418,8 @@ int32_t fpo_layer_optimize_grouped(int32_t n_layers, int64_t T, int64_t d, int64
 #define FPO_MAX_NS_SIDE 65536
 
 /* Bytes of workspace fpo_orthogonalize_grouped needs (0 on invalid sizes): per matrix of
- * rows x cols with smaller side m about 6 rows cols + 4 m^2 bytes (bf16) or 12 rows cols +
- * 8 m^2 (fp32). */
+ * rows x cols with smaller side m about 6 rows cols + 4 m^2 bytes (bf16), or 12 rows cols +
+ * 8 m^2 and at most 5 MB (fp32, and bf16 with a side of at most 64). */
 size_t fpo_orthogonalize_workspace(int32_t n_layers, int64_t rows, int64_t cols, int32_t dtype);
 
 /*
@@ -445,11 +445,11 @@ size_t fpo_orthogonalize_workspace(int32_t n_layers, int64_t rows, int64_t cols,
  *
  * bf16: products of fp16 operands scaled by powers of two from the bounds (11 bits instead of
  * bf16's 8), fp32 accumulation, the linear term a X from 22 bits of X, whatever its rank;
- * rows and cols multiples of 8; a side of at most 64 as in fp32 calls.  fp32: operands as sums of two fp16 numbers (22 bits), three
- * products, fp32 sums rounded to nearest every 64 products, the linear term in fp32; any
- * sizes.  Sides up to FPO_MAX_NS_SIDE.  A matrix with a NaN or an infinity gives NaN
- * throughout, and no other matrix changes.  Deterministic, and independent of what else is in
- * the group.
+ * rows and cols multiples of 8; matrices with a side of at most 64 as in fp32 calls.
+ * fp32: operands as sums of two fp16 numbers (22 bits), three products, fp32 sums rounded to
+ * nearest every 64 products, the linear term in fp32; any sizes.
+ * Sides up to FPO_MAX_NS_SIDE.  A matrix with a NaN or an infinity gives NaN throughout, and
+ * no other matrix changes.  Deterministic, and independent of what else is in the group.
  */
 int32_t fpo_orthogonalize_grouped(int32_t n_layers, int64_t rows, int64_t cols, int32_t dtype,
                                   const void* const* G, int32_t steps, const float* coeffs, float eps,

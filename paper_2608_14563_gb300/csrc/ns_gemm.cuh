@@ -165,12 +165,12 @@ __device__ __forceinline__ float2 unpack_f16x2(uint32_t w) {
     return __half22float2(*reinterpret_cast<const __half2*>(&w));
 }
 
-// An accumulator is free again: arrival on the barrier `bar` of the pair's leader.  Relaxed: what
-// goes before it are TMEM loads, which tcgen05.wait::ld and the tcgen05 fence order, and nothing in
-// memory is handed over.  (A release at cluster scope waits for the warp's stores and took most
-// of a k-block's turn in the kSplit kernels: fp32 2048 x 8192, five steps, 2046 us and 1649.)
+// An accumulator is free again: arrival on the barrier `bar` of the pair's leader.  What goes before
+// it are TMEM loads, which tcgen05.wait::ld and the tcgen05 fence order, and nothing in memory is
+// handed over: no release at cluster scope, which waits for the warp's stores and took most
+// of a k-block's turn in the kSplit kernels (fp32 2048 x 8192, five steps, 2046 us and 1640).
 __device__ __forceinline__ void arrive_leader(uint32_t bar) {
-    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(
+    asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(
                      mapa_shared(bar, 0))
                  : "memory");
 }
