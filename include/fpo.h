@@ -355,8 +355,8 @@ size_t fpo_layernorm_vjp_workspace(int64_t T, int64_t d, int32_t dtype);
  * 256-byte aligned; may be NULL where that is 0 and when dgamma and dbeta are both NULL; it
  * holds no status word.
  * T = 0 sets dgamma and dbeta to zero.  Types, sizes and alignment as fpo_layernorm.
- * A wait of either kernel that runs out (fpo_set_wait_limit_ns) leaves NaN in the rows that
- * it did not reach, and in dgamma and dbeta.
+ * A wait that runs out (fpo_set_wait_limit_ns; here and in fpo_layernorm) leaves NaN in the
+ * rows or parts of rows that were not reached, and in dgamma and dbeta.
  */
 int32_t fpo_layernorm_vjp(int64_t T, int64_t d, int32_t dtype, const void* g, const void* x,
                           const void* gamma, float eps, float min_rms, void* g_out, float* dgamma,

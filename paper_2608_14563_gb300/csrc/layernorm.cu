@@ -430,8 +430,8 @@ __global__ void __launch_bounds__(ln_threads<TH>(), ln_min_blocks<TH, true>())
 // With n elements in s, (s - mu)^2 <= (d / n) sigma^2 (the squares around mu of those n are part of
 // d sigma^2): the difference loses a factor of 1 + 2 d / n of its 24 bits, at most.
 //
-// Every wait is bounded.  One that runs out ends the block, which leaves NaN in the rows that it
-// did not reach and in its weight sums.
+// Every wait is bounded.  One that runs out ends the block, whose warps leave NaN in the rows (of
+// their columns) that they did not reach, and in their weight sums.
 constexpr int kLnMaxSlots = 16;
 constexpr int kLnStreamSmem = 220 * 1024;  // of dynamic shared memory: weights and slots
 

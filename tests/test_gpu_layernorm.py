@@ -221,8 +221,8 @@ def test_calls_on_two_streams_at_once(fpo):
 
 
 def test_a_wait_that_runs_out_leaves_nan(fpo):
-    """With the wait limit at a microsecond the stream kernels may give up: every row is right or
-    NaN; with the default limit the results are as before."""
+    """With the wait limit at a microsecond the stream kernels may give up: every element is right
+    or NaN; with the default limit the results are as before."""
     x, gamma, beta, g = inputs("bf16", 4100, 2568)
     d = x.shape[1]
 
@@ -240,10 +240,7 @@ def test_a_wait_that_runs_out_leaves_nan(fpo):
         short = call()
     finally:
         fpo.set_wait_limit_ns(2_000_000_000)
-    for a, b in zip(want[:2], short[:2]):
-        lost = b.isnan().all(1)
-        assert torch.equal(a[~lost], b[~lost])
-    for a, b in zip(want[2:], short[2:]):
+    for a, b in zip(want, short):
         assert (b.isnan() | (a == b)).all()
     assert all(torch.equal(a, b) for a, b in zip(want, call()))
 
