@@ -790,9 +790,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ns_threads<BN, kSpli
         const uint32_t buf = sbase + L::kOutOffset + static_cast<uint32_t>(warp - kFirst) * kOutBufBytes;
         int acc = 0;
         uint32_t acc_phase = 0;
-        // The lanes poll one by one, and lane 0 arrives alone: the warp is brought together after
-        // both, for tcgen05.ld writes the registers of all its lanes (without this, now and then
-        // over those of a lane still on its way).
+        // One answer for the warp, whose lanes poll one by one; it is together again after lane 0's
+        // arrival, and at every load of the accumulator (tmem_ld_32x32b_x32).
         auto ready = [&] {
             const bool in_time = mbar_wait_cl(tfull_bar(acc), acc_phase, guard);
             if (!__all_sync(0xffffffffu, in_time)) return false;

@@ -390,7 +390,9 @@ __global__ void __launch_bounds__(gemm_threads<Epi>(), 1)
             const bool ok = epilogue_tile<BN, Epi>(
                 ep, g, mb * kBM + q * 32, nb, (warp - 2) / 4, t_row, io,
                 [&] {
-                    if (!mbar_wait(tfull_bar(acc), acc_phase, guard)) return false;
+                    // one answer for the warp: its lanes wait, and run out of time, one by one
+                    const bool in_time = mbar_wait(tfull_bar(acc), acc_phase, guard);
+                    if (!__all_sync(0xffffffffu, in_time)) return false;
                     tc_fence_after();
                     return true;
                 },

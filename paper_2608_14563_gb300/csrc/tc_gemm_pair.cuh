@@ -52,8 +52,8 @@ constexpr int kPairBM = 256;  // output rows of one pair tile
 // host-input copy (csrc/host_copy.cu), which runs beside them.  A quarter of the SM has 16384
 // registers for its 2 (4 epilogue warps) or 3 (8) warps of the GEMM and the copy's.  Without
 // the limit the projection took 226 and the update 168, and the copies of a step's inputs ran
-// after the projection instead of beside it (27.05 instead of 23.97 ms a step).  At 160
-// two epilogues spill a little: EpiUpdate<2> 24 bytes, EpiStoreGroupF32<2> 20.
+// after the projection instead of beside it (27.05 instead of 23.97 ms a step).  No epilogue
+// spills at the limit.
 template <class Epi>
 constexpr int pair_regs() {
     constexpr int kRegs = Epi::kWarps == 4 ? 224 : 160;
@@ -421,7 +421,9 @@ __global__ void __cluster_dims__(2, 1, 1) __maxnreg__(pair_regs<Epi>())
         int acc = 0;
         uint32_t acc_phase = 0;
         auto ready = [&] {
-            if (!mbar_wait_cl(tfull_bar(acc), acc_phase, guard)) return false;
+            // one answer for the warp: its lanes wait, and run out of time, one by one
+            const bool in_time = mbar_wait_cl(tfull_bar(acc), acc_phase, guard);
+            if (!__all_sync(0xffffffffu, in_time)) return false;
             tc_fence_after();
             return true;
         };
