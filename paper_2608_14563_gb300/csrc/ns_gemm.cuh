@@ -1216,7 +1216,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1)
             // here, also one without a tile: none may count for a phase ahead of time
             if (warp == 2 && lane == 0 && ok) ns_wait_count(p.count, f * arrivals, guard);
             epilogue_sync();
-            ok = ok && !*abort_flag;
+            // (the flag may rise between the reads of two lanes: the warp goes on or gives up as one)
+            ok = __all_sync(0xffffffffu, ok && !*abort_flag);
             for (long long t = cluster; ok && t < sh.g.tiles; t += n_clusters) {
                 int g, mb, nb;
                 ns_tile<BN>(t, sh, g, mb, nb);

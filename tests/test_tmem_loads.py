@@ -52,3 +52,20 @@ def test_a_warp_gives_up_on_an_accumulator_as_one():
             after = text[m.end():m.end() + 160]
             assert re.search(r"if \(!__all_sync\(0xffffffffu, in_time\)\) return false;", after), name
     assert waits >= 4
+
+
+def test_a_warp_reads_the_abort_flag_as_one():
+    """Outside the waits themselves (one lane's, or voted on by their callers) the flag, which any
+    warp of the block may raise at any time, is read through a vote."""
+    reads = 0
+    for name, text in _sources():
+        if not name.endswith("gemm.cuh") and not name.endswith("gemm_pair.cuh"):
+            continue
+        for m in re.finditer(r"\*(?:g\.)?abort_flag\b(?! = )", text):
+            line = text[text.rindex("\n", 0, m.start()) + 1:text.index("\n", m.end())]
+            if "volatile int*" in line:
+                continue  # its declaration
+            reads += 1
+            in_wait = re.search(r"if \(\*g\.abort_flag\) return false;", line)
+            assert in_wait or "__all_sync(0xffffffffu," in line, (name, line)
+    assert reads >= 3
