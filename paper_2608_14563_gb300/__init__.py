@@ -243,8 +243,28 @@ def _nbytes(t: torch.Tensor) -> int:
     return t.numel() * t.element_size()
 
 
-def _workspace(nbytes: int, device) -> torch.Tensor:
-    return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device)
+def _empty(shape, dtype, device, stream) -> torch.Tensor:
+    """A tensor that belongs to the stream the call runs on.  Taken on the current stream while the
+    call is given another one, its memory could still be in use by earlier work of the current
+    stream, and would go to the next allocation there while the call's kernels still run."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):  # anything with a handle
+        stream = torch.cuda.ExternalStream(stream.cuda_stream, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _workspace(nbytes: int, device, stream) -> torch.Tensor:
+    return _empty(max(int(nbytes), 256), torch.uint8, device, stream)
+
+
+def _result(shape, device, stream) -> torch.Tensor:
+    """An fp64 result that the caller will read, also on the current stream."""
+    t = _empty(shape, torch.float64, device, stream)
+    if stream is not None:
+        t.record_stream(torch.cuda.current_stream(device))
+    return t
 
 
 def _expect(t, shape, dtype, name):
@@ -295,7 +315,7 @@ def error_signal(h, norm_w, W_U, targets, g_out, *, eps=1e-6, min_rms=0.5, loss_
                              loss_scale=loss_scale, t_chunk=t_chunk, stage_events=stage_events,
                              algo=algo, per_chunk_events=per_chunk_events)
     if workspace is None:
-        workspace = _workspace(error_signal_workspace(desc), h.device)
+        workspace = _workspace(error_signal_workspace(desc), h.device, stream)
     rc = _lib.fpo_error_signal(ctypes.byref(desc), _ptr(h), _ptr(norm_w), _ptr(W_U), _ptr(targets),
                                _ptr(g_out), _ptr(lse_out), _ptr(loss_out), _ptr(workspace),
                                _nbytes(workspace), _stream(stream))
@@ -322,7 +342,7 @@ def layer_update(g, A, lr, *, W_master=None, W_out=None, G_out=None, workspace=N
     T, d = g.shape
     d_ff = A.shape[1]
     if workspace is None:
-        workspace = _workspace(layer_update_workspace(), g.device)
+        workspace = _workspace(layer_update_workspace(), g.device, stream)
     rc = _lib.fpo_layer_update(T, d, d_ff, _dtype_code(g), _ptr(g), _ptr(A), float(lr),
                                _ptr(W_master), _ptr(W_out), _ptr(G_out), _ptr(workspace),
                                _nbytes(workspace), _stream(stream))
@@ -343,7 +363,7 @@ def layer_update_grouped(g, As, lr, *, W_masters=None, W_outs=None, G_outs=None,
     T, d = g.shape
     d_ff = As[0].shape[1]
     if workspace is None:
-        workspace = _workspace(layer_update_workspace(), g.device)
+        workspace = _workspace(layer_update_workspace(), g.device, stream)
     rc = _lib.fpo_layer_update_grouped(n, T, d, d_ff, _dtype_code(g), _ptr(g), _ptr_array(As, n),
                                        float(lr), _ptr_array(W_masters, n), _ptr_array(W_outs, n),
                                        _ptr_array(G_outs, n), _ptr(workspace), _nbytes(workspace),
@@ -359,7 +379,7 @@ def layer_update_grouped_signals(gs, As, lr, *, W_masters=None, W_outs=None, G_o
     T, d = gs[0].shape
     d_ff = As[0].shape[1]
     if workspace is None:
-        workspace = _workspace(layer_update_workspace(), gs[0].device)
+        workspace = _workspace(layer_update_workspace(), gs[0].device, stream)
     rc = _lib.fpo_layer_update_grouped_signals(
         n, T, d, d_ff, _dtype_code(gs[0]), _ptr_array(gs, n), _ptr_array(As, n), float(lr),
         _ptr_array(W_masters, n), _ptr_array(W_outs, n), _ptr_array(G_outs, n), _ptr(workspace),
@@ -385,7 +405,7 @@ def layer_optimize_grouped(gs, As, opt, W_masters, *, W_outs=None, states1=None,
     T, d = gs[0].shape
     d_ff = As[0].shape[1]
     if workspace is None:
-        workspace = _workspace(layer_optimize_workspace(n, d, d_ff), gs[0].device)
+        workspace = _workspace(layer_optimize_workspace(n, d, d_ff), gs[0].device, stream)
     rc = _lib.fpo_layer_optimize_grouped(
         n, T, d, d_ff, _dtype_code(gs[0]), _ptr_array(gs, n), _ptr_array(As, n), ctypes.byref(opt),
         _ptr_array(W_masters, n), _ptr_array(W_outs, n), _ptr_array(states1, n),
@@ -430,7 +450,7 @@ def orthogonalize_grouped(Gs, Os, *, steps=5, coeffs=None, eps=1e-7, workspace=N
     _expect_all(Os, n, G.shape, G.dtype, "Os")
     dt = _dtype_code(G)
     if workspace is None:
-        workspace = _workspace(orthogonalize_workspace(n, rows, cols, dt), G.device)
+        workspace = _workspace(orthogonalize_workspace(n, rows, cols, dt), G.device, stream)
     co = _coeffs(coeffs, steps)
     rc = _lib.fpo_orthogonalize_grouped(n, rows, cols, dt, _ptr_array(Gs, n), int(steps), co,
                                         float(eps), _ptr_array(Os, n), _ptr(workspace),
@@ -470,7 +490,7 @@ def layer_muon_grouped(gs, As, opt, W_masters, momenta, *, W_outs=None, workspac
     _expect_all(W_outs, n, (d, d_ff), dtype, "W_outs")
     dt = _dtype_code(gs[0])
     if workspace is None:
-        workspace = _workspace(layer_muon_workspace(n, d, d_ff, dt), gs[0].device)
+        workspace = _workspace(layer_muon_workspace(n, d, d_ff, dt), gs[0].device, stream)
     rc = _lib.fpo_layer_muon_grouped(n, T, d, d_ff, dt, _ptr_array(gs, n), _ptr_array(As, n),
                                      ctypes.byref(opt), _ptr_array(W_masters, n),
                                      _ptr_array(W_outs, n), _ptr_array(momenta, n),
@@ -484,7 +504,7 @@ def gate_up_signals(g, W3_init, a, b, dA, dB, *, workspace=None, stream=None):
     T, d = g.shape
     d_ff = W3_init.shape[1]
     if workspace is None:
-        workspace = _workspace(layer_update_workspace(), g.device)
+        workspace = _workspace(layer_update_workspace(), g.device, stream)
     rc = _lib.fpo_gate_up_signals(T, d, d_ff, _dtype_code(g), _ptr(g), _ptr(W3_init), _ptr(a),
                                   _ptr(b), _ptr(dA), _ptr(dB), _ptr(workspace), _nbytes(workspace),
                                   _stream(stream))
@@ -556,7 +576,7 @@ def layernorm_vjp(g, x, gamma, g_out, *, eps=1e-5, min_rms=0.5, dgamma=None, dbe
     if workspace is None and (dgamma is not None or dbeta is not None):
         need = layernorm_vjp_workspace(T, d, _dtype_code(x))
         if need:  # (0: a short batch)
-            workspace = _workspace(need, x.device)
+            workspace = _workspace(need, x.device, stream)
     rc = _lib.fpo_layernorm_vjp(T, d, _dtype_code(x), _ptr(g), _ptr(x), _ptr(gamma), float(eps),
                                 float(min_rms), _ptr(g_out), _ptr(dgamma), _ptr(dbeta),
                                 _ptr(workspace), 0 if workspace is None else _nbytes(workspace),
@@ -574,9 +594,9 @@ def cosine(X, Y, out=None, *, workspace=None, stream=None):
     """fpo_cosine: returns a device fp64 tensor [<X,Y>, |X|^2, |Y|^2, cos]."""
     n = X.numel()
     if out is None:
-        out = torch.empty(4, dtype=torch.float64, device=X.device)
+        out = _result(4, X.device, stream)
     if workspace is None:
-        workspace = _workspace(cosine_workspace(n), X.device)
+        workspace = _workspace(cosine_workspace(n), X.device, stream)
     rc = _lib.fpo_cosine(n, _dtype_code(X), _ptr(X), _ptr(Y), _ptr(out), _ptr(workspace),
                          _nbytes(workspace), _stream(stream))
     _check(rc, "fpo_cosine")
@@ -599,9 +619,9 @@ def cosine_grouped(X, Y, out=None, *, workspace=None, stream=None):
     if any(t.dtype != X[0].dtype for t in list(X) + list(Y)):
         raise TypeError("X and Y share one dtype")
     if out is None:
-        out = torch.empty(n_layers, 4, dtype=torch.float64, device=X[0].device)
+        out = _result((n_layers, 4), X[0].device, stream)
     if workspace is None:
-        workspace = _workspace(cosine_grouped_workspace(n_layers, n), X[0].device)
+        workspace = _workspace(cosine_grouped_workspace(n_layers, n), X[0].device, stream)
     xarr = (_vp * n_layers)(*[_ptr(t) for t in X])
     yarr = (_vp * n_layers)(*[_ptr(t) for t in Y])
     rc = _lib.fpo_cosine_grouped(n_layers, n, _dtype_code(X[0]), xarr, yarr, _ptr(out),
@@ -623,9 +643,9 @@ def layer_grad_cosine_grouped(g, As, Ys, G_outs, out=None, *, workspace=None, st
     T, d = g.shape
     d_ff = As[0].shape[1]
     if out is None:
-        out = torch.empty(n, 4, dtype=torch.float64, device=g.device)
+        out = _result((n, 4), g.device, stream)
     if workspace is None:
-        workspace = _workspace(layer_grad_cosine_workspace(n, d, d_ff), g.device)
+        workspace = _workspace(layer_grad_cosine_workspace(n, d, d_ff), g.device, stream)
     arr = lambda ts: (_vp * n)(*[_ptr(t) for t in ts])  # noqa: E731
     rc = _lib.fpo_layer_grad_cosine_grouped(n, T, d, d_ff, _dtype_code(g), _ptr(g), arr(As),
                                             arr(Ys), arr(G_outs), _ptr(out), _ptr(workspace),
@@ -650,9 +670,9 @@ def norm_ratio(G, W, rel_step=0.01, out=None, *, workspace=None, stream=None):
     if any(t.dtype != G[0].dtype for t in G) or any(t.dtype != W[0].dtype for t in W):
         raise TypeError("the G_l share one dtype and the W_l share one dtype")
     if out is None:
-        out = torch.empty(n_layers, 4, dtype=torch.float64, device=G[0].device)
+        out = _result((n_layers, 4), G[0].device, stream)
     if workspace is None:
-        workspace = _workspace(norm_ratio_workspace(n_layers, n), G[0].device)
+        workspace = _workspace(norm_ratio_workspace(n_layers, n), G[0].device, stream)
     garr = (_vp * n_layers)(*[_ptr(t) for t in G])
     warr = (_vp * n_layers)(*[_ptr(t) for t in W])
     rc = _lib.fpo_norm_ratio(n_layers, n, _dtype_code(G[0]), garr, _dtype_code(W[0]), warr,
