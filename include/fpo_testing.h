@@ -72,6 +72,13 @@ int64_t fpo_testing_direct_fixup_rows(const fpo_error_signal_desc* desc,
 uint64_t fpo_testing_kernel_launches(void);
 
 /*
+ * The bounds of the singular values that fpo_orthogonalize_grouped scales its operands by:
+ * bounds[k] the largest |a s + b s^3 + c s^5| of step k over [0, bounds[k - 1]] ([0, 1] for the
+ * first).  coeffs: steps triples (a, b, c), finite; host memory, no device call.
+ */
+void fpo_testing_ns_bounds(int32_t steps, const float* coeffs, double* bounds);
+
+/*
  * Failure-detection check of the bounded waits every kernel uses: launches one
  * block that waits on a shared-memory mbarrier nothing ever arrives on, with
  * a limit of `limit_ns` nanoseconds.  The wait gives up, the kernel records

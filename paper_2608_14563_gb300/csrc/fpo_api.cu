@@ -1061,6 +1061,10 @@ void fpo_testing_set_band(int32_t band) { set_band_override(band); }
 
 uint64_t fpo_testing_kernel_launches(void) { return fpo::launches(); }
 
+void fpo_testing_ns_bounds(int32_t steps, const float* coeffs, double* bounds) {
+    ns_bounds(steps, coeffs, bounds);
+}
+
 int64_t fpo_testing_direct_fixup_rows(const fpo_error_signal_desc* desc, const void* workspace,
                                       void* stream) {
     if (es_check_desc(desc) != FPO_OK || !workspace || desc->T == 0) return -1;

@@ -302,6 +302,8 @@ struct NsTarget {
     float* const* W;
     float keep, rate;
 };
+// Bound of the singular values after every step (3 coefficients per step; 1 at the start).
+void ns_bounds(int steps, const float* coeffs, double* bounds);
 // Whether finite coefficients (3 per step) keep the iteration's bounds in range.
 bool ns_coeffs_ok(int steps, const float* coeffs);
 size_t ns_workspace_bytes(int n, int rows, int cols, int dtype, bool muon);

@@ -596,15 +596,13 @@ double odd_max(double c1, double c3, double c5, double u) {
             if (v > best) best = v;
         }
     };
-    // c1 + 3 c3 z + 5 c5 z^2 = 0
-    if (c5 != 0.0) {
-        const double q = 9.0 * c3 * c3 - 20.0 * c5 * c1;
-        if (q >= 0.0) {
-            at((-3.0 * c3 + sqrt(q)) / (10.0 * c5));
-            at((-3.0 * c3 - sqrt(q)) / (10.0 * c5));
-        }
-    } else if (c3 != 0.0) {
-        at(-c1 / (3.0 * c3));
+    // The roots of c1 + 3 c3 z + 5 c5 z^2 as h / (5 c5) and c1 / h, h = -(3 c3 +- sqrt(..)) / 2 with
+    // the sign that adds: neither is lost to cancellation, however small c5 or c1 is.
+    const double q = 9.0 * c3 * c3 - 20.0 * c5 * c1;
+    if (q >= 0.0) {
+        const double h = -0.5 * (3.0 * c3 + copysign(sqrt(q), c3));
+        if (c5 != 0.0) at(h / (5.0 * c5));
+        if (h != 0.0) at(c1 / h);
     }
     return best;
 }
@@ -882,6 +880,12 @@ cudaError_t run_momentum(int n, int T, int rows, int cols, const NsMomentum& mom
 }
 
 }  // namespace
+
+void ns_bounds(int steps, const float* coeffs, double* bounds) {
+    double u = 1.0;
+    for (int k = 0; k < steps; ++k)
+        bounds[k] = u = odd_max(coeffs[3 * k], coeffs[3 * k + 1], coeffs[3 * k + 2], u);
+}
 
 bool ns_coeffs_ok(int steps, const float* coeffs) {
     double u = 1.0;
