@@ -450,6 +450,7 @@ size_t fpo_orthogonalize_workspace(int32_t n_layers, int64_t rows, int64_t cols,
  * nearest every 64 products, the linear term in fp32; any sizes.
  * Sides up to FPO_MAX_NS_SIDE.  A matrix with a NaN or an infinity gives NaN throughout, and
  * no other matrix changes.  Deterministic, and independent of what else is in the group.
+ * After a wait that ran out (FPO_ERR_TIMEOUT in the status word) O holds no result.
  */
 int32_t fpo_orthogonalize_grouped(int32_t n_layers, int64_t rows, int64_t cols, int32_t dtype,
                                   const void* const* G, int32_t steps, const float* coeffs, float eps,
@@ -490,6 +491,8 @@ size_t fpo_layer_muon_workspace(int32_t n_layers, int64_t d, int64_t d_ff, int32
  * NULL); all HOST arrays of n_layers device pointers.  g and A entries may repeat, the others
  * not; nor may one stand in two arrays, but for W_out[l] = W_master[l] in fp32 (FPO_ERR_ARG).
  * No relative clip: the step's norm is lr scale ||O_l||_F, about lr scale sqrt(rank).
+ * After a wait that ran out (FPO_ERR_TIMEOUT in the status word) W_master and W_out are as
+ * before the call; momentum may have taken the step, as a whole or in parts.
  * workspace: fpo_layer_muon_workspace() bytes, 256-byte aligned (device status word first).
  * Sizes and precision as fpo_orthogonalize_grouped.
  */

@@ -185,8 +185,8 @@ __global__ void __launch_bounds__(kPassThreads)
     if (threadIdx.x == 0) part[static_cast<size_t>(layer) * gridDim.x + blockIdx.x] = t;
 }
 
-// W <- keep W - rate O, and out (or null) = W in the call's type.  A pass of its own: 12 to 18 bytes
-// an element.
+// W <- keep W - rate O, and out (or null) = W in the call's type; neither where a wait of the call
+// has run out, for O is then no result.  A pass of its own: 12 to 18 bytes an element.
 struct NsWeights {
     const float* O[kMaxGroups];
     float* W[kMaxGroups];
@@ -195,9 +195,11 @@ struct NsWeights {
 
 template <typename TT>
 __global__ void __launch_bounds__(kPassThreads)
-    ns_weight_kernel(const __grid_constant__ NsWeights p, size_t n, float keep, float rate) {
+    ns_weight_kernel(const __grid_constant__ NsWeights p, size_t n, float keep, float rate,
+                     const unsigned* status) {
     grid_dependency_trigger();
     grid_dependency_wait();
+    if (*status != 0) return;
     const int layer = blockIdx.y;
     const float* O = p.O[layer];
     float* W = p.W[layer];
@@ -987,9 +989,9 @@ cudaError_t launch_newton_schulz(int n, int rows, int cols, int dtype, const voi
     const dim3 wgrid(static_cast<unsigned>(units < 2048 ? units : 2048), n);
     if (f32)
         return launch_chained(ns_weight_kernel<float>, wgrid, kPassThreads, 0, st, w, numel, to.keep,
-                              to.rate);
+                              to.rate, static_cast<const unsigned*>(status));
     return launch_chained(ns_weight_kernel<__nv_bfloat16>, wgrid, kPassThreads, 0, st, w, numel,
-                          to.keep, to.rate);
+                          to.keep, to.rate, static_cast<const unsigned*>(status));
 }
 
 }  // namespace fpo
