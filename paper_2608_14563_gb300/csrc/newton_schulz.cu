@@ -513,8 +513,8 @@ cudaError_t launch_ns(const typename Epi::Maps& maps, const typename Epi::Params
     sh.splits = kSplit ? ns_splits(ns_matrix_tiles(M, N, tri), K) : 1;
     sh.slots = rg.slots;
     sh.counts = rg.counts;
-    constexpr int kThreads = ns_threads<BN, kSplit>();
-    if constexpr (ns_first_warp<BN, kSplit>() == 4) {
+    constexpr int kThreads = ns_threads<BN, kSplit, Epi>();
+    if constexpr (ns_first_warp<BN, kSplit, Epi>() == 4) {
         // the warpgroups' new shares have to fit into what the block is launched with: an increase
         // beyond it would never be granted
         static std::atomic<int> regs{0};
@@ -824,12 +824,6 @@ cudaError_t run_iteration(const NsLayout& L, uint8_t* ws, int n, int rows, int c
 }
 
 // G_l = g[l]^T A[l] (bf16) with the momentum in the epilogue; *parts: the partial sums per layer.
-// A launch takes at most kGradTokens tokens, the sums so far waiting in U: the tensor core
-// truncates its fp32 sums (ns_gemm.cuh), so their error grows with the tokens in one
-// accumulator (in norm 4e-6 of G for 4096 tokens, 1.9e-5 for 16384; 1.4e-5 and 8.3e-5 where all products
-// are positive).  16384 tokens, 4096 x 11008, one Newton-Schulz step: 1616 us, 1480 in one
-// launch, 1778 in launches of 2048.
-constexpr int kGradTokens = 4096;
 cudaError_t run_momentum(int n, int T, int rows, int cols, const NsMomentum& mom, float* U,
                          size_t u_stride, double* part, int* parts, unsigned* status,
                          cudaStream_t st) {
@@ -849,36 +843,26 @@ cudaError_t run_momentum(int n, int T, int rows, int cols, const NsMomentum& mom
     const bool narrow = 4 * tiles <= di.sm_count;  // as in run_ns
     ep.n_blocks = narrow ? (cols + 127) / 128 : (cols + 255) / 256;
     *parts = ep.m_blocks * ep.n_blocks * 2 * kNsWarps;
-    const int launches = T / kGradTokens + (T % kGradTokens != 0);
-    const int share = static_cast<int>(round_up(T / launches + (T % launches != 0), kBK));
-    for (int t0 = 0; t0 < T;) {
-        const int t = T - t0 < share ? T - t0 : share;
-        NsGradMaps maps;
-        for (int l = 0; l < kMaxGroups; ++l) {
-            if (l >= n) {
-                maps.a[l] = maps.a[0];
-                maps.b[l] = maps.b[0];
-                continue;
-            }
-            const auto* gl = static_cast<const __half*>(mom.g[l]) + static_cast<size_t>(t0) * rows;
-            const auto* Al = static_cast<const __half*>(mom.A[l]) + static_cast<size_t>(t0) * cols;
-            const NsOperand g = {{gl, nullptr}, rows, t, 1, rows, static_cast<size_t>(t) * rows};
-            const NsOperand A = {{Al, nullptr}, cols, t, 1, cols, static_cast<size_t>(t) * cols};
-            if (!ns_map(&maps.a[l], g, 0, true, 64, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16) ||
-                !ns_map(&maps.b[l], A, 0, true, 64, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16))
-                return cudaErrorInvalidValue;
+    NsGradMaps maps;
+    for (int l = 0; l < kMaxGroups; ++l) {
+        if (l >= n) {
+            maps.a[l] = maps.a[0];
+            maps.b[l] = maps.b[0];
+            continue;
         }
-        ep.add = t0 > 0;
-        ep.last = t0 + t >= T;
-        const cudaError_t e =
-            narrow ? launch_ns<128, true, true, false, EpiMomentum<128>>(maps, ep, rows, cols, t, n, false,
-                                                                         {}, status, st)
-                   : launch_ns<256, true, true, false, EpiMomentum<256>>(maps, ep, rows, cols, t, n, false,
-                                                                         {}, status, st);
-        if (e != cudaSuccess) return e;
-        t0 += t;
+        const NsOperand g = {{static_cast<const __half*>(mom.g[l]), nullptr}, rows, T, 1, rows,
+                             static_cast<size_t>(T) * rows};
+        const NsOperand A = {{static_cast<const __half*>(mom.A[l]), nullptr}, cols, T, 1, cols,
+                             static_cast<size_t>(T) * cols};
+        if (!ns_map(&maps.a[l], g, 0, true, 64, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16) ||
+            !ns_map(&maps.b[l], A, 0, true, 64, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16))
+            return cudaErrorInvalidValue;
     }
-    return cudaSuccess;
+    if (narrow)
+        return launch_ns<128, true, true, false, EpiMomentum<128>>(maps, ep, rows, cols, T, n, false, {},
+                                                                   status, st);
+    return launch_ns<256, true, true, false, EpiMomentum<256>>(maps, ep, rows, cols, T, n, false, {},
+                                                               status, st);
 }
 
 }  // namespace

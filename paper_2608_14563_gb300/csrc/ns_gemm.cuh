@@ -24,7 +24,8 @@
 // to nearest, while the next k-blocks fill other accumulators: 64 sums per thread with BN 128,
 // 0.85 us a k-block (0.4 of MMAs at the tensor rate, 0.6 of operands from shared memory), and 128
 // with BN 256, 1.03 us (0.8 of MMAs), where the warps share registers out anew (with 168 each
-// the loop spilled and took 2.7 us).
+// the loop spilled and took 2.7 us).  The gradient of the Muon step (EpiMomentum) is drained the
+// same way, every kRun stages.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -55,6 +56,13 @@ __host__ __device__ constexpr uint32_t idesc_f16_f32(int M, int N, bool a_mn, bo
 constexpr int kNsWarps = 8;                   // epilogue warps
 constexpr int kNsThreads = 64 + 32 * kNsWarps;
 
+// Stages whose sums one accumulator holds before the epilogue warps add it to their registers
+// ("drained"); 0: all of a tile's.
+template <bool kSplit, class Epi>
+constexpr int ns_run() {
+    return kSplit ? 1 : Epi::kRun;
+}
+
 // Accumulators in TMEM.  kSplit: four, as the MMAs of a k-block take no longer than the way to
 // the epilogue warps and back (eight fp32 256 x 4096, five steps: 421 us with two, 388 with four).
 constexpr int kNsMaxAccs = 4;
@@ -63,17 +71,18 @@ constexpr int ns_accs() {
     return kSplit && BN == 128 ? kNsMaxAccs : 2;
 }
 
-// Warps before the epilogue's.  kSplit with 256 columns: a warpgroup of its own for the producer and
-// the MMA issuer, whose registers the epilogue's two warpgroups take over (128 sums a thread):
-// 384 threads are launched with 168 each (launch_ns looks), and go on with 40, 232 and 232.
+// Warps before the epilogue's.  kSplit with 256 columns, and EpiMomentum, which holds the momentum
+// beside the sums: a warpgroup of its own for the producer and the MMA issuer, whose registers the
+// epilogue's two warpgroups take over (128 sums a thread): 384 threads are launched with 168 each
+// (launch_ns looks), and go on with 40, 232 and 232.
 constexpr int kNsFewRegs = 40, kNsManyRegs = 232;
-template <int BN, bool kSplit>
+template <int BN, bool kSplit, class Epi>
 constexpr int ns_first_warp() {
-    return kSplit && BN == 256 ? 4 : 2;
+    return (kSplit ? BN == 256 : Epi::kRun > 0) ? 4 : 2;
 }
-template <int BN, bool kSplit>
+template <int BN, bool kSplit, class Epi>
 constexpr int ns_threads() {
-    return 32 * (ns_first_warp<BN, kSplit>() + kNsWarps);
+    return 32 * (ns_first_warp<BN, kSplit, Epi>() + kNsWarps);
 }
 template <int R>
 __device__ __forceinline__ void ns_more_registers() {
@@ -220,6 +229,7 @@ template <int BN, bool kSplit>
 struct EpiSym : EpiSymBase<kSplit> {
     using Maps = NsMaps;
     static constexpr bool kBf16 = false;
+    static constexpr int kRun = 0;
     using Params = typename EpiSymBase<kSplit>::Params;
     static constexpr int kParts = kSplit ? 2 : 1;
     static constexpr int kChunks = BN / 2 / 32;
@@ -368,6 +378,7 @@ template <int BN, bool kSplit, int kOut>
 struct EpiApply : EpiApplyBase<kSplit, kOut> {
     using Maps = NsMaps;
     static constexpr bool kBf16 = false;
+    static constexpr int kRun = 0;
     using Out = typename EpiApplyBase<kSplit, kOut>::Out;
     using Params = typename EpiApplyBase<kSplit, kOut>::Params;
     static constexpr int kChunks = BN / 2 / 32;
@@ -498,6 +509,11 @@ struct EpiApply : EpiApplyBase<kSplit, kOut> {
 // (nesterov) or M, both fp32 [M, N] (N a multiple of 8), and the sum of U's squares over the
 // warp's part of the tile to part[matrix][tile][16 warps of the pair].  (The library's
 // EpiStoreGroupF32 followed by a pass over G, M and U took 97 us for two 8192 x 2048 matrices.)
+//
+// M is a state in fp32, and the tensor core truncates its sums: with 4096 tokens in one accumulator
+// M was 3.4e-6 off in norm, six times an fp32 product's error (all products positive: 1.4e-5).  So
+// the accumulator is drained every 512 tokens: 4.8e-7 (7.1e-7) for any number of tokens, beside
+// an fp32 product's 2e-7 to 1.5e-6.  Two 4096 x 11008 layers, the whole step: 5.30 ms, 5.29 without.
 struct EpiMomentumBase {
     struct Params {
         float* M[kMaxGroups];
@@ -507,7 +523,6 @@ struct EpiMomentumBase {
         int rows, cols, m_blocks, n_blocks;
         float mu;
         bool nesterov;
-        bool add, last;       // U holds the sums of the tokens before; these are the last tokens
     };
 };
 
@@ -527,6 +542,7 @@ template <int BN>
 struct EpiMomentum : EpiMomentumBase {
     using Maps = NsGradMaps;
     static constexpr bool kBf16 = true;
+    static constexpr int kRun = 4;  // stages of 128 tokens
     static constexpr int kChunks = BN / 2 / 32;
     static constexpr int kAcc = 8;
 
@@ -534,9 +550,9 @@ struct EpiMomentum : EpiMomentumBase {
     double* slot;
     int r0, c0, rows, cols;
     float mu;
-    bool nesterov, add, last;
+    bool nesterov;
     double squares;
-    float4 m[kAcc];           // of the next chunk: M, before the last tokens the sums so far
+    float4 m[kAcc];    // M of the next chunk
 
     __device__ __forceinline__ bool in(int i, int c) const {
         return r0 + 4 * i < rows && c0 + 32 * c < cols;
@@ -548,14 +564,12 @@ struct EpiMomentum : EpiMomentumBase {
 #pragma unroll
         for (int i = 0; i < kAcc; ++i) {
             m[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (in(i, c) && (last || add))
-                m[i] = *reinterpret_cast<const float4*>((last ? M : U) + at(i, c));
+            if (in(i, c)) m[i] = *reinterpret_cast<const float4*>(M + at(i, c));
         }
     }
     __device__ __forceinline__ EpiMomentum(const Params& p, int g, int row0, int col0, int lane, bool)
         : M(p.M[g]), U(p.U + g * p.u_stride), r0(row0 + lane / 8), c0(col0 + 4 * (lane % 8)),
-          rows(p.rows), cols(p.cols), mu(p.mu), nesterov(p.nesterov), add(p.add), last(p.last),
-          squares(0.0) {
+          rows(p.rows), cols(p.cols), mu(p.mu), nesterov(p.nesterov), squares(0.0) {
         const int warps = 2 * kNsWarps;  // of a tile: 8 blocks of 32 rows x 2 halves of the columns
         const long long tile = (static_cast<long long>(g) * p.m_blocks + row0 / kPairBM) * p.n_blocks +
                                col0 / BN;
@@ -568,32 +582,24 @@ struct EpiMomentum : EpiMomentumBase {
         float run = 0.f;
 #pragma unroll
         for (int i = 0; i < kAcc; ++i) {
-            float4 g = ld_shared_f4(ns_piece(buf, lane, i));
-            if (add) {
-                float4 s = m[i];
-                if (last && in(i, c)) s = *reinterpret_cast<const float4*>(U + at(i, c));
-                g = make_float4(g.x + s.x, g.y + s.y, g.z + s.z, g.w + s.w);
+            const float4 g = ld_shared_f4(ns_piece(buf, lane, i));
+            float4 a = m[i];
+            a.x = fmaf(mu, a.x, g.x);
+            a.y = fmaf(mu, a.y, g.y);
+            a.z = fmaf(mu, a.z, g.z);
+            a.w = fmaf(mu, a.w, g.w);
+            float4 u = a;
+            if (nesterov) {
+                u.x = fmaf(mu, a.x, g.x);
+                u.y = fmaf(mu, a.y, g.y);
+                u.z = fmaf(mu, a.z, g.z);
+                u.w = fmaf(mu, a.w, g.w);
             }
-            float4 u = g;
-            if (last) {
-                float4 a = m[i];
-                a.x = fmaf(mu, a.x, g.x);
-                a.y = fmaf(mu, a.y, g.y);
-                a.z = fmaf(mu, a.z, g.z);
-                a.w = fmaf(mu, a.w, g.w);
-                u = a;
-                if (nesterov) {
-                    u.x = fmaf(mu, a.x, g.x);
-                    u.y = fmaf(mu, a.y, g.y);
-                    u.z = fmaf(mu, a.z, g.z);
-                    u.w = fmaf(mu, a.w, g.w);
-                }
-                if (in(i, c)) {
-                    *reinterpret_cast<float4*>(M + at(i, c)) = a;
-                    run += square_sum4(u, squares);
-                }
+            if (in(i, c)) {
+                *reinterpret_cast<float4*>(M + at(i, c)) = a;
+                *reinterpret_cast<float4*>(U + at(i, c)) = u;
+                run += square_sum4(u, squares);
             }
-            if (in(i, c)) *reinterpret_cast<float4*>(U + at(i, c)) = u;
         }
         squares += run;
         if (c + 1 < kChunks) fetch(c + 1);
@@ -603,20 +609,21 @@ struct EpiMomentum : EpiMomentumBase {
         double t = squares;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
-        if (lane == 0 && last) *slot = t;
+        if (lane == 0) *slot = t;
         __syncwarp();
     }
 };
 
 // ---------------------------------------------------------------------------
 template <int BN, bool A_MN, bool B_MN, bool kSplit, class Epi>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ns_threads<BN, kSplit>(), 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ns_threads<BN, kSplit, Epi>(), 1)
     ns_gemm_kernel(const __grid_constant__ typename Epi::Maps maps,
                    const __grid_constant__ typename Epi::Params ep, const NsShape sh,
                    unsigned int* status, unsigned long long wait_limit_ns) {
     using L = NsSmem<BN>;
     constexpr int kStages = L::kStages;
     constexpr int kSub = kSplit ? 1 : 2;   // k-blocks (and full barriers) per stage
+    constexpr int kRun = ns_run<kSplit, Epi>();
     constexpr uint32_t kIdesc = Epi::kBf16 ? idesc_bf16_f32(kPairBM, BN, A_MN, B_MN)
                                            : idesc_f16_f32(kPairBM, BN, A_MN, B_MN);
     constexpr uint16_t kBoth = 0x3;
@@ -642,7 +649,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ns_threads<BN, kSpli
 
     const uint32_t bar0 = sbase + L::kBarOffset;
     constexpr int kFull = kStages * kSub, kAccs = ns_accs<kSplit, BN>();
-    constexpr int kFirst = ns_first_warp<BN, kSplit>();
+    constexpr int kFirst = ns_first_warp<BN, kSplit, Epi>();
     auto full_bar = [&](int s, int j) { return bar0 + 8u * (s * kSub + j); };
     auto empty_bar = [&](int s) { return bar0 + 8u * (kFull + s); };
     auto tfull_bar = [&](int a) { return bar0 + 8u * (kFull + kStages + a); };
@@ -727,9 +734,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ns_threads<BN, kSpli
                 uint32_t phase = 0, acc_phase = 0;
                 bool ok = true, issued_any = false;
                 for (long long u = cluster; ok && u < units; u += n_clusters) {
-                    const int k1 = first_k(u, 1);
-                    for (int kb = first_k(u, 0); kb < k1; ++kb) {
-                        if (kSplit || kb == 0) {
+                    const int k0 = first_k(u, 0), k1 = first_k(u, 1);
+                    for (int kb = k0; kb < k1; ++kb) {
+                        const bool first = kRun > 0 ? (kb - k0) % (kRun > 0 ? kRun : 1) == 0 : kb == k0;
+                        if (first) {
                             if (!mbar_wait_cl(tempty_bar(acc), acc_phase ^ 1u, guard)) {
                                 ok = false;
                                 break;
@@ -760,7 +768,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ns_threads<BN, kSpli
                                 for (int kk = 0; kk < kBK / kUmmaK; ++kk)
                                     tc_mma_bf16_pair(d_tmem, operand_desc<A_MN>(sa + j * L::kABox, kk),
                                                      operand_desc<B_MN>(sb + j * L::kBBox, kk), kIdesc,
-                                                     (kb != 0 || j != 0 || kk != 0) ? 1u : 0u);
+                                                     (!first || j != 0 || kk != 0) ? 1u : 0u);
                                 issued_any = true;
                             }
                             if (!ok) break;
@@ -768,7 +776,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ns_threads<BN, kSpli
                         issued_any = true;
                         tc_commit_pair_multicast(empty_bar(stage), kBoth);
                         if (++stage == kStages) { stage = 0; phase ^= 1u; }
-                        if (kSplit || kb == k1 - 1) {
+                        if (kb == k1 - 1 || (kRun > 0 && (kb - k0) % (kRun > 0 ? kRun : 1) == kRun - 1)) {
                             tc_commit_pair_multicast(tfull_bar(acc), kBoth);
                             if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
                         }
@@ -818,16 +826,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ns_threads<BN, kSpli
             const int row0 = mb * kPairBM + 128 * static_cast<int>(rank) + 32 * q;
             const int col0 = nb * BN + half * kWarpCols;
             const bool mirror = sh.tri && nb * BN / kPairBM != mb;
-            if constexpr (kSplit) {
-                float s[kChunks][32];
+            // the sums of the unit's accumulators, a run of stages each, in registers
+            float s[kRun > 0 ? kChunks : 1][32];
+            auto drain = [&] {
 #pragma unroll
                 for (int c = 0; c < kChunks; ++c)
 #pragma unroll
                     for (int j = 0; j < 32; ++j) s[c][j] = 0.f;
                 const int k1 = first_k(u, 1);
-                for (int kb = first_k(u, 0); ok && kb < k1; ++kb) {
-                    ok = ready();
-                    if (!ok) break;
+                for (int kb = first_k(u, 0); kb < k1; kb += kRun) {
+                    if (!ready()) return false;
                     const uint32_t tr = t_row();
 #pragma unroll
                     for (int c = 0; c < kChunks; ++c) {
@@ -838,6 +846,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ns_threads<BN, kSpli
                         for (int j = 0; j < 32; ++j) s[c][j] += v[j];
                     }
                 }
+                return true;
+            };
+            if constexpr (kSplit) {
+                ok = drain();
                 if (!ok) break;
                 if (splits > 1) {
                     constexpr int kWarpSums = kChunks * 32 * 32;
@@ -872,6 +884,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ns_threads<BN, kSpli
                     }
                 }
                 Epi epi(ep, g, row0, col0, lane, mirror);
+#pragma unroll
+                for (int c = 0; c < kChunks; ++c) epi.template chunk<0>(s[c], buf, lane, c);
+                epi.finish(lane);
+            } else if constexpr (kRun > 0) {
+                Epi epi(ep, g, row0, col0, lane, mirror);
+                ok = drain();
+                if (!ok) break;
 #pragma unroll
                 for (int c = 0; c < kChunks; ++c) epi.template chunk<0>(s[c], buf, lane, c);
                 epi.finish(lane);
