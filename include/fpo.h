@@ -489,7 +489,8 @@ size_t fpo_layer_muon_workspace(int32_t n_layers, int64_t d, int64_t d_ff, int32
  * g [T, d], A [T, d_ff] in dtype (not read for T = 0: G_l = 0), W_master and momentum
  * [d, d_ff] fp32, updated in place, W_out [d, d_ff] in dtype (the array or an entry may be
  * NULL); all HOST arrays of n_layers device pointers.  g and A entries may repeat, the others
- * not; nor may one stand in two arrays, but for W_out[l] = W_master[l] in fp32 (FPO_ERR_ARG).
+ * not; nor may one of the others stand in two arrays, but for W_out[l] = W_master[l] in fp32, nor a
+ * momentum be a g or A (FPO_ERR_ARG).
  * No relative clip: the step's norm is lr scale ||O_l||_F, about lr scale sqrt(rank).
  * After a wait that ran out (FPO_ERR_TIMEOUT in the status word) W_master and W_out are as
  * before the call; momentum may have taken the step, as a whole or in parts.

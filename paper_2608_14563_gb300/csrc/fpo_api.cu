@@ -740,13 +740,16 @@ int32_t fpo_layer_muon_grouped(int32_t n_layers, int64_t T, int64_t d, int64_t d
         repeats(n_layers, reinterpret_cast<const void* const*>(momentum)) ||
         repeats(n_layers, W_out))
         return FPO_ERR_ARG;
-    // a momentum is no master and no W_out, and another layer's master no W_out
+    // a momentum is no master, no W_out and no g or A (which are read while it is written), and
+    // another layer's master no W_out
     for (int l = 0; l < n_layers; ++l) {
         const void* w = W_out ? W_out[l] : nullptr;
-        for (int k = 0; k < n_layers; ++k)
+        for (int k = 0; k < n_layers; ++k) {
             if (momentum[l] == W_master[k] ||
                 (w && (w == momentum[k] || (w == W_master[k] && (k != l || dtype == FPO_BF16)))))
                 return FPO_ERR_ARG;
+            if (T > 0 && (g[k] == momentum[l] || A[k] == momentum[l])) return FPO_ERR_ARG;
+        }
     }
     if (!workspace || workspace_bytes < fpo_layer_muon_workspace(n_layers, d, d_ff, dtype))
         return FPO_ERR_WORKSPACE;
