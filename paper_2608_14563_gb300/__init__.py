@@ -206,7 +206,20 @@ def _check(code: int, where: str) -> None:
         raise FpoError(code, where)
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _on_current_device(t: torch.Tensor) -> None:
+    """Kernels run on the current device, where another one's memory may not be mapped."""
+    device = t.get_device()  # -1: not CUDA memory, which _ptr refuses
+    if device >= 0 and device != _current_device():
+        raise ValueError(f"libfpo runs on the current device, cuda:{_current_device()}; "
+                         f"got a tensor of cuda:{device}")
+
+
 def _dtype_code(t: torch.Tensor) -> int:
+    """The type of a call, that of its leading tensor."""
+    _on_current_device(t)
     if t.dtype == torch.bfloat16:
         return BF16
     if t.dtype == torch.float32:
@@ -699,6 +712,7 @@ def h2d_copy(dsts, srcs, *, stream=None):
     for c in range(0, len(srcs), MAX_COPY_BUFFERS):
         ds, ss = dsts[c:c + MAX_COPY_BUFFERS], srcs[c:c + MAX_COPY_BUFFERS]
         n = len(ss)
+        _on_current_device(ds[0])
         darr = (_vp * n)(*[_ptr(t) for t in ds])
         sarr = (_vp * n)(*[t.data_ptr() for t in ss])
         barr = (_sz * n)(*[t.numel() * t.element_size() for t in ss])
