@@ -1083,9 +1083,6 @@ cudaError_t with_form(const RowForm& f, F&& fn) {
         case 512: return fn(Int<kMax512>{}, Int<512>{});
         default: break;
     }
-    if constexpr (kMax >= 16) {
-        if (f.nv == 16) return fn(Int<16>{}, Int<32>{});
-    }
     if constexpr (kMax >= 8) {
         if (f.nv == 8) return fn(Int<8>{}, Int<32>{});
     }

@@ -334,15 +334,16 @@ size_t norm_parts(int rows, int cols, bool muon) {
 struct NsLayout {
     int m, ld, ldm;              // the smaller side, row strides of X and of A, B
     size_t xs, ms;               // elements of one layer's X, A
-    size_t counts, slots;        // split: of the products' ranges (NsShape)
+    size_t counts, slots;        // split: of the ranges of A = X X^T (NsShape)
     size_t part, sum, U, u_stride, hi[2], lo[2], x32, A[2], B[2], total;
     size_t clear;                // bytes from the start to be zero before a call
 };
 
-// Tiles of one matrix of a kSplit product [M, N], and the ranges that their k-blocks are split
-// into: as many as half of the 76 clusters hold of one matrix, of 16 k-blocks or more.  It goes
-// by the matrix's sizes only, so that its result does not depend on the group.  Five steps, with
-// and without: 767 x 2049 one matrix 314 and 349 us, two 380 and 413, eight 977 and 944; eight
+// Tiles of one matrix of a kSplit product [M, N], and the ranges that the k-blocks of A = X X^T (X^T X)
+// are split into: as many as half of the 76 clusters hold of one matrix, of 16 k-blocks or more.
+// (For A^2 and X', whose k is the smaller side, the same rule would never give two: 32 k-blocks are
+// 72 tiles or more.)  It goes by the matrix's sizes only, so that its result does not depend on the
+// group.  Five steps, with and without: 767 x 2049 one matrix 314 and 349 us, two 380 and 413, eight 977 and 944; eight
 // 256 x 4096 388 and 510, eight 512 x 2048 580 and 525; two 64 x 8192 231 and 555.  (Ranges of 8
 // k-blocks: eight 512 x 1024 392 instead of 332.)
 long long ns_matrix_tiles(int M, int N, bool tri) {
@@ -383,21 +384,13 @@ NsLayout ns_layout(int n, int rows, int cols, int dtype, bool muon) {
     };
     L.clear = 2 * sizeof(unsigned);  // the status word and the chain kernel's counter
     if (split) {
-        const long long sym = ns_matrix_tiles(L.m, L.m, true), app = ns_matrix_tiles(rows, cols, false);
-        long long tiles = 0, units = 0;  // of the products that are split
-        // `wide`: tiles of 128 columns that those of 256 cover
-        auto product = [&](long long t, long long wide, int K) {
-            const int s = ns_splits(t, K);
-            if (s == 1) return;
-            if (t > tiles) tiles = t;
-            if (wide * s > units) units = wide * s;
-        };
-        product(sym, sym, rows < cols ? cols : rows);
-        product(sym, sym, L.m);
-        product(app, 2ll * ((rows + 255) / 256) * ((cols + 255) / 256), L.m);
-        L.counts = take(n * tiles * 2 * kNsWarps * sizeof(unsigned));
-        L.clear = at;
-        L.slots = take(n * units * (kPairBM * 128 * sizeof(float)));
+        const long long tiles = ns_matrix_tiles(L.m, L.m, true);
+        const long long ranges = ns_splits(tiles, rows < cols ? cols : rows);
+        if (ranges > 1) {
+            L.counts = take(n * tiles * 2 * kNsWarps * sizeof(unsigned));
+            L.clear = at;
+            L.slots = take(n * tiles * ranges * (kPairBM * 128 * sizeof(float)));
+        }
     }
     const size_t x = n * L.xs * 2, a = n * L.ms * 2;
     L.part = take(static_cast<size_t>(n) * norm_parts(rows, cols, muon) * sizeof(double));
@@ -480,7 +473,7 @@ int resident_clusters(int threads, int smem_bytes, int sm_count) {
     return n;
 }
 
-// Where the ranges of a kSplit product leave their sums.
+// Where the ranges of A = X X^T leave their sums (kSplit; null: no ranges).
 struct NsRanges {
     float* slots;
     unsigned* counts;
@@ -510,7 +503,7 @@ cudaError_t launch_ns(const typename Epi::Maps& maps, const typename Epi::Params
         tri ? static_cast<long long>(sh.g.m_blocks) * (sh.g.m_blocks + 1) / 2 * (kPairBM / BN)
             : static_cast<long long>(sh.g.m_blocks) * sh.g.n_blocks;
     sh.g.tiles = groups * per;
-    sh.splits = kSplit ? ns_splits(ns_matrix_tiles(M, N, tri), K) : 1;
+    sh.splits = Epi::kRanges && rg.slots ? ns_splits(ns_matrix_tiles(M, N, tri), K) : 1;
     sh.slots = rg.slots;
     sh.counts = rg.counts;
     constexpr int kThreads = ns_threads<BN, kSplit, Epi>();
@@ -567,7 +560,7 @@ cudaError_t run_ns(const NsOperand& A, const NsOperand& B, const typename Epi<12
     bool wide = 4 * tiles > di.sm_count;
     if constexpr (kSplit) {
         const long long narrow = ns_matrix_tiles(M, N, tri), clusters = di.sm_count / 2;
-        const int splits = ns_splits(narrow, K), blocks = (K + kBK - 1) / kBK / splits;
+        const int splits = rg.slots ? ns_splits(narrow, K) : 1, blocks = (K + kBK - 1) / kBK / splits;
         auto waves = [&](long long units) { return (units + clusters - 1) / clusters; };
         wide = waves(tiles * splits) * (1030 * blocks + 12000) <
                waves(A.n * narrow * splits) * (850 * blocks + 4000);
@@ -624,6 +617,7 @@ double quad_max(double b, double c, double t1) {
 int scale_exp(double bound) { return 15 - static_cast<int>(ceil(log2(bound))); }
 
 NsRanges ns_ranges(const NsLayout& L, uint8_t* ws) {
+    if (L.slots == 0) return {};
     return {reinterpret_cast<float*>(ws + L.slots), reinterpret_cast<unsigned*>(ws + L.counts)};
 }
 
@@ -633,7 +627,6 @@ cudaError_t run_apply(const NsOperand& X, const NsOperand& B, bool tall, const N
                       int cur, bool next_lo, typename EpiApplyBase<kSplit, kOut>::Params& ep,
                       unsigned* status, cudaStream_t st) {
     const int rows = X.outer, cols = X.inner;
-    const NsRanges rg = ns_ranges(L, ws);
     ep.s.hi = X.p[0];
     ep.s.lo = reinterpret_cast<__half*>(ws + L.lo[cur]);
     ep.s.next_hi = reinterpret_cast<__half*>(ws + L.hi[cur ^ 1]);
@@ -646,10 +639,10 @@ cudaError_t run_apply(const NsOperand& X, const NsOperand& B, bool tall, const N
     // wide: B X with B K-major and X MN-major; tall: X B, both K-major (B is symmetric)
     if (tall)
         return run_ns<false, false, kSplit, ApplyOf<kSplit, kOut>::template T>(X, B, ep, rows, cols,
-                                                                              cols, false, rg, status,
+                                                                              cols, false, {}, status,
                                                                               st);
     return run_ns<false, true, kSplit, ApplyOf<kSplit, kOut>::template T>(B, X, ep, rows, cols, rows,
-                                                                         false, rg, status, st);
+                                                                         false, {}, status, st);
 }
 
 // The coefficients of every product with the powers of two that X, A and B are stored with: X_k
@@ -712,7 +705,7 @@ cudaError_t run_steps(const NsLayout& L, uint8_t* ws, int n, int rows, int cols,
         sp.out[1] = at(L.B[1]);
         sp.lin_coef = co[k].b_lin;
         sp.acc_coef = co[k].b_acc;
-        e = run_ns<false, false, kSplit, SymOf<kSplit>::template T>(A, A, sp, L.m, L.m, L.m, true, rg,
+        e = run_ns<false, false, kSplit, SymOf<kSplit>::template T>(A, A, sp, L.m, L.m, L.m, true, {},
                                                                     status, st);
         if (e != cudaSuccess) return e;
         // X' = a X + B X

@@ -109,10 +109,10 @@ struct NsSmem {
 struct NsShape {
     GemmShape g;   // M, N, K, blocks; tiles of all matrices
     bool tri;      // only tiles that reach under or onto the diagonal (M = N)
-    // kSplit: a tile's k-blocks in `splits` ranges of their own units (unit u: range u % splits of
-    // tile u / splits).  With splits > 1 every warp of a unit leaves its sums in slots[unit][CTA]
-    // [warp], and the last of a tile to arrive at counts[tile][CTA][warp] (zero before and
-    // after) adds them in the ranges' order and goes on to the epilogue: none waits.
+    // EpiSym with kSplit (kRanges): a tile's k-blocks in `splits` ranges of their own units (unit u:
+    // range u % splits of tile u / splits).  With splits > 1 every warp of a unit leaves its sums in
+    // slots[unit][CTA][warp], and the last of a tile to arrive at counts[tile][CTA][warp] (zero
+    // before and after) adds them in the ranges' order and goes on to the epilogue: none waits.
     int splits;
     float* slots;
     unsigned* counts;
@@ -230,6 +230,7 @@ struct EpiSym : EpiSymBase<kSplit> {
     using Maps = NsMaps;
     static constexpr bool kBf16 = false;
     static constexpr int kRun = 0;
+    static constexpr bool kRanges = kSplit;
     using Params = typename EpiSymBase<kSplit>::Params;
     static constexpr int kParts = kSplit ? 2 : 1;
     static constexpr int kChunks = BN / 2 / 32;
@@ -379,6 +380,7 @@ struct EpiApply : EpiApplyBase<kSplit, kOut> {
     using Maps = NsMaps;
     static constexpr bool kBf16 = false;
     static constexpr int kRun = 0;
+    static constexpr bool kRanges = false;
     using Out = typename EpiApplyBase<kSplit, kOut>::Out;
     using Params = typename EpiApplyBase<kSplit, kOut>::Params;
     static constexpr int kChunks = BN / 2 / 32;
@@ -543,6 +545,7 @@ struct EpiMomentum : EpiMomentumBase {
     using Maps = NsGradMaps;
     static constexpr bool kBf16 = true;
     static constexpr int kRun = 4;  // stages of 128 tokens
+    static constexpr bool kRanges = false;
     static constexpr int kChunks = BN / 2 / 32;
     static constexpr int kAcc = 8;
 
@@ -639,7 +642,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ns_threads<BN, kSpli
     const long long cluster = blockIdx.x / 2;
     const long long n_clusters = gridDim.x / 2;
     const int tile_k = (sh.g.k_blocks + kSub - 1) / kSub;  // stages per tile
-    const int splits = kSplit ? sh.splits : 1;
+    const int splits = Epi::kRanges ? sh.splits : 1;
     const long long units = sh.g.tiles * splits;
     // first stage of a unit's range
     auto first_k = [&](long long u, int add) {
@@ -851,7 +854,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ns_threads<BN, kSpli
             if constexpr (kSplit) {
                 ok = drain();
                 if (!ok) break;
-                if (splits > 1) {
+                if (Epi::kRanges && splits > 1) {
                     constexpr int kWarpSums = kChunks * 32 * 32;
                     const int w = static_cast<int>(rank) * kNsWarps + warp - kFirst;
                     float* mine = sh.slots + (u * 2 * kNsWarps + w) * kWarpSums + lane;
