@@ -38,3 +38,22 @@ def test_what_may_be_shared(call):
     assert call(Wo=None) == WORKSPACE
     assert call(T=0, g=(9, 5), A=(7, 6)) == WORKSPACE  # no tokens: not read
     assert call(T=0, g=None, A=None) == WORKSPACE
+
+
+def test_workspace_is_what_the_header_says():
+    """6 rows cols' + 4 m m' (bf16), 12 rows cols' + 8 m m' and at most 5 MB (fp32, and bf16 with a
+    side of at most 64) per matrix, cols' and m' rounded up to 64; beside it 16 KB of small parts and
+    their alignment."""
+    import paper_2608_14563_gb300 as fpo
+    for dtype in (0, 1):
+        for rows, cols in ((65536, 1), (1, 65536), (33, 70), (64, 8), (767, 2049), (4096, 11008), (8, 4096),
+                           (72, 136), (3000, 200), (257, 2300)):
+            if dtype == 1 and (rows % 8 or cols % 8):
+                continue
+            m = min(rows, cols)
+            split = dtype == 0 or m <= 64
+            ld, ldm = -(-cols // 64) * 64, -(-m // 64) * 64
+            parts = (12 if split else 6) * rows * ld + (8 if split else 4) * m * ldm
+            for n in (1, 3):
+                extra = fpo.orthogonalize_workspace(n, rows, cols, dtype) - n * parts
+                assert 0 <= extra <= 16384 + (n * 5 * 10 ** 6 if split else 0), (dtype, rows, cols, n)
