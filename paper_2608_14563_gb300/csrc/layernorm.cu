@@ -18,9 +18,9 @@
 // shared memory instead, with the roles on warps of their own.  Rows of more than 8192 elements
 // are read in several passes, and their weight sums by a kernel of their own.
 //
-// Bound: HBM.  bf16 16384 x 4096: forward 47 us, 5.7 TB/s; backward with both weight gradients
-// 72 us, 5.6 TB/s.  Small calls are bound by the host (a call is 6 to 8 us of it, 2 to 5 on the
-// GPU).
+// Bound: HBM.  bf16 16384 x 4096, call after call: forward 50 us, 5.4 TB/s; backward with both
+// weight gradients 76 us, 5.3 TB/s.  Small calls are bound by the host (a call is 7 to 8 us of it,
+// 2 to 5 on the GPU).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <math.h>
@@ -423,7 +423,7 @@ __global__ void __launch_bounds__(ln_threads<TH>(), ln_min_blocks<TH, true>())
 // of a row each, and CW warps, whose threads keep the same NV vectors of columns throughout,
 // apply them in row order.  A row costs 25 shuffles and no barrier of the block; with a row's
 // sums over 256 threads (layernorm_vjp_kernel) 256 shuffles and two barriers of the block were
-// most of its time.  bf16 16384 x 4096: 67 us, 6.0 TB/s (floor 59), and 5 us for the last sums.
+// most of its time.  bf16 16384 x 4096: 76 us with the last sums (floor 59), 93 there.
 //
 // The statistics take one pass, with the mean s of the row's first 32 vectors as the origin:
 //   var = mean((x - s)^2) - mean(x - s)^2,  mean(u (x - mu)) = mean(u (x - s)) - mean(x - s) mean(u)
@@ -1044,27 +1044,37 @@ int vjp_blocks(int T, const RowForm& f) {
     return want < cap ? want : cap;
 }
 // Short batches: all of it on one cluster, in at most kLnClusterRounds rounds over the blocks'
-// row groups.  bf16 200 x 256, 4 rounds: a call takes 7.7 us, 16.2 on the two kernels with a
-// fresh workspace (4.8 and 3.7 us on the GPU, in a graph); at 8 rounds (512 x 256) 8.4 and
-// 16.5, but 6.8 and 4.1 on the GPU.
+// row groups.  One cluster spares a launch and the workspace, and is slower on the GPU, which counts
+// in a graph: the limit keeps that to a microsecond.  bf16 256 x 256, 4 rounds, cluster and two
+// kernels: 8.2 and 15.2 us a call, 7.5 and 9.4 with a workspace of the caller's, 4.3 and 3.7 in a graph;
+// 512 x 256, 8 rounds: 8.4 and 15.5, 8.3 and 9.6, but 6.5 and 4.5.
 constexpr int kLnClusterRounds = 4;
 bool one_cluster(int T, const RowForm& f) {
     return f.nv != 0 && f.th != 512 && T <= kLnClusterRounds * kLnCluster * (256 / f.th);
 }
 // Many long rows of 16-byte vectors: the stream kernels, a block to an SM.  Backward (us, stream
-// kernel and register kernel): bf16 16384 x 4096 72 and 90, 16384 x 2560 66 and 84, 8192 x 8192
-// 87 and 95, 300 x 4096 11 and 18; fp32 8192 x 4096 67 and 175, 16384 x 2048 71 and 73; rows of 4 KB
-// come out even (bf16 16384 x 2048 50 and 48), shorter ones worse (32768 x 1024 81 and 46).
+// kernel and register kernel): bf16 16384 x 4096 76 and 93, 16384 x 2560 70 and 87, 8192 x 8192
+// 90 and 98, 300 x 4096 13 and 21; fp32 8192 x 4096 71 and 178, 16384 x 2048 74 and 76; rows of 4 KB
+// come out worse (bf16 16384 x 2048 68 and 51, fp32 16384 x 1024 48 and 43), as do shorter ones
+// (bf16 32768 x 1024 117 and 49).
 bool streamed(int T, int d, int vec, int esz) {
     return vec > 1 && T >= 256 && d * esz > 4096 && d <= 8192;
 }
 // Forward: where a row leaves threads of the register kernel without elements.  bf16 8192 x 5120
-// 33 and 50 us, 16384 x 2560 34 and 40, fp32 8192 x 4096 47 and 59; full ones: bf16 16384 x
-// 4096 48 and 47, fp32 4096 x 8192 60 and 46, and 1024 x 4096 6.5 and 4.3.
+// 35 and 52 us, 16384 x 2560 37 and 43, fp32 8192 x 4096 50 and 62; full ones: bf16 16384 x
+// 4096 52 and 50, fp32 4096 x 8192 60 and 48; short batches: bf16 1024 x 4096 10 and 8.
 bool fwd_streamed(int T, int d, int vec, int esz, const RowForm& f) {
     return T >= 4096 && d * esz > 4096 && d < f.nv * f.th * vec;
 }
 int stream_blocks(int T) { return T < 152 ? T : 152; }
+
+// The form of a backward pass, and so what it needs of the workspace: one rule for both.
+enum LnForm { kLongForm, kClusterForm, kStreamForm, kBlockForm };
+LnForm vjp_form(int T, int d, int vec, int esz, const RowForm& f) {
+    if (f.nv == 0) return kLongForm;
+    if (one_cluster(T, f)) return kClusterForm;  // (without weight sums: blocks)
+    return streamed(T, d, vec, esz) ? kStreamForm : kBlockForm;
+}
 constexpr int kLongRanges = 64;
 int long_ranges(int T) { return T < kLongRanges ? T : kLongRanges; }
 
@@ -1145,9 +1155,10 @@ cudaError_t run_vjp(const void* g, const void* x, const void* gamma, int T, int 
     auto* oo = static_cast<TT*>(out);
     const bool sums = dgamma || dbeta;
     const RowForm f = row_form<TT, VEC>(d);
+    const LnForm form = vjp_form(T, d, VEC, sizeof(TT), f);
     int parts = 0;
     cudaError_t e;
-    if (f.nv == 0) {
+    if (form == kLongForm) {
         float2* stats = sums ? reinterpret_cast<float2*>(ws) : nullptr;
         const int grid = T < 4 * sms() ? T : 4 * sms();
         layernorm_vjp_long_kernel<TT, VEC>
@@ -1160,7 +1171,7 @@ cudaError_t run_vjp(const void* g, const void* x, const void* gamma, int T, int 
         e = launch_chained(layernorm_cols_kernel<TT>,
                            dim3((d + kColThreads - 1) / kColThreads, parts), kColThreads, 0, st, gg,
                            xx, static_cast<const float2*>(stats), T, d, ws);
-    } else if (streamed(T, d, VEC, sizeof(TT))) {
+    } else if (form == kStreamForm) {
         if constexpr (VEC > 1) {
             parts = stream_blocks(T);
             auto launch = [&](auto nv, auto cw, auto sw, auto mode) {
@@ -1177,20 +1188,20 @@ cudaError_t run_vjp(const void* g, const void* x, const void* gamma, int T, int 
                     note_launch();
                 return cudaGetLastError();
             };
-            auto form = [&](auto nv, auto cw, auto sw) {
+            auto run = [&](auto nv, auto cw, auto sw) {
                 return sums ? launch(nv, cw, sw, Int<1>{}) : launch(nv, cw, sw, Int<0>{});
             };
             const int n = d / VEC;
             if constexpr (VEC == 4)
-                e = n <= 512    ? form(Int<2>{}, Int<8>{}, Int<8>{})
-                    : n <= 1024 ? form(Int<4>{}, Int<8>{}, Int<8>{})
-                                : form(Int<4>{}, Int<16>{}, Int<3>{});
+                e = n <= 512    ? run(Int<2>{}, Int<8>{}, Int<8>{})
+                    : n <= 1024 ? run(Int<4>{}, Int<8>{}, Int<8>{})
+                                : run(Int<4>{}, Int<16>{}, Int<3>{});
             else
-                e = n <= 512 ? form(Int<2>{}, Int<8>{}, Int<8>{}) : form(Int<2>{}, Int<16>{}, Int<7>{});
+                e = n <= 512 ? run(Int<2>{}, Int<8>{}, Int<8>{}) : run(Int<2>{}, Int<16>{}, Int<7>{});
         } else {
             e = cudaErrorInvalidValue;  // (streamed)
         }
-    } else if (sums && one_cluster(T, f)) {
+    } else if (form == kClusterForm && sums) {
         return with_form<TT, VEC>(f, [&](auto nv, auto th) {
             constexpr int NV = decltype(nv)::value, TH = decltype(th)::value;
             if constexpr (TH != 512) {
@@ -1236,16 +1247,17 @@ cudaError_t run_vjp(const void* g, const void* x, const void* gamma, int T, int 
 }  // namespace
 
 size_t layernorm_vjp_floats(int dtype, int T, int d) {
-    const RowForm f = dtype == 1   ? row_form<__nv_bfloat16, 8>(d)
-                      : d % 4 == 0 ? row_form<float, 4>(d)
-                                   : row_form<float, 1>(d);
-    if (one_cluster(T, f)) return 0;
-    const size_t stats = f.nv == 0 ? 2 * static_cast<size_t>(T) : 0;
-    const size_t parts = f.nv == 0 ? long_ranges(T)
-                         : streamed(T, d, dtype == 1 ? 8 : d % 4 == 0 ? 4 : 1, dtype == 1 ? 2 : 4)
-                             ? stream_blocks(T)
-                             : vjp_blocks(T, f);
-    return stats + parts * 2 * static_cast<size_t>(d);
+    const int vec = dtype == 1 ? 8 : d % 4 == 0 ? 4 : 1;
+    const RowForm f = vec == 8   ? row_form<__nv_bfloat16, 8>(d)
+                      : vec == 4 ? row_form<float, 4>(d)
+                                 : row_form<float, 1>(d);
+    const size_t sums = 2 * static_cast<size_t>(d);
+    switch (vjp_form(T, d, vec, dtype == 1 ? 2 : 4, f)) {
+        case kLongForm: return 2 * static_cast<size_t>(T) + long_ranges(T) * sums;
+        case kClusterForm: return 0;
+        case kStreamForm: return stream_blocks(T) * sums;
+        default: return vjp_blocks(T, f) * sums;
+    }
 }
 
 cudaError_t launch_layernorm_fwd(int dtype, const void* x, const void* gamma, const void* beta,
