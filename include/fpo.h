@@ -447,8 +447,8 @@ size_t fpo_orthogonalize_workspace(int32_t n_layers, int64_t rows, int64_t cols,
  * bf16: products of fp16 operands scaled by powers of two from the bounds (11 bits instead of
  * bf16's 8), fp32 accumulation, the linear term a X from 22 bits of X in every step but the last
  * (there from the operand: nothing grows after it, and the same X in both terms is the smaller
- * error), whatever its rank: 1.9e-3 to 2.5e-3 off in norm, the rounding to bf16 (1.7e-3) among it;
- * Muon's O, in fp32, 0.7e-3 to 1.9e-3.  rows and cols multiples of 8; matrices with a side of at
+ * error), whatever its rank: 1.9e-3 to 2.6e-3 off in norm, the rounding to bf16 (1.7e-3) among it;
+ * Muon's O, in fp32, 0.7e-3 to 2.0e-3.  rows and cols multiples of 8; matrices with a side of at
  * most 64 as in fp32 calls.
  * fp32: operands as sums of two fp16 numbers (22 bits), three products, fp32 sums rounded to
  * nearest every 64 products, the linear term in fp32; any sizes.

@@ -13,7 +13,7 @@
 // scaled by powers of two: the host bounds every X_k, A and B from the polynomials' maxima on
 // the interval that the singular values can reach, so nothing overflows, and fp16's small end
 // lies 2^-39 below the bound.  bf16 calls keep X's low part for the linear term (EpiApply);
-// against fp64 their result is then off by 0.7e-3 to 1.9e-3 in norm before its own rounding
+// against fp64 their result is then off by 0.7e-3 to 2.0e-3 in norm before its own rounding
 // (1.7e-3), whatever the rank.  fp32 calls, and bf16 ones of few rows or columns (ns_split), take
 // every operand as the sum of two fp16 matrices (22 bits) and three products: 1e-6 to 2e-6.
 //
@@ -22,7 +22,7 @@
 // alone): norm 29, cast 46, A 118, B 51, X' 242 (last 218): the products at 70 to 84% of the tensor
 // rate in whole waves of tiles on 76 clusters, 136 tiles of A taking two and the 688 of X' ten.
 // Muon: the gradient's GEMM with the momentum and the squares in its epilogue, and a last pass
-// over the masters at the copy rate (4096 x 11008 twice: 476 and 186 us).
+// over the masters at the copy rate (4096 x 11008 twice, 4096 tokens: 536 and 189 us).
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -358,7 +358,7 @@ int ns_splits(long long tiles, int K) {
 
 // kSplit: fp32 calls, and bf16 ones of few rows or columns: there the rounding errors of single
 // entries of A and B average out least.  In norm the bf16 result of fp16 products is off by 2.3e-3 to
-// 3.9e-3 for sides of 8 to 64, 2.1e-3 to 2.4e-3 for longer ones (its own rounding, and all of
+// 3.9e-3 for sides of 8 to 64, 2.0e-3 to 2.6e-3 for longer ones (its own rounding, and all of
 // it with kSplit: 1.7e-3).  Two 64 x 256 matrices take 121 us instead of 83, sixteen 64 x 4096
 // 399 instead of 280, one 16 x 8192 200 instead of 239.
 bool ns_split(int dtype, int rows, int cols) {
