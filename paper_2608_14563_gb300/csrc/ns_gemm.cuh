@@ -629,6 +629,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ns_threads<BN, kSpli
     constexpr int kStages = L::kStages;
     constexpr int kSub = kSplit ? 1 : 2;   // k-blocks (and full barriers) per stage
     constexpr int kRun = ns_run<kSplit, Epi>();
+    constexpr bool kDrained = kRun > 0;
     constexpr uint32_t kIdesc = Epi::kBf16 ? idesc_bf16_f32(kPairBM, BN, A_MN, B_MN)
                                            : idesc_f16_f32(kPairBM, BN, A_MN, B_MN);
     constexpr uint16_t kBoth = 0x3;
@@ -741,7 +742,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ns_threads<BN, kSpli
                 for (long long u = cluster; ok && u < units; u += n_clusters) {
                     const int k0 = first_k(u, 0), k1 = first_k(u, 1);
                     for (int kb = k0; kb < k1; ++kb) {
-                        const bool first = kRun > 0 ? (kb - k0) % (kRun > 0 ? kRun : 1) == 0 : kb == k0;
+                        bool first = kb == k0, last = kb == k1 - 1;  // of an accumulator
+                        if constexpr (kDrained) {
+                            first = (kb - k0) % kRun == 0;
+                            last = last || (kb - k0) % kRun == kRun - 1;
+                        }
                         if (first) {
                             if (!mbar_wait_cl(tempty_bar(acc), acc_phase ^ 1u, guard)) {
                                 ok = false;
@@ -781,7 +786,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ns_threads<BN, kSpli
                         issued_any = true;
                         tc_commit_pair_multicast(empty_bar(stage), kBoth);
                         if (++stage == kStages) { stage = 0; phase ^= 1u; }
-                        if (kb == k1 - 1 || (kRun > 0 && (kb - k0) % (kRun > 0 ? kRun : 1) == kRun - 1)) {
+                        if (last) {
                             tc_commit_pair_multicast(tfull_bar(acc), kBoth);
                             if (++acc == kAccs) { acc = 0; acc_phase ^= 1u; }
                         }
@@ -831,74 +836,79 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(ns_threads<BN, kSpli
             const int row0 = mb * kPairBM + 128 * static_cast<int>(rank) + 32 * q;
             const int col0 = nb * BN + half * kWarpCols;
             const bool mirror = sh.tri && nb * BN / kPairBM != mb;
-            // the sums of the unit's accumulators, a run of stages each, in registers
-            float s[kRun > 0 ? kChunks : 1][32];
-            auto drain = [&] {
-#pragma unroll
-                for (int c = 0; c < kChunks; ++c)
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) s[c][j] = 0.f;
-                const int k1 = first_k(u, 1);
-                for (int kb = first_k(u, 0); kb < k1; kb += kRun) {
-                    if (!ready()) return false;
-                    const uint32_t tr = t_row();
-#pragma unroll
-                    for (int c = 0; c < kChunks; ++c) {
-                        float v[32];
-                        tmem_ld_32x32b_x32(tr + 32 * c, v);
-                        if (c == kChunks - 1) release();  // it is all in registers
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) s[c][j] += v[j];
-                    }
-                }
-                return true;
-            };
-            if constexpr (kSplit) {
-                ok = drain();
-                if (!ok) break;
-                if (Epi::kRanges && splits > 1) {
-                    constexpr int kWarpSums = kChunks * 32 * 32;
-                    const int w = static_cast<int>(rank) * kNsWarps + warp - kFirst;
-                    float* mine = sh.slots + (u * 2 * kNsWarps + w) * kWarpSums + lane;
-#pragma unroll
-                    for (int c = 0; c < kChunks; ++c)
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) mine[(c * 32 + j) * 32] = s[c][j];
-                    __threadfence();
-                    __syncwarp();
-                    unsigned* count = sh.counts + t * 2 * kNsWarps + w;
-                    unsigned before = 0;
-                    if (lane == 0) before = atomicAdd(count, 1u);
-                    before = __shfl_sync(0xffffffffu, before, 0);
-                    if (before + 1 != static_cast<unsigned>(splits)) continue;
-                    __threadfence();
-                    if (lane == 0) *count = 0;
+            if constexpr (kDrained) {
+                // the sums of the unit's accumulators, a run of stages each, in registers
+                float s[kChunks][32];
+                auto drain = [&] {
 #pragma unroll
                     for (int c = 0; c < kChunks; ++c)
 #pragma unroll
                         for (int j = 0; j < 32; ++j) s[c][j] = 0.f;
-                    const float* from =
-                        sh.slots + (t * splits * 2 * kNsWarps + w) * kWarpSums + lane;
-                    for (int r = 0; r < splits; ++r) {
+                    const int k1 = first_k(u, 1);
+                    for (int kb = first_k(u, 0); kb < k1; kb += kRun) {
+                        if (!ready()) return false;
+                        const uint32_t tr = t_row();
 #pragma unroll
-                        for (int c = 0; c < kChunks; ++c)
+                        for (int c = 0; c < kChunks; ++c) {
+                            float v[32];
+                            tmem_ld_32x32b_x32(tr + 32 * c, v);
+                            if (c == kChunks - 1) release();  // it is all in registers
 #pragma unroll
-                            for (int j = 0; j < 32; ++j)
-                                s[c][j] += __ldcg(from + (c * 32 + j) * 32);
-                        from += 2 * kNsWarps * kWarpSums;
+                            for (int j = 0; j < 32; ++j) s[c][j] += v[j];
+                        }
                     }
+                    return true;
+                };
+                auto finish = [&](Epi& epi) {
+#pragma unroll
+                    for (int c = 0; c < kChunks; ++c) epi.template chunk<0>(s[c], buf, lane, c);
+                    epi.finish(lane);
+                };
+                if constexpr (!kSplit) {
+                    Epi epi(ep, g, row0, col0, lane, mirror);  // (its first loads arrive meanwhile)
+                    ok = drain();
+                    if (!ok) break;
+                    finish(epi);
+                } else {
+                    ok = drain();
+                    if (!ok) break;
+                    if constexpr (Epi::kRanges) {
+                        if (splits > 1) {
+                            constexpr int kWarpSums = kChunks * 32 * 32;
+                            const int w = static_cast<int>(rank) * kNsWarps + warp - kFirst;
+                            float* mine = sh.slots + (u * 2 * kNsWarps + w) * kWarpSums + lane;
+#pragma unroll
+                            for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+                                for (int j = 0; j < 32; ++j) mine[(c * 32 + j) * 32] = s[c][j];
+                            __threadfence();
+                            __syncwarp();
+                            unsigned* count = sh.counts + t * 2 * kNsWarps + w;
+                            unsigned before = 0;
+                            if (lane == 0) before = atomicAdd(count, 1u);
+                            before = __shfl_sync(0xffffffffu, before, 0);
+                            if (before + 1 != static_cast<unsigned>(splits)) continue;
+                            __threadfence();
+                            if (lane == 0) *count = 0;
+#pragma unroll
+                            for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+                                for (int j = 0; j < 32; ++j) s[c][j] = 0.f;
+                            const float* from =
+                                sh.slots + (t * splits * 2 * kNsWarps + w) * kWarpSums + lane;
+                            for (int r = 0; r < splits; ++r) {
+#pragma unroll
+                                for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+                                    for (int j = 0; j < 32; ++j)
+                                        s[c][j] += __ldcg(from + (c * 32 + j) * 32);
+                                from += 2 * kNsWarps * kWarpSums;
+                            }
+                        }
+                    }
+                    Epi epi(ep, g, row0, col0, lane, mirror);
+                    finish(epi);
                 }
-                Epi epi(ep, g, row0, col0, lane, mirror);
-#pragma unroll
-                for (int c = 0; c < kChunks; ++c) epi.template chunk<0>(s[c], buf, lane, c);
-                epi.finish(lane);
-            } else if constexpr (kRun > 0) {
-                Epi epi(ep, g, row0, col0, lane, mirror);
-                ok = drain();
-                if (!ok) break;
-#pragma unroll
-                for (int c = 0; c < kChunks; ++c) epi.template chunk<0>(s[c], buf, lane, c);
-                epi.finish(lane);
             } else {
                 Epi epi(ep, g, row0, col0, lane, mirror);
                 ok = ready();
