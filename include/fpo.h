@@ -351,9 +351,9 @@ size_t fpo_layernorm_vjp_workspace(int64_t T, int64_t d, int32_t dtype);
  * g, x, g_out [T, d] and gamma [d] in dtype; gamma NULL: ones.  dgamma, dbeta [d] fp32.
  * Each output may be NULL (not all three).  g_out may not overlap g or x, nor dgamma dbeta
  * (FPO_ERR_ARG where they are the same).  The weight sums are added in a fixed order that
- * depends on T and d only (repeat calls give identical bits).  workspace: fpo_layernorm_vjp_workspace() bytes,
- * 256-byte aligned; may be NULL where that is 0 and when dgamma and dbeta are both NULL; it
- * holds no status word.
+ * depends on T and d only (repeat calls give identical bits).  workspace:
+ * fpo_layernorm_vjp_workspace() bytes, 256-byte aligned; may be NULL where that is 0 and when
+ * dgamma and dbeta are both NULL; it holds no status word.
  * T = 0 sets dgamma and dbeta to zero.  Types, sizes and alignment as fpo_layernorm.
  * A wait that runs out (fpo_set_wait_limit_ns; here and in fpo_layernorm) leaves NaN in the
  * rows or parts of rows that were not reached, and in dgamma and dbeta.

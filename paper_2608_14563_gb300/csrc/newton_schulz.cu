@@ -339,13 +339,13 @@ struct NsLayout {
     size_t clear;                // bytes from the start to be zero before a call
 };
 
-// Tiles of one matrix of a kSplit product [M, N], and the ranges that the k-blocks of A = X X^T (X^T X)
-// are split into: as many as half of the 76 clusters hold of one matrix, of 16 k-blocks or more.
-// (For A^2 and X', whose k is the smaller side, the same rule would never give two: 32 k-blocks are
-// 72 tiles or more.)  It goes by the matrix's sizes only, so that its result does not depend on the
-// group.  Five steps, with and without: 767 x 2049 one matrix 314 and 349 us, two 380 and 413, eight 977 and 944; eight
-// 256 x 4096 388 and 510, eight 512 x 2048 580 and 525; two 64 x 8192 231 and 555.  (Ranges of 8
-// k-blocks: eight 512 x 1024 392 instead of 332.)
+// Tiles of one matrix of a kSplit product [M, N], and the ranges that the k-blocks of A = X X^T
+// (X^T X) are split into: as many as half of the 76 clusters hold of one matrix, of 16 k-blocks or
+// more.  (For A^2 and X', whose k is the smaller side, the same rule would never give two: 32 k-blocks
+// are 72 tiles or more.)  It goes by the matrix's sizes only, so that its result does not depend on
+// the group.  Five steps, with and without: 767 x 2049 one matrix 314 and 349 us, two 380 and 413,
+// eight 977 and 944; eight 256 x 4096 388 and 510, eight 512 x 2048 580 and 525; two 64 x 8192 231
+// and 555.  (Ranges of 8 k-blocks: eight 512 x 1024 392 instead of 332.)
 long long ns_matrix_tiles(int M, int N, bool tri) {
     const long long mb = (M + 255) / 256;
     return tri ? mb * (mb + 1) : mb * ((N + 127) / 128);
