@@ -215,6 +215,7 @@ void set_gemm_variant(int v);
 int gemm_variant();
 // Override of the L2 rasterisation band height in tiles (0 = default).
 void set_band_override(int b);
+int band_override();
 
 // Plain GEMM with an fp32 store epilogue (test entry point).
 cudaError_t launch_test_gemm_bf16(int M, int N, int K, bool a_mn, bool b_mn, const void* A,
