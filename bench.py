@@ -771,7 +771,7 @@ AUTO_T_CHUNK = 8192
 
 # Files that define each kernel whose DRAM traffic profiles/traffic.json records.
 GEMM_SOURCES = ("tc_gemm.cuh", "tc_gemm_pair.cuh", "epilogues.cuh", "error_math.cuh", "ptx.cuh",
-                "gemm_bf16.cu")
+                "gemm_launch.cuh", "gemm_bf16.cu")
 KERNEL_SOURCES = {
     "logits_lse_pass": GEMM_SOURCES,
     "projection": GEMM_SOURCES,
