@@ -16,7 +16,9 @@
  * post-FFN and pre-MLP RMSNorm VJPs and per-layer signals (fpo_rmsnorm_vjp,
  * fpo_layer_signals, fpo_layer_update_grouped_signals), optimizers with the relative clip
  * (fpo_layer_optimize_grouped, fpo_layer_muon_grouped; fpo_orthogonalize_grouped), LayerNorm
- * and its VJP (fpo_layernorm, fpo_layernorm_vjp), the gate/up signals through the cached
+ * and its VJP (fpo_layernorm, fpo_layernorm_vjp), linear layers with their bias, activation and
+ * residual and their VJP (fpo_linear, fpo_linear_vjp), AdamW over every tensor of a model, its
+ * moments in fp32 or in 8 bits (fpo_adamw_grouped), the gate/up signals through the cached
  * W3_init (fpo_gate_up_signals) and the App. C update-magnitude ratio
  * (fpo_norm_ratio).  fpo_h2d_copy stages a step's inputs from host memory.
  *
@@ -413,6 +415,162 @@ int32_t fpo_layer_optimize_grouped(int32_t n_layers, int64_t T, int64_t d, int64
                                    void* const* W_out, float* const* state1,
                                    float* const* state2, void* workspace, size_t workspace_bytes,
                                    void* stream);
+
+/* Activations of a linear layer, with their derivatives:
+ *   RELU       max(z, 0)                          1 for z > 0, else 0
+ *   GELU       z Phi(z)                           Phi(z) + z phi(z)
+ *   GELU_TANH  z (1 + tanh u(z)) / 2              of that expression, u = sqrt(2 / pi) (z + 0.044715 z^3)
+ *   SILU       z sigma(z)                         sigma(z) (1 + z (1 - sigma(z)))                       */
+typedef enum fpo_activation {
+    FPO_ACT_NONE = 0,
+    FPO_ACT_RELU = 1,
+    FPO_ACT_GELU = 2,
+    FPO_ACT_GELU_TANH = 3,
+    FPO_ACT_SILU = 4
+} fpo_activation;
+
+/* Bytes of workspace fpo_linear needs on the current device (0 on invalid sizes): 256, for at
+ * most 128 tokens in bf16 up to 152 kB more per padded token (16, 32, 64 or 128), for larger bf16
+ * batches whose tiles leave a wave partly empty up to 60 MB for the parts of split tiles. */
+size_t fpo_linear_workspace(int64_t T, int64_t d_out, int64_t d_in, int32_t dtype);
+
+/*
+ * fpo_linear -- a linear layer with its bias, activation and residual in the product's epilogue,
+ * for the model families whose MLP is act(h W1^T + b1) W2^T + b2 + x (those with LayerNorm): the
+ * up-projection leaves the cached down-projection inputs A_l of fpo_layer_update_grouped.
+ *
+ *   Z = X W^T + bias,  Y = act(Z) + residual
+ *
+ * X        [T, d_in], W [d_out, d_in] (the nn.Linear layout), dtype
+ * bias     [d_out] dtype, or NULL
+ * residual [T, d_out] dtype, or NULL; may be Y itself
+ * Y        [T, d_out] dtype
+ * Z_out    [T, d_out] dtype, or NULL: the pre-activation, which fpo_linear_vjp reads
+ * act      fpo_activation
+ * workspace fpo_linear_workspace() bytes, 256-byte aligned (device status word first)
+ * No output may overlap an input or another output (but for Y = residual), nor the workspace
+ * anything (FPO_ERR_ARG).  fp32 accumulation; bias, activation and residual on the fp32 sums,
+ * one rounding each for Z and Y.  Deterministic.  T = 0 writes nothing.
+ * NaN and infinities follow the formulas (RELU keeps a NaN).  After a wait that ran out
+ * (FPO_ERR_TIMEOUT) Y and Z_out hold no result.
+ */
+int32_t fpo_linear(int64_t T, int64_t d_out, int64_t d_in, int32_t dtype, int32_t act,
+                   const void* X, const void* W, const void* bias, const void* residual, void* Y,
+                   void* Z_out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace fpo_linear_vjp needs on the current device (0 on invalid arguments): that of
+ * the two products, at most 512 d_out to 4864 d_out for the bias gradient's parts, and with an
+ * activation T d_out elements. */
+size_t fpo_linear_vjp_workspace(int64_t T, int64_t d_out, int64_t d_in, int32_t dtype, int32_t act);
+
+/*
+ * fpo_linear_vjp -- the backward pass of fpo_linear, optionally through the activation in front of
+ * it, X = act_in(Z_in):
+ *
+ *   dZ    = dY (.) act'(Z)
+ *   dX    = (dZ W) (.) act_in'(Z_in)       the signal at X, or with act_in at Z_in
+ *   dW    = dZ^T X,  dbias = sum_t dZ_t
+ *
+ * (the residual's gradient is dY).  A chain of layers runs from the top: the down-projection with
+ * act_in and the kept Z_out of the up-projection, then the up-projection with its dX as dY.
+ *
+ * dY, Z [T, d_out], X, Z_in [T, d_in], W [d_out, d_in] in dtype; Z is read for act, Z_in for act_in
+ * (and dX), X for dW, W for dX, and may be NULL otherwise
+ * dX [T, d_in], dW [d_out, d_in] in dtype, dbias [d_out] fp32: each may be NULL, not all three
+ * workspace  fpo_linear_vjp_workspace() bytes, 256-byte aligned (device status word first)
+ * Outputs may not overlap what is read, one another or the workspace (FPO_ERR_ARG).  fp32
+ * accumulation; dbias adds dZ before its rounding to dtype, in a fixed order; the products take it
+ * rounded.  Deterministic.  T = 0 sets dW and dbias to zero.  After a wait that ran out
+ * (FPO_ERR_TIMEOUT) dX and dW hold no result.
+ */
+int32_t fpo_linear_vjp(int64_t T, int64_t d_out, int64_t d_in, int32_t dtype, int32_t act,
+                       const void* dY, const void* Z, const void* X, const void* W, int32_t act_in,
+                       const void* Z_in, void* dX, void* dW, float* dbias, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
+/* Consecutive elements of a tensor that share the scales of their 8-bit moments. */
+#define FPO_ADAMW_BLOCK 256
+/* Largest tensor of fpo_adamw_grouped (its tensors together have at most 2^31 chunks of 2048). */
+#define FPO_MAX_ADAMW_ELEMENTS ((int64_t)1 << 40)
+
+/* One tensor of fpo_adamw_grouped: n elements, dense; every pointer but the scales' 16-byte
+ * aligned. */
+typedef struct fpo_adamw_tensor {
+    int64_t n;            /* elements, >= 0 (0: the tensor is skipped)                     */
+    const void* G;        /* gradient in g_dtype                                           */
+    float* W_master;      /* fp32, updated in place                                        */
+    void* W_out;          /* W_master rounded to w_dtype, or NULL                          */
+    void* state1;         /* first moment: fp32, or with state_bits 8 one byte per element */
+    void* state2;         /* second moment, the same                                       */
+    float* scale1;        /* state_bits 8: ceil(n / FPO_ADAMW_BLOCK) scales of state1      */
+    float* scale2;        /* and of state2                                                 */
+    int32_t g_dtype;      /* fpo_dtype of G                                                */
+    int32_t w_dtype;      /* fpo_dtype of W_out                                            */
+    int32_t state_bits;   /* 32 or 8                                                       */
+    float weight_decay;   /* of this tensor (0 for biases and norm weights, usually)       */
+} fpo_adamw_tensor;
+
+/* Rates of fpo_adamw_grouped, in double: 1 - beta2 and the bias corrections keep their digits (in
+ * float, 1 - 0.999 is 1.3e-5 off). */
+typedef struct fpo_adamw_desc {
+    double lr;
+    double beta1, beta2;   /* moment decays in [0, 1) (0.9, 0.999)              */
+    double eps;            /* 1e-8                                              */
+    double clip_frac;      /* relative clip bound (0.01)                        */
+    int64_t step;          /* step index t >= 1, for the bias corrections       */
+    int32_t clip;          /* fpo_clip_mode, of each tensor by itself           */
+} fpo_adamw_desc;
+
+/* Bytes of workspace fpo_adamw_grouped needs for tensors of n[k] elements: 0 without a clip (and
+ * on invalid sizes). */
+size_t fpo_adamw_workspace(int32_t n_tensors, const int64_t* n, int32_t clip);
+
+/*
+ * fpo_adamw_grouped -- the AdamW step of fpo_layer_optimize_grouped (Sec. 3.1) on many tensors of
+ * any sizes with given gradients: a model's matrices, biases and norm weights together, one launch
+ * per 128 tensors (three with a clip).
+ *   m <- beta1 m + (1 - beta1) G,  v <- beta2 v + (1 - beta2) G G
+ *   step = -lr (m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps) + weight_decay W)
+ *   W_master += s step,  W_out = W_master rounded
+ * in fp32 with the rates rounded to fp32; the moments' products and sums are rounded one by one, as
+ * written from left to right, so that the codes of 8-bit moments are those of any fp32 arithmetic.
+ * The clip is that of App. A per tensor: s = min(1, clip_frac ||W|| / ||step||), or G scaled so
+ * before the moments see it.
+ *
+ * tensors  HOST array; W_master, W_out, the states and the scales may not overlap one another, a G
+ *          or the workspace (FPO_ERR_ARG), but for an fp32 W_out that is W_master; G may repeat
+ * workspace  with a clip fpo_adamw_workspace() bytes, 256-byte aligned; it holds no status word
+ * step, rates and seed are read at the call: a captured call replays with them.
+ *
+ * 8-bit moments.  Each FPO_ADAMW_BLOCK consecutive elements have one power of two as scale, which
+ * brings their largest magnitude x to x / scale in [2^7, 2^8) (m), [2^14, 2^15) (v); it is at least
+ * 2^-107 (2^-114).  The value of a code is scale times
+ *   m   sign (the top bit), 4 exponent bits e, 3 mantissa bits f: (1 + f / 8) 2^(e - 7), f / 8 2^-6
+ *       for e = 0 (the e4m3 format)
+ *   v   5 exponent bits e, 3 mantissa bits f: (1 + f / 8) 2^(e - 16), f / 8 2^-15 for e = 0
+ * All bytes 0 is a valid start (m = v = 0).  The step is taken from the fp32 moments; they are then
+ * rounded to one of the two codes beside them, to the upper in magnitude where the fraction of the
+ * distance and a 16-bit random fraction add up to 1 or more: the expected value is kept (rounded to
+ * nearest, v could not follow changes of 0.1% a step).  v > 0 never becomes 0.  The random bits
+ * are a hash of seed, opt->step, the tensor's index, the block and the element, all modulo 2^32:
+ *   mix(h): h ^= h >> 16; h *= 0x6A09E667; h ^= h >> 13; h *= 0xBB67AE85; h ^= h >> 16
+ *   key = mix(mix(mix(mix(lo(seed) + 0x9E3779B9) ^ hi(seed)) ^ step) + tensor), per block mix(key ^ block)
+ *   h = that + element * 0x9E3779B9; h ^= h >> 15; h *= 0x6A09E667; h ^= h >> 16
+ * (the upper half for m, the lower for v): the same call gives the same bits.  A block with a NaN
+ * or an infinity in a new moment gets a NaN scale there; of its weights only those elements are
+ * affected in that step.
+ */
+int32_t fpo_adamw_grouped(int32_t n_tensors, const fpo_adamw_tensor* tensors,
+                          const fpo_adamw_desc* opt, uint64_t seed, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
+/*
+ * fpo_adamw_state_values -- n 8-bit moments as numbers (checkpoints, inspection): out[i] in
+ * out_dtype, exact in both.  moment: 1 (state1) or 2 (state2); scales: ceil(n / FPO_ADAMW_BLOCK).
+ * codes and out 16-byte aligned.  No workspace; asynchronous on `stream`.
+ */
+int32_t fpo_adamw_state_values(int64_t n, int32_t moment, const void* codes, const float* scales,
+                               int32_t out_dtype, void* out, void* stream);
 
 /* Largest side of a matrix that fpo_orthogonalize_grouped and fpo_layer_muon_grouped take. */
 #define FPO_MAX_NS_SIDE 65536

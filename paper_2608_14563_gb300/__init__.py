@@ -11,6 +11,7 @@ paper_2608_14563_gb300.build`` or ``__graft_entry__.build()``).
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import torch
@@ -22,6 +23,7 @@ F32, BF16 = 0, 1
 OK = 0
 MAX_GROUPED_LAYERS = 64
 STAGE_EVENTS = 7
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = 0, 1, 2, 3, 4
 ES_AUTO, ES_RECOMPUTE, ES_STORED_LOGITS, ES_DIRECT = 0, 1, 2, 3
 AUTO_T_CHUNK = 8192  # FPO_AUTO_T_CHUNK: tokens per error-matrix chunk when t_chunk is 0
 
@@ -37,6 +39,7 @@ if _lib.fpo_abi_version() != ABI_VERSION:
 
 _vp, _i64, _i32, _f32, _sz = (ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_float,
                               ctypes.c_size_t)
+_f64 = ctypes.c_double
 
 
 class ErrorSignalDesc(ctypes.Structure):
@@ -103,6 +106,40 @@ _lib.fpo_layer_optimize_grouped.argtypes = [_i32, _i64, _i64, _i64, _i32, ctypes
                                             ctypes.POINTER(_vp), ctypes.POINTER(_vp),
                                             ctypes.POINTER(_vp), ctypes.POINTER(_vp), _vp, _sz, _vp]
 _lib.fpo_layer_optimize_grouped.restype = _i32
+
+
+_lib.fpo_linear_workspace.argtypes = [_i64, _i64, _i64, _i32]
+_lib.fpo_linear_workspace.restype = _sz
+_lib.fpo_linear.argtypes = [_i64, _i64, _i64, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.fpo_linear.restype = _i32
+_lib.fpo_linear_vjp_workspace.argtypes = [_i64, _i64, _i64, _i32, _i32]
+_lib.fpo_linear_vjp_workspace.restype = _sz
+_lib.fpo_linear_vjp.argtypes = [_i64, _i64, _i64, _i32, _i32, _vp, _vp, _vp, _vp, _i32, _vp, _vp, _vp,
+                                _vp, _vp, _sz, _vp]
+_lib.fpo_linear_vjp.restype = _i32
+
+
+class AdamwTensor(ctypes.Structure):
+    """Mirror of fpo_adamw_tensor."""
+    _fields_ = [("n", _i64), ("G", _vp), ("W_master", _vp), ("W_out", _vp), ("state1", _vp),
+                ("state2", _vp), ("scale1", _vp), ("scale2", _vp), ("g_dtype", _i32),
+                ("w_dtype", _i32), ("state_bits", _i32), ("weight_decay", _f32)]
+
+
+class AdamwDesc(ctypes.Structure):
+    """Mirror of fpo_adamw_desc."""
+    _fields_ = [("lr", _f64), ("beta1", _f64), ("beta2", _f64), ("eps", _f64), ("clip_frac", _f64),
+                ("step", _i64), ("clip", _i32)]
+
+
+ADAMW_BLOCK = 256  # FPO_ADAMW_BLOCK: elements that share the scales of their 8-bit moments
+_lib.fpo_adamw_workspace.argtypes = [_i32, ctypes.POINTER(_i64), _i32]
+_lib.fpo_adamw_workspace.restype = _sz
+_lib.fpo_adamw_grouped.argtypes = [_i32, ctypes.POINTER(AdamwTensor), ctypes.POINTER(AdamwDesc),
+                                   ctypes.c_uint64, _vp, _sz, _vp]
+_lib.fpo_adamw_grouped.restype = _i32
+_lib.fpo_adamw_state_values.argtypes = [_i64, _i32, _vp, _vp, _i32, _vp, _vp]
+_lib.fpo_adamw_state_values.restype = _i32
 
 
 class MuonDesc(ctypes.Structure):
@@ -403,8 +440,12 @@ def layer_update_grouped_signals(gs, As, lr, *, W_masters=None, W_outs=None, G_o
 
 def optimizer_desc(kind=OPT_ADAMW, *, lr=1e-4, momentum=0.9, beta1=0.9, beta2=0.999, eps=1e-8,
                    weight_decay=0.01, clip=CLIP_STEP, clip_frac=0.01, step=1):
-    return OptimizerDesc(int(kind), int(clip), float(lr), float(momentum), float(beta1),
-                         float(beta2), float(eps), float(weight_decay), float(clip_frac), int(step))
+    d = OptimizerDesc(int(kind), int(clip), float(lr), float(momentum), float(beta1),
+                      float(beta2), float(eps), float(weight_decay), float(clip_frac), int(step))
+    # the rates as given, for the entry points that take them in double
+    d.exact = dict(lr=float(lr), beta1=float(beta1), beta2=float(beta2), eps=float(eps),
+                   weight_decay=float(weight_decay), clip_frac=float(clip_frac))
+    return d
 
 
 def layer_optimize_workspace(n_layers, d, d_ff) -> int:
@@ -596,6 +637,165 @@ def layernorm_vjp(g, x, gamma, g_out, *, eps=1e-5, min_rms=0.5, dgamma=None, dbe
                                 _stream(stream))
     _check(rc, "fpo_layernorm_vjp")
     return g_out
+
+
+class _Entry:
+    """An entry point all of whose tensor arguments have to lie on the current device (the other
+    functions here look at a call's leading tensor)."""
+
+    def __init__(self, fn):
+        functools.update_wrapper(self, fn)
+
+    def __call__(self, *args, **kw):
+        for t in (*args, *kw.values()):
+            if isinstance(t, torch.Tensor):
+                _on_current_device(t)
+        return self.__wrapped__(*args, **kw)
+
+
+# --------------------------------------------------------------------------- linear layers
+def linear_workspace(T, d_out, d_in, dtype=BF16) -> int:
+    return int(_lib.fpo_linear_workspace(int(T), int(d_out), int(d_in), int(dtype)))
+
+
+@_Entry
+def linear(x, W, y, *, bias=None, act=ACT_NONE, residual=None, z_out=None, workspace=None,
+           stream=None):
+    """fpo_linear: y = act(x W^T + bias) + residual, for x [T, d_in] and W [d_out, d_in] of one
+    dtype; residual may be y.  z_out takes the pre-activation, which linear_vjp reads.  Returns the
+    workspace tensor (its first word holds the device status)."""
+    T, d_in = x.shape
+    d_out = W.shape[0]
+    _expect(W, (d_out, d_in), x.dtype, "W")
+    _expect(y, (T, d_out), x.dtype, "y")
+    _expect(bias, (d_out,), x.dtype, "bias")
+    _expect(residual, (T, d_out), x.dtype, "residual")
+    _expect(z_out, (T, d_out), x.dtype, "z_out")
+    dt = _dtype_code(x)
+    if workspace is None:
+        workspace = _workspace(linear_workspace(T, d_out, d_in, dt), x.device, stream)
+    rc = _lib.fpo_linear(T, d_out, d_in, dt, int(act), _ptr(x), _ptr(W), _ptr(bias), _ptr(residual),
+                         _ptr(y), _ptr(z_out), _ptr(workspace), _nbytes(workspace), _stream(stream))
+    _check(rc, "fpo_linear")
+    return workspace
+
+
+def linear_vjp_workspace(T, d_out, d_in, dtype=BF16, act=ACT_NONE) -> int:
+    return int(_lib.fpo_linear_vjp_workspace(int(T), int(d_out), int(d_in), int(dtype), int(act)))
+
+
+@_Entry
+def linear_vjp(dy, x, W, dx, *, act=ACT_NONE, z=None, act_in=ACT_NONE, z_in=None, dW=None,
+               dbias=None, workspace=None, stream=None):
+    """fpo_linear_vjp: with dz = dy act'(z), dx = (dz W) act_in'(z_in), dW = dz^T x and the fp32
+    dbias = sum_t dz; dx, dW and dbias may be None (not all), x is read for dW, W for dx.  Returns
+    the workspace tensor (its first word holds the device status)."""
+    T, d_out = dy.shape
+    for t, name in ((W, "W"), (dW, "dW"), (x, "x"), (dx, "dx"), (z_in, "z_in")):
+        if t is not None:
+            d_in = t.shape[1]
+            break
+    else:
+        d_in = 8  # the bias gradient alone
+    _expect(x, (T, d_in), dy.dtype, "x")
+    _expect(W, (d_out, d_in), dy.dtype, "W")
+    _expect(dx, (T, d_in), dy.dtype, "dx")
+    _expect(z, (T, d_out), dy.dtype, "z")
+    _expect(z_in, (T, d_in), dy.dtype, "z_in")
+    _expect(dW, (d_out, d_in), dy.dtype, "dW")
+    _expect(dbias, (d_out,), torch.float32, "dbias")
+    dt = _dtype_code(dy)
+    if workspace is None:
+        workspace = _workspace(linear_vjp_workspace(T, d_out, d_in, dt, act), dy.device, stream)
+    rc = _lib.fpo_linear_vjp(T, d_out, d_in, dt, int(act), _ptr(dy), _ptr(z), _ptr(x), _ptr(W),
+                             int(act_in), _ptr(z_in), _ptr(dx), _ptr(dW), _ptr(dbias),
+                             _ptr(workspace), _nbytes(workspace), _stream(stream))
+    _check(rc, "fpo_linear_vjp")
+    return workspace
+
+
+# --------------------------------------------------------------------------- AdamW over many tensors
+def adamw_workspace(sizes, clip=CLIP_NONE) -> int:
+    return int(_lib.fpo_adamw_workspace(len(sizes), (_i64 * len(sizes))(*sizes), int(clip)))
+
+
+@_Entry
+def adamw_grouped(Gs, opt, W_masters, states1, states2, *, scales1=None, scales2=None, W_outs=None,
+                  weight_decays=None, seed=0, workspace=None, stream=None):
+    """fpo_adamw_grouped: one AdamW step (optimizer_desc, per-tensor relative clip) on any number of
+    tensors with given gradients; what belongs to a tensor has its number of elements, in any shape.
+    Gs: fp32 or bf16, each its own; W_masters: fp32; states1 and
+    states2: fp32, or float8_e4m3fn and uint8 with fp32 scales1 and scales2 of one element per
+    ADAMW_BLOCK (None entries where the states are fp32; zeros are a valid start).  W_outs: fp32 or
+    bf16, the list or an entry may be None; weight_decays: one per tensor, by default the
+    descriptor's.  seed: of the 8-bit states' rounding.  Returns the workspace (None without a clip)."""
+    n = len(Gs)
+    rest = (W_masters, states1, states2, scales1, scales2, W_outs, weight_decays)
+    if n == 0 or any(ts is not None and len(ts) != n for ts in rest):
+        raise ValueError("one entry per tensor expected in every list")
+    sizes = [G.numel() for G in Gs]
+    m_types = [m.dtype for m in states1]
+    small = [dt != torch.float32 for dt in m_types]
+    none = [None] * n
+    scales1, scales2, W_outs = scales1 or none, scales2 or none, W_outs or none
+
+    def check(name, ts, counts, types):
+        for t, c, want in zip(ts, counts, types):
+            if t is not None and (t.dtype != want or t.numel() != c):
+                raise ValueError(f"{name}: expected {c} elements of {want}, got {t.numel()} of {t.dtype}")
+
+    f32 = [torch.float32] * n
+    check("W_masters", W_masters, sizes, f32)
+    check("states1", states1, sizes, [torch.float8_e4m3fn if s else torch.float32 for s in small])
+    check("states2", states2, sizes, [torch.uint8 if s else torch.float32 for s in small])
+    check("W_outs", W_outs, sizes, [t if t is None else t.dtype for t in W_outs])
+    blocks = [-(-c // ADAMW_BLOCK) for c in sizes]
+    check("scales1", scales1, blocks, f32)
+    check("scales2", scales2, blocks, f32)
+    if any(s and (a is None or b is None) for s, a, b in zip(small, scales1, scales2)):
+        raise ValueError("8-bit states need scales1 and scales2")
+    if opt.kind != OPT_ADAMW:
+        raise ValueError("adamw_grouped takes the descriptor of OPT_ADAMW")
+
+    def rate(name, field=None):  # as given to optimizer_desc, or the field if it was set since
+        v = getattr(opt, field or name)
+        given = getattr(opt, "exact", {}).get(name, v)
+        return given if _f32(given).value == v else v
+
+    desc = AdamwDesc(rate("lr"), rate("beta1"), rate("beta2"), rate("eps", "adam_eps"), rate("clip_frac"),
+                     opt.step, opt.clip)
+    g_types = [_dtype_code(G) for G in Gs]
+    w_types = [F32 if t is None else _dtype_code(t) for t in W_outs]
+    decays = [rate("weight_decay")] * n if weight_decays is None else [float(w) for w in weight_decays]
+    for ts in (W_masters, states1, states2):
+        for t in ts:
+            _on_current_device(t)
+    cols = [[_ptr(t) for t in ts] for ts in (Gs, W_masters, W_outs, states1, states2, scales1, scales2)]
+    table = (AdamwTensor * n)(*zip(sizes, *cols, g_types, w_types, [8 if s else 32 for s in small],
+                                   decays))
+    if workspace is None and opt.clip != CLIP_NONE:
+        workspace = _workspace(adamw_workspace(sizes, opt.clip), Gs[0].device, stream)
+    rc = _lib.fpo_adamw_grouped(n, table, ctypes.byref(desc), int(seed) & 0xffffffffffffffff,
+                                _ptr(workspace), 0 if workspace is None else _nbytes(workspace),
+                                _stream(stream))
+    _check(rc, "fpo_adamw_grouped")
+    return workspace
+
+
+@_Entry
+def adamw_state_values(codes, scales, out, *, stream=None):
+    """fpo_adamw_state_values: the values of 8-bit moments (float8_e4m3fn: first, uint8: second)
+    with their scales, into out (fp32 or bf16, the same shape)."""
+    if codes.dtype not in (torch.float8_e4m3fn, torch.uint8):
+        raise TypeError("codes are float8_e4m3fn (first moments) or uint8 (second moments)")
+    n = codes.numel()
+    dt = _dtype_code(out)
+    _expect(out, codes.shape, out.dtype, "out")
+    _expect(scales, (-(-n // ADAMW_BLOCK),), torch.float32, "scales")
+    moment = 1 if codes.dtype == torch.float8_e4m3fn else 2
+    _check(_lib.fpo_adamw_state_values(n, moment, _ptr(codes), _ptr(scales), dt, _ptr(out),
+                                       _stream(stream)), "fpo_adamw_state_values")
+    return out
 
 
 # --------------------------------------------------------------------------- cosine

@@ -4,10 +4,13 @@
 // memory or synchronises (except fpo_get_device_status).
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <atomic>
 #include <climits>
 #include <cmath>
 #include <mutex>
+#include <new>
+#include <vector>
 
 #include "../../include/fpo.h"
 #include "../../include/fpo_testing.h"
@@ -160,6 +163,28 @@ EsLayout es_layout(const fpo_error_signal_desc* d) {
     L.sk = off;        off = align_up(off + (d->dtype == FPO_BF16 ? proj_sk_scratch_bytes() : 0));
     L.total = off;
     return L;
+}
+
+// Memory that a call reads or writes, to find what it would write and also use otherwise.
+struct Span {
+    uintptr_t from, to;
+    bool write;
+};
+Span span(const void* p, size_t bytes, bool write) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p);
+    return Span{a, p ? a + bytes : a, write};
+}
+// Whether a written span meets another one (empty ones meet none).
+bool spans_clash(Span* s, size_t n) {
+    std::sort(s, s + n, [](const Span& a, const Span& b) { return a.from < b.from; });
+    uintptr_t any = 0, written = 0;  // ends of what came before
+    for (size_t i = 0; i < n; ++i) {
+        if (s[i].to == s[i].from) continue;
+        if (s[i].from < (s[i].write ? any : written)) return true;
+        any = std::max(any, s[i].to);
+        if (s[i].write) written = std::max(written, s[i].to);
+    }
+    return false;
 }
 
 }  // namespace
@@ -780,6 +805,217 @@ int32_t fpo_layer_muon_grouped(int32_t n_layers, int64_t T, int64_t d, int64_t d
     const NsTarget to{W_out, W_master, 1.f - opt->lr * opt->weight_decay, opt->lr * opt->scale};
     return cuda_status(launch_newton_schulz(n_layers, di, fi, dtype, nullptr, &mom, opt->eps,
                                             opt->steps, co, to, workspace, status, st));
+}
+
+namespace {
+
+int32_t linear_check(int64_t T, int64_t d_out, int64_t d_in, int32_t dtype) {
+    if (dtype != FPO_F32 && dtype != FPO_BF16) return FPO_ERR_DTYPE;
+    if (T < 0 || d_in <= 0 || d_out <= 0 || T > INT_MAX || d_in > INT_MAX || d_out > INT_MAX)
+        return FPO_ERR_SHAPE;
+    if (dtype == FPO_BF16 && (d_in % 8 != 0 || d_out % 8 != 0)) return FPO_ERR_SHAPE;
+    return FPO_OK;
+}
+bool act_ok(int32_t act) { return act >= FPO_ACT_NONE && act <= FPO_ACT_SILU; }
+
+// Clears the first `bytes` of a workspace (the status word, counters behind it).
+cudaError_t clear(void* workspace, size_t bytes, cudaStream_t st) {
+    return cudaMemsetAsync(workspace, 0, bytes, st);
+}
+
+}  // namespace
+
+size_t fpo_linear_workspace(int64_t T, int64_t d_out, int64_t d_in, int32_t dtype) {
+    if (linear_check(T, d_out, d_in, dtype) != FPO_OK) return 0;
+    return linear_workspace_bytes(dtype, static_cast<int>(T), static_cast<int>(d_out),
+                                  static_cast<int>(d_in));
+}
+
+int32_t fpo_linear(int64_t T, int64_t d_out, int64_t d_in, int32_t dtype, int32_t act,
+                   const void* X, const void* W, const void* bias, const void* residual, void* Y,
+                   void* Z_out, void* workspace, size_t workspace_bytes, void* stream) {
+    int32_t rc = linear_check(T, d_out, d_in, dtype);
+    if (rc != FPO_OK) return rc;
+    if (!act_ok(act)) return FPO_ERR_ARG;
+    if (T > 0 && (!X || !W || !Y)) return FPO_ERR_NULL;
+    if (!aligned16(X) || !aligned16(W) || !aligned16(bias) || !aligned16(residual) ||
+        !aligned16(Y) || !aligned16(Z_out))
+        return FPO_ERR_ALIGN;
+    if (!workspace || workspace_bytes < fpo_linear_workspace(T, d_out, d_in, dtype))
+        return FPO_ERR_WORKSPACE;
+    if ((reinterpret_cast<uintptr_t>(workspace) % kAlign) != 0) return FPO_ERR_ALIGN;
+    const size_t e = dtype == FPO_BF16 ? 2 : 4, t = static_cast<size_t>(T),
+                 o = static_cast<size_t>(d_out), k = static_cast<size_t>(d_in);
+    Span s[] = {span(X, t * k * e, false),    span(W, o * k * e, false),
+                span(bias, o * e, false),     span(residual == Y ? nullptr : residual, t * o * e, false),
+                span(Y, t * o * e, true),     span(Z_out, t * o * e, true),
+                span(workspace, workspace_bytes, true)};
+    if (spans_clash(s, sizeof(s) / sizeof(s[0]))) return FPO_ERR_ARG;
+    rc = check_arch();
+    if (rc != FPO_OK) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const int Ti = static_cast<int>(T), N = static_cast<int>(d_out), K = static_cast<int>(d_in);
+    FPO_TRY(clear(workspace, T == 0 ? sizeof(unsigned) : linear_clear_bytes(dtype, Ti, N, K), st));
+    if (T == 0) return FPO_OK;
+    const LinearFwd p{Ti, N, K, act, X, W, bias, residual, Y, Z_out};
+    return cuda_status(launch_linear(dtype, p, workspace, st));
+}
+
+size_t fpo_linear_vjp_workspace(int64_t T, int64_t d_out, int64_t d_in, int32_t dtype, int32_t act) {
+    if (linear_check(T, d_out, d_in, dtype) != FPO_OK || !act_ok(act)) return 0;
+    return linear_vjp_workspace_bytes(dtype, static_cast<int>(T), static_cast<int>(d_out),
+                                      static_cast<int>(d_in), act);
+}
+
+int32_t fpo_linear_vjp(int64_t T, int64_t d_out, int64_t d_in, int32_t dtype, int32_t act,
+                       const void* dY, const void* Z, const void* X, const void* W, int32_t act_in,
+                       const void* Z_in, void* dX, void* dW, float* dbias, void* workspace,
+                       size_t workspace_bytes, void* stream) {
+    int32_t rc = linear_check(T, d_out, d_in, dtype);
+    if (rc != FPO_OK) return rc;
+    if (!act_ok(act) || !act_ok(act_in)) return FPO_ERR_ARG;
+    if (!dX && !dW && !dbias) return FPO_ERR_NULL;
+    const bool slope = act != FPO_ACT_NONE, slope_in = act_in != FPO_ACT_NONE;
+    if (T > 0 && (!dY || (slope && !Z) || (dX && !W) || (dX && slope_in && !Z_in) || (dW && !X)))
+        return FPO_ERR_NULL;
+    if (!aligned16(dY) || !aligned16(Z) || !aligned16(X) || !aligned16(W) || !aligned16(Z_in) ||
+        !aligned16(dX) || !aligned16(dW) || !aligned16(dbias))
+        return FPO_ERR_ALIGN;
+    if (!workspace || workspace_bytes < fpo_linear_vjp_workspace(T, d_out, d_in, dtype, act))
+        return FPO_ERR_WORKSPACE;
+    if ((reinterpret_cast<uintptr_t>(workspace) % kAlign) != 0) return FPO_ERR_ALIGN;
+    const size_t e = dtype == FPO_BF16 ? 2 : 4, t = static_cast<size_t>(T),
+                 o = static_cast<size_t>(d_out), k = static_cast<size_t>(d_in);
+    Span s[] = {span(dY, t * o * e, false),
+                span(slope ? Z : nullptr, t * o * e, false),
+                span(dW ? X : nullptr, t * k * e, false),
+                span(dX ? W : nullptr, o * k * e, false),
+                span(dX && slope_in ? Z_in : nullptr, t * k * e, false),
+                span(dX, t * k * e, true),
+                span(dW, o * k * e, true),
+                span(dbias, o * 4, true),
+                span(workspace, workspace_bytes, true)};
+    if (spans_clash(s, sizeof(s) / sizeof(s[0]))) return FPO_ERR_ARG;
+    rc = check_arch();
+    if (rc != FPO_OK) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const int Ti = static_cast<int>(T), N = static_cast<int>(d_out), K = static_cast<int>(d_in);
+    if (T == 0) {
+        FPO_TRY(clear(workspace, sizeof(unsigned), st));
+        if (dW) FPO_TRY(cudaMemsetAsync(dW, 0, o * k * e, st));
+        if (dbias) FPO_TRY(cudaMemsetAsync(dbias, 0, o * 4, st));
+        return FPO_OK;
+    }
+    FPO_TRY(clear(workspace, linear_vjp_clear_bytes(dtype, Ti, N, K), st));
+    const LinearVjp p{Ti, N, K, act, act_in, dY, Z, X, W, Z_in, dX, dW, dbias};
+    return cuda_status(launch_linear_vjp(dtype, p, workspace, st));
+}
+
+size_t fpo_adamw_workspace(int32_t n_tensors, const int64_t* n, int32_t clip) {
+    if (n_tensors < 1 || !n || clip == FPO_CLIP_NONE) return 0;
+    for (int k = 0; k < n_tensors; ++k)
+        if (n[k] < 0 || n[k] > FPO_MAX_ADAMW_ELEMENTS) return 0;
+    return align_up(adamw_workspace_floats(n_tensors, n) * sizeof(float));
+}
+
+int32_t fpo_adamw_grouped(int32_t n_tensors, const fpo_adamw_tensor* tensors,
+                          const fpo_adamw_desc* opt, uint64_t seed, void* workspace,
+                          size_t workspace_bytes, void* stream) {
+    if (!tensors || !opt) return FPO_ERR_NULL;
+    if (n_tensors < 1) return FPO_ERR_SHAPE;
+    if (opt->clip < FPO_CLIP_NONE || opt->clip > FPO_CLIP_GRADIENT || !(opt->lr == opt->lr) ||
+        !(opt->eps == opt->eps) || !(opt->clip_frac >= 0.0) || opt->step < 1 ||
+        !(opt->beta1 >= 0.0 && opt->beta1 < 1.0) || !(opt->beta2 >= 0.0 && opt->beta2 < 1.0))
+        return FPO_ERR_ARG;
+    // host memory for the checks and the launch's table; no exception leaves the library
+    std::vector<Span> spans;
+    std::vector<AdamTensor> table;
+    std::vector<int64_t> sizes;
+    try {
+        spans.reserve(static_cast<size_t>(n_tensors) * 7 + 1);
+        table.reserve(static_cast<size_t>(n_tensors));
+        sizes.reserve(static_cast<size_t>(n_tensors));
+    } catch (const std::bad_alloc&) {
+        return FPO_ERR_SHAPE;
+    }
+    for (int k = 0; k < n_tensors; ++k) {
+        const fpo_adamw_tensor& t = tensors[k];
+        if (t.n < 0 || t.n > FPO_MAX_ADAMW_ELEMENTS) return FPO_ERR_SHAPE;
+        if ((t.g_dtype != FPO_F32 && t.g_dtype != FPO_BF16) ||
+            (t.w_dtype != FPO_F32 && t.w_dtype != FPO_BF16))
+            return FPO_ERR_DTYPE;
+        if (t.state_bits != 32 && t.state_bits != 8) return FPO_ERR_ARG;
+        if (!(t.weight_decay == t.weight_decay)) return FPO_ERR_ARG;
+        const bool small = t.state_bits == 8;
+        if (t.n > 0 && (!t.G || !t.W_master || !t.state1 || !t.state2 ||
+                        (small && (!t.scale1 || !t.scale2))))
+            return FPO_ERR_NULL;
+        if (!aligned16(t.G) || !aligned16(t.W_master) || !aligned16(t.W_out) ||
+            !aligned16(t.state1) || !aligned16(t.state2) ||
+            (small && ((reinterpret_cast<uintptr_t>(t.scale1) |
+                        reinterpret_cast<uintptr_t>(t.scale2)) & 3u)))
+            return FPO_ERR_ALIGN;
+        const size_t n = static_cast<size_t>(t.n), st = small ? 1 : 4,
+                     blocks = (n + kAdamBlock - 1) / kAdamBlock;
+        spans.push_back(span(t.G, n * (t.g_dtype == FPO_BF16 ? 2 : 4), false));
+        spans.push_back(span(t.W_master, n * 4, true));
+        // an fp32 W_out may be the master itself
+        if (!(t.w_dtype == FPO_F32 && t.W_out == t.W_master))
+            spans.push_back(span(t.W_out, n * (t.w_dtype == FPO_BF16 ? 2 : 4), true));
+        spans.push_back(span(t.state1, n * st, true));
+        spans.push_back(span(t.state2, n * st, true));
+        if (small) {
+            spans.push_back(span(t.scale1, blocks * 4, true));
+            spans.push_back(span(t.scale2, blocks * 4, true));
+        }
+        table.push_back(AdamTensor{t.n, t.G, t.W_master,
+                                   t.W_out == t.W_master ? nullptr : t.W_out, t.state1, t.state2,
+                                   t.scale1, t.scale2, t.weight_decay, t.g_dtype == FPO_BF16,
+                                   t.w_dtype == FPO_BF16, small});
+        sizes.push_back(t.n);
+    }
+    if (opt->clip != FPO_CLIP_NONE) {
+        if (!workspace || workspace_bytes < fpo_adamw_workspace(n_tensors, sizes.data(), opt->clip))
+            return FPO_ERR_WORKSPACE;
+        if ((reinterpret_cast<uintptr_t>(workspace) % kAlign) != 0) return FPO_ERR_ALIGN;
+        spans.push_back(span(workspace, workspace_bytes, true));
+    }
+    if (spans_clash(spans.data(), spans.size())) return FPO_ERR_ARG;
+    const int32_t rc = check_arch();
+    if (rc != FPO_OK) return rc;
+    const double t = static_cast<double>(opt->step);
+    AdamRates r;
+    r.clip = opt->clip;
+    r.lr = static_cast<float>(opt->lr);
+    r.eps = static_cast<float>(opt->eps);
+    r.clip_frac = static_cast<float>(opt->clip_frac);
+    r.b1 = static_cast<float>(opt->beta1);
+    r.a1 = static_cast<float>(1.0 - opt->beta1);
+    r.b2 = static_cast<float>(opt->beta2);
+    r.a2 = static_cast<float>(1.0 - opt->beta2);
+    r.inv_bc1 = static_cast<float>(1.0 / (1.0 - pow(opt->beta1, t)));
+    r.inv_sqrt_bc2 = static_cast<float>(1.0 / sqrt(1.0 - pow(opt->beta2, t)));
+    return cuda_status(launch_adamw(n_tensors, table.data(), r, seed, opt->step,
+                                    static_cast<float*>(workspace), static_cast<cudaStream_t>(stream)));
+}
+
+int32_t fpo_adamw_state_values(int64_t n, int32_t moment, const void* codes, const float* scales,
+                               int32_t out_dtype, void* out, void* stream) {
+    if (out_dtype != FPO_F32 && out_dtype != FPO_BF16) return FPO_ERR_DTYPE;
+    if (moment != 1 && moment != 2) return FPO_ERR_ARG;
+    if (n < 0 || n > FPO_MAX_ADAMW_ELEMENTS) return FPO_ERR_SHAPE;
+    if (n > 0 && (!codes || !scales || !out)) return FPO_ERR_NULL;
+    if (!aligned16(codes) || !aligned16(out) || (reinterpret_cast<uintptr_t>(scales) & 3u))
+        return FPO_ERR_ALIGN;
+    const size_t s = static_cast<size_t>(n);
+    Span sp[] = {span(codes, s, false), span(scales, (s + kAdamBlock - 1) / kAdamBlock * 4, false),
+                 span(out, s * (out_dtype == FPO_BF16 ? 2 : 4), true)};
+    if (spans_clash(sp, 3)) return FPO_ERR_ARG;
+    const int32_t rc = check_arch();
+    if (rc != FPO_OK) return rc;
+    if (n == 0) return FPO_OK;
+    return cuda_status(launch_state_values(moment == 1, n, codes, scales, out_dtype, out,
+                                           static_cast<cudaStream_t>(stream)));
 }
 
 int32_t fpo_gate_up_signals(int64_t T, int64_t d, int64_t d_ff, int32_t dtype, const void* g,

@@ -209,6 +209,73 @@ cudaError_t launch_optimizer(int dtype, int n_layers, size_t n_elem, const Optim
                              float* const* s1, float* const* s2, double* partials, float* scales,
                              bool norms_done, cudaStream_t st);
 
+// ------------------------------------------------------------ AdamW over many tensors (adamw.cu)
+constexpr int kAdamBlock = 256;  // consecutive elements of a tensor that share an 8-bit moment's scale
+struct AdamTensor {
+    int64_t n;
+    const void* G;
+    float* W;
+    void* W_out;     // or null
+    void* m;         // fp32, or e4m3 codes with state8
+    void* v;         // fp32, or codes of 5 exponent and 3 mantissa bits
+    float* m_scale;  // state8: one per kAdamBlock elements
+    float* v_scale;
+    float weight_decay;
+    bool g_bf16, out_bf16, state8;
+};
+struct AdamRates {
+    int clip;             // 0 none, 1 the step, 2 the gradient
+    float lr, eps, clip_frac;
+    float b1, a1, b2, a2;         // decays, and 1 - them
+    float inv_bc1, inv_sqrt_bc2;  // bias corrections 1 / (1 - b1^t), 1 / sqrt(1 - b2^t)
+};
+// Floats of workspace a step with a clip needs.
+size_t adamw_workspace_floats(int n_tensors, const int64_t* n);
+// The rounding bits depend on `step` too.
+cudaError_t launch_adamw(int n_tensors, const AdamTensor* ts, const AdamRates& op, uint64_t seed,
+                         int64_t step, float* ws, cudaStream_t st);
+// out[n] (dtype 0 = fp32, 1 = bf16) = the values of first (is_signed) or second moments.
+cudaError_t launch_state_values(bool is_signed, long long n, const void* codes, const float* scales,
+                                int out_dtype, void* out, cudaStream_t st);
+
+// ------------------------------------------------------------ linear layers (linear.cu, simt_f32.cu)
+// Y[T, N] = act(X[T, K] W[N, K]^T + bias) + residual, Z = the pre-activation; bias, residual and
+// Z may be null.  act: act_math.cuh.  The workspace's first kLinearHead bytes (status word,
+// counters) are zero before a call.
+struct LinearFwd {
+    int T, N, K, act;
+    const void* X;
+    const void* W;
+    const void* bias;
+    const void* residual;
+    void* Y;
+    void* Z;
+};
+// dZ = dY (.) act'(Z), dX[T, K] = (dZ W) (.) act_in'(Z_in), dW[N, K] = dZ^T X, dbias[N] (fp32) =
+// column sums of dZ; dX, dW and dbias may be null.
+struct LinearVjp {
+    int T, N, K, act, act_in;
+    const void* dY;
+    const void* Z;
+    const void* X;
+    const void* W;
+    const void* Z_in;
+    void* dX;
+    void* dW;
+    float* dbias;
+};
+size_t linear_workspace_bytes(int dtype, int T, int N, int K);
+size_t linear_vjp_workspace_bytes(int dtype, int T, int N, int K, int act);
+// Bytes at the workspace's start that are zero before a call.
+size_t linear_clear_bytes(int dtype, int T, int N, int K);
+size_t linear_vjp_clear_bytes(int dtype, int T, int N, int K);
+cudaError_t launch_linear(int dtype, const LinearFwd& p, void* workspace, cudaStream_t st);
+cudaError_t launch_linear_vjp(int dtype, const LinearVjp& p, void* workspace, cudaStream_t st);
+// The fp32 products of the two (FFMA).
+cudaError_t launch_linear_f32(const LinearFwd& p, cudaStream_t st);
+cudaError_t launch_linear_dx_f32(int T, int N, int K, const float* dZ, const float* W,
+                                 const float* Z_in, int act_in, float* dX, cudaStream_t st);
+
 // Which tcgen05 GEMM kernel the launchers use: 0 = single-CTA 128 x 256 tiles,
 // 1 = CTA-pair 256 x 256 tiles.
 void set_gemm_variant(int v);

@@ -1,0 +1,710 @@
+// linear.cu -- the linear layer Y = act(X W^T + b) + R and its backward pass (bf16; the fp32
+// products are in simt_f32.cu).
+//
+//   forward    Z = X W^T + b       M = T  N = N  K = K    A, B K-major
+//   signal     dX = dZ W           M = T  N = K  K = N    A K-major, B MN-major
+//   gradient   dW = dZ^T X         M = N  N = K  K = T    A, B MN-major
+//
+// Large batches run on the pair tiles of tc_gemm_pair.cuh with the epilogues of
+// linear_epilogues.cuh.  Batches of at most kFewT tokens run on few_tokens_kernel, with the
+// weights as the 128-row operand and the tokens along N.  What the layer's own activation does to
+// the signal, and the bias gradient, are one pass over dY (signal_kernel).
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include "gemm_launch.cuh"
+#include "internal.h"
+#include "linear_epilogues.cuh"
+
+namespace fpo {
+namespace {
+
+constexpr size_t kHead = 256;  // status word
+size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+
+// ------------------------------------------------------------------ few tokens
+// Y^T = W X^T: 128 rows of the weights (features) by BT tokens per tile, one CTA each.  The
+// tiles' k-blocks, tile by tile, are one sequence of units that the CTAs share out evenly, so
+// that every SM streams the same number of weight bytes whatever the number of tiles: CTA c has
+// units [c U / C, (c + 1) U / C).  A tile that lies in one CTA's range goes from the accumulator
+// to the output.  Of the others each CTA leaves its sums in scratch, and the warp that is the
+// last of a tile's to do so (a counter per tile and quarter of its rows) adds them in CTA order,
+// whichever it is: the sums do not depend on the order in which the CTAs finish, and no CTA
+// waits for another.
+//   warp 0      TMA producer: a k-block of weights (16 KB) and of tokens per stage
+//   warp 1      TMEM, MMAs (128 x BT x 16)
+//   warps 2..5  epilogue: one feature per lane
+// Bound: the weights' bytes.
+constexpr int kFewT = 128;
+
+template <int BT>
+struct FewSmem {
+    static constexpr int kWBytes = kBM * kBK * 2;
+    static constexpr int kXBytes = BT * kBK * 2;
+    static constexpr int kStageBytes = kWBytes + kXBytes;
+    static constexpr int kFit = 221184 / kStageBytes;
+    static constexpr int kStages = kFit < 12 ? kFit : 12;
+    static constexpr int kBarOffset = kStages * kStageBytes;
+    static constexpr int kNumBars = 2 * kStages + 5;
+    static constexpr int kMiscOffset = kBarOffset + kNumBars * 8;
+    static constexpr int kBytes = kMiscOffset + 16 + 1024;
+};
+
+struct FewShape {
+    int M, T;            // features, tokens
+    int k_blocks, tiles;
+    long long units;     // tiles * k_blocks
+    float* scratch;      // [2 CTAs][BT][128]: slot 2 c + 1 has a tile's first k-blocks
+    unsigned* counters;  // [tiles][4], zero at the start
+};
+
+// CTA c's units, and the CTA of a unit.
+__device__ __forceinline__ long long few_start(const FewShape& s, long long c, long long C) {
+    return c * s.units / C;
+}
+__device__ __forceinline__ int few_owner(const FewShape& s, long long u, long long C) {
+    return static_cast<int>(((u + 1) * C - 1) / s.units);
+}
+
+// One feature of the tokens from t0 on through the epilogue: consecutive lanes are consecutive
+// features.
+__device__ __forceinline__ void few_out(const LinearOut& p, int feature, int t0, int n,
+                                        const float (&v)[32]) {
+    if (feature >= p.N) return;
+    const float bias = p.bias ? __bfloat162float(p.bias[feature]) : 0.f;
+    with_act(p.act, [&](auto act) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+            if (j >= n) break;
+            const long long o = (t0 + j) * p.ld + feature;
+            const float z = v[j] + bias;
+            if (p.Z) p.Z[o] = __float2bfloat16_rn(z);
+            float y = act_value<act.value, true>(z);
+            if (p.residual) y += __bfloat162float(p.residual[o]);
+            p.Y[o] = __float2bfloat16_rn(y);
+        }
+    });
+}
+__device__ __forceinline__ void few_out(const SlopeOut& p, int feature, int t0, int n,
+                                        const float (&v)[32]) {
+    if (feature >= p.N) return;
+    with_act(p.z ? p.act : kActNone, [&](auto act) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+            if (j >= n) break;
+            const long long o = (t0 + j) * p.ld + feature;
+            float x = v[j];
+            if constexpr (act.value != kActNone)
+                x *= act_slope<act.value, true>(__bfloat162float(p.z[o]));
+            p.X[o] = __float2bfloat16_rn(x);
+        }
+    });
+}
+
+template <int BT, bool W_MN, class Out>
+__global__ void __launch_bounds__(192, 1)
+    few_tokens_kernel(const __grid_constant__ CUtensorMap wmap,
+                      const __grid_constant__ CUtensorMap xmap, const __grid_constant__ Out out,
+                      const FewShape sh, unsigned* status, unsigned long long wait_limit_ns) {
+    using L = FewSmem<BT>;
+    constexpr int kStages = L::kStages;
+    constexpr uint32_t kIdesc = idesc_bf16_f32(kBM, BT, W_MN, false);
+    constexpr int kAccCols = BT < 32 ? 32 : BT;
+    constexpr int kTmemCols = 2 * kAccCols;
+
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw);
+    const uint32_t pad = (1024u - (raw & 1023u)) & 1023u;
+    uint8_t* smem = smem_raw + pad;
+    const uint32_t sbase = raw + pad;
+    const uint32_t bar0 = sbase + L::kBarOffset;
+    auto full_bar = [&](int s) { return bar0 + 8u * s; };
+    auto empty_bar = [&](int s) { return bar0 + 8u * (kStages + s); };
+    auto tfull_bar = [&](int a) { return bar0 + 8u * (2 * kStages + a); };
+    auto tempty_bar = [&](int a) { return bar0 + 8u * (2 * kStages + 2 + a); };
+    const uint32_t drain_bar = bar0 + 8u * (2 * kStages + 4);
+    uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(smem + L::kMiscOffset);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + L::kMiscOffset + 4);
+
+    const int warp = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(full_bar(s), 1);
+            mbar_init(empty_bar(s), 1);
+        }
+        for (int a = 0; a < 2; ++a) {
+            mbar_init(tfull_bar(a), 1);
+            mbar_init(tempty_bar(a), 4);
+        }
+        mbar_init(drain_bar, 1);
+        *abort_flag = 0;
+        fence_mbar_init();
+        tma_prefetch_desc(&wmap);
+        tma_prefetch_desc(&xmap);
+    }
+    if (warp == 1) {
+        tmem_alloc<kTmemCols>(smem_u32(tmem_holder));
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = *tmem_holder;
+    grid_dependency_wait();
+
+    const WaitGuard guard{abort_flag, status, wait_limit_ns};
+    const long long C = gridDim.x;
+    const long long u0 = few_start(sh, blockIdx.x, C), u1 = few_start(sh, blockIdx.x + 1, C);
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int stage = 0;
+            uint32_t phase = 0;
+            uint32_t issued_mask = 0, issued_parity = 0;
+            int tile = static_cast<int>(u0 / sh.k_blocks), kb = static_cast<int>(u0 % sh.k_blocks);
+            for (long long u = u0; u < u1; ++u) {
+                if (!mbar_wait(empty_bar(stage), phase ^ 1u, guard)) break;
+                const uint32_t sw = sbase + stage * L::kStageBytes;
+                mbar_arrive_expect_tx(full_bar(stage), L::kStageBytes);
+                load_operand<W_MN, kBM>(&wmap, sw, full_bar(stage), tile * kBM, kb * kBK);
+                load_operand<false, BT>(&xmap, sw + L::kWBytes, full_bar(stage), 0, kb * kBK);
+                issued_mask |= 1u << stage;
+                issued_parity = (issued_parity & ~(1u << stage)) | (phase << stage);
+                if (++stage == kStages) { stage = 0; phase ^= 1u; }
+                if (++kb == sh.k_blocks) { kb = 0; ++tile; }
+            }
+            grid_dependency_trigger();
+            for (int s = 0; s < kStages; ++s)  // no copy lands in shared memory after exit
+                if (issued_mask & (1u << s))
+                    mbar_wait_drain(full_bar(s), (issued_parity >> s) & 1u, kDrainLimitNs);
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (lane == 0) {
+            int stage = 0, acc = 0;
+            uint32_t phase = 0, acc_phase = 0;
+            bool ok = true, issued_any = false;
+            int kb = static_cast<int>(u0 % sh.k_blocks);
+            for (long long u = u0; u < u1 && ok;) {
+                const long long end = min(u1, u + sh.k_blocks - kb);  // of this tile's segment
+                if (!mbar_wait(tempty_bar(acc), acc_phase ^ 1u, guard)) { ok = false; break; }
+                tc_fence_after();
+                const uint32_t d_tmem = tmem_base + static_cast<uint32_t>(acc * kAccCols);
+                bool first = true;
+                for (; u < end; ++u) {
+                    if (!mbar_wait(full_bar(stage), phase, guard)) { ok = false; break; }
+                    tc_fence_after();
+                    const uint32_t sw = sbase + stage * L::kStageBytes;
+                    const uint32_t sx = sw + L::kWBytes;
+#pragma unroll
+                    for (int kk = 0; kk < kBK / kUmmaK; ++kk)
+                        tc_mma_bf16(d_tmem, operand_desc<W_MN>(sw, kk), operand_desc<false>(sx, kk),
+                                    kIdesc, !first || kk != 0 ? 1u : 0u);
+                    first = false;
+                    issued_any = true;
+                    tc_commit(empty_bar(stage));
+                    if (++stage == kStages) { stage = 0; phase ^= 1u; }
+                }
+                if (!ok) break;
+                kb = 0;
+                tc_commit(tfull_bar(acc));
+                if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+            }
+            if (issued_any) {  // the MMAs issued end before TMEM and shared memory go away
+                tc_commit(drain_bar);
+                mbar_wait_drain(drain_bar, 0, kDrainLimitNs);
+            }
+        }
+        __syncwarp();
+    } else {
+        const int q = warp & 3;  // TMEM lane quarter this warp may access
+        int acc = 0;
+        uint32_t acc_phase = 0;
+        int tile = static_cast<int>(u0 / sh.k_blocks), kb = static_cast<int>(u0 % sh.k_blocks);
+        for (long long u = u0; u < u1;) {
+            const long long end = min(u1, u + sh.k_blocks - kb);
+            const bool whole = kb == 0 && end - u == sh.k_blocks;
+            const int feature = tile * kBM + q * 32 + lane;
+            const uint32_t t_row = tmem_base + (static_cast<uint32_t>(q * 32) << 16) +
+                                   static_cast<uint32_t>(acc * kAccCols);
+            // one answer for the warp: its lanes wait, and run out of time, one by one
+            auto ready = [&] {
+                const bool in_time = mbar_wait(tfull_bar(acc), acc_phase, guard);
+                if (!__all_sync(0xffffffffu, in_time)) return false;
+                tc_fence_after();
+                return true;
+            };
+            if (!ready()) break;
+            float* slot = sh.scratch + (static_cast<long long>(2 * blockIdx.x + (kb == 0)) * BT) * kBM +
+                          q * 32 + lane;
+#pragma unroll 1
+            for (int t0 = 0; t0 < sh.T; t0 += 32) {
+                float v[32];
+                tmem_ld_32x32b_x32(t_row + t0, v);
+                if (t0 + 32 >= sh.T) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(tempty_bar(acc));
+                }
+                const int n = min(32, sh.T - t0);
+                if (whole) {
+                    few_out(out, feature, t0, n, v);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j)
+                        if (j < n) slot[(t0 + j) * kBM] = v[j];
+                }
+            }
+            if (!whole) {
+                // the last of the tile's CTAs adds their sums
+                const long long first_unit = static_cast<long long>(tile) * sh.k_blocks;
+                const int c0 = few_owner(sh, first_unit, C);
+                const int c1 = few_owner(sh, first_unit + sh.k_blocks - 1, C);
+                __threadfence();
+                __syncwarp();
+                unsigned before = 0;
+                if (lane == 0) before = atomicAdd(sh.counters + 4 * tile + q, 1u);
+                before = __shfl_sync(0xffffffffu, before, 0);
+                if (before == static_cast<unsigned>(c1 - c0)) {
+                    __threadfence();
+#pragma unroll 1
+                    for (int t0 = 0; t0 < sh.T; t0 += 32) {
+                        const int n = min(32, sh.T - t0);
+                        float v[32];
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = 0.f;
+#pragma unroll 1
+                        for (int c = c0; c <= c1; ++c) {
+                            const float* s =
+                                sh.scratch + (static_cast<long long>(2 * c + (c == c0)) * BT + t0) * kBM +
+                                q * 32 + lane;
+#pragma unroll
+                            for (int j = 0; j < 32; ++j)
+                                if (j < n) v[j] += __ldcg(s + j * kBM);
+                        }
+                        few_out(out, feature, t0, n, v);
+                    }
+                }
+            }
+            if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
+            u = end;
+            kb = 0;
+            ++tile;
+        }
+        __syncwarp();
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc<kTmemCols>(tmem_base);
+    }
+}
+
+int sm_count() {
+    DevInfo di;
+    return current_device_info(&di) ? di.sm_count : 152;
+}
+
+int few_bt(int T) { return T <= 16 ? 16 : T <= 32 ? 32 : T <= 64 ? 64 : 128; }
+
+// CTAs of a problem: one per SM while each has at least 4 k-blocks.
+long long few_ctas(int M, int K) {
+    const long long units = static_cast<long long>((M + kBM - 1) / kBM) * ((K + kBK - 1) / kBK);
+    const long long most = (units + 3) / 4, sms = sm_count();
+    return most < sms ? most : sms;
+}
+size_t few_counter_bytes(int M) { return up256(static_cast<size_t>((M + kBM - 1) / kBM) * 16); }
+size_t few_scratch_bytes(int M, int K, int T) {
+    return static_cast<size_t>(2 * few_ctas(M, K)) * few_bt(T) * kBM * 4;
+}
+
+// W: [M, K] (K-major) or, W_MN, [K, M]; X [T, K]; head: the counters, then the scratch.
+template <int BT, bool W_MN, class Out>
+cudaError_t run_few_bt(const void* W, const void* X, int M, int K, int T, const Out& out,
+                       uint8_t* counters, float* scratch, unsigned* status, cudaStream_t st) {
+    using L = FewSmem<BT>;
+    constexpr auto kern = few_tokens_kernel<BT, W_MN, Out>;
+    const cudaError_t e = set_smem_limit<kern>(L::kBytes);
+    if (e != cudaSuccess) return e;
+    CUtensorMap wmap, xmap;
+    const bool ok = W_MN ? map_mnmajor(&wmap, W, K, M) : map_kmajor(&wmap, W, M, K, kBM);
+    if (!ok || !map_kmajor(&xmap, X, T, K, BT)) return cudaErrorInvalidValue;
+    FewShape sh;
+    sh.M = M;
+    sh.T = T;
+    sh.k_blocks = (K + kBK - 1) / kBK;
+    sh.tiles = (M + kBM - 1) / kBM;
+    sh.units = static_cast<long long>(sh.tiles) * sh.k_blocks;
+    sh.scratch = scratch;
+    sh.counters = reinterpret_cast<unsigned*>(counters);
+    return launch_chained(kern, dim3(static_cast<unsigned>(few_ctas(M, K))), 192, L::kBytes, st, wmap,
+                          xmap, out, sh, status, wait_limit_ns());
+}
+template <bool W_MN, class Out>
+cudaError_t run_few(const void* W, const void* X, int M, int K, int T, const Out& out,
+                    uint8_t* counters, float* scratch, unsigned* status, cudaStream_t st) {
+    switch (few_bt(T)) {
+        case 16: return run_few_bt<16, W_MN>(W, X, M, K, T, out, counters, scratch, status, st);
+        case 32: return run_few_bt<32, W_MN>(W, X, M, K, T, out, counters, scratch, status, st);
+        case 64: return run_few_bt<64, W_MN>(W, X, M, K, T, out, counters, scratch, status, st);
+        default: return run_few_bt<128, W_MN>(W, X, M, K, T, out, counters, scratch, status, st);
+    }
+}
+
+// ------------------------------------------------------------------ pair tiles
+// Clusters of the pair kernels at once (76 without a device: two SMs of 152 each).
+int linear_clusters() {
+    using L = GemmPairSmem<256, kPairStages, pair_ksub<256, false, false>()>;
+    constexpr auto kern = tc_gemm_pair_kernel<256, false, false, kPairStages, 1, EpiLinear<2>>;
+    DevInfo di;
+    int c = 76;
+    if (current_device_info(&di) && set_smem_limit<kern>(L::kBytes) == cudaSuccess)
+        c = resident_clusters<kern>(gemm_threads<EpiLinear<2>>(), L::kBytes, di.sm_count, 2);
+    cudaGetLastError();
+    return c;
+}
+
+// How a product runs: 128-column tiles, K ranges per tile (all of them, or with `tail` those of
+// the last partial wave), and the units of scratch.
+struct PairPlan {
+    bool half = false, tail = false;
+    int split = 0;
+    long long units = 0;
+};
+
+PairPlan pair_plan(int M, int N, int K) {
+    PairPlan p;
+    const long long tiles = static_cast<long long>((M + 255) / 256) * ((N + 255) / 256);
+    const int kb = (K + kBK - 1) / kBK;
+    const long long clusters = linear_clusters();
+    const double block_ns = 344.0;  // a 64-deep k-block of a 256 x 256 pair tile under load
+    auto parts_ns = [](double waves, double units) {  // store and sum of the parts, a launch
+        return waves * 2500.0 + 4000.0 + units * 262144.0 / 4300.0;
+    };
+    if (tiles >= clusters) {
+        const SkPlan t = tail_plan(tiles, clusters, kb);
+        if (t.tail_tiles > 0) {
+            const long long units = t.tail_tiles * t.tail_split;
+            const double waves = static_cast<double>((units + clusters - 1) / clusters);
+            const double split = waves * ((kb + t.tail_split - 1) / t.tail_split) * block_ns +
+                                 parts_ns(waves, static_cast<double>(units));
+            if (split < kb * block_ns) {
+                p.tail = true;
+                p.units = units;
+            }
+        }
+        return p;
+    }
+    double best = kb * block_ns;
+    if (2 * tiles <= clusters) {
+        p.half = true;
+        best = kb * block_ns * 0.6;
+    }
+    for (int S = 2; S <= 32 && kb / S >= 8 && tiles * S <= kTailWaves * clusters; ++S) {
+        const double waves = static_cast<double>((tiles * S + clusters - 1) / clusters);
+        const double cost = waves * ((kb + S - 1) / S) * block_ns +
+                            parts_ns(waves, static_cast<double>(tiles * S));
+        if (cost < best) {
+            best = cost;
+            p.half = false;
+            p.split = S;
+            p.units = tiles * S;
+        }
+    }
+    return p;
+}
+
+size_t pair_scratch_bytes(int M, int N, int K) {
+    return static_cast<size_t>(pair_plan(M, N, K).units) * kPairBM * 256 * sizeof(float);
+}
+
+template <class Out>
+__global__ void __launch_bounds__(kFixupThreads)
+    linear_fixup_kernel(const GemmShape sh, const float* scratch, const __grid_constant__ Out out) {
+    grid_dependency_trigger();
+    grid_dependency_wait();
+    int row, n;
+    float s4[4];
+    if (!sk_tail_sum<256>(sh, scratch, row, n, s4)) return;
+    out_row4(out, row * out.ld + n, n, s4);
+}
+
+// C[M, N] = A B^T through Epi.  A_MN: A is [K, M], else [M, K]; B_MN: B is [K, N], else [N, K].
+template <bool A_MN, bool B_MN, template <int> class Epi, class Out>
+cudaError_t run_pair(const void* A, const void* B, int M, int N, int K, const Out& out,
+                     float* scratch, unsigned* status, cudaStream_t st) {
+    const PairPlan pp = pair_plan(M, N, K);
+    GemmMaps<1> maps;
+    bool ok = A_MN ? map_mnmajor(&maps.a[0], A, K, M) : map_kmajor(&maps.a[0], A, M, K, kBM);
+    ok = ok && (B_MN ? map_mnmajor(&maps.b[0], B, K, N)
+                     : map_kmajor(&maps.b[0], B, N, K, pp.half ? kHalfBN / 2 : 128));
+    if (!ok) return cudaErrorInvalidValue;
+    if (pp.half)
+        return run_gemm_pair<kHalfBN, A_MN, B_MN, kHalfStages, 1, Epi<1>>(
+            maps, out, make_shape(M, N, K, kHalfBN, 1, band_for(true), kPairBM), status, st);
+    const GemmShape sh = make_shape(M, N, K, 256, 1, band_for(true), kPairBM);
+    SkPlan plan;
+    const cudaError_t e = run_gemm_pair<256, A_MN, B_MN, kPairStages, 1, Epi<2>>(
+        maps, out, sh, status, st, pp.units > 0 ? scratch : nullptr, &plan, pp.split);
+    if (e != cudaSuccess || plan.tail_tiles <= 0) return e;
+    return launch_chained(linear_fixup_kernel<Out>, sk_fixup_grid<256>(plan), kFixupThreads, 0, st,
+                          sk_fixup_shape(plan, sh), static_cast<const float*>(scratch), out);
+}
+
+// ------------------------------------------------------------------ the signal at the layer's own output
+// dZ = dY (.) act'(Z) (dZ and Z null: dY as it is) and the sums of its columns, before rounding,
+// over a range of rows: part[range][N].  16 lanes to kV columns each and 16 rows at a time;
+// a thread adds its rows in order, the block's 16 in order.
+// Bound: HBM, one pass over dY and Z.
+constexpr int kSigThreads = 256, kSigLanes = 16, kSigRows = kSigThreads / kSigLanes;
+
+template <typename T, int kV>
+__device__ __forceinline__ void sig_load(const T* p, float (&x)[kV]) {
+    if constexpr (kV == 8) {
+        const uint4 u = *reinterpret_cast<const uint4*>(p);
+        float a[4], b[4];
+        unpack4(make_uint2(u.x, u.y), a);
+        unpack4(make_uint2(u.z, u.w), b);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            x[k] = a[k];
+            x[4 + k] = b[k];
+        }
+    } else if constexpr (kV == 4) {
+        const float4 u = *reinterpret_cast<const float4*>(p);
+        x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w;
+    } else {
+        x[0] = p[0];
+    }
+}
+template <typename T, int kV>
+__device__ __forceinline__ void sig_store(T* p, const float (&x)[kV]) {
+    if constexpr (kV == 8) {
+        *reinterpret_cast<uint4*>(p) =
+            make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
+                       pack_bf16x2(x[6], x[7]));
+    } else if constexpr (kV == 4) {
+        *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+    } else {
+        p[0] = x[0];
+    }
+}
+
+template <typename T, int kV>
+__global__ void __launch_bounds__(kSigThreads)
+    signal_kernel(const T* dY, const T* Z, int act, int rows, int N, int rows_per, T* dZ,
+                  float* part) {
+    __shared__ float sums[kSigRows][kSigLanes * kV + 1];
+    grid_dependency_trigger();
+    grid_dependency_wait();
+    const int lane = threadIdx.x % kSigLanes, row_lane = threadIdx.x / kSigLanes;
+    const int col = (blockIdx.x * kSigLanes + lane) * kV;
+    const int r0 = blockIdx.y * rows_per, r1 = min(rows, r0 + rows_per);
+    float s[kV];
+#pragma unroll
+    for (int k = 0; k < kV; ++k) s[k] = 0.f;
+    if (col < N) {
+        with_act(Z ? act : kActNone, [&](auto a) {
+#pragma unroll 4
+            for (int r = r0 + row_lane; r < r1; r += kSigRows) {
+                const long long o = static_cast<long long>(r) * N + col;
+                float x[kV];
+                sig_load<T, kV>(dY + o, x);
+                if constexpr (a.value != kActNone) {
+                    float z[kV];
+                    sig_load<T, kV>(Z + o, z);
+#pragma unroll
+                    for (int k = 0; k < kV; ++k) x[k] *= act_slope<a.value, kV == 8>(z[k]);
+                    sig_store<T, kV>(dZ + o, x);
+                }
+#pragma unroll
+                for (int k = 0; k < kV; ++k) s[k] += x[k];
+            }
+        });
+    }
+    if (!part) return;
+#pragma unroll
+    for (int k = 0; k < kV; ++k) sums[row_lane][lane * kV + k] = s[k];
+    __syncthreads();
+    for (int c = threadIdx.x; c < kSigLanes * kV; c += kSigThreads) {
+        const int n = blockIdx.x * kSigLanes * kV + c;
+        if (n >= N) continue;
+        float t = 0.f;
+#pragma unroll
+        for (int r = 0; r < kSigRows; ++r) t += sums[r][c];
+        part[static_cast<long long>(blockIdx.y) * N + n] = t;
+    }
+}
+
+// dbias = the ranges' sums in order.
+__global__ void __launch_bounds__(kSigThreads)
+    bias_sum_kernel(const float* part, int ranges, int N, float* dbias) {
+    grid_dependency_trigger();
+    grid_dependency_wait();
+    const int n = blockIdx.x * kSigThreads + threadIdx.x;
+    if (n >= N) return;
+    float t = 0.f;
+#pragma unroll 8
+    for (int r = 0; r < ranges; ++r) t += part[static_cast<long long>(r) * N + n];
+    dbias[n] = t;
+}
+
+struct SignalPlan {
+    int cols;      // column blocks
+    int rows_per;  // rows of a range, a multiple of kSigRows
+    int ranges;
+};
+int sig_v(int dtype, int N) { return dtype == 1 ? 8 : N % 4 == 0 ? 4 : 1; }
+SignalPlan signal_plan(int dtype, int T, int N) {
+    const int per = kSigLanes * sig_v(dtype, N);
+    SignalPlan p;
+    p.cols = (N + per - 1) / per;
+    const long long blocks = 8LL * sm_count();
+    long long ranges = blocks / p.cols;
+    const long long most = (T + 63) / 64;  // of at least 64 rows
+    if (ranges > most) ranges = most;
+    if (ranges < 1) ranges = 1;
+    p.rows_per = static_cast<int>((((T + ranges - 1) / ranges) + kSigRows - 1) / kSigRows * kSigRows);
+    p.ranges = (T + p.rows_per - 1) / p.rows_per;
+    return p;
+}
+
+template <typename T, int kV>
+cudaError_t run_signal_v(const LinearVjp& p, T* dZ, float* part, const SignalPlan& sp,
+                         cudaStream_t st) {
+    float* to = p.dbias && sp.ranges == 1 ? p.dbias : p.dbias ? part : nullptr;
+    const cudaError_t e = launch_chained(
+        signal_kernel<T, kV>, dim3(sp.cols, sp.ranges), kSigThreads, 0, st,
+        static_cast<const T*>(p.dY), static_cast<const T*>(p.act != kActNone ? p.Z : nullptr), p.act,
+        p.T, p.N, sp.rows_per, dZ, to);
+    if (e != cudaSuccess || !p.dbias || sp.ranges == 1) return e;
+    return launch_chained(bias_sum_kernel, dim3((p.N + kSigThreads - 1) / kSigThreads), kSigThreads,
+                          0, st, static_cast<const float*>(part), sp.ranges, p.N, p.dbias);
+}
+
+}  // namespace
+
+size_t linear_clear_bytes(int dtype, int T, int N, int K) {
+    return dtype == 1 && T <= kFewT ? kHead + few_counter_bytes(N) : sizeof(unsigned);
+}
+size_t linear_workspace_bytes(int dtype, int T, int N, int K) {
+    if (dtype != 1 || T == 0) return kHead;
+    if (T <= kFewT) return kHead + few_counter_bytes(N) + few_scratch_bytes(N, K, T);
+    return kHead + pair_scratch_bytes(T, N, K);
+}
+
+cudaError_t launch_linear(int dtype, const LinearFwd& p, void* workspace, cudaStream_t st) {
+    if (dtype == 0) return launch_linear_f32(p, st);
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    unsigned* status = reinterpret_cast<unsigned*>(ws);
+    LinearOut out;
+    out.bias = static_cast<const __nv_bfloat16*>(p.bias);
+    out.residual = static_cast<const __nv_bfloat16*>(p.residual);
+    out.Y = static_cast<__nv_bfloat16*>(p.Y);
+    out.Z = static_cast<__nv_bfloat16*>(p.Z);
+    out.ld = p.N;
+    out.M = p.T;
+    out.N = p.N;
+    out.act = p.act;
+    if (p.T <= kFewT)
+        return run_few<false>(p.W, p.X, p.N, p.K, p.T, out, ws + kHead,
+                              reinterpret_cast<float*>(ws + kHead + few_counter_bytes(p.N)), status,
+                              st);
+    return run_pair<false, false, EpiLinear>(p.X, p.W, p.T, p.N, p.K, out,
+                                             reinterpret_cast<float*>(ws + kHead), status, st);
+}
+
+namespace {
+
+// The backward pass's workspace: status word, counters of few_tokens_kernel, dZ (with an
+// activation), the bias ranges' sums, scratch of the products' parts.
+struct VjpLayout {
+    size_t dz, part, scratch, total;
+};
+VjpLayout vjp_layout(int dtype, int T, int N, int K, int act) {
+    VjpLayout l;
+    size_t off = kHead + (dtype == 1 && T <= kFewT ? few_counter_bytes(K) : 0);
+    l.dz = off;
+    if (act != kActNone) off = up256(off + static_cast<size_t>(T) * N * (dtype == 1 ? 2 : 4));
+    l.part = off;
+    off = up256(off + static_cast<size_t>(signal_plan(dtype, T, N).ranges) * N * sizeof(float));
+    l.scratch = off;
+    size_t scratch = 0;
+    if (dtype == 1) {
+        scratch = pair_scratch_bytes(N, K, T);
+        const size_t dx = T <= kFewT ? few_scratch_bytes(K, N, T) : pair_scratch_bytes(T, K, N);
+        scratch = dx > scratch ? dx : scratch;
+    }
+    l.total = off + scratch;
+    return l;
+}
+
+}  // namespace
+
+size_t linear_vjp_clear_bytes(int dtype, int T, int N, int K) {
+    return dtype == 1 && T <= kFewT ? kHead + few_counter_bytes(K) : sizeof(unsigned);
+}
+size_t linear_vjp_workspace_bytes(int dtype, int T, int N, int K, int act) {
+    return T == 0 ? kHead : vjp_layout(dtype, T, N, K, act).total;
+}
+
+cudaError_t launch_linear_vjp(int dtype, const LinearVjp& p, void* workspace, cudaStream_t st) {
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    unsigned* status = reinterpret_cast<unsigned*>(ws);
+    const VjpLayout l = vjp_layout(dtype, p.T, p.N, p.K, p.act);
+    float* part = reinterpret_cast<float*>(ws + l.part);
+    float* scratch = reinterpret_cast<float*>(ws + l.scratch);
+    const void* dZ = p.dY;
+    cudaError_t e = cudaSuccess;
+    if (p.act != kActNone) dZ = ws + l.dz;
+    if (p.act != kActNone || p.dbias) {
+        const SignalPlan sp = signal_plan(dtype, p.T, p.N);
+        void* to = p.act != kActNone ? ws + l.dz : nullptr;
+        if (dtype == 1)
+            e = run_signal_v<__nv_bfloat16, 8>(p, static_cast<__nv_bfloat16*>(to), part, sp, st);
+        else if (sig_v(dtype, p.N) == 4)
+            e = run_signal_v<float, 4>(p, static_cast<float*>(to), part, sp, st);
+        else
+            e = run_signal_v<float, 1>(p, static_cast<float*>(to), part, sp, st);
+        if (e != cudaSuccess) return e;
+    }
+    if (dtype == 0) {
+        const float* dzf = static_cast<const float*>(dZ);
+        if (p.dX)
+            e = launch_linear_dx_f32(p.T, p.N, p.K, dzf, static_cast<const float*>(p.W),
+                                     static_cast<const float*>(p.act_in != kActNone ? p.Z_in : nullptr),
+                                     p.act_in, static_cast<float*>(p.dX), st);
+        if (e != cudaSuccess || !p.dW) return e;
+        const float* x = static_cast<const float*>(p.X);
+        float* dw = static_cast<float*>(p.dW);
+        return launch_update_f32(1, p.T, p.N, p.K, &dzf, &x, 0.f, nullptr, nullptr, &dw, st);
+    }
+    if (p.dX) {
+        SlopeOut out;
+        out.z = static_cast<const __nv_bfloat16*>(p.act_in != kActNone ? p.Z_in : nullptr);
+        out.X = static_cast<__nv_bfloat16*>(p.dX);
+        out.ld = p.K;
+        out.M = p.T;
+        out.N = p.K;
+        out.act = p.act_in;
+        e = p.T <= kFewT ? run_few<true>(p.W, dZ, p.K, p.N, p.T, out, ws + kHead, scratch, status, st)
+                         : run_pair<false, true, EpiSlope>(dZ, p.W, p.T, p.K, p.N, out, scratch,
+                                                           status, st);
+        if (e != cudaSuccess) return e;
+    }
+    if (!p.dW) return cudaSuccess;
+    SlopeOut out;
+    out.z = nullptr;
+    out.X = static_cast<__nv_bfloat16*>(p.dW);
+    out.ld = p.K;
+    out.M = p.N;
+    out.N = p.K;
+    out.act = kActNone;
+    return run_pair<true, true, EpiSlope>(dZ, p.X, p.N, p.K, p.T, out, scratch, status, st);
+}
+
+}  // namespace fpo

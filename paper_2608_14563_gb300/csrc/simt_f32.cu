@@ -22,6 +22,7 @@
 #include <atomic>
 #include <type_traits>
 
+#include "act_math.cuh"
 #include "error_math.cuh"
 #include "internal.h"
 #include "ptx.cuh"
@@ -69,6 +70,20 @@ struct SEpiSwiglu {  // dA = e b silu'(a), dB = e silu(a) from e = g W3 and cach
     const float* a;
     const float* b;
     long long ld;
+};
+struct SEpiLinear {  // z = v + bias, Y = act(z) + residual; bias, residual and Z may be null
+    const float* bias;
+    const float* residual;
+    float* Y;
+    float* Z;
+    long long ld;
+    int act;
+};
+struct SEpiSlope {  // dX = v act'(z_in); z_in null: v
+    const float* z_in;
+    float* dX;
+    long long ld;
+    int act;
 };
 struct SEpiUpdate {
     float* W_master[kMaxG];
@@ -335,6 +350,47 @@ __global__ void __launch_bounds__(kThreads, 2)
                     }
                     st4(ep.dA + off, da, nv, vec);
                     st4(ep.dB + off, db, nv, vec);
+                } else if constexpr (std::is_same_v<Epi, SEpiLinear>) {
+                    const long long off = row * ep.ld + col;
+                    const bool vec = (ep.ld & 3) == 0;
+                    float z[4] = {v[0], v[1], v[2], v[3]}, r[4] = {0.f, 0.f, 0.f, 0.f};
+                    if (ep.bias) {
+                        const float4 b4 = ld4(ep.bias + col, nv, true);
+                        z[0] += b4.x;
+                        z[1] += b4.y;
+                        z[2] += b4.z;
+                        z[3] += b4.w;
+                    }
+                    if (ep.Z) st4(ep.Z + off, z, nv, vec);
+                    if (ep.residual) {
+                        const float4 r4 = ld4(ep.residual + off, nv, vec);
+                        r[0] = r4.x;
+                        r[1] = r4.y;
+                        r[2] = r4.z;
+                        r[3] = r4.w;
+                    }
+                    with_act(ep.act, [&](auto act) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) z[j] = act_value<act.value, false>(z[j]);
+                    });
+                    if (ep.residual) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) z[j] += r[j];
+                    }
+                    st4(ep.Y + off, z, nv, vec);
+                } else if constexpr (std::is_same_v<Epi, SEpiSlope>) {
+                    const long long off = row * ep.ld + col;
+                    const bool vec = (ep.ld & 3) == 0;
+                    float o[4] = {v[0], v[1], v[2], v[3]};
+                    if (ep.z_in) {
+                        const float4 z4 = ld4(ep.z_in + off, nv, vec);
+                        const float z[4] = {z4.x, z4.y, z4.z, z4.w};
+                        with_act(ep.act, [&](auto act) {
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) o[j] *= act_slope<act.value, false>(z[j]);
+                        });
+                    }
+                    st4(ep.dX + off, o, nv, vec);
                 } else {
                     const long long off = row * ep.ld + col;
                     const bool vec = (ep.ld & 3) == 0;
@@ -489,6 +545,21 @@ cudaError_t launch_swiglu_f32(int T, int d, int d_ff, const float* g, const floa
     // e[t, f] = sum_j g[t, j] W3[j, f]: A(m=t, k=j) = g[t*d + j], B(n=f, k=j) = W3[j*d_ff + f]
     SEpiSwiglu ep{dA, dB, a, b, d_ff};
     return run<true, false>(ops_of(g, d, W3, d_ff, T, d_ff, d, T), ep, 1, st);
+}
+
+cudaError_t launch_linear_f32(const LinearFwd& p, cudaStream_t st) {
+    const SEpiLinear ep{static_cast<const float*>(p.bias), static_cast<const float*>(p.residual),
+                        static_cast<float*>(p.Y), static_cast<float*>(p.Z), p.N, p.act};
+    return run<true, true>(ops_of(static_cast<const float*>(p.X), p.K,
+                                  static_cast<const float*>(p.W), p.K, p.T, p.N, p.K, p.T),
+                           ep, 1, st);
+}
+
+cudaError_t launch_linear_dx_f32(int T, int N, int K, const float* dZ, const float* W,
+                                 const float* Z_in, int act_in, float* dX, cudaStream_t st) {
+    // dX[t, i] = sum_o dZ[t, o] W[o, i]
+    const SEpiSlope ep{Z_in, dX, K, act_in};
+    return run<true, false>(ops_of(dZ, N, W, K, T, K, N, T), ep, 1, st);
 }
 
 cudaError_t launch_update_f32(int n, int T, int d, int d_ff, const float* const* g,
