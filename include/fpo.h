@@ -429,9 +429,9 @@ typedef enum fpo_activation {
     FPO_ACT_SILU = 4
 } fpo_activation;
 
-/* Bytes of workspace fpo_linear needs on the current device (0 on invalid sizes): 256, for at
- * most 128 tokens in bf16 up to 152 kB more per padded token (16, 32, 64 or 128), for larger bf16
- * batches whose tiles leave a wave partly empty up to 60 MB for the parts of split tiles. */
+/* Bytes of workspace fpo_linear needs on the current device (0 on invalid sizes): 256, for 5 to 32
+ * tokens in bf16 up to 160 kB more per padded token (16 or 32), for larger bf16 batches whose tiles
+ * leave a wave partly empty up to 60 MB for the parts of split tiles. */
 size_t fpo_linear_workspace(int64_t T, int64_t d_out, int64_t d_in, int32_t dtype);
 
 /*
@@ -515,7 +515,7 @@ typedef struct fpo_adamw_tensor {
 typedef struct fpo_adamw_desc {
     double lr;
     double beta1, beta2;   /* moment decays in [0, 1) (0.9, 0.999)              */
-    double eps;            /* 1e-8                                              */
+    double eps;            /* >= 0 (1e-8); below 2^-63 it counts as 2^-63       */
     double clip_frac;      /* relative clip bound (0.01)                        */
     int64_t step;          /* step index t >= 1, for the bias corrections       */
     int32_t clip;          /* fpo_clip_mode, of each tensor by itself           */
@@ -528,7 +528,7 @@ size_t fpo_adamw_workspace(int32_t n_tensors, const int64_t* n, int32_t clip);
 /*
  * fpo_adamw_grouped -- the AdamW step of fpo_layer_optimize_grouped (Sec. 3.1) on many tensors of
  * any sizes with given gradients: a model's matrices, biases and norm weights together, one launch
- * per 128 tensors (three with a clip).
+ * per 128 tensors with one kind of moments (three with a clip).
  *   m <- beta1 m + (1 - beta1) G,  v <- beta2 v + (1 - beta2) G G
  *   step = -lr (m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps) + weight_decay W)
  *   W_master += s step,  W_out = W_master rounded

@@ -13,6 +13,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
+import struct
 
 import torch
 
@@ -124,6 +125,10 @@ class AdamwTensor(ctypes.Structure):
     _fields_ = [("n", _i64), ("G", _vp), ("W_master", _vp), ("W_out", _vp), ("state1", _vp),
                 ("state2", _vp), ("scale1", _vp), ("scale2", _vp), ("g_dtype", _i32),
                 ("w_dtype", _i32), ("state_bits", _i32), ("weight_decay", _f32)]
+
+
+_ADAMW_TENSOR = struct.Struct("@q7Piiif")  # the same, packed
+assert _ADAMW_TENSOR.size == ctypes.sizeof(AdamwTensor)
 
 
 class AdamwDesc(ctypes.Structure):
@@ -273,6 +278,16 @@ def _ptr(t):
     if not t.is_contiguous():
         raise ValueError("libfpo takes contiguous tensors")
     return t.data_ptr()
+
+
+def _ptrs(ts):
+    """_ptr of a list (0 for None), on the current device."""
+    here = _current_device()
+    for t in ts:
+        if t is not None and (t.get_device() != here or not t.is_contiguous()):
+            _on_current_device(t)
+            _ptr(t)
+    return [0 if t is None else t.data_ptr() for t in ts]
 
 
 # torch's private call for a stream's handle, where this torch has it
@@ -740,18 +755,23 @@ def adamw_grouped(Gs, opt, W_masters, states1, states2, *, scales1=None, scales2
     scales1, scales2, W_outs = scales1 or none, scales2 or none, W_outs or none
 
     def check(name, ts, counts, types):
-        for t, c, want in zip(ts, counts, types):
-            if t is not None and (t.dtype != want or t.numel() != c):
-                raise ValueError(f"{name}: expected {c} elements of {want}, got {t.numel()} of {t.dtype}")
+        if [t.numel() for t in ts] != counts or [t.dtype for t in ts] != types:
+            for t, c, want in zip(ts, counts, types):
+                if t.dtype != want or t.numel() != c:
+                    raise ValueError(f"{name}: expected {c} elements of {want}, got {t.numel()} of {t.dtype}")
+
+    def given(ts, xs):
+        return [x for t, x in zip(ts, xs) if t is not None]
 
     f32 = [torch.float32] * n
     check("W_masters", W_masters, sizes, f32)
     check("states1", states1, sizes, [torch.float8_e4m3fn if s else torch.float32 for s in small])
     check("states2", states2, sizes, [torch.uint8 if s else torch.float32 for s in small])
-    check("W_outs", W_outs, sizes, [t if t is None else t.dtype for t in W_outs])
+    outs = given(W_outs, W_outs)
+    check("W_outs", outs, given(W_outs, sizes), [t.dtype for t in outs])
     blocks = [-(-c // ADAMW_BLOCK) for c in sizes]
-    check("scales1", scales1, blocks, f32)
-    check("scales2", scales2, blocks, f32)
+    check("scales1", given(scales1, scales1), given(scales1, blocks), given(scales1, f32))
+    check("scales2", given(scales2, scales2), given(scales2, blocks), given(scales2, f32))
     if any(s and (a is None or b is None) for s, a, b in zip(small, scales1, scales2)):
         raise ValueError("8-bit states need scales1 and scales2")
     if opt.kind != OPT_ADAMW:
@@ -765,17 +785,14 @@ def adamw_grouped(Gs, opt, W_masters, states1, states2, *, scales1=None, scales2
     desc = AdamwDesc(rate("lr"), rate("beta1"), rate("beta2"), rate("eps", "adam_eps"), rate("clip_frac"),
                      opt.step, opt.clip)
     g_types = [_dtype_code(G) for G in Gs]
-    w_types = [F32 if t is None else _dtype_code(t) for t in W_outs]
+    w_types = [F32 if t is None else BF16 if t.dtype == torch.bfloat16 else _dtype_code(t) for t in W_outs]
     decays = [rate("weight_decay")] * n if weight_decays is None else [float(w) for w in weight_decays]
-    for ts in (W_masters, states1, states2):
-        for t in ts:
-            _on_current_device(t)
-    cols = [[_ptr(t) for t in ts] for ts in (Gs, W_masters, W_outs, states1, states2, scales1, scales2)]
-    table = (AdamwTensor * n)(*zip(sizes, *cols, g_types, w_types, [8 if s else 32 for s in small],
-                                   decays))
+    cols = [_ptrs(ts) for ts in (Gs, W_masters, W_outs, states1, states2, scales1, scales2)]
+    table = b"".join(map(_ADAMW_TENSOR.pack, sizes, *cols, g_types, w_types,
+                         [8 if s else 32 for s in small], decays))
     if workspace is None and opt.clip != CLIP_NONE:
         workspace = _workspace(adamw_workspace(sizes, opt.clip), Gs[0].device, stream)
-    rc = _lib.fpo_adamw_grouped(n, table, ctypes.byref(desc), int(seed) & 0xffffffffffffffff,
+    rc = _lib.fpo_adamw_grouped(n, ctypes.cast(table, ctypes.POINTER(AdamwTensor)), ctypes.byref(desc), int(seed) & 0xffffffffffffffff,
                                 _ptr(workspace), 0 if workspace is None else _nbytes(workspace),
                                 _stream(stream))
     _check(rc, "fpo_adamw_grouped")

@@ -2,9 +2,13 @@
 // matrices: biases, norm weights, any matrix with a given gradient), the moments in fp32 or in
 // 8 bits, with the relative clip of App. A per tensor.
 //
-// A tensor is cut into chunks of 2048 elements, 8 per thread of a block; the blocks walk the
-// chunks of all tensors, and a chunk's tensor is found from the table of first chunks in the
-// launch's parameters.  Without a clip that is one launch.  With one, a first pass leaves
+// A tensor is cut into chunks, 128 elements per warp of a block and quad of a lane (so that every
+// access of a warp is whole lines): 4 quads with fp32 moments, whose traffic wants the loads in
+// flight, 2 with 8-bit ones, whose arithmetic wants the warps.  A block takes one chunk of any
+// tensor, found from the table of first chunks in the launch's parameters.  Blocks that stay and
+// walk the chunks were slower, their warps in step with one another between loading and storing
+// (90M elements, bf16 gradients, us: fp32 moments 361, resident blocks 395, with 2 quads 445;
+// 8-bit 262, 265, with 4 quads 299).  Without a clip that is one launch.  With one, a first pass leaves
 // (||W||^2, ||x||^2) of every chunk, x the step or the gradient, a second adds them per tensor
 // in a fixed order, and the third takes the step scaled.
 //
@@ -25,6 +29,7 @@
 //
 // Bound: HBM.
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 #include <cuda_runtime.h>
 #include <math.h>
 
@@ -34,9 +39,16 @@ namespace fpo {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kPer = 8;                        // elements per thread
-constexpr int kChunk = kThreads * kPer;        // elements of a block's turn
-static_assert(kAdamBlock == 32 * kPer, "a warp's share has one scale");
+// Quads of a lane, elements of a thread, a warp and a block's turn.  Element 4 q + i of a lane is
+// 128 q + 4 lane + i of its warp's.
+template <bool kState8>
+struct Share {
+    static constexpr int kQuads = kState8 ? 2 : 4;
+    static constexpr int kPer = 4 * kQuads;
+    static constexpr int kWarp = 32 * kPer;
+    static constexpr int kChunk = kThreads / 32 * kWarp;
+};
+static_assert(Share<true>::kWarp == kAdamBlock, "a warp's share has one scale");
 
 // Odd words for the rounding bits: fractions of the golden ratio, sqrt(2) and sqrt(3).
 constexpr uint32_t kPhi = 0x9E3779B9u, kSqrt2 = 0x6A09E667u, kSqrt3 = 0xBB67AE85u;
@@ -47,8 +59,8 @@ __host__ __device__ __forceinline__ uint32_t mix(uint32_t h) {
     return h ^ (h >> 16);
 }
 
-// The tensors of one launch.  Flags: g and W_out in bf16, moments in 8 bits.
-enum : uint8_t { kG16 = 1, kOut16 = 2, kState8 = 4 };
+// The tensors of one launch.  Flags: g and W_out in bf16.
+enum : uint8_t { kG16 = 1, kOut16 = 2 };
 template <int CAP>
 struct Table {
     const void* g[CAP];
@@ -74,71 +86,70 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
     return *reinterpret_cast<const uint32_t*>(&p);
 }
 
-// 8 elements from i (a multiple of 8) of an array, those from n on as zeros.
-__device__ __forceinline__ void load8(const float* p, long long i, long long n, float (&x)[kPer]) {
-    if (i + kPer <= n) {
+// Four elements from i (a multiple of 4) of an array; not kFull: those from n on are zeros, and
+// stay as they are.
+template <bool kFull>
+__device__ __forceinline__ void load4(const float* p, long long i, long long n, float* x) {
+    if (kFull || i + 4 <= n) {
         const float4 a = *reinterpret_cast<const float4*>(p + i);
-        const float4 b = *reinterpret_cast<const float4*>(p + i + 4);
         x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-        x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
     } else {
 #pragma unroll
-        for (int k = 0; k < kPer; ++k) x[k] = i + k < n ? p[i + k] : 0.f;
+        for (int k = 0; k < 4; ++k) x[k] = i + k < n ? p[i + k] : 0.f;
     }
 }
-__device__ __forceinline__ void load8(const __nv_bfloat16* p, long long i, long long n,
-                                      float (&x)[kPer]) {
-    if (i + kPer <= n) {
-        const uint4 u = *reinterpret_cast<const uint4*>(p + i);
-        const float2 a = unpack_bf16x2(u.x), b = unpack_bf16x2(u.y), c = unpack_bf16x2(u.z),
-                     d = unpack_bf16x2(u.w);
+template <bool kFull>
+__device__ __forceinline__ void load4(const __nv_bfloat16* p, long long i, long long n, float* x) {
+    if (kFull || i + 4 <= n) {
+        const uint2 u = *reinterpret_cast<const uint2*>(p + i);
+        const float2 a = unpack_bf16x2(u.x), b = unpack_bf16x2(u.y);
         x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y;
-        x[4] = c.x; x[5] = c.y; x[6] = d.x; x[7] = d.y;
     } else {
 #pragma unroll
-        for (int k = 0; k < kPer; ++k) x[k] = i + k < n ? __bfloat162float(p[i + k]) : 0.f;
+        for (int k = 0; k < 4; ++k) x[k] = i + k < n ? __bfloat162float(p[i + k]) : 0.f;
     }
 }
-__device__ __forceinline__ void store8(float* p, long long i, long long n, const float (&x)[kPer]) {
-    if (i + kPer <= n) {
+template <bool kFull>
+__device__ __forceinline__ void store4(float* p, long long i, long long n, const float* x) {
+    if (kFull || i + 4 <= n) {
         *reinterpret_cast<float4*>(p + i) = make_float4(x[0], x[1], x[2], x[3]);
-        *reinterpret_cast<float4*>(p + i + 4) = make_float4(x[4], x[5], x[6], x[7]);
     } else {
 #pragma unroll
-        for (int k = 0; k < kPer; ++k)
+        for (int k = 0; k < 4; ++k)
             if (i + k < n) p[i + k] = x[k];
     }
 }
-__device__ __forceinline__ void store8(__nv_bfloat16* p, long long i, long long n,
-                                       const float (&x)[kPer]) {
-    if (i + kPer <= n) {
-        *reinterpret_cast<uint4*>(p + i) =
-            make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
-                       pack_bf16x2(x[6], x[7]));
+template <bool kFull>
+__device__ __forceinline__ void store4(__nv_bfloat16* p, long long i, long long n, const float* x) {
+    if (kFull || i + 4 <= n) {
+        *reinterpret_cast<uint2*>(p + i) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
     } else {
 #pragma unroll
-        for (int k = 0; k < kPer; ++k)
+        for (int k = 0; k < 4; ++k)
             if (i + k < n) p[i + k] = __float2bfloat16_rn(x[k]);
     }
 }
-__device__ __forceinline__ uint2 load_codes(const uint8_t* p, long long i, long long n) {
-    if (i + kPer <= n) return *reinterpret_cast<const uint2*>(p + i);
-    uint32_t w[2] = {0u, 0u};
+template <bool kFull>
+__device__ __forceinline__ uint32_t load_codes(const uint8_t* p, long long i, long long n) {
+    if (kFull || i + 4 <= n) return *reinterpret_cast<const uint32_t*>(p + i);
+    uint32_t w = 0u;
 #pragma unroll
-    for (int k = 0; k < kPer; ++k)
-        if (i + k < n) w[k / 4] |= static_cast<uint32_t>(p[i + k]) << (8 * (k % 4));
-    return make_uint2(w[0], w[1]);
+    for (int k = 0; k < 4; ++k)
+        if (i + k < n) w |= static_cast<uint32_t>(p[i + k]) << (8 * k);
+    return w;
 }
-__device__ __forceinline__ void store_codes(uint8_t* p, long long i, long long n, uint2 c) {
-    if (i + kPer <= n) {
-        *reinterpret_cast<uint2*>(p + i) = c;
+template <bool kFull>
+__device__ __forceinline__ void store_codes(uint8_t* p, long long i, long long n, uint32_t c) {
+    if (kFull || i + 4 <= n) {
+        *reinterpret_cast<uint32_t*>(p + i) = c;
         return;
     }
-    const uint32_t w[2] = {c.x, c.y};
 #pragma unroll
-    for (int k = 0; k < kPer; ++k)
-        if (i + k < n) p[i + k] = static_cast<uint8_t>(w[k / 4] >> (8 * (k % 4)));
+    for (int k = 0; k < 4; ++k)
+        if (i + k < n) p[i + k] = static_cast<uint8_t>(c >> (8 * k));
 }
+
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 
 // The two formats: exponent at the block's maximum, factor to fp32's subnormal range and back.
 template <bool kSigned>
@@ -147,11 +158,6 @@ struct Format {
     static constexpr uint32_t kDown = (127u - (kSigned ? 120u : 111u)) << 23;  // 2^-120, 2^-111
     static constexpr uint32_t kUp = (127u + (kSigned ? 120u : 111u)) << 23;
 
-    static __device__ __forceinline__ float value(uint32_t code, float scale) {
-        const uint32_t mag = kSigned ? (code & 0x7fu) << 20 : code << 20;
-        const float x = __uint_as_float(mag) * __uint_as_float(kUp) * scale;
-        return kSigned ? __uint_as_float(__float_as_uint(x) | ((code & 0x80u) << 24)) : x;
-    }
     // The scale of a block from the bits of its largest magnitude, at least 2^-100 (of a block
     // of zeros too); NaN where that is an infinity or a NaN.
     static __device__ __forceinline__ float scale(uint32_t amax) {
@@ -159,69 +165,148 @@ struct Format {
         if (e == 255u) return __uint_as_float(0x7fffffffu);
         return __uint_as_float(((e > 27u ? e : 27u) - kTop) << 23);
     }
-    static __device__ __forceinline__ uint32_t code(float x, float inv_scale, uint32_t u16) {
-        const float y = fabsf(x) * inv_scale * __uint_as_float(kDown);
-        uint32_t c = ((__float_as_uint(y) + (u16 << 4)) >> 20) & 0xffu;
-        if (kSigned) return c | ((__float_as_uint(x) >> 24) & 0x80u);
-        return x > 0.f && c == 0u ? 1u : c;
-    }
 };
 
+// The values of four codes (m by the hardware's conversion of e4m3 to fp16, which is exact).
 template <bool kSigned>
-__device__ __forceinline__ void from_codes(uint2 c, float scale, float (&x)[kPer]) {
+__device__ __forceinline__ void from_codes(uint32_t c, float scale, float* x) {
 #pragma unroll
-    for (int k = 0; k < kPer; ++k)
-        x[k] = Format<kSigned>::value(((k < 4 ? c.x : c.y) >> (8 * (k % 4))) & 0xffu, scale);
+    for (int k = 0; k < 4; k += 2) {
+        float2 v;
+        if constexpr (kSigned) {
+            uint32_t h;
+            asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\t}"
+                : "=r"(h)
+                : "r"(c >> (8 * k)));
+            v = __half22float2(*reinterpret_cast<const __half2*>(&h));
+        } else {
+            const uint32_t a = k == 0 ? c << 20 : c << 4, b = k == 0 ? c << 12 : c >> 4;
+            v = __fmul2_rn(make_float2(__uint_as_float(a & 0x0ff00000u), __uint_as_float(b & 0x0ff00000u)),
+                           both(__uint_as_float(Format<false>::kUp)));
+        }
+        v = __fmul2_rn(v, both(scale));  // (2^111 and the scale apart: their product may be out of range)
+        x[k] = v.x;
+        x[k + 1] = v.y;
+    }
 }
 
-// Codes of a warp's 256 values; returns the block's scale.  r: 32 random bits per element, m
-// takes the upper half and v the lower.
+// max(|a|, |b|), NaN where either is.
+__device__ __forceinline__ float max_abs(float a, float b) {
+    float m;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(fabsf(a)), "f"(fabsf(b)));
+    return m;
+}
+
+// Codes of a warp's block of 256 values, eight per lane (x, and 32 random bits r of each: m takes
+// the upper half, v the lower); returns the block's scale.
 template <bool kSigned>
-__device__ __forceinline__ float to_codes(const float (&x)[kPer], const uint32_t (&r)[kPer],
-                                          uint2& c) {
-    uint32_t amax = 0u;
+__device__ __forceinline__ float to_codes(const float* x, const uint32_t* r, uint32_t (&c)[2]) {
+    float top = max_abs(x[0], x[1]);
 #pragma unroll
-    for (int k = 0; k < kPer; ++k) amax = max(amax, __float_as_uint(x[k]) & 0x7fffffffu);
-    amax = __reduce_max_sync(0xffffffffu, amax);
-    const float scale = Format<kSigned>::scale(amax);
+    for (int k = 2; k < 8; ++k) top = max_abs(top, x[k]);
+    const float scale =
+        Format<kSigned>::scale(__reduce_max_sync(0xffffffffu, __float_as_uint(top) & 0x7fffffffu));
     // of a power of two, exact
     const float inv = __uint_as_float((254u << 23) - __float_as_uint(scale));
-    uint32_t w[2] = {0u, 0u};
+    uint32_t code[8];
 #pragma unroll
-    for (int k = 0; k < kPer; ++k) {
-        const uint32_t u = kSigned ? r[k] >> 16 : r[k] & 0xffffu;
-        w[k / 4] |= Format<kSigned>::code(x[k], inv, u) << (8 * (k % 4));
+    for (int k = 0; k < 8; k += 2) {
+        float2 y = __fmul2_rn(make_float2(x[k], x[k + 1]), both(inv));
+        y = __fmul2_rn(y, both(__uint_as_float(Format<kSigned>::kDown)));
+        const uint32_t b[2] = {__float_as_uint(y.x), __float_as_uint(y.y)};
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t u = kSigned ? r[k + i] >> 16 : r[k + i] & 0xffffu;
+            const uint32_t t = b[i] + (u << 4);  // (a sign stays: bits 27 to 30 are 0)
+            if (kSigned)
+                code[k + i] = (t >> 20) | ((t >> 24) & 0x80u);  // (its byte is what counts)
+            else
+                code[k + i] = x[k + i] > 0.f ? max(t >> 20, 1u) : t >> 20;
+        }
     }
-    c = make_uint2(w[0], w[1]);
+#pragma unroll
+    for (int k = 0; k < 2; ++k)  // their low bytes
+        c[k] = __byte_perm(__byte_perm(code[4 * k], code[4 * k + 1], 0x0040),
+                           __byte_perm(code[4 * k + 2], code[4 * k + 3], 0x0040), 0x5410);
     return scale;
 }
 
-// New moments and the unclipped step of one element.  The moments' products and sums are rounded
-// one by one (no FMA): an 8-bit code next to a border would otherwise depend on how the compiler
-// joins them.
-__device__ __forceinline__ float adamw_step(const AdamRates& op, float wd, float g, float w,
-                                            float& m, float& v) {
-    m = __fadd_rn(__fmul_rn(op.b1, m), __fmul_rn(op.a1, g));
-    v = __fadd_rn(__fmul_rn(op.b2, v), __fmul_rn(__fmul_rn(op.a2, g), g));
-    const float denom = sqrtf(v) * op.inv_sqrt_bc2 + op.eps;
-    return -op.lr * (m * op.inv_bc1 / denom + wd * w);
+__device__ __forceinline__ float sqrt_approx(float x) {
+    float y;
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float rcp_approx(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
 
-// What a pass does with a chunk: the clip's sums (kNorms, of the step where op.clip is 1, else
-// of the gradient) or the step itself.
-template <bool kNorms, bool kState8>
-__device__ __forceinline__ void chunk(const AdamRates& op, float wd, uint32_t key, bool g16,
-                                      bool out16, const void* g_, float* w_, void* wo_, void* m_,
-                                      void* v_, float* ms_, float* vs_, long long i, long long n,
-                                      float gscale, float sscale, float& ww, float& xx) {
+// New moments and the unclipped steps of a thread's elements.  The moments' products and sums are
+// rounded one by one (no FMA): an 8-bit code next to a border would otherwise depend on how the
+// compiler joins them.  Square root and reciprocal are the MUFU's, within 2^-22 of the step, which
+// is itself some 2^-10 of a weight.
+template <int kPer>
+__device__ __forceinline__ void adamw_step(const AdamRates& op, float wd, float gscale,
+                                           const float (&g)[kPer], const float (&w)[kPer],
+                                           float (&m)[kPer], float (&v)[kPer], float (&d)[kPer]) {
+#pragma unroll
+    for (int k = 0; k < kPer; k += 2) {
+        const float2 g2 = __fmul2_rn(make_float2(g[k], g[k + 1]), both(gscale));
+        const float2 m2 = __fadd2_rn(__fmul2_rn(both(op.b1), make_float2(m[k], m[k + 1])),
+                                     __fmul2_rn(both(op.a1), g2));
+        const float2 v2 = __fadd2_rn(__fmul2_rn(both(op.b2), make_float2(v[k], v[k + 1])),
+                                     __fmul2_rn(__fmul2_rn(both(op.a2), g2), g2));
+        m[k] = m2.x;
+        m[k + 1] = m2.y;
+        v[k] = v2.x;
+        v[k + 1] = v2.y;
+        const float2 den = __ffma2_rn(make_float2(sqrt_approx(v2.x), sqrt_approx(v2.y)),
+                                      both(op.inv_sqrt_bc2), both(op.eps));
+        const float2 q = __fmul2_rn(__fmul2_rn(m2, both(op.inv_bc1)),
+                                    make_float2(rcp_approx(den.x), rcp_approx(den.y)));
+        const float2 s = __fmul2_rn(__ffma2_rn(both(wd), make_float2(w[k], w[k + 1]), q), both(-op.lr));
+        d[k] = s.x;
+        d[k + 1] = s.y;
+    }
+}
+
+// One tensor's entry of the table.
+struct Entry {
+    const void* g;
+    float* w;
+    void* wo;
+    void* m;
+    void* v;
+    float* ms;
+    float* vs;
+    long long n;
+    uint32_t key;
+    float wd;
+    bool g16, out16;
+};
+
+// What a pass does with a warp's elements from i0: the clip's sums (kNorms, of the step where
+// op.clip is 1, else of the gradient) or the step itself.  kFull: all of them are there; else the
+// first at least is.
+template <bool kNorms, bool kState8, bool kFull>
+__device__ __forceinline__ void take(const AdamRates& op, const Entry& e, long long i0, float gscale,
+                                     float sscale, float& ww, float& xx) {
+    constexpr int kQuads = Share<kState8>::kQuads, kPer = Share<kState8>::kPer;
     float g[kPer], w[kPer], m[kPer], v[kPer];
-    const long long block = i / kAdamBlock;
-    const bool any = block * kAdamBlock < n;  // of the warp's 256 elements
-    if (g16)
-        load8(static_cast<const __nv_bfloat16*>(g_), i, n, g);
-    else
-        load8(static_cast<const float*>(g_), i, n, g);
-    load8(w_, i, n, w);
+    const int lane = threadIdx.x & 31;
+    const long long n = e.n, i1 = i0 + 4 * lane;
+    if (e.g16) {
+#pragma unroll
+        for (int q = 0; q < kQuads; ++q)
+            load4<kFull>(static_cast<const __nv_bfloat16*>(e.g), i1 + 128 * q, n, g + 4 * q);
+    } else {
+#pragma unroll
+        for (int q = 0; q < kQuads; ++q)
+            load4<kFull>(static_cast<const float*>(e.g), i1 + 128 * q, n, g + 4 * q);
+    }
+#pragma unroll
+    for (int q = 0; q < kQuads; ++q) load4<kFull>(e.w, i1 + 128 * q, n, w + 4 * q);
     if (kNorms && op.clip == 2) {  // the gradient's norm needs no state
 #pragma unroll
         for (int k = 0; k < kPer; ++k) {
@@ -230,56 +315,78 @@ __device__ __forceinline__ void chunk(const AdamRates& op, float wd, uint32_t ke
         }
         return;
     }
+    const long long block = i0 / kAdamBlock;
     if constexpr (kState8) {
-        const uint2 mc = load_codes(static_cast<const uint8_t*>(m_), i, n);
-        const uint2 vc = load_codes(static_cast<const uint8_t*>(v_), i, n);
-        from_codes<true>(mc, any ? ms_[block] : 0.f, m);
-        from_codes<false>(vc, any ? vs_[block] : 0.f, v);
+        const float msc = e.ms[block], vsc = e.vs[block];
+        uint32_t mc[kQuads], vc[kQuads];
+#pragma unroll
+        for (int q = 0; q < kQuads; ++q) {
+            mc[q] = load_codes<kFull>(static_cast<const uint8_t*>(e.m), i1 + 128 * q, n);
+            vc[q] = load_codes<kFull>(static_cast<const uint8_t*>(e.v), i1 + 128 * q, n);
+        }
+#pragma unroll
+        for (int q = 0; q < kQuads; ++q) {
+            from_codes<true>(mc[q], msc, m + 4 * q);
+            from_codes<false>(vc[q], vsc, v + 4 * q);
+        }
     } else {
-        load8(static_cast<const float*>(m_), i, n, m);
-        load8(static_cast<const float*>(v_), i, n, v);
-    }
 #pragma unroll
-    for (int k = 0; k < kPer; ++k) {
-        const float st = adamw_step(op, wd, gscale * g[k], w[k], m[k], v[k]);
-        if constexpr (kNorms) {
-            const float d = i + k < n ? st : 0.f;
+        for (int q = 0; q < kQuads; ++q) {
+            load4<kFull>(static_cast<const float*>(e.m), i1 + 128 * q, n, m + 4 * q);
+            load4<kFull>(static_cast<const float*>(e.v), i1 + 128 * q, n, v + 4 * q);
+        }
+    }
+    float d[kPer];
+    adamw_step(op, e.wd, gscale, g, w, m, v, d);
+    if constexpr (kNorms) {
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {
+            // (no element: eps 0 would divide by 0)
+            if (!kFull && i1 + 128 * (k / 4) + k % 4 >= n) d[k] = 0.f;
             ww = fmaf(w[k], w[k], ww);
-            xx = fmaf(d, d, xx);
-        } else {
-            w[k] = fmaf(sscale, st, w[k]);
+            xx = fmaf(d[k], d[k], xx);
+        }
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) w[k] = fmaf(sscale, d[k], w[k]);
+#pragma unroll
+    for (int q = 0; q < kQuads; ++q) store4<kFull>(e.w, i1 + 128 * q, n, w + 4 * q);
+    if (e.wo) {
+#pragma unroll
+        for (int q = 0; q < kQuads; ++q) {
+            if (e.out16)
+                store4<kFull>(static_cast<__nv_bfloat16*>(e.wo), i1 + 128 * q, n, w + 4 * q);
+            else
+                store4<kFull>(static_cast<float*>(e.wo), i1 + 128 * q, n, w + 4 * q);
         }
     }
-    if constexpr (!kNorms) {
-        store8(w_, i, n, w);
-        if (wo_) {
-            if (out16)
-                store8(static_cast<__nv_bfloat16*>(wo_), i, n, w);
-            else
-                store8(static_cast<float*>(wo_), i, n, w);
-        }
-        if constexpr (kState8) {
-            const uint32_t lane = threadIdx.x & 31u;
-            uint32_t h = mix(key ^ static_cast<uint32_t>(block)) + lane * kPer * kPhi;
-            uint32_t r[kPer];
+    if constexpr (kState8) {
+        const uint32_t h0 = mix(e.key ^ static_cast<uint32_t>(block)) + 4u * lane * kPhi;
+        uint32_t r[kPer];
 #pragma unroll
-            for (int k = 0; k < kPer; ++k, h += kPhi) {
-                r[k] = (h ^ (h >> 15)) * kSqrt2;
-                r[k] ^= r[k] >> 16;
-            }
-            uint2 mc, vc;
-            const float msc = to_codes<true>(m, r, mc);
-            const float vsc = to_codes<false>(v, r, vc);
-            if (!any) return;
-            store_codes(static_cast<uint8_t*>(m_), i, n, mc);
-            store_codes(static_cast<uint8_t*>(v_), i, n, vc);
-            if (lane == 0) {
-                ms_[block] = msc;
-                vs_[block] = vsc;
-            }
-        } else {
-            store8(static_cast<float*>(m_), i, n, m);
-            store8(static_cast<float*>(v_), i, n, v);
+        for (int k = 0; k < kPer; ++k) {
+            const uint32_t h = h0 + (128u * (k / 4) + k % 4) * kPhi;
+            r[k] = (h ^ (h >> 15)) * kSqrt2;
+            r[k] ^= r[k] >> 16;
+        }
+        uint32_t mc[kQuads], vc[kQuads];
+        const float msc = to_codes<true>(m, r, mc);
+        const float vsc = to_codes<false>(v, r, vc);
+#pragma unroll
+        for (int q = 0; q < kQuads; ++q) {
+            store_codes<kFull>(static_cast<uint8_t*>(e.m), i1 + 128 * q, n, mc[q]);
+            store_codes<kFull>(static_cast<uint8_t*>(e.v), i1 + 128 * q, n, vc[q]);
+        }
+        if (lane == 0) {
+            e.ms[block] = msc;
+            e.vs[block] = vsc;
+        }
+    } else {
+#pragma unroll
+        for (int q = 0; q < kQuads; ++q) {
+            store4<kFull>(static_cast<float*>(e.m), i1 + 128 * q, n, m + 4 * q);
+            store4<kFull>(static_cast<float*>(e.v), i1 + 128 * q, n, v + 4 * q);
         }
     }
 }
@@ -291,49 +398,46 @@ __device__ __forceinline__ float warp_sum(float x) {
 }
 
 // kNorms: part[chunk] = the chunk's two sums.  Else scales[tensor] (null: 1) clips the step.
-template <int CAP, bool kNorms>
-__global__ void __launch_bounds__(kThreads)
+template <int CAP, bool kNorms, bool kState8>
+__global__ void __launch_bounds__(kThreads, kNorms ? (kState8 ? 5 : 3) : (kState8 ? 4 : 2))
     adamw_kernel(const __grid_constant__ Table<CAP> t, const __grid_constant__ AdamRates op,
                  float2* __restrict__ part, const float* __restrict__ scales) {
-    const int total = t.first[t.count];
-    int k = 0;
-    for (int c = blockIdx.x; c < total; c += gridDim.x) {
-        // the chunk's tensor: the last whose first chunk is not behind it (some have none)
-        int hi = t.count;
-        while (hi - k > 1) {
-            const int mid = (k + hi) / 2;
-            if (t.first[mid] <= c)
-                k = mid;
-            else
-                hi = mid;
-        }
-        const long long i = static_cast<long long>(c - t.first[k]) * kChunk + threadIdx.x * kPer;
-        const uint8_t f = t.flags[k];
-        const float sc = scales ? scales[k] : 1.f;
-        const float gscale = op.clip == 2 ? sc : 1.f, sscale = op.clip == 1 ? sc : 1.f;
-        float ww = 0.f, xx = 0.f;
-        if (f & kState8)
-            chunk<kNorms, true>(op, t.wd[k], t.key[k], f & kG16, f & kOut16, t.g[k], t.w[k], t.wo[k],
-                                t.m[k], t.v[k], t.ms[k], t.vs[k], i, t.n[k], gscale, sscale, ww, xx);
+    using S = Share<kState8>;
+    const int warp = threadIdx.x / 32;
+    // behind a norms pass from the end: what that pass read last is still in L2
+    const int c = !kNorms && scales ? gridDim.x - 1 - blockIdx.x : blockIdx.x;
+    int k = 0, hi = t.count;  // the chunk's tensor: the last whose first chunk is not behind it
+    while (hi - k > 1) {
+        const int mid = (k + hi) / 2;
+        if (t.first[mid] <= c)
+            k = mid;
         else
-            chunk<kNorms, false>(op, t.wd[k], t.key[k], f & kG16, f & kOut16, t.g[k], t.w[k],
-                                 t.wo[k], t.m[k], t.v[k], t.ms[k], t.vs[k], i, t.n[k], gscale,
-                                 sscale, ww, xx);
-        if constexpr (kNorms) {
-            __shared__ float2 sh[kThreads / 32];
-            ww = warp_sum(ww);
-            xx = warp_sum(xx);
-            __syncthreads();  // the chunk before is read
-            if ((threadIdx.x & 31) == 0) sh[threadIdx.x / 32] = make_float2(ww, xx);
-            __syncthreads();
-            if (threadIdx.x == 0) {
-                float2 s = sh[0];
-                for (int q = 1; q < kThreads / 32; ++q) {
-                    s.x += sh[q].x;
-                    s.y += sh[q].y;
-                }
-                part[c] = s;
+            hi = mid;
+    }
+    const Entry e{t.g[k],  t.w[k], t.wo[k],  t.m[k],  t.v[k], t.ms[k],
+                  t.vs[k], t.n[k], t.key[k], t.wd[k], (t.flags[k] & kG16) != 0,
+                  (t.flags[k] & kOut16) != 0};
+    const long long i0 = static_cast<long long>(c - t.first[k]) * S::kChunk + warp * S::kWarp;
+    const float sc = scales ? scales[k] : 1.f;
+    const float gscale = op.clip == 2 ? sc : 1.f, sscale = op.clip == 1 ? sc : 1.f;
+    float ww = 0.f, xx = 0.f;
+    if (i0 + S::kWarp <= e.n)
+        take<kNorms, kState8, true>(op, e, i0, gscale, sscale, ww, xx);
+    else if (i0 < e.n)
+        take<kNorms, kState8, false>(op, e, i0, gscale, sscale, ww, xx);
+    if constexpr (kNorms) {
+        __shared__ float2 sh[kThreads / 32];
+        ww = warp_sum(ww);
+        xx = warp_sum(xx);
+        if ((threadIdx.x & 31) == 0) sh[warp] = make_float2(ww, xx);
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            float2 s = sh[0];
+            for (int i = 1; i < kThreads / 32; ++i) {
+                s.x += sh[i].x;
+                s.y += sh[i].y;
             }
+            part[c] = s;
         }
     }
 }
@@ -372,26 +476,45 @@ __global__ void __launch_bounds__(kThreads)
 }
 
 // out[i] = the value of an 8-bit moment (exact in bf16: 4 significant bits times a power of two).
+// Bound: HBM.
 template <bool kSigned, typename Out>
 __global__ void __launch_bounds__(kThreads)
     state_values_kernel(const uint8_t* __restrict__ codes, const float* __restrict__ scales,
                         long long n, Out* __restrict__ out) {
-    const long long i = (blockIdx.x * static_cast<long long>(kThreads) + threadIdx.x) * kPer;
-    if (i >= n) return;
-    float x[kPer];
-    from_codes<kSigned>(load_codes(codes, i, n), scales[i / kAdamBlock], x);
-    store8(out, i, n, x);
+    using S = Share<true>;
+    const long long i0 = blockIdx.x * static_cast<long long>(S::kChunk) + threadIdx.x / 32 * S::kWarp;
+    if (i0 >= n) return;
+    const long long i1 = i0 + 4 * (threadIdx.x & 31);
+    const bool full = i0 + S::kWarp <= n;
+    uint32_t c[S::kQuads];
+    const float scale = scales[i0 / kAdamBlock];
+#pragma unroll
+    for (int q = 0; q < S::kQuads; ++q)
+        c[q] = full ? load_codes<true>(codes, i1 + 128 * q, n) : load_codes<false>(codes, i1 + 128 * q, n);
+#pragma unroll
+    for (int q = 0; q < S::kQuads; ++q) {
+        float x[4];
+        from_codes<kSigned>(c[q], scale, x);
+        if (full)
+            store4<true>(out, i1 + 128 * q, n, x);
+        else
+            store4<false>(out, i1 + 128 * q, n, x);
+    }
 }
 
-long long chunks_of(long long n) { return (n + kChunk - 1) / kChunk; }
+template <bool kState8>
+long long chunks_of(long long n) {
+    return (n + Share<kState8>::kChunk - 1) / Share<kState8>::kChunk;
+}
 
-template <int CAP>
-cudaError_t run_adamw(int first, int count, const AdamTensor* ts, const AdamRates& op,
+// Tensors ids[0, count) of the call, all with the same kind of state.
+template <int CAP, bool kState8>
+cudaError_t run_adamw(const int* ids, int count, const AdamTensor* ts, const AdamRates& op,
                       uint32_t key, float2* part, float* scales, cudaStream_t st) {
     Table<CAP> t = {};
     long long total = 0;
     for (int k = 0; k < count; ++k) {
-        const AdamTensor& a = ts[first + k];
+        const AdamTensor& a = ts[ids[k]];
         t.g[k] = a.G;
         t.w[k] = a.W;
         t.wo[k] = a.W_out;
@@ -401,22 +524,18 @@ cudaError_t run_adamw(int first, int count, const AdamTensor* ts, const AdamRate
         t.vs[k] = a.v_scale;
         t.n[k] = a.n;
         t.first[k] = static_cast<int>(total);
-        t.key[k] = mix(key + static_cast<uint32_t>(first + k));
+        t.key[k] = mix(key + static_cast<uint32_t>(ids[k]));
         t.wd[k] = a.weight_decay;
-        t.flags[k] = static_cast<uint8_t>((a.g_bf16 ? kG16 : 0) | (a.out_bf16 ? kOut16 : 0) |
-                                          (a.state8 ? kState8 : 0));
-        total += chunks_of(a.n);
+        t.flags[k] = static_cast<uint8_t>((a.g_bf16 ? kG16 : 0) | (a.out_bf16 ? kOut16 : 0));
+        total += chunks_of<kState8>(a.n);
+        if (total > 0x7fffffff) return cudaErrorInvalidValue;
     }
     t.count = count;
     t.first[count] = static_cast<int>(total);
     if (total == 0) return cudaSuccess;
-    if (total > 0x7fffffff) return cudaErrorInvalidValue;
-    DevInfo di;
-    if (!current_device_info(&di)) return cudaErrorUnknown;
-    const long long most = 8LL * di.sm_count;
-    const unsigned grid = static_cast<unsigned>(total < most ? total : most);
+    const unsigned grid = static_cast<unsigned>(total);
     if (op.clip != 0) {
-        adamw_kernel<CAP, true><<<grid, kThreads, 0, st>>>(t, op, part, nullptr), note_launch();
+        adamw_kernel<CAP, true, kState8><<<grid, kThreads, 0, st>>>(t, op, part, nullptr), note_launch();
         cudaError_t e = cudaGetLastError();
         if (e != cudaSuccess) return e;
         adamw_scale_kernel<CAP><<<count, kThreads, 0, st>>>(t, part, op.clip_frac, scales),
@@ -424,25 +543,39 @@ cudaError_t run_adamw(int first, int count, const AdamTensor* ts, const AdamRate
         e = cudaGetLastError();
         if (e != cudaSuccess) return e;
     }
-    adamw_kernel<CAP, false><<<grid, kThreads, 0, st>>>(t, op, nullptr,
-                                                         op.clip != 0 ? scales : nullptr),
+    adamw_kernel<CAP, false, kState8>
+        <<<grid, kThreads, 0, st>>>(t, op, nullptr, op.clip != 0 ? scales : nullptr),
         note_launch();
     return cudaGetLastError();
 }
 
-}  // namespace
-
 // Tensors of one launch: the table of a few is a tenth of the parameters of many.
 constexpr int kFew = 12, kMany = 128;
 
-size_t adamw_workspace_floats(int n_tensors, const int64_t* n) {
-    long long most = 0;
-    for (int f = 0; f < n_tensors; f += kMany) {
-        long long total = 0;
-        for (int k = f; k < n_tensors && k < f + kMany; ++k) total += chunks_of(n[k]);
-        most = total > most ? total : most;
+template <bool kState8>
+cudaError_t run_kind(int n_tensors, const AdamTensor* ts, const AdamRates& op, uint32_t key, float* ws,
+                     cudaStream_t st) {
+    float2* part = reinterpret_cast<float2*>(ws ? ws + kMany : nullptr);
+    int ids[kMany], count = 0;
+    for (int k = 0; k <= n_tensors; ++k) {
+        if (k < n_tensors && ts[k].state8 == kState8 && ts[k].n > 0) ids[count++] = k;
+        if (count < kMany && (k < n_tensors || count == 0)) continue;
+        const cudaError_t e =
+            count <= kFew ? run_adamw<kFew, kState8>(ids, count, ts, op, key, part, ws, st)
+                          : run_adamw<kMany, kState8>(ids, count, ts, op, key, part, ws, st);
+        if (e != cudaSuccess) return e;
+        count = 0;
     }
-    return static_cast<size_t>(kMany + 2 * most);  // the scales, then the chunks' sums
+    return cudaSuccess;
+}
+
+}  // namespace
+
+size_t adamw_workspace_floats(int n_tensors, const int64_t* n) {
+    // the scales of a launch's tensors, then its chunks' sums (at most those of all tensors)
+    long long all = 0;
+    for (int k = 0; k < n_tensors; ++k) all += chunks_of<true>(n[k]);  // (the smaller chunks)
+    return static_cast<size_t>(kMany + 2 * all);
 }
 
 cudaError_t launch_adamw(int n_tensors, const AdamTensor* ts, const AdamRates& op, uint64_t seed,
@@ -450,19 +583,13 @@ cudaError_t launch_adamw(int n_tensors, const AdamTensor* ts, const AdamRates& o
     uint32_t key = mix(static_cast<uint32_t>(seed) + kPhi);
     key = mix(key ^ static_cast<uint32_t>(seed >> 32));
     key = mix(key ^ static_cast<uint32_t>(step));
-    float2* part = reinterpret_cast<float2*>(ws ? ws + kMany : nullptr);
-    for (int f = 0; f < n_tensors; f += kMany) {
-        const int count = n_tensors - f < kMany ? n_tensors - f : kMany;
-        const cudaError_t e = count <= kFew ? run_adamw<kFew>(f, count, ts, op, key, part, ws, st)
-                                            : run_adamw<kMany>(f, count, ts, op, key, part, ws, st);
-        if (e != cudaSuccess) return e;
-    }
-    return cudaSuccess;
+    const cudaError_t e = run_kind<false>(n_tensors, ts, op, key, ws, st);
+    return e != cudaSuccess ? e : run_kind<true>(n_tensors, ts, op, key, ws, st);
 }
 
 cudaError_t launch_state_values(bool is_signed, long long n, const void* codes, const float* scales,
                                 int out_dtype, void* out, cudaStream_t st) {
-    const long long blocks = (n + kChunk - 1) / kChunk;
+    const long long blocks = chunks_of<true>(n);
     if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
     const unsigned grid = static_cast<unsigned>(blocks);
     const uint8_t* c = static_cast<const uint8_t*>(codes);

@@ -820,7 +820,7 @@ bool act_ok(int32_t act) { return act >= FPO_ACT_NONE && act <= FPO_ACT_SILU; }
 
 // Clears the first `bytes` of a workspace (the status word, counters behind it).
 cudaError_t clear(void* workspace, size_t bytes, cudaStream_t st) {
-    return cudaMemsetAsync(workspace, 0, bytes, st);
+    return bytes ? cudaMemsetAsync(workspace, 0, bytes, st) : cudaSuccess;
 }
 
 }  // namespace
@@ -855,8 +855,8 @@ int32_t fpo_linear(int64_t T, int64_t d_out, int64_t d_in, int32_t dtype, int32_
     if (rc != FPO_OK) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const int Ti = static_cast<int>(T), N = static_cast<int>(d_out), K = static_cast<int>(d_in);
-    FPO_TRY(clear(workspace, T == 0 ? sizeof(unsigned) : linear_clear_bytes(dtype, Ti, N, K), st));
-    if (T == 0) return FPO_OK;
+    if (T == 0) return cuda_status(clear(workspace, sizeof(unsigned), st));
+    FPO_TRY(clear(workspace, linear_clear_bytes(dtype, Ti, N, K), st));
     const LinearFwd p{Ti, N, K, act, X, W, bias, residual, Y, Z_out};
     return cuda_status(launch_linear(dtype, p, workspace, st));
 }
@@ -924,7 +924,7 @@ int32_t fpo_adamw_grouped(int32_t n_tensors, const fpo_adamw_tensor* tensors,
     if (!tensors || !opt) return FPO_ERR_NULL;
     if (n_tensors < 1) return FPO_ERR_SHAPE;
     if (opt->clip < FPO_CLIP_NONE || opt->clip > FPO_CLIP_GRADIENT || !(opt->lr == opt->lr) ||
-        !(opt->eps == opt->eps) || !(opt->clip_frac >= 0.0) || opt->step < 1 ||
+        !(opt->eps >= 0.0) || !(opt->clip_frac >= 0.0) || opt->step < 1 ||
         !(opt->beta1 >= 0.0 && opt->beta1 < 1.0) || !(opt->beta2 >= 0.0 && opt->beta2 < 1.0))
         return FPO_ERR_ARG;
     // host memory for the checks and the launch's table; no exception leaves the library
@@ -987,7 +987,7 @@ int32_t fpo_adamw_grouped(int32_t n_tensors, const fpo_adamw_tensor* tensors,
     AdamRates r;
     r.clip = opt->clip;
     r.lr = static_cast<float>(opt->lr);
-    r.eps = static_cast<float>(opt->eps);
+    r.eps = std::max(static_cast<float>(opt->eps), 0x1p-63f);
     r.clip_frac = static_cast<float>(opt->clip_frac);
     r.b1 = static_cast<float>(opt->beta1);
     r.a1 = static_cast<float>(1.0 - opt->beta1);

@@ -240,8 +240,7 @@ cudaError_t launch_state_values(bool is_signed, long long n, const void* codes, 
 
 // ------------------------------------------------------------ linear layers (linear.cu, simt_f32.cu)
 // Y[T, N] = act(X[T, K] W[N, K]^T + bias) + residual, Z = the pre-activation; bias, residual and
-// Z may be null.  act: act_math.cuh.  The workspace's first kLinearHead bytes (status word,
-// counters) are zero before a call.
+// Z may be null.  act: act_math.cuh.
 struct LinearFwd {
     int T, N, K, act;
     const void* X;
@@ -266,7 +265,8 @@ struct LinearVjp {
 };
 size_t linear_workspace_bytes(int dtype, int T, int N, int K);
 size_t linear_vjp_workspace_bytes(int dtype, int T, int N, int K, int act);
-// Bytes at the workspace's start that are zero before a call.
+// Bytes at the workspace's start that are zero before a call (0: the status word is written by the
+// call's kernel).
 size_t linear_clear_bytes(int dtype, int T, int N, int K);
 size_t linear_vjp_clear_bytes(int dtype, int T, int N, int K);
 cudaError_t launch_linear(int dtype, const LinearFwd& p, void* workspace, cudaStream_t st);

@@ -12,6 +12,7 @@
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
+#include <string.h>
 
 #include "gemm_launch.cuh"
 #include "internal.h"
@@ -36,7 +37,7 @@ size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 //   warp 1      TMEM, MMAs (128 x BT x 16)
 //   warps 2..5  epilogue: one feature per lane
 // Bound: the weights' bytes.
-constexpr int kFewT = 128;
+constexpr int kFewT = 32;
 
 template <int BT>
 struct FewSmem {
@@ -68,38 +69,66 @@ __device__ __forceinline__ int few_owner(const FewShape& s, long long u, long lo
 }
 
 // One feature of the tokens from t0 on through the epilogue: consecutive lanes are consecutive
-// features.
+// features.  What it reads is loaded for all tokens before anything is stored (a load behind a store
+// to memory that may be the same waits for itself alone: 128 tokens took 110 us instead of 35).
+__device__ __forceinline__ void few_load(const __nv_bfloat16* p, long long o, long long ld, int n,
+                                         uint16_t (&u)[32]) {
+    const uint16_t* q = reinterpret_cast<const uint16_t*>(p) + o;
+#pragma unroll
+    for (int j = 0; j < 32; ++j) u[j] = j < n ? q[j * ld] : 0;
+}
+__device__ __forceinline__ float bf16_bits(uint16_t u) {
+    return __uint_as_float(static_cast<uint32_t>(u) << 16);
+}
 __device__ __forceinline__ void few_out(const LinearOut& p, int feature, int t0, int n,
-                                        const float (&v)[32]) {
+                                        float (&v)[32]) {
     if (feature >= p.N) return;
-    const float bias = p.bias ? __bfloat162float(p.bias[feature]) : 0.f;
+    const long long o = t0 * p.ld + feature;
+    uint16_t r[32];
+    if (p.residual) few_load(p.residual, o, p.ld, n, r);
+    if (p.bias) {
+        const float bias = __bfloat162float(p.bias[feature]);
+#pragma unroll
+        for (int j = 0; j < 32; ++j) v[j] += bias;
+    }
+    if (p.Z) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+            if (j < n) p.Z[o + j * p.ld] = __float2bfloat16_rn(v[j]);
+    }
     with_act(p.act, [&](auto act) {
 #pragma unroll
-        for (int j = 0; j < 32; ++j) {
+        for (int j = 0; j < 32; j += 2) {
             if (j >= n) break;
-            const long long o = (t0 + j) * p.ld + feature;
-            const float z = v[j] + bias;
-            if (p.Z) p.Z[o] = __float2bfloat16_rn(z);
-            float y = act_value<act.value, true>(z);
-            if (p.residual) y += __bfloat162float(p.residual[o]);
-            p.Y[o] = __float2bfloat16_rn(y);
+            const float2 y = act_value2<act.value>(make_float2(v[j], v[j + 1]));
+            v[j] = y.x;
+            v[j + 1] = y.y;
         }
     });
+#pragma unroll
+    for (int j = 0; j < 32; ++j)
+        if (j < n) p.Y[o + j * p.ld] = __float2bfloat16_rn(p.residual ? v[j] + bf16_bits(r[j]) : v[j]);
 }
 __device__ __forceinline__ void few_out(const SlopeOut& p, int feature, int t0, int n,
-                                        const float (&v)[32]) {
+                                        float (&v)[32]) {
     if (feature >= p.N) return;
-    with_act(p.z ? p.act : kActNone, [&](auto act) {
+    const long long o = t0 * p.ld + feature;
+    if (p.z) {
+        uint16_t z[32];
+        few_load(p.z, o, p.ld, n, z);
+        with_act(p.act, [&](auto act) {
 #pragma unroll
-        for (int j = 0; j < 32; ++j) {
-            if (j >= n) break;
-            const long long o = (t0 + j) * p.ld + feature;
-            float x = v[j];
-            if constexpr (act.value != kActNone)
-                x *= act_slope<act.value, true>(__bfloat162float(p.z[o]));
-            p.X[o] = __float2bfloat16_rn(x);
-        }
-    });
+            for (int j = 0; j < 32; j += 2) {
+                if (j >= n) break;
+                const float2 s = act_slope2<act.value>(make_float2(bf16_bits(z[j]), bf16_bits(z[j + 1])));
+                v[j] *= s.x;
+                v[j + 1] *= s.y;
+            }
+        });
+    }
+#pragma unroll
+    for (int j = 0; j < 32; ++j)
+        if (j < n) p.X[o + j * p.ld] = __float2bfloat16_rn(v[j]);
 }
 
 template <int BT, bool W_MN, class Out>
@@ -304,12 +333,26 @@ __global__ void __launch_bounds__(192, 1)
     }
 }
 
+// The weights as an operand of few_tokens_kernel: 256 bytes of a row at a time from DRAM (two
+// k-blocks, the second of which the same SM wants next).
+bool map_weights(CUtensorMap* m, const void* W, int rows, int cols, int box_rows) {
+    const EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
+    cuuint64_t strides[1] = {static_cast<cuuint64_t>(cols) * 2};
+    cuuint32_t box[2] = {64, static_cast<cuuint32_t>(box_rows)};
+    cuuint32_t es[2] = {1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(W), dims, strides, box, es,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 int sm_count() {
     DevInfo di;
     return current_device_info(&di) ? di.sm_count : 152;
 }
 
-int few_bt(int T) { return T <= 16 ? 16 : T <= 32 ? 32 : T <= 64 ? 64 : 128; }
+int few_bt(int T) { return T <= 16 ? 16 : 32; }
 
 // CTAs of a problem: one per SM while each has at least 4 k-blocks.
 long long few_ctas(int M, int K) {
@@ -331,7 +374,7 @@ cudaError_t run_few_bt(const void* W, const void* X, int M, int K, int T, const 
     const cudaError_t e = set_smem_limit<kern>(L::kBytes);
     if (e != cudaSuccess) return e;
     CUtensorMap wmap, xmap;
-    const bool ok = W_MN ? map_mnmajor(&wmap, W, K, M) : map_kmajor(&wmap, W, M, K, kBM);
+    const bool ok = W_MN ? map_weights(&wmap, W, K, M, kBK) : map_weights(&wmap, W, M, K, kBM);
     if (!ok || !map_kmajor(&xmap, X, T, K, BT)) return cudaErrorInvalidValue;
     FewShape sh;
     sh.M = M;
@@ -347,11 +390,88 @@ cudaError_t run_few_bt(const void* W, const void* X, int M, int K, int T, const 
 template <bool W_MN, class Out>
 cudaError_t run_few(const void* W, const void* X, int M, int K, int T, const Out& out,
                     uint8_t* counters, float* scratch, unsigned* status, cudaStream_t st) {
-    switch (few_bt(T)) {
-        case 16: return run_few_bt<16, W_MN>(W, X, M, K, T, out, counters, scratch, status, st);
-        case 32: return run_few_bt<32, W_MN>(W, X, M, K, T, out, counters, scratch, status, st);
-        case 64: return run_few_bt<64, W_MN>(W, X, M, K, T, out, counters, scratch, status, st);
-        default: return run_few_bt<128, W_MN>(W, X, M, K, T, out, counters, scratch, status, st);
+    if (few_bt(T) == 16)
+        return run_few_bt<16, W_MN>(W, X, M, K, T, out, counters, scratch, status, st);
+    return run_few_bt<32, W_MN>(W, X, M, K, T, out, counters, scratch, status, st);
+}
+
+// ------------------------------------------------------------------ one to four tokens
+// Y = act(X W^T + b) + R for T <= kRowT tokens: a warp per feature, whose row of the weights the
+// lanes read 16 bytes each, kRowAhead loads at a time; X comes from L1, and a butterfly adds the
+// lanes' sums.  Nothing has to be set up or added across blocks: one launch, which also clears the
+// status word (no kernel of the call waits for anything).
+// Bound: the weights' bytes.
+constexpr int kRowT = 4, kRowWarps = 8, kRowAhead = 4;
+
+__device__ __forceinline__ uint4 ld_stream(const uint4* p) {
+    uint4 u;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w)
+                 : "l"(p));
+    return u;
+}
+
+template <int kT>
+__global__ void __launch_bounds__(32 * kRowWarps)
+    row_kernel(const __nv_bfloat16* __restrict__ X, const __nv_bfloat16* __restrict__ W, int N, int K,
+               const __grid_constant__ LinearOut out, unsigned* status) {
+    if (blockIdx.x == 0 && threadIdx.x == 0) *status = 0u;
+    const int lane = threadIdx.x % 32, feature = blockIdx.x * kRowWarps + threadIdx.x / 32;
+    if (feature >= N) return;
+    const int vecs = K / 8;
+    const uint4* w = reinterpret_cast<const uint4*>(W + static_cast<long long>(feature) * K);
+    float2 acc[kT];
+#pragma unroll
+    for (int t = 0; t < kT; ++t) acc[t] = make_float2(0.f, 0.f);
+    for (int v0 = lane; v0 < vecs; v0 += 32 * kRowAhead) {
+        uint4 u[kRowAhead];
+#pragma unroll
+        for (int i = 0; i < kRowAhead; ++i)
+            u[i] = v0 + 32 * i < vecs ? ld_stream(w + v0 + 32 * i) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int i = 0; i < kRowAhead; ++i) {
+            if (v0 + 32 * i >= vecs) break;
+            const float2 a = unpack2(u[i].x), b = unpack2(u[i].y), c = unpack2(u[i].z), d = unpack2(u[i].w);
+#pragma unroll
+            for (int t = 0; t < kT; ++t) {
+                const uint4 x = reinterpret_cast<const uint4*>(X + static_cast<long long>(t) * K)[v0 + 32 * i];
+                acc[t] = fma2(a, unpack2(x.x), acc[t]);
+                acc[t] = fma2(b, unpack2(x.y), acc[t]);
+                acc[t] = fma2(c, unpack2(x.z), acc[t]);
+                acc[t] = fma2(d, unpack2(x.w), acc[t]);
+            }
+        }
+    }
+    float s = 0.f;  // lane t has token t's
+#pragma unroll
+    for (int t = 0; t < kT; ++t) {
+        const float r = warp_sum_f32(acc[t].x + acc[t].y);
+        if (lane == t) s = r;
+    }
+    if (lane >= kT) return;
+    const long long o = lane * out.ld + feature;
+    float2 z = make_float2(s, 0.f);
+    if (out.bias) z.x += __bfloat162float(out.bias[feature]);
+    if (out.Z) out.Z[o] = __float2bfloat16_rn(z.x);
+    with_act(out.act, [&](auto act) { z = act_value2<act.value>(z); });
+    if (out.residual) z.x += __bfloat162float(out.residual[o]);
+    out.Y[o] = __float2bfloat16_rn(z.x);
+}
+
+template <int kT>
+cudaError_t run_rows_t(const LinearFwd& p, const LinearOut& out, unsigned* status, cudaStream_t st) {
+    row_kernel<kT><<<(p.N + kRowWarps - 1) / kRowWarps, 32 * kRowWarps, 0, st>>>(
+        static_cast<const __nv_bfloat16*>(p.X), static_cast<const __nv_bfloat16*>(p.W), p.N, p.K, out,
+        status),
+        note_launch();
+    return cudaGetLastError();
+}
+cudaError_t run_rows(const LinearFwd& p, const LinearOut& out, unsigned* status, cudaStream_t st) {
+    switch (p.T) {
+        case 1: return run_rows_t<1>(p, out, status, st);
+        case 2: return run_rows_t<2>(p, out, status, st);
+        case 3: return run_rows_t<3>(p, out, status, st);
+        default: return run_rows_t<4>(p, out, status, st);
     }
 }
 
@@ -359,11 +479,11 @@ cudaError_t run_few(const void* W, const void* X, int M, int K, int T, const Out
 // Clusters of the pair kernels at once (76 without a device: two SMs of 152 each).
 int linear_clusters() {
     using L = GemmPairSmem<256, kPairStages, pair_ksub<256, false, false>()>;
-    constexpr auto kern = tc_gemm_pair_kernel<256, false, false, kPairStages, 1, EpiLinear<2>>;
+    constexpr auto kern = tc_gemm_pair_kernel<256, false, false, kPairStages, 1, EpiLinear<256>>;
     DevInfo di;
     int c = 76;
     if (current_device_info(&di) && set_smem_limit<kern>(L::kBytes) == cudaSuccess)
-        c = resident_clusters<kern>(gemm_threads<EpiLinear<2>>(), L::kBytes, di.sm_count, 2);
+        c = resident_clusters<kern>(gemm_threads<EpiLinear<256>>(), L::kBytes, di.sm_count, 2);
     cudaGetLastError();
     return c;
 }
@@ -433,6 +553,12 @@ __global__ void __launch_bounds__(kFixupThreads)
     out_row4(out, row * out.ld + n, n, s4);
 }
 
+bool out_maps(EpiLinear<256>::Params* p) {
+    return map_out_bf16(&p->ymap, p->o.Y, p->o.M, p->o.N) &&
+           map_out_bf16(&p->zmap, p->o.Z ? p->o.Z : p->o.Y, p->o.M, p->o.N);
+}
+bool out_maps(EpiSlope<256>::Params* p) { return map_out_bf16(&p->xmap, p->o.X, p->o.M, p->o.N); }
+
 // C[M, N] = A B^T through Epi.  A_MN: A is [K, M], else [M, K]; B_MN: B is [K, N], else [N, K].
 template <bool A_MN, bool B_MN, template <int> class Epi, class Out>
 cudaError_t run_pair(const void* A, const void* B, int M, int N, int K, const Out& out,
@@ -442,14 +568,19 @@ cudaError_t run_pair(const void* A, const void* B, int M, int N, int K, const Ou
     bool ok = A_MN ? map_mnmajor(&maps.a[0], A, K, M) : map_kmajor(&maps.a[0], A, M, K, kBM);
     ok = ok && (B_MN ? map_mnmajor(&maps.b[0], B, K, N)
                      : map_kmajor(&maps.b[0], B, N, K, pp.half ? kHalfBN / 2 : 128));
-    if (!ok) return cudaErrorInvalidValue;
-    if (pp.half)
-        return run_gemm_pair<kHalfBN, A_MN, B_MN, kHalfStages, 1, Epi<1>>(
-            maps, out, make_shape(M, N, K, kHalfBN, 1, band_for(true), kPairBM), status, st);
+    typename Epi<256>::Params ep;
+    ep.o = out;
+    if (!ok || !out_maps(&ep)) return cudaErrorInvalidValue;
+    if (pp.half) {
+        typename Epi<kHalfBN>::Params eh;
+        memcpy(&eh, &ep, sizeof(eh));  // the same fields for every tile width
+        return run_gemm_pair<kHalfBN, A_MN, B_MN, kHalfStages, 1, Epi<kHalfBN>>(
+            maps, eh, make_shape(M, N, K, kHalfBN, 1, band_for(true), kPairBM), status, st);
+    }
     const GemmShape sh = make_shape(M, N, K, 256, 1, band_for(true), kPairBM);
     SkPlan plan;
-    const cudaError_t e = run_gemm_pair<256, A_MN, B_MN, kPairStages, 1, Epi<2>>(
-        maps, out, sh, status, st, pp.units > 0 ? scratch : nullptr, &plan, pp.split);
+    const cudaError_t e = run_gemm_pair<256, A_MN, B_MN, kPairStages, 1, Epi<256>>(
+        maps, ep, sh, status, st, pp.units > 0 ? scratch : nullptr, &plan, pp.split);
     if (e != cudaSuccess || plan.tail_tiles <= 0) return e;
     return launch_chained(linear_fixup_kernel<Out>, sk_fixup_grid<256>(plan), kFixupThreads, 0, st,
                           sk_fixup_shape(plan, sh), static_cast<const float*>(scratch), out);
@@ -466,14 +597,9 @@ template <typename T, int kV>
 __device__ __forceinline__ void sig_load(const T* p, float (&x)[kV]) {
     if constexpr (kV == 8) {
         const uint4 u = *reinterpret_cast<const uint4*>(p);
-        float a[4], b[4];
-        unpack4(make_uint2(u.x, u.y), a);
-        unpack4(make_uint2(u.z, u.w), b);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            x[k] = a[k];
-            x[4 + k] = b[k];
-        }
+        const float2 a = unpack2(u.x), b = unpack2(u.y), c = unpack2(u.z), d = unpack2(u.w);
+        x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y;
+        x[4] = c.x; x[5] = c.y; x[6] = d.x; x[7] = d.y;
     } else if constexpr (kV == 4) {
         const float4 u = *reinterpret_cast<const float4*>(p);
         x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w;
@@ -517,8 +643,17 @@ __global__ void __launch_bounds__(kSigThreads)
                 if constexpr (a.value != kActNone) {
                     float z[kV];
                     sig_load<T, kV>(Z + o, z);
+                    if constexpr (kV == 8) {  // bf16
 #pragma unroll
-                    for (int k = 0; k < kV; ++k) x[k] *= act_slope<a.value, kV == 8>(z[k]);
+                        for (int k = 0; k < kV; k += 2) {
+                            const float2 s2 = act_slope2<a.value>(make_float2(z[k], z[k + 1]));
+                            x[k] *= s2.x;
+                            x[k + 1] *= s2.y;
+                        }
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < kV; ++k) x[k] *= act_slope<a.value>(z[k]);
+                    }
                     sig_store<T, kV>(dZ + o, x);
                 }
 #pragma unroll
@@ -589,10 +724,11 @@ cudaError_t run_signal_v(const LinearVjp& p, T* dZ, float* part, const SignalPla
 }  // namespace
 
 size_t linear_clear_bytes(int dtype, int T, int N, int K) {
+    if (dtype == 1 && T <= kRowT) return 0;  // the kernel does it
     return dtype == 1 && T <= kFewT ? kHead + few_counter_bytes(N) : sizeof(unsigned);
 }
 size_t linear_workspace_bytes(int dtype, int T, int N, int K) {
-    if (dtype != 1 || T == 0) return kHead;
+    if (dtype != 1 || T <= kRowT) return kHead;
     if (T <= kFewT) return kHead + few_counter_bytes(N) + few_scratch_bytes(N, K, T);
     return kHead + pair_scratch_bytes(T, N, K);
 }
@@ -610,6 +746,7 @@ cudaError_t launch_linear(int dtype, const LinearFwd& p, void* workspace, cudaSt
     out.M = p.T;
     out.N = p.N;
     out.act = p.act;
+    if (p.T <= kRowT) return run_rows(p, out, status, st);
     if (p.T <= kFewT)
         return run_few<false>(p.W, p.X, p.N, p.K, p.T, out, ws + kHead,
                               reinterpret_cast<float*>(ws + kHead + few_counter_bytes(p.N)), status,

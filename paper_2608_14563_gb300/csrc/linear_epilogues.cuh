@@ -1,7 +1,11 @@
-// linear_epilogues.cuh -- 8-warp epilogues (tc_gemm.cuh, RowChunk) of the linear layer's
-// products: bias, activation and residual of the forward pass, the slope of the activation
-// below in the backward pass.  What a chunk reads is loaded as one batch when the chunk before
-// is done (epilogues.cuh says why).
+// linear_epilogues.cuh -- epilogues (tc_gemm.cuh) of the linear layer's products: bias, activation
+// and residual of the forward pass, the slope of the activation below in the backward pass.
+//
+// One row per thread, 32 columns at a time, written through the warp's staging buffers by TMA.  What
+// a row reads beside the accumulator (residual, pre-activation) is loaded one chunk ahead, 64 bytes
+// of 32 rows, and its other half line is in L1 by then.  The 8-warp form of the other epilogues that
+// read matrices (RowChunk: every global access 256 bytes of two rows, through shared memory twice)
+// takes 2 to 3 times the instructions; these run beside the MMAs of a GPU at its power cap.
 #pragma once
 
 #include "act_math.cuh"
@@ -9,18 +13,12 @@
 
 namespace fpo {
 
-__device__ __forceinline__ void unpack4(uint2 u, float (&x)[4]) {
-    x[0] = __uint_as_float(u.x << 16);
-    x[1] = __uint_as_float(u.x & 0xffff0000u);
-    x[2] = __uint_as_float(u.y << 16);
-    x[3] = __uint_as_float(u.y & 0xffff0000u);
+__device__ __forceinline__ float2 unpack2(uint32_t u) {
+    return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
 }
-__device__ __forceinline__ uint2 pack4(const float (&x)[4]) {
-    return make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
-}
+__device__ __forceinline__ uint32_t pack2(float2 x) { return pack_bf16x2(x.x, x.y); }
 
-// z = v + bias; Z = z; Y = act(z) + residual.  Any of bias, residual and Z may be null; with
-// none of them and no activation the plain product, rounded (the weight gradient).
+// z = v + bias; Z = z; Y = act(z) + residual.  Any of bias, residual and Z may be null.
 struct LinearOut {
     const __nv_bfloat16* bias;      // [N]
     const __nv_bfloat16* residual;  // [M, N]
@@ -37,164 +35,169 @@ struct SlopeOut {
     int M, N, act;
 };
 
-// N summed values of a row at element offset o (columns from c) through the epilogue, for the
-// kernels that sum the parts of split tiles.
-template <int kN>
-__device__ __forceinline__ void out_row(const LinearOut& p, long long o, int c, float (&v)[kN]) {
-#pragma unroll
-    for (int k = 0; k < kN; ++k) {
-        if (p.bias) v[k] += __bfloat162float(p.bias[c + k]);
-        if (p.Z) p.Z[o + k] = __float2bfloat16_rn(v[k]);
-    }
-    with_act(p.act, [&](auto act) {
-#pragma unroll
-        for (int k = 0; k < kN; ++k) v[k] = act_value<act.value, true>(v[k]);
-    });
-#pragma unroll
-    for (int k = 0; k < kN; ++k) {
-        if (p.residual) v[k] += __bfloat162float(p.residual[o + k]);
-        p.Y[o + k] = __float2bfloat16_rn(v[k]);
-    }
-}
-template <int kN>
-__device__ __forceinline__ void out_row(const SlopeOut& p, long long o, int, float (&v)[kN]) {
-    if (p.z) {
-        float z[kN];
-#pragma unroll
-        for (int k = 0; k < kN; ++k) z[k] = __bfloat162float(p.z[o + k]);
-        with_act(p.act, [&](auto act) {
-#pragma unroll
-            for (int k = 0; k < kN; ++k) v[k] *= act_slope<act.value, true>(z[k]);
-        });
-    }
-#pragma unroll
-    for (int k = 0; k < kN; ++k) p.X[o + k] = __float2bfloat16_rn(v[k]);
-}
-// 4 of them, 8-byte aligned.
-__device__ __forceinline__ void out_row4(const LinearOut& p, long long o, int c, float (&v)[4]) {
+// 4 summed values at element offset o (a multiple of 4; columns from c) through the epilogue, for
+// the kernel that adds the parts of split tiles.
+__device__ __forceinline__ void out_row4(const LinearOut& p, long long o, int c, const float (&v)[4]) {
+    float2 a = make_float2(v[0], v[1]), b = make_float2(v[2], v[3]);
     if (p.bias) {
-        float b[4];
-        unpack4(*reinterpret_cast<const uint2*>(p.bias + c), b);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] += b[k];
+        const uint2 u = *reinterpret_cast<const uint2*>(p.bias + c);
+        a = add2(a, unpack2(u.x));
+        b = add2(b, unpack2(u.y));
     }
-    if (p.Z) *reinterpret_cast<uint2*>(p.Z + o) = pack4(v);
+    if (p.Z) *reinterpret_cast<uint2*>(p.Z + o) = make_uint2(pack2(a), pack2(b));
     with_act(p.act, [&](auto act) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = act_value<act.value, true>(v[k]);
+        a = act_value2<act.value>(a);
+        b = act_value2<act.value>(b);
     });
     if (p.residual) {
-        float r[4];
-        unpack4(*reinterpret_cast<const uint2*>(p.residual + o), r);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] += r[k];
+        const uint2 u = *reinterpret_cast<const uint2*>(p.residual + o);
+        a = add2(a, unpack2(u.x));
+        b = add2(b, unpack2(u.y));
     }
-    *reinterpret_cast<uint2*>(p.Y + o) = pack4(v);
+    *reinterpret_cast<uint2*>(p.Y + o) = make_uint2(pack2(a), pack2(b));
 }
-__device__ __forceinline__ void out_row4(const SlopeOut& p, long long o, int, float (&v)[4]) {
+__device__ __forceinline__ void out_row4(const SlopeOut& p, long long o, int, const float (&v)[4]) {
+    float2 a = make_float2(v[0], v[1]), b = make_float2(v[2], v[3]);
     if (p.z) {
-        float z[4];
-        unpack4(*reinterpret_cast<const uint2*>(p.z + o), z);
+        const uint2 u = *reinterpret_cast<const uint2*>(p.z + o);
         with_act(p.act, [&](auto act) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] *= act_slope<act.value, true>(z[k]);
+            a = mul2(a, act_slope2<act.value>(unpack2(u.x)));
+            b = mul2(b, act_slope2<act.value>(unpack2(u.y)));
         });
     }
-    *reinterpret_cast<uint2*>(p.X + o) = pack4(v);
+    *reinterpret_cast<uint2*>(p.X + o) = make_uint2(pack2(a), pack2(b));
 }
 
-template <int kCG>
+// 32 columns of a row, one chunk ahead.
+struct RowAhead {
+    uint4 u[4];
+    // p: the row's first element, null for none; columns outside the matrix (N: a multiple of 8) are
+    // zeros.
+    __device__ __forceinline__ void load(const __nv_bfloat16* p, int col, int N) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            u[q] = p && col + 8 * q < N ? *reinterpret_cast<const uint4*>(p + col + 8 * q)
+                                        : make_uint4(0u, 0u, 0u, 0u);
+    }
+    __device__ __forceinline__ float2 at(int j) const {  // columns 2 j and 2 j + 1
+        const uint4& q = u[j / 4];
+        return unpack2(j % 4 == 0 ? q.x : j % 4 == 1 ? q.y : j % 4 == 2 ? q.z : q.w);
+    }
+};
+
+// 32 columns of the thread's row into the left or right half of a staging buffer (64 columns; the
+// layout of out_stage_row), so that no registers hold the left half while the right is formed.
+__device__ __forceinline__ void stage_half(uint32_t buf, int r, bool right, const uint32_t (&w)[16]) {
+    const uint32_t row = buf + static_cast<uint32_t>(r) * 128u;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        const uint32_t piece = static_cast<uint32_t>(right ? c + 4 : c) ^ (static_cast<uint32_t>(r) & 7u);
+        st_shared_v4(row + (piece << 4), w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
+    }
+}
+// Before a left half is staged: the stores that read the buffers last have done so.
+template <int kBuffers>
+__device__ __forceinline__ void stage_ready(const EpiIO& io) {
+    if (io.lane == 0) bulk_wait_group_read<2 - kBuffers>();
+    __syncwarp();
+}
+__device__ __forceinline__ uint32_t stage_buf(const EpiIO& io, uint32_t ahead) {
+    return io.out + ((io.count + ahead) & 1u) * kOutBufBytes;
+}
+
+template <int BN>
 struct EpiLinear {
-    using Params = LinearOut;
-    static constexpr int kWarps = 8, kColGroups = kCG;
-    using R = RowChunk;
-    RowPos<kCG> pos;
-    uint2 b[kCG];      // bias of the lane's columns of each column group
-    uint2 r[R::kAcc];  // residual of the next chunk
+    static constexpr int kWarps = 4;
+    struct Params {
+        CUtensorMap ymap, zmap;  // Y and Z, boxes 64 x 32
+        LinearOut o;
+    };
+    const __nv_bfloat16* res;
+    RowAhead r;
 
-    __device__ __forceinline__ void load(const Params& p, int c) {
-        if (!p.residual) return;
-#pragma unroll
-        for (int i = 0; i < R::kAcc; ++i)
-            r[i] = *reinterpret_cast<const uint2*>(pos.src(p.residual, p.ld, R::kAcc * c + i));
+    __device__ __forceinline__ EpiLinear(const Params& p, int, int row, int n0) {
+        res = p.o.residual && row < p.o.M ? p.o.residual + row * p.o.ld : nullptr;
+        if (p.o.residual) r.load(res, n0, p.o.N);
     }
 
-    __device__ __forceinline__ EpiLinear(const Params& p, int, int row0, int n0, int lane)
-        : pos(p.M, p.N, p.ld, row0, n0, lane) {
+    __device__ __forceinline__ void chunk(const Params& p, const float (&v)[32], int col0, int c0,
+                                          EpiIO& io) {
+        if (io.row0 >= p.o.M || (col0 & ~63) >= p.o.N) return;
+        const bool right = (c0 & 32) != 0, two = p.o.Z != nullptr;
+        float2 x[16];
+        RowAhead b;
+        if (p.o.bias) b.load(p.o.bias, col0, p.o.N);
 #pragma unroll
-        for (int k = 0; k < kCG; ++k) {
-            const int c = n0 + k * R::kCols + 4 * (lane % R::kLanes);
-            b[k] = p.bias && c < p.N ? *reinterpret_cast<const uint2*>(p.bias + c)
-                                     : make_uint2(0u, 0u);
+        for (int j = 0; j < 16; ++j) {
+            x[j] = make_float2(v[2 * j], v[2 * j + 1]);
+            if (p.o.bias) x[j] = add2(x[j], b.at(j));
         }
-        load(p, 0);
-    }
-
-    __device__ __forceinline__ void chunk(const Params& p, uint32_t buf, int lane, int c) {
-        float bias[4];
-        unpack4(c % kCG == 0 ? b[0] : b[kCG - 1], bias);
-        with_act(p.act, [&](auto act) {
+        if (!right) {
+            if (two)
+                stage_ready<2>(io);
+            else
+                stage_ready<1>(io);
+        }
+        uint32_t w[16];
+        if (two) {
 #pragma unroll
-            for (int i = 0; i < R::kAcc; ++i) {
-                const float4 v4 = R::read(buf, lane, i);
-                float v[4] = {v4.x + bias[0], v4.y + bias[1], v4.z + bias[2], v4.w + bias[3]};
-                const bool in = pos.in(R::kAcc * c + i);
-                const long long o = pos.at(p.ld, R::kAcc * c + i);
-                if (p.Z && in) *reinterpret_cast<uint2*>(p.Z + o) = pack4(v);
+            for (int j = 0; j < 16; ++j) w[j] = pack2(x[j]);
+            stage_half(stage_buf(io, 0), io.lane, right, w);
+        }
+        with_act(p.o.act, [&](auto act) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) v[k] = act_value<act.value, true>(v[k]);
-                if (p.residual) {
-                    float q[4];
-                    unpack4(r[i], q);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) v[k] += q[k];
-                }
-                if (in) *reinterpret_cast<uint2*>(p.Y + o) = pack4(v);
-            }
+            for (int j = 0; j < 16; ++j) x[j] = act_value2<act.value>(x[j]);
         });
-        if (c + 1 < pos.kChunks) load(p, c + 1);
+        if (p.o.residual) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) x[j] = add2(x[j], r.at(j));
+            if (c0 + 32 < BN) r.load(res, col0 + 32, p.o.N);
+        }
+#pragma unroll
+        for (int j = 0; j < 16; ++j) w[j] = pack2(x[j]);
+        stage_half(stage_buf(io, two ? 1 : 0), io.lane, right, w);
+        if (!right) return;
+        if (two) out_commit(io, &p.zmap, stage_buf(io, 0), col0 - 32, io.row0);
+        out_commit(io, &p.ymap, stage_buf(io, 0), col0 - 32, io.row0);
     }
 
     __device__ __forceinline__ void finish(const Params&, int) {}
 };
 
-template <int kCG>
+template <int BN>
 struct EpiSlope {
-    using Params = SlopeOut;
-    static constexpr int kWarps = 8, kColGroups = kCG;
-    using R = RowChunk;
-    RowPos<kCG> pos;
-    uint2 zr[R::kAcc];  // pre-activations of the next chunk
+    static constexpr int kWarps = 4;
+    struct Params {
+        CUtensorMap xmap;  // X, boxes 64 x 32
+        SlopeOut o;
+    };
+    const __nv_bfloat16* zrow;
+    RowAhead r;
 
-    __device__ __forceinline__ void load(const Params& p, int c) {
-        if (!p.z) return;
-#pragma unroll
-        for (int i = 0; i < R::kAcc; ++i)
-            zr[i] = *reinterpret_cast<const uint2*>(pos.src(p.z, p.ld, R::kAcc * c + i));
+    __device__ __forceinline__ EpiSlope(const Params& p, int, int row, int n0) {
+        zrow = p.o.z && row < p.o.M ? p.o.z + row * p.o.ld : nullptr;
+        if (p.o.z) r.load(zrow, n0, p.o.N);
     }
 
-    __device__ __forceinline__ EpiSlope(const Params& p, int, int row0, int n0, int lane)
-        : pos(p.M, p.N, p.ld, row0, n0, lane) {
-        load(p, 0);
-    }
-
-    __device__ __forceinline__ void chunk(const Params& p, uint32_t buf, int lane, int c) {
-        with_act(p.z ? p.act : kActNone, [&](auto act) {
+    __device__ __forceinline__ void chunk(const Params& p, const float (&v)[32], int col0, int c0,
+                                          EpiIO& io) {
+        if (io.row0 >= p.o.M || (col0 & ~63) >= p.o.N) return;
+        const bool right = (c0 & 32) != 0;
+        uint32_t w[16];
+        if (p.o.z) {
+            with_act(p.o.act, [&](auto act) {
 #pragma unroll
-            for (int i = 0; i < R::kAcc; ++i) {
-                const float4 v4 = R::read(buf, lane, i);
-                float v[4] = {v4.x, v4.y, v4.z, v4.w};
-                if constexpr (act.value != kActNone) {
-                    float z[4];
-                    unpack4(zr[i], z);
+                for (int j = 0; j < 16; ++j)
+                    w[j] = pack2(mul2(make_float2(v[2 * j], v[2 * j + 1]), act_slope2<act.value>(r.at(j))));
+            });
+            if (c0 + 32 < BN) r.load(zrow, col0 + 32, p.o.N);
+        } else {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) v[k] *= act_slope<act.value, true>(z[k]);
-                }
-                if (pos.in(R::kAcc * c + i))
-                    *reinterpret_cast<uint2*>(p.X + pos.at(p.ld, R::kAcc * c + i)) = pack4(v);
-            }
-        });
-        if (c + 1 < pos.kChunks) load(p, c + 1);
+            for (int j = 0; j < 16; ++j) w[j] = pack_bf16x2(v[2 * j], v[2 * j + 1]);
+        }
+        if (!right) stage_ready<1>(io);
+        stage_half(stage_buf(io, 0), io.lane, right, w);
+        if (right) out_commit(io, &p.xmap, stage_buf(io, 0), col0 - 32, io.row0);
     }
 
     __device__ __forceinline__ void finish(const Params&, int) {}

@@ -371,7 +371,7 @@ __global__ void __launch_bounds__(kThreads, 2)
                     }
                     with_act(ep.act, [&](auto act) {
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) z[j] = act_value<act.value, false>(z[j]);
+                        for (int j = 0; j < 4; ++j) z[j] = act_value<act.value>(z[j]);
                     });
                     if (ep.residual) {
 #pragma unroll
@@ -387,7 +387,7 @@ __global__ void __launch_bounds__(kThreads, 2)
                         const float z[4] = {z4.x, z4.y, z4.z, z4.w};
                         with_act(ep.act, [&](auto act) {
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) o[j] *= act_slope<act.value, false>(z[j]);
+                            for (int j = 0; j < 4; ++j) o[j] *= act_slope<act.value>(z[j]);
                         });
                     }
                     st4(ep.dX + off, o, nv, vec);

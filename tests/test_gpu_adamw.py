@@ -3,7 +3,7 @@ bits, with moments in fp32 and in 8 bits.
 
 Tolerances.  The moments are two fp32 operations each on terms of one sign or two: 2^-23 of the
 magnitudes.  The step is a quotient, a square root and five products and sums: 2^-20 of its terms'
-magnitudes; the weight one more rounding, 2^-24 of it.  The clip factor comes from fp32 sums of 2048
+magnitudes; the weight one more rounding, 2^-24 of it.  The clip factor comes from fp32 sums of at most 4096
 squares by trees of at most 24 additions and fp64 above: 2^-19.  8-bit codes equal the definition's but where
 value and random fraction come within 1e-4 of a unit of the border (the fp32 moments' error, at
 most 2^-22 of 16 units, is far below that): there the other one beside it is right too."""
@@ -17,8 +17,8 @@ pytestmark = pytest.mark.gpu
 
 BLOCK = 256
 HYPER = dict(lr=3e-3, beta1=0.9, beta2=0.99, eps=1e-8)
-# one element, a thread's 8, a block's 256, a chunk's 2048, and around them
-SIZES = [1, 7, 8, 9, 255, 256, 257, 1000, 2047, 2048, 2049, 4097, 65536, 70001]
+# one element, a thread's 8, a block's 256, a chunk's 2048 or 4096, and around them
+SIZES = [1, 7, 8, 9, 255, 256, 257, 511, 513, 1000, 2047, 2049, 4095, 4096, 4097, 9001, 65536, 70001]
 
 
 def decode_m(code, scale):
