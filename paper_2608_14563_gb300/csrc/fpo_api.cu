@@ -995,6 +995,7 @@ int32_t fpo_adamw_grouped(int32_t n_tensors, const fpo_adamw_tensor* tensors,
     r.a2 = static_cast<float>(1.0 - opt->beta2);
     r.inv_bc1 = static_cast<float>(1.0 / (1.0 - pow(opt->beta1, t)));
     r.inv_sqrt_bc2 = static_cast<float>(1.0 / sqrt(1.0 - pow(opt->beta2, t)));
+    r.one = 1.f;
     return cuda_status(launch_adamw(n_tensors, table.data(), r, seed, opt->step,
                                     static_cast<float*>(workspace), static_cast<cudaStream_t>(stream)));
 }

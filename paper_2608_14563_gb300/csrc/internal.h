@@ -228,6 +228,7 @@ struct AdamRates {
     float lr, eps, clip_frac;
     float b1, a1, b2, a2;         // decays, and 1 - them
     float inv_bc1, inv_sqrt_bc2;  // bias corrections 1 / (1 - b1^t), 1 / sqrt(1 - b2^t)
+    float one;                    // 1 (adamw.cu, add_rn)
 };
 // Floats of workspace a step with a clip needs.
 size_t adamw_workspace_floats(int n_tensors, const int64_t* n);

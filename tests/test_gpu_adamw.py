@@ -176,6 +176,17 @@ def test_steps_match_the_definition(fpo, bits, clip, sizes):
         check(x, before, t, clip)
 
 
+@pytest.mark.parametrize("n", [4096 * 7, 70001])
+def test_moments_are_rounded_as_written(fpo, n):
+    """Each product and sum of the new moments by itself, as any fp32 arithmetic has it."""
+    for g16 in (0, 1):
+        x = Tensors([n], 32, g16=g16)
+        g, m, v = x.G[0].float(), x.m[0].clone(), x.v[0].clone()
+        x.step(fpo, 3)
+        b1, b2 = HYPER["beta1"], HYPER["beta2"]
+        assert torch.equal(x.m[0], b1 * m + (1 - b1) * g) and torch.equal(x.v[0], b2 * v + (1 - b2) * g * g)
+
+
 def test_empty_tensors_are_skipped(fpo):
     for bits in (32, 8):
         for clip in (0, 1):
