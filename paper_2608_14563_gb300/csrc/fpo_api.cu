@@ -906,7 +906,6 @@ int32_t fpo_linear_vjp(int64_t T, int64_t d_out, int64_t d_in, int32_t dtype, in
         if (dbias) FPO_TRY(cudaMemsetAsync(dbias, 0, o * 4, st));
         return FPO_OK;
     }
-    FPO_TRY(clear(workspace, linear_vjp_clear_bytes(dtype, Ti, N, K), st));
     const LinearVjp p{Ti, N, K, act, act_in, dY, Z, X, W, Z_in, dX, dW, dbias};
     return cuda_status(launch_linear_vjp(dtype, p, workspace, st));
 }

@@ -170,12 +170,13 @@ inline SkPlan tail_plan(long long tiles, long long clusters, int k_blocks) {
 }
 
 // With sk_scratch non-null, the tiles are split by `split` k ranges each when that is above
-// 1, else those of the last partial wave by tail_plan (SegCursor); the caller then runs
-// sk_fixup over them (plan->tail_tiles > 0).  sk_scratch holds 256 x BN fp32 per unit.
+// 1, else those of the last partial wave by tail_plan, or as *tail says (SegCursor); the caller
+// then runs sk_fixup over them (plan->tail_tiles > 0).  sk_scratch holds 256 x BN fp32 per unit.
 template <int BN, bool A_MN, bool B_MN, int STAGES, int MAXG, class Epi>
 cudaError_t run_gemm_pair(const GemmMaps<MAXG>& maps, const typename Epi::Params& ep,
                           const GemmShape& sh_in, unsigned* status, cudaStream_t st,
-                          float* sk_scratch = nullptr, SkPlan* plan = nullptr, int split = 0) {
+                          float* sk_scratch = nullptr, SkPlan* plan = nullptr, int split = 0,
+                          const SkPlan* tail = nullptr) {
     if (plan) *plan = SkPlan{};
     if (sh_in.tiles <= 0 || sh_in.k_blocks <= 0) return cudaSuccess;
     using L = GemmPairSmem<BN, STAGES, pair_ksub<BN, A_MN, B_MN>()>;
@@ -196,7 +197,7 @@ cudaError_t run_gemm_pair(const GemmMaps<MAXG>& maps, const typename Epi::Params
             p.tail_tiles = sh.tiles;
             p.tail_split = split;
         } else {
-            p = tail_plan(sh.tiles, clusters, sh.k_blocks);
+            p = tail ? *tail : tail_plan(sh.tiles, clusters, sh.k_blocks);
         }
         if (p.tail_tiles > 0) {
             sh.tail_tiles = p.tail_tiles;

@@ -269,8 +269,8 @@ size_t linear_vjp_workspace_bytes(int dtype, int T, int N, int K, int act);
 // Bytes at the workspace's start that are zero before a call (0: the status word is written by the
 // call's kernel).
 size_t linear_clear_bytes(int dtype, int T, int N, int K);
-size_t linear_vjp_clear_bytes(int dtype, int T, int N, int K);
 cudaError_t launch_linear(int dtype, const LinearFwd& p, void* workspace, cudaStream_t st);
+// Clears what it needs of the workspace itself.
 cudaError_t launch_linear_vjp(int dtype, const LinearVjp& p, void* workspace, cudaStream_t st);
 // The fp32 products of the two (FFMA).
 cudaError_t launch_linear_f32(const LinearFwd& p, cudaStream_t st);

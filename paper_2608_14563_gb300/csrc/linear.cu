@@ -488,52 +488,44 @@ int linear_clusters() {
     return c;
 }
 
-// How a product runs: 128-column tiles, K ranges per tile (all of them, or with `tail` those of
-// the last partial wave), and the units of scratch.
+// How a product runs: 128-column tiles, k ranges of every tile (split), or of those of the last
+// partial wave (tail), and the units of scratch.
 struct PairPlan {
-    bool half = false, tail = false;
+    bool half = false;
     int split = 0;
+    SkPlan tail;
     long long units = 0;
 };
 
+// The cheapest by a 64-deep k-block of a 256 x 256 tile (325 ns), storing the parts of a wave of
+// units (2500), the fixup's launch (5000) and its read of a unit (100).  4096 x 4096 x 11008 (256
+// tiles on 76 clusters): the last 28 tiles whole 56 us, in 2 ranges 41, in the 5 that fill the waves
+// best 48 (the product 244 us).
 PairPlan pair_plan(int M, int N, int K) {
     PairPlan p;
     const long long tiles = static_cast<long long>((M + 255) / 256) * ((N + 255) / 256);
     const int kb = (K + kBK - 1) / kBK;
     const long long clusters = linear_clusters();
-    const double block_ns = 344.0;  // a 64-deep k-block of a 256 x 256 pair tile under load
-    auto parts_ns = [](double waves, double units) {  // store and sum of the parts, a launch
-        return waves * 2500.0 + 4000.0 + units * 262144.0 / 4300.0;
-    };
-    if (tiles >= clusters) {
-        const SkPlan t = tail_plan(tiles, clusters, kb);
-        if (t.tail_tiles > 0) {
-            const long long units = t.tail_tiles * t.tail_split;
-            const double waves = static_cast<double>((units + clusters - 1) / clusters);
-            const double split = waves * ((kb + t.tail_split - 1) / t.tail_split) * block_ns +
-                                 parts_ns(waves, static_cast<double>(units));
-            if (split < kb * block_ns) {
-                p.tail = true;
-                p.units = units;
-            }
-        }
-        return p;
-    }
-    double best = kb * block_ns;
+    const long long left = tiles < clusters ? tiles : tiles % clusters;
+    if (left == 0) return p;
+    double best = kb * 325.0;
     if (2 * tiles <= clusters) {
         p.half = true;
-        best = kb * block_ns * 0.6;
+        best = kb * 195.0;
     }
-    for (int S = 2; S <= 32 && kb / S >= 8 && tiles * S <= kTailWaves * clusters; ++S) {
-        const double waves = static_cast<double>((tiles * S + clusters - 1) / clusters);
-        const double cost = waves * ((kb + S - 1) / S) * block_ns +
-                            parts_ns(waves, static_cast<double>(tiles * S));
-        if (cost < best) {
-            best = cost;
-            p.half = false;
-            p.split = S;
-            p.units = tiles * S;
-        }
+    for (int S = 2; S <= 32 && kb / S >= 8 && left * S <= kTailWaves * clusters; ++S) {
+        const double waves = static_cast<double>((left * S + clusters - 1) / clusters);
+        const double cost = waves * (((kb + S - 1) / S) * 325.0 + 2500.0) + 5000.0 + left * S * 100.0;
+        if (cost >= best) continue;
+        best = cost;
+        p.half = false;
+        p.units = left * S;
+        p.split = S;
+    }
+    if (tiles >= clusters && p.units > 0) {
+        p.tail.tail_tiles = left;
+        p.tail.tail_split = p.split;
+        p.split = 0;
     }
     return p;
 }
@@ -580,7 +572,7 @@ cudaError_t run_pair(const void* A, const void* B, int M, int N, int K, const Ou
     const GemmShape sh = make_shape(M, N, K, 256, 1, band_for(true), kPairBM);
     SkPlan plan;
     const cudaError_t e = run_gemm_pair<256, A_MN, B_MN, kPairStages, 1, Epi<256>>(
-        maps, ep, sh, status, st, pp.units > 0 ? scratch : nullptr, &plan, pp.split);
+        maps, ep, sh, status, st, pp.units > 0 ? scratch : nullptr, &plan, pp.split, &pp.tail);
     if (e != cudaSuccess || plan.tail_tiles <= 0) return e;
     return launch_chained(linear_fixup_kernel<Out>, sk_fixup_grid<256>(plan), kFixupThreads, 0, st,
                           sk_fixup_shape(plan, sh), static_cast<const float*>(scratch), out);
@@ -620,13 +612,19 @@ __device__ __forceinline__ void sig_store(T* p, const float (&x)[kV]) {
     }
 }
 
+// status (or null): this kernel is the call's first and clears it and `clear_words` words behind it.
+// With more ranges than one the last block of a column group to finish (counters, zero at the start)
+// adds the ranges' sums in their order.
 template <typename T, int kV>
 __global__ void __launch_bounds__(kSigThreads)
-    signal_kernel(const T* dY, const T* Z, int act, int rows, int N, int rows_per, T* dZ,
-                  float* part) {
+    signal_kernel(const T* dY, const T* Z, int act, int rows, int N, int rows_per, T* dZ, float* part,
+                  float* dbias, unsigned* counters, unsigned* status, int clear_words) {
     __shared__ float sums[kSigRows][kSigLanes * kV + 1];
+    __shared__ bool last;
     grid_dependency_trigger();
     grid_dependency_wait();
+    if (status && blockIdx.x == 0 && blockIdx.y == 0)
+        for (int i = threadIdx.x; i < clear_words; i += kSigThreads) status[i] = 0u;
     const int lane = threadIdx.x % kSigLanes, row_lane = threadIdx.x / kSigLanes;
     const int col = (blockIdx.x * kSigLanes + lane) * kV;
     const int r0 = blockIdx.y * rows_per, r1 = min(rows, r0 + rows_per);
@@ -635,7 +633,7 @@ __global__ void __launch_bounds__(kSigThreads)
     for (int k = 0; k < kV; ++k) s[k] = 0.f;
     if (col < N) {
         with_act(Z ? act : kActNone, [&](auto a) {
-#pragma unroll 4
+#pragma unroll 8
             for (int r = r0 + row_lane; r < r1; r += kSigRows) {
                 const long long o = static_cast<long long>(r) * N + col;
                 float x[kV];
@@ -661,30 +659,33 @@ __global__ void __launch_bounds__(kSigThreads)
             }
         });
     }
-    if (!part) return;
+    if (!dbias) return;
 #pragma unroll
     for (int k = 0; k < kV; ++k) sums[row_lane][lane * kV + k] = s[k];
     __syncthreads();
-    for (int c = threadIdx.x; c < kSigLanes * kV; c += kSigThreads) {
-        const int n = blockIdx.x * kSigLanes * kV + c;
-        if (n >= N) continue;
-        float t = 0.f;
+    const int c = threadIdx.x, n = blockIdx.x * kSigLanes * kV + c;
+    const bool mine = c < kSigLanes * kV && n < N;
+    float t = 0.f;
+    if (mine) {
 #pragma unroll
         for (int r = 0; r < kSigRows; ++r) t += sums[r][c];
-        part[static_cast<long long>(blockIdx.y) * N + n] = t;
     }
-}
-
-// dbias = the ranges' sums in order.
-__global__ void __launch_bounds__(kSigThreads)
-    bias_sum_kernel(const float* part, int ranges, int N, float* dbias) {
-    grid_dependency_trigger();
-    grid_dependency_wait();
-    const int n = blockIdx.x * kSigThreads + threadIdx.x;
-    if (n >= N) return;
-    float t = 0.f;
-#pragma unroll 8
-    for (int r = 0; r < ranges; ++r) t += part[static_cast<long long>(r) * N + n];
+    if (gridDim.y == 1) {
+        if (mine) dbias[n] = t;
+        return;
+    }
+    if (mine) part[static_cast<long long>(blockIdx.y) * N + n] = t;
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) last = atomicAdd(counters + blockIdx.x, 1u) == gridDim.y - 1;
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    if (!mine) return;
+    t = 0.f;
+#pragma unroll 16
+    for (int r = 0; r < static_cast<int>(gridDim.y); ++r)
+        t += __ldcg(part + static_cast<long long>(r) * N + n);
     dbias[n] = t;
 }
 
@@ -698,7 +699,7 @@ SignalPlan signal_plan(int dtype, int T, int N) {
     const int per = kSigLanes * sig_v(dtype, N);
     SignalPlan p;
     p.cols = (N + per - 1) / per;
-    const long long blocks = 8LL * sm_count();
+    const long long blocks = 4LL * sm_count();
     long long ranges = blocks / p.cols;
     const long long most = (T + 63) / 64;  // of at least 64 rows
     if (ranges > most) ranges = most;
@@ -708,17 +709,18 @@ SignalPlan signal_plan(int dtype, int T, int N) {
     return p;
 }
 
+size_t signal_counter_bytes(const SignalPlan& p) {
+    return p.ranges > 1 ? up256(static_cast<size_t>(p.cols) * sizeof(unsigned)) : 0;
+}
+
 template <typename T, int kV>
-cudaError_t run_signal_v(const LinearVjp& p, T* dZ, float* part, const SignalPlan& sp,
-                         cudaStream_t st) {
-    float* to = p.dbias && sp.ranges == 1 ? p.dbias : p.dbias ? part : nullptr;
-    const cudaError_t e = launch_chained(
+cudaError_t run_signal_v(const LinearVjp& p, T* dZ, float* part, unsigned* counters, unsigned* status,
+                         size_t clear_bytes, const SignalPlan& sp, cudaStream_t st) {
+    return launch_chained(
         signal_kernel<T, kV>, dim3(sp.cols, sp.ranges), kSigThreads, 0, st,
         static_cast<const T*>(p.dY), static_cast<const T*>(p.act != kActNone ? p.Z : nullptr), p.act,
-        p.T, p.N, sp.rows_per, dZ, to);
-    if (e != cudaSuccess || !p.dbias || sp.ranges == 1) return e;
-    return launch_chained(bias_sum_kernel, dim3((p.N + kSigThreads - 1) / kSigThreads), kSigThreads,
-                          0, st, static_cast<const float*>(part), sp.ranges, p.N, p.dbias);
+        p.T, p.N, sp.rows_per, dZ, part, p.dbias, counters, status,
+        static_cast<int>(clear_bytes / sizeof(unsigned)));
 }
 
 }  // namespace
@@ -757,18 +759,21 @@ cudaError_t launch_linear(int dtype, const LinearFwd& p, void* workspace, cudaSt
 
 namespace {
 
-// The backward pass's workspace: status word, counters of few_tokens_kernel, dZ (with an
-// activation), the bias ranges' sums, scratch of the products' parts.
+// The backward pass's workspace: status word, counters of few_tokens_kernel and of signal_kernel,
+// dZ (with an activation), the bias ranges' sums, scratch of the products' parts.
 struct VjpLayout {
-    size_t dz, part, scratch, total;
+    size_t few, sig, clear, dz, part, scratch, total;
 };
 VjpLayout vjp_layout(int dtype, int T, int N, int K, int act) {
     VjpLayout l;
-    size_t off = kHead + (dtype == 1 && T <= kFewT ? few_counter_bytes(K) : 0);
-    l.dz = off;
+    const SignalPlan sp = signal_plan(dtype, T, N);
+    l.few = kHead;
+    l.sig = l.few + (dtype == 1 && T <= kFewT ? few_counter_bytes(K) : 0);
+    l.clear = l.dz = l.sig + signal_counter_bytes(sp);
+    size_t off = l.dz;
     if (act != kActNone) off = up256(off + static_cast<size_t>(T) * N * (dtype == 1 ? 2 : 4));
     l.part = off;
-    off = up256(off + static_cast<size_t>(signal_plan(dtype, T, N).ranges) * N * sizeof(float));
+    off = up256(off + static_cast<size_t>(sp.ranges) * N * sizeof(float));
     l.scratch = off;
     size_t scratch = 0;
     if (dtype == 1) {
@@ -782,9 +787,6 @@ VjpLayout vjp_layout(int dtype, int T, int N, int K, int act) {
 
 }  // namespace
 
-size_t linear_vjp_clear_bytes(int dtype, int T, int N, int K) {
-    return dtype == 1 && T <= kFewT ? kHead + few_counter_bytes(K) : sizeof(unsigned);
-}
 size_t linear_vjp_workspace_bytes(int dtype, int T, int N, int K, int act) {
     return T == 0 ? kHead : vjp_layout(dtype, T, N, K, act).total;
 }
@@ -793,20 +795,30 @@ cudaError_t launch_linear_vjp(int dtype, const LinearVjp& p, void* workspace, cu
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     unsigned* status = reinterpret_cast<unsigned*>(ws);
     const VjpLayout l = vjp_layout(dtype, p.T, p.N, p.K, p.act);
+    const SignalPlan sp = signal_plan(dtype, p.T, p.N);
     float* part = reinterpret_cast<float*>(ws + l.part);
     float* scratch = reinterpret_cast<float*>(ws + l.scratch);
-    const void* dZ = p.dY;
+    const bool signal = p.act != kActNone || p.dbias;
+    // one range of rows: no counters, and signal_kernel clears what the products need.  That it may
+    // start before the kernel in front of the call has ended is in its own wait's hands
+    const bool clears = signal && sp.ranges == 1;
     cudaError_t e = cudaSuccess;
-    if (p.act != kActNone) dZ = ws + l.dz;
-    if (p.act != kActNone || p.dbias) {
-        const SignalPlan sp = signal_plan(dtype, p.T, p.N);
+    if (!clears) e = cudaMemsetAsync(ws, 0, l.clear, st);
+    if (e != cudaSuccess) return e;
+    const void* dZ = p.act != kActNone ? ws + l.dz : p.dY;
+    if (signal) {
         void* to = p.act != kActNone ? ws + l.dz : nullptr;
+        unsigned* counters = reinterpret_cast<unsigned*>(ws + l.sig);
+        unsigned* first = clears ? status : nullptr;
         if (dtype == 1)
-            e = run_signal_v<__nv_bfloat16, 8>(p, static_cast<__nv_bfloat16*>(to), part, sp, st);
+            e = run_signal_v<__nv_bfloat16, 8>(p, static_cast<__nv_bfloat16*>(to), part, counters,
+                                               first, l.clear, sp, st);
         else if (sig_v(dtype, p.N) == 4)
-            e = run_signal_v<float, 4>(p, static_cast<float*>(to), part, sp, st);
+            e = run_signal_v<float, 4>(p, static_cast<float*>(to), part, counters, first, l.clear, sp,
+                                       st);
         else
-            e = run_signal_v<float, 1>(p, static_cast<float*>(to), part, sp, st);
+            e = run_signal_v<float, 1>(p, static_cast<float*>(to), part, counters, first, l.clear, sp,
+                                       st);
         if (e != cudaSuccess) return e;
     }
     if (dtype == 0) {
@@ -828,9 +840,9 @@ cudaError_t launch_linear_vjp(int dtype, const LinearVjp& p, void* workspace, cu
         out.M = p.T;
         out.N = p.K;
         out.act = p.act_in;
-        e = p.T <= kFewT ? run_few<true>(p.W, dZ, p.K, p.N, p.T, out, ws + kHead, scratch, status, st)
-                         : run_pair<false, true, EpiSlope>(dZ, p.W, p.T, p.K, p.N, out, scratch,
-                                                           status, st);
+        e = p.T <= kFewT
+                ? run_few<true>(p.W, dZ, p.K, p.N, p.T, out, ws + l.few, scratch, status, st)
+                : run_pair<false, true, EpiSlope>(dZ, p.W, p.T, p.K, p.N, out, scratch, status, st);
         if (e != cudaSuccess) return e;
     }
     if (!p.dW) return cudaSuccess;
