@@ -38,6 +38,7 @@ size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 //   warps 2..5  epilogue: one feature per lane
 // Bound: the weights' bytes.
 constexpr int kFewT = 32;
+constexpr int kFewAhead = 4;  // CTAs' sums in flight
 
 template <int BT>
 struct FewSmem {
@@ -68,37 +69,36 @@ __device__ __forceinline__ int few_owner(const FewShape& s, long long u, long lo
     return static_cast<int>(((u + 1) * C - 1) / s.units);
 }
 
-// One feature of the tokens from t0 on through the epilogue: consecutive lanes are consecutive
-// features.  What it reads is loaded for all tokens before anything is stored (a load behind a store
+// One feature of the n tokens through the epilogue: consecutive lanes are consecutive features.  What it reads is loaded for all tokens before anything is stored (a load behind a store
 // to memory that may be the same waits for itself alone: 128 tokens took 110 us instead of 35).
+template <int BT>
 __device__ __forceinline__ void few_load(const __nv_bfloat16* p, long long o, long long ld, int n,
-                                         uint16_t (&u)[32]) {
+                                         uint16_t (&u)[BT]) {
     const uint16_t* q = reinterpret_cast<const uint16_t*>(p) + o;
 #pragma unroll
-    for (int j = 0; j < 32; ++j) u[j] = j < n ? q[j * ld] : 0;
+    for (int j = 0; j < BT; ++j) u[j] = j < n ? q[j * ld] : 0;
 }
 __device__ __forceinline__ float bf16_bits(uint16_t u) {
     return __uint_as_float(static_cast<uint32_t>(u) << 16);
 }
-__device__ __forceinline__ void few_out(const LinearOut& p, int feature, int t0, int n,
-                                        float (&v)[32]) {
+template <int BT>
+__device__ __forceinline__ void few_out(const LinearOut& p, int feature, int n, float (&v)[BT]) {
     if (feature >= p.N) return;
-    const long long o = t0 * p.ld + feature;
-    uint16_t r[32];
-    if (p.residual) few_load(p.residual, o, p.ld, n, r);
+    uint16_t r[BT];
+    if (p.residual) few_load(p.residual, feature, p.ld, n, r);
     if (p.bias) {
         const float bias = __bfloat162float(p.bias[feature]);
 #pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] += bias;
+        for (int j = 0; j < BT; ++j) v[j] += bias;
     }
     if (p.Z) {
 #pragma unroll
-        for (int j = 0; j < 32; ++j)
-            if (j < n) p.Z[o + j * p.ld] = __float2bfloat16_rn(v[j]);
+        for (int j = 0; j < BT; ++j)
+            if (j < n) p.Z[j * p.ld + feature] = __float2bfloat16_rn(v[j]);
     }
     with_act(p.act, [&](auto act) {
 #pragma unroll
-        for (int j = 0; j < 32; j += 2) {
+        for (int j = 0; j < BT; j += 2) {
             if (j >= n) break;
             const float2 y = act_value2<act.value>(make_float2(v[j], v[j + 1]));
             v[j] = y.x;
@@ -106,19 +106,19 @@ __device__ __forceinline__ void few_out(const LinearOut& p, int feature, int t0,
         }
     });
 #pragma unroll
-    for (int j = 0; j < 32; ++j)
-        if (j < n) p.Y[o + j * p.ld] = __float2bfloat16_rn(p.residual ? v[j] + bf16_bits(r[j]) : v[j]);
+    for (int j = 0; j < BT; ++j)
+        if (j < n)
+            p.Y[j * p.ld + feature] = __float2bfloat16_rn(p.residual ? v[j] + bf16_bits(r[j]) : v[j]);
 }
-__device__ __forceinline__ void few_out(const SlopeOut& p, int feature, int t0, int n,
-                                        float (&v)[32]) {
+template <int BT>
+__device__ __forceinline__ void few_out(const SlopeOut& p, int feature, int n, float (&v)[BT]) {
     if (feature >= p.N) return;
-    const long long o = t0 * p.ld + feature;
     if (p.z) {
-        uint16_t z[32];
-        few_load(p.z, o, p.ld, n, z);
+        uint16_t z[BT];
+        few_load(p.z, feature, p.ld, n, z);
         with_act(p.act, [&](auto act) {
 #pragma unroll
-            for (int j = 0; j < 32; j += 2) {
+            for (int j = 0; j < BT; j += 2) {
                 if (j >= n) break;
                 const float2 s = act_slope2<act.value>(make_float2(bf16_bits(z[j]), bf16_bits(z[j + 1])));
                 v[j] *= s.x;
@@ -127,8 +127,8 @@ __device__ __forceinline__ void few_out(const SlopeOut& p, int feature, int t0, 
         });
     }
 #pragma unroll
-    for (int j = 0; j < 32; ++j)
-        if (j < n) p.X[o + j * p.ld] = __float2bfloat16_rn(v[j]);
+    for (int j = 0; j < BT; ++j)
+        if (j < n) p.X[j * p.ld + feature] = __float2bfloat16_rn(v[j]);
 }
 
 template <int BT, bool W_MN, class Out>
@@ -139,7 +139,8 @@ __global__ void __launch_bounds__(192, 1)
     using L = FewSmem<BT>;
     constexpr int kStages = L::kStages;
     constexpr uint32_t kIdesc = idesc_bf16_f32(kBM, BT, W_MN, false);
-    constexpr int kAccCols = BT < 32 ? 32 : BT;
+    static_assert(BT <= 32, "one load of the accumulator");
+    constexpr int kAccCols = 32;
     constexpr int kTmemCols = 2 * kAccCols;
 
     extern __shared__ uint8_t smem_raw[];
@@ -266,27 +267,21 @@ __global__ void __launch_bounds__(192, 1)
                 return true;
             };
             if (!ready()) break;
-            float* slot = sh.scratch + (static_cast<long long>(2 * blockIdx.x + (kb == 0)) * BT) * kBM +
-                          q * 32 + lane;
-#pragma unroll 1
-            for (int t0 = 0; t0 < sh.T; t0 += 32) {
-                float v[32];
-                tmem_ld_32x32b_x32(t_row + t0, v);
-                if (t0 + 32 >= sh.T) {
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(tempty_bar(acc));
-                }
-                const int n = min(32, sh.T - t0);
-                if (whole) {
-                    few_out(out, feature, t0, n, v);
-                } else {
+            float w[32], v[BT];
+            tmem_ld_32x32b_x32(t_row, w);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(tempty_bar(acc));
 #pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        if (j < n) slot[(t0 + j) * kBM] = v[j];
-                }
-            }
-            if (!whole) {
+            for (int j = 0; j < BT; ++j) v[j] = w[j];
+            if (whole) {
+                few_out(out, feature, sh.T, v);
+            } else {
+                float* slot = sh.scratch +
+                              (static_cast<long long>(2 * blockIdx.x + (kb == 0)) * BT) * kBM + q * 32 + lane;
+#pragma unroll
+                for (int j = 0; j < BT; ++j)
+                    if (j < sh.T) slot[j * kBM] = v[j];
                 // the last of the tile's CTAs adds their sums
                 const long long first_unit = static_cast<long long>(tile) * sh.k_blocks;
                 const int c0 = few_owner(sh, first_unit, C);
@@ -298,23 +293,31 @@ __global__ void __launch_bounds__(192, 1)
                 before = __shfl_sync(0xffffffffu, before, 0);
                 if (before == static_cast<unsigned>(c1 - c0)) {
                     __threadfence();
-#pragma unroll 1
-                    for (int t0 = 0; t0 < sh.T; t0 += 32) {
-                        const int n = min(32, sh.T - t0);
-                        float v[32];
+                    // (CTA c0 has the tile's first k-blocks: its odd slot)
+                    const float* s0 =
+                        sh.scratch + static_cast<long long>(2 * c0 + 1) * BT * kBM + q * 32 + lane;
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = 0.f;
+                    for (int j = 0; j < BT; ++j) v[j] = j < sh.T ? __ldcg(s0 + j * kBM) : 0.f;
+                    // several CTAs' loads in flight: one by one each waits for L2
 #pragma unroll 1
-                        for (int c = c0; c <= c1; ++c) {
-                            const float* s =
-                                sh.scratch + (static_cast<long long>(2 * c + (c == c0)) * BT + t0) * kBM +
-                                q * 32 + lane;
+                    for (int c = c0 + 1; c <= c1; c += kFewAhead) {
+                        float x[kFewAhead][BT];
 #pragma unroll
-                            for (int j = 0; j < 32; ++j)
-                                if (j < n) v[j] += __ldcg(s + j * kBM);
+                        for (int i = 0; i < kFewAhead; ++i) {
+                            const float* s = sh.scratch +
+                                             static_cast<long long>(2 * min(c + i, c1)) * BT * kBM +
+                                             q * 32 + lane;
+#pragma unroll
+                            for (int j = 0; j < BT; ++j) x[i][j] = j < sh.T ? __ldcg(s + j * kBM) : 0.f;
                         }
-                        few_out(out, feature, t0, n, v);
+#pragma unroll
+                        for (int i = 0; i < kFewAhead; ++i) {
+                            if (c + i > c1) break;
+#pragma unroll
+                            for (int j = 0; j < BT; ++j) v[j] += x[i][j];
+                        }
                     }
+                    few_out(out, feature, sh.T, v);
                 }
             }
             if (++acc == 2) { acc = 0; acc_phase ^= 1u; }

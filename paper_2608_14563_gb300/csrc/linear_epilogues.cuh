@@ -118,6 +118,14 @@ struct EpiLinear {
     __device__ __forceinline__ EpiLinear(const Params& p, int, int row, int n0) {
         res = p.o.residual && row < p.o.M ? p.o.residual + row * p.o.ld : nullptr;
         if (p.o.residual) r.load(res, n0, p.o.N);
+        // the tile's bias into L1 while the mainloop runs: each chunk's load of it would wait for L2
+        const int c = n0 + 8 * static_cast<int>(threadIdx.x & 31);
+        if (p.o.bias && c < n0 + BN && c < p.o.N) touch(p.o.bias + c);
+    }
+
+    static __device__ __forceinline__ void touch(const __nv_bfloat16* p) {
+        uint32_t u;
+        asm volatile("ld.global.u32 %0, [%1];" : "=r"(u) : "l"(p));
     }
 
     __device__ __forceinline__ void chunk(const Params& p, const float (&v)[32], int col0, int c0,
