@@ -662,8 +662,10 @@ class _Entry:
         functools.update_wrapper(self, fn)
 
     def __call__(self, *args, **kw):
+        here = _current_device()
         for t in (*args, *kw.values()):
-            if isinstance(t, torch.Tensor):
+            # (-1: not CUDA memory, which _ptr refuses)
+            if isinstance(t, torch.Tensor) and t.get_device() not in (here, -1):
                 _on_current_device(t)
         return self.__wrapped__(*args, **kw)
 
