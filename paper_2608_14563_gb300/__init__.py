@@ -280,14 +280,24 @@ def _ptr(t):
     return t.data_ptr()
 
 
+_is_contiguous, _data_ptr, _numel = (
+    torch.Tensor.is_contiguous, torch.Tensor.data_ptr, torch.Tensor.numel)
+
+
 def _ptrs(ts):
-    """_ptr of a list (0 for None), on the current device."""
-    here = _current_device()
-    for t in ts:
-        if t is not None and (t.get_device() != here or not t.is_contiguous()):
+    """_ptr of every entry of a list (0 for None), all on the current device."""
+    some = [t for t in ts if t is not None]
+    devices = {t.get_device() for t in some}
+    if (len(devices) > 1 or -1 in devices or devices - {_current_device()}
+            or not all(map(_is_contiguous, some))):
+        for t in some:
             _on_current_device(t)
             _ptr(t)
-    return [0 if t is None else t.data_ptr() for t in ts]
+    ptrs = list(map(_data_ptr, some))
+    if len(some) == len(ts):
+        return ptrs
+    it = iter(ptrs)
+    return [0 if t is None else next(it) for t in ts]
 
 
 # torch's private call for a stream's handle, where this torch has it
@@ -662,10 +672,9 @@ class _Entry:
         functools.update_wrapper(self, fn)
 
     def __call__(self, *args, **kw):
-        here = _current_device()
-        for t in (*args, *kw.values()):
-            # (-1: not CUDA memory, which _ptr refuses)
-            if isinstance(t, torch.Tensor) and t.get_device() not in (here, -1):
+        ts = [t for t in (*args, *kw.values()) if isinstance(t, torch.Tensor)]
+        if len({t.get_device() for t in ts}) > 1:  # (of one device: the leading tensor's check)
+            for t in ts:
                 _on_current_device(t)
         return self.__wrapped__(*args, **kw)
 
@@ -736,6 +745,9 @@ def adamw_workspace(sizes, clip=CLIP_NONE) -> int:
     return int(_lib.fpo_adamw_workspace(len(sizes), (_i64 * len(sizes))(*sizes), int(clip)))
 
 
+_DTYPES = {torch.bfloat16: BF16}
+
+
 @_Entry
 def adamw_grouped(Gs, opt, W_masters, states1, states2, *, scales1=None, scales2=None, W_outs=None,
                   weight_decays=None, seed=0, workspace=None, stream=None):
@@ -750,14 +762,16 @@ def adamw_grouped(Gs, opt, W_masters, states1, states2, *, scales1=None, scales2
     rest = (W_masters, states1, states2, scales1, scales2, W_outs, weight_decays)
     if n == 0 or any(ts is not None and len(ts) != n for ts in rest):
         raise ValueError("one entry per tensor expected in every list")
-    sizes = [G.numel() for G in Gs]
+    sizes = list(map(_numel, Gs))
     m_types = [m.dtype for m in states1]
     small = [dt != torch.float32 for dt in m_types]
     none = [None] * n
-    scales1, scales2, W_outs = scales1 or none, scales2 or none, W_outs or none
+    scales1 = none if scales1 is None else scales1
+    scales2 = none if scales2 is None else scales2
+    W_outs = none if W_outs is None else W_outs
 
     def check(name, ts, counts, types):
-        if [t.numel() for t in ts] != counts or [t.dtype for t in ts] != types:
+        if list(map(_numel, ts)) != counts or [t.dtype for t in ts] != types:
             for t, c, want in zip(ts, counts, types):
                 if t.dtype != want or t.numel() != c:
                     raise ValueError(f"{name}: expected {c} elements of {want}, got {t.numel()} of {t.dtype}")
@@ -786,8 +800,8 @@ def adamw_grouped(Gs, opt, W_masters, states1, states2, *, scales1=None, scales2
 
     desc = AdamwDesc(rate("lr"), rate("beta1"), rate("beta2"), rate("eps", "adam_eps"), rate("clip_frac"),
                      opt.step, opt.clip)
-    g_types = [_dtype_code(G) for G in Gs]
-    w_types = [F32 if t is None else BF16 if t.dtype == torch.bfloat16 else _dtype_code(t) for t in W_outs]
+    g_types = [_DTYPES.get(G.dtype) or _dtype_code(G) for G in Gs]
+    w_types = [F32 if t is None else _DTYPES.get(t.dtype) or _dtype_code(t) for t in W_outs]
     decays = [rate("weight_decay")] * n if weight_decays is None else [float(w) for w in weight_decays]
     cols = [_ptrs(ts) for ts in (Gs, W_masters, W_outs, states1, states2, scales1, scales2)]
     table = b"".join(map(_ADAMW_TENSOR.pack, sizes, *cols, g_types, w_types,

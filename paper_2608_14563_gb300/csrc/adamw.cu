@@ -253,21 +253,23 @@ __device__ __forceinline__ float2 add_rn(float2 a, float2 b, float one) {
     return __ffma2_rn(a, both(one), b);
 }
 
-template <int kPer>
+// kNew: m and v advance by g; else they have.  d: the unclipped step.
+template <bool kNew, int kPer>
 __device__ __forceinline__ void adamw_step(const AdamRates& op, float wd, float gscale,
                                            const float (&g)[kPer], const float (&w)[kPer],
                                            float (&m)[kPer], float (&v)[kPer], float (&d)[kPer]) {
 #pragma unroll
     for (int k = 0; k < kPer; k += 2) {
-        const float2 g2 = __fmul2_rn(make_float2(g[k], g[k + 1]), both(gscale));
-        const float2 m2 = add_rn(__fmul2_rn(both(op.b1), make_float2(m[k], m[k + 1])),
-                                 __fmul2_rn(both(op.a1), g2), op.one);
-        const float2 v2 = add_rn(__fmul2_rn(both(op.b2), make_float2(v[k], v[k + 1])),
-                                 __fmul2_rn(__fmul2_rn(both(op.a2), g2), g2), op.one);
-        m[k] = m2.x;
-        m[k + 1] = m2.y;
-        v[k] = v2.x;
-        v[k + 1] = v2.y;
+        float2 m2 = make_float2(m[k], m[k + 1]), v2 = make_float2(v[k], v[k + 1]);
+        if constexpr (kNew) {
+            const float2 g2 = __fmul2_rn(make_float2(g[k], g[k + 1]), both(gscale));
+            m2 = add_rn(__fmul2_rn(both(op.b1), m2), __fmul2_rn(both(op.a1), g2), op.one);
+            v2 = add_rn(__fmul2_rn(both(op.b2), v2), __fmul2_rn(__fmul2_rn(both(op.a2), g2), g2), op.one);
+            m[k] = m2.x;
+            m[k + 1] = m2.y;
+            v[k] = v2.x;
+            v[k + 1] = v2.y;
+        }
         const float2 den = __ffma2_rn(make_float2(sqrt_approx(v2.x), sqrt_approx(v2.y)),
                                       both(op.inv_sqrt_bc2), both(op.eps));
         const float2 q = __fmul2_rn(__fmul2_rn(m2, both(op.inv_bc1)),
@@ -293,17 +295,24 @@ struct Entry {
     bool g16, out16;
 };
 
-// What a pass does with a warp's elements from i0: the clip's sums (kNorms, of the step where
-// op.clip is 1, else of the gradient) or the step itself.  kFull: all of them are there; else the
-// first at least is.
-template <bool kNorms, bool kState8, bool kFull>
+// The passes.  kStep: the whole step.  kNorms: the clip's sums, of the step where op.clip is 1, else
+// of the gradient.  fp32 moments with the clip on the step advance in the first pass already
+// (kMoments), and the step is taken from them (kApply): 40 bytes an element instead of 42.  (8-bit
+// ones would have been rounded by then.)
+enum Pass { kStep, kNorms, kMoments, kApply };
+
+// What a pass does with a warp's elements from i0.  kFull: all of them are there; else the first at
+// least is.
+template <Pass kPass, bool kState8, bool kFull>
 __device__ __forceinline__ void take(const AdamRates& op, const Entry& e, long long i0, float gscale,
                                      float sscale, float& ww, float& xx) {
     constexpr int kQuads = Share<kState8>::kQuads, kPer = Share<kState8>::kPer;
     float g[kPer], w[kPer], m[kPer], v[kPer];
     const int lane = threadIdx.x & 31;
     const long long n = e.n, i1 = i0 + 4 * lane;
-    if (e.g16) {
+    if (kPass == kApply) {
+        // no gradient is needed
+    } else if (e.g16) {
 #pragma unroll
         for (int q = 0; q < kQuads; ++q)
             load4<kFull>(static_cast<const __nv_bfloat16*>(e.g), i1 + 128 * q, n, g + 4 * q);
@@ -314,7 +323,7 @@ __device__ __forceinline__ void take(const AdamRates& op, const Entry& e, long l
     }
 #pragma unroll
     for (int q = 0; q < kQuads; ++q) load4<kFull>(e.w, i1 + 128 * q, n, w + 4 * q);
-    if (kNorms && op.clip == 2) {  // the gradient's norm needs no state
+    if (kPass == kNorms && op.clip == 2) {  // the gradient's norm needs no state
 #pragma unroll
         for (int k = 0; k < kPer; ++k) {
             ww = fmaf(w[k], w[k], ww);
@@ -344,8 +353,15 @@ __device__ __forceinline__ void take(const AdamRates& op, const Entry& e, long l
         }
     }
     float d[kPer];
-    adamw_step(op, e.wd, gscale, g, w, m, v, d);
-    if constexpr (kNorms) {
+    adamw_step<kPass != kApply>(op, e.wd, gscale, g, w, m, v, d);
+    auto store_moments = [&] {
+#pragma unroll
+        for (int q = 0; q < kQuads; ++q) {
+            store4<kFull>(static_cast<float*>(e.m), i1 + 128 * q, n, m + 4 * q);
+            store4<kFull>(static_cast<float*>(e.v), i1 + 128 * q, n, v + 4 * q);
+        }
+    };
+    if constexpr (kPass == kNorms || kPass == kMoments) {
 #pragma unroll
         for (int k = 0; k < kPer; ++k) {
             // (no element: eps 0 would divide by 0)
@@ -353,6 +369,7 @@ __device__ __forceinline__ void take(const AdamRates& op, const Entry& e, long l
             ww = fmaf(w[k], w[k], ww);
             xx = fmaf(d[k], d[k], xx);
         }
+        if constexpr (kPass == kMoments) store_moments();
         return;
     }
 #pragma unroll
@@ -389,12 +406,8 @@ __device__ __forceinline__ void take(const AdamRates& op, const Entry& e, long l
             e.ms[block] = msc;
             e.vs[block] = vsc;
         }
-    } else {
-#pragma unroll
-        for (int q = 0; q < kQuads; ++q) {
-            store4<kFull>(static_cast<float*>(e.m), i1 + 128 * q, n, m + 4 * q);
-            store4<kFull>(static_cast<float*>(e.v), i1 + 128 * q, n, v + 4 * q);
-        }
+    } else if constexpr (kPass == kStep) {
+        store_moments();
     }
 }
 
@@ -404,15 +417,17 @@ __device__ __forceinline__ float warp_sum(float x) {
     return x;
 }
 
-// kNorms: part[chunk] = the chunk's two sums.  Else scales[tensor] (null: 1) clips the step.
-template <int CAP, bool kNorms, bool kState8>
-__global__ void __launch_bounds__(kThreads, kNorms ? (kState8 ? 5 : 3) : (kState8 ? 4 : 2))
+constexpr bool sums(Pass p) { return p == kNorms || p == kMoments; }
+
+// Passes with sums: part[chunk] = the chunk's two.  Else scales[tensor] (null: 1) clips the step.
+template <int CAP, Pass kPass, bool kState8>
+__global__ void __launch_bounds__(kThreads, kPass == kNorms ? (kState8 ? 5 : 3) : (kState8 ? 4 : 2))
     adamw_kernel(const __grid_constant__ Table<CAP> t, const __grid_constant__ AdamRates op,
                  float2* __restrict__ part, const float* __restrict__ scales) {
     using S = Share<kState8>;
     const int warp = threadIdx.x / 32;
     // behind a norms pass from the end: what that pass read last is still in L2
-    const int c = !kNorms && scales ? gridDim.x - 1 - blockIdx.x : blockIdx.x;
+    const int c = !sums(kPass) && scales ? gridDim.x - 1 - blockIdx.x : blockIdx.x;
     int k = 0, hi = t.count;  // the chunk's tensor: the last whose first chunk is not behind it
     while (hi - k > 1) {
         const int mid = (k + hi) / 2;
@@ -429,10 +444,10 @@ __global__ void __launch_bounds__(kThreads, kNorms ? (kState8 ? 5 : 3) : (kState
     const float gscale = op.clip == 2 ? sc : 1.f, sscale = op.clip == 1 ? sc : 1.f;
     float ww = 0.f, xx = 0.f;
     if (i0 + S::kWarp <= e.n)
-        take<kNorms, kState8, true>(op, e, i0, gscale, sscale, ww, xx);
+        take<kPass, kState8, true>(op, e, i0, gscale, sscale, ww, xx);
     else if (i0 < e.n)
-        take<kNorms, kState8, false>(op, e, i0, gscale, sscale, ww, xx);
-    if constexpr (kNorms) {
+        take<kPass, kState8, false>(op, e, i0, gscale, sscale, ww, xx);
+    if constexpr (sums(kPass)) {
         __shared__ float2 sh[kThreads / 32];
         ww = warp_sum(ww);
         xx = warp_sum(xx);
@@ -541,18 +556,25 @@ cudaError_t run_adamw(const int* ids, int count, const AdamTensor* ts, const Ada
     t.first[count] = static_cast<int>(total);
     if (total == 0) return cudaSuccess;
     const unsigned grid = static_cast<unsigned>(total);
-    if (op.clip != 0) {
-        adamw_kernel<CAP, true, kState8><<<grid, kThreads, 0, st>>>(t, op, part, nullptr), note_launch();
-        cudaError_t e = cudaGetLastError();
-        if (e != cudaSuccess) return e;
-        adamw_scale_kernel<CAP><<<count, kThreads, 0, st>>>(t, part, op.clip_frac, scales),
+    if (op.clip == 0) {
+        adamw_kernel<CAP, kStep, kState8><<<grid, kThreads, 0, st>>>(t, op, nullptr, nullptr),
             note_launch();
-        e = cudaGetLastError();
-        if (e != cudaSuccess) return e;
+        return cudaGetLastError();
     }
-    adamw_kernel<CAP, false, kState8>
-        <<<grid, kThreads, 0, st>>>(t, op, nullptr, op.clip != 0 ? scales : nullptr),
-        note_launch();
+    constexpr Pass kFirst = kState8 ? kNorms : kMoments, kLast = kState8 ? kStep : kApply;
+    if (op.clip == 1)
+        adamw_kernel<CAP, kFirst, kState8><<<grid, kThreads, 0, st>>>(t, op, part, nullptr), note_launch();
+    else
+        adamw_kernel<CAP, kNorms, kState8><<<grid, kThreads, 0, st>>>(t, op, part, nullptr), note_launch();
+    cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    adamw_scale_kernel<CAP><<<count, kThreads, 0, st>>>(t, part, op.clip_frac, scales), note_launch();
+    e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    if (op.clip == 1)
+        adamw_kernel<CAP, kLast, kState8><<<grid, kThreads, 0, st>>>(t, op, nullptr, scales), note_launch();
+    else
+        adamw_kernel<CAP, kStep, kState8><<<grid, kThreads, 0, st>>>(t, op, nullptr, scales), note_launch();
     return cudaGetLastError();
 }
 
