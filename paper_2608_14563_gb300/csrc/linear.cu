@@ -26,25 +26,31 @@ size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
 // ------------------------------------------------------------------ few tokens
 // Y^T = W X^T: 128 rows of the weights (features) by BT tokens per tile, one CTA each.  The
-// tiles' k-blocks, tile by tile, are one sequence of units that the CTAs share out evenly, so
+// tiles' k-steps, tile by tile, are one sequence of units that the CTAs share out evenly, so
 // that every SM streams the same number of weight bytes whatever the number of tiles: CTA c has
 // units [c U / C, (c + 1) U / C).  A tile that lies in one CTA's range goes from the accumulator
 // to the output.  Of the others each CTA leaves its sums in scratch, and the warp that is the
 // last of a tile's to do so (a counter per tile and quarter of its rows) adds them in CTA order,
 // whichever it is: the sums do not depend on the order in which the CTAs finish, and no CTA
 // waits for another.
-//   warp 0      TMA producer: a k-block of weights (16 KB) and of tokens per stage
+//   warp 0      TMA producer: a k-step, two 64-deep k-blocks, of weights and tokens per stage
 //   warp 1      TMEM, MMAs (128 x BT x 16)
 //   warps 2..5  epilogue: one feature per lane
-// Bound: the weights' bytes.
+// Bound: the weights' bytes, with a fixed part of some 8 us; under that the thread that issues the
+// MMAs, whose k-blocks with a commit each took some 540 cycles however few columns they had, so
+// that tiles which have an SM each are no faster for being narrow.  us on pair tiles and here, from
+// memory, K 4096 to 11008 features and 11008 to 4096: 5 tokens 41.7 26.8, 38.4 25.2; 16 tokens 38.3
+// 28.3, 34.9 25.8; 32 tokens 38.6 30.6, 35.2 27.9.  With 64 tokens 38.8 37.4, 36.6 32.8, but 1024 to
+// 1024 features 15.3 16.4; with more the sums of the parts, one warp per 32 features, are slower
+// than the whole product on pair tiles.
 constexpr int kFewT = 32;
-constexpr int kFewAhead = 4;  // CTAs' sums in flight
 
 template <int BT>
 struct FewSmem {
+    static constexpr int kSub = 2;  // 64-deep k-blocks per stage
     static constexpr int kWBytes = kBM * kBK * 2;
     static constexpr int kXBytes = BT * kBK * 2;
-    static constexpr int kStageBytes = kWBytes + kXBytes;
+    static constexpr int kStageBytes = kSub * (kWBytes + kXBytes);
     static constexpr int kFit = 221184 / kStageBytes;
     static constexpr int kStages = kFit < 12 ? kFit : 12;
     static constexpr int kBarOffset = kStages * kStageBytes;
@@ -54,10 +60,10 @@ struct FewSmem {
 };
 
 struct FewShape {
-    int M, T;            // features, tokens
-    int k_blocks, tiles;
-    long long units;     // tiles * k_blocks
-    float* scratch;      // [2 CTAs][BT][128]: slot 2 c + 1 has a tile's first k-blocks
+    int T;               // tokens, at most BT
+    int k_steps;
+    long long units;     // tiles * k_steps
+    float* scratch;      // [2 CTAs][BT][128]: slot 2 c + 1 has a tile's first k-steps
     unsigned* counters;  // [tiles][4], zero at the start
 };
 
@@ -69,36 +75,36 @@ __device__ __forceinline__ int few_owner(const FewShape& s, long long u, long lo
     return static_cast<int>(((u + 1) * C - 1) / s.units);
 }
 
-// One feature of the n tokens through the epilogue: consecutive lanes are consecutive features.  What it reads is loaded for all tokens before anything is stored (a load behind a store
+// One feature of the n tokens through the epilogue: consecutive lanes are consecutive
+// features.  What it reads is loaded for all tokens before anything is stored (a load behind a store
 // to memory that may be the same waits for itself alone: 128 tokens took 110 us instead of 35).
-template <int BT>
-__device__ __forceinline__ void few_load(const __nv_bfloat16* p, long long o, long long ld, int n,
-                                         uint16_t (&u)[BT]) {
-    const uint16_t* q = reinterpret_cast<const uint16_t*>(p) + o;
+template <int kN>
+__device__ __forceinline__ void few_load(const __nv_bfloat16* p, long long ld, int n, uint16_t (&u)[kN]) {
+    const uint16_t* q = reinterpret_cast<const uint16_t*>(p);
 #pragma unroll
-    for (int j = 0; j < BT; ++j) u[j] = j < n ? q[j * ld] : 0;
+    for (int j = 0; j < kN; ++j) u[j] = j < n ? q[j * ld] : 0;
 }
 __device__ __forceinline__ float bf16_bits(uint16_t u) {
     return __uint_as_float(static_cast<uint32_t>(u) << 16);
 }
-template <int BT>
-__device__ __forceinline__ void few_out(const LinearOut& p, int feature, int n, float (&v)[BT]) {
+template <int kN>
+__device__ __forceinline__ void few_out(const LinearOut& p, int feature, int n, float (&v)[kN]) {
     if (feature >= p.N) return;
-    uint16_t r[BT];
-    if (p.residual) few_load(p.residual, feature, p.ld, n, r);
+    uint16_t r[kN];
+    if (p.residual) few_load(p.residual + feature, p.ld, n, r);
     if (p.bias) {
         const float bias = __bfloat162float(p.bias[feature]);
 #pragma unroll
-        for (int j = 0; j < BT; ++j) v[j] += bias;
+        for (int j = 0; j < kN; ++j) v[j] += bias;
     }
     if (p.Z) {
 #pragma unroll
-        for (int j = 0; j < BT; ++j)
+        for (int j = 0; j < kN; ++j)
             if (j < n) p.Z[j * p.ld + feature] = __float2bfloat16_rn(v[j]);
     }
     with_act(p.act, [&](auto act) {
 #pragma unroll
-        for (int j = 0; j < BT; j += 2) {
+        for (int j = 0; j < kN; j += 2) {
             if (j >= n) break;
             const float2 y = act_value2<act.value>(make_float2(v[j], v[j + 1]));
             v[j] = y.x;
@@ -106,19 +112,18 @@ __device__ __forceinline__ void few_out(const LinearOut& p, int feature, int n, 
         }
     });
 #pragma unroll
-    for (int j = 0; j < BT; ++j)
-        if (j < n)
-            p.Y[j * p.ld + feature] = __float2bfloat16_rn(p.residual ? v[j] + bf16_bits(r[j]) : v[j]);
+    for (int j = 0; j < kN; ++j)
+        if (j < n) p.Y[j * p.ld + feature] = __float2bfloat16_rn(p.residual ? v[j] + bf16_bits(r[j]) : v[j]);
 }
-template <int BT>
-__device__ __forceinline__ void few_out(const SlopeOut& p, int feature, int n, float (&v)[BT]) {
+template <int kN>
+__device__ __forceinline__ void few_out(const SlopeOut& p, int feature, int n, float (&v)[kN]) {
     if (feature >= p.N) return;
     if (p.z) {
-        uint16_t z[BT];
-        few_load(p.z, feature, p.ld, n, z);
+        uint16_t z[kN];
+        few_load(p.z + feature, p.ld, n, z);
         with_act(p.act, [&](auto act) {
 #pragma unroll
-            for (int j = 0; j < BT; j += 2) {
+            for (int j = 0; j < kN; j += 2) {
                 if (j >= n) break;
                 const float2 s = act_slope2<act.value>(make_float2(bf16_bits(z[j]), bf16_bits(z[j + 1])));
                 v[j] *= s.x;
@@ -127,7 +132,7 @@ __device__ __forceinline__ void few_out(const SlopeOut& p, int feature, int n, f
         });
     }
 #pragma unroll
-    for (int j = 0; j < BT; ++j)
+    for (int j = 0; j < kN; ++j)
         if (j < n) p.X[j * p.ld + feature] = __float2bfloat16_rn(v[j]);
 }
 
@@ -137,11 +142,12 @@ __global__ void __launch_bounds__(192, 1)
                       const __grid_constant__ CUtensorMap xmap, const __grid_constant__ Out out,
                       const FewShape sh, unsigned* status, unsigned long long wait_limit_ns) {
     using L = FewSmem<BT>;
-    constexpr int kStages = L::kStages;
+    constexpr int kStages = L::kStages, kSub = L::kSub;
     constexpr uint32_t kIdesc = idesc_bf16_f32(kBM, BT, W_MN, false);
     static_assert(BT <= 32, "one load of the accumulator");
     constexpr int kAccCols = 32;
     constexpr int kTmemCols = 2 * kAccCols;
+    constexpr int kAhead = BT <= 16 ? 4 : 2;  // CTAs' sums in flight
 
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
@@ -187,23 +193,29 @@ __global__ void __launch_bounds__(192, 1)
     const WaitGuard guard{abort_flag, status, wait_limit_ns};
     const long long C = gridDim.x;
     const long long u0 = few_start(sh, blockIdx.x, C), u1 = few_start(sh, blockIdx.x + 1, C);
+    const int tile0 = static_cast<int>(u0 / sh.k_steps), k0 = static_cast<int>(u0 % sh.k_steps);
 
     if (warp == 0) {
         if (lane == 0) {
             int stage = 0;
             uint32_t phase = 0;
             uint32_t issued_mask = 0, issued_parity = 0;
-            int tile = static_cast<int>(u0 / sh.k_blocks), kb = static_cast<int>(u0 % sh.k_blocks);
+            int tile = tile0, ks = k0;
             for (long long u = u0; u < u1; ++u) {
                 if (!mbar_wait(empty_bar(stage), phase ^ 1u, guard)) break;
-                const uint32_t sw = sbase + stage * L::kStageBytes;
+                const uint32_t sw = sbase + stage * L::kStageBytes, sx = sw + kSub * L::kWBytes;
                 mbar_arrive_expect_tx(full_bar(stage), L::kStageBytes);
-                load_operand<W_MN, kBM>(&wmap, sw, full_bar(stage), tile * kBM, kb * kBK);
-                load_operand<false, BT>(&xmap, sw + L::kWBytes, full_bar(stage), 0, kb * kBK);
+#pragma unroll
+                for (int j = 0; j < kSub; ++j) {
+                    const int k = (ks * kSub + j) * kBK;
+                    load_operand<W_MN, kBM>(&wmap, sw + j * L::kWBytes, full_bar(stage),
+                                            tile * kBM, k);
+                    load_operand<false, BT>(&xmap, sx + j * L::kXBytes, full_bar(stage), 0, k);
+                }
                 issued_mask |= 1u << stage;
                 issued_parity = (issued_parity & ~(1u << stage)) | (phase << stage);
                 if (++stage == kStages) { stage = 0; phase ^= 1u; }
-                if (++kb == sh.k_blocks) { kb = 0; ++tile; }
+                if (++ks == sh.k_steps) { ks = 0; ++tile; }
             }
             grid_dependency_trigger();
             for (int s = 0; s < kStages; ++s)  // no copy lands in shared memory after exit
@@ -216,9 +228,9 @@ __global__ void __launch_bounds__(192, 1)
             int stage = 0, acc = 0;
             uint32_t phase = 0, acc_phase = 0;
             bool ok = true, issued_any = false;
-            int kb = static_cast<int>(u0 % sh.k_blocks);
+            int ks = k0;
             for (long long u = u0; u < u1 && ok;) {
-                const long long end = min(u1, u + sh.k_blocks - kb);  // of this tile's segment
+                const long long end = min(u1, u + sh.k_steps - ks);  // of this tile's segment
                 if (!mbar_wait(tempty_bar(acc), acc_phase ^ 1u, guard)) { ok = false; break; }
                 tc_fence_after();
                 const uint32_t d_tmem = tmem_base + static_cast<uint32_t>(acc * kAccCols);
@@ -226,19 +238,21 @@ __global__ void __launch_bounds__(192, 1)
                 for (; u < end; ++u) {
                     if (!mbar_wait(full_bar(stage), phase, guard)) { ok = false; break; }
                     tc_fence_after();
-                    const uint32_t sw = sbase + stage * L::kStageBytes;
-                    const uint32_t sx = sw + L::kWBytes;
+                    const uint32_t sw = sbase + stage * L::kStageBytes, sx = sw + kSub * L::kWBytes;
 #pragma unroll
-                    for (int kk = 0; kk < kBK / kUmmaK; ++kk)
-                        tc_mma_bf16(d_tmem, operand_desc<W_MN>(sw, kk), operand_desc<false>(sx, kk),
-                                    kIdesc, !first || kk != 0 ? 1u : 0u);
+                    for (int j = 0; j < kSub; ++j)
+#pragma unroll
+                        for (int kk = 0; kk < kBK / kUmmaK; ++kk)
+                            tc_mma_bf16(d_tmem, operand_desc<W_MN>(sw + j * L::kWBytes, kk),
+                                        operand_desc<false>(sx + j * L::kXBytes, kk), kIdesc,
+                                        !first || j != 0 || kk != 0 ? 1u : 0u);
                     first = false;
                     issued_any = true;
                     tc_commit(empty_bar(stage));
                     if (++stage == kStages) { stage = 0; phase ^= 1u; }
                 }
                 if (!ok) break;
-                kb = 0;
+                ks = 0;
                 tc_commit(tfull_bar(acc));
                 if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
             }
@@ -252,10 +266,10 @@ __global__ void __launch_bounds__(192, 1)
         const int q = warp & 3;  // TMEM lane quarter this warp may access
         int acc = 0;
         uint32_t acc_phase = 0;
-        int tile = static_cast<int>(u0 / sh.k_blocks), kb = static_cast<int>(u0 % sh.k_blocks);
+        int tile = tile0, ks = k0;
         for (long long u = u0; u < u1;) {
-            const long long end = min(u1, u + sh.k_blocks - kb);
-            const bool whole = kb == 0 && end - u == sh.k_blocks;
+            const long long end = min(u1, u + sh.k_steps - ks);
+            const bool whole = ks == 0 && end - u == sh.k_steps;
             const int feature = tile * kBM + q * 32 + lane;
             const uint32_t t_row = tmem_base + (static_cast<uint32_t>(q * 32) << 16) +
                                    static_cast<uint32_t>(acc * kAccCols);
@@ -267,6 +281,8 @@ __global__ void __launch_bounds__(192, 1)
                 return true;
             };
             if (!ready()) break;
+            float* slot = sh.scratch + static_cast<long long>(2 * blockIdx.x + (ks == 0)) * BT * kBM +
+                          q * 32 + lane;
             float w[32], v[BT];
             tmem_ld_32x32b_x32(t_row, w);
             tc_fence_before();
@@ -277,15 +293,13 @@ __global__ void __launch_bounds__(192, 1)
             if (whole) {
                 few_out(out, feature, sh.T, v);
             } else {
-                float* slot = sh.scratch +
-                              (static_cast<long long>(2 * blockIdx.x + (kb == 0)) * BT) * kBM + q * 32 + lane;
 #pragma unroll
                 for (int j = 0; j < BT; ++j)
                     if (j < sh.T) slot[j * kBM] = v[j];
                 // the last of the tile's CTAs adds their sums
-                const long long first_unit = static_cast<long long>(tile) * sh.k_blocks;
+                const long long first_unit = static_cast<long long>(tile) * sh.k_steps;
                 const int c0 = few_owner(sh, first_unit, C);
-                const int c1 = few_owner(sh, first_unit + sh.k_blocks - 1, C);
+                const int c1 = few_owner(sh, first_unit + sh.k_steps - 1, C);
                 __threadfence();
                 __syncwarp();
                 unsigned before = 0;
@@ -293,25 +307,23 @@ __global__ void __launch_bounds__(192, 1)
                 before = __shfl_sync(0xffffffffu, before, 0);
                 if (before == static_cast<unsigned>(c1 - c0)) {
                     __threadfence();
-                    // (CTA c0 has the tile's first k-blocks: its odd slot)
-                    const float* s0 =
-                        sh.scratch + static_cast<long long>(2 * c0 + 1) * BT * kBM + q * 32 + lane;
+                    const float* part = sh.scratch + q * 32 + lane;
+                    // (CTA c0 has the tile's first k-steps: its odd slot)
+                    const float* s0 = part + static_cast<long long>(2 * c0 + 1) * BT * kBM;
 #pragma unroll
                     for (int j = 0; j < BT; ++j) v[j] = j < sh.T ? __ldcg(s0 + j * kBM) : 0.f;
                     // several CTAs' loads in flight: one by one each waits for L2
 #pragma unroll 1
-                    for (int c = c0 + 1; c <= c1; c += kFewAhead) {
-                        float x[kFewAhead][BT];
+                    for (int c = c0 + 1; c <= c1; c += kAhead) {
+                        float x[kAhead][BT];
 #pragma unroll
-                        for (int i = 0; i < kFewAhead; ++i) {
-                            const float* s = sh.scratch +
-                                             static_cast<long long>(2 * min(c + i, c1)) * BT * kBM +
-                                             q * 32 + lane;
+                        for (int i = 0; i < kAhead; ++i) {
+                            const float* s = part + static_cast<long long>(2 * min(c + i, c1)) * BT * kBM;
 #pragma unroll
                             for (int j = 0; j < BT; ++j) x[i][j] = j < sh.T ? __ldcg(s + j * kBM) : 0.f;
                         }
 #pragma unroll
-                        for (int i = 0; i < kFewAhead; ++i) {
+                        for (int i = 0; i < kAhead; ++i) {
                             if (c + i > c1) break;
 #pragma unroll
                             for (int j = 0; j < BT; ++j) v[j] += x[i][j];
@@ -322,7 +334,7 @@ __global__ void __launch_bounds__(192, 1)
             }
             if (++acc == 2) { acc = 0; acc_phase ^= 1u; }
             u = end;
-            kb = 0;
+            ks = 0;
             ++tile;
         }
         __syncwarp();
@@ -355,20 +367,28 @@ int sm_count() {
     return current_device_info(&di) ? di.sm_count : 152;
 }
 
-int few_bt(int T) { return T <= 16 ? 16 : 32; }
-
-// CTAs of a problem: one per SM while each has at least 4 k-blocks.
-long long few_ctas(int M, int K) {
-    const long long units = static_cast<long long>((M + kBM - 1) / kBM) * ((K + kBK - 1) / kBK);
-    const long long most = (units + 3) / 4, sms = sm_count();
-    return most < sms ? most : sms;
+// The tiles and k-steps of a problem of M features, and its CTAs: one per SM while each has at
+// least 2 k-steps.
+struct FewPlan {
+    int k_steps;
+    long long tiles, units, ctas;
+};
+FewPlan few_plan(int M, int K) {
+    FewPlan p;
+    p.k_steps = (K + 2 * kBK - 1) / (2 * kBK);
+    p.tiles = (M + kBM - 1) / kBM;
+    p.units = p.tiles * p.k_steps;
+    const long long most = (p.units + 1) / 2, sms = sm_count();
+    p.ctas = most < sms ? most : sms;
+    return p;
 }
+int few_bt(int T) { return T <= 16 ? 16 : 32; }
 size_t few_counter_bytes(int M) { return up256(static_cast<size_t>((M + kBM - 1) / kBM) * 16); }
 size_t few_scratch_bytes(int M, int K, int T) {
-    return static_cast<size_t>(2 * few_ctas(M, K)) * few_bt(T) * kBM * 4;
+    return static_cast<size_t>(2 * few_plan(M, K).ctas) * few_bt(T) * kBM * 4;
 }
 
-// W: [M, K] (K-major) or, W_MN, [K, M]; X [T, K]; head: the counters, then the scratch.
+// W: [M, K] (K-major) or, W_MN, [K, M]; X [T, K].
 template <int BT, bool W_MN, class Out>
 cudaError_t run_few_bt(const void* W, const void* X, int M, int K, int T, const Out& out,
                        uint8_t* counters, float* scratch, unsigned* status, cudaStream_t st) {
@@ -379,16 +399,15 @@ cudaError_t run_few_bt(const void* W, const void* X, int M, int K, int T, const 
     CUtensorMap wmap, xmap;
     const bool ok = W_MN ? map_weights(&wmap, W, K, M, kBK) : map_weights(&wmap, W, M, K, kBM);
     if (!ok || !map_kmajor(&xmap, X, T, K, BT)) return cudaErrorInvalidValue;
+    const FewPlan p = few_plan(M, K);
     FewShape sh;
-    sh.M = M;
     sh.T = T;
-    sh.k_blocks = (K + kBK - 1) / kBK;
-    sh.tiles = (M + kBM - 1) / kBM;
-    sh.units = static_cast<long long>(sh.tiles) * sh.k_blocks;
+    sh.k_steps = p.k_steps;
+    sh.units = p.units;
     sh.scratch = scratch;
     sh.counters = reinterpret_cast<unsigned*>(counters);
-    return launch_chained(kern, dim3(static_cast<unsigned>(few_ctas(M, K))), 192, L::kBytes, st, wmap,
-                          xmap, out, sh, status, wait_limit_ns());
+    return launch_chained(kern, dim3(static_cast<unsigned>(p.ctas)), 192, L::kBytes, st, wmap, xmap,
+                          out, sh, status, wait_limit_ns());
 }
 template <bool W_MN, class Out>
 cudaError_t run_few(const void* W, const void* X, int M, int K, int T, const Out& out,
@@ -754,8 +773,8 @@ cudaError_t launch_linear(int dtype, const LinearFwd& p, void* workspace, cudaSt
     if (p.T <= kRowT) return run_rows(p, out, status, st);
     if (p.T <= kFewT)
         return run_few<false>(p.W, p.X, p.N, p.K, p.T, out, ws + kHead,
-                              reinterpret_cast<float*>(ws + kHead + few_counter_bytes(p.N)), status,
-                              st);
+                              reinterpret_cast<float*>(ws + kHead + few_counter_bytes(p.N)),
+                              status, st);
     return run_pair<false, false, EpiLinear>(p.X, p.W, p.T, p.N, p.K, out,
                                              reinterpret_cast<float*>(ws + kHead), status, st);
 }
@@ -771,7 +790,8 @@ VjpLayout vjp_layout(int dtype, int T, int N, int K, int act) {
     VjpLayout l;
     const SignalPlan sp = signal_plan(dtype, T, N);
     l.few = kHead;
-    l.sig = l.few + (dtype == 1 && T <= kFewT ? few_counter_bytes(K) : 0);
+    const bool few = dtype == 1 && T <= kFewT;
+    l.sig = l.few + (few ? few_counter_bytes(K) : 0);
     l.clear = l.dz = l.sig + signal_counter_bytes(sp);
     size_t off = l.dz;
     if (act != kActNone) off = up256(off + static_cast<size_t>(T) * N * (dtype == 1 ? 2 : 4));
@@ -781,7 +801,7 @@ VjpLayout vjp_layout(int dtype, int T, int N, int K, int act) {
     size_t scratch = 0;
     if (dtype == 1) {
         scratch = pair_scratch_bytes(N, K, T);
-        const size_t dx = T <= kFewT ? few_scratch_bytes(K, N, T) : pair_scratch_bytes(T, K, N);
+        const size_t dx = few ? few_scratch_bytes(K, N, T) : pair_scratch_bytes(T, K, N);
         scratch = dx > scratch ? dx : scratch;
     }
     l.total = off + scratch;
