@@ -5,10 +5,11 @@
 //   signal     dX = dZ W           M = T  N = K  K = N    A K-major, B MN-major
 //   gradient   dW = dZ^T X         M = N  N = K  K = T    A, B MN-major
 //
-// Large batches run on the pair tiles of tc_gemm_pair.cuh with the epilogues of
-// linear_epilogues.cuh.  Batches of at most kFewT tokens run on few_tokens_kernel, with the
-// weights as the 128-row operand and the tokens along N.  What the layer's own activation does to
-// the signal, and the bias gradient, are one pass over dY (signal_kernel).
+// Large batches run on the tiles of tc_gemm_pair.cuh, or where these are few of tc_gemm.cuh, with
+// the epilogues of linear_epilogues.cuh.  Batches of at most kFewT tokens run on
+// few_tokens_kernel, with the weights as the 128-row operand and the tokens along N, and forward
+// with at most kRowT on row_kernel.  What the layer's own activation does to the signal, and the
+// bias gradient, are one pass over dY (signal_kernel).
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -144,7 +145,7 @@ __global__ void __launch_bounds__(192, 1)
     using L = FewSmem<BT>;
     constexpr int kStages = L::kStages, kSub = L::kSub;
     constexpr uint32_t kIdesc = idesc_bf16_f32(kBM, BT, W_MN, false);
-    static_assert(BT <= 32, "one load of the accumulator");
+    static_assert(kHalfBN == 128 && BT <= 32, "one load of the accumulator");
     constexpr int kAccCols = 32;
     constexpr int kTmemCols = 2 * kAccCols;
     constexpr int kAhead = BT <= 16 ? 4 : 2;  // CTAs' sums in flight
@@ -510,44 +511,64 @@ int linear_clusters() {
     return c;
 }
 
-// How a product runs: 128-column tiles, k ranges of every tile (split), or of those of the last
+// How a product runs: on one CTA's tiles of 128 rows by `single` columns, on pair tiles of 128
+// columns (half) or on those of 256, with k ranges of every tile (split), or of those of the last
 // partial wave (tail), and the units of scratch.
 struct PairPlan {
+    int single = 0;
     bool half = false;
     int split = 0;
     SkPlan tail;
     long long units = 0;
 };
 
-// The cheapest by a 64-deep k-block of a 256 x 256 tile (325 ns), storing the parts of a wave of
-// units (2500), the fixup's launch (5000) and its read of a unit (100).  4096 x 4096 x 11008 (256
-// tiles on 76 clusters): the last 28 tiles whole 56 us, in 2 ranges 41, in the 5 that fill the waves
-// best 48 (the product 244 us).
+// The cheapest by what was measured, in ns.  A 64-deep k-block of a 256 x 256 pair tile takes 325,
+// where one wave has all tiles: pair tiles of 128 columns 300, one CTA's of 128 columns 355 and of 64
+// columns 290 (the issuing thread, not the arithmetic, sets their pace), and a launch and its
+// epilogue 9000 on pairs and 6000 on single CTAs, which have no partner to wait for.  Split tiles
+// add the store of the parts of a wave of units (2500), the fixup's launch (5000) and its read of a
+// unit (100).
+//   T x K x N, us: 200 x 256 x 384 12.3 on pairs, 8.3 on 64-column CTAs; 128 x 1024 x 1024 16.4,
+//   12.3; 200 x 4096 x 4096 28.7, 26.7; 64 x 4096 x 11008 38.8, 28.9 on 128-column ones.  4096 x
+//   11008 x 4096 (256 tiles on 76 clusters): the last 28 tiles whole 56, in 2 ranges 41, in the 5 that
+//   fill the waves best 48 (the product 239).
 PairPlan pair_plan(int M, int N, int K) {
     PairPlan p;
     const long long tiles = static_cast<long long>((M + 255) / 256) * ((N + 255) / 256);
     const int kb = (K + kBK - 1) / kBK;
-    const long long clusters = linear_clusters();
+    const long long clusters = linear_clusters(), sms = sm_count();
     const long long left = tiles < clusters ? tiles : tiles % clusters;
     if (left == 0) return p;
-    double best = kb * 325.0;
+    double best = 9000.0 + kb * 325.0;
     if (2 * tiles <= clusters) {
         p.half = true;
-        best = kb * 195.0;
+        best = 9000.0 + kb * 300.0;
     }
     for (int S = 2; S <= 32 && kb / S >= 8 && left * S <= kTailWaves * clusters; ++S) {
         const double waves = static_cast<double>((left * S + clusters - 1) / clusters);
-        const double cost = waves * (((kb + S - 1) / S) * 325.0 + 2500.0) + 5000.0 + left * S * 100.0;
+        const double cost =
+            9000.0 + waves * (((kb + S - 1) / S) * 325.0 + 2500.0) + 5000.0 + left * S * 100.0;
         if (cost >= best) continue;
         best = cost;
         p.half = false;
         p.units = left * S;
         p.split = S;
     }
-    if (tiles >= clusters && p.units > 0) {
-        p.tail.tail_tiles = left;
-        p.tail.tail_split = p.split;
-        p.split = 0;
+    if (tiles >= clusters) {
+        if (p.units > 0) {
+            p.tail.tail_tiles = left;
+            p.tail.tail_split = p.split;
+            p.split = 0;
+        }
+        return p;
+    }
+    for (int width : {128, 64}) {
+        const long long n = static_cast<long long>((M + 127) / 128) * ((N + width - 1) / width);
+        const double cost = 6000.0 + kb * (width == 128 ? 355.0 : 290.0);
+        if (n > sms || cost >= best) continue;
+        best = cost;
+        p = PairPlan{};
+        p.single = width;
     }
     return p;
 }
@@ -580,17 +601,25 @@ cudaError_t run_pair(const void* A, const void* B, int M, int N, int K, const Ou
     const PairPlan pp = pair_plan(M, N, K);
     GemmMaps<1> maps;
     bool ok = A_MN ? map_mnmajor(&maps.a[0], A, K, M) : map_kmajor(&maps.a[0], A, M, K, kBM);
-    ok = ok && (B_MN ? map_mnmajor(&maps.b[0], B, K, N)
-                     : map_kmajor(&maps.b[0], B, N, K, pp.half ? kHalfBN / 2 : 128));
+    const int b_rows = pp.single ? pp.single : pp.half ? kHalfBN / 2 : 128;
+    ok = ok && (B_MN ? map_mnmajor(&maps.b[0], B, K, N) : map_kmajor(&maps.b[0], B, N, K, b_rows));
     typename Epi<256>::Params ep;
     ep.o = out;
     if (!ok || !out_maps(&ep)) return cudaErrorInvalidValue;
-    if (pp.half) {
-        typename Epi<kHalfBN>::Params eh;
-        memcpy(&eh, &ep, sizeof(eh));  // the same fields for every tile width
+    // the parameters of every tile width have the same fields
+    typename Epi<128>::Params e128;
+    typename Epi<64>::Params e64;
+    memcpy(&e128, &ep, sizeof(e128));
+    memcpy(&e64, &ep, sizeof(e64));
+    if (pp.single == 64)
+        return run_gemm<64, A_MN, B_MN, 8, 1, Epi<64>>(
+            maps, e64, make_shape(M, N, K, 64, 1, band_for(false)), status, st);
+    if (pp.single == 128)
+        return run_gemm<128, A_MN, B_MN, 6, 1, Epi<128>>(
+            maps, e128, make_shape(M, N, K, 128, 1, band_for(false)), status, st);
+    if (pp.half)
         return run_gemm_pair<kHalfBN, A_MN, B_MN, kHalfStages, 1, Epi<kHalfBN>>(
-            maps, eh, make_shape(M, N, K, kHalfBN, 1, band_for(true), kPairBM), status, st);
-    }
+            maps, e128, make_shape(M, N, K, kHalfBN, 1, band_for(true), kPairBM), status, st);
     const GemmShape sh = make_shape(M, N, K, 256, 1, band_for(true), kPairBM);
     SkPlan plan;
     const cudaError_t e = run_gemm_pair<256, A_MN, B_MN, kPairStages, 1, Epi<256>>(
