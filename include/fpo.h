@@ -429,6 +429,9 @@ typedef enum fpo_activation {
     FPO_ACT_SILU = 4
 } fpo_activation;
 
+/* Largest T, d_out and d_in of fpo_linear and fpo_linear_vjp. */
+#define FPO_MAX_LINEAR_SIZE (1 << 30)
+
 /* Bytes of workspace fpo_linear needs on the current device (0 on invalid sizes): 256, for 5 to 32
  * tokens in bf16 up to 160 kB more per padded token (16 or 32), for larger bf16 batches whose tiles
  * leave a wave partly empty up to 60 MB for the parts of split tiles. */
@@ -447,7 +450,8 @@ size_t fpo_linear_workspace(int64_t T, int64_t d_out, int64_t d_in, int32_t dtyp
  * Y        [T, d_out] dtype
  * Z_out    [T, d_out] dtype, or NULL: the pre-activation, which fpo_linear_vjp reads
  * act      fpo_activation
- * workspace fpo_linear_workspace() bytes, 256-byte aligned (device status word first)
+ * workspace fpo_linear_workspace() bytes, 256-byte aligned (device status word first); not shared
+ *          with a call that runs at the same time
  * No output may overlap an input or another output (but for Y = residual), nor the workspace
  * anything (FPO_ERR_ARG).  fp32 accumulation; bias, activation and residual on the fp32 sums,
  * one rounding each for Z and Y.  Deterministic.  T = 0 writes nothing.
@@ -535,11 +539,12 @@ size_t fpo_adamw_workspace(int32_t n_tensors, const int64_t* n, int32_t clip);
  * in fp32 with the rates rounded to fp32; the moments' products and sums are rounded one by one, as
  * written from left to right, so that the codes of 8-bit moments are those of any fp32 arithmetic.
  * The clip is that of App. A per tensor: s = min(1, clip_frac ||W|| / ||step||), or G scaled so
- * before the moments see it.
+ * before the moments see it (a tensor of zeros does not move under it).
  *
  * tensors  HOST array; W_master, W_out, the states and the scales may not overlap one another, a G
  *          or the workspace (FPO_ERR_ARG), but for an fp32 W_out that is W_master; G may repeat
- * workspace  with a clip fpo_adamw_workspace() bytes, 256-byte aligned; it holds no status word
+ * workspace  with a clip fpo_adamw_workspace() bytes, 256-byte aligned; it holds no status word, and
+ *          is not shared with a call that runs at the same time
  * step, rates and seed are read at the call: a captured call replays with them.
  *
  * 8-bit moments.  Each FPO_ADAMW_BLOCK consecutive elements have one power of two as scale, which

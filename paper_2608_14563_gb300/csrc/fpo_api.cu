@@ -811,7 +811,9 @@ namespace {
 
 int32_t linear_check(int64_t T, int64_t d_out, int64_t d_in, int32_t dtype) {
     if (dtype != FPO_F32 && dtype != FPO_BF16) return FPO_ERR_DTYPE;
-    if (T < 0 || d_in <= 0 || d_out <= 0 || T > INT_MAX || d_in > INT_MAX || d_out > INT_MAX)
+    // (room for the tiles' rounding in 32 bits)
+    if (T < 0 || d_in <= 0 || d_out <= 0 || T > FPO_MAX_LINEAR_SIZE || d_in > FPO_MAX_LINEAR_SIZE ||
+        d_out > FPO_MAX_LINEAR_SIZE)
         return FPO_ERR_SHAPE;
     if (dtype == FPO_BF16 && (d_in % 8 != 0 || d_out % 8 != 0)) return FPO_ERR_SHAPE;
     return FPO_OK;

@@ -145,7 +145,7 @@ __global__ void __launch_bounds__(192, 1)
     using L = FewSmem<BT>;
     constexpr int kStages = L::kStages, kSub = L::kSub;
     constexpr uint32_t kIdesc = idesc_bf16_f32(kBM, BT, W_MN, false);
-    static_assert(kHalfBN == 128 && BT <= 32, "one load of the accumulator");
+    static_assert(BT <= 32, "one load of the accumulator");
     constexpr int kAccCols = 32;
     constexpr int kTmemCols = 2 * kAccCols;
     constexpr int kAhead = BT <= 16 ? 4 : 2;  // CTAs' sums in flight
@@ -607,8 +607,10 @@ cudaError_t run_pair(const void* A, const void* B, int M, int N, int K, const Ou
     ep.o = out;
     if (!ok || !out_maps(&ep)) return cudaErrorInvalidValue;
     // the parameters of every tile width have the same fields
+    static_assert(kHalfBN == 128, "e128");
     typename Epi<128>::Params e128;
     typename Epi<64>::Params e64;
+    static_assert(sizeof(ep) == sizeof(e128) && sizeof(ep) == sizeof(e64), "the same fields");
     memcpy(&e128, &ep, sizeof(e128));
     memcpy(&e64, &ep, sizeof(e64));
     if (pp.single == 64)

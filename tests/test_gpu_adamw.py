@@ -204,6 +204,30 @@ def test_empty_tensors_are_skipped(fpo):
                 assert np.abs(x.W[k].double().cpu().numpy() - w1).max() <= 1e-6
 
 
+@pytest.mark.parametrize("clip", [0, 1, 2])
+def test_both_kinds_of_moments_in_one_call(fpo, clip):
+    """The same bits as each kind has in a call of its own where its tensors keep their places."""
+    sizes = [300, 5000, 1, 257, 4096, 70]
+    small, large = Tensors(sizes, 8, g16=0), Tensors(sizes, 32, g16=0)
+    mixed = Tensors(sizes, 32, g16=0)
+    kinds = [8, 32, 8, 32, 32, 8]
+    other = Tensors(sizes, 8, g16=0)
+    for k, bits in enumerate(kinds):
+        if bits == 8:
+            mixed.m[k], mixed.v[k] = other.m[k], other.v[k]
+    mixed.ms = [other.ms[k] if b == 8 else None for k, b in enumerate(kinds)]
+    mixed.vs = [other.vs[k] if b == 8 else None for k, b in enumerate(kinds)]
+    for x in (small, large, mixed):
+        x.G, x.W = [g.clone() for g in large.G], [w.clone() for w in large.W]
+    for t in (1, 2):
+        for x in (small, large, mixed):
+            x.step(fpo, t, clip)
+    for k, bits in enumerate(kinds):
+        want = small if bits == 8 else large
+        for a, b in ((mixed.W, want.W), (mixed.m, want.m), (mixed.v, want.v)):
+            assert torch.equal(a[k].view(torch.uint8), b[k].view(torch.uint8)), k
+
+
 def test_the_step_is_that_of_the_layer_optimizer(fpo):
     """That of fpo_layer_optimize_grouped on the gradient it forms (fp32, no clip), but for roundings
     and its rates in float: 1 - 0.999f is 1.3e-5 off, 1 - 0.9f 2.4e-7, both relative."""

@@ -19,14 +19,17 @@ HALF = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}
 ACTS = ["none", "relu", "gelu", "gelu_tanh", "silu"]
 
 # one element; one to four tokens of wide layers; the padded token counts of short batches and their limits;
-# a tile's edges; k ranges of few tiles; 128-column tiles; a split last wave; long and short k
+# a tile's edges; single CTAs' tiles of 64 and 128 columns; pair tiles of 128 columns; k ranges of few
+# tiles; a split last wave; long and short k
 SHAPES = [("bf16", 1, 8, 8), ("bf16", 1, 4096, 1416), ("bf16", 1, 72, 11008), ("bf16", 3, 64, 128),
           ("bf16", 2, 4104, 136), ("bf16", 4, 11008, 72),
           ("bf16", 5, 1032, 264), ("bf16", 16, 200, 136), ("bf16", 17, 264, 1000), ("bf16", 32, 4096, 1000),
           ("bf16", 33, 520, 72), ("bf16", 64, 1032, 640),
-          ("bf16", 65, 2056, 264), ("bf16", 128, 1024, 2056), ("bf16", 129, 64, 264), ("bf16", 200, 256, 384),
+          ("bf16", 65, 2056, 264), ("bf16", 128, 1024, 2056), ("bf16", 64, 4096, 4104), ("bf16", 129, 64, 264), ("bf16", 200, 256, 384),
+          ("bf16", 513, 1032, 4104), ("bf16", 1024, 11008, 1032),
           ("bf16", 256, 4096, 512), ("bf16", 257, 2056, 1032), ("bf16", 700, 4096, 512),
-          ("bf16", 1024, 8, 4104), ("bf16", 2000, 136, 8), ("bf16", 5000, 2056, 2048),
+          ("bf16", 384, 4096, 4096), ("bf16", 1024, 8, 4104), ("bf16", 2000, 136, 8),
+          ("bf16", 5000, 2056, 2048), ("bf16", 5000, 11008, 2048),
           ("bf16", 9000, 1024, 1288), ("f32", 1, 1, 1), ("f32", 7, 3, 5), ("f32", 1, 700, 1001),
           ("f32", 130, 67, 129), ("f32", 200, 256, 384), ("f32", 777, 767, 129), ("f32", 65, 2049, 64)]
 
@@ -182,10 +185,13 @@ def test_gradients_match_differences(fpo, act, act_in, T, k, n):
         assert abs((grad.double() * u).sum() - want) <= lim
 
 
-@pytest.mark.parametrize("T", [3, 20, 100, 300])
-def test_in_place_residual(fpo, T):
-    d = inputs("bf16", T, 264, 520)
-    y = torch.empty(T, 520, dtype=torch.bfloat16, device="cuda")
+# rows, few tokens, single CTAs, k ranges of every tile, pair tiles with a split last wave; fp32
+@pytest.mark.parametrize("dtype,T,k,n", [("bf16", 3, 264, 520), ("bf16", 20, 264, 520), ("bf16", 100, 264, 520),
+                                         ("bf16", 1024, 11008, 1032), ("bf16", 384, 4096, 4096),
+                                         ("bf16", 5000, 11008, 2048), ("f32", 70, 900, 65), ("f32", 300, 64, 132)])
+def test_in_place_residual(fpo, dtype, T, k, n):
+    d = inputs(dtype, T, k, n)
+    y = torch.empty(T, n, dtype=DT[dtype], device="cuda")
     fpo.linear(d["x"], d["W"], y, bias=d["bias"], act=fpo.ACT_SILU, residual=d["residual"])
     r = d["residual"].clone()
     fpo.linear(d["x"], d["W"], r, bias=d["bias"], act=fpo.ACT_SILU, residual=r)
@@ -193,7 +199,7 @@ def test_in_place_residual(fpo, T):
 
 
 @pytest.mark.parametrize("dtype,T,k,n", [("bf16", 3, 4096, 1000), ("bf16", 7, 4096, 1000), ("bf16", 30, 4096, 136), ("bf16", 256, 4096, 512),
-                                         ("bf16", 5000, 2056, 2048), ("f32", 70, 900, 65)])
+                                         ("bf16", 5000, 11008, 2048), ("f32", 70, 900, 65)])
 def test_same_bits_every_time(fpo, dtype, T, k, n):
     d = inputs(dtype, T, k, n)
 

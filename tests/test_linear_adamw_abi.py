@@ -33,6 +33,8 @@ def test_linear_refusals(fpo):
     assert call(dtype=2) == DTYPE and call(dtype=-1) == DTYPE
     assert call(T=-1) == SHAPE and call(n=0) == SHAPE and call(k=0) == SHAPE
     assert call(n=516) == SHAPE and call(k=260) == SHAPE and call(T=1 << 31) == SHAPE
+    big = (1 << 30) + 8
+    assert call(T=big, size=1 << 40) == SHAPE and call(n=big) == SHAPE and call(k=big, dtype=0) == SHAPE
     assert call(n=515, k=3, dtype=0, size=256) in NO_GPU
     assert call(act=5) == ARG and call(act=-1) == ARG
     assert call(x=None) == NULL and call(w=None) == NULL and call(y=None) == NULL
