@@ -754,7 +754,7 @@ SignalPlan signal_plan(int dtype, int T, int N) {
     p.cols = (N + per - 1) / per;
     const long long blocks = 4LL * sm_count();
     long long ranges = blocks / p.cols;
-    const long long most = (T + 63) / 64;  // of at least 64 rows
+    const long long most = (T + 255) / 256;  // of at least 256 rows: one needs no counters
     if (ranges > most) ranges = most;
     if (ranges < 1) ranges = 1;
     p.rows_per = static_cast<int>((((T + ranges - 1) / ranges) + kSigRows - 1) / kSigRows * kSigRows);
