@@ -499,24 +499,28 @@ __global__ void __launch_bounds__(kThreads)
 
 // out[i] = the value of an 8-bit moment (exact in bf16: 4 significant bits times a power of two).
 // Bound: HBM.
+constexpr int kValueQuads = 4, kValueWarp = 128 * kValueQuads, kValueChunk = kThreads / 32 * kValueWarp;
+
 template <bool kSigned, typename Out>
 __global__ void __launch_bounds__(kThreads)
     state_values_kernel(const uint8_t* __restrict__ codes, const float* __restrict__ scales,
                         long long n, Out* __restrict__ out) {
-    using S = Share<true>;
-    const long long i0 = blockIdx.x * static_cast<long long>(S::kChunk) + threadIdx.x / 32 * S::kWarp;
+    const long long i0 = blockIdx.x * static_cast<long long>(kValueChunk) + threadIdx.x / 32 * kValueWarp;
     if (i0 >= n) return;
     const long long i1 = i0 + 4 * (threadIdx.x & 31);
-    const bool full = i0 + S::kWarp <= n;
-    uint32_t c[S::kQuads];
-    const float scale = scales[i0 / kAdamBlock];
+    const bool full = i0 + kValueWarp <= n;
+    uint32_t c[kValueQuads];
+    float scale[kValueQuads / 2];
 #pragma unroll
-    for (int q = 0; q < S::kQuads; ++q)
+    for (int q = 0; q < kValueQuads; ++q)
         c[q] = full ? load_codes<true>(codes, i1 + 128 * q, n) : load_codes<false>(codes, i1 + 128 * q, n);
 #pragma unroll
-    for (int q = 0; q < S::kQuads; ++q) {
+    for (int b = 0; b < kValueQuads / 2; ++b)
+        scale[b] = i0 + kAdamBlock * b < n ? scales[i0 / kAdamBlock + b] : 0.f;
+#pragma unroll
+    for (int q = 0; q < kValueQuads; ++q) {
         float x[4];
-        from_codes<kSigned>(c[q], scale, x);
+        from_codes<kSigned>(c[q], scale[q / 2], x);
         if (full)
             store4<true>(out, i1 + 128 * q, n, x);
         else
@@ -618,7 +622,7 @@ cudaError_t launch_adamw(int n_tensors, const AdamTensor* ts, const AdamRates& o
 
 cudaError_t launch_state_values(bool is_signed, long long n, const void* codes, const float* scales,
                                 int out_dtype, void* out, cudaStream_t st) {
-    const long long blocks = chunks_of<true>(n);
+    const long long blocks = (n + kValueChunk - 1) / kValueChunk;
     if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
     const unsigned grid = static_cast<unsigned>(blocks);
     const uint8_t* c = static_cast<const uint8_t*>(codes);

@@ -423,8 +423,10 @@ cudaError_t run_few(const void* W, const void* X, int M, int K, int T, const Out
 // lanes read 16 bytes each, kRowAhead loads at a time; X comes from L1, and a butterfly adds the
 // lanes' sums.  Nothing has to be set up or added across blocks: one launch, which also clears the
 // status word (no kernel of the call waits for anything).
-// Bound: the weights' bytes.
-constexpr int kRowT = 4, kRowWarps = 8, kRowAhead = 4;
+// Bound: the weights' bytes: 4096 to 11008 features 17.8 us (5.1 TB/s; few_tokens_kernel 28), to
+// 44032 56 (6.4 TB/s).  8 and 16 loads ahead 19.2 and 20.3; 8 warps a block the same, and with four
+// tokens 26.2 instead of 23.9.
+constexpr int kRowT = 4, kRowWarps = 4, kRowAhead = 4;
 
 __device__ __forceinline__ uint4 ld_stream(const uint4* p) {
     uint4 u;
