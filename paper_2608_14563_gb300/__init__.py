@@ -664,19 +664,26 @@ def layernorm_vjp(g, x, gamma, g_out, *, eps=1e-5, min_rms=0.5, dgamma=None, dbe
     return g_out
 
 
-class _Entry:
-    """An entry point all of whose tensor arguments have to lie on the current device (the other
-    functions here look at a call's leading tensor)."""
+def _entry(fn):
+    """An entry point all of whose tensors, not the leading one alone, are looked at for their device
+    (_at): an object that calls fn, without a call of its own in between."""
+    kind = type("entry", (), {"__call__": staticmethod(fn), "__doc__": fn.__doc__})
+    return functools.update_wrapper(kind(), fn)
 
-    def __init__(self, fn):
-        functools.update_wrapper(self, fn)
 
-    def __call__(self, *args, **kw):
-        ts = [t for t in (*args, *kw.values()) if isinstance(t, torch.Tensor)]
-        if len({t.get_device() for t in ts}) > 1:  # (of one device: the leading tensor's check)
-            for t in ts:
-                _on_current_device(t)
-        return self.__wrapped__(*args, **kw)
+def _at(here, t):
+    """_ptr of a tensor that is to lie on device `here`, the leading tensor's (-1: none)."""
+    if t is None:
+        return None
+    if t.get_device() != here or here < 0 or not t.is_contiguous():
+        _on_current_device(t)
+        _ptr(t)
+    return t.data_ptr()
+
+
+def _fits(t, shape, dtype, name):
+    if t is not None and (t.shape != shape or t.dtype is not dtype):
+        _expect(t, shape, dtype, name)
 
 
 # --------------------------------------------------------------------------- linear layers
@@ -684,7 +691,7 @@ def linear_workspace(T, d_out, d_in, dtype=BF16) -> int:
     return int(_lib.fpo_linear_workspace(int(T), int(d_out), int(d_in), int(dtype)))
 
 
-@_Entry
+@_entry
 def linear(x, W, y, *, bias=None, act=ACT_NONE, residual=None, z_out=None, workspace=None,
            stream=None):
     """fpo_linear: y = act(x W^T + bias) + residual, for x [T, d_in] and W [d_out, d_in] of one
@@ -692,17 +699,21 @@ def linear(x, W, y, *, bias=None, act=ACT_NONE, residual=None, z_out=None, works
     workspace tensor (its first word holds the device status)."""
     T, d_in = x.shape
     d_out = W.shape[0]
-    _expect(W, (d_out, d_in), x.dtype, "W")
-    _expect(y, (T, d_out), x.dtype, "y")
-    _expect(bias, (d_out,), x.dtype, "bias")
-    _expect(residual, (T, d_out), x.dtype, "residual")
-    _expect(z_out, (T, d_out), x.dtype, "z_out")
+    _fits(W, (d_out, d_in), x.dtype, "W")
+    _fits(y, (T, d_out), x.dtype, "y")
+    _fits(bias, (d_out,), x.dtype, "bias")
+    _fits(residual, (T, d_out), x.dtype, "residual")
+    _fits(z_out, (T, d_out), x.dtype, "z_out")
     dt = _dtype_code(x)
+    here = x.get_device()
+    xp, Wp, bp, rp, yp, zp = (_at(here, x), _at(here, W), _at(here, bias), _at(here, residual),
+                              _at(here, y), _at(here, z_out))
     if workspace is None:
-        workspace = _workspace(linear_workspace(T, d_out, d_in, dt), x.device, stream)
-    rc = _lib.fpo_linear(T, d_out, d_in, dt, int(act), _ptr(x), _ptr(W), _ptr(bias), _ptr(residual),
-                         _ptr(y), _ptr(z_out), _ptr(workspace), _nbytes(workspace), _stream(stream))
-    _check(rc, "fpo_linear")
+        workspace = _workspace(_lib.fpo_linear_workspace(T, d_out, d_in, dt), x.device, stream)
+    rc = _lib.fpo_linear(T, d_out, d_in, dt, act, xp, Wp, bp, rp, yp, zp, _at(here, workspace),
+                         _nbytes(workspace), _stream(stream))
+    if rc:
+        _check(rc, "fpo_linear")
     return workspace
 
 
@@ -710,7 +721,7 @@ def linear_vjp_workspace(T, d_out, d_in, dtype=BF16, act=ACT_NONE) -> int:
     return int(_lib.fpo_linear_vjp_workspace(int(T), int(d_out), int(d_in), int(dtype), int(act)))
 
 
-@_Entry
+@_entry
 def linear_vjp(dy, x, W, dx, *, act=ACT_NONE, z=None, act_in=ACT_NONE, z_in=None, dW=None,
                dbias=None, workspace=None, stream=None):
     """fpo_linear_vjp: with dz = dy act'(z), dx = (dz W) act_in'(z_in), dW = dz^T x and the fp32
@@ -723,20 +734,24 @@ def linear_vjp(dy, x, W, dx, *, act=ACT_NONE, z=None, act_in=ACT_NONE, z_in=None
             break
     else:
         d_in = 8  # the bias gradient alone
-    _expect(x, (T, d_in), dy.dtype, "x")
-    _expect(W, (d_out, d_in), dy.dtype, "W")
-    _expect(dx, (T, d_in), dy.dtype, "dx")
-    _expect(z, (T, d_out), dy.dtype, "z")
-    _expect(z_in, (T, d_in), dy.dtype, "z_in")
-    _expect(dW, (d_out, d_in), dy.dtype, "dW")
-    _expect(dbias, (d_out,), torch.float32, "dbias")
+    _fits(x, (T, d_in), dy.dtype, "x")
+    _fits(W, (d_out, d_in), dy.dtype, "W")
+    _fits(dx, (T, d_in), dy.dtype, "dx")
+    _fits(z, (T, d_out), dy.dtype, "z")
+    _fits(z_in, (T, d_in), dy.dtype, "z_in")
+    _fits(dW, (d_out, d_in), dy.dtype, "dW")
+    _fits(dbias, (d_out,), torch.float32, "dbias")
     dt = _dtype_code(dy)
+    here = dy.get_device()
+    dyp, zp, xp, Wp, zip_, dxp, dWp, dbp = (
+        _at(here, dy), _at(here, z), _at(here, x), _at(here, W), _at(here, z_in), _at(here, dx),
+        _at(here, dW), _at(here, dbias))
     if workspace is None:
-        workspace = _workspace(linear_vjp_workspace(T, d_out, d_in, dt, act), dy.device, stream)
-    rc = _lib.fpo_linear_vjp(T, d_out, d_in, dt, int(act), _ptr(dy), _ptr(z), _ptr(x), _ptr(W),
-                             int(act_in), _ptr(z_in), _ptr(dx), _ptr(dW), _ptr(dbias),
-                             _ptr(workspace), _nbytes(workspace), _stream(stream))
-    _check(rc, "fpo_linear_vjp")
+        workspace = _workspace(_lib.fpo_linear_vjp_workspace(T, d_out, d_in, dt, act), dy.device, stream)
+    rc = _lib.fpo_linear_vjp(T, d_out, d_in, dt, act, dyp, zp, xp, Wp, act_in, zip_, dxp, dWp, dbp,
+                             _at(here, workspace), _nbytes(workspace), _stream(stream))
+    if rc:
+        _check(rc, "fpo_linear_vjp")
     return workspace
 
 
@@ -748,7 +763,7 @@ def adamw_workspace(sizes, clip=CLIP_NONE) -> int:
 _DTYPES = {torch.bfloat16: BF16}
 
 
-@_Entry
+@_entry
 def adamw_grouped(Gs, opt, W_masters, states1, states2, *, scales1=None, scales2=None, W_outs=None,
                   weight_decays=None, seed=0, workspace=None, stream=None):
     """fpo_adamw_grouped: one AdamW step (optimizer_desc, per-tensor relative clip) on any number of
@@ -815,7 +830,7 @@ def adamw_grouped(Gs, opt, W_masters, states1, states2, *, scales1=None, scales2
     return workspace
 
 
-@_Entry
+@_entry
 def adamw_state_values(codes, scales, out, *, stream=None):
     """fpo_adamw_state_values: the values of 8-bit moments (float8_e4m3fn: first, uint8: second)
     with their scales, into out (fp32 or bf16, the same shape)."""
@@ -826,7 +841,8 @@ def adamw_state_values(codes, scales, out, *, stream=None):
     _expect(out, codes.shape, out.dtype, "out")
     _expect(scales, (-(-n // ADAMW_BLOCK),), torch.float32, "scales")
     moment = 1 if codes.dtype == torch.float8_e4m3fn else 2
-    _check(_lib.fpo_adamw_state_values(n, moment, _ptr(codes), _ptr(scales), dt, _ptr(out),
+    here = out.get_device()
+    _check(_lib.fpo_adamw_state_values(n, moment, _at(here, codes), _at(here, scales), dt, _at(here, out),
                                        _stream(stream)), "fpo_adamw_state_values")
     return out
 

@@ -464,24 +464,49 @@ __global__ void __launch_bounds__(kThreads, kPass == kNorms ? (kState8 ? 5 : 3) 
     }
 }
 
-// scales[k] = min(1, clip_frac ||W|| / ||x||) from the tensor's chunk sums: thread-strided
-// fp64, a fixed butterfly, then the warps in order.
+// A sum of fp32 numbers and what its additions rounded off (Knuth's two-sum), 48 bits in all.
+struct TwoSum {
+    float hi = 0.f, lo = 0.f;
+    __device__ __forceinline__ void add(float x) {
+        const float s = __fadd_rn(hi, x), b = __fsub_rn(s, hi);
+        lo = __fadd_rn(lo, __fadd_rn(__fsub_rn(hi, __fsub_rn(s, b)), __fsub_rn(x, b)));
+        hi = s;
+    }
+    __device__ __forceinline__ double value() const {
+        return isfinite(hi) ? static_cast<double>(hi) + lo : static_cast<double>(hi);
+    }
+};
+
+// scales[k] = min(1, clip_frac ||W|| / ||x||) from the tensor's chunk sums: thread-strided, a fixed
+// butterfly, then the warps in order.  One block per tensor, whose few fp64 adders would take 10 us
+// for the 22,000 chunks of 45M elements (20 to 33 us with loads one by one); the threads add pairs
+// of fp32 numbers instead, eight loads ahead.
+constexpr int kScaleThreads = 512, kScaleAhead = 8;
+
 template <int CAP>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kScaleThreads)
     adamw_scale_kernel(const __grid_constant__ Table<CAP> t, const float2* __restrict__ part,
                        float clip_frac, float* __restrict__ scales) {
-    const int k = blockIdx.x;
-    double ww = 0.0, xx = 0.0;
-    for (int c = t.first[k] + threadIdx.x; c < t.first[k + 1]; c += kThreads) {
-        ww += part[c].x;
-        xx += part[c].y;
+    const int k = blockIdx.x, end = t.first[k + 1];
+    TwoSum w, x;
+    for (int c = t.first[k] + threadIdx.x; c < end; c += kScaleThreads * kScaleAhead) {
+        float2 p[kScaleAhead];
+#pragma unroll
+        for (int i = 0; i < kScaleAhead; ++i)
+            p[i] = c + i * kScaleThreads < end ? part[c + i * kScaleThreads] : make_float2(0.f, 0.f);
+#pragma unroll
+        for (int i = 0; i < kScaleAhead; ++i) {
+            w.add(p[i].x);
+            x.add(p[i].y);
+        }
     }
+    double ww = w.value(), xx = x.value();
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
         ww += __shfl_xor_sync(0xffffffffu, ww, o);
         xx += __shfl_xor_sync(0xffffffffu, xx, o);
     }
-    __shared__ double sh[2][kThreads / 32];
+    __shared__ double sh[2][kScaleThreads / 32];
     if ((threadIdx.x & 31) == 0) {
         sh[0][threadIdx.x / 32] = ww;
         sh[1][threadIdx.x / 32] = xx;
@@ -489,7 +514,7 @@ __global__ void __launch_bounds__(kThreads)
     __syncthreads();
     if (threadIdx.x != 0) return;
     ww = xx = 0.0;
-    for (int q = 0; q < kThreads / 32; ++q) {
+    for (int q = 0; q < kScaleThreads / 32; ++q) {
         ww += sh[0][q];
         xx += sh[1][q];
     }
@@ -572,7 +597,7 @@ cudaError_t run_adamw(const int* ids, int count, const AdamTensor* ts, const Ada
         adamw_kernel<CAP, kNorms, kState8><<<grid, kThreads, 0, st>>>(t, op, part, nullptr), note_launch();
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
-    adamw_scale_kernel<CAP><<<count, kThreads, 0, st>>>(t, part, op.clip_frac, scales), note_launch();
+    adamw_scale_kernel<CAP><<<count, kScaleThreads, 0, st>>>(t, part, op.clip_frac, scales), note_launch();
     e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     if (op.clip == 1)

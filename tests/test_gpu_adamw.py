@@ -347,6 +347,27 @@ def test_nan_and_infinity(fpo, bits):
             assert np.isnan(m[256:512]).all() and np.isnan(v[256:512]).all()
 
 
+def test_an_infinite_gradient_under_the_clip(fpo):
+    """On the gradient the norm is infinite and the factor 0: the other elements see no gradient.  On
+    the step the norm is NaN (infinity by infinity) and the factor 1."""
+    for clip in (1, 2):
+        x = Tensors([1024], 32, g16=0)
+        x.G[0][300] = float("inf")
+        g, w, m, v = x.before()[0]
+        x.step(fpo, 1, clip)
+        if clip == 2:
+            g = 0 * np.where(np.isfinite(g), g, 0)
+        g = np.where(np.isfinite(g), g, 0)
+        m1, v1, _, _, w1 = definition(g, w, m, v, 0.0, 1, 0)
+        ok = np.arange(1024) != 300
+        gm, gv = x.moments(0)
+        # (m is a difference where the signs differ: 2^-22 of both terms, as in check())
+        assert (np.abs(gm - m1) <= 2.0 ** -22 * (np.abs(m) + np.abs(g)))[ok].all()
+        assert np.allclose(gv[ok], v1[ok], rtol=1e-6, atol=0)
+        assert np.allclose(x.W[0].double().cpu().numpy()[ok], w1[ok], rtol=0, atol=1e-6)
+        assert not np.isfinite(gm[300])
+
+
 def test_zero_blocks_and_extreme_sizes(fpo):
     """Moments over the range of fp32: scales stay in range, values within a unit."""
     n = 2560
