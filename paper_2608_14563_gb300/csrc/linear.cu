@@ -504,11 +504,11 @@ cudaError_t run_rows(const LinearFwd& p, const LinearOut& out, unsigned* status,
 // Clusters of the pair kernels at once (76 without a device: two SMs of 152 each).
 int linear_clusters() {
     using L = GemmPairSmem<256, kPairStages, pair_ksub<256, false, false>()>;
-    constexpr auto kern = tc_gemm_pair_kernel<256, false, false, kPairStages, 1, EpiLinear<256>>;
+    constexpr auto kern = tc_gemm_pair_kernel<256, false, false, kPairStages, 1, EpiLinear<256, kActNone>>;
     DevInfo di;
     int c = 76;
     if (current_device_info(&di) && set_smem_limit<kern>(L::kBytes) == cudaSuccess)
-        c = resident_clusters<kern>(gemm_threads<EpiLinear<256>>(), L::kBytes, di.sm_count, 2);
+        c = resident_clusters<kern>(gemm_threads<EpiLinear<256, kActNone>>(), L::kBytes, di.sm_count, 2);
     cudaGetLastError();
     return c;
 }
@@ -590,44 +590,73 @@ __global__ void __launch_bounds__(kFixupThreads)
     out_row4(out, row * out.ld + n, n, s4);
 }
 
-bool out_maps(EpiLinear<256>::Params* p) {
+bool out_maps(EpiLinear<256, kActAny>::Params* p) {
     return map_out_bf16(&p->ymap, p->o.Y, p->o.M, p->o.N) &&
            map_out_bf16(&p->zmap, p->o.Z ? p->o.Z : p->o.Y, p->o.M, p->o.N);
 }
-bool out_maps(EpiSlope<256>::Params* p) { return map_out_bf16(&p->xmap, p->o.X, p->o.M, p->o.N); }
+bool out_maps(EpiSlope<256, kActAny>::Params* p) {
+    return map_out_bf16(&p->xmap, p->o.X, p->o.M, p->o.N);
+}
+
+// Parameters for another width or activation of an epilogue: the fields are the same.
+template <class To, class From>
+To params_as(const From& from) {
+    static_assert(sizeof(To) == sizeof(From), "the same fields");
+    To to;
+    memcpy(&to, &from, sizeof(to));
+    return to;
+}
 
 // C[M, N] = A B^T through Epi.  A_MN: A is [K, M], else [M, K]; B_MN: B is [K, N], else [N, K].
-template <bool A_MN, bool B_MN, template <int> class Epi, class Out>
-cudaError_t run_pair(const void* A, const void* B, int M, int N, int K, const Out& out,
+// kPlain: there is no activation (fewer kernels to compile).
+template <bool A_MN, bool B_MN, bool kPlain, template <int, int> class Epi, class Out>
+cudaError_t run_pair(const void* A, const void* B, int M, int N, int K, const Out& out, int act,
                      float* scratch, unsigned* status, cudaStream_t st) {
+    constexpr int kAny = kPlain ? kActNone : kActAny;
     const PairPlan pp = pair_plan(M, N, K);
     GemmMaps<1> maps;
     bool ok = A_MN ? map_mnmajor(&maps.a[0], A, K, M) : map_kmajor(&maps.a[0], A, M, K, kBM);
     const int b_rows = pp.single ? pp.single : pp.half ? kHalfBN / 2 : 128;
     ok = ok && (B_MN ? map_mnmajor(&maps.b[0], B, K, N) : map_kmajor(&maps.b[0], B, N, K, b_rows));
-    typename Epi<256>::Params ep;
+    typename Epi<256, kActAny>::Params ep;
     ep.o = out;
     if (!ok || !out_maps(&ep)) return cudaErrorInvalidValue;
-    // the parameters of every tile width have the same fields
-    static_assert(kHalfBN == 128, "e128");
-    typename Epi<128>::Params e128;
-    typename Epi<64>::Params e64;
-    static_assert(sizeof(ep) == sizeof(e128) && sizeof(ep) == sizeof(e64), "the same fields");
-    memcpy(&e128, &ep, sizeof(e128));
-    memcpy(&e64, &ep, sizeof(e64));
-    if (pp.single == 64)
-        return run_gemm<64, A_MN, B_MN, 8, 1, Epi<64>>(
-            maps, e64, make_shape(M, N, K, 64, 1, band_for(false)), status, st);
-    if (pp.single == 128)
-        return run_gemm<128, A_MN, B_MN, 6, 1, Epi<128>>(
-            maps, e128, make_shape(M, N, K, 128, 1, band_for(false)), status, st);
-    if (pp.half)
-        return run_gemm_pair<kHalfBN, A_MN, B_MN, kHalfStages, 1, Epi<kHalfBN>>(
-            maps, e128, make_shape(M, N, K, kHalfBN, 1, band_for(true), kPairBM), status, st);
+    if (pp.single == 64) {
+        using E = Epi<64, kAny>;
+        return run_gemm<64, A_MN, B_MN, 8, 1, E>(maps, params_as<typename E::Params>(ep),
+                                                 make_shape(M, N, K, 64, 1, band_for(false)), status, st);
+    }
+    if (pp.single == 128) {
+        using E = Epi<128, kAny>;
+        return run_gemm<128, A_MN, B_MN, 6, 1, E>(maps, params_as<typename E::Params>(ep),
+                                                  make_shape(M, N, K, 128, 1, band_for(false)), status, st);
+    }
+    if (pp.half) {
+        using E = Epi<kHalfBN, kAny>;
+        return run_gemm_pair<kHalfBN, A_MN, B_MN, kHalfStages, 1, E>(
+            maps, params_as<typename E::Params>(ep),
+            make_shape(M, N, K, kHalfBN, 1, band_for(true), kPairBM), status, st);
+    }
     const GemmShape sh = make_shape(M, N, K, 256, 1, band_for(true), kPairBM);
     SkPlan plan;
-    const cudaError_t e = run_gemm_pair<256, A_MN, B_MN, kPairStages, 1, Epi<256>>(
-        maps, ep, sh, status, st, pp.units > 0 ? scratch : nullptr, &plan, pp.split, &pp.tail);
+    auto run = [&](auto a) {
+        using E = Epi<256, decltype(a)::value>;
+        return run_gemm_pair<256, A_MN, B_MN, kPairStages, 1, E>(
+            maps, params_as<typename E::Params>(ep), sh, status, st, pp.units > 0 ? scratch : nullptr,
+            &plan, pp.split, &pp.tail);
+    };
+    cudaError_t e;
+    if constexpr (kPlain) {
+        e = run(std::integral_constant<int, kActNone>{});
+    } else {
+        switch (act) {
+            case kActRelu: e = run(std::integral_constant<int, kActRelu>{}); break;
+            case kActGelu: e = run(std::integral_constant<int, kActGelu>{}); break;
+            case kActGeluTanh: e = run(std::integral_constant<int, kActGeluTanh>{}); break;
+            case kActSilu: e = run(std::integral_constant<int, kActSilu>{}); break;
+            default: e = run(std::integral_constant<int, kActNone>{}); break;
+        }
+    }
     if (e != cudaSuccess || plan.tail_tiles <= 0) return e;
     return launch_chained(linear_fixup_kernel<Out>, sk_fixup_grid<256>(plan), kFixupThreads, 0, st,
                           sk_fixup_shape(plan, sh), static_cast<const float*>(scratch), out);
@@ -808,8 +837,8 @@ cudaError_t launch_linear(int dtype, const LinearFwd& p, void* workspace, cudaSt
         return run_few<false>(p.W, p.X, p.N, p.K, p.T, out, ws + kHead,
                               reinterpret_cast<float*>(ws + kHead + few_counter_bytes(p.N)),
                               status, st);
-    return run_pair<false, false, EpiLinear>(p.X, p.W, p.T, p.N, p.K, out,
-                                             reinterpret_cast<float*>(ws + kHead), status, st);
+    return run_pair<false, false, false, EpiLinear>(p.X, p.W, p.T, p.N, p.K, out, p.act,
+                                                    reinterpret_cast<float*>(ws + kHead), status, st);
 }
 
 namespace {
@@ -898,7 +927,8 @@ cudaError_t launch_linear_vjp(int dtype, const LinearVjp& p, void* workspace, cu
         out.act = p.act_in;
         e = p.T <= kFewT
                 ? run_few<true>(p.W, dZ, p.K, p.N, p.T, out, ws + l.few, scratch, status, st)
-                : run_pair<false, true, EpiSlope>(dZ, p.W, p.T, p.K, p.N, out, scratch, status, st);
+                : run_pair<false, true, false, EpiSlope>(dZ, p.W, p.T, p.K, p.N, out, p.act_in, scratch,
+                                                           status, st);
         if (e != cudaSuccess) return e;
     }
     if (!p.dW) return cudaSuccess;
@@ -909,7 +939,7 @@ cudaError_t launch_linear_vjp(int dtype, const LinearVjp& p, void* workspace, cu
     out.M = p.N;
     out.N = p.K;
     out.act = kActNone;
-    return run_pair<true, true, EpiSlope>(dZ, p.X, p.N, p.K, p.T, out, scratch, status, st);
+    return run_pair<true, true, true, EpiSlope>(dZ, p.X, p.N, p.K, p.T, out, kActNone, scratch, status, st);
 }
 
 }  // namespace fpo

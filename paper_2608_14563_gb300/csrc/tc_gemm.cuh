@@ -183,12 +183,23 @@ struct RowChunk {
     }
 };
 
+// Whether an epilogue takes one row per thread: with 4 warps, and where it says so (kByRow).
+template <class Epi, class = void>
+struct EpiByRow {
+    static constexpr bool value = Epi::kWarps == 4;
+};
+template <class Epi>
+struct EpiByRow<Epi, decltype(static_cast<void>(Epi::kByRow))> {
+    static constexpr bool value = Epi::kByRow;
+};
+
 // The epilogue's warps.  With Epi::kWarps = 4 each warp owns 32 rows of the CTA's 128 and
 // walks all BN columns, one row per thread (Epi(params, group, row, n0); chunk(params,
 // v[32], column, offset in the tile, io); finish(params, n_block)).  With 8, two warps
-// share the rows and take half of the columns each, and every chunk goes through the warp's
-// staging buffer (RowChunk; Epi(params, group, first row, first column, lane);
-// chunk(params, staged chunk, lane, chunk index); finish(params, lane)).  The functor
+// share the rows and take half of the columns each, by row (Epi::kByRow; n0 the warp's first
+// column) or so that every chunk goes through the warp's staging buffer (RowChunk;
+// Epi(params, group, first row, first column, lane); chunk(params, staged chunk, lane,
+// chunk index); finish(params, lane)).  The functor
 // is made before the accumulator is awaited, so that what its constructor loads arrives
 // during the mainloop.  `ready` waits for the accumulator (false: give up), `release`
 // gives it back once its last columns are in registers.
@@ -196,16 +207,17 @@ template <int BN, class Epi, class Ready, class Release>
 __device__ __forceinline__ bool epilogue_tile(const typename Epi::Params& ep, int g, int row0,
                                               int nb, int warp_half, uint32_t t_row, EpiIO& io,
                                               Ready ready, Release release) {
-    if constexpr (Epi::kWarps == 4) {
-        const int n0 = nb * BN;
+    if constexpr (EpiByRow<Epi>::value) {
+        constexpr int kChunks = BN / 32 / (Epi::kWarps / 4);  // of a warp
+        const int n0 = nb * BN, first = Epi::kWarps == 4 ? 0 : warp_half * kChunks;
         io.row0 = row0;
-        Epi epi(ep, g, row0 + io.lane, n0);
+        Epi epi(ep, g, row0 + io.lane, n0 + first * 32);
         if (!ready()) return false;
 #pragma unroll 1
-        for (int c = 0; c < BN / 32; ++c) {
+        for (int c = first; c < first + kChunks; ++c) {
             float v[32];
             tmem_ld_32x32b_x32(t_row + c * 32, v);
-            if (c == BN / 32 - 1) release();
+            if (c == first + kChunks - 1) release();
             epi.chunk(ep, v, n0 + c * 32, c * 32, io);
         }
         epi.finish(ep, nb);
