@@ -8,7 +8,7 @@
 // Large batches run on the tiles of tc_gemm_pair.cuh, or where these are few of tc_gemm.cuh, with
 // the epilogues of linear_epilogues.cuh.  Batches of at most kFewT tokens run on
 // few_tokens_kernel, with the weights as the 128-row operand and the tokens along N, and forward
-// with at most kRowT on row_kernel.  What the layer's own activation does to the signal, and the
+// with at most row_tokens on row_kernel.  What the layer's own activation does to the signal, and the
 // bias gradient, are one pass over dY (signal_kernel).
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -381,6 +381,12 @@ FewPlan few_plan(int M, int K) {
     p.units = p.tiles * p.k_steps;
     const long long most = (p.units + 1) / 2, sms = sm_count();
     p.ctas = most < sms ? most : sms;
+    // A tile's parts are read by one CTA in turn, each in about a third of the time of a step: more than
+    // sqrt(3.5 k_steps) of them take longer than they save.  20 tokens, 12216 to 488 features 18.5 us
+    // (22.6 without this limit, 17.1 with half of it), 16384 to 128 18.5 (30.8, 17.8), 1024 to 1024
+    // 10.5 (11.3, 13.7); 4096 and 11008 to 1024 and more the same
+    const long long cap = p.tiles * static_cast<long long>(sqrt(3.5 * p.k_steps));
+    if (p.ctas > cap) p.ctas = cap;
     return p;
 }
 int few_bt(int T) { return T <= 16 ? 16 : 32; }
@@ -418,52 +424,102 @@ cudaError_t run_few(const void* W, const void* X, int M, int K, int T, const Out
     return run_few_bt<32, W_MN>(W, X, M, K, T, out, counters, scratch, status, st);
 }
 
-// ------------------------------------------------------------------ one to four tokens
-// Y = act(X W^T + b) + R for T <= kRowT tokens: a warp per feature, whose row of the weights the
-// lanes read 16 bytes each, kRowAhead loads at a time; X comes from L1, and a butterfly adds the
-// lanes' sums.  Nothing has to be set up or added across blocks: one launch, which also clears the
-// status word (no kernel of the call waits for anything).
-// Bound: the weights' bytes: 4096 to 11008 features 17.8 us (5.1 TB/s; few_tokens_kernel 28), to
-// 44032 56 (6.4 TB/s).  8 and 16 loads ahead 19.2 and 20.3; 8 warps a block the same, and with four
-// tokens 26.2 instead of 23.9.
-constexpr int kRowT = 4, kRowWarps = 4, kRowAhead = 4;
+// ------------------------------------------------------------------ a few rows of X
+// Y = act(X W^T + b) + R for T <= row_tokens(dtype): a warp per feature, whose row of the weights the
+// lanes read 16 bytes each (fp32 rows that are no multiple of that: 4), some loads ahead; X comes from
+// L1, and a butterfly adds the lanes' sums.  Nothing has to be set up or added across blocks: one
+// launch, which also clears the status word (no kernel of the call waits for anything).
+// Bound: the weights' bytes.  bf16, 4096 to 11008 features 17.8 us (5.1 TB/s; few_tokens_kernel 28),
+// to 44032 56 (6.4 TB/s).  8 and 16 loads ahead 19.2 and 20.3; 8 warps a block the same, and with four
+// tokens 26.2 instead of 23.9.  fp32 goes to 16 tokens, since the 64-row tiles of the products that take
+// over there cost the same down to one: 3000 to 3000 features, weights in L2, 1 token 5.9 us, 4 8.3, 8
+// 13, 16 25, 17 (on tiles) 46; 767 to 1537 5.2, 5.8, 7.9, 9.5, 16.6.
+constexpr int kRowWarps = 4;
+constexpr int row_tokens(int dtype) { return dtype == 1 ? 4 : 16; }
 
-__device__ __forceinline__ uint4 ld_stream(const uint4* p) {
+template <typename T>
+struct RowOut {
+    const T* bias;
+    const T* residual;
+    T* Y;
+    T* Z;
+    int act;
+};
+
+// A vector of kV values as it is loaded, and acc + w (.) x over it.
+template <typename T, int kV>
+struct RowVec {  // 16 bytes
+    static constexpr int kAhead = 4;
     uint4 u;
-    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
-                 : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w)
-                 : "l"(p));
-    return u;
-}
+    __device__ __forceinline__ void load(const T* p) { u = *reinterpret_cast<const uint4*>(p); }
+    __device__ __forceinline__ void load_stream(const T* p) {
+        asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w)
+                     : "l"(p));
+    }
+    __device__ __forceinline__ void zero() { u = make_uint4(0u, 0u, 0u, 0u); }
+    __device__ __forceinline__ float2 dot(const RowVec& x, float2 acc) const {
+        if constexpr (kV == 8) {
+            acc = fma2(unpack2(u.x), unpack2(x.u.x), acc);
+            acc = fma2(unpack2(u.y), unpack2(x.u.y), acc);
+            acc = fma2(unpack2(u.z), unpack2(x.u.z), acc);
+            return fma2(unpack2(u.w), unpack2(x.u.w), acc);
+        } else {
+            acc = fma2(pair(u.x, u.y), pair(x.u.x, x.u.y), acc);
+            return fma2(pair(u.z, u.w), pair(x.u.z, x.u.w), acc);
+        }
+    }
+    static __device__ __forceinline__ float2 pair(uint32_t a, uint32_t b) {
+        return make_float2(__uint_as_float(a), __uint_as_float(b));
+    }
+};
+template <>
+struct RowVec<float, 1> {
+    static constexpr int kAhead = 8;
+    float f;
+    __device__ __forceinline__ void load(const float* p) { f = *p; }
+    __device__ __forceinline__ void load_stream(const float* p) { f = __ldcs(p); }
+    __device__ __forceinline__ void zero() { f = 0.f; }
+    __device__ __forceinline__ float2 dot(const RowVec& x, float2 acc) const {
+        return make_float2(fmaf(f, x.f, acc.x), 0.f);
+    }
+};
 
-template <int kT>
+__device__ __forceinline__ float row_value(const float* p) { return *p; }
+__device__ __forceinline__ float row_value(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+__device__ __forceinline__ void row_store(float* p, float x) { *p = x; }
+__device__ __forceinline__ void row_store(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
+
+// kT >= tokens: those behind the last are read as it, and not written.
+template <typename T, int kV, int kT>
 __global__ void __launch_bounds__(32 * kRowWarps)
-    row_kernel(const __nv_bfloat16* __restrict__ X, const __nv_bfloat16* __restrict__ W, int N, int K,
-               const __grid_constant__ LinearOut out, unsigned* status) {
+    row_kernel(const T* __restrict__ X, const T* __restrict__ W, int tokens, int N, int K,
+               const __grid_constant__ RowOut<T> out, unsigned* status) {
+    using Vec = RowVec<T, kV>;
     if (blockIdx.x == 0 && threadIdx.x == 0) *status = 0u;
     const int lane = threadIdx.x % 32, feature = blockIdx.x * kRowWarps + threadIdx.x / 32;
     if (feature >= N) return;
-    const int vecs = K / 8;
-    const uint4* w = reinterpret_cast<const uint4*>(W + static_cast<long long>(feature) * K);
+    const int vecs = K / kV;
+    const T* w = W + static_cast<long long>(feature) * K;
     float2 acc[kT];
 #pragma unroll
     for (int t = 0; t < kT; ++t) acc[t] = make_float2(0.f, 0.f);
-    for (int v0 = lane; v0 < vecs; v0 += 32 * kRowAhead) {
-        uint4 u[kRowAhead];
+    for (int v0 = lane; v0 < vecs; v0 += 32 * Vec::kAhead) {
+        Vec u[Vec::kAhead];
 #pragma unroll
-        for (int i = 0; i < kRowAhead; ++i)
-            u[i] = v0 + 32 * i < vecs ? ld_stream(w + v0 + 32 * i) : make_uint4(0u, 0u, 0u, 0u);
+        for (int i = 0; i < Vec::kAhead; ++i) {
+            u[i].zero();
+            if (v0 + 32 * i < vecs) u[i].load_stream(w + static_cast<long long>(v0 + 32 * i) * kV);
+        }
 #pragma unroll
-        for (int i = 0; i < kRowAhead; ++i) {
+        for (int i = 0; i < Vec::kAhead; ++i) {
             if (v0 + 32 * i >= vecs) break;
-            const float2 a = unpack2(u[i].x), b = unpack2(u[i].y), c = unpack2(u[i].z), d = unpack2(u[i].w);
 #pragma unroll
             for (int t = 0; t < kT; ++t) {
-                const uint4 x = reinterpret_cast<const uint4*>(X + static_cast<long long>(t) * K)[v0 + 32 * i];
-                acc[t] = fma2(a, unpack2(x.x), acc[t]);
-                acc[t] = fma2(b, unpack2(x.y), acc[t]);
-                acc[t] = fma2(c, unpack2(x.z), acc[t]);
-                acc[t] = fma2(d, unpack2(x.w), acc[t]);
+                Vec x;
+                x.load(X + static_cast<long long>(min(t, tokens - 1)) * K +
+                       static_cast<long long>(v0 + 32 * i) * kV);
+                acc[t] = u[i].dot(x, acc[t]);
             }
         }
     }
@@ -473,31 +529,44 @@ __global__ void __launch_bounds__(32 * kRowWarps)
         const float r = warp_sum_f32(acc[t].x + acc[t].y);
         if (lane == t) s = r;
     }
-    if (lane >= kT) return;
-    const long long o = lane * out.ld + feature;
-    float2 z = make_float2(s, 0.f);
-    if (out.bias) z.x += __bfloat162float(out.bias[feature]);
-    if (out.Z) out.Z[o] = __float2bfloat16_rn(z.x);
-    with_act(out.act, [&](auto act) { z = act_value2<act.value>(z); });
-    if (out.residual) z.x += __bfloat162float(out.residual[o]);
-    out.Y[o] = __float2bfloat16_rn(z.x);
+    if (lane >= tokens) return;
+    const long long o = static_cast<long long>(lane) * N + feature;
+    if (out.bias) s += row_value(out.bias + feature);
+    if (out.Z) row_store(out.Z + o, s);
+    with_act(out.act, [&](auto act) {
+        if constexpr (std::is_same_v<T, float>)
+            s = act_value<act.value>(s);
+        else
+            s = act_value2<act.value>(make_float2(s, 0.f)).x;
+    });
+    if (out.residual) s += row_value(out.residual + o);
+    row_store(out.Y + o, s);
 }
 
-template <int kT>
-cudaError_t run_rows_t(const LinearFwd& p, const LinearOut& out, unsigned* status, cudaStream_t st) {
-    row_kernel<kT><<<(p.N + kRowWarps - 1) / kRowWarps, 32 * kRowWarps, 0, st>>>(
-        static_cast<const __nv_bfloat16*>(p.X), static_cast<const __nv_bfloat16*>(p.W), p.N, p.K, out,
-        status),
+template <typename T, int kV, int kT>
+cudaError_t run_rows_t(const LinearFwd& p, unsigned* status, cudaStream_t st) {
+    const RowOut<T> out{static_cast<const T*>(p.bias), static_cast<const T*>(p.residual),
+                        static_cast<T*>(p.Y), static_cast<T*>(p.Z), p.act};
+    row_kernel<T, kV, kT><<<(p.N + kRowWarps - 1) / kRowWarps, 32 * kRowWarps, 0, st>>>(
+        static_cast<const T*>(p.X), static_cast<const T*>(p.W), p.T, p.N, p.K, out, status),
         note_launch();
     return cudaGetLastError();
 }
-cudaError_t run_rows(const LinearFwd& p, const LinearOut& out, unsigned* status, cudaStream_t st) {
-    switch (p.T) {
-        case 1: return run_rows_t<1>(p, out, status, st);
-        case 2: return run_rows_t<2>(p, out, status, st);
-        case 3: return run_rows_t<3>(p, out, status, st);
-        default: return run_rows_t<4>(p, out, status, st);
+template <typename T, int kV>
+cudaError_t run_rows_v(const LinearFwd& p, unsigned* status, cudaStream_t st) {
+    if (p.T == 1) return run_rows_t<T, kV, 1>(p, status, st);
+    if (p.T == 2) return run_rows_t<T, kV, 2>(p, status, st);
+    if constexpr (std::is_same_v<T, float>) {
+        if (p.T > 8) return run_rows_t<T, kV, 16>(p, status, st);
+        if (p.T > 4) return run_rows_t<T, kV, 8>(p, status, st);
+    } else {
+        if (p.T == 3) return run_rows_t<T, kV, 3>(p, status, st);
     }
+    return run_rows_t<T, kV, 4>(p, status, st);
+}
+cudaError_t run_rows(int dtype, const LinearFwd& p, unsigned* status, cudaStream_t st) {
+    if (dtype == 1) return run_rows_v<__nv_bfloat16, 8>(p, status, st);
+    return p.K % 4 == 0 ? run_rows_v<float, 4>(p, status, st) : run_rows_v<float, 1>(p, status, st);
 }
 
 // ------------------------------------------------------------------ pair tiles
@@ -810,19 +879,20 @@ cudaError_t run_signal_v(const LinearVjp& p, T* dZ, float* part, unsigned* count
 }  // namespace
 
 size_t linear_clear_bytes(int dtype, int T, int N, int K) {
-    if (dtype == 1 && T <= kRowT) return 0;  // the kernel does it
+    if (T <= row_tokens(dtype)) return 0;  // the kernel does it
     return dtype == 1 && T <= kFewT ? kHead + few_counter_bytes(N) : sizeof(unsigned);
 }
 size_t linear_workspace_bytes(int dtype, int T, int N, int K) {
-    if (dtype != 1 || T <= kRowT) return kHead;
+    if (dtype != 1 || T <= row_tokens(dtype)) return kHead;
     if (T <= kFewT) return kHead + few_counter_bytes(N) + few_scratch_bytes(N, K, T);
     return kHead + pair_scratch_bytes(T, N, K);
 }
 
 cudaError_t launch_linear(int dtype, const LinearFwd& p, void* workspace, cudaStream_t st) {
-    if (dtype == 0) return launch_linear_f32(p, st);
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     unsigned* status = reinterpret_cast<unsigned*>(ws);
+    if (p.T <= row_tokens(dtype)) return run_rows(dtype, p, status, st);
+    if (dtype == 0) return launch_linear_f32(p, st);
     LinearOut out;
     out.bias = static_cast<const __nv_bfloat16*>(p.bias);
     out.residual = static_cast<const __nv_bfloat16*>(p.residual);
@@ -832,7 +902,6 @@ cudaError_t launch_linear(int dtype, const LinearFwd& p, void* workspace, cudaSt
     out.M = p.T;
     out.N = p.N;
     out.act = p.act;
-    if (p.T <= kRowT) return run_rows(p, out, status, st);
     if (p.T <= kFewT)
         return run_few<false>(p.W, p.X, p.N, p.K, p.T, out, ws + kHead,
                               reinterpret_cast<float*>(ws + kHead + few_counter_bytes(p.N)),

@@ -170,6 +170,51 @@ struct SliceLoader {
     }
 };
 
+// SEpiSlope over a thread's rows row0 + 64 g + 0..3 and columns col0 + 64 h + 0..3 (g, h < kH; with a
+// split those of its block's rank).  What four rows read is loaded before the first of them is used,
+// and the activation is chosen once: row by row, where every load and branch waits for itself, 8903 x
+// 23 x 1370 with gelu's slope took 80 us, so 60 (34 without); 3906 x 118 x 2602 125 and 121.  The
+// forward epilogue gains nothing by it and its products lose 2% to the registers.
+template <int kH>
+__device__ __forceinline__ void slope_rows(const SimtOps& ops, const SEpiSlope& ep,
+                                           const float2 (&acc)[4 * kH][2 * kH], int row0, int col0,
+                                           int rank) {
+    const bool vec = (ep.ld & 3) == 0;
+    auto mine = [&](int i) {  // row i of the thread
+        return row0 + 64 * (i / 4) + i % 4 < ops.M && (ops.splits == 1 || i % ops.splits == rank);
+    };
+    auto at = [&](int i, int h) { return (row0 + 64 * (i / 4) + i % 4) * ep.ld + col0 + 64 * h; };
+    with_act(ep.z_in ? ep.act : kActNone, [&](auto act) {
+#pragma unroll
+        for (int g = 0; g < kH; ++g) {
+            float4 z[4][kH];
+            if constexpr (act.value != kActNone) {
+#pragma unroll
+                for (int q = 0; q < 4 * kH; ++q) {
+                    const int i = 4 * g + q / kH, h = q % kH;
+                    z[q / kH][h] = mine(i) ? ld4(ep.z_in + at(i, h), ops.N - col0 - 64 * h, vec)
+                                           : make_float4(0.f, 0.f, 0.f, 0.f);
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < 4 * kH; ++q) {
+                const int i = 4 * g + q / kH, h = q % kH;
+                const int nv = ops.N - col0 - 64 * h;  // columns inside the matrix (4 or more: all)
+                if (nv <= 0 || !mine(i)) continue;
+                float v[4] = {acc[i][2 * h].x, acc[i][2 * h].y, acc[i][2 * h + 1].x,
+                              acc[i][2 * h + 1].y};
+                if constexpr (act.value != kActNone) {
+                    const float4& z4 = z[q / kH][h];
+                    const float x[4] = {z4.x, z4.y, z4.z, z4.w};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[j] *= act_slope<act.value>(x[j]);
+                }
+                st4(ep.dX + at(i, h), v, nv, vec);
+            }
+        }
+    });
+}
+
 // Thread (tx, ty) of 16 x 16 owns rows 64 i + 4 ty + 0..3 and columns 64 h + 4 tx + 0..3 of
 // the tile for i, h < BT / 64.
 template <int BT, bool kAKC, bool kBKC, class Epi>
@@ -285,123 +330,114 @@ __global__ void __launch_bounds__(kThreads, 2)
         cluster_sync();  // no block leaves while another reads its shared memory
     }
 
+    if constexpr (std::is_same_v<Epi, SEpiSlope>) {
+        slope_rows<kH>(ops, ep, acc, m0 + 4 * ty, n0 + 4 * tx, rank);
+    } else {
 #pragma unroll
-    for (int i = 0; i < kR; ++i) {
-        if (S > 1 && i % S != rank) continue;
-        const int row = m0 + 64 * (i / 4) + 4 * ty + i % 4;
-        const bool rv = row < ops.M;
-        if constexpr (std::is_same_v<Epi, SEpiLse>) {
-            // all 16 threads sharing this row take part in the reductions
-            const int yt = rv ? ep.y[row] : -1;
+        for (int i = 0; i < kR; ++i) {
+            if (S > 1 && i % S != rank) continue;
+            const int row = m0 + 64 * (i / 4) + 4 * ty + i % 4;
+            const bool rv = row < ops.M;
+            if constexpr (std::is_same_v<Epi, SEpiLse>) {
+                // all 16 threads sharing this row take part in the reductions
+                const int yt = rv ? ep.y[row] : -1;
 #pragma unroll
-            for (int h = 0; h < kH; ++h) {
-                const int col = n0 + 64 * h + 4 * tx;
-                const int nv = ops.N - col;  // columns inside the matrix (4 or more: all)
-                const float v[4] = {acc[i][2 * h].x, acc[i][2 * h].y, acc[i][2 * h + 1].x,
-                                    acc[i][2 * h + 1].y};
-                float mx = -INFINITY;
+                for (int h = 0; h < kH; ++h) {
+                    const int col = n0 + 64 * h + 4 * tx;
+                    const int nv = ops.N - col;  // columns inside the matrix (4 or more: all)
+                    const float v[4] = {acc[i][2 * h].x, acc[i][2 * h].y, acc[i][2 * h + 1].x,
+                                        acc[i][2 * h + 1].y};
+                    float mx = -INFINITY;
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (j < nv) mx = fmaxf(mx, v[j]);
-                mx = hmax16(mx);
-                float s = 0.f;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (j < nv) {
-                        s += expf(v[j] - mx);
-                        if (rv && col + j == yt && ep.zy) ep.zy[row] = v[j];
-                    }
-                }
-                s = hsum16(s);
-                if (rv && ep.z && nv > 0) st4(ep.z + row * ep.ldz + col, v, nv, true);
-                if (rv && tx == 0 && n0 + 64 * h < ops.N)
-                    ep.part[static_cast<long long>(row) * ep.part_ld + n0 / 64 + h] =
-                        make_float2(mx, s);
-            }
-        } else {
-            if (!rv) continue;
-#pragma unroll
-            for (int h = 0; h < kH; ++h) {
-                const int col = n0 + 64 * h + 4 * tx;
-                const int nv = ops.N - col;  // columns inside the matrix (4 or more: all)
-                if (nv <= 0) continue;
-                const float v[4] = {acc[i][2 * h].x, acc[i][2 * h].y, acc[i][2 * h + 1].x,
-                                    acc[i][2 * h + 1].y};
-                if constexpr (std::is_same_v<Epi, SEpiError>) {
-                    const float l = ep.lse[row];
-                    const int yt = ep.y[row];
-                    float e[4];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) e[j] = error_value_f32(v[j], l, col + j == yt, ep.s);
-                    st4(ep.E + row * ep.ldE + col, e, nv, true);
-                } else if constexpr (std::is_same_v<Epi, SEpiStore>) {
-                    st4(ep.C + row * ep.ld + col, v, nv, (ep.ld & 3) == 0);
-                } else if constexpr (std::is_same_v<Epi, SEpiSwiglu>) {
-                    const long long off = row * ep.ld + col;
-                    const bool vec = (ep.ld & 3) == 0;
-                    const float4 a4 = ld4(ep.a + off, nv, vec), b4 = ld4(ep.b + off, nv, vec);
-                    const float xa[4] = {a4.x, a4.y, a4.z, a4.w}, xb[4] = {b4.x, b4.y, b4.z, b4.w};
-                    float da[4], db[4];
+                    for (int j = 0; j < 4; ++j)
+                        if (j < nv) mx = fmaxf(mx, v[j]);
+                    mx = hmax16(mx);
+                    float s = 0.f;
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const float sg = 1.f / (1.f + expf(-xa[j]));
-                        da[j] = v[j] * xb[j] * sg * fmaf(xa[j], 1.f - sg, 1.f);
-                        db[j] = v[j] * xa[j] * sg;
+                        if (j < nv) {
+                            s += expf(v[j] - mx);
+                            if (rv && col + j == yt && ep.zy) ep.zy[row] = v[j];
+                        }
                     }
-                    st4(ep.dA + off, da, nv, vec);
-                    st4(ep.dB + off, db, nv, vec);
-                } else if constexpr (std::is_same_v<Epi, SEpiLinear>) {
-                    const long long off = row * ep.ld + col;
-                    const bool vec = (ep.ld & 3) == 0;
-                    float z[4] = {v[0], v[1], v[2], v[3]}, r[4] = {0.f, 0.f, 0.f, 0.f};
-                    if (ep.bias) {
-                        const float4 b4 = ld4(ep.bias + col, nv, true);
-                        z[0] += b4.x;
-                        z[1] += b4.y;
-                        z[2] += b4.z;
-                        z[3] += b4.w;
-                    }
-                    if (ep.Z) st4(ep.Z + off, z, nv, vec);
-                    if (ep.residual) {
-                        const float4 r4 = ld4(ep.residual + off, nv, vec);
-                        r[0] = r4.x;
-                        r[1] = r4.y;
-                        r[2] = r4.z;
-                        r[3] = r4.w;
-                    }
-                    with_act(ep.act, [&](auto act) {
+                    s = hsum16(s);
+                    if (rv && ep.z && nv > 0) st4(ep.z + row * ep.ldz + col, v, nv, true);
+                    if (rv && tx == 0 && n0 + 64 * h < ops.N)
+                        ep.part[static_cast<long long>(row) * ep.part_ld + n0 / 64 + h] =
+                            make_float2(mx, s);
+                }
+            } else {
+                if (!rv) continue;
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) z[j] = act_value<act.value>(z[j]);
-                    });
-                    if (ep.residual) {
+                for (int h = 0; h < kH; ++h) {
+                    const int col = n0 + 64 * h + 4 * tx;
+                    const int nv = ops.N - col;  // columns inside the matrix (4 or more: all)
+                    if (nv <= 0) continue;
+                    const float v[4] = {acc[i][2 * h].x, acc[i][2 * h].y, acc[i][2 * h + 1].x,
+                                        acc[i][2 * h + 1].y};
+                    if constexpr (std::is_same_v<Epi, SEpiError>) {
+                        const float l = ep.lse[row];
+                        const int yt = ep.y[row];
+                        float e[4];
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) z[j] += r[j];
-                    }
-                    st4(ep.Y + off, z, nv, vec);
-                } else if constexpr (std::is_same_v<Epi, SEpiSlope>) {
-                    const long long off = row * ep.ld + col;
-                    const bool vec = (ep.ld & 3) == 0;
-                    float o[4] = {v[0], v[1], v[2], v[3]};
-                    if (ep.z_in) {
-                        const float4 z4 = ld4(ep.z_in + off, nv, vec);
-                        const float z[4] = {z4.x, z4.y, z4.z, z4.w};
+                        for (int j = 0; j < 4; ++j) e[j] = error_value_f32(v[j], l, col + j == yt, ep.s);
+                        st4(ep.E + row * ep.ldE + col, e, nv, true);
+                    } else if constexpr (std::is_same_v<Epi, SEpiStore>) {
+                        st4(ep.C + row * ep.ld + col, v, nv, (ep.ld & 3) == 0);
+                    } else if constexpr (std::is_same_v<Epi, SEpiSwiglu>) {
+                        const long long off = row * ep.ld + col;
+                        const bool vec = (ep.ld & 3) == 0;
+                        const float4 a4 = ld4(ep.a + off, nv, vec), b4 = ld4(ep.b + off, nv, vec);
+                        const float xa[4] = {a4.x, a4.y, a4.z, a4.w}, xb[4] = {b4.x, b4.y, b4.z, b4.w};
+                        float da[4], db[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const float sg = 1.f / (1.f + expf(-xa[j]));
+                            da[j] = v[j] * xb[j] * sg * fmaf(xa[j], 1.f - sg, 1.f);
+                            db[j] = v[j] * xa[j] * sg;
+                        }
+                        st4(ep.dA + off, da, nv, vec);
+                        st4(ep.dB + off, db, nv, vec);
+                    } else if constexpr (std::is_same_v<Epi, SEpiLinear>) {
+                        const long long off = row * ep.ld + col;
+                        const bool vec = (ep.ld & 3) == 0;
+                        float z[4] = {v[0], v[1], v[2], v[3]}, r[4] = {0.f, 0.f, 0.f, 0.f};
+                        if (ep.bias) {
+                            const float4 b4 = ld4(ep.bias + col, nv, true);
+                            z[0] += b4.x;
+                            z[1] += b4.y;
+                            z[2] += b4.z;
+                            z[3] += b4.w;
+                        }
+                        if (ep.Z) st4(ep.Z + off, z, nv, vec);
+                        if (ep.residual) {
+                            const float4 r4 = ld4(ep.residual + off, nv, vec);
+                            r[0] = r4.x;
+                            r[1] = r4.y;
+                            r[2] = r4.z;
+                            r[3] = r4.w;
+                        }
                         with_act(ep.act, [&](auto act) {
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) o[j] *= act_slope<act.value>(z[j]);
+                            for (int j = 0; j < 4; ++j) z[j] = act_value<act.value>(z[j]);
                         });
+                        if (ep.residual) {
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) z[j] += r[j];
+                        }
+                        st4(ep.Y + off, z, nv, vec);
+                    } else {
+                        const long long off = row * ep.ld + col;
+                        const bool vec = (ep.ld & 3) == 0;
+                        if (float* wm = ep.W_master[g]) {
+                            const float4 w4 = ld4(wm + off, nv, vec);
+                            const float nw[4] = {fmaf(ep.neg_lr, v[0], w4.x), fmaf(ep.neg_lr, v[1], w4.y),
+                                                 fmaf(ep.neg_lr, v[2], w4.z), fmaf(ep.neg_lr, v[3], w4.w)};
+                            st4(wm + off, nw, nv, vec);
+                            if (ep.W_out[g]) st4(ep.W_out[g] + off, nw, nv, vec);
+                        }
+                        if (ep.G_out[g]) st4(ep.G_out[g] + off, v, nv, vec);
                     }
-                    st4(ep.dX + off, o, nv, vec);
-                } else {
-                    const long long off = row * ep.ld + col;
-                    const bool vec = (ep.ld & 3) == 0;
-                    if (float* wm = ep.W_master[g]) {
-                        const float4 w4 = ld4(wm + off, nv, vec);
-                        const float nw[4] = {fmaf(ep.neg_lr, v[0], w4.x), fmaf(ep.neg_lr, v[1], w4.y),
-                                             fmaf(ep.neg_lr, v[2], w4.z), fmaf(ep.neg_lr, v[3], w4.w)};
-                        st4(wm + off, nw, nv, vec);
-                        if (ep.W_out[g]) st4(ep.W_out[g] + off, nw, nv, vec);
-                    }
-                    if (ep.G_out[g]) st4(ep.G_out[g] + off, v, nv, vec);
                 }
             }
         }

@@ -31,6 +31,8 @@ SHAPES = [("bf16", 1, 8, 8), ("bf16", 1, 4096, 1416), ("bf16", 1, 72, 11008), ("
           ("bf16", 384, 4096, 4096), ("bf16", 1024, 8, 4104), ("bf16", 2000, 136, 8),
           ("bf16", 5000, 2056, 2048), ("bf16", 5000, 11008, 2048),
           ("bf16", 9000, 1024, 1288), ("f32", 1, 1, 1), ("f32", 7, 3, 5), ("f32", 1, 700, 1001),
+          ("f32", 2, 4096, 72), ("f32", 3, 301, 1000), ("f32", 5, 1024, 264), ("f32", 11, 2049, 65),
+          ("f32", 16, 2048, 136), ("f32", 17, 2048, 136),
           ("f32", 130, 67, 129), ("f32", 200, 256, 384), ("f32", 777, 767, 129), ("f32", 65, 2049, 64)]
 
 
@@ -188,7 +190,7 @@ def test_gradients_match_differences(fpo, act, act_in, T, k, n):
 # rows, few tokens, single CTAs, k ranges of every tile, pair tiles with a split last wave; fp32
 @pytest.mark.parametrize("dtype,T,k,n", [("bf16", 3, 264, 520), ("bf16", 20, 264, 520), ("bf16", 100, 264, 520),
                                          ("bf16", 1024, 11008, 1032), ("bf16", 384, 4096, 4096),
-                                         ("bf16", 5000, 11008, 2048), ("f32", 70, 900, 65), ("f32", 300, 64, 132)])
+                                         ("bf16", 5000, 11008, 2048), ("f32", 6, 264, 520), ("f32", 70, 900, 65), ("f32", 300, 64, 132)])
 def test_in_place_residual(fpo, dtype, T, k, n):
     d = inputs(dtype, T, k, n)
     y = torch.empty(T, n, dtype=DT[dtype], device="cuda")
@@ -215,7 +217,7 @@ def test_same_bits_every_time(fpo, dtype, T, k, n):
         assert all(torch.equal(a, b) for a, b in zip(first, run()))
 
 
-@pytest.mark.parametrize("dtype,T", [("bf16", 9), ("bf16", 300), ("f32", 40)])
+@pytest.mark.parametrize("dtype,T", [("bf16", 9), ("bf16", 300), ("f32", 9), ("f32", 40)])
 def test_nan_and_infinity_stay_in_their_rows(fpo, dtype, T):
     k, n = 136, 264
     d = inputs(dtype, T, k, n)
