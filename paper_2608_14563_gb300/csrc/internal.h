@@ -276,6 +276,8 @@ cudaError_t launch_linear_vjp(int dtype, const LinearVjp& p, void* workspace, cu
 cudaError_t launch_linear_f32(const LinearFwd& p, cudaStream_t st);
 cudaError_t launch_linear_dx_f32(int T, int N, int K, const float* dZ, const float* W,
                                  const float* Z_in, int act_in, float* dX, cudaStream_t st);
+cudaError_t launch_linear_dw_f32(int T, int N, int K, const float* dZ, const float* X, float* dW,
+                                 cudaStream_t st);
 
 // Which tcgen05 GEMM kernel the launchers use: 0 = single-CTA 128 x 256 tiles,
 // 1 = CTA-pair 256 x 256 tiles.

@@ -982,9 +982,8 @@ cudaError_t launch_linear_vjp(int dtype, const LinearVjp& p, void* workspace, cu
                                      static_cast<const float*>(p.act_in != kActNone ? p.Z_in : nullptr),
                                      p.act_in, static_cast<float*>(p.dX), st);
         if (e != cudaSuccess || !p.dW) return e;
-        const float* x = static_cast<const float*>(p.X);
-        float* dw = static_cast<float*>(p.dW);
-        return launch_update_f32(1, p.T, p.N, p.K, &dzf, &x, 0.f, nullptr, nullptr, &dw, st);
+        return launch_linear_dw_f32(p.T, p.N, p.K, dzf, static_cast<const float*>(p.X),
+                                    static_cast<float*>(p.dW), st);
     }
     if (p.dX) {
         SlopeOut out;

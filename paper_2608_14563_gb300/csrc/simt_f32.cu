@@ -518,15 +518,55 @@ cudaError_t run_tile(SimtOps ops, const Epi& ep, int groups, cudaStream_t st) {
 }
 
 
-// Tiles of 128 or 64, whichever simt_cost estimates faster (the same sums either way).
+// How a product of the linear layer runs (its sums have no order of another call's to keep): tiles and
+// blocks per cluster along K by the same measured rates, and by what a wave of blocks costs beside its
+// slices, alone on their SMs or not: 2600 or 7700 cycles, with a split 3100 or 6300 more.  Clusters of
+// more than 4 blocks have an SM to each block only up to nine tenths of the SMs.
+//   M x N x K, us by simt_split and by this: 513 x 511 x 1025 41 and 28 (128-tiles by 7; 64 by 4), 118 x
+//   2602 x 3906 122 and 90 (128 by 7; 128 by 6), 100 x 3000 x 3000 105 and 76, 656 x 287 x 522 25 and 17,
+//   3906 x 2602 x 118 86 and 76 (one wave's set-up more than simt_cost counts); of 36 products the
+//   choice is within 4% of the best of all tiles and splits in 31, and 24% off at most (10 us for 8).
+struct LinearSplit {
+    int tile, splits;
+};
+LinearSplit linear_split(int M, int N, int K) {
+    const int sms = sm_count(), slices = (K + kKs - 1) / kKs;
+    LinearSplit best{128, 1};
+    double least = 0.0;
+    for (int BT = 64; BT <= 128; BT += 64) {
+        const bool wide = BT == 128;
+        const double alone = wide ? 3450.0 : 1420.0, shared = wide ? 2770.0 : 970.0;
+        const long long tiles = simt_tiles(M, N, BT);
+        for (int S = 1; S <= kMaxSplit && (S == 1 || slices / S >= 4); ++S) {
+            const long long cap = S > 4 ? (2LL * sms / S) * 9 / 10 : 2LL * sms / S;  // clusters at once
+            const long long full = tiles / cap, rem = tiles % cap;
+            const double wave = (wide ? 7700.0 : 2600.0) + (S == 1 ? 0.0 : wide ? 6300.0 : 3100.0);
+            const double steps = (slices + S - 1) / S;
+            double cost = full * (steps * 2 * shared + wave);
+            if (rem > 0)
+                cost += steps * (rem * S <= (S > 4 ? 0.91 : 1.0) * sms ? alone : 2 * shared) + wave;
+            if (least == 0.0 || cost < least) {
+                least = cost;
+                best = {BT, S};
+            }
+        }
+    }
+    return best;
+}
+
+// Tiles of 128 or 64: `tile`, or, 0, whichever simt_cost estimates faster (the same sums either way).
 template <bool kAKC, bool kBKC, class Epi>
-cudaError_t run(const SimtOps& ops, const Epi& ep, int groups, cudaStream_t st) {
+cudaError_t run(const SimtOps& ops, const Epi& ep, int groups, cudaStream_t st, int tile = 0) {
     if (ops.M <= 0 || ops.N <= 0) return cudaSuccess;
-    const int sms = sm_count(), slices = (ops.K + kKs - 1) / kKs;
-    const double c128 = simt_cost(128, groups * simt_tiles(ops.M, ops.N, 128), slices, ops.splits, sms);
-    const double c64 = simt_cost(64, groups * simt_tiles(ops.M, ops.N, 64), slices, ops.splits, sms);
-    const int tile = g_simt_tile.load(std::memory_order_relaxed);
-    if (tile ? tile == 128 : c128 <= c64) return run_tile<128, kAKC, kBKC>(ops, ep, groups, st);
+    if (const int forced = g_simt_tile.load(std::memory_order_relaxed)) tile = forced;
+    if (tile == 0) {
+        const int sms = sm_count(), slices = (ops.K + kKs - 1) / kKs;
+        const double c128 =
+            simt_cost(128, groups * simt_tiles(ops.M, ops.N, 128), slices, ops.splits, sms);
+        const double c64 = simt_cost(64, groups * simt_tiles(ops.M, ops.N, 64), slices, ops.splits, sms);
+        tile = c128 <= c64 ? 128 : 64;
+    }
+    if (tile == 128) return run_tile<128, kAKC, kBKC>(ops, ep, groups, st);
     return run_tile<64, kAKC, kBKC>(ops, ep, groups, st);
 }
 
@@ -545,6 +585,14 @@ SimtOps ops_of(const float* A, long long lda, const float* B, long long ldb, int
     o.vec_a = lda % 4 == 0;  // the bases are 16-byte aligned
     o.vec_b = ldb % 4 == 0;
     return o;
+}
+
+// A product of the linear layer.
+template <bool kAKC, bool kBKC, class Epi>
+cudaError_t run_linear(SimtOps ops, const Epi& ep, cudaStream_t st) {
+    const LinearSplit l = linear_split(ops.M, ops.N, ops.K);
+    ops.splits = l.splits;
+    return run<kAKC, kBKC>(ops, ep, 1, st, l.tile);
 }
 
 }  // namespace
@@ -586,16 +634,25 @@ cudaError_t launch_swiglu_f32(int T, int d, int d_ff, const float* g, const floa
 cudaError_t launch_linear_f32(const LinearFwd& p, cudaStream_t st) {
     const SEpiLinear ep{static_cast<const float*>(p.bias), static_cast<const float*>(p.residual),
                         static_cast<float*>(p.Y), static_cast<float*>(p.Z), p.N, p.act};
-    return run<true, true>(ops_of(static_cast<const float*>(p.X), p.K,
-                                  static_cast<const float*>(p.W), p.K, p.T, p.N, p.K, p.T),
-                           ep, 1, st);
+    return run_linear<true, true>(ops_of(static_cast<const float*>(p.X), p.K,
+                                         static_cast<const float*>(p.W), p.K, p.T, p.N, p.K, p.T),
+                                  ep, st);
 }
 
 cudaError_t launch_linear_dx_f32(int T, int N, int K, const float* dZ, const float* W,
                                  const float* Z_in, int act_in, float* dX, cudaStream_t st) {
     // dX[t, i] = sum_o dZ[t, o] W[o, i]
     const SEpiSlope ep{Z_in, dX, K, act_in};
-    return run<true, false>(ops_of(dZ, N, W, K, T, K, N, T), ep, 1, st);
+    return run_linear<true, false>(ops_of(dZ, N, W, K, T, K, N, T), ep, st);
+}
+
+cudaError_t launch_linear_dw_f32(int T, int N, int K, const float* dZ, const float* X, float* dW,
+                                 cudaStream_t st) {
+    // dW[o, i] = sum_t dZ[t, o] X[t, i]: the update's kernel, which leaves the gradient only
+    SEpiUpdate ep = {};
+    ep.G_out[0] = dW;
+    ep.ld = K;
+    return run_linear<false, false>(ops_of(dZ, N, X, K, N, K, T, N), ep, st);
 }
 
 cudaError_t launch_update_f32(int n, int T, int d, int d_ff, const float* const* g,
