@@ -766,8 +766,9 @@ __device__ __forceinline__ void sig_store(T* p, const float (&x)[kV]) {
 }
 
 // status (or null): this kernel is the call's first and clears it and `clear_words` words behind it.
-// With more ranges than one the last block of a column group to finish (counters, zero at the start)
-// adds the ranges' sums in their order.
+// With more ranges than one their sums are added in their order: without counters the ranges are the
+// blocks of one cluster, whose first reads the others' shared memory; with them (zero at the start)
+// by the last block of a column group to finish.
 template <typename T, int kV>
 __global__ void __launch_bounds__(kSigThreads)
     signal_kernel(const T* dY, const T* Z, int act, int rows, int N, int rows_per, T* dZ, float* part,
@@ -827,6 +828,23 @@ __global__ void __launch_bounds__(kSigThreads)
         if (mine) dbias[n] = t;
         return;
     }
+    if (!counters) {
+        __shared__ float total[kSigLanes * kV];
+        if (mine) total[c] = t;
+        __syncwarp();
+        cluster_sync();
+        if (mine && blockIdx.y == 0) {
+            const uint32_t at = smem_u32(total + c);
+            t = 0.f;
+#pragma unroll 8
+            for (unsigned r = 0; r < gridDim.y; ++r)
+                t += __uint_as_float(ld_shared_cluster_u32(mapa_shared(at, r)));
+            dbias[n] = t;
+        }
+        __syncwarp();
+        cluster_sync();  // until the first has read this one's
+        return;
+    }
     if (mine) part[static_cast<long long>(blockIdx.y) * N + n] = t;
     __threadfence();
     __syncthreads();
@@ -846,34 +864,59 @@ struct SignalPlan {
     int cols;      // column blocks
     int rows_per;  // rows of a range, a multiple of kSigRows
     int ranges;
+    bool cluster;  // the ranges are a cluster's blocks (or one)
 };
 int sig_v(int dtype, int N) { return dtype == 1 ? 8 : N % 4 == 0 ? 4 : 1; }
-SignalPlan signal_plan(int dtype, int T, int N) {
-    const int per = kSigLanes * sig_v(dtype, N);
+// Up to 2048 rows, or 8192 without an activation to compute, the ranges are a cluster's blocks, of 64 or
+// 256 rows at least: no counters to clear and wait for.  us with 256 rows and counters, and so: 512 x
+// 1024 fp32 gelu 18.5 and 5.9, bias sums alone 8.3 and 3.1; 2048 x 256 bf16 gelu 14.5 and 8.9, alone 8.6
+// and 3.2; 200 x 256 bf16 gelu (one range) 6.6 and 4.1.  Above that eight blocks of a column group are too
+// few: 4096 x 128 fp32 gelu 18.6 and 24.9, 8192 x 256 bf16 14.4 and 27.8, alone 8.3 and 6.0; 16384 x 128
+// alone 8.5 and 9.7.
+SignalPlan signal_plan(int dtype, int T, int N, int act) {
+    const int per = kSigLanes * sig_v(dtype, N), least = act == kActNone ? 256 : 64;
     SignalPlan p;
     p.cols = (N + per - 1) / per;
-    const long long blocks = 4LL * sm_count();
-    long long ranges = blocks / p.cols;
-    const long long most = (T + 255) / 256;  // of at least 256 rows: one needs no counters
+    p.cluster = T <= (act == kActNone ? 8192 : 2048);
+    const long long most = 4LL * sm_count() / p.cols;  // ranges
+    long long ranges = p.cluster ? (T + least - 1) / least : (T + 255) / 256;
+    if (p.cluster && ranges > 8) ranges = 8;
     if (ranges > most) ranges = most;
     if (ranges < 1) ranges = 1;
     p.rows_per = static_cast<int>((((T + ranges - 1) / ranges) + kSigRows - 1) / kSigRows * kSigRows);
     p.ranges = (T + p.rows_per - 1) / p.rows_per;
+    if (p.ranges == 1) p.cluster = true;
     return p;
 }
 
 size_t signal_counter_bytes(const SignalPlan& p) {
-    return p.ranges > 1 ? up256(static_cast<size_t>(p.cols) * sizeof(unsigned)) : 0;
+    return p.cluster ? 0 : up256(static_cast<size_t>(p.cols) * sizeof(unsigned));
 }
 
 template <typename T, int kV>
 cudaError_t run_signal_v(const LinearVjp& p, T* dZ, float* part, unsigned* counters, unsigned* status,
                          size_t clear_bytes, const SignalPlan& sp, cudaStream_t st) {
-    return launch_chained(
-        signal_kernel<T, kV>, dim3(sp.cols, sp.ranges), kSigThreads, 0, st,
-        static_cast<const T*>(p.dY), static_cast<const T*>(p.act != kActNone ? p.Z : nullptr), p.act,
-        p.T, p.N, sp.rows_per, dZ, part, p.dbias, counters, status,
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(sp.cols, sp.ranges, 1);
+    cfg.blockDim = dim3(kSigThreads, 1, 1);
+    cfg.stream = st;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // as launch_chained
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = 1;
+    at[1].val.clusterDim.y = static_cast<unsigned>(sp.ranges);
+    at[1].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = sp.cluster && sp.ranges > 1 ? 2 : 1;
+    note_launch();
+    const cudaError_t e = cudaLaunchKernelEx(
+        &cfg, signal_kernel<T, kV>, static_cast<const T*>(p.dY),
+        static_cast<const T*>(p.act != kActNone ? p.Z : nullptr), p.act, p.T, p.N, sp.rows_per, dZ, part,
+        p.dbias, sp.cluster ? nullptr : counters, status,
         static_cast<int>(clear_bytes / sizeof(unsigned)));
+    if (e != cudaSuccess) cudaGetLastError();
+    return e;
 }
 
 }  // namespace
@@ -919,7 +962,7 @@ struct VjpLayout {
 };
 VjpLayout vjp_layout(int dtype, int T, int N, int K, int act) {
     VjpLayout l;
-    const SignalPlan sp = signal_plan(dtype, T, N);
+    const SignalPlan sp = signal_plan(dtype, T, N, act);
     l.few = kHead;
     const bool few = dtype == 1 && T <= kFewT;
     l.sig = l.few + (few ? few_counter_bytes(K) : 0);
@@ -927,7 +970,7 @@ VjpLayout vjp_layout(int dtype, int T, int N, int K, int act) {
     size_t off = l.dz;
     if (act != kActNone) off = up256(off + static_cast<size_t>(T) * N * (dtype == 1 ? 2 : 4));
     l.part = off;
-    off = up256(off + static_cast<size_t>(sp.ranges) * N * sizeof(float));
+    if (!sp.cluster) off = up256(off + static_cast<size_t>(sp.ranges) * N * sizeof(float));
     l.scratch = off;
     size_t scratch = 0;
     if (dtype == 1) {
@@ -949,13 +992,13 @@ cudaError_t launch_linear_vjp(int dtype, const LinearVjp& p, void* workspace, cu
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     unsigned* status = reinterpret_cast<unsigned*>(ws);
     const VjpLayout l = vjp_layout(dtype, p.T, p.N, p.K, p.act);
-    const SignalPlan sp = signal_plan(dtype, p.T, p.N);
+    const SignalPlan sp = signal_plan(dtype, p.T, p.N, p.act);
     float* part = reinterpret_cast<float*>(ws + l.part);
     float* scratch = reinterpret_cast<float*>(ws + l.scratch);
     const bool signal = p.act != kActNone || p.dbias;
-    // one range of rows: no counters, and signal_kernel clears what the products need.  That it may
-    // start before the kernel in front of the call has ended is in its own wait's hands
-    const bool clears = signal && sp.ranges == 1;
+    // no counters: signal_kernel clears what the products need.  That it may start before the kernel
+    // in front of the call has ended is in its own wait's hands
+    const bool clears = signal && sp.cluster;
     cudaError_t e = cudaSuccess;
     if (!clears) e = cudaMemsetAsync(ws, 0, l.clear, st);
     if (e != cudaSuccess) return e;

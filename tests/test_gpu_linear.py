@@ -158,6 +158,27 @@ def test_outputs_alone(fpo, dtype, T, k, n):
         assert torch.equal(one[i], whole[i])
 
 
+# one range of rows, a cluster's and, above 2048 (with an activation) and 8192 rows, joined by counters;
+# column groups that end inside; more column groups than blocks are wanted
+@pytest.mark.parametrize("dtype,T,n", [("bf16", 1, 8), ("bf16", 64, 136), ("bf16", 65, 136), ("bf16", 257, 264),
+                                       ("bf16", 513, 20000), ("bf16", 2048, 136), ("bf16", 2049, 1032),
+                                       ("bf16", 8192, 72), ("bf16", 8193, 72), ("f32", 63, 7), ("f32", 129, 260),
+                                       ("f32", 513, 1025), ("f32", 300, 40004), ("f32", 2049, 33), ("f32", 8193, 20)])
+def test_bias_sums(fpo, dtype, T, n):
+    d = inputs(dtype, T, 1 if dtype == "f32" else 8, n)
+    for act in ("none", "silu"):
+        db = torch.full((n + 4,), 7.0, device="cuda")
+        z = d["z"] if act != "none" else None
+        for _ in range(2):
+            ws = fpo.linear_vjp(d["dy"], None, None, None, act=act_of(fpo, act), z=z, dbias=db[:n])
+            assert fpo.get_device_status(ws) == fpo.OK
+            dz = d["dy"].double() * slope64(act, d["z"].double())
+            edz = d["dy"].double().abs() * 2.0 ** -17 if act != "none" else torch.zeros_like(dz)
+            # a thread's rows, the block's 16, the ranges
+            close(db[:n], dz.sum(0), 2.0 ** -24, (T / 16 + 640) * 2.0 ** -24 * dz.abs().sum(0) + edz.sum(0))
+            assert (db[n:] == 7).all()
+
+
 @pytest.mark.parametrize("act,act_in", [("gelu", "silu"), ("silu", "gelu_tanh"), ("gelu_tanh", "gelu")])
 @pytest.mark.parametrize("T,k,n", [(3, 40, 24), (140, 33, 65)])
 def test_gradients_match_differences(fpo, act, act_in, T, k, n):
