@@ -463,8 +463,8 @@ int32_t fpo_linear(int64_t T, int64_t d_out, int64_t d_in, int32_t dtype, int32_
                    void* Z_out, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Bytes of workspace fpo_linear_vjp needs on the current device (0 on invalid arguments): that of
- * the two products, for the bias gradient's parts 4 d_out or (152 SMs) 311 kB, whichever is more, at
- * most, and with an activation T d_out elements. */
+ * the two products, above 8192 rows (2048 with an activation) for the bias gradient's parts 4 d_out or
+ * (152 SMs) 311 kB, whichever is more, at most, and with an activation T d_out elements. */
 size_t fpo_linear_vjp_workspace(int64_t T, int64_t d_out, int64_t d_in, int32_t dtype, int32_t act);
 
 /*
