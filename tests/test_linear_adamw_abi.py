@@ -98,7 +98,8 @@ def test_workspaces_are_what_the_header_says(fpo):
         assert fpo.linear_workspace(T, n, k, fpo.F32) == 256
         for act in (fpo.ACT_NONE, fpo.ACT_SILU):
             v = fpo.linear_vjp_workspace(T, n, k, fpo.BF16, act)
-            assert v - (T * n * 2 if act else 0) >= 256 + 4 * n
+            parts = 4 * n if T > (2048 if act else 8192) else 0  # below that the ranges are a cluster
+            assert v - (T * n * 2 if act else 0) >= 256 + parts
     assert fpo.linear_workspace(0, 64, 64) == 256 and fpo.linear_vjp_workspace(0, 64, 64) == 256
     assert fpo.linear_workspace(4, 12, 64) == 0 and fpo.linear_workspace(-1, 64, 64) == 0
     assert fpo.linear_vjp_workspace(4, 64, 64, 7) == 0 and fpo.linear_vjp_workspace(4, 64, 64, 1, 9) == 0
