@@ -823,9 +823,9 @@ def adamw_grouped(Gs, opt, W_masters, states1, states2, *, scales1=None, scales2
                          [8 if s else 32 for s in small], decays))
     if workspace is None and opt.clip != CLIP_NONE:
         workspace = _workspace(adamw_workspace(sizes, opt.clip), Gs[0].device, stream)
-    rc = _lib.fpo_adamw_grouped(n, ctypes.cast(table, ctypes.POINTER(AdamwTensor)), ctypes.byref(desc), int(seed) & 0xffffffffffffffff,
-                                _ptr(workspace), 0 if workspace is None else _nbytes(workspace),
-                                _stream(stream))
+    rc = _lib.fpo_adamw_grouped(n, ctypes.cast(table, ctypes.POINTER(AdamwTensor)),
+                                ctypes.byref(desc), int(seed) & 0xffffffffffffffff, _ptr(workspace),
+                                0 if workspace is None else _nbytes(workspace), _stream(stream))
     _check(rc, "fpo_adamw_grouped")
     return workspace
 
