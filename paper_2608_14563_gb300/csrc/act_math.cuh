@@ -6,14 +6,19 @@
 //   silu       z s(z)                        s (1 + z (1 - s)),     s the logistic function
 // (0.5 (1 + tanh u) is s(2 u), which keeps its digits where 1 + tanh u cancels.)
 //
-// act_value and act_slope are the fp32 forms.  act_value2 and act_slope2 take two values at a time
-// where the result is rounded to bf16: packed f32x2 arithmetic, the MUFU exponential and
-// reciprocal (some units of 2^-22), and for gelu
+// For gelu both forms take
 //   erfc(x) = exp(-x^2) t Q(t),  t = 1 / (1 + 0.38 x),  x >= 0,
-// Q the polynomial of degree 6 that fits exp(x^2) erfc(x) / t best relative to it (1.1e-6 off over
-// [0, 14], by iterated reweighted least squares; Phi(z) = erfc(|z| / sqrt 2) / 2 or 1 minus it keeps
-// its digits in the tail).  With erfcf the up-projection of 16384 tokens took 1135 us instead of
-// 906 with gelu tanh: the epilogue's instructions cost power and issue slots beside the MMAs.
+// Q the polynomial that fits exp(x^2) erfc(x) / t best relative to it (over [0, 14], in fp32 [0, 10]) by iterated
+// reweighted least squares; Phi(z) = erfc(|z| / sqrt 2) / 2 or 1 minus it keeps its digits in the tail.
+//
+// act_value and act_slope are the fp32 forms: Q of degree 8 (2e-8 off), what z^2 rounds off put back into
+// the exponential, the MUFU reciprocal: Phi within 4e-7, 6e-8 on average.  With erfcf, expf and a
+// division the slope pass over 8192 x 1024 with gelu took 35 us instead of 27, dX of 3906 x 118 x 2602
+// 121 instead of 86.
+// act_value2 and act_slope2 take two values at a time where the result is rounded to bf16: packed
+// f32x2 arithmetic, the MUFU exponential and reciprocal (some units of 2^-22), Q of degree 6 (1.1e-6
+// off).  With erfcf the up-projection of 16384 tokens took 1135 us instead of 906 with gelu tanh: the
+// epilogue's instructions cost power and issue slots beside the MMAs.
 #pragma once
 
 #include <math.h>
@@ -24,8 +29,13 @@ namespace fpo {
 
 enum : int { kActNone = 0, kActRelu = 1, kActGelu = 2, kActGeluTanh = 3, kActSilu = 4 };
 
+__device__ __forceinline__ float rcp_approx(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 __device__ __forceinline__ float logistic(float x) {
-    return 1.f / (1.f + expf(-x));  // x < -88: exp is infinite and the quotient 0
+    return rcp_approx(1.f + expf(-x));  // x < -88: exp is infinite and its reciprocal 0
 }
 
 constexpr float kGeluU = 0.7978845608028654f;   // sqrt(2 / pi)
@@ -33,10 +43,32 @@ constexpr float kGeluC = 0.044715f;
 constexpr float kSqrtHalf = 0.7071067811865476f;
 constexpr float kInvSqrt2Pi = 0.3989422804014327f;
 
+// exp(-z^2 / 2) and Phi(z); beyond 16 the one is 0 and the other 0 or 1 (0 for a NaN).
+__device__ __forceinline__ void normal(float z, float& e, float& cdf) {
+    const float a = fminf(fabsf(z), 16.f), t = rcp_approx(fmaf(a, 0.38f * kSqrtHalf, 1.f));
+    const float h = a * a, rest = fmaf(a, a, -h);
+    e = expf(-0.5f * h);
+    e = fmaf(e, -0.5f * rest, e);
+    float q = fmaf(t, 0.0589897118f, -0.26239594f);
+    q = fmaf(t, q, 0.364107609f);
+    q = fmaf(t, q, -0.161752464f);
+    q = fmaf(t, q, 0.230237057f);
+    q = fmaf(t, q, 0.138554962f);
+    q = fmaf(t, q, 0.203932415f);
+    q = fmaf(t, q, 0.213915459f);
+    q = fmaf(t, q, 0.21441121f);
+    const float tail = 0.5f * t * (q * e);  // Phi(-|z|)
+    cdf = z > 0.f ? 1.f - tail : tail;
+}
+
 template <int kAct>
 __device__ __forceinline__ float act_value(float z) {
     if constexpr (kAct == kActRelu) return z < 0.f ? 0.f : z;  // (NaN stays)
-    if constexpr (kAct == kActGelu) return 0.5f * z * erfcf(-kSqrtHalf * z);
+    if constexpr (kAct == kActGelu) {
+        float e, cdf;
+        normal(z, e, cdf);
+        return z * cdf;
+    }
     if constexpr (kAct == kActGeluTanh)
         return z * logistic(2.f * kGeluU * z * fmaf(kGeluC * z, z, 1.f));
     if constexpr (kAct == kActSilu) return z * logistic(z);
@@ -46,8 +78,11 @@ __device__ __forceinline__ float act_value(float z) {
 template <int kAct>
 __device__ __forceinline__ float act_slope(float z) {
     if constexpr (kAct == kActRelu) return z > 0.f ? 1.f : 0.f;
-    if constexpr (kAct == kActGelu)
-        return fmaf(z, kInvSqrt2Pi * expf(-0.5f * z * z), 0.5f * erfcf(-kSqrtHalf * z));
+    if constexpr (kAct == kActGelu) {
+        float e, cdf;
+        normal(z, e, cdf);
+        return fmaf(z, kInvSqrt2Pi * e, cdf);
+    }
     if constexpr (kAct == kActGeluTanh) {
         // beyond 12 the slope is 0 or 1 to fp32, and z^2 could overflow against s (1 - s) = 0
         if (fabsf(z) > 12.f) return z > 0.f ? 1.f : 0.f;
@@ -67,11 +102,6 @@ __device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) { return __ffma2_rn(a, b, c); }
 __device__ __forceinline__ float2 mul2(float2 a, float2 b) { return __fmul2_rn(a, b); }
 __device__ __forceinline__ float2 add2(float2 a, float2 b) { return __fadd2_rn(a, b); }
-__device__ __forceinline__ float rcp_approx(float x) {
-    float y;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 __device__ __forceinline__ float exp2_approx(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

@@ -172,8 +172,8 @@ struct SliceLoader {
 
 // SEpiSlope over a thread's rows row0 + 64 g + 0..3 and columns col0 + 64 h + 0..3 (g, h < kH; with a
 // split those of its block's rank).  What four rows read is loaded before the first of them is used,
-// and the activation is chosen once: row by row, where every load and branch waits for itself, 8903 x
-// 23 x 1370 with gelu's slope took 80 us, so 60 (34 without); 3906 x 118 x 2602 125 and 121.  The
+// and the activation is chosen once: 8903 x 23 x 1370 with gelu's slope 48 us, two rows at a time 49, one
+// 51 (33 without an activation); row by row, where every branch waited for itself too, 20 more.  The
 // forward epilogue gains nothing by it and its products lose 2% to the registers.
 template <int kH>
 __device__ __forceinline__ void slope_rows(const SimtOps& ops, const SEpiSlope& ep,
