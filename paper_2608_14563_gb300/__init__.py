@@ -824,7 +824,8 @@ def adamw_grouped(Gs, opt, W_masters, states1, states2, *, scales1=None, scales2
     if workspace is None and opt.clip != CLIP_NONE:
         workspace = _workspace(adamw_workspace(sizes, opt.clip), Gs[0].device, stream)
     rc = _lib.fpo_adamw_grouped(n, ctypes.cast(table, ctypes.POINTER(AdamwTensor)),
-                                ctypes.byref(desc), int(seed) & 0xffffffffffffffff, _ptr(workspace),
+                                ctypes.byref(desc), int(seed) & 0xffffffffffffffff,
+                                _at(Gs[0].get_device(), workspace),
                                 0 if workspace is None else _nbytes(workspace), _stream(stream))
     _check(rc, "fpo_adamw_grouped")
     return workspace
