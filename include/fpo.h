@@ -481,7 +481,8 @@ size_t fpo_linear_vjp_workspace(int64_t T, int64_t d_out, int64_t d_in, int32_t 
  * dY, Z [T, d_out], X, Z_in [T, d_in], W [d_out, d_in] in dtype; Z is read for act, Z_in for act_in
  * (and dX), X for dW, W for dX, and may be NULL otherwise
  * dX [T, d_in], dW [d_out, d_in] in dtype, dbias [d_out] fp32: each may be NULL, not all three
- * workspace  fpo_linear_vjp_workspace() bytes, 256-byte aligned (device status word first)
+ * workspace  fpo_linear_vjp_workspace() bytes, 256-byte aligned (device status word first); without
+ *          dX or dW less will do, for dbias alone as many as for a layer of any d_in
  * Outputs may not overlap what is read, one another or the workspace (FPO_ERR_ARG).  fp32
  * accumulation; dbias adds dZ before its rounding to dtype, in a fixed order; the products take it
  * rounded.  Deterministic.  T = 0 sets dW and dbias to zero.  After a wait that ran out

@@ -866,7 +866,7 @@ int32_t fpo_linear(int64_t T, int64_t d_out, int64_t d_in, int32_t dtype, int32_
 size_t fpo_linear_vjp_workspace(int64_t T, int64_t d_out, int64_t d_in, int32_t dtype, int32_t act) {
     if (linear_check(T, d_out, d_in, dtype) != FPO_OK || !act_ok(act)) return 0;
     return linear_vjp_workspace_bytes(dtype, static_cast<int>(T), static_cast<int>(d_out),
-                                      static_cast<int>(d_in), act);
+                                      static_cast<int>(d_in), act, true, true);
 }
 
 int32_t fpo_linear_vjp(int64_t T, int64_t d_out, int64_t d_in, int32_t dtype, int32_t act,
@@ -883,7 +883,9 @@ int32_t fpo_linear_vjp(int64_t T, int64_t d_out, int64_t d_in, int32_t dtype, in
     if (!aligned16(dY) || !aligned16(Z) || !aligned16(X) || !aligned16(W) || !aligned16(Z_in) ||
         !aligned16(dX) || !aligned16(dW) || !aligned16(dbias))
         return FPO_ERR_ALIGN;
-    if (!workspace || workspace_bytes < fpo_linear_vjp_workspace(T, d_out, d_in, dtype, act))
+    if (!workspace || workspace_bytes < linear_vjp_workspace_bytes(
+                          dtype, static_cast<int>(T), static_cast<int>(d_out), static_cast<int>(d_in),
+                          act, dX != nullptr, dW != nullptr))
         return FPO_ERR_WORKSPACE;
     if ((reinterpret_cast<uintptr_t>(workspace) % kAlign) != 0) return FPO_ERR_ALIGN;
     const size_t e = dtype == FPO_BF16 ? 2 : 4, t = static_cast<size_t>(T),

@@ -265,7 +265,8 @@ struct LinearVjp {
     float* dbias;
 };
 size_t linear_workspace_bytes(int dtype, int T, int N, int K);
-size_t linear_vjp_workspace_bytes(int dtype, int T, int N, int K, int act);
+// Of a call with dX (dx) and dW (dw) among its outputs.
+size_t linear_vjp_workspace_bytes(int dtype, int T, int N, int K, int act, bool dx, bool dw);
 // Bytes at the workspace's start that are zero before a call (0: the status word is written by the
 // call's kernel).
 size_t linear_clear_bytes(int dtype, int T, int N, int K);

@@ -956,16 +956,17 @@ cudaError_t launch_linear(int dtype, const LinearFwd& p, void* workspace, cudaSt
 namespace {
 
 // The backward pass's workspace: status word, counters of few_tokens_kernel and of signal_kernel,
-// dZ (with an activation), the bias ranges' sums, scratch of the products' parts.
+// dZ (with an activation), the bias ranges' sums, scratch of the products' parts; dx, dw: whether those
+// products run (the bias gradient's share does not depend on K).
 struct VjpLayout {
     size_t few, sig, clear, dz, part, scratch, total;
 };
-VjpLayout vjp_layout(int dtype, int T, int N, int K, int act) {
+VjpLayout vjp_layout(int dtype, int T, int N, int K, int act, bool dx, bool dw) {
     VjpLayout l;
     const SignalPlan sp = signal_plan(dtype, T, N, act);
     l.few = kHead;
     const bool few = dtype == 1 && T <= kFewT;
-    l.sig = l.few + (few ? few_counter_bytes(K) : 0);
+    l.sig = l.few + (few && dx ? few_counter_bytes(K) : 0);
     l.clear = l.dz = l.sig + signal_counter_bytes(sp);
     size_t off = l.dz;
     if (act != kActNone) off = up256(off + static_cast<size_t>(T) * N * (dtype == 1 ? 2 : 4));
@@ -973,10 +974,10 @@ VjpLayout vjp_layout(int dtype, int T, int N, int K, int act) {
     if (!sp.cluster) off = up256(off + static_cast<size_t>(sp.ranges) * N * sizeof(float));
     l.scratch = off;
     size_t scratch = 0;
-    if (dtype == 1) {
-        scratch = pair_scratch_bytes(N, K, T);
-        const size_t dx = few ? few_scratch_bytes(K, N, T) : pair_scratch_bytes(T, K, N);
-        scratch = dx > scratch ? dx : scratch;
+    if (dtype == 1 && dw) scratch = pair_scratch_bytes(N, K, T);
+    if (dtype == 1 && dx) {
+        const size_t parts = few ? few_scratch_bytes(K, N, T) : pair_scratch_bytes(T, K, N);
+        scratch = parts > scratch ? parts : scratch;
     }
     l.total = off + scratch;
     return l;
@@ -984,14 +985,14 @@ VjpLayout vjp_layout(int dtype, int T, int N, int K, int act) {
 
 }  // namespace
 
-size_t linear_vjp_workspace_bytes(int dtype, int T, int N, int K, int act) {
-    return T == 0 ? kHead : vjp_layout(dtype, T, N, K, act).total;
+size_t linear_vjp_workspace_bytes(int dtype, int T, int N, int K, int act, bool dx, bool dw) {
+    return T == 0 ? kHead : vjp_layout(dtype, T, N, K, act, dx, dw).total;
 }
 
 cudaError_t launch_linear_vjp(int dtype, const LinearVjp& p, void* workspace, cudaStream_t st) {
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     unsigned* status = reinterpret_cast<unsigned*>(ws);
-    const VjpLayout l = vjp_layout(dtype, p.T, p.N, p.K, p.act);
+    const VjpLayout l = vjp_layout(dtype, p.T, p.N, p.K, p.act, p.dX != nullptr, p.dW != nullptr);
     const SignalPlan sp = signal_plan(dtype, p.T, p.N, p.act);
     float* part = reinterpret_cast<float*>(ws + l.part);
     float* scratch = reinterpret_cast<float*>(ws + l.scratch);
