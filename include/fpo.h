@@ -540,7 +540,8 @@ size_t fpo_adamw_workspace(int32_t n_tensors, const int64_t* n, int32_t clip);
  * in fp32 with the rates rounded to fp32; the moments' products and sums are rounded one by one, as
  * written from left to right, so that the codes of 8-bit moments are those of any fp32 arithmetic.
  * The clip is that of App. A per tensor: s = min(1, clip_frac ||W|| / ||step||), or G scaled so
- * before the moments see it (a tensor of zeros does not move under it).
+ * before the moments see it (a tensor of zeros does not move under it).  The norms are those of any
+ * fp32 numbers, to 2^-20, also where their squares leave fp32's range; s is held in fp32.
  *
  * tensors  HOST array; W_master, W_out, the states and the scales may not overlap one another, a G
  *          or the workspace (FPO_ERR_ARG), but for an fp32 W_out that is W_master; G may repeat

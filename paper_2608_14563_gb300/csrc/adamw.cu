@@ -29,9 +29,10 @@
 // A block with a NaN or an infinity among its new m (v) gets a NaN scale: NaN throughout.
 //
 // Bound: HBM.  90M elements, no clip, step clip, gradient clip: fp32 moments 361 us (7.0 TB/s of the 28
-// bytes an element), 518 (two passes' 516 at the copy rate), 470; 8-bit moments 238 (6.1 TB/s of 16;
-// the rounding's hash and the scales' maxima take issue slots), 405, 360 (the norms pass computes the
-// step a second time, for keeping it would cost more bytes than the moments).
+// bytes an element), 515 (two passes' 516 at the copy rate), 470; 8-bit moments 237 (6.1 TB/s of 16;
+// the rounding's hash and the scales' maxima take issue slots), 390, 342 (the norms pass computes the
+// step a second time, for keeping it would cost more bytes than the moments).  Squares outside fp32's
+// range are added a second time, scaled: gradients of zeros, which look like such, take 477 for 468.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -284,6 +285,57 @@ __device__ __forceinline__ void adamw_step(const AdamRates& op, float wd, float 
     }
 }
 
+__device__ __forceinline__ float warp_sum(float x) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+    return x;
+}
+
+// Sums of squares as 32-bit words.  In [2^-100, 2^90] (a launch's 2^31 chunks then stay in range, and
+// what squares lose under fp32's numbers is below 2^-40 of the sum), 0, an infinity or a NaN: the fp32
+// number.  Else, marked by the sign bit, the upper half of a double, rounded: 2^-21 of the sum.
+__device__ __forceinline__ float wide_word(double x) {
+    const long long b = __double_as_longlong(x) + 0x80000000ll;
+    return __uint_as_float(static_cast<uint32_t>(b >> 32) | 0x80000000u);
+}
+__device__ __forceinline__ bool is_wide(float word) { return __float_as_int(word) < 0; }
+__device__ __forceinline__ double wide_value(float word) {
+    return __hiloint2double(__float_as_int(word) & 0x7fffffff, 0);
+}
+
+__device__ __forceinline__ bool in_range(float s) { return s >= 0x1p-100f && s <= 0x1p90f; }
+
+// The word of a warp's values whose sum of squares s is not in range: magnitudes below 2^-50, or some
+// from 2^40 up to 2^128, are squared where fp32 has their squares.
+template <int kPer>
+__device__ __forceinline__ float far_square_sum(float s, const float (&x)[kPer]) {
+    const bool low = s < 0x1p-100f;
+    const float f = low ? 0x1p100f : 0x1p-70f;
+    float t = 0.f;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) t = fmaf(x[k] * f, x[k] * f, t);
+    t = warp_sum(t);
+    if (t == 0.f || !(t < __int_as_float(0x7f800000))) return fabsf(t);
+    return wide_word(static_cast<double>(t) * (low ? 0x1p-200 : 0x1p140));
+}
+
+// The words of a warp's weights and of its gradients or steps, the same in every lane.
+template <int kPer>
+__device__ __forceinline__ void square_sums(const float (&w)[kPer], const float (&x)[kPer], float& ww,
+                                            float& xx) {
+    ww = xx = 0.f;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+        ww = fmaf(w[k], w[k], ww);
+        xx = fmaf(x[k], x[k], xx);
+    }
+    ww = warp_sum(ww);
+    xx = warp_sum(xx);
+    if (in_range(ww) && in_range(xx)) return;
+    if (!in_range(ww)) ww = far_square_sum(ww, w);
+    if (!in_range(xx)) xx = far_square_sum(xx, x);
+}
+
 // One tensor's entry of the table.
 struct Entry {
     const void* g;
@@ -306,7 +358,7 @@ struct Entry {
 enum Pass { kStep, kNorms, kMoments, kApply };
 
 // What a pass does with a warp's elements from i0.  kFull: all of them are there; else the first at
-// least is.
+// least is.  ww, xx: the words of a pass with sums.
 template <Pass kPass, bool kState8, bool kFull>
 __device__ __forceinline__ void take(const AdamRates& op, const Entry& e, long long i0, float gscale,
                                      float sscale, float& ww, float& xx) {
@@ -328,11 +380,7 @@ __device__ __forceinline__ void take(const AdamRates& op, const Entry& e, long l
 #pragma unroll
     for (int q = 0; q < kQuads; ++q) load4<kFull>(e.w, i1 + 128 * q, n, w + 4 * q);
     if (kPass == kNorms && op.clip == 2) {  // the gradient's norm needs no state
-#pragma unroll
-        for (int k = 0; k < kPer; ++k) {
-            ww = fmaf(w[k], w[k], ww);
-            xx = fmaf(g[k], g[k], xx);
-        }
+        square_sums(w, g, ww, xx);
         return;
     }
     const long long block = i0 / kAdamBlock;
@@ -366,14 +414,13 @@ __device__ __forceinline__ void take(const AdamRates& op, const Entry& e, long l
         }
     };
     if constexpr (kPass == kNorms || kPass == kMoments) {
+        if constexpr (!kFull) {
 #pragma unroll
-        for (int k = 0; k < kPer; ++k) {
-            // (no element: eps 0 would divide by 0)
-            if (!kFull && i1 + 128 * (k / 4) + k % 4 >= n) d[k] = 0.f;
-            ww = fmaf(w[k], w[k], ww);
-            xx = fmaf(d[k], d[k], xx);
+            for (int k = 0; k < kPer; ++k)  // (no element: eps 0 would divide by 0)
+                if (i1 + 128 * (k / 4) + k % 4 >= n) d[k] = 0.f;
         }
         if constexpr (kPass == kMoments) store_moments();
+        square_sums(w, d, ww, xx);
         return;
     }
 #pragma unroll
@@ -415,15 +462,25 @@ __device__ __forceinline__ void take(const AdamRates& op, const Entry& e, long l
     }
 }
 
-__device__ __forceinline__ float warp_sum(float x) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-    return x;
+// The word of the block's, from its warps' in order.
+__device__ __forceinline__ float add_words(const float* words) {
+    float s = words[0];
+    bool wide = is_wide(s);
+    for (int i = 1; i < kThreads / 32; ++i) {
+        s += words[i];
+        wide |= is_wide(words[i]);
+    }
+    if (!wide) return s;
+    double d = 0.0;
+    for (int i = 0; i < kThreads / 32; ++i)
+        d += is_wide(words[i]) ? wide_value(words[i]) : static_cast<double>(words[i]);
+    if (d < 0x1p-100 || (d > 0x1p90 && isfinite(d))) return wide_word(d);
+    return fabsf(static_cast<float>(d));
 }
 
 constexpr bool sums(Pass p) { return p == kNorms || p == kMoments; }
 
-// Passes with sums: part[chunk] = the chunk's two.  Else scales[tensor] (null: 1) clips the step.
+// Passes with sums: part[chunk] = the words of the chunk's two.  Else scales[tensor] (null: 1) clips the step.
 template <int CAP, Pass kPass, bool kState8>
 __global__ void __launch_bounds__(kThreads, kPass == kNorms ? (kState8 ? 5 : 3) : (kState8 ? 4 : 2))
     adamw_kernel(const __grid_constant__ Table<CAP> t, const __grid_constant__ AdamRates op,
@@ -452,36 +509,38 @@ __global__ void __launch_bounds__(kThreads, kPass == kNorms ? (kState8 ? 5 : 3) 
     else if (i0 < e.n)
         take<kPass, kState8, false>(op, e, i0, gscale, sscale, ww, xx);
     if constexpr (sums(kPass)) {
-        __shared__ float2 sh[kThreads / 32];
-        ww = warp_sum(ww);
-        xx = warp_sum(xx);
-        if ((threadIdx.x & 31) == 0) sh[warp] = make_float2(ww, xx);
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            float2 s = sh[0];
-            for (int i = 1; i < kThreads / 32; ++i) {
-                s.x += sh[i].x;
-                s.y += sh[i].y;
-            }
-            part[c] = s;
+        __shared__ float sh[2][kThreads / 32];
+        if ((threadIdx.x & 31) == 0) {
+            sh[0][warp] = ww;
+            sh[1][warp] = xx;
         }
+        __syncthreads();
+        if (warp < 2 && (threadIdx.x & 31) == 0) reinterpret_cast<float*>(part + c)[warp] = add_words(sh[warp]);
     }
 }
 
-// A sum of fp32 numbers and what its additions rounded off (Knuth's two-sum), 48 bits in all.
+// A sum of words: of the fp32 numbers with what the additions rounded off (Knuth's two-sum), 48 bits in
+// all, and of the wide ones in fp64.
 struct TwoSum {
     float hi = 0.f, lo = 0.f;
+    double wide = 0.0;
     __device__ __forceinline__ void add(float x) {
         const float s = __fadd_rn(hi, x), b = __fsub_rn(s, hi);
         lo = __fadd_rn(lo, __fadd_rn(__fsub_rn(hi, __fsub_rn(s, b)), __fsub_rn(x, b)));
         hi = s;
     }
+    __device__ __forceinline__ void add_word(float x) {
+        if (is_wide(x))
+            wide += wide_value(x);
+        else
+            add(x);
+    }
     __device__ __forceinline__ double value() const {
-        return isfinite(hi) ? static_cast<double>(hi) + lo : static_cast<double>(hi);
+        return isfinite(hi) ? static_cast<double>(hi) + lo + wide : static_cast<double>(hi);
     }
 };
 
-// scales[k] = min(1, clip_frac ||W|| / ||x||) from the tensor's chunk sums: thread-strided, a fixed
+// scales[k] = min(1, clip_frac ||W|| / ||x||) from the tensor's chunk sums (words): thread-strided, a fixed
 // butterfly, then the warps in order.  One block per tensor, whose few fp64 adders would take 10 us
 // for the 22,000 chunks of 45M elements (20 to 33 us with loads one by one); the threads add pairs
 // of fp32 numbers instead, eight loads ahead.
@@ -498,10 +557,20 @@ __global__ void __launch_bounds__(kScaleThreads)
 #pragma unroll
         for (int i = 0; i < kScaleAhead; ++i)
             p[i] = c + i * kScaleThreads < end ? part[c + i * kScaleThreads] : make_float2(0.f, 0.f);
+        int wide = 0;  // (one branch for all of them)
 #pragma unroll
-        for (int i = 0; i < kScaleAhead; ++i) {
-            w.add(p[i].x);
-            x.add(p[i].y);
+        for (int i = 0; i < kScaleAhead; ++i) wide |= __float_as_int(p[i].x) | __float_as_int(p[i].y);
+        if (wide >= 0) {
+#pragma unroll
+            for (int i = 0; i < kScaleAhead; ++i) {
+                w.add(p[i].x);
+                x.add(p[i].y);
+            }
+        } else {
+            for (int i = 0; i < kScaleAhead; ++i) {
+                w.add_word(p[i].x);
+                x.add_word(p[i].y);
+            }
         }
     }
     double ww = w.value(), xx = x.value();
