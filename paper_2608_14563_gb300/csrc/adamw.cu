@@ -658,26 +658,21 @@ cudaError_t run_adamw(const int* ids, int count, const AdamTensor* ts, const Ada
     t.first[count] = static_cast<int>(total);
     if (total == 0) return cudaSuccess;
     const unsigned grid = static_cast<unsigned>(total);
-    if (op.clip == 0) {
-        adamw_kernel<CAP, kStep, kState8><<<grid, kThreads, 0, st>>>(t, op, nullptr, nullptr),
-            note_launch();
-        return cudaGetLastError();
-    }
+    float2* const no_part = nullptr;
+    const float* const no_scales = nullptr;
+    if (op.clip == 0)
+        return launch_plain(adamw_kernel<CAP, kStep, kState8>, grid, kThreads, st, t, op, no_part, no_scales);
     constexpr Pass kFirst = kState8 ? kNorms : kMoments, kLast = kState8 ? kStep : kApply;
-    if (op.clip == 1)
-        adamw_kernel<CAP, kFirst, kState8><<<grid, kThreads, 0, st>>>(t, op, part, nullptr), note_launch();
-    else
-        adamw_kernel<CAP, kNorms, kState8><<<grid, kThreads, 0, st>>>(t, op, part, nullptr), note_launch();
-    cudaError_t e = cudaGetLastError();
+    cudaError_t e = op.clip == 1
+        ? launch_plain(adamw_kernel<CAP, kFirst, kState8>, grid, kThreads, st, t, op, part, no_scales)
+        : launch_plain(adamw_kernel<CAP, kNorms, kState8>, grid, kThreads, st, t, op, part, no_scales);
     if (e != cudaSuccess) return e;
-    adamw_scale_kernel<CAP><<<count, kScaleThreads, 0, st>>>(t, part, op.clip_frac, scales), note_launch();
-    e = cudaGetLastError();
+    e = launch_plain(adamw_scale_kernel<CAP>, static_cast<unsigned>(count), kScaleThreads, st, t, part,
+                     op.clip_frac, scales);
     if (e != cudaSuccess) return e;
-    if (op.clip == 1)
-        adamw_kernel<CAP, kLast, kState8><<<grid, kThreads, 0, st>>>(t, op, nullptr, scales), note_launch();
-    else
-        adamw_kernel<CAP, kStep, kState8><<<grid, kThreads, 0, st>>>(t, op, nullptr, scales), note_launch();
-    return cudaGetLastError();
+    return op.clip == 1
+        ? launch_plain(adamw_kernel<CAP, kLast, kState8>, grid, kThreads, st, t, op, no_part, scales)
+        : launch_plain(adamw_kernel<CAP, kStep, kState8>, grid, kThreads, st, t, op, no_part, scales);
 }
 
 // Tensors of one launch: the table of a few is a tenth of the parameters of many.
@@ -724,19 +719,12 @@ cudaError_t launch_state_values(bool is_signed, long long n, const void* codes, 
     if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
     const unsigned grid = static_cast<unsigned>(blocks);
     const uint8_t* c = static_cast<const uint8_t*>(codes);
-    if (is_signed) {
-        if (out_dtype == 1)
-            state_values_kernel<true><<<grid, kThreads, 0, st>>>(c, scales, n, static_cast<__nv_bfloat16*>(out));
-        else
-            state_values_kernel<true><<<grid, kThreads, 0, st>>>(c, scales, n, static_cast<float*>(out));
-    } else {
-        if (out_dtype == 1)
-            state_values_kernel<false><<<grid, kThreads, 0, st>>>(c, scales, n, static_cast<__nv_bfloat16*>(out));
-        else
-            state_values_kernel<false><<<grid, kThreads, 0, st>>>(c, scales, n, static_cast<float*>(out));
-    }
-    note_launch();
-    return cudaGetLastError();
+    auto run = [&](auto kern, auto* to) { return launch_plain(kern, grid, kThreads, st, c, scales, n, to); };
+    __nv_bfloat16* const h = static_cast<__nv_bfloat16*>(out);
+    float* const f = static_cast<float*>(out);
+    if (is_signed)
+        return out_dtype == 1 ? run(state_values_kernel<true, __nv_bfloat16>, h) : run(state_values_kernel<true, float>, f);
+    return out_dtype == 1 ? run(state_values_kernel<false, __nv_bfloat16>, h) : run(state_values_kernel<false, float>, f);
 }
 
 }  // namespace fpo

@@ -214,11 +214,12 @@ int proj_clusters() {
     using L = GemmPairSmem<kWideBN, kWideStages, pair_ksub<kWideBN, false, true>()>;
     constexpr auto kern = tc_gemm_pair_kernel<kWideBN, false, true, kWideStages, 1, EpiProjVjp>;
     DevInfo di;
-    int c = 128;
-    if (current_device_info(&di) && set_smem_limit<kern>(L::kBytes) == cudaSuccess)
-        c = resident_clusters<kern>(gemm_threads<EpiProjVjp>(), L::kBytes, di.sm_count, 2);
-    cudaGetLastError();
-    return c;
+    if (current_device_info(&di)) {
+        if (set_smem_limit<kern>(L::kBytes) == cudaSuccess)
+            return resident_clusters<kern>(gemm_threads<EpiProjVjp>(), L::kBytes, di.sm_count, 2);
+        cudaGetLastError();  // its own (one that the caller left pending stays)
+    }
+    return 128;
 }
 
 // K ranges per tile of the projection of a batch of T tokens, or 0: batches with at least

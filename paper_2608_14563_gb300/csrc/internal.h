@@ -7,6 +7,7 @@
 #include <stdint.h>
 
 #include <atomic>
+#include <utility>
 
 namespace fpo {
 
@@ -85,6 +86,20 @@ cudaError_t launch_chained(void (*kern)(P...), dim3 grid, unsigned threads, size
     cfg.numAttrs = 1;
     note_launch();
     const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, static_cast<P>(args)...);
+    if (e != cudaSuccess) cudaGetLastError();
+    return e;
+}
+
+// Launches a kernel behind everything in the stream.  What is returned (and cleared) is this launch's
+// error: one that the caller left pending is neither.
+template <class... P, class... A>
+cudaError_t launch_plain(void (*kern)(P...), unsigned grid, unsigned threads, cudaStream_t st, A&&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid, 1, 1);
+    cfg.blockDim = dim3(threads, 1, 1);
+    cfg.stream = st;
+    note_launch();
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, std::forward<A>(args)...);
     if (e != cudaSuccess) cudaGetLastError();
     return e;
 }

@@ -547,10 +547,9 @@ template <typename T, int kV, int kT>
 cudaError_t run_rows_t(const LinearFwd& p, unsigned* status, cudaStream_t st) {
     const RowOut<T> out{static_cast<const T*>(p.bias), static_cast<const T*>(p.residual),
                         static_cast<T*>(p.Y), static_cast<T*>(p.Z), p.act};
-    row_kernel<T, kV, kT><<<(p.N + kRowWarps - 1) / kRowWarps, 32 * kRowWarps, 0, st>>>(
-        static_cast<const T*>(p.X), static_cast<const T*>(p.W), p.T, p.N, p.K, out, status),
-        note_launch();
-    return cudaGetLastError();
+    return launch_plain(row_kernel<T, kV, kT>, static_cast<unsigned>((p.N + kRowWarps - 1) / kRowWarps),
+                        32 * kRowWarps, st, static_cast<const T*>(p.X), static_cast<const T*>(p.W), p.T, p.N,
+                        p.K, out, status);
 }
 template <typename T, int kV>
 cudaError_t run_rows_v(const LinearFwd& p, unsigned* status, cudaStream_t st) {
@@ -575,11 +574,12 @@ int linear_clusters() {
     using L = GemmPairSmem<256, kPairStages, pair_ksub<256, false, false>()>;
     constexpr auto kern = tc_gemm_pair_kernel<256, false, false, kPairStages, 1, EpiLinear<256, kActNone>>;
     DevInfo di;
-    int c = 76;
-    if (current_device_info(&di) && set_smem_limit<kern>(L::kBytes) == cudaSuccess)
-        c = resident_clusters<kern>(gemm_threads<EpiLinear<256, kActNone>>(), L::kBytes, di.sm_count, 2);
-    cudaGetLastError();
-    return c;
+    if (current_device_info(&di)) {
+        if (set_smem_limit<kern>(L::kBytes) == cudaSuccess)
+            return resident_clusters<kern>(gemm_threads<EpiLinear<256, kActNone>>(), L::kBytes, di.sm_count, 2);
+        cudaGetLastError();  // its own (one that the caller left pending stays)
+    }
+    return 76;
 }
 
 // How a product runs: on one CTA's tiles of 128 rows by `single` columns, on pair tiles of 128
