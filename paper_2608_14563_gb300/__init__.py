@@ -665,8 +665,9 @@ def layernorm_vjp(g, x, gamma, g_out, *, eps=1e-5, min_rms=0.5, dgamma=None, dbe
 
 
 def _entry(fn):
-    """An entry point all of whose tensors, not the leading one alone, are looked at for their device
-    (_at): an object that calls fn, without a call of its own in between."""
+    """Marks an entry point all of whose tensors, not the leading one alone, are looked at for their
+    device (_at).  It becomes a callable object with fn's name, documentation and signature, which
+    inspect.isfunction does not find: who lists entry points looks for callables."""
     kind = type("entry", (), {"__call__": staticmethod(fn), "__doc__": fn.__doc__})
     return functools.update_wrapper(kind(), fn)
 
