@@ -12,7 +12,8 @@
 // reweighted least squares; Phi(z) = erfc(|z| / sqrt 2) / 2 or 1 minus it keeps its digits in the tail.
 //
 // act_value and act_slope are the fp32 forms: Q of degree 8 (2e-8 off), what z^2 rounds off put back into
-// the exponential, the MUFU reciprocal: Phi within 4e-7, 6e-8 on average.  With erfcf, expf and a
+// the exponential, the MUFU reciprocal: z Phi within 4.8e-7 of its value over 440,000 z, 4e-8 on
+// average; gelu's slope within 2.2e-7, silu's within 1e-6, gelu tanh's within 2e-6.  With erfcf, expf and a
 // division the slope pass over 8192 x 1024 with gelu took 35 us instead of 27, dX of 3906 x 118 x 2602
 // 121 instead of 86.
 // act_value2 and act_slope2 take two values at a time where the result is rounded to bf16: packed
