@@ -408,6 +408,8 @@ size_t fpo_layer_optimize_workspace(int32_t n_layers, int64_t d, int64_t d_ff);
  * holds n_layers x d x d_ff x 4 bytes: G_l, or with bf16 and FPO_CLIP_STEP the
  * unclipped steps, which the GEMM's epilogue forms from G_l (and the state) without
  * storing G_l.  g, A, W_out: as fpo_layer_update_grouped_signals.
+ * The clip's norms add squares in fp32: magnitudes below 4e-23 count as 0 in them, and a partial
+ * sum above 3.4e38 makes them infinite.
  */
 int32_t fpo_layer_optimize_grouped(int32_t n_layers, int64_t T, int64_t d, int64_t d_ff,
                                    int32_t dtype, const void* const* g, const void* const* A,
@@ -485,7 +487,8 @@ size_t fpo_linear_vjp_workspace(int64_t T, int64_t d_out, int64_t d_in, int32_t 
  *          dX or dW less will do, for dbias alone as many as for a layer of any d_in
  * Outputs may not overlap what is read, one another or the workspace (FPO_ERR_ARG).  fp32
  * accumulation; dbias adds dZ before its rounding to dtype, in a fixed order; the products take it
- * rounded.  Deterministic.  T = 0 sets dW and dbias to zero.  After a wait that ran out
+ * rounded: in bf16 and with an act, dX and dW have some sqrt(2) times the error of their own
+ * rounding (2.35e-3 for 1.66e-3 of their norm).  Deterministic.  T = 0 sets dW and dbias to zero.  After a wait that ran out
  * (FPO_ERR_TIMEOUT) dX and dW hold no result.
  */
 int32_t fpo_linear_vjp(int64_t T, int64_t d_out, int64_t d_in, int32_t dtype, int32_t act,
@@ -516,7 +519,7 @@ typedef struct fpo_adamw_tensor {
 } fpo_adamw_tensor;
 
 /* Rates of fpo_adamw_grouped, in double: 1 - beta2 and the bias corrections keep their digits (in
- * float, 1 - 0.999 is 1.3e-5 off). */
+ * float, 1 - 0.999 is 1.3e-5 off, by which fpo_layer_optimize_grouped's second moments differ). */
 typedef struct fpo_adamw_desc {
     double lr;
     double beta1, beta2;   /* moment decays in [0, 1) (0.9, 0.999)              */

@@ -37,9 +37,9 @@ size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 //   warp 0      TMA producer: a k-step, two 64-deep k-blocks, of weights and tokens per stage
 //   warp 1      TMEM, MMAs (128 x BT x 16)
 //   warps 2..5  epilogue: one feature per lane
-// Bound: the weights' bytes, with a fixed part of some 8 us; under that the thread that issues the
-// MMAs, whose k-blocks with a commit each took some 540 cycles however few columns they had, so
-// that tiles which have an SM each are no faster for being narrow.  us on pair tiles and here, from
+// Bound: the weights' bytes, with a fixed part of some 8 us; under that a CTA's own pace, some 540
+// cycles for a k-block with a commit of its own however few columns it had, so that tiles which
+// have an SM each are no faster for being narrow.  us on pair tiles and here, from
 // memory, K 4096 to 11008 features and 11008 to 4096: 5 tokens 41.7 26.8, 38.4 25.2; 16 tokens 38.3
 // 28.3, 34.9 25.8; 32 tokens 38.6 30.6, 35.2 27.9.  With 64 tokens 38.8 37.4, 36.6 32.8, but 1024 to
 // 1024 features 15.3 16.4; with more the sums of the parts, one warp per 32 features, are slower
@@ -595,8 +595,10 @@ struct PairPlan {
 
 // The cheapest by what was measured, in ns.  A 64-deep k-block of a 256 x 256 pair tile takes 325,
 // where one wave has all tiles: pair tiles of 128 columns 300, one CTA's of 128 columns 355 and of 64
-// columns 290 (the issuing thread, not the arithmetic, sets their pace), and a launch and its
-// epilogue 9000 on pairs and 6000 on single CTAs, which have no partner to wait for.  Split tiles
+// columns 290, and a launch and its epilogue 9000 on pairs and 6000 on single CTAs, which have no
+// partner to wait for.  (From L2 a single CTA's pace is its own, and not that of something the CTAs
+// share: with 2, 8, 18, 38 and 76 CTAs a k-block of 64 columns took 291, 299, 288, 288 and 280 ns, one
+// of 128 columns 256 to 258 with each; all 152 took 261 and, their operands beyond L2, 305.)  Split tiles
 // add the store of the parts of a wave of units (2500), the fixup's launch (5000) and its read of a
 // unit (100).
 //   T x K x N, us: 200 x 256 x 384 12.3 on pairs, 8.3 on 64-column CTAs; 128 x 1024 x 1024 16.4,
@@ -867,8 +869,8 @@ struct SignalPlan {
     bool cluster;  // the ranges are a cluster's blocks (or one)
 };
 int sig_v(int dtype, int N) { return dtype == 1 ? 8 : N % 4 == 0 ? 4 : 1; }
-// Up to 2048 rows, or 8192 without an activation to compute, the ranges are a cluster's blocks, of 64 or
-// 256 rows at least: no counters to clear and wait for.  us with 256 rows and counters, and so (fp32
+// Up to 2048 rows, or 8192 without an activation to compute, the ranges are a cluster's blocks, one for
+// every 64 or 256 rows begun and at most eight: no counters to clear and wait for.  us with 256 rows and counters, and so (fp32
 // with a slower gelu than now's, 4.5): 512 x 1024 fp32 gelu 18.5 and 5.9, bias sums alone 8.3 and 3.1;
 // 2048 x 256 bf16 gelu 14.5 and 8.9, alone 8.6 and 3.2; 200 x 256 bf16 gelu (one range) 6.6 and 4.1.
 // Above that eight blocks of a column group are too few: 4096 x 128 fp32 gelu 18.6 and 24.9, 8192 x 256
