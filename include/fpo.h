@@ -488,8 +488,8 @@ size_t fpo_linear_vjp_workspace(int64_t T, int64_t d_out, int64_t d_in, int32_t 
  * Outputs may not overlap what is read, one another or the workspace (FPO_ERR_ARG).  fp32
  * accumulation; dbias adds dZ before its rounding to dtype, in a fixed order; the products take it
  * rounded: in bf16 and with an act, dX and dW have some sqrt(2) times the error of their own
- * rounding (2.35e-3 for 1.66e-3 of their norm).  Deterministic.  T = 0 sets dW and dbias to zero.  After a wait that ran out
- * (FPO_ERR_TIMEOUT) dX and dW hold no result.
+ * rounding (2.35e-3 for 1.66e-3 of their norm).  Deterministic.  T = 0 sets dW and dbias to zero.
+ * After a wait that ran out (FPO_ERR_TIMEOUT) dX and dW hold no result.
  */
 int32_t fpo_linear_vjp(int64_t T, int64_t d_out, int64_t d_in, int32_t dtype, int32_t act,
                        const void* dY, const void* Z, const void* X, const void* W, int32_t act_in,

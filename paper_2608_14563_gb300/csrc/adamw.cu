@@ -470,7 +470,7 @@ __device__ __forceinline__ float add_words(const float* words) {
         s += words[i];
         wide |= is_wide(words[i]);
     }
-    if (!wide) return s;
+    if (!wide) return fabsf(s);  // (a NaN's sign bit is no mark)
     double d = 0.0;
     for (int i = 0; i < kThreads / 32; ++i)
         d += is_wide(words[i]) ? wide_value(words[i]) : static_cast<double>(words[i]);
@@ -720,11 +720,13 @@ cudaError_t launch_state_values(bool is_signed, long long n, const void* codes, 
     const unsigned grid = static_cast<unsigned>(blocks);
     const uint8_t* c = static_cast<const uint8_t*>(codes);
     auto run = [&](auto kern, auto* to) { return launch_plain(kern, grid, kThreads, st, c, scales, n, to); };
-    __nv_bfloat16* const h = static_cast<__nv_bfloat16*>(out);
-    float* const f = static_cast<float*>(out);
-    if (is_signed)
-        return out_dtype == 1 ? run(state_values_kernel<true, __nv_bfloat16>, h) : run(state_values_kernel<true, float>, f);
-    return out_dtype == 1 ? run(state_values_kernel<false, __nv_bfloat16>, h) : run(state_values_kernel<false, float>, f);
+    if (out_dtype == 1) {
+        __nv_bfloat16* const to = static_cast<__nv_bfloat16*>(out);
+        return is_signed ? run(state_values_kernel<true, __nv_bfloat16>, to)
+                         : run(state_values_kernel<false, __nv_bfloat16>, to);
+    }
+    float* const to = static_cast<float*>(out);
+    return is_signed ? run(state_values_kernel<true, float>, to) : run(state_values_kernel<false, float>, to);
 }
 
 }  // namespace fpo

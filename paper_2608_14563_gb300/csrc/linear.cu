@@ -870,9 +870,9 @@ struct SignalPlan {
 };
 int sig_v(int dtype, int N) { return dtype == 1 ? 8 : N % 4 == 0 ? 4 : 1; }
 // Up to 2048 rows, or 8192 without an activation to compute, the ranges are a cluster's blocks, one for
-// every 64 or 256 rows begun and at most eight: no counters to clear and wait for.  us with 256 rows and counters, and so (fp32
-// with a slower gelu than now's, 4.5): 512 x 1024 fp32 gelu 18.5 and 5.9, bias sums alone 8.3 and 3.1;
-// 2048 x 256 bf16 gelu 14.5 and 8.9, alone 8.6 and 3.2; 200 x 256 bf16 gelu (one range) 6.6 and 4.1.
+// every 64 or 256 rows begun and at most eight: no counters to clear and wait for.  us with 256 rows
+// and counters, and so (fp32 with a slower gelu than now's, 4.5): 512 x 1024 fp32 gelu 18.5 and 5.9,
+// bias sums alone 8.3 and 3.1; 2048 x 256 bf16 gelu 14.5 and 8.9, alone 8.6 and 3.2; 200 x 256 bf16 gelu (one range) 6.6 and 4.1.
 // Above that eight blocks of a column group are too few: 4096 x 128 fp32 gelu 18.6 and 24.9, 8192 x 256
 // bf16 14.4 and 27.8, alone 8.3 and 6.0; 16384 x 128 alone 8.5 and 9.7.
 SignalPlan signal_plan(int dtype, int T, int N, int act) {
